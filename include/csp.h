@@ -317,6 +317,160 @@ csp_status csp_decode_step(const csp_params* p, csp_tensor q, csp_tensor k, csp_
                            const uint8_t* query_label, int32_t first_step, float* out, float* acc_self,
                            float* acc_cross, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/*
+ * What csp_chunk_attn does to a logit o = scale <q, k> before the softmax.  Zeros and null pointers change nothing.
+ *   softcap    c > 0: o becomes c tanh(o / c)
+ *   slopes     [H_q] fp32 or NULL: slopes[hq] * |position of the query - position of the key| is subtracted, after the cap
+ *   positions  int32, >= 0, of the cached rows: element (b,h,t) at positions[b*pos_stride_b + h*pos_stride_h + t]; NULL: row
+ *              t is at position t.  A pruned cache keeps the positions its rows had (the keep_idx of the prune), per
+ *              head; a head stride of 0 shares one row of positions.  Read only when slopes are given
+ *   documents  int32 document of every cached row, addressed like positions, or NULL: a query sees rows of its own only
+ *   prefix     int32 element (b,h) at prefix[b*prefix_stride_b + h*prefix_stride_h], or NULL: the first that many rows of
+ *              the unit are seen by every query of the chunk, also by those in front of them (an image in the prompt that
+ *              is attended to in both directions); values are clamped to [0, n_rows]
+ */
+typedef struct {
+    float softcap;
+    const float* slopes;
+    const int32_t* positions; int64_t pos_stride_b, pos_stride_h;
+    const int32_t* documents; int64_t doc_stride_b, doc_stride_h;
+    const int32_t* prefix; int64_t prefix_stride_b, prefix_stride_h;
+} csp_score_mods;
+
+/* Bytes of scratch that csp_chunk_attn and csp_chunk_attn_paged need for chunks of up to max_new tokens (status word,
+ * work counters, partial results of split caches).  The first 256 bytes must be zero before first use
+ * (csp_workspace_reset). */
+size_t csp_chunk_workspace_bytes(const csp_params* p, int32_t max_new);
+
+/*
+ * Attention of a chunk of new tokens over a cache that already holds their rows (a prompt in chunks, several decoded
+ * tokens, or, with max_new 1, one decode step), normalised like csp_decode_attn (Eq. 5-7).  Sequence b brings
+ * N = n_new[b] tokens, the last N rows of every one of its heads: token i is row r = n_rows[b,hkv] - N + i and sees the
+ * rows t <= r (and those that `mods` adds or takes away):
+ *   out[b,hq,i,:] = sum_t e^{o_t} / (n + sum_j e^{o_j}) v[b,hkv,t,:],   lse[b,hq,i] = ln sum_t e^{o_t}
+ *   q       [B, H_q, max_new, d] bf16, out [B, H_q, max_new, d] bf16; any strides (e.g. of a [B, max_new, H_q, d] tensor)
+ *   k, v    [B, H_kv, out_capacity, d] bf16; p->out_capacity is the row capacity, p->max_len / window / recent are not
+ *           used.  Rows t >= n_rows[b,h] may hold anything; rows that are only masked must be finite
+ *   n_rows  [B, H_kv] int32 device: rows per head, the chunk's own included; values outside [0, out_capacity] are
+ *           clamped and flagged CSP_DEV_BAD_LEN
+ *   n_new_or_null [B] int32 device; NULL: max_new for every sequence.  Values outside [0, max_new] are clamped and
+ *           flagged; out and lse of tokens i >= n_new[b] are left as they were
+ *   lse_or_null [B, H_q, max_new] fp32 dense: without n, so that the last W tokens' values are what csp_score and
+ *           csp_prune_layer take as lse_or_null (when mods is NULL)
+ * A token that sees nothing (or whose row would be negative: flagged) gets a zero vector and a lse of -infinity.
+ * bf16 caches with head_dim 64 or 128.  Sums and the softmax are held in fp32; weights are rounded to bf16 once before
+ * they meet V, the result once more.  Nothing is allocated; the caller owns the workspace.
+ */
+csp_status csp_chunk_attn(const csp_params* p, int32_t max_new, csp_tensor q, csp_tensor k, csp_tensor v,
+                          const int32_t* n_rows, const int32_t* n_new_or_null, const csp_score_mods* mods_or_null,
+                          csp_tensor out, float* lse_or_null,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* The same over a paged cache; k_pool, v_pool and pages as for csp_decode_attn_paged (page_rows a multiple of 128,
+ * max_pages * page_rows >= out_capacity).  A page number outside the pool is flagged CSP_DEV_BAD_LEN; its rows read as
+ * zeros.  positions, documents and prefix stay arrays over logical rows. */
+csp_status csp_chunk_attn_paged(const csp_params* p, int32_t max_new, csp_tensor q, csp_tensor k_pool, csp_tensor v_pool,
+                                const csp_pages* pages, const int32_t* n_rows, const int32_t* n_new_or_null,
+                                const csp_score_mods* mods_or_null, csp_tensor out, float* lse_or_null,
+                                void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Bytes of scratch (a status word) that csp_append_paged and csp_pages_copy need; 256 zeroed bytes. */
+size_t csp_append_workspace_bytes(const csp_params* p);
+
+/*
+ * The rows of a chunk of new tokens go to the pages: row n_rows[b,h] + i of unit (b,h) becomes k_new[b,h,i,:] and
+ * v_new[b,h,i,:] for i < n_new[b], and n_rows_out[b,h] = n_rows[b,h] + n_new[b].
+ *   k_new, v_new  [B, H_kv, max_new, d] (any strides), bf16 or fp32 like the pools (p->dtype)
+ *   pages         as for csp_prune_layer_paged; the pages must be there (csp_pages_reserve) and belong to one sequence
+ *   n_rows_out    may be n_rows itself
+ * A unit whose n_rows is negative (CSP_DEV_BAD_LEN), or whose rows would pass out_capacity or the table
+ * (CSP_DEV_CAPACITY), keeps its rows and its count; n_new is clamped to [0, max_new] (CSP_DEV_BAD_LEN); a row whose page
+ * number is outside the pool is not written (CSP_DEV_BAD_LEN).
+ */
+csp_status csp_append_paged(const csp_params* p, int32_t max_new, csp_tensor k_new, csp_tensor v_new,
+                            const int32_t* n_new_or_null, csp_tensor k_pool, csp_tensor v_pool, const csp_pages* pages,
+                            const int32_t* n_rows, int32_t* n_rows_out,
+                            void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Whose pages are whose.  All arrays are device memory of the caller, changed in place:
+ *   page_table [batch, max_pages]  as in csp_pages; entries at or behind held[b] are not read
+ *   held       [batch]             pages that the sequence holds: the leading entries of its table row
+ *   refs       [n_pages]           table entries that name the page; 0: the page is free.  Sequences that share a prefix
+ *                                  share its pages
+ *   n_rows     [batch, n_heads]    rows in use per head (what a prune leaves in n_out, what csp_append_paged counts up);
+ *                                  n_heads may also run over the layers of a model whose layers share one table
+ * The caller starts with held and refs zero and changes table, held and refs only through these calls.  A call changes
+ * nothing but what it says; entries that contradict each other (a page number outside the pool, a page that is named but
+ * counted free) are flagged CSP_DEV_BAD_LEN and left alone.  Page numbers are taken lowest first, in the order of
+ * sequence and table index, so that the same calls give the same tables.
+ */
+typedef struct {
+    int32_t* page_table;
+    int32_t* held;
+    int32_t* refs;
+    int32_t* n_rows;
+    int32_t batch, n_heads, max_pages, page_rows, n_pages;
+} csp_page_state;
+
+/* Bytes of scratch that the csp_pages_* calls need (status word and lists).  The first 256 bytes must be zero before
+ * first use (csp_workspace_reset).  0 for sizes that are refused. */
+size_t csp_pages_workspace_bytes(const csp_page_state* s);
+
+/*
+ * Sequence dst[i] becomes a copy of sequence src[i] that shares its pages: table row, held and n_rows are copied, refs
+ * counted up; no row is moved (csp_pages_reserve gives pages of its own to whoever writes).
+ *   src, dst   [n] int32 device.  dst[i] must hold no pages, is named once, and is no src of the same call; a fork that
+ *              breaks this, or names a sequence outside [0, batch), is flagged CSP_DEV_BAD_LEN and skipped (of two
+ *              forks to one dst the first is done)
+ */
+csp_status csp_pages_fork(const csp_page_state* s, const int32_t* src, const int32_t* dst, int32_t n,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Room for n_new[b] more rows in every sequence, in pages that nobody else names: afterwards sequence b holds at least
+ * ceil((largest n_rows[b,:] + n_new[b]) / page_rows) pages, and every page from the one that holds row
+ * (smallest n_rows[b,:]) on - or, with whole != 0, every page in use - is named by b alone, so that csp_append_paged
+ * (whole: csp_prune_layer_paged in place) may write it.  Shared pages are replaced by free ones; when all sequences that
+ * share a page ask for one of their own, the last keeps it.
+ *   n_new_or_null  [batch] int32 device; NULL: no more rows
+ *   moves          [max_moves, 2] int32 device: (from, to) of the pages whose rows csp_pages_copy has to copy next, in
+ *                  every layer's pools; n_moves [1] int32 device: how many.  No `to` is a `from`, and none is named twice
+ * If the pool, a table row or moves is too small, nothing is changed, n_moves is 0 and CSP_DEV_CAPACITY is flagged; a
+ * negative n_rows or n_new does the same with CSP_DEV_BAD_LEN.
+ */
+csp_status csp_pages_reserve(const csp_page_state* s, const int32_t* n_new_or_null, int32_t whole,
+                             int32_t* moves, int32_t max_moves, int32_t* n_moves,
+                             void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Pages behind the rows in use go back: sequence b keeps its first ceil(largest n_rows[b,:] / page_rows) pages, the table
+ * entries behind them become -1 and refs count down (n_rows of zero gives a sequence up altogether).  A sequence with a
+ * negative n_rows (a prune that did not fit) is flagged CSP_DEV_BAD_LEN and keeps all; so is one with more rows than
+ * its pages hold. */
+csp_status csp_pages_free(const csp_page_state* s, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Moves the pages in use together: afterwards they are the pages [0, live) of the pool, and everything behind can be
+ * given to someone else.  The pages in use at or behind `live` move to the free ones in front of it, both in ascending
+ * order; tables and refs follow.  moves, max_moves and n_moves as for csp_pages_reserve (csp_pages_copy comes next);
+ * with moves too small nothing is changed and CSP_DEV_CAPACITY is flagged.
+ */
+csp_status csp_pages_compact(const csp_page_state* s, int32_t* moves, int32_t max_moves, int32_t* n_moves,
+                             void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Copies whole pages of K and V, all heads: page moves[i][1] becomes page moves[i][0] for i < *n_moves.  One call per
+ * layer whose pools follow the table.
+ *   k_pool, v_pool  [n_pages, H_kv, page_rows, d] (strided); bf16 or fp32 (p->dtype)
+ *   moves, n_moves  as csp_pages_reserve and csp_pages_compact leave them; no page may be both from and to.  Page numbers
+ *                   outside the pool are flagged CSP_DEV_BAD_LEN and skipped, an n_moves outside [0, max_moves] is
+ *                   clamped and flagged
+ * page_rows here may be any positive number.  Workspace: csp_append_workspace_bytes, or that of the csp_pages_* calls.
+ */
+csp_status csp_pages_copy(const csp_params* p, csp_tensor k_pool, csp_tensor v_pool, int32_t n_pages, int32_t page_rows,
+                          const int32_t* moves, int32_t max_moves, const int32_t* n_moves,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Bytes of device staging that csp_prune_layer_host needs for these parameters. */
 size_t csp_host_staging_bytes(const csp_params* p);
 

@@ -28,7 +28,9 @@ EXPORTS = ("csp_workspace_bytes", "csp_workspace_reset", "csp_score", "csp_selec
            "csp_status_string", "csp_prune_layer_static", "csp_static_workspace_limit",
            "csp_decode_workspace_bytes", "csp_decode_attn", "csp_decode_step_workspace_bytes", "csp_decode_step",
            "csp_weight_histogram", "csp_probe_ex2_rate", "csp_prune_layer_paged",
-           "csp_decode_attn_paged", "csp_select_compact")
+           "csp_decode_attn_paged", "csp_select_compact", "csp_chunk_workspace_bytes", "csp_chunk_attn", "csp_chunk_attn_paged",
+           "csp_append_workspace_bytes", "csp_append_paged", "csp_pages_workspace_bytes", "csp_pages_fork",
+           "csp_pages_reserve", "csp_pages_free", "csp_pages_compact", "csp_pages_copy")
 HIST_BINS, HIST_LO, HIST_WIDTH = 64, -32.0, 0.5
 
 
@@ -44,6 +46,19 @@ class CTensor(C.Structure):
 
 class CPages(C.Structure):
     _fields_ = [("page_table", C.c_void_p), ("max_pages", C.c_int32), ("page_rows", C.c_int32), ("n_pages", C.c_int32)]
+
+
+class CScoreMods(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("slopes", C.c_void_p),
+                ("positions", C.c_void_p), ("pos_stride_b", C.c_int64), ("pos_stride_h", C.c_int64),
+                ("documents", C.c_void_p), ("doc_stride_b", C.c_int64), ("doc_stride_h", C.c_int64),
+                ("prefix", C.c_void_p), ("prefix_stride_b", C.c_int64), ("prefix_stride_h", C.c_int64)]
+
+
+class CPageState(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("held", C.c_void_p), ("refs", C.c_void_p), ("n_rows", C.c_void_p),
+                ("batch", C.c_int32), ("n_heads", C.c_int32), ("max_pages", C.c_int32), ("page_rows", C.c_int32),
+                ("n_pages", C.c_int32)]
 
 
 class CParams(C.Structure):
@@ -75,6 +90,68 @@ class Params:
         return CParams(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.window,
                        self.recent, self.max_len, self.out_capacity, self.dtype, self.n, self.scale,
                        self.combine, self.select_mode, self.head_reduce)
+
+
+@dataclass
+class ScoreMods:
+    """What chunk_attn does to the logits (csp_score_mods).  slopes fp32 [Hq]; positions, documents int32 [B, cap] (shared
+    by the heads) or [B, Hkv, cap]; prefix int32 [B] or [B, 1] (shared) or [B, Hkv]."""
+    softcap: float = 0.0
+    slopes: Optional[torch.Tensor] = None
+    positions: Optional[torch.Tensor] = None
+    documents: Optional[torch.Tensor] = None
+    prefix: Optional[torch.Tensor] = None
+
+    def tensors(self):
+        return [t for t in (self.slopes, self.positions, self.documents, self.prefix) if t is not None]
+
+    def c(self, p: "Params") -> CScoreMods:
+        m = CScoreMods(softcap=float(self.softcap))
+        if self.slopes is not None:
+            assert self.slopes.dtype == torch.float32 and self.slopes.is_contiguous() and self.slopes.numel() == p.n_q_heads
+            m.slopes = self.slopes.data_ptr()
+        for name, short in (("positions", "pos"), ("documents", "doc")):
+            t = getattr(self, name)
+            if t is None:
+                continue
+            assert t.dtype == torch.int32 and t.dim() in (2, 3) and t.stride(-1) == 1, f"{name}: int32 [B, (Hkv,) rows]"
+            assert t.shape[0] == p.batch and t.shape[-1] >= p.out_capacity and (t.dim() == 2 or t.shape[1] == p.n_kv_heads)
+            setattr(m, name, t.data_ptr())
+            setattr(m, short + "_stride_b", t.stride(0))
+            setattr(m, short + "_stride_h", t.stride(1) if t.dim() == 3 else 0)
+        if self.prefix is not None:
+            t = self.prefix
+            assert t.dtype == torch.int32 and t.dim() in (1, 2) and t.shape[0] == p.batch
+            assert t.dim() == 1 or t.shape[1] in (1, p.n_kv_heads)
+            m.prefix, m.prefix_stride_b = t.data_ptr(), t.stride(0)
+            m.prefix_stride_h = t.stride(1) if t.dim() == 2 and t.shape[1] > 1 else 0
+        return m
+
+
+@dataclass
+class PageState:
+    """Whose pages are whose (csp_page_state): int32 tensors page_table [B, max_pages], held [B], refs [n_pages],
+    n_rows [B, heads], all dense and changed in place by the pages_* calls."""
+    page_table: torch.Tensor
+    held: torch.Tensor
+    refs: torch.Tensor
+    n_rows: torch.Tensor
+    page_rows: int
+
+    def c(self) -> CPageState:
+        for t in (self.page_table, self.held, self.refs, self.n_rows):
+            assert t.dtype == torch.int32 and t.is_contiguous()
+        assert self.page_table.dim() == 2 and self.n_rows.dim() == 2
+        assert self.held.numel() == self.page_table.shape[0] == self.n_rows.shape[0]
+        return CPageState(self.page_table.data_ptr(), self.held.data_ptr(), self.refs.data_ptr(), self.n_rows.data_ptr(),
+                          self.page_table.shape[0], self.n_rows.shape[1], self.page_table.shape[1], self.page_rows,
+                          self.refs.numel())
+
+
+def new_page_state(batch: int, n_heads: int, max_pages: int, page_rows: int, n_pages: int, device="cuda") -> PageState:
+    """A pool of n_pages free pages and `batch` sequences that hold none."""
+    z = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device=device)  # noqa: E731
+    return PageState(z(batch, max_pages).fill_(-1), z(batch), z(n_pages), z(batch, n_heads), page_rows)
 
 
 _lib = None
@@ -134,6 +211,29 @@ def lib() -> C.CDLL:
                                             CTensor, CTensor, vp, vp, vp, vp, vp, vp, sz, vp]
         l.csp_decode_attn_paged.restype = C.c_int
         l.csp_decode_attn_paged.argtypes = [P, CTensor, CTensor, CTensor, C.POINTER(CPages), vp, vp, vp, sz, vp]
+        M, G, S, i32 = C.POINTER(CScoreMods), C.POINTER(CPages), C.POINTER(CPageState), C.c_int32
+        l.csp_chunk_workspace_bytes.restype = sz
+        l.csp_chunk_workspace_bytes.argtypes = [P, i32]
+        l.csp_chunk_attn.restype = C.c_int
+        l.csp_chunk_attn.argtypes = [P, i32, CTensor, CTensor, CTensor, vp, vp, M, CTensor, vp, vp, sz, vp]
+        l.csp_chunk_attn_paged.restype = C.c_int
+        l.csp_chunk_attn_paged.argtypes = [P, i32, CTensor, CTensor, CTensor, G, vp, vp, M, CTensor, vp, vp, sz, vp]
+        l.csp_append_workspace_bytes.restype = sz
+        l.csp_append_workspace_bytes.argtypes = [P]
+        l.csp_append_paged.restype = C.c_int
+        l.csp_append_paged.argtypes = [P, i32, CTensor, CTensor, vp, CTensor, CTensor, G, vp, vp, vp, sz, vp]
+        l.csp_pages_workspace_bytes.restype = sz
+        l.csp_pages_workspace_bytes.argtypes = [S]
+        l.csp_pages_fork.restype = C.c_int
+        l.csp_pages_fork.argtypes = [S, vp, vp, i32, vp, sz, vp]
+        l.csp_pages_reserve.restype = C.c_int
+        l.csp_pages_reserve.argtypes = [S, vp, i32, vp, i32, vp, vp, sz, vp]
+        l.csp_pages_free.restype = C.c_int
+        l.csp_pages_free.argtypes = [S, vp, sz, vp]
+        l.csp_pages_compact.restype = C.c_int
+        l.csp_pages_compact.argtypes = [S, vp, i32, vp, vp, sz, vp]
+        l.csp_pages_copy.restype = C.c_int
+        l.csp_pages_copy.argtypes = [P, CTensor, CTensor, i32, i32, vp, i32, vp, vp, sz, vp]
         l.csp_probe_ex2_rate.restype = C.c_int
         l.csp_probe_ex2_rate.argtypes = [C.c_int32, C.c_int32, vp, sz, C.POINTER(C.c_int64), vp]
         l.csp_weight_histogram.restype = C.c_int
@@ -327,6 +427,156 @@ def decode_attn_paged(p: Params, q, k_pool, v_pool, page_table, n_rows, out, ws)
     pg = CPages(page_table.data_ptr(), page_table.shape[1], k_pool.shape[2], k_pool.shape[0])
     _check(lib().csp_decode_attn_paged(C.byref(cp), qt, tensor4(k_pool), tensor4(v_pool), C.byref(pg), _ptr(n_rows),
                                        _ptr(out), _ptr(ws), ws.numel(), _stream()), "csp_decode_attn_paged")
+
+
+def _here(*tensors):
+    """The kernels run on the current device and stream: refuses tensors that live elsewhere."""
+    dev = torch.device("cuda", torch.cuda.current_device())
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensor on {t.device}, but the current device is {dev}")
+
+
+def _counts(t: Optional[torch.Tensor], shape):
+    assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == tuple(shape)), \
+        f"int32 tensor of shape {tuple(shape)} expected"
+    return _ptr(t)
+
+
+def _status_workspace(n: int, where: str, device) -> torch.Tensor:
+    if n == 0:
+        raise CspError(ERR_UNSUPPORTED, where)
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def chunk_workspace_bytes(p: Params, max_new: int) -> int:
+    cp = p.c()
+    return int(lib().csp_chunk_workspace_bytes(C.byref(cp), int(max_new)))
+
+
+def new_chunk_workspace(p: Params, max_new: int, device="cuda") -> torch.Tensor:
+    """Allocates (with torch) and zeroes a workspace for chunk_attn with chunks of up to max_new tokens."""
+    return _status_workspace(chunk_workspace_bytes(p, max_new), "csp_chunk_workspace_bytes", device)
+
+
+def _chunk_args(p: Params, q, k, v, n_rows, out, ws, n_new, mods, lse):
+    _here(q, k, v, n_rows, out, ws, n_new, lse, *(mods.tensors() if mods is not None else []))
+    T = q.shape[2] if q.dim() == 4 else -1
+    want = (p.batch, p.n_q_heads, T, p.head_dim)
+    assert tuple(q.shape) == want and tuple(out.shape) == want, f"q and out: [B, Hq, new tokens, d] = {want}"
+    assert all(t.dtype == torch.bfloat16 for t in (q, k, v, out)), "bf16 tensors expected"
+    assert k.shape[1] == v.shape[1] == p.n_kv_heads and k.shape[3] == v.shape[3] == p.head_dim
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == want[:3])
+    return T, _counts(n_rows, (p.batch, p.n_kv_heads)), _counts(n_new, (p.batch,)), \
+        None if mods is None else C.byref(mods.c(p))
+
+
+def chunk_attn(p: Params, q, k, v, n_rows, out, ws, n_new=None, mods: Optional[ScoreMods] = None, lse=None):
+    """q, out bf16 [B, Hq, new tokens, d] (any strides); k, v [B, Hkv, out_capacity, d]; n_rows int32 [B, Hkv], the new rows
+    included; n_new int32 [B]; lse fp32 [B, Hq, new tokens]."""
+    cp = p.c()
+    T, rows, new, m = _chunk_args(p, q, k, v, n_rows, out, ws, n_new, mods, lse)
+    assert k.shape[0] == v.shape[0] == p.batch and k.shape[2] >= p.out_capacity and v.shape[2] >= p.out_capacity
+    _check(lib().csp_chunk_attn(C.byref(cp), T, tensor4(q), tensor4(k), tensor4(v), rows, new, m, tensor4(out), _ptr(lse),
+                                _ptr(ws), ws.numel(), _stream()), "csp_chunk_attn")
+
+
+def chunk_attn_paged(p: Params, q, k_pool, v_pool, page_table, n_rows, out, ws, n_new=None,
+                     mods: Optional[ScoreMods] = None, lse=None):
+    """chunk_attn over pools [n_pages, Hkv, page_rows, d] addressed through page_table int32 [B, max_pages]."""
+    cp = p.c()
+    T, rows, new, m = _chunk_args(p, q, k_pool, v_pool, n_rows, out, ws, n_new, mods, lse)
+    pg = _pool_pages(p, k_pool, v_pool, page_table)
+    _check(lib().csp_chunk_attn_paged(C.byref(cp), T, tensor4(q), tensor4(k_pool), tensor4(v_pool), C.byref(pg), rows, new, m,
+                                      tensor4(out), _ptr(lse), _ptr(ws), ws.numel(), _stream()), "csp_chunk_attn_paged")
+
+
+def _pool_pages(p: Params, k_pool, v_pool, page_table) -> CPages:
+    _here(k_pool, v_pool, page_table)
+    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.dim() == 2
+    assert page_table.shape[0] == p.batch and k_pool.shape == v_pool.shape and k_pool.dim() == 4
+    return CPages(page_table.data_ptr(), page_table.shape[1], k_pool.shape[2], k_pool.shape[0])
+
+
+def new_append_workspace(p: Params, device="cuda") -> torch.Tensor:
+    """Allocates (with torch) and zeroes a workspace for append_paged and pages_copy."""
+    cp = p.c()
+    return _status_workspace(int(lib().csp_append_workspace_bytes(C.byref(cp))), "csp_append_workspace_bytes", device)
+
+
+def _cache_dtype(p: Params, *tensors):
+    want = torch.float32 if p.dtype == F32 else torch.bfloat16
+    assert all(t.dtype == want and t.shape[1] == p.n_kv_heads and t.shape[3] == p.head_dim for t in tensors)
+
+
+def append_paged(p: Params, k_new, v_new, k_pool, v_pool, page_table, n_rows, n_rows_out, ws, n_new=None):
+    """k_new, v_new [B, Hkv, new tokens, d] go behind the n_rows rows of every head; n_rows_out may be n_rows."""
+    cp = p.c()
+    _here(k_new, v_new, n_rows, n_rows_out, ws, n_new)
+    pg = _pool_pages(p, k_pool, v_pool, page_table)
+    _cache_dtype(p, k_new, v_new, k_pool, v_pool)
+    assert k_new.shape == v_new.shape and k_new.shape[0] == p.batch
+    _check(lib().csp_append_paged(C.byref(cp), k_new.shape[2], tensor4(k_new), tensor4(v_new), _counts(n_new, (p.batch,)),
+                                  tensor4(k_pool), tensor4(v_pool), C.byref(pg), _counts(n_rows, (p.batch, p.n_kv_heads)),
+                                  _counts(n_rows_out, (p.batch, p.n_kv_heads)), _ptr(ws), ws.numel(), _stream()),
+           "csp_append_paged")
+
+
+def new_pages_workspace(state: PageState, device="cuda") -> torch.Tensor:
+    """Allocates (with torch) and zeroes a workspace for the pages_* calls."""
+    cs = state.c()
+    return _status_workspace(int(lib().csp_pages_workspace_bytes(C.byref(cs))), "csp_pages_workspace_bytes", device)
+
+
+def _page_state(state: PageState, ws, *tensors) -> CPageState:
+    _here(state.page_table, state.held, state.refs, state.n_rows, ws, *tensors)
+    return state.c()
+
+
+def _moves(moves, n_moves):
+    assert moves.dtype == torch.int32 and moves.is_contiguous() and moves.dim() == 2 and moves.shape[1] == 2
+    return _ptr(moves), moves.shape[0], _counts(n_moves, (1,))
+
+
+def pages_fork(state: PageState, src, dst, ws):
+    """Sequence dst[i] (which holds no pages) becomes a copy of src[i] that shares its pages; src, dst int32 [n]."""
+    cs = _page_state(state, ws, src, dst)
+    n = src.numel()
+    _check(lib().csp_pages_fork(C.byref(cs), _counts(src, (n,)), _counts(dst, (n,)), n, _ptr(ws), ws.numel(), _stream()),
+           "csp_pages_fork")
+
+
+def pages_reserve(state: PageState, moves, n_moves, ws, n_new=None, whole: bool = False):
+    """Room for n_new[b] more rows in pages of the sequence's own (whole: all of its pages); moves int32 [most, 2] and
+    n_moves int32 [1] receive what pages_copy has to copy."""
+    cs = _page_state(state, ws, moves, n_moves, n_new)
+    m, most, n = _moves(moves, n_moves)
+    _check(lib().csp_pages_reserve(C.byref(cs), _counts(n_new, (state.page_table.shape[0],)), int(whole), m, most, n, _ptr(ws),
+                                   ws.numel(), _stream()), "csp_pages_reserve")
+
+
+def pages_free(state: PageState, ws):
+    """Pages behind the rows in use go back to the pool."""
+    cs = _page_state(state, ws)
+    _check(lib().csp_pages_free(C.byref(cs), _ptr(ws), ws.numel(), _stream()), "csp_pages_free")
+
+
+def pages_compact(state: PageState, moves, n_moves, ws):
+    """Moves the pages in use to the front of the pool; moves and n_moves as for pages_reserve."""
+    cs = _page_state(state, ws, moves, n_moves)
+    m, most, n = _moves(moves, n_moves)
+    _check(lib().csp_pages_compact(C.byref(cs), m, most, n, _ptr(ws), ws.numel(), _stream()), "csp_pages_compact")
+
+
+def pages_copy(p: Params, k_pool, v_pool, moves, n_moves, ws):
+    """Copies the pages listed in moves, K and V, all heads: one call per layer."""
+    cp = p.c()
+    _here(k_pool, v_pool, moves, n_moves, ws)
+    _cache_dtype(p, k_pool, v_pool)
+    assert k_pool.shape == v_pool.shape
+    m, most, n = _moves(moves, n_moves)
+    _check(lib().csp_pages_copy(C.byref(cp), tensor4(k_pool), tensor4(v_pool), k_pool.shape[0], k_pool.shape[2], m, most, n,
+                                _ptr(ws), ws.numel(), _stream()), "csp_pages_copy")
 
 
 def static_workspace_limit() -> int:

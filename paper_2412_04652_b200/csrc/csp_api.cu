@@ -560,6 +560,203 @@ csp_status csp_decode_step(const csp_params* p, csp_tensor q, csp_tensor k, csp_
     return launch_decode_attn(*p, q, k, v, n_rows, out, workspace, static_cast<cudaStream_t>(cuda_stream), &step);
 }
 
+// ---- chunk attention over a dense or paged cache
+namespace {
+
+bool status_area_ok(const void* ws, size_t bytes, size_t need) {
+    return ws && bytes >= need && uintptr_t(ws) % 256 == 0;
+}
+
+// rows of a written tensor must not share memory: every axis that has more than one entry steps over a whole row
+bool rows_apart(const csp_params& p, const csp_tensor& t, int batch, int heads, int rows) {
+    return (rows <= 1 || t.stride_t >= p.head_dim) && (heads <= 1 || t.stride_h >= p.head_dim) &&
+           (batch <= 1 || t.stride_b >= p.head_dim);
+}
+
+bool pages_ok(const csp_pages* pg, int64_t rows) {
+    return pg && pg->page_table && pg->page_rows > 0 && pg->page_rows % 128 == 0 && pg->max_pages > 0 && pg->n_pages > 0 &&
+           int64_t(pg->max_pages) * pg->page_rows >= rows;
+}
+
+csp_status chunk_attn(const csp_params* p, int32_t max_new, const csp_tensor& q, const csp_tensor& k, const csp_tensor& v,
+                      const csp_pages* pages, const int32_t* n_rows, const int32_t* n_new, const csp_score_mods* mods,
+                      const csp_tensor& out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    csp_status st = check_params(p);
+    if (st != CSP_OK) return st;
+    if (max_new < 0 || !q.ptr || !k.ptr || !v.ptr || !n_rows || !out.ptr) return CSP_ERR_INVALID_ARG;
+    if (mods && !(mods->softcap >= 0.f && mods->softcap <= 1e30f)) return CSP_ERR_INVALID_ARG;
+    if (p->dtype != CSP_BF16 || (p->head_dim != 64 && p->head_dim != 128)) return CSP_ERR_UNSUPPORTED;
+    if (!tensor_ok(*p, q) || !tensor_ok(*p, k) || !tensor_ok(*p, v) || !tensor_ok(*p, out)) return CSP_ERR_UNSUPPORTED;
+    if (!rows_apart(*p, out, p->batch, p->n_q_heads, max_new)) return CSP_ERR_UNSUPPORTED;
+    if (int64_t(max_new) * (p->n_q_heads / p->n_kv_heads) > (1 << 24)) return CSP_ERR_UNSUPPORTED;
+    if (!status_area_ok(workspace, workspace_bytes, chunk_workspace_bytes(*p, max_new))) return CSP_ERR_WORKSPACE;
+    if ((st = check_arch()) != CSP_OK) return st;
+    ChunkArgs a;
+    a.n_rows = n_rows; a.n_new = n_new;
+    a.out = static_cast<uint16_t*>(out.ptr); a.o_sb = out.stride_b; a.o_sh = out.stride_h; a.o_st = out.stride_t;
+    a.lse = lse;
+    a.status = static_cast<int32_t*>(workspace);
+    a.batch = p->batch; a.n_kv_heads = p->n_kv_heads; a.group = p->n_q_heads / p->n_kv_heads;
+    a.capacity = p->out_capacity; a.max_new = max_new;
+    a.n = p->n;
+    a.scale = p->scale > 0.f ? p->scale : 1.0f / sqrtf(float(p->head_dim));
+    a.mods = ModArgs{0.f, nullptr, nullptr, 0, 0, nullptr, 0, 0, nullptr, 0, 0};
+    if (mods) {
+        a.mods = ModArgs{mods->softcap, mods->slopes,
+                         mods->slopes ? mods->positions : nullptr, mods->pos_stride_b, mods->pos_stride_h,
+                         mods->documents, mods->doc_stride_b, mods->doc_stride_h,
+                         mods->prefix, mods->prefix_stride_b, mods->prefix_stride_h};
+    }
+    a.page_table = pages ? pages->page_table : nullptr;
+    a.max_pages = pages ? pages->max_pages : 0;
+    a.page_rows = pages ? pages->page_rows : 1;
+    a.n_pages = pages ? pages->n_pages : 0;
+    if (p->batch == 0 || max_new == 0) return CSP_OK;
+    return launch_chunk_attn(*p, a, q, k, v, pages, workspace, static_cast<cudaStream_t>(cuda_stream));
+}
+
+}  // namespace
+
+size_t csp_chunk_workspace_bytes(const csp_params* p, int32_t max_new) {
+    if (check_params(p) != CSP_OK || max_new < 0) return 0;
+    return chunk_workspace_bytes(*p, max_new);
+}
+
+csp_status csp_chunk_attn(const csp_params* p, int32_t max_new, csp_tensor q, csp_tensor k, csp_tensor v,
+                          const int32_t* n_rows, const int32_t* n_new_or_null, const csp_score_mods* mods_or_null,
+                          csp_tensor out, float* lse_or_null, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return chunk_attn(p, max_new, q, k, v, nullptr, n_rows, n_new_or_null, mods_or_null, out, lse_or_null, workspace,
+                      workspace_bytes, cuda_stream);
+}
+
+csp_status csp_chunk_attn_paged(const csp_params* p, int32_t max_new, csp_tensor q, csp_tensor k_pool, csp_tensor v_pool,
+                                const csp_pages* pages, const int32_t* n_rows, const int32_t* n_new_or_null,
+                                const csp_score_mods* mods_or_null, csp_tensor out, float* lse_or_null, void* workspace,
+                                size_t workspace_bytes, void* cuda_stream) {
+    if (!p || !pages_ok(pages, p->out_capacity)) return CSP_ERR_INVALID_ARG;
+    return chunk_attn(p, max_new, q, k_pool, v_pool, pages, n_rows, n_new_or_null, mods_or_null, out, lse_or_null,
+                      workspace, workspace_bytes, cuda_stream);
+}
+
+// ---- pages of a paged cache
+size_t csp_append_workspace_bytes(const csp_params* p) { return check_params(p) == CSP_OK ? kStatusBytes : 0; }
+
+csp_status csp_append_paged(const csp_params* p, int32_t max_new, csp_tensor k_new, csp_tensor v_new,
+                            const int32_t* n_new_or_null, csp_tensor k_pool, csp_tensor v_pool, const csp_pages* pages,
+                            const int32_t* n_rows, int32_t* n_rows_out, void* workspace, size_t workspace_bytes,
+                            void* cuda_stream) {
+    csp_status st = check_params(p);
+    if (st != CSP_OK) return st;
+    if (max_new < 0 || !k_new.ptr || !v_new.ptr || !k_pool.ptr || !v_pool.ptr || !n_rows || !n_rows_out)
+        return CSP_ERR_INVALID_ARG;
+    if (!pages_ok(pages, p->out_capacity)) return CSP_ERR_INVALID_ARG;
+    if (!tensor_ok(*p, k_new) || !tensor_ok(*p, v_new) || !tensor_ok(*p, k_pool) || !tensor_ok(*p, v_pool))
+        return CSP_ERR_UNSUPPORTED;
+    if (!rows_apart(*p, k_pool, pages->n_pages, p->n_kv_heads, pages->page_rows) ||
+        !rows_apart(*p, v_pool, pages->n_pages, p->n_kv_heads, pages->page_rows))
+        return CSP_ERR_UNSUPPORTED;
+    if (!status_area_ok(workspace, workspace_bytes, kStatusBytes)) return CSP_ERR_WORKSPACE;
+    if ((st = check_arch()) != CSP_OK) return st;
+    const int64_t es = elem_size(*p);
+    AppendArgs a;
+    a.k_new = k_new.ptr; a.v_new = v_new.ptr; a.k = k_pool.ptr; a.v = v_pool.ptr;
+    a.kn_sb = k_new.stride_b * es / 16; a.kn_sh = k_new.stride_h * es / 16; a.kn_st = k_new.stride_t * es / 16;
+    a.vn_sb = v_new.stride_b * es / 16; a.vn_sh = v_new.stride_h * es / 16; a.vn_st = v_new.stride_t * es / 16;
+    a.k_sb = k_pool.stride_b * es / 16; a.k_sh = k_pool.stride_h * es / 16; a.k_st = k_pool.stride_t * es / 16;
+    a.v_sb = v_pool.stride_b * es / 16; a.v_sh = v_pool.stride_h * es / 16; a.v_st = v_pool.stride_t * es / 16;
+    a.n_new = n_new_or_null; a.n_rows = n_rows; a.n_rows_out = n_rows_out;
+    a.units = p->batch * p->n_kv_heads; a.n_kv_heads = p->n_kv_heads; a.max_new = max_new; a.capacity = p->out_capacity;
+    a.chunks_per_row = int(p->head_dim * es / 16);
+    a.page_table = pages->page_table; a.max_pages = pages->max_pages; a.page_rows = pages->page_rows;
+    a.n_pages = pages->n_pages;
+    a.status = static_cast<int32_t*>(workspace);
+    return launch_append(a, static_cast<cudaStream_t>(cuda_stream));
+}
+
+namespace {
+
+csp_status check_page_state(const csp_page_state* s) {
+    if (!s) return CSP_ERR_INVALID_ARG;
+    if (s->batch < 0 || s->n_heads <= 0 || s->max_pages <= 0 || s->page_rows <= 0 || s->n_pages <= 0)
+        return CSP_ERR_INVALID_ARG;
+    // a table entry's place is kept in 32 bits
+    if (int64_t(s->batch) * s->max_pages > 0x7fffffffLL || s->n_pages > (1 << 30)) return CSP_ERR_UNSUPPORTED;
+    return CSP_OK;
+}
+
+csp_status check_page_call(const csp_page_state* s, const void* ws, size_t bytes) {
+    csp_status st = check_page_state(s);
+    if (st != CSP_OK) return st;
+    if (!s->page_table || !s->held || !s->refs || !s->n_rows) return CSP_ERR_INVALID_ARG;
+    if (!status_area_ok(ws, bytes, pages_workspace_bytes(*s))) return CSP_ERR_WORKSPACE;
+    return CSP_OK;
+}
+
+}  // namespace
+
+size_t csp_pages_workspace_bytes(const csp_page_state* s) {
+    return check_page_state(s) == CSP_OK ? pages_workspace_bytes(*s) : 0;
+}
+
+csp_status csp_pages_fork(const csp_page_state* s, const int32_t* src, const int32_t* dst, int32_t n, void* workspace,
+                          size_t workspace_bytes, void* cuda_stream) {
+    if (n < 0 || (n > 0 && (!src || !dst))) return CSP_ERR_INVALID_ARG;
+    csp_status st = check_page_call(s, workspace, workspace_bytes);
+    if (st != CSP_OK || (st = check_arch()) != CSP_OK) return st;
+    return launch_pages_fork(page_args(*s, workspace), src, dst, n, static_cast<cudaStream_t>(cuda_stream));
+}
+
+csp_status csp_pages_reserve(const csp_page_state* s, const int32_t* n_new_or_null, int32_t whole, int32_t* moves,
+                             int32_t max_moves, int32_t* n_moves, void* workspace, size_t workspace_bytes,
+                             void* cuda_stream) {
+    if (max_moves < 0 || (max_moves > 0 && !moves) || !n_moves) return CSP_ERR_INVALID_ARG;
+    if (uintptr_t(moves) % 8) return CSP_ERR_UNSUPPORTED;
+    csp_status st = check_page_call(s, workspace, workspace_bytes);
+    if (st != CSP_OK || (st = check_arch()) != CSP_OK) return st;
+    return launch_pages_reserve(page_args(*s, workspace), n_new_or_null, whole ? 1 : 0, moves, max_moves, n_moves,
+                                static_cast<cudaStream_t>(cuda_stream));
+}
+
+csp_status csp_pages_free(const csp_page_state* s, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    csp_status st = check_page_call(s, workspace, workspace_bytes);
+    if (st != CSP_OK || (st = check_arch()) != CSP_OK) return st;
+    return launch_pages_free(page_args(*s, workspace), static_cast<cudaStream_t>(cuda_stream));
+}
+
+csp_status csp_pages_compact(const csp_page_state* s, int32_t* moves, int32_t max_moves, int32_t* n_moves,
+                             void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (max_moves < 0 || (max_moves > 0 && !moves) || !n_moves) return CSP_ERR_INVALID_ARG;
+    if (uintptr_t(moves) % 8) return CSP_ERR_UNSUPPORTED;
+    csp_status st = check_page_call(s, workspace, workspace_bytes);
+    if (st != CSP_OK || (st = check_arch()) != CSP_OK) return st;
+    return launch_pages_compact(page_args(*s, workspace), moves, max_moves, n_moves, static_cast<cudaStream_t>(cuda_stream));
+}
+
+csp_status csp_pages_copy(const csp_params* p, csp_tensor k_pool, csp_tensor v_pool, int32_t n_pages, int32_t page_rows,
+                          const int32_t* moves, int32_t max_moves, const int32_t* n_moves, void* workspace,
+                          size_t workspace_bytes, void* cuda_stream) {
+    csp_status st = check_params(p);
+    if (st != CSP_OK) return st;
+    if (!k_pool.ptr || !v_pool.ptr || n_pages <= 0 || page_rows <= 0 || max_moves < 0 || (max_moves > 0 && !moves) || !n_moves)
+        return CSP_ERR_INVALID_ARG;
+    if (!tensor_ok(*p, k_pool) || !tensor_ok(*p, v_pool) || uintptr_t(moves) % 8) return CSP_ERR_UNSUPPORTED;
+    if (!rows_apart(*p, k_pool, n_pages, p->n_kv_heads, page_rows) || !rows_apart(*p, v_pool, n_pages, p->n_kv_heads, page_rows))
+        return CSP_ERR_UNSUPPORTED;
+    const int64_t es = elem_size(*p);
+    if (int64_t(page_rows) * (p->head_dim * es / 16) > (1 << 30)) return CSP_ERR_UNSUPPORTED;   // 16-byte chunks are counted in 32 bits
+    if (!status_area_ok(workspace, workspace_bytes, kStatusBytes)) return CSP_ERR_WORKSPACE;
+    if ((st = check_arch()) != CSP_OK) return st;
+    PageCopyArgs a;
+    a.k = k_pool.ptr; a.v = v_pool.ptr;
+    a.k_sb = k_pool.stride_b * es / 16; a.k_sh = k_pool.stride_h * es / 16; a.k_st = k_pool.stride_t * es / 16;
+    a.v_sb = v_pool.stride_b * es / 16; a.v_sh = v_pool.stride_h * es / 16; a.v_st = v_pool.stride_t * es / 16;
+    a.n_kv_heads = p->n_kv_heads; a.n_pages = n_pages; a.page_rows = page_rows;
+    a.chunks_per_row = int(p->head_dim * es / 16);
+    a.moves = reinterpret_cast<const int2*>(moves); a.max_moves = max_moves; a.n_moves = n_moves;
+    a.status = static_cast<int32_t*>(workspace);
+    return launch_pages_copy(a, static_cast<cudaStream_t>(cuda_stream));
+}
+
 csp_status csp_device_status(void* workspace, void* cuda_stream, int32_t* host_out) {
     if (!workspace) return CSP_ERR_WORKSPACE;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);

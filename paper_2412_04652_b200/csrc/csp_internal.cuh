@@ -185,4 +185,62 @@ csp_status launch_decode_attn(const csp_params& p, const csp_tensor& q, const cs
                               const int32_t* n_rows, float* out, void* ws, cudaStream_t s,
                               const DecodeStepArgs* step = nullptr, const csp_pages* pages = nullptr);
 
+// ---- chunk attention (csp_chunk.cu) -------------------------------------------------------
+// csp_score_mods as the kernels take it: null pointers where there is nothing
+struct ModArgs {
+    float softcap;                                   // 0: none
+    const float* slopes;
+    const int32_t* positions; int64_t pos_sb, pos_sh;
+    const int32_t* documents; int64_t doc_sb, doc_sh;
+    const int32_t* prefix; int64_t prefix_sb, prefix_sh;
+};
+
+struct ChunkArgs {
+    const int32_t* n_rows;                           // [B, Hkv]
+    const int32_t* n_new;                            // [B], or null: max_new
+    uint16_t* out; int64_t o_sb, o_sh, o_st;         // bf16, element strides
+    float* lse;                                      // [B, Hq, max_new] or null
+    int32_t* status;
+    int32_t batch, n_kv_heads, group, capacity, max_new;
+    float n, scale;
+    ModArgs mods;
+    const int32_t* page_table; int32_t max_pages, page_rows, n_pages;   // null: dense cache
+};
+size_t chunk_workspace_bytes(const csp_params& p, int max_new);
+csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_tensor& q, const csp_tensor& k,
+                             const csp_tensor& v, const csp_pages* pages, void* ws, cudaStream_t s);
+
+// ---- pages of a paged cache (csp_pages.cu) -------------------------------------------------
+struct PageArgs {
+    int32_t* table; int32_t* held; int32_t* refs; int32_t* n_rows;
+    int32_t batch, n_heads, max_pages, page_rows, n_pages;
+    int32_t* status;
+    // lists in the workspace: per page, and first / need per sequence
+    int32_t* claims; int32_t* last; int32_t* list; int32_t* first; int32_t* need;
+};
+struct PageCopyArgs {
+    void* k; void* v;
+    int64_t k_sb, k_sh, k_st, v_sb, v_sh, v_st;      // in 16-byte units
+    int32_t n_kv_heads, n_pages, page_rows, chunks_per_row;
+    const int2* moves; int32_t max_moves; const int32_t* n_moves;
+    int32_t* status;
+};
+struct AppendArgs {
+    const void* k_new; const void* v_new; void* k; void* v;
+    int64_t kn_sb, kn_sh, kn_st, vn_sb, vn_sh, vn_st, k_sb, k_sh, k_st, v_sb, v_sh, v_st;   // in 16-byte units
+    const int32_t* n_new; const int32_t* n_rows; int32_t* n_rows_out;
+    int32_t units, n_kv_heads, max_new, capacity, chunks_per_row;
+    const int32_t* page_table; int32_t max_pages, page_rows, n_pages;
+    int32_t* status;
+};
+size_t pages_workspace_bytes(const csp_page_state& s);
+PageArgs page_args(const csp_page_state& s, void* ws);
+csp_status launch_pages_fork(const PageArgs& a, const int32_t* src, const int32_t* dst, int n, cudaStream_t s);
+csp_status launch_pages_reserve(const PageArgs& a, const int32_t* n_new, int whole, int32_t* moves, int max_moves,
+                                int32_t* n_moves, cudaStream_t s);
+csp_status launch_pages_free(const PageArgs& a, cudaStream_t s);
+csp_status launch_pages_compact(const PageArgs& a, int32_t* moves, int max_moves, int32_t* n_moves, cudaStream_t s);
+csp_status launch_pages_copy(const PageCopyArgs& a, cudaStream_t s);
+csp_status launch_append(const AppendArgs& a, cudaStream_t s);
+
 }  // namespace csp
