@@ -170,6 +170,11 @@ csp_status launch_select_compact(const csp_params& p, const SelectArgs& sa, cons
 bool make_cache_tensor_map(CUtensorMap* map, const csp_tensor& t, int dtype, int head_dim, int rows, int heads,
                            int batch, int box_rows);
 
+// 4-D tensor map over bf16 queries [batch, heads, tokens, head_dim] whose boxes hold 64 columns of box_tokens tokens, the
+// box_heads heads of a token as neighbouring rows
+bool make_query_tensor_map(CUtensorMap* map, const csp_tensor& t, int head_dim, int heads, int tokens, int batch,
+                           int box_heads, int box_tokens);
+
 // decode attention over the pruned cache (csp_decode.cu)
 int decode_splits(const csp_params& p);
 size_t decode_workspace_bytes(const csp_params& p);
