@@ -23,14 +23,13 @@
 // softmax runs while the tensor cores work for the other.
 #include <limits.h>
 
-#include "csp_internal.cuh"
+#include "csp_chunk.cuh"
 #include "csp_tc.cuh"
 
 namespace csp {
 namespace {
 using namespace dev;
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kGroupWarps = 4;
 constexpr int kSoftmaxWarps = 2 * kGroupWarps;
 constexpr int kChProducerWarp = kSoftmaxWarps, kChMmaWarp = kSoftmaxWarps + 1;
@@ -41,19 +40,11 @@ constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
 constexpr int kEntries = 8;                              // ring of tile entries
 constexpr int kEntryWords = 16;
 constexpr int kMinTiles = 2;                             // no item of a split cache is shorter than one tile per group
-constexpr int kMaxSplits = 64;
-constexpr int kSeesAll = 1 << 30;
 constexpr uint32_t kUnset = 0xBF800000u;                 // -1.0f: no sum of weights has these bits
 
 // what an entry says
 enum EntryWord { kKind, kTile0, kAct, kSeq, kHead, kTok0, kRows, kNew, kSplit, kActive, kQSlots, kFirst, kPair, kPrefix };
 enum EntryKind { kEntryTile, kEntryEnd, kEntryStop };
-
-struct ChunkPlan {                                       // sizes that host and device agree on
-    int tok_tile;                                        // tokens in a row tile: 128 / G
-    int n_pairs, splits, row_slots;                      // row pairs per unit, splits per pair, rows of a partial result
-    int n_items;
-};
 
 struct ChunkSmem { uint32_t q, meta, entries, ml, bars, misc, total; };
 template <int NH, bool kMeta>
@@ -75,47 +66,6 @@ struct ChunkShape {
         return s;
     }
 };
-
-// What the rows of a pair look at.
-struct PairRange {
-    int rows, n_new, tok0, count;                        // rows of the unit, tokens of the sequence, first token, tokens here
-    int row0, prefix;                                    // row of the first token; clamped prefix
-    int kv_end[2];                                       // keys that row tile 0 / the whole pair can see: [0, kv_end)
-    int tiles, per_split, active;
-};
-__device__ __forceinline__ PairRange pair_range(const ChunkArgs& a, const ChunkPlan& pl, int u, int pair) {
-    PairRange x;
-    const int b = u / a.n_kv_heads, h = u % a.n_kv_heads;
-    x.rows = min(max(a.n_rows[u], 0), a.capacity);
-    x.n_new = a.n_new ? min(max(a.n_new[b], 0), a.max_new) : a.max_new;
-    x.tok0 = pair * 2 * pl.tok_tile;
-    x.count = min(x.n_new - x.tok0, 2 * pl.tok_tile);
-    x.row0 = x.rows - x.n_new + x.tok0;
-    x.prefix = a.mods.prefix ? min(max(a.mods.prefix[int64_t(b) * a.mods.prefix_sb + int64_t(h) * a.mods.prefix_sh], 0), x.rows) : 0;
-    const int last0 = x.row0 + min(x.count, pl.tok_tile) - 1, last1 = x.row0 + x.count - 1;
-    x.kv_end[0] = last0 < 0 ? 0 : max(last0 + 1, x.prefix);
-    x.kv_end[1] = last1 < 0 ? 0 : max(last1 + 1, x.prefix);
-    x.tiles = (x.kv_end[1] + kTileKeys - 1) / kTileKeys;
-    // a unit is divided by its own length, so that batches of any length below the capacity are spread evenly
-    x.per_split = max(kMinTiles, (x.tiles + pl.splits - 1) / pl.splits);
-    x.active = max(1, (x.tiles + x.per_split - 1) / x.per_split);
-    return x;
-}
-
-__device__ __forceinline__ float rcpf(float x) {
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-// bounded wait of a whole warp: all lanes come back with the same answer
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
-}
 
 template <int NH, bool kCap, bool kBias, bool kDoc>
 __global__ void __launch_bounds__(kChThreads, 1)
@@ -173,7 +123,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kChProducerWarp) {
         // =============================== producer ===============================
-        int32_t* const next_item = a.status + 8;
         uint32_t n_entry = 0, n_stage = 0, q_uses[2] = {0, 0}, n_small = 0;
         bool ok = true;
         auto publish = [&](int32_t word) {               // lane l < kEntryWords brings word l
@@ -187,12 +136,12 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             if (ok && lane == 0) mbar_arrive(ent_full + 8 * e);
             ++n_entry;
         };
-        int w = blockIdx.x, ahead = 0;
-        if (lane == 0) ahead = int(gridDim.x) + atomicAdd(next_item, 1);
+        ItemDraw draw;
+        draw.init(lane, a.status, pl.n_items);
+        int w = blockIdx.x;
         while (ok && w < pl.n_items) {
             const int w_now = w;
-            w = __shfl_sync(0xffffffffu, ahead, 0);
-            if (w < pl.n_items && lane == 0) ahead = int(gridDim.x) + atomicAdd(next_item, 1);   // looked at an item later
+            w = draw.next(lane);
             const int split = w_now % pl.splits, up = w_now / pl.splits, pair = up % pl.n_pairs, u = up / pl.n_pairs;
             const int b = u / a.n_kv_heads, h = u % a.n_kv_heads;
             const PairRange x = pair_range(a, pl, u, pair);
@@ -343,8 +292,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 }
                 atomicOr(a.status, CSP_DEV_TIMEOUT);
             }
-            // the counters are zero again for the next call: the last CTA has drawn its last item
-            if (atomicAdd(a.status + 9, 1) == int(gridDim.x) - 1) { *next_item = 0; a.status[9] = 0; }
+            draw.done();
         }
         __syncwarp();
     } else if (warp == kChMmaWarp) {
@@ -735,23 +683,28 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const ChunkArgs a, con
 
 // ---- host side -----------------------------------------------------------------------------------------------------
 
-// How many parts the keys of a pair are divided into.  An estimate of the time in SM clocks, from the kernel's own
-// figures: a key tile (two row tiles: their products; one: its share of the memory stream), what an item costs besides, what the
-// merge kernel costs.  With fewer items than SMs the longest item counts, otherwise the waves plus half an item for the
-// uneven end.
-int pick_splits(int64_t pairs, int rows, int64_t cap_tiles, int sms) {
-    const double tile = rows > 128 ? 2400. : 2800., item = 4000., merge = 6000.;
+// How many parts the keys of a pair are divided into.  An estimate of the time in SM clocks, from the kernels' own
+// figures: a key tile, what an item costs besides, what the joining kernel costs.  With fewer items than SMs the longest
+// item counts, otherwise the waves plus half an item for the uneven end.
+constexpr int kMaxSplits = 64;
+int pick_splits(int64_t pairs, int64_t cap_tiles, int min_tiles, double tile, double item, int sms) {
+    const double join = 6000.;
     int best = 1;
     double best_cost = 0;
     for (int s = 1; s <= kMaxSplits; ++s) {
         const int64_t per = (cap_tiles + s - 1) / s;
-        if (s > 1 && per < kMinTiles) break;
+        if (s > 1 && per < min_tiles) break;
         const double one = double(per) * tile + item, items = double(pairs) * s;
-        const double cost = one * (items <= sms ? 1. : items / sms + 0.5) + (s > 1 ? merge : 0.);
+        const double cost = one * (items <= sms ? 1. : items / sms + 0.5) + (s > 1 ? join : 0.);
         if (s == 1 || cost < best_cost * 0.98) { best = s; best_cost = cost; }
     }
     return best;
 }
+
+// Up to sixteen query rows per KV head (single tokens above all) go to the kernel that streams the cache through
+// warp-level products: its rows are spread over all threads, where a tcgen05 row tile would leave most of them idle.
+// Measured for one token, 32 sequences x 32 heads, 410 - 1640 rows each, d = 128: TODO us there, 173 us in row tiles.
+constexpr int kFewRows = 16;
 
 ChunkPlan chunk_plan(const csp_params& p, int max_new) {
     ChunkPlan pl;
@@ -760,8 +713,14 @@ ChunkPlan chunk_plan(const csp_params& p, int max_new) {
     pl.n_pairs = (max_new + 2 * pl.tok_tile - 1) / (2 * pl.tok_tile);
     if (pl.n_pairs < 1) pl.n_pairs = 1;
     pl.row_slots = (max_new < 2 * pl.tok_tile ? max_new : 2 * pl.tok_tile) * G;
+    const bool few = pl.row_slots <= kFewRows;
+    pl.key_tile = few ? 64 : kTileKeys;
+    pl.min_tiles = few ? 2 : kMinTiles;
     const int64_t pairs = int64_t(p.batch) * p.n_kv_heads * pl.n_pairs;
-    pl.splits = pick_splits(pairs, pl.row_slots, (int64_t(p.out_capacity) + kTileKeys - 1) / kTileKeys, sm_count());
+    // a tile of 64 or 128 keys as a share of the memory stream, or the products of two row tiles
+    const double tile = few ? 1400. : pl.row_slots > 128 ? 2400. : 2800.;
+    pl.splits = pick_splits(pairs, (int64_t(p.out_capacity) + pl.key_tile - 1) / pl.key_tile, pl.min_tiles, tile,
+                            few ? 2500. : 4000., sm_count());
     const int64_t items = pairs * pl.splits;
     pl.n_items = items > 0x3fffffffLL ? -1 : int(items);
     return pl;
@@ -824,12 +783,17 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
     const int map_rows = pages ? pages->page_rows : (p.out_capacity > 0 ? p.out_capacity : 1);
     const int map_outer = pages ? pages->n_pages : p.batch;
     const int box_tokens = pl.tok_tile < a.max_new ? pl.tok_tile : a.max_new;
-    if (!make_query_tensor_map(&tq, q, p.head_dim, p.n_q_heads, a.max_new, p.batch, a.group, box_tokens) ||
-        !make_cache_tensor_map(&tk, k, p.dtype, p.head_dim, map_rows, p.n_kv_heads, map_outer, kTileKeys) ||
-        !make_cache_tensor_map(&tv, v, p.dtype, p.head_dim, map_rows, p.n_kv_heads, map_outer, kTileKeys))
+    if (!make_cache_tensor_map(&tk, k, p.dtype, p.head_dim, map_rows, p.n_kv_heads, map_outer, pl.key_tile) ||
+        !make_cache_tensor_map(&tv, v, p.dtype, p.head_dim, map_rows, p.n_kv_heads, map_outer, pl.key_tile))
         return CSP_ERR_UNSUPPORTED;
-    const csp_status st = p.head_dim == 64 ? launch_nh<1>(a, pl, tq, tk, tv, partial, ml, s)
-                                           : launch_nh<2>(a, pl, tq, tk, tv, partial, ml, s);
+    csp_status st;
+    if (pl.row_slots <= kFewRows) {
+        st = launch_chunk_few(p, a, pl, q, tk, tv, partial, ml, s);
+    } else {
+        if (!make_query_tensor_map(&tq, q, p.head_dim, p.n_q_heads, a.max_new, p.batch, a.group, box_tokens))
+            return CSP_ERR_UNSUPPORTED;
+        st = p.head_dim == 64 ? launch_nh<1>(a, pl, tq, tk, tv, partial, ml, s) : launch_nh<2>(a, pl, tq, tk, tv, partial, ml, s);
+    }
     if (st != CSP_OK || pl.splits == 1) return st;
     const int64_t rows = int64_t(pl.n_items / pl.splits) * pl.row_slots;
     const unsigned blocks = unsigned((rows + 7) / 8);

@@ -1,0 +1,395 @@
+// Chunk attention with up to sixteen query rows (token x head) per KV head: single tokens, and a few tokens at once.
+// One pass over K and V, bound by HBM (512 bytes per cached row and KV head at d = 128); the products are far too thin
+// for a tcgen05 row tile of 128, whose softmax would run on a quarter of one warp group.  Here the rows are the M of a
+// warp-level m16n8k16 product and the keys of a tile are spread over the warps, so every thread has a few logits.
+//
+// Same organisation as the decode kernel: one CTA per SM stays resident and draws items (a range of 64-key tiles of
+// one unit) from a counter.
+//   warp 4      producer: streams tiles of K and V with TMA (128-byte swizzle, no multicast) through a ring of six
+//               stages and says with each stage which tile it holds; an item ends with a stage without data
+//   warps 0-3   each owns 16 keys of every tile: S = Q K^T, modifiers and mask, running softmax with a lazily raised
+//               reference, then P V with the weights as a bf16 head plus a bf16 remainder (two products per fragment),
+//               so that only the result is rounded to bf16.  At the end of an item the four warps' results are
+//               joined in a fixed order; an undivided unit is finished here, a divided one leaves a partial result
+#include <limits.h>
+
+#include "csp_chunk.cuh"
+
+namespace csp {
+namespace {
+using namespace dev;
+
+constexpr int kFewTile = 64;                             // keys per stage
+constexpr int kFewWarps = 4;                             // consumer warps, 16 keys of every tile each
+constexpr int kFewThreads = 32 * (kFewWarps + 1);
+constexpr int kFewStages = 6;                            // 32 KB each at d = 128
+constexpr int kFewBlock = kFewTile * 128;                // bytes of one 64-column block of a tile
+
+struct FewQuery { const uint16_t* q; int64_t sb, sh, st; };
+
+__device__ __forceinline__ void ldsm_x4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+
+template <int NH, int RH>
+struct FewShape {
+    static constexpr int D = 64 * NH, R = 8 * RH;
+    static constexpr uint32_t kTileBytes = NH * kFewBlock, kStageBytes = 2 * kTileBytes;
+    static constexpr uint32_t kMerge = kFewStages * kStageBytes;                       // [warp][R][D + 2] floats
+    static constexpr uint32_t kBars = kMerge + kFewWarps * R * (D + 2) * 4;            // full, empty, join
+    static constexpr uint32_t kInfo = kBars + (2 * kFewStages + 1) * 8;                // int2 per stage: item, tile
+    static constexpr uint32_t kMisc = kInfo + kFewStages * 8;
+    static constexpr uint32_t kTotal = kMisc + 16;
+};
+
+template <int NH, int RH>   // head_dim = 64 NH, 8 RH query rows
+__global__ void __launch_bounds__(kFewThreads, 1)
+chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const ChunkArgs a,
+                 const ChunkPlan pl, const FewQuery qy, float* const partial, float2* const partial_ml) {
+    using Shape = FewShape<NH, RH>;
+    constexpr int D = Shape::D, R = Shape::R;
+    constexpr int KS = D / 16;                           // k-steps of S = Q K^T
+    constexpr int NT = D / 8;                            // 8-column tiles of the output
+    constexpr uint32_t kTileBytes = Shape::kTileBytes, kStageBytes = Shape::kStageBytes;
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
+    float* const merge = reinterpret_cast<float*>(base_ptr + Shape::kMerge);
+    const uint32_t full_bar = base + Shape::kBars, empty_bar = full_bar + 8 * kFewStages, join_bar = empty_bar + 8 * kFewStages;
+    volatile int* const info = reinterpret_cast<volatile int*>(base_ptr + Shape::kInfo);
+    volatile int* const abort_flag = reinterpret_cast<volatile int*>(base_ptr + Shape::kMisc);
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.group;
+    const ModArgs& md = a.mods;
+    if (tid == 0) {
+        *abort_flag = 0;
+        for (int s = 0; s < kFewStages; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, kFewWarps); }
+        mbar_init(join_bar, kFewWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+
+    if (warp == kFewWarps) {
+        // =============================== producer ===============================
+        uint32_t it = 0;
+        bool ok = true;
+        auto stage = [&](int item, int tile) {           // the next stage, free, with what it holds written beside it
+            const uint32_t s = it % kFewStages;
+            ok = ok && warp_wait(empty_bar + 8 * s, ((it / kFewStages) & 1u) ^ 1u, abort_flag);
+            if (ok && lane == 0) { info[2 * s] = item; info[2 * s + 1] = tile; }
+            ++it;
+            return s;
+        };
+        auto marker = [&](int item) {                    // a stage without data: the item has no more tiles (-1: no more items)
+            const uint32_t s = stage(item, -1);
+            if (ok && lane == 0) mbar_arrive(full_bar + 8 * s);
+        };
+        ItemDraw draw;
+        draw.init(lane, a.status, pl.n_items);
+        int w = blockIdx.x;
+        while (ok && w < pl.n_items) {
+            const int w_now = w;
+            w = draw.next(lane);
+            const int split = w_now % pl.splits, u = w_now / pl.splits, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
+            const PairRange x = pair_range(a, pl, u, 0);
+            if (split == 0 && lane == 0) {
+                const int rows = a.n_rows[u], more = a.n_new ? a.n_new[b] : a.max_new;
+                if (rows != x.rows || more != x.n_new || x.n_new > x.rows) atomicOr(a.status, CSP_DEV_BAD_LEN);
+            }
+            if (x.count <= 0 || split >= x.active) continue;
+            const int tile0 = split * x.per_split, tile1 = min(x.tiles, tile0 + x.per_split);
+            const int32_t* const docs = md.documents ? md.documents + int64_t(b) * md.doc_sb + int64_t(h) * md.doc_sh : nullptr;
+            int doc_lo = INT_MAX, doc_hi = INT_MIN;
+            if (docs) {                                  // sixteen rows at most
+                const int r = x.row0 + lane;
+                if (lane < x.count && r >= 0) doc_lo = doc_hi = docs[r];
+                doc_lo = __reduce_min_sync(0xffffffffu, doc_lo);
+                doc_hi = __reduce_max_sync(0xffffffffu, doc_hi);
+            }
+            int pages = 0, d_next[2] = {0, 0};
+            auto fetch_docs = [&](int tile) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int t = tile * kFewTile + lane + 32 * j;
+                    d_next[j] = t < x.kv_end[1] ? docs[t] : INT_MIN;
+                }
+            };
+            if (docs && tile0 < tile1) fetch_docs(tile0);
+            for (int tile = tile0; tile < tile1 && ok; ++tile) {
+                if (a.page_table && ((tile - tile0) & 31) == 0) {
+                    const int mine = tile + lane;
+                    pages = mine < tile1 ? a.page_table[int64_t(b) * a.max_pages + int64_t(mine) * kFewTile / a.page_rows] : 0;
+                }
+                if (docs) {                              // a tile without any of the tokens' documents is skipped
+                    bool hit = false;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) hit |= tile * kFewTile + lane + 32 * j < x.kv_end[1] && d_next[j] >= doc_lo && d_next[j] <= doc_hi;
+                    if (tile + 1 < tile1) fetch_docs(tile + 1);
+                    if (!__any_sync(0xffffffffu, hit)) continue;
+                }
+                int outer = b, row = tile * kFewTile;
+                if (a.page_table) {
+                    // a page number outside the pool becomes an out-of-range coordinate: zeros arrive, nothing faults
+                    outer = __shfl_sync(0xffffffffu, pages, (tile - tile0) & 31);
+                    if (outer < 0 || outer >= a.n_pages) {
+                        if (lane == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
+                        outer = a.n_pages;
+                    }
+                    row %= a.page_rows;
+                }
+                const uint32_t s = stage(w_now, tile);
+                if (ok && lane == 0) {
+                    mbar_expect_tx(full_bar + 8 * s, kStageBytes);
+#pragma unroll
+                    for (int hb = 0; hb < NH; ++hb) {
+                        tma_load_4d(base + s * kStageBytes + hb * kFewBlock, &tmap_k, full_bar + 8 * s, hb * 64, row, h, outer);
+                        tma_load_4d(base + s * kStageBytes + kTileBytes + hb * kFewBlock, &tmap_v, full_bar + 8 * s, hb * 64, row, h, outer);
+                    }
+                }
+            }
+            marker(w_now);
+        }
+        if (ok) marker(-1);
+        if (lane == 0) {
+            if (!ok) {
+                // let copies that were issued land before the CTA's shared memory is given up
+                for (int s = 0; s < kFewStages; ++s) {
+                    const unsigned long long t0 = global_ns();
+                    while (!mbar_try_wait(full_bar + 8 * s, 0) && !mbar_try_wait(full_bar + 8 * s, 1) && global_ns() - t0 < kWaitLimitNs / 8) {}
+                }
+                atomicOr(a.status, CSP_DEV_TIMEOUT);
+            }
+            draw.done();
+        }
+    } else {
+        // =============================== consumer warps ===============================
+        const int gq = lane >> 2, qd = lane & 3;         // this thread's query row (and row + 8) and column pair
+        // ldmatrix row addresses: lane l supplies row (l % 8) of matrix (l / 8)
+        const int kr = warp * 16 + ((lane >> 4) << 3) + (lane & 7);      // K: matrices 2,3 are the second 8 rows
+        const int kc = (lane >> 3) & 1;                                  //    matrices 1,3 the second 8 columns
+        const int vr = warp * 16 + (((lane >> 3) & 1) << 3) + (lane & 7);  // V: matrices 1,3 are the second 8 rows
+        const int vc = lane >> 4;                                        //    matrices 2,3 the next 8 columns
+        const float scale2 = a.scale * kLog2e;
+        const bool capped = md.softcap > 0.f;
+        // capped: x = c tanh(o / c) = c - 2 c / (1 + e^{2 o / c}), all in the base-2 domain
+        const float cap2 = md.softcap * kLog2e, cap_in = capped ? 2.f * kLog2e * a.scale / md.softcap : 0.f;
+        uint32_t it = 0, n_join = 0;
+        int item = -1, b = 0, h = 0, u = 0, split = 0;
+        PairRange x = {};
+        uint32_t qa[KS][4];
+        float acc[NT][4];
+        float m_run[RH], l_run[RH], q_pos[RH], slope2[RH];
+        int lim[RH], q_doc[RH], pos_ref = 0;
+        const int32_t* docs = nullptr;
+        const int32_t* poss = nullptr;
+        for (;;) {
+            const uint32_t s = it % kFewStages;
+            if (!warp_wait(full_bar + 8 * s, (it / kFewStages) & 1u, abort_flag)) break;
+            ++it;
+            const int w = info[2 * s], tile = info[2 * s + 1];
+            if (w < 0) break;
+            if (w != item) {
+                item = w;
+                split = w % pl.splits; u = w / pl.splits; b = u / a.n_kv_heads; h = u % a.n_kv_heads;
+                x = pair_range(a, pl, u, 0);
+                docs = md.documents ? md.documents + int64_t(b) * md.doc_sb + int64_t(h) * md.doc_sh : nullptr;
+                poss = md.slopes && md.positions ? md.positions + int64_t(b) * md.pos_sb + int64_t(h) * md.pos_sh : nullptr;
+                // positions count from the last token's, so that near ones are exact in fp32
+                const int row_last = max(x.row0 + x.count - 1, 0);
+                pos_ref = md.slopes && x.rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
+#pragma unroll
+                for (int rr = 0; rr < RH; ++rr) {
+                    const int m = gq + 8 * rr, tok = m / G, head = h * G + m % G, r = x.row0 + tok;
+                    const bool valid = tok < x.count, sees = valid && r >= 0;
+                    const uint16_t* const qrow = qy.q + int64_t(b) * qy.sb + int64_t(head) * qy.sh + int64_t(tok) * qy.st;
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) {
+                        qa[ks][rr] = valid ? *reinterpret_cast<const uint32_t*>(qrow + ks * 16 + 2 * qd) : 0u;
+                        qa[ks][rr + 2] = valid ? *reinterpret_cast<const uint32_t*>(qrow + ks * 16 + 8 + 2 * qd) : 0u;
+                    }
+                    lim[rr] = !valid ? kSeesAll : sees ? max(r, x.prefix - 1) : -1;
+                    q_doc[rr] = docs && sees ? docs[r] : 0;
+                    q_pos[rr] = md.slopes && sees ? float((poss ? poss[r] : r) - pos_ref) : 0.f;
+                    slope2[rr] = md.slopes && sees ? md.slopes[head] * kLog2e : 0.f;
+                    m_run[rr] = kNeg;
+                    l_run[rr] = 0.f;
+                }
+                if (RH == 1) {
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) qa[ks][1] = qa[ks][3] = 0u;
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
+            }
+            if (tile >= 0) {
+                const uint32_t k_s = base + s * kStageBytes, v_s = k_s + kTileBytes;
+                const int row_t = tile * kFewTile, row_w = row_t + warp * 16, r0 = row_w + 2 * qd;
+                // what the modifiers need to know of this thread's four keys, fetched before the products
+                int k_doc[4] = {0, 0, 0, 0}, k_pos[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int t = r0 + (j & 1) + (j >> 1) * 8;
+                    if (docs && t < x.rows) k_doc[j] = docs[t];
+                    if (md.slopes) k_pos[j] = poss ? (t < x.rows ? poss[t] : pos_ref) : t;
+                }
+                if (row_w + 16 > x.rows) {
+                    // Rows past the end hold whatever the cache holds: their weights are zero, but zero times a
+                    // non-finite value is not, so clear this warp's value rows beyond the end.
+                    for (int j = lane; j < 16 * NH * 8; j += 32) {
+                        const int r = warp * 16 + j / (NH * 8), c = j % (NH * 8);
+                        if (row_t + r >= x.rows)
+                            *reinterpret_cast<uint4*>(base_ptr + (v_s - base) + (c >> 3) * kFewBlock + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
+                                make_uint4(0, 0, 0, 0);
+                    }
+                    __syncwarp();
+                }
+                // ---- S = Q K^T for 16 keys: two 8-key tiles
+                float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const int chunk = ks * 2 + kc;
+                    uint32_t kb[4];
+                    ldmatrix_x4(kb, k_s + (chunk >> 3) * kFewBlock + kr * 128 + (((chunk & 7) ^ (kr & 7)) << 4));
+                    mma_bf16(s0, qa[ks], kb[0], kb[1]);
+                    mma_bf16(s1, qa[ks], kb[2], kb[3]);
+                }
+                uint32_t ph[4] = {0u, 0u, 0u, 0u}, pr[4] = {0u, 0u, 0u, 0u};      // weights: bf16 head, bf16 remainder
+#pragma unroll
+                for (int rr = 0; rr < RH; ++rr) {
+                    float xs[4] = {s0[2 * rr], s0[2 * rr + 1], s1[2 * rr], s1[2 * rr + 1]};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int t = r0 + (j & 1) + (j >> 1) * 8;
+                        xs[j] = capped ? fmaf(-2.f * cap2, rcpf(1.f + ex2f(xs[j] * cap_in)), cap2) : xs[j] * scale2;
+                        if (md.slopes) xs[j] = fmaf(-slope2[rr], fabsf(q_pos[rr] - float(k_pos[j] - pos_ref)), xs[j]);
+                        const bool sees = t <= lim[rr] && t < x.rows && (!docs || k_doc[j] == q_doc[rr]);
+                        xs[j] = sees ? xs[j] : kNeg;
+                    }
+                    float mx = fmaxf(fmaxf(xs[0], xs[1]), fmaxf(xs[2], xs[3]));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                    if (mx > m_run[rr] + kLazy) {        // same decision in the four lanes of a row
+                        const float alpha = ex2f(m_run[rr] - mx);
+                        l_run[rr] *= alpha;
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) { acc[t][2 * rr] *= alpha; acc[t][2 * rr + 1] *= alpha; }
+                        m_run[rr] = mx;
+                    }
+                    float p[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) p[j] = xs[j] == kNeg ? 0.f : ex2f(xs[j] - m_run[rr]);
+                    l_run[rr] += (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t hd = pack_bf16(p[2 * j], p[2 * j + 1]);
+                        ph[rr + 2 * j] = hd;
+                        pr[rr + 2 * j] = pack_bf16(p[2 * j] - __uint_as_float(hd << 16), p[2 * j + 1] - __uint_as_float(hd & 0xffff0000u));
+                    }
+                }
+                // ---- acc += P V
+#pragma unroll
+                for (int t = 0; t < NT; t += 2) {
+                    const int chunk = t + vc;
+                    uint32_t vb[4];
+                    ldsm_x4_t(vb, v_s + (chunk >> 3) * kFewBlock + vr * 128 + (((chunk & 7) ^ (vr & 7)) << 4));
+                    mma_bf16(acc[t], ph, vb[0], vb[1]);
+                    mma_bf16(acc[t], pr, vb[0], vb[1]);
+                    mma_bf16(acc[t + 1], ph, vb[2], vb[3]);
+                    mma_bf16(acc[t + 1], pr, vb[2], vb[3]);
+                }
+                if (row_w + 16 > x.rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(empty_bar + 8 * s);
+                continue;
+            }
+            // ---- end of the item: this warp's rows to shared memory, then the four warps' results joined in order
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty_bar + 8 * s);
+            // everybody has read what the previous item left there
+            if (n_join > 0 && !warp_wait(join_bar, (n_join - 1u) & 1u, abort_flag)) break;
+#pragma unroll
+            for (int rr = 0; rr < RH; ++rr) {
+                l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 1);
+                l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 2);
+                float* const mine = merge + (warp * R + gq + 8 * rr) * (D + 2);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    *reinterpret_cast<float2*>(mine + t * 8 + 2 * qd) = make_float2(acc[t][2 * rr], acc[t][2 * rr + 1]);
+                if (qd == 0) *reinterpret_cast<float2*>(mine + D) = make_float2(m_run[rr], l_run[rr]);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(join_bar);
+            if (!warp_wait(join_bar, n_join & 1u, abort_flag)) break;
+            n_join += 2;
+            const bool final = x.active == 1;
+            constexpr int C = D / 32;                    // columns per lane: a warp takes every fourth row
+            for (int m = warp; m < x.count * G; m += kFewWarps) {
+                float2 st[kFewWarps];
+                float mm = kNeg;
+#pragma unroll
+                for (int ww = 0; ww < kFewWarps; ++ww) {
+                    st[ww] = *reinterpret_cast<const float2*>(merge + (ww * R + m) * (D + 2) + D);
+                    mm = fmaxf(mm, st[ww].x);
+                }
+                float l = 0.f, o[C];
+#pragma unroll
+                for (int c = 0; c < C; ++c) o[c] = 0.f;
+#pragma unroll
+                for (int ww = 0; ww < kFewWarps; ++ww) {
+                    const float wgt = ex2f(st[ww].x - mm);
+                    l += st[ww].y * wgt;
+#pragma unroll
+                    for (int c = 0; c < C; c += 2) {
+                        const float2 y = *reinterpret_cast<const float2*>(merge + (ww * R + m) * (D + 2) + lane * C + c);
+                        o[c] += y.x * wgt;
+                        o[c + 1] += y.y * wgt;
+                    }
+                }
+                const int tok = m / G, head = h * G + m % G;
+                if (final) {
+                    const float inv = l == 0.f ? 0.f : 1.f / (a.n * ex2f(-mm) + l);      // l == 0: nothing was seen
+                    uint32_t* const out = reinterpret_cast<uint32_t*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st + lane * C);
+#pragma unroll
+                    for (int c = 0; c < C; c += 2) out[c / 2] = l == 0.f ? 0u : pack_bf16(o[c] * inv, o[c + 1] * inv);
+                    if (a.lse && lane == 0)
+                        a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
+                } else {
+                    const int64_t slot = (int64_t(u) * pl.splits + split) * pl.row_slots + m;
+#pragma unroll
+                    for (int c = 0; c < C; c += 2) *reinterpret_cast<float2*>(partial + slot * D + lane * C + c) = make_float2(o[c], o[c + 1]);
+                    if (lane == 0) partial_ml[slot] = make_float2(mm, l);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(join_bar);        // waited for before the area is written again
+        }
+    }
+}
+
+template <int NH, int RH>
+csp_status launch_few(const ChunkArgs& a, const ChunkPlan& pl, const FewQuery& q, const CUtensorMap& tk, const CUtensorMap& tv,
+                      float* partial, float2* ml, cudaStream_t s) {
+    constexpr int smem = int(FewShape<NH, RH>::kTotal) + 1024;
+    static_assert(smem <= 227 * 1024, "shared memory of one CTA");
+    auto kern = chunk_few_kernel<NH, RH>;
+    static std::atomic<bool> configured[kMaxDevices];
+    if (!raise_smem_limit(kern, smem, configured)) return CSP_ERR_CUDA;
+    const int sms = sm_count();
+    kern<<<pl.n_items < sms ? pl.n_items : sms, kFewThreads, smem, s>>>(tk, tv, a, pl, q, partial, ml);
+    return cudaGetLastError() == cudaSuccess ? CSP_OK : CSP_ERR_CUDA;
+}
+
+}  // namespace
+
+csp_status launch_chunk_few(const csp_params& p, const ChunkArgs& a, const ChunkPlan& pl, const csp_tensor& q,
+                            const CUtensorMap& tk, const CUtensorMap& tv, float* partial, float2* ml, cudaStream_t s) {
+    const FewQuery qy = {static_cast<const uint16_t*>(q.ptr), q.stride_b, q.stride_h, q.stride_t};
+    if (pl.row_slots <= 8)
+        return p.head_dim == 64 ? launch_few<1, 1>(a, pl, qy, tk, tv, partial, ml, s) : launch_few<2, 1>(a, pl, qy, tk, tv, partial, ml, s);
+    return p.head_dim == 64 ? launch_few<1, 2>(a, pl, qy, tk, tv, partial, ml, s) : launch_few<2, 2>(a, pl, qy, tk, tv, partial, ml, s);
+}
+
+}  // namespace csp
