@@ -594,6 +594,7 @@ csp_status chunk_attn(const csp_params* p, int32_t max_new, const csp_tensor& q,
     ChunkArgs a;
     a.n_rows = n_rows; a.n_new = n_new;
     a.out = static_cast<uint16_t*>(out.ptr); a.o_sb = out.stride_b; a.o_sh = out.stride_h; a.o_st = out.stride_t;
+    a.out_wide = uintptr_t(out.ptr) % 32 == 0 && out.stride_b % 16 == 0 && out.stride_h % 16 == 0 && out.stride_t % 16 == 0;
     a.lse = lse;
     a.status = static_cast<int32_t*>(workspace);
     a.batch = p->batch; a.n_kv_heads = p->n_kv_heads; a.group = p->n_q_heads / p->n_kv_heads;

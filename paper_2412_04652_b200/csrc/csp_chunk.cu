@@ -4,24 +4,25 @@
 // One pass over the keys with a running reference m (base-2 exponent) and sum l per query row.  The G query heads that
 // share a KV head and the tokens of the chunk together are the rows of a tcgen05 tile of 128: row = token * G + head,
 // so a tile of keys is fetched once for all of them.  A work item is a pair of such row tiles (up to 256 rows) of one
-// (sequence, KV head) unit against a range of 128-key tiles; one CTA per SM stays resident and draws items from a
-// counter.  Where there are few items (few heads, few tokens, a long cache) the keys of a unit are split over several
-// items, which leave un-normalised partial results for a second small kernel.
+// (sequence, KV head) unit against its 128-key tiles; one CTA per SM stays resident and works off an equal share of all
+// key tiles (see Share).  An item that was cut between CTAs leaves un-normalised partial results for a second small kernel.
 //
 // Inside a CTA
-//   warp 8      producer: looks up pages, streams K and V tiles (128-byte swizzle, TMA, no multicast) through a ring of
+//   warp 16     producer: looks up pages, streams K and V tiles (128-byte swizzle, TMA, no multicast) through a ring of
 //               shared-memory stages, stages positions and documents of the keys, and tells the other warps through a
 //               small ring of entries which tile comes next (so that whatever it skips is skipped by everybody)
-//   warp 9      one thread issues tcgen05.mma: S_g = Q K^T (128 x 128, fp32 in tensor memory) and O_g += P_g V
-//   warps 0-3, 4-7  two softmax groups g = 0, 1, one query row per thread.  A group reads its S from tensor memory,
-//               applies modifiers and mask, and writes the weights as bf16 back over S, where the second product
-//               reads them as its A operand; O stays in tensor memory.  The reference is raised only when a logit
+//   warp 17     one elected lane issues tcgen05.mma: S_g = Q K^T (128 x 128, fp32 in tensor memory) and O_g += P_g V
+//   warps 0-7, 8-15  two softmax groups g = 0, 1; two threads share a query row, half of the columns each.  A group reads
+//               its S from tensor memory, applies modifiers and mask, and writes the weights as bf16 back over S, where
+//               the second product reads them as its A operand; O stays in tensor memory.  The reference is raised only when a logit
 //               exceeds it by more than 2^8, which is rare after the first tile, so the O rows are rescaled (by the
 //               softmax thread itself) hardly ever.
 // With more than 128 rows in an item, group g takes row tile g and both see every key tile; with fewer, both take the
 // same rows and alternate over the key tiles (their results are joined when the item ends): either way one group's
 // softmax runs while the tensor cores work for the other.
 #include <limits.h>
+
+#include <type_traits>
 
 #include "csp_chunk.cuh"
 #include "csp_tc.cuh"
@@ -30,36 +31,37 @@ namespace csp {
 namespace {
 using namespace dev;
 
-constexpr int kGroupWarps = 4;
+constexpr int kGroupWarps = 8;                           // two per TMEM lane quarter: each takes half of the columns
 constexpr int kSoftmaxWarps = 2 * kGroupWarps;
 constexpr int kChProducerWarp = kSoftmaxWarps, kChMmaWarp = kSoftmaxWarps + 1;
 constexpr int kChThreads = 32 * (kSoftmaxWarps + 4);      // registers are shared out by groups of four warps: two stay idle
-// Registers per thread.  The kernel is launched with 168 (what 384 threads may have); the softmax threads hold a whole
-// row of S (128) and take 216, the other four warps make do with 72: 2 * 128 * 216 + 128 * 72 = 384 * 168.
-constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
+// Registers per thread.  The kernel is launched with 96 (what 640 threads may have); the softmax threads, which hold a
+// quarter of a row of S at a time, take 104, the other four warps make do with 64: 512 * 104 + 128 * 64 = 640 * 96.
+constexpr int kSoftmaxRegs = 104, kOtherRegs = 64;
 constexpr int kEntries = 8;                              // ring of tile entries
-constexpr int kEntryWords = 16;
-constexpr int kMinTiles = 2;                             // no item of a split cache is shorter than one tile per group
+constexpr int kEntryWords = 12;
 constexpr uint32_t kUnset = 0xBF800000u;                 // -1.0f: no sum of weights has these bits
 
-// what an entry says
-enum EntryWord { kKind, kTile0, kAct, kSeq, kHead, kTok0, kRows, kNew, kSplit, kActive, kQSlots, kFirst, kPair, kPrefix };
-enum EntryKind { kEntryTile, kEntryEnd, kEntryStop };
+// What an entry says.  The first two words are all that a tile needs (one 8-byte load): flags and the tile's first key;
+// the others describe the item and are read where it starts and ends.
+enum EntryWord { kFlags, kTile0, kSeq, kHead, kTok0, kRows, kNew, kPart, kPrefix };
+enum EntryFlags { kTileOf0 = 1, kTileOf1 = 2, kEnd = 4, kStop = 8, kFirst = 16, kSlot0 = 32, kSlot1 = 64, kHasQ = 128 };
 
-struct ChunkSmem { uint32_t q, meta, entries, ml, bars, misc, total; };
+struct ChunkSmem { uint32_t q, meta, entries, pair, join, bars, misc, total; };
 template <int NH, bool kMeta>
 struct ChunkShape {
-    static constexpr int kStages = NH == 2 ? (kMeta ? 4 : 5) : 8;
+    static constexpr int kStages = NH == 2 ? 4 : 8;
     static constexpr uint32_t kStageBytes = NH * kBlockBytes;            // one tile of K or of V
     static constexpr uint32_t kQBytes = NH * kBlockBytes;                // one row tile of Q
-    static constexpr int kBars = 2 * kStages + 2 * kEntries + 4 + 6 + 2;
+    static constexpr int kBars = 2 * kStages + 2 * kEntries + 4 + 6 + 2 + 8;
     __host__ __device__ static constexpr ChunkSmem plan() {
         ChunkSmem s = {};
         uint32_t off = uint32_t(kStages) * kStageBytes;
         s.q = off;       off += 2 * kQBytes;
         s.meta = off;    off += kMeta ? kEntries * 1024 : 0;             // [entry][128] positions, then documents
         s.entries = off; off += kEntries * kEntryWords * 4;
-        s.ml = off;      off += 2 * 128 * 4;                             // one value per row and group, exchanged twice
+        s.pair = off;    off += 2 * 4 * 128 * 4;                         // [parity][group][half][row]: exchanged by the halves of a row
+        s.join = off;    off += 2 * 2 * 128 * 4;                         // [group][row] reference, then sum
         s.bars = off;    off += kBars * 8;
         s.misc = off;    off += 16;
         s.total = off;
@@ -71,7 +73,7 @@ template <int NH, bool kCap, bool kBias, bool kDoc>
 __global__ void __launch_bounds__(kChThreads, 1)
 chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                   const __grid_constant__ CUtensorMap tmap_v, const ChunkArgs a, const ChunkPlan pl,
-                  float* const partial, float2* const partial_ml) {
+                  ChunkParts* const parts, float* const partial, float2* const partial_ml) {
     constexpr int D = 64 * NH;
     constexpr bool kMeta = kBias || kDoc;
     using Shape = ChunkShape<NH, kMeta>;
@@ -86,12 +88,14 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
     constexpr ChunkSmem sp = Shape::plan();
     int32_t* const entries = reinterpret_cast<int32_t*>(base_ptr + sp.entries);
-    float* const ml = reinterpret_cast<float*>(base_ptr + sp.ml);
+    float* const pair_buf = reinterpret_cast<float*>(base_ptr + sp.pair);
+    float* const join_buf = reinterpret_cast<float*>(base_ptr + sp.join);
     const uint32_t kv_full = base + sp.bars, kv_empty = kv_full + 8 * NST;
     const uint32_t ent_full = kv_empty + 8 * NST, ent_empty = ent_full + 8 * kEntries;
     const uint32_t q_full = ent_empty + 8 * kEntries, q_empty = q_full + 16;      // [2] each
-    const uint32_t s_full = q_empty + 16, p_full = s_full + 16, pv_done = p_full + 16;   // [2] each
-    const uint32_t join_bar = pv_done + 16, drain_bar = join_bar + 8;
+    const uint32_t s_full = q_empty + 16, pv_done = s_full + 16, p_full = pv_done + 16;   // [2] each
+    const uint32_t join_bar = p_full + 16, drain_bar = join_bar + 8;
+    const uint32_t pair_bar = drain_bar + 8;                                      // [2][4]: the two warps of a lane quarter
     volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + sp.misc);
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(base_ptr + sp.misc + 4);
 
@@ -102,7 +106,9 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         for (int e = 0; e < kEntries; ++e) { mbar_init(ent_full + 8 * e, 1); mbar_init(ent_empty + 8 * e, kSoftmaxWarps + 1); }
         for (int g = 0; g < 2; ++g) {
             mbar_init(q_full + 8 * g, 1); mbar_init(q_empty + 8 * g, 1);
-            mbar_init(s_full + 8 * g, 1); mbar_init(p_full + 8 * g, kGroupWarps); mbar_init(pv_done + 8 * g, 1);
+            mbar_init(s_full + 8 * g, 1); mbar_init(pv_done + 8 * g, 1);
+            mbar_init(p_full + 8 * g, kGroupWarps);
+            for (int q = 0; q < 4; ++q) mbar_init(pair_bar + 32 * g + 8 * q, 2);
         }
         mbar_init(join_bar, kSoftmaxWarps);
         mbar_init(drain_bar, 1);
@@ -114,9 +120,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         tmem_relinquish();
     }
     tc_fence_before();
-    __syncthreads();
+    Share share = find_share<kChThreads>(a, pl, reinterpret_cast<int*>(base_ptr + sp.pair));      // (synchronises)
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    asm volatile("griddepcontrol.launch_dependents;");   // the joining kernel may get ready
     const uint32_t tmem_o[2] = {tmem, tmem + 128u}, tmem_s[2] = {tmem + 256u, tmem + 384u};
 
     if (warp >= kSoftmaxWarps) {
@@ -127,7 +134,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         bool ok = true;
         auto publish = [&](int32_t word) {               // lane l < kEntryWords brings word l
             const uint32_t e = n_entry % kEntries;
-            ok = ok && warp_wait(ent_empty + 8 * e, ((n_entry / kEntries) & 1u) ^ 1u, abort_flag);
+            warp_wait(ent_empty + 8 * e, ((n_entry / kEntries) & 1u) ^ 1u, abort_flag);
+            ok = ok && !warp_aborted(abort_flag);
             if (lane < kEntryWords) entries[e * kEntryWords + lane] = word;
             return e;
         };
@@ -136,23 +144,43 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             if (ok && lane == 0) mbar_arrive(ent_full + 8 * e);
             ++n_entry;
         };
+        if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, -1, 0, 0};
+        // Documents make the weight of an item unknown (tiles without any of its documents are skipped): where every block
+        // has several items anyway, they are drawn whole, one after the other.
+        const bool drawn = kDoc && pl.n_items >= 2 * pl.grid;
         ItemDraw draw;
-        draw.init(lane, a.status, pl.n_items);
-        int w = blockIdx.x;
-        while (ok && w < pl.n_items) {
-            const int w_now = w;
-            w = draw.next(lane);
-            const int split = w_now % pl.splits, up = w_now / pl.splits, pair = up % pl.n_pairs, u = up / pl.n_pairs;
-            const int b = u / a.n_kv_heads, h = u % a.n_kv_heads;
-            const PairRange x = pair_range(a, pl, u, pair);
-            if (pair == 0 && split == 0 && lane == 0) {
-                const int rows = a.n_rows[u], more = a.n_new ? a.n_new[b] : a.max_new;
-                if (rows != x.rows || more != x.n_new || x.n_new > x.rows) atomicOr(a.status, CSP_DEV_BAD_LEN);
+        if (drawn) share = Share{-1, 0, pl.n_items, 0};
+        const uint32_t tiles_per_page = uint32_t(a.page_rows) / uint32_t(kTileKeys);      // (dense: not used)
+        auto page_of = [&](int b, int tile) {            // the page of a tile that lies inside the cache
+            return a.page_table[int64_t(b) * a.max_pages + uint32_t(tile) / tiles_per_page];
+        };
+        PairRange next = {};
+        int next_page = 0;                               // lane l: page of the next item's tile l (of its first 32)
+        auto look_up = [&](int item) {
+            if (item > share.item1 || item >= pl.n_items) return;
+            const int u = item / pl.n_pairs;
+            next = pair_range(a, pl, u, item - u * pl.n_pairs);
+            const int tile = (item == share.item0 ? share.tile0 : 0) + lane;
+            if (a.page_table && next.count > 0 && tile < next.tiles) next_page = page_of(u / a.n_kv_heads, tile);
+        };
+        if (drawn) draw.init(lane, a.status, pl.n_items);
+        int item = drawn ? int(blockIdx.x) : share.item0, coming = 0;
+        look_up(item);
+        for (; ok && item <= share.item1 && item < pl.n_items; item = coming) {
+            coming = drawn ? draw.next(lane) : item + 1;
+            const int u = item / pl.n_pairs, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
+            const PairRange x = next;
+            int pages = next_page;                       // lane l: the page of tile 32 j + l
+            const int tile0 = item == share.item0 ? share.tile0 : 0, tile1 = item == share.item1 ? share.tile1 : x.tiles;
+            if (x.count <= 0 || (item == share.item1 && tile1 == 0)) { look_up(coming); continue; }
+            // which partial result the item goes to: none (the item is whole), the one that goes on, the one that begins
+            const int part = tile0 > 0 ? 2 * int(blockIdx.x) : tile1 < x.tiles ? 2 * int(blockIdx.x) + 1 : -1;
+            if (lane == 0 && part >= 0) {
+                if (tile0 > 0) { parts[blockIdx.x].more = item; parts[blockIdx.x].last = tile1 == x.tiles; }
+                else parts[blockIdx.x].first = item;
             }
-            if (x.count <= 0 || split >= x.active) continue;
             const bool big = x.count > pl.tok_tile;      // more than one row tile
-            const int tile0 = split * x.per_split, tile1 = min(x.tiles, tile0 + x.per_split);
-            const int q_slots = big ? 3 : 1 << (n_small++ & 1u);     // which of the two Q slots: slot g for group g, or one for both
+            const int q_slots = big ? kSlot0 | kSlot1 : n_small++ & 1u ? kSlot1 : kSlot0;   // slot g for group g, or one for both
             const int32_t* const docs = kDoc ? a.mods.documents + int64_t(b) * a.mods.doc_sb + int64_t(h) * a.mods.doc_sh : nullptr;
             const int32_t* const poss = kBias && a.mods.positions ? a.mods.positions + int64_t(b) * a.mods.pos_sb + int64_t(h) * a.mods.pos_sh : nullptr;
             // positions are staged relative to the last token's, so that near ones are exact in fp32
@@ -179,11 +207,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 case kTok0: word = x.tok0; break;
                 case kRows: word = x.rows; break;
                 case kNew: word = x.n_new; break;
-                case kSplit: word = split; break;
-                case kActive: word = x.active; break;
-                case kQSlots: word = q_slots; break;
-                case kFirst: word = 1; break;
-                case kPair: word = pair; break;
+                case kPart: word = part; break;
+                case kFlags: word = kFirst | q_slots; break;
                 case kPrefix: word = x.prefix; break;
             }
             int n_done = 0;
@@ -192,8 +217,9 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 q_loaded = true;
 #pragma unroll
                 for (int slot = 0; slot < 2; ++slot) {
-                    if (!(q_slots >> slot & 1)) continue;
-                    ok = ok && warp_wait(q_empty + 8 * slot, (q_uses[slot] & 1u) ^ 1u, abort_flag);
+                    if (!(q_slots & kSlot0 << slot)) continue;
+                    warp_wait(q_empty + 8 * slot, (q_uses[slot] & 1u) ^ 1u, abort_flag);
+                    ok = ok && !warp_aborted(abort_flag);
                     ++q_uses[slot];
                     if (ok && lane == 0) {
                         mbar_expect_tx(q_full + 8 * slot, uint32_t(NH * a.group * min(pl.tok_tile, a.max_new)) * 128u);
@@ -204,7 +230,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     }
                 }
             };
-            int pages = 0;                               // lane l: the page of tile 32 j + l
             int d_next[4] = {0, 0, 0, 0}, p_next[4] = {0, 0, 0, 0};
             auto fetch_meta = [&](int tile) {            // documents and positions of one tile's keys, a tile ahead of their use
 #pragma unroll
@@ -216,12 +241,14 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 }
             };
             if (kMeta && tile0 < tile1) fetch_meta(tile0);
+            bool q_free = tile0 < tile1 && !kDoc;        // (with documents it is not known yet whether Q is needed at all)
+#pragma unroll
+            for (int slot = 0; slot < 2; ++slot)
+                if (q_slots & kSlot0 << slot) q_free = q_free && mbar_test(q_empty + 8 * slot, (q_uses[slot] & 1u) ^ 1u);
+            if (__all_sync(0xffffffffu, q_free)) load_q();
             for (int tile = tile0; tile < tile1 && ok; ++tile) {
                 const int t0 = tile * kTileKeys;
-                if (a.page_table && ((tile - tile0) & 31) == 0) {
-                    const int mine = tile + lane;
-                    pages = mine < tile1 ? a.page_table[int64_t(b) * a.max_pages + int64_t(mine) * kTileKeys / a.page_rows] : 0;
-                }
+                if (a.page_table && tile > tile0 && ((tile - tile0) & 31) == 0) pages = tile + lane < tile1 ? page_of(b, tile + lane) : 0;
                 int d_now[4], p_now[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) { d_now[j] = d_next[j]; p_now[j] = p_next[j]; }
@@ -242,8 +269,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 }
                 if (act == 0) continue;
                 if (!big) act = 1 << (n_done & 1);       // the groups take turns
-                const uint32_t e = publish(lane == kTile0 ? t0 : lane == kAct ? act : lane == kKind ? int(kEntryTile) : word);
-                if (lane == kFirst) word = 0;
+                const uint32_t e = publish(lane == kTile0 ? t0 : lane == kFlags ? word | act : word);
+                if (lane == kFlags) word &= ~kFirst;
                 if (kMeta) {
                     float* const mp = reinterpret_cast<float*>(base_ptr + sp.meta + e * 1024);
                     int32_t* const md = reinterpret_cast<int32_t*>(base_ptr + sp.meta + e * 1024 + 512);
@@ -262,12 +289,13 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                         if (lane == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
                         outer = a.n_pages;
                     }
-                    row = t0 % a.page_rows;
+                    row = int(uint32_t(tile) % tiles_per_page) * kTileKeys;
                 }
 #pragma unroll
                 for (int which = 0; which < 2; ++which, ++n_stage) {
                     const uint32_t s = n_stage % NST;
-                    ok = ok && warp_wait(kv_empty + 8 * s, ((n_stage / NST) & 1u) ^ 1u, abort_flag);
+                    warp_wait(kv_empty + 8 * s, ((n_stage / NST) & 1u) ^ 1u, abort_flag);
+                    ok = ok && !warp_aborted(abort_flag);
                     if (ok && lane == 0) {
                         mbar_expect_tx(kv_full + 8 * s, kStageBytes);
 #pragma unroll
@@ -276,13 +304,15 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                                         row, h, outer);
                     }
                 }
-                // Q goes behind the first two tiles (which need no more than four stages): its slot may still be in use
-                if (++n_done == 2) load_q();
+                // Q goes behind the first two tiles (which need no more than four stages) if its slot is still in use
+                if (++n_done == 1) look_up(coming);
+                if (n_done == 2 && !q_loaded) load_q();
             }
-            if (n_done == 1) load_q();
-            announce(publish(lane == kKind ? int(kEntryEnd) : lane == kAct ? (q_loaded ? 1 : 0) : word));
+            if (n_done == 1 && !q_loaded) load_q();
+            if (n_done == 0) look_up(coming);
+            announce(publish(lane == kFlags ? word | kEnd | (q_loaded ? kHasQ : 0) : word));
         }
-        if (ok) announce(publish(lane == kKind ? int(kEntryStop) : 0));
+        if (ok) announce(publish(lane == kFlags ? kStop : 0));
         if (lane == 0) {
             if (!ok) {
                 // let copies that were issued land before the CTA's shared memory is given up
@@ -292,84 +322,95 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 }
                 atomicOr(a.status, CSP_DEV_TIMEOUT);
             }
-            draw.done();
+            if (drawn) draw.done();
         }
         __syncwarp();
     } else if (warp == kChMmaWarp) {
         // =============================== MMA issuer ===============================
-        if (lane == 0) {
-            uint32_t n_entry = 0, q_uses[2] = {0, 0}, n_p[2] = {0, 0};
-            int n_tile = 0, pend[2] = {-1, -1};          // tiles so far; tile whose P V product a group still owes
-            bool started[2] = {false, false};            // the group has a product in this item (O holds something)
-            bool ok = true;
-            auto product = [&](int g) {                  // O_g += P_g V of the owed tile
-                const uint32_t n = 2u * uint32_t(pend[g]) + 1u, s = n % NST;
-                ok = ok && mbar_wait(p_full + 8 * g, n_p[g] & 1u, abort_flag) && mbar_wait(kv_full + 8 * s, (n / NST) & 1u, abort_flag);
-                ++n_p[g];
-                if (!ok) return;
-                tc_fence_after();
+        // The whole warp walks the entries, so that everything is uniform; one elected lane issues.  (With the loop inside
+        // `lane == 0` every descriptor went through vector registers: issuing took 140 clocks per instruction, twice
+        // what the tensor core needs to execute it.)
+        uint32_t n_entry = 0, q_uses[2] = {0, 0}, n_p[2] = {0, 0};
+        int n_tile = 0, pend[2] = {-1, -1}, v_here = -1; // tiles so far; tile whose P V product a group still owes; last tile of V seen
+        bool started[2] = {false, false};                // the group has a product in this item (O holds something)
+        auto product = [&](int g) {                      // O_g += P_g V of the owed tile
+            const uint32_t n = 2u * uint32_t(pend[g]) + 1u, s = n % NST;
+            if (v_here != pend[g]) { warp_wait(kv_full + 8 * s, (n / NST) & 1u, abort_flag); v_here = pend[g]; }
+            const uint64_t vd = sw128_desc_mn(base + s * kStageBytes, kBlockBytes);
+            warp_wait(p_full + 8 * g, n_p[g] & 1u, abort_flag);
+            tc_fence_after();
+            if (elect_one()) {
 #pragma unroll
                 for (int k = 0; k < kTileKeys / 16; ++k)
-                    tc_mma_bf16_ts(tmem_o[g], tmem_s[g] + 8u * k, sw128_desc_mn(base + s * kStageBytes + 2048u * k, kBlockBytes), kIdescO,
-                                   (k > 0 || started[g]) ? 1u : 0u);
-                started[g] = true;
+                    tc_mma_bf16_ts(tmem_o[g], tmem_s[g] + 8u * (k & 3) + 64u * (k >> 2), vd + uint64_t(k * (2048 >> 4)), kIdescO, (k > 0 || started[g]) ? 1u : 0u);
                 tc_commit(pv_done + 8 * g);
-                if (pend[g ^ 1] != pend[g]) tc_commit(kv_empty + 8 * s);     // nobody else waits for this tile of V
-                pend[g] = -1;
-            };
-            while (ok) {
-                const uint32_t e = n_entry % kEntries;
-                ok = mbar_wait(ent_full + 8 * e, (n_entry / kEntries) & 1u, abort_flag);
-                if (!ok) break;
-                const volatile int32_t* const en = entries + e * kEntryWords;
-                const int kind = en[kKind], act = en[kAct], q_slots = en[kQSlots], first = en[kFirst];
-                mbar_arrive(ent_empty + 8 * e);
-                ++n_entry;
-                if (kind == kEntryStop) break;
-                if (kind == kEntryTile) {
-                    if (first) {
-                        started[0] = started[1] = false;
+                if (pend[g ^ 1] != pend[g]) tc_commit(kv_empty + 8 * s);         // nobody else waits for this tile of V
+            }
+            __syncwarp();
+            ++n_p[g];
+            started[g] = true;
+            pend[g] = -1;
+        };
+        for (;;) {
+            const uint32_t e = n_entry % kEntries;
+            warp_wait(ent_full + 8 * e, (n_entry / kEntries) & 1u, abort_flag);
+            if (warp_aborted(abort_flag)) break;
+            const int flags = entries[e * kEntryWords + kFlags];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ent_empty + 8 * e);
+            ++n_entry;
+            if (flags & kStop) break;
+            if (!(flags & kEnd)) {
+                if (flags & kFirst) {
+                    started[0] = started[1] = false;
 #pragma unroll
-                        for (int slot = 0; slot < 2; ++slot) {
-                            if (!(q_slots >> slot & 1)) continue;
-                            ok = ok && mbar_wait(q_full + 8 * slot, q_uses[slot] & 1u, abort_flag);
-                            ++q_uses[slot];
-                        }
+                    for (int slot = 0; slot < 2; ++slot) {
+                        if (!(flags & kSlot0 << slot)) continue;
+                        warp_wait(q_full + 8 * slot, q_uses[slot] & 1u, abort_flag);
+                        ++q_uses[slot];
                     }
-                    const uint32_t n = 2u * uint32_t(n_tile), s = n % NST;
-                    ok = ok && mbar_wait(kv_full + 8 * s, (n / NST) & 1u, abort_flag);
-                    if (!ok) break;
+                }
+                const uint32_t n = 2u * uint32_t(n_tile), s = n % NST;
+                warp_wait(kv_full + 8 * s, (n / NST) & 1u, abort_flag);
+                const uint64_t kd = sw128_desc(base + s * kStageBytes);
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        if (!(act >> g & 1)) continue;
-                        if (pend[g] >= 0) product(g);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t q_s = base + sp.q + uint32_t(q_slots == 3 ? g : q_slots >> 1) * Shape::kQBytes;
+                for (int g = 0; g < 2; ++g) {
+                    if (!(flags & kTileOf0 << g)) continue;
+                    if (pend[g] >= 0) product(g);
+                    tc_fence_after();
+                    const uint64_t qd = sw128_desc(base + sp.q + ((flags & kSlot1) && (g == 1 || !(flags & kSlot0)) ? Shape::kQBytes : 0u));
+                    if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k) {
-                            const uint32_t off = uint32_t(k >> 2) * kBlockBytes + uint32_t(k & 3) * 32u;
-                            tc_mma_bf16(tmem_s[g], sw128_desc(q_s + off), sw128_desc(base + s * kStageBytes + off), kIdescS, k > 0 ? 1u : 0u);
+                            constexpr int kColumnStep = 32 >> 4, kBlockStep = kBlockBytes >> 4;
+                            const uint64_t off = uint64_t((k >> 2) * kBlockStep + (k & 3) * kColumnStep);
+                            tc_mma_bf16(tmem_s[g], qd + off, kd + off, kIdescS, k > 0 ? 1u : 0u);
                         }
                         tc_commit(s_full + 8 * g);
-                        pend[g] = n_tile;
+                        if (g == 1 || !(flags & kTileOf1)) tc_commit(kv_empty + 8 * s);
                     }
-                    tc_commit(kv_empty + 8 * s);
-                    // a group that sits this tile out pays what it owes now: its tile of V must not hold up the ring
+                    __syncwarp();
+                    pend[g] = n_tile;
+                }
+                // a group that sits this tile out pays what it owes now: its tile of V must not hold up the ring
 #pragma unroll
-                    for (int g = 0; g < 2; ++g)
-                        if (!(act >> g & 1) && pend[g] >= 0) product(g);
-                    ++n_tile;
-                } else {
+                for (int g = 0; g < 2; ++g)
+                    if (!(flags & kTileOf0 << g) && pend[g] >= 0) product(g);
+                ++n_tile;
+            } else {
 #pragma unroll
-                    for (int g = 0; g < 2; ++g)
-                        if (pend[g] >= 0) product(g);
+                for (int g = 0; g < 2; ++g)
+                    if (pend[g] >= 0) product(g);
+                if (elect_one()) {
 #pragma unroll
                     for (int slot = 0; slot < 2; ++slot)
-                        if (act && (q_slots >> slot & 1)) tc_commit(q_empty + 8 * slot);
+                        if ((flags & kHasQ) && (flags & kSlot0 << slot)) tc_commit(q_empty + 8 * slot);
                 }
+                __syncwarp();
             }
-            // nothing may be in flight when the tensor memory goes back
+        }
+        // nothing may be in flight when the tensor memory goes back
+        if (elect_one()) {
             tc_commit(drain_bar);
             const unsigned long long t0 = global_ns();
             while (!mbar_try_wait(drain_bar, 0) && global_ns() - t0 < kWaitLimitNs / 8) {}
@@ -379,31 +420,50 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     } else {
         // =============================== softmax groups ===============================
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        const int g = warp / kGroupWarps, m = tid & 127, G = a.group;
+        const int g = warp / kGroupWarps, half = (warp >> 2) & 1, m = (warp & 3) * 32 + lane, G = a.group;
         const uint32_t lane_base = uint32_t((warp & 3) * 32) << 16;
-        const uint32_t my_s = tmem_s[g] + lane_base, my_o = tmem_o[g] + lane_base;
+        // this thread's 64 columns of its row of S; its 64 weights go over the first half of them
+        const uint32_t my_s = tmem_s[g] + lane_base + 64u * half;
         const float scale2 = a.scale * kLog2e;
         // capped: x = c tanh(o / c) = c - 2 c / (1 + e^{2 o / c}), all in the base-2 domain
         const float cap2 = kCap ? a.mods.softcap * kLog2e : 0.f, cap_in = kCap ? 2.f * kLog2e * a.scale / a.mods.softcap : 0.f;
-        uint32_t n_entry = 0, n_tile = 0, n_mine = 0, n_join = 0;
+        uint32_t n_entry = 0, n_tile = 0, n_mine = 0, n_join = 0, n_pair = 0;
         float m_run = kNeg, l_run = 0.f;
-        int lim = -1, q_doc = 0, in_item = 0;
+        int lim = -1, q_doc = 0, rows = 0;
         float q_pos = 0.f, slope2 = 0.f;
-        bool valid = false, live = false;
-        int tok = 0, head = 0;
+        bool valid = false, live = false, started = false;     // started: the group has a tile in this item
+        // what the other half of this row says
+        auto other_half = [&](float mine) {
+            float* const box = pair_buf + ((n_pair & 1u) * 4 + g * 2) * 128 + m;
+            const uint32_t bar = pair_bar + 32 * g + 8 * (warp & 3);
+            box[half * 128] = mine;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+            warp_wait(bar, n_pair & 1u, abort_flag);
+            ++n_pair;
+            return box[(half ^ 1) * 128];
+        };
+        auto join = [&] {                                // all warps of both groups
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(join_bar);
+            warp_wait(join_bar, n_join++ & 1u, abort_flag);
+            tc_fence_after();
+        };
         for (;;) {
             const uint32_t e = n_entry % kEntries;
-            if (!warp_wait(ent_full + 8 * e, (n_entry / kEntries) & 1u, abort_flag)) break;
+            warp_wait(ent_full + 8 * e, (n_entry / kEntries) & 1u, abort_flag);
+            if (warp_aborted(abort_flag)) break;
             const int32_t* const en = entries + e * kEntryWords;
-            const int kind = en[kKind];
-            if (kind == kEntryStop) break;
-            const int t0 = en[kTile0], act = en[kAct], rows = en[kRows], q_slots = en[kQSlots], b = en[kSeq], h = en[kHead];
-            const bool big = q_slots == 3;
-            if (en[kFirst]) {
+            const int2 head_words = *reinterpret_cast<const int2*>(en);
+            const int flags = head_words.x, t0 = head_words.y;
+            if (flags & kStop) break;
+            if (flags & kFirst) {
                 // this thread's query row: token m / G of its row tile, head m % G
-                const int n_new = en[kNew], local = m / G;
-                head = h * G + m - local * G;
-                tok = en[kTok0] + (big ? g * pl.tok_tile : 0) + local;
+                const int n_new = en[kNew], local = m / G, b = en[kSeq], h = en[kHead];
+                const bool big = (flags & kSlot0) && (flags & kSlot1);
+                rows = en[kRows];
+                const int head = h * G + m - local * G, tok = en[kTok0] + (big ? g * pl.tok_tile : 0) + local;
                 valid = local < pl.tok_tile && tok < n_new;
                 const int r = rows - n_new + tok;
                 const bool sees = valid && r >= 0;
@@ -412,7 +472,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 live = __any_sync(0xffffffffu, valid);
                 m_run = kNeg;
                 l_run = 0.f;
-                in_item = 0;
+                started = false;
                 if (kDoc) q_doc = sees ? a.mods.documents[int64_t(b) * a.mods.doc_sb + int64_t(h) * a.mods.doc_sh + r] : 0;
                 if (kBias) {
                     const int32_t* const poss = a.mods.positions ? a.mods.positions + int64_t(b) * a.mods.pos_sb + int64_t(h) * a.mods.pos_sh : nullptr;
@@ -422,84 +482,98 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     slope2 = sees ? a.mods.slopes[head] * kLog2e : 0.f;
                 }
             }
-            if (kind == kEntryTile) {
+            if (!(flags & kEnd)) {
                 const uint32_t v_stage = 2u * n_tile + 1u;
                 ++n_tile;
-                if (!(act >> g & 1)) {
+                ++n_entry;
+                if (!(flags & kTileOf0 << g)) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(ent_empty + 8 * e);
-                    ++n_entry;
                     continue;
                 }
                 if (t0 + kTileKeys > rows) {
                     // Rows past the end hold whatever the cache holds: their weights are zero, but zero times a non-finite
                     // value is not, so clear these rows of V.  (Both groups may do it: they write the same zeros.)
                     const uint32_t s = v_stage % NST;
-                    if (!warp_wait(kv_full + 8 * s, (v_stage / NST) & 1u, abort_flag)) break;
-                    for (int j = m; j < (kTileKeys - (rows - t0)) * NH * 8; j += 128) {
+                    warp_wait(kv_full + 8 * s, (v_stage / NST) & 1u, abort_flag);
+                    for (int j = tid % (32 * kGroupWarps); j < (kTileKeys - (rows - t0)) * NH * 8; j += 32 * kGroupWarps) {
                         const int r = rows - t0 + j / (NH * 8), c = j % (NH * 8);
                         *reinterpret_cast<uint4*>(base_ptr + s * kStageBytes + (c >> 3) * kBlockBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
                             make_uint4(0, 0, 0, 0);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
-                if (!warp_wait(s_full + 8 * g, n_mine & 1u, abort_flag)) break;
+                warp_wait(s_full + 8 * g, n_mine & 1u, abort_flag);
                 tc_fence_after();
                 if (live) {
-                    uint32_t v[4][32];
+                    constexpr bool kScaled = kCap || kBias;           // the logits are scaled before the maximum is known
+                    const bool masked = __any_sync(0xffffffffu, t0 + kTileKeys - 1 > lim);
+                    float mx = -INFINITY;
+                    // First pass over the row, 32 columns at a time: modifiers, mask and maximum.  What was changed goes back to
+                    // tensor memory; holding the row instead would take the registers that two warps per quarter need.
+#pragma unroll 1
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t v[32];
+                        tc_ld_row32(v, my_s + 32u * j);
+                        tc_wait_ld();
+                        tc_loaded(v);
+                        if (kScaled) {
+                            const float4* const mp = reinterpret_cast<const float4*>(base_ptr + sp.meta + e * 1024 + 256 * half) + 8 * j;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) tc_ld_row32(v[j], my_s + 32u * j);
-                    tc_wait_ld();
-                    constexpr bool kScaled = kCap || kBias;           // v holds base-2 logits rather than raw products
-                    if (kScaled) {
-                        const float4* const mp = reinterpret_cast<const float4*>(base_ptr + sp.meta + e * 1024);
+                            for (int c = 0; c < 32; c += 4) {
+                                float4 pos = make_float4(0.f, 0.f, 0.f, 0.f);
+                                if (kBias) pos = mp[c >> 2];
+                                const float pp[4] = {pos.x, pos.y, pos.z, pos.w};
 #pragma unroll
-                        for (int c = 0; c < 128; c += 4) {
-                            float4 pos = make_float4(0.f, 0.f, 0.f, 0.f);
-                            if (kBias) pos = mp[c >> 2];
-                            const float pp[4] = {pos.x, pos.y, pos.z, pos.w};
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                uint32_t& r = v[c >> 5][(c & 31) + j];
-                                float s = __uint_as_float(r);
-                                s = kCap ? fmaf(-2.f * cap2, rcpf(1.f + ex2f(s * cap_in)), cap2) : s * scale2;
-                                if (kBias) s = fmaf(-slope2, fabsf(q_pos - pp[j]), s);
-                                r = __float_as_uint(s);
+                                for (int k = 0; k < 4; ++k) {
+                                    float x = __uint_as_float(v[c + k]);
+                                    x = kCap ? fmaf(-2.f * cap2, rcpf(1.f + ex2f(x * cap_in)), cap2) : x * scale2;
+                                    if (kBias) x = fmaf(-slope2, fabsf(q_pos - pp[k]), x);
+                                    v[c + k] = __float_as_uint(x);
+                                }
                             }
                         }
-                    }
-                    if (kDoc) {
-                        const int4* const md = reinterpret_cast<const int4*>(base_ptr + sp.meta + e * 1024 + 512);
+                        if (kDoc) {
+                            const int4* const md = reinterpret_cast<const int4*>(base_ptr + sp.meta + e * 1024 + 512 + 256 * half) + 8 * j;
 #pragma unroll
-                        for (int c = 0; c < 128; c += 4) {
-                            const int4 d4 = md[c >> 2];
-                            const int dd[4] = {d4.x, d4.y, d4.z, d4.w};
+                            for (int c = 0; c < 32; c += 4) {
+                                const int4 d4 = md[c >> 2];
+                                const int dd[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                if (dd[j] != q_doc) v[c >> 5][(c & 31) + j] = __float_as_uint(-INFINITY);
+                                for (int k = 0; k < 4; ++k)
+                                    if (dd[k] != q_doc) v[c + k] = __float_as_uint(-INFINITY);
+                            }
                         }
+                        if (masked) {
+                            const int n_see = lim - t0 + 1 - 64 * half - 32 * j;      // columns c < n_see are visible
+#pragma unroll
+                            for (int c = 0; c < 32; ++c)
+                                if (c >= n_see) v[c] = __float_as_uint(-INFINITY);
+                        }
+                        if (kScaled || kDoc || masked) tc_st_row32(my_s + 32u * j, v);
+                        float m4[4] = {mx, -INFINITY, -INFINITY, -INFINITY};          // four chains: the latency of one would show
+#pragma unroll
+                        for (int c = 0; c < 32; c += 8)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                m4[k] = fmax3_nan(m4[k], __uint_as_float(v[c + 2 * k]), __uint_as_float(v[c + 2 * k + 1]));
+                        mx = fmax3_nan(fmax3_nan(m4[0], m4[1], m4[2]), m4[3], m4[3]);
                     }
-                    if (__any_sync(0xffffffffu, t0 + kTileKeys - 1 > lim)) {
-                        const int n_see = lim - t0 + 1;               // columns c < n_see are visible
-#pragma unroll
-                        for (int c = 0; c < 128; ++c)
-                            if (c >= n_see) v[c >> 5][c & 31] = __float_as_uint(-INFINITY);
-                    }
-                    float mx = -INFINITY;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int c = 0; c < 32; c += 2) mx = fmax3(mx, __uint_as_float(v[j][c]), __uint_as_float(v[j][c + 1]));
+                    if (kScaled || kDoc || masked) tc_wait_st();
                     if (!kScaled) mx *= scale2;
-                    const bool raise = mx > m_run + (in_item ? kLazy : 0.f);
+                    const float mx_other = other_half(mx);
+                    mx = fmax3_nan(mx, mx_other, mx_other);
+                    // (a NaN among the logits raises the reference to NaN, and the whole row with it)
+                    const bool raise = valid && !(mx <= m_run + (started ? kLazy : 0.f));
                     if (__any_sync(0xffffffffu, raise)) {
                         const float m_new = raise ? mx : m_run, alpha = ex2f(m_run - m_new);
-                        if (in_item) {
-                            // O holds products with weights relative to the old reference
-                            if (!warp_wait(pv_done + 8 * g, (n_mine - 1u) & 1u, abort_flag)) break;
+                        if (started) {
+                            // O holds products with weights relative to the old reference; each half rescales half of the row
+                            const uint32_t my_o = tmem_o[g] + lane_base + uint32_t(half * (D / 2));
+                            warp_wait(pv_done + 8 * g, (n_mine - 1u) & 1u, abort_flag);
                             tc_fence_after();
-#pragma unroll
-                            for (int c = 0; c < D; c += 16) {         // sixteen at a time: the row of S is held meanwhile
+#pragma unroll 1
+                            for (int c = 0; c < D / 2; c += 16) {     
                                 uint32_t o[16];
                                 tc_ld_row16(o, my_o + c);
                                 tc_wait_ld();
@@ -512,80 +586,72 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                         m_run = m_new;
                     }
                     const float ref = m_run == kNeg ? 0.f : m_run;    // a row that has seen nothing yet: all weights zero
-                    const float2 neg = make_float2(-ref, -ref), sc = kScaled ? make_float2(1.f, 1.f) : make_float2(scale2, scale2);
-                    float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t pk[16];
+                    const float2 neg = make_float2(-ref, -ref), sc = make_float2(scale2, scale2);
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll 1
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t v[32], pk[16];
+                        tc_ld_row32(v, my_s + 32u * j);
+                        tc_wait_ld();
+                        tc_loaded(v);
 #pragma unroll
                         for (int c = 0; c < 32; c += 2) {
-                            const float2 x = make_float2(__uint_as_float(v[j][c]), __uint_as_float(v[j][c + 1]));
-                            const float2 p = ex2f2(kScaled ? __fadd2_rn(x, neg) : __ffma2_rn(x, sc, neg));
-                            sum = __fadd2_rn(sum, p);
+                            float2 x = make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+                            x = kScaled ? __fadd2_rn(x, neg) : __ffma2_rn(x, sc, neg);
+                            const float2 p = ex2f2(x);
+                            sum[c / 2 % 2] = __fadd2_rn(sum[c / 2 % 2], p);
                             pk[c >> 1] = pack_bf16(p.x, p.y);
                         }
                         tc_st_row16(my_s + 16u * j, pk);
                     }
-                    l_run += sum.x + sum.y;
+                    l_run += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     tc_wait_st();
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) { mbar_arrive(p_full + 8 * g); mbar_arrive(ent_empty + 8 * e); }
                 ++n_mine;
-                ++in_item;
-                ++n_entry;
+                started = true;
                 continue;
             }
             // ---------------------------------- end of the item ----------------------------------
-            const int split = en[kSplit], active = en[kActive], pair = en[kPair];
+            const int part_slot = en[kPart], b = en[kSeq], h = en[kHead], tok0 = en[kTok0];
+            const bool big = (flags & kSlot0) && (flags & kSlot1);
             __syncwarp();
             if (lane == 0) mbar_arrive(ent_empty + 8 * e);
             ++n_entry;
-            if (in_item) {
-                if (!warp_wait(pv_done + 8 * g, (n_mine - 1u) & 1u, abort_flag)) break;
-                tc_fence_after();
-            }
-            float m_all = m_run, l_all = l_run, w0 = in_item ? 1.f : 0.f, w1 = 0.f;
-            bool has0 = in_item > 0, has1 = false;
+            if (started) warp_wait(pv_done + 8 * g, (n_mine - 1u) & 1u, abort_flag);
+            tc_fence_after();
+            float l_all = l_run + other_half(l_run);
+            float m_all = m_run, w0 = 1.f, w1 = 0.f;
+            bool has0 = started, has1 = false;
             if (!big) {
-                // both groups hold part of the same rows: exchange reference and sum, then each writes half the columns
-                ml[g * 128 + m] = m_run;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(join_bar);
-                if (!warp_wait(join_bar, n_join++ & 1u, abort_flag)) break;
-                const float m_other = ml[(g ^ 1) * 128 + m];
-                m_all = fmaxf(m_run, m_other);
-                const float mine = ex2f(m_run - m_all);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(join_bar);
-                if (!warp_wait(join_bar, n_join++ & 1u, abort_flag)) break;
-                ml[g * 128 + m] = in_item ? l_run * mine : __uint_as_float(kUnset);     // the group had no tile: its O is not set
-                __syncwarp();
-                tc_fence_before();
-                if (lane == 0) mbar_arrive(join_bar);
-                if (!warp_wait(join_bar, n_join++ & 1u, abort_flag)) break;
-                tc_fence_after();
-                const float l0 = ml[m], l1 = ml[128 + m];
+                // both groups hold part of the same rows: exchange reference and sum, then each half row writes a quarter
+                if (half == 0) {
+                    join_buf[g * 128 + m] = m_run;
+                    join_buf[256 + g * 128 + m] = started ? l_all : __uint_as_float(kUnset);     // the group had no tile: its O is not set
+                }
+                join();
+                const float m0 = join_buf[m], m1 = join_buf[128 + m], l0 = join_buf[256 + m], l1 = join_buf[384 + m];
                 has0 = __float_as_uint(l0) != kUnset;
                 has1 = __float_as_uint(l1) != kUnset;
-                l_all = (has0 ? l0 : 0.f) + (has1 ? l1 : 0.f);
-                const float other = ex2f(m_other - m_all);
-                w0 = g == 0 ? mine : other;
-                w1 = g == 0 ? other : mine;
+                m_all = fmax3_nan(m0, m1, m1);
+                w0 = ex2f(m0 - m_all);
+                w1 = ex2f(m1 - m_all);
+                l_all = (has0 ? l0 * w0 : 0.f) + (has1 ? l1 * w1 : 0.f);
             }
             if (live) {
-                const bool final = active == 1;
+                const int local = m / G, head = h * G + m - local * G, tok = tok0 + (big ? g * pl.tok_tile : 0) + local;
+                const bool final = part_slot < 0;
                 const float denom = a.n * ex2f(-m_all) + l_all;
                 const float inv = final ? 1.f / denom : 1.f;
                 const uint32_t o0 = (big ? tmem_o[g] : tmem_o[0]) + lane_base, o1 = tmem_o[1] + lane_base;
                 uint16_t* const out = a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st;
-                const int64_t slot = (int64_t(b * a.n_kv_heads + h) * pl.n_pairs + pair) * pl.splits + split;
-                const int row = (tok - pair * 2 * pl.tok_tile) * G + (head - h * G);
-                float* const part = partial + (slot * pl.row_slots + row) * D;
+                const int row = (tok - tok0) * G + (head - h * G);
+                float* const part = partial + (int64_t(part_slot) * (D / 4) * pl.row_slots + row) * 4;
                 const bool zero = l_all == 0.f;          // saw nothing; a NaN among what it saw comes out as NaN
-                // a pair's columns all belong to its group; of shared rows each group writes half
-                const int c_begin = big ? 0 : g * (D / 2), c_end = big ? D : c_begin + D / 2;
+                // a row tile's columns are shared by the two halves, those of shared rows by both groups' halves
+                const int c_begin = big ? half * (D / 2) : (g * 2 + half) * (D / 4), c_end = c_begin + (big ? D / 2 : D / 4);
 #pragma unroll 1
                 for (int c = c_begin; c < c_end; c += 16) {
                     uint32_t x0[16], x1[16];
@@ -599,34 +665,30 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     }
                     if (!valid) continue;
                     if (final) {
+                        uint32_t y[8];
 #pragma unroll
-                        for (int j = 0; j < 16; j += 8) {
-                            uint4 y;
-                            y.x = pack_bf16(__uint_as_float(x0[j]), __uint_as_float(x0[j + 1]));
-                            y.y = pack_bf16(__uint_as_float(x0[j + 2]), __uint_as_float(x0[j + 3]));
-                            y.z = pack_bf16(__uint_as_float(x0[j + 4]), __uint_as_float(x0[j + 5]));
-                            y.w = pack_bf16(__uint_as_float(x0[j + 6]), __uint_as_float(x0[j + 7]));
-                            *reinterpret_cast<uint4*>(out + c + j) = y;
+                        for (int j = 0; j < 8; ++j) y[j] = pack_bf16(__uint_as_float(x0[2 * j]), __uint_as_float(x0[2 * j + 1]));
+                        if (a.out_wide) {
+                            st_global_32(out + c, y);
+                        } else {
+                            *reinterpret_cast<uint4*>(out + c) = make_uint4(y[0], y[1], y[2], y[3]);
+                            *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(y[4], y[5], y[6], y[7]);
                         }
                     } else {
+                        // four columns of neighbouring rows lie next to each other: a warp's store is one piece of 512 bytes
 #pragma unroll
                         for (int j = 0; j < 16; j += 4)
-                            *reinterpret_cast<uint4*>(part + c + j) = make_uint4(x0[j], x0[j + 1], x0[j + 2], x0[j + 3]);
+                            *reinterpret_cast<uint4*>(part + int64_t((c + j) / 4) * pl.row_slots * 4) = make_uint4(x0[j], x0[j + 1], x0[j + 2], x0[j + 3]);
                     }
                 }
-                if (valid && (big || g == 0)) {
-                    if (!final) partial_ml[slot * pl.row_slots + row] = make_float2(m_all, l_all);
+                if (valid && half == 0 && (big || g == 0)) {
+                    if (!final) partial_ml[int64_t(part_slot) * pl.row_slots + row] = make_float2(m_all, l_all);
                     else if (a.lse)
                         a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = zero ? -INFINITY : (m_all + log2f(l_all)) * kLn2;
                 }
             }
-            if (!big) {
-                // the other group has read this group's O, and the exchange area is free again
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(join_bar);
-                if (!warp_wait(join_bar, n_join++ & 1u, abort_flag)) break;
-            }
+            // the other group has read this group's O, and the exchange area is free again
+            if (!big) join();
         }
     }
 
@@ -638,68 +700,52 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     }
 }
 
-// out = sum_s O_s 2^(m_s - m) / (n 2^-m + sum_s l_s 2^(m_s - m)) over the parts of a split pair; one warp per query row
+// out = sum_s O_s 2^(m_s - m) / (n 2^-m + sum_s l_s 2^(m_s - m)) over the parts of a cut item; one warp per query row.  Block
+// (c, .) joins the item that begins in block c of the main kernel and goes on in c + 1, ... until one says it is the last.
+constexpr int kJoinWarps = 8;
 template <int D>
-__global__ void __launch_bounds__(256) chunk_merge_kernel(const ChunkArgs a, const ChunkPlan pl, const float* partial,
-                                                          const float2* partial_ml) {
-    constexpr int C = D / 32;                            // columns per lane
-    const int lane = threadIdx.x & 31, G = a.group;
-    const int64_t id = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    const int row = int(id % pl.row_slots);
-    const int64_t up = id / pl.row_slots;
-    const int pair = int(up % pl.n_pairs), u = int(up / pl.n_pairs);
-    if (u >= a.batch * a.n_kv_heads) return;
-    const int b = u / a.n_kv_heads, h = u % a.n_kv_heads;
-    const PairRange x = pair_range(a, pl, u, pair);
-    const int tok = x.tok0 + row / G, head = h * G + row % G;
-    if (x.active <= 1 || tok >= x.n_new) return;         // nothing was split; the item itself wrote the result
-    const int64_t slot0 = up * pl.splits;
+__global__ void __launch_bounds__(32 * kJoinWarps) chunk_join_kernel(const ChunkArgs a, const ChunkPlan pl, const ChunkParts* parts,
+                                                                     const float* partial, const float2* partial_ml) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // launched early: the main kernel has to be through
+    const int c0 = blockIdx.x, item = parts[c0].first;
+    if (item < 0) return;
+    const int lane = threadIdx.x & 31, G = a.group, row = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
+    const int u = item / pl.n_pairs, pair = item - u * pl.n_pairs, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
+    const int tok = pair * 2 * pl.tok_tile + row / G, head = h * G + row % G;
+    const int n_new = a.n_new ? min(max(a.n_new[b], 0), a.max_new) : a.max_new;
+    if (row >= pl.row_slots || tok >= n_new) return;
+    int n_parts = 1;
+    for (int c = c0 + 1; c < pl.grid; c += 32) {
+        const bool in = c + lane < pl.grid;
+        const uint32_t last = __ballot_sync(0xffffffffu, in && parts[c + lane].last);
+        if (last) { n_parts += __ffs(last); break; }
+        n_parts += 32;
+    }
+    n_parts = min(n_parts, pl.grid - c0);
+    auto slot = [&](int s) { return (int64_t(2 * (c0 + s)) + (s == 0 ? 1 : 0)) * pl.row_slots + row; };
     float m = kNeg;
-    for (int s = lane; s < x.active; s += 32) m = fmaxf(m, partial_ml[(slot0 + s) * pl.row_slots + row].x);
+    for (int s = lane; s < n_parts; s += 32) m = fmaxf(m, partial_ml[slot(s)].x);
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    float l = 0.f, o[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = 0.f;
+    float l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int chunk = lane % (D / 4);                    // (d = 64: the lanes' second half repeats the first's work)
 #pragma unroll 4
-    for (int s = 0; s < x.active; ++s) {
-        const float2 p = partial_ml[(slot0 + s) * pl.row_slots + row];
+    for (int s = 0; s < n_parts; ++s) {
+        const float2 p = partial_ml[slot(s)];
         const float w = ex2f(p.x - m);
-        const float* const src = partial + ((slot0 + s) * pl.row_slots + row) * D + lane * C;
-        float y[C];
-        if (C == 4) *reinterpret_cast<float4*>(y) = *reinterpret_cast<const float4*>(src);
-        else *reinterpret_cast<float2*>(y) = *reinterpret_cast<const float2*>(src);
+        const float4 y = *reinterpret_cast<const float4*>(partial + ((slot(s) - row) * (D / 4) + int64_t(chunk) * pl.row_slots + row) * 4);
         l += p.y * w;
-#pragma unroll
-        for (int c = 0; c < C; ++c) o[c] += y[c] * w;
+        o.x += y.x * w; o.y += y.y * w; o.z += y.z * w; o.w += y.w * w;
     }
     const float inv = l == 0.f ? 0.f : 1.f / (a.n * ex2f(-m) + l);
-    uint32_t* const out = reinterpret_cast<uint32_t*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st + lane * C);
-#pragma unroll
-    for (int c = 0; c < C; c += 2) out[c / 2] = pack_bf16(o[c] * inv, o[c + 1] * inv);
+    uint2* const out = reinterpret_cast<uint2*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st + chunk * 4);
+    if (lane < D / 4) *out = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
     if (a.lse && lane == 0)
         a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
-
-// How many parts the keys of a pair are divided into.  An estimate of the time in SM clocks, from the kernels' own
-// figures: a key tile, what an item costs besides, what the joining kernel costs.  With fewer items than SMs the longest
-// item counts, otherwise the waves plus half an item for the uneven end.
-constexpr int kMaxSplits = 64;
-int pick_splits(int64_t pairs, int64_t cap_tiles, int min_tiles, double tile, double item, int sms) {
-    const double join = 6000.;
-    int best = 1;
-    double best_cost = 0;
-    for (int s = 1; s <= kMaxSplits; ++s) {
-        const int64_t per = (cap_tiles + s - 1) / s;
-        if (s > 1 && per < min_tiles) break;
-        const double one = double(per) * tile + item, items = double(pairs) * s;
-        const double cost = one * (items <= sms ? 1. : items / sms + 0.5) + (s > 1 ? join : 0.);
-        if (s == 1 || cost < best_cost * 0.98) { best = s; best_cost = cost; }
-    }
-    return best;
-}
 
 // Up to sixteen query rows per KV head (single tokens above all) go to the kernel that streams the cache through
 // warp-level products: its rows are spread over all threads, where a tcgen05 row tile would leave most of them idle.
@@ -715,22 +761,23 @@ ChunkPlan chunk_plan(const csp_params& p, int max_new) {
     pl.row_slots = (max_new < 2 * pl.tok_tile ? max_new : 2 * pl.tok_tile) * G;
     const bool few = pl.row_slots <= kFewRows;
     pl.key_tile = few ? 64 : kTileKeys;
-    pl.min_tiles = few ? 2 : kMinTiles;
-    const int64_t pairs = int64_t(p.batch) * p.n_kv_heads * pl.n_pairs;
-    // a tile of 64 or 128 keys as a share of the memory stream, or the products of two row tiles
-    const double tile = few ? 1400. : pl.row_slots > 128 ? 2400. : 2800.;
-    pl.splits = pick_splits(pairs, (int64_t(p.out_capacity) + pl.key_tile - 1) / pl.key_tile, pl.min_tiles, tile,
-                            few ? 2500. : 4000., sm_count());
-    const int64_t items = pairs * pl.splits;
-    pl.n_items = items > 0x3fffffffLL ? -1 : int(items);
+    pl.min_tiles = 2;
+    pl.item_cost = 2;
+    const int64_t items = int64_t(p.batch) * p.n_kv_heads * pl.n_pairs;
+    const int64_t weight = (int64_t(p.out_capacity) + pl.key_tile - 1) / pl.key_tile + pl.item_cost;      // of an item, at most
+    pl.n_items = items > 0x3fffffffLL / weight ? -1 : int(items);
+    // no more blocks than there can be shares of the smallest size
+    const int64_t most = (items > 65536 ? 65536 : items) * weight / (pl.item_cost + pl.min_tiles) + 1;
+    pl.grid = most < sm_count() ? int(most) : sm_count();
     return pl;
 }
 
-struct PartialLayout { size_t ml, o, total; };
+struct PartialLayout { size_t parts, ml, o, total; };
 PartialLayout partial_layout(const csp_params& p, const ChunkPlan& pl) {
     PartialLayout x;
-    const size_t rows = pl.splits > 1 && pl.n_items > 0 ? size_t(pl.n_items) * size_t(pl.row_slots) : 0;
-    x.ml = kStatusBytes;
+    const size_t rows = size_t(2) * pl.grid * pl.row_slots;
+    x.parts = kStatusBytes;
+    x.ml = x.parts + round256(size_t(pl.grid) * sizeof(ChunkParts));
     x.o = x.ml + round256(rows * sizeof(float2));
     x.total = x.o + round256(rows * size_t(p.head_dim) * 4);
     return x;
@@ -738,30 +785,29 @@ PartialLayout partial_layout(const csp_params& p, const ChunkPlan& pl) {
 
 template <int NH, bool kCap, bool kBias, bool kDoc>
 csp_status launch_variant(const ChunkArgs& a, const ChunkPlan& pl, const CUtensorMap& tq, const CUtensorMap& tk,
-                          const CUtensorMap& tv, float* partial, float2* ml, cudaStream_t s) {
+                          const CUtensorMap& tv, ChunkParts* parts, float* partial, float2* ml, cudaStream_t s) {
     constexpr int smem = int(ChunkShape<NH, kBias || kDoc>::plan().total) + 1024;
     static_assert(smem <= 227 * 1024, "shared memory of one CTA");
     auto kern = chunk_attn_kernel<NH, kCap, kBias, kDoc>;
     static std::atomic<bool> configured[kMaxDevices];
     if (!raise_smem_limit(kern, smem, configured)) return CSP_ERR_CUDA;
-    const int sms = sm_count();
-    kern<<<pl.n_items < sms ? pl.n_items : sms, kChThreads, smem, s>>>(tq, tk, tv, a, pl, partial, ml);
+    kern<<<pl.grid, kChThreads, smem, s>>>(tq, tk, tv, a, pl, parts, partial, ml);
     return cudaGetLastError() == cudaSuccess ? CSP_OK : CSP_ERR_CUDA;
 }
 
 template <int NH>
 csp_status launch_nh(const ChunkArgs& a, const ChunkPlan& pl, const CUtensorMap& tq, const CUtensorMap& tk,
-                     const CUtensorMap& tv, float* partial, float2* ml, cudaStream_t s) {
+                     const CUtensorMap& tv, ChunkParts* parts, float* partial, float2* ml, cudaStream_t s) {
     const int which = (a.mods.softcap > 0.f ? 4 : 0) | (a.mods.slopes ? 2 : 0) | (a.mods.documents ? 1 : 0);
     switch (which) {
-        case 0: return launch_variant<NH, false, false, false>(a, pl, tq, tk, tv, partial, ml, s);
-        case 1: return launch_variant<NH, false, false, true>(a, pl, tq, tk, tv, partial, ml, s);
-        case 2: return launch_variant<NH, false, true, false>(a, pl, tq, tk, tv, partial, ml, s);
-        case 3: return launch_variant<NH, false, true, true>(a, pl, tq, tk, tv, partial, ml, s);
-        case 4: return launch_variant<NH, true, false, false>(a, pl, tq, tk, tv, partial, ml, s);
-        case 5: return launch_variant<NH, true, false, true>(a, pl, tq, tk, tv, partial, ml, s);
-        case 6: return launch_variant<NH, true, true, false>(a, pl, tq, tk, tv, partial, ml, s);
-        default: return launch_variant<NH, true, true, true>(a, pl, tq, tk, tv, partial, ml, s);
+        case 0: return launch_variant<NH, false, false, false>(a, pl, tq, tk, tv, parts, partial, ml, s);
+        case 1: return launch_variant<NH, false, false, true>(a, pl, tq, tk, tv, parts, partial, ml, s);
+        case 2: return launch_variant<NH, false, true, false>(a, pl, tq, tk, tv, parts, partial, ml, s);
+        case 3: return launch_variant<NH, false, true, true>(a, pl, tq, tk, tv, parts, partial, ml, s);
+        case 4: return launch_variant<NH, true, false, false>(a, pl, tq, tk, tv, parts, partial, ml, s);
+        case 5: return launch_variant<NH, true, false, true>(a, pl, tq, tk, tv, parts, partial, ml, s);
+        case 6: return launch_variant<NH, true, true, false>(a, pl, tq, tk, tv, parts, partial, ml, s);
+        default: return launch_variant<NH, true, true, true>(a, pl, tq, tk, tv, parts, partial, ml, s);
     }
 }
 
@@ -775,8 +821,9 @@ size_t chunk_workspace_bytes(const csp_params& p, int max_new) {
 csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_tensor& q, const csp_tensor& k,
                              const csp_tensor& v, const csp_pages* pages, void* ws, cudaStream_t s) {
     const ChunkPlan pl = chunk_plan(p, a.max_new);
-    if (pl.n_items < 0) return CSP_ERR_UNSUPPORTED;
+    if (pl.n_items < 0) return CSP_ERR_UNSUPPORTED;      // key tiles are counted in 32 bits
     const PartialLayout lay = partial_layout(p, pl);
+    ChunkParts* const parts = reinterpret_cast<ChunkParts*>(static_cast<char*>(ws) + lay.parts);
     float* const partial = reinterpret_cast<float*>(static_cast<char*>(ws) + lay.o);
     float2* const ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + lay.ml);
     CUtensorMap tq, tk, tv;
@@ -788,18 +835,25 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
         return CSP_ERR_UNSUPPORTED;
     csp_status st;
     if (pl.row_slots <= kFewRows) {
-        st = launch_chunk_few(p, a, pl, q, tk, tv, partial, ml, s);
+        st = launch_chunk_few(p, a, pl, q, tk, tv, parts, partial, ml, s);
     } else {
         if (!make_query_tensor_map(&tq, q, p.head_dim, p.n_q_heads, a.max_new, p.batch, a.group, box_tokens))
             return CSP_ERR_UNSUPPORTED;
-        st = p.head_dim == 64 ? launch_nh<1>(a, pl, tq, tk, tv, partial, ml, s) : launch_nh<2>(a, pl, tq, tk, tv, partial, ml, s);
+        st = p.head_dim == 64 ? launch_nh<1>(a, pl, tq, tk, tv, parts, partial, ml, s) : launch_nh<2>(a, pl, tq, tk, tv, parts, partial, ml, s);
     }
-    if (st != CSP_OK || pl.splits == 1) return st;
-    const int64_t rows = int64_t(pl.n_items / pl.splits) * pl.row_slots;
-    const unsigned blocks = unsigned((rows + 7) / 8);
-    if (p.head_dim == 64) chunk_merge_kernel<64><<<blocks, 256, 0, s>>>(a, pl, partial, ml);
-    else chunk_merge_kernel<128><<<blocks, 256, 0, s>>>(a, pl, partial, ml);
-    return cudaGetLastError() == cudaSuccess ? CSP_OK : CSP_ERR_CUDA;
+    if (st != CSP_OK || pl.grid == 1) return st;         // a single block cuts nothing
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(pl.grid, (pl.row_slots + kJoinWarps - 1) / kJoinWarps);
+    cfg.blockDim = dim3(32 * kJoinWarps);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;         // it waits for the main kernel by itself
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    const cudaError_t err = p.head_dim == 64 ? cudaLaunchKernelEx(&cfg, chunk_join_kernel<64>, a, pl, (const ChunkParts*)parts, (const float*)partial, (const float2*)ml)
+                                             : cudaLaunchKernelEx(&cfg, chunk_join_kernel<128>, a, pl, (const ChunkParts*)parts, (const float*)partial, (const float2*)ml);
+    if (err != cudaSuccess) { cudaGetLastError(); return CSP_ERR_CUDA; }
+    return CSP_OK;
 }
 
 }  // namespace csp

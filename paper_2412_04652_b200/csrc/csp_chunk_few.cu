@@ -3,8 +3,8 @@
 // for a tcgen05 row tile of 128, whose softmax would run on a quarter of one warp group.  Here the rows are the M of a
 // warp-level m16n8k16 product and the keys of a tile are spread over the warps, so every thread has a few logits.
 //
-// Same organisation as the decode kernel: one CTA per SM stays resident and draws items (a range of 64-key tiles of
-// one unit) from a counter.
+// Same organisation as the decode kernel: one CTA per SM stays resident and works off an equal share of all
+// 64-key tiles of all units.
 //   warp 4      producer: streams tiles of K and V with TMA (128-byte swizzle, no multicast) through a ring of six
 //               stages and says with each stage which tile it holds; an item ends with a stage without data
 //   warps 0-3   each owns 16 keys of every tile: S = Q K^T, modifiers and mask, running softmax with a lazily raised
@@ -46,7 +46,7 @@ struct FewShape {
 template <int NH, int RH>   // head_dim = 64 NH, 8 RH query rows
 __global__ void __launch_bounds__(kFewThreads, 1)
 chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const ChunkArgs a,
-                 const ChunkPlan pl, const FewQuery qy, float* const partial, float2* const partial_ml) {
+                 const ChunkPlan pl, const FewQuery qy, ChunkParts* const parts, float* const partial, float2* const partial_ml) {
     using Shape = FewShape<NH, RH>;
     constexpr int D = Shape::D, R = Shape::R;
     constexpr int KS = D / 16;                           // k-steps of S = Q K^T
@@ -70,7 +70,8 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    __syncthreads();
+    const Share share = find_share<kFewThreads>(a, pl, reinterpret_cast<int*>(merge));      // (synchronises)
+    asm volatile("griddepcontrol.launch_dependents;");   // the joining kernel may get ready
 
     if (warp == kFewWarps) {
         // =============================== producer ===============================
@@ -78,7 +79,8 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         bool ok = true;
         auto stage = [&](int item, int tile) {           // the next stage, free, with what it holds written beside it
             const uint32_t s = it % kFewStages;
-            ok = ok && warp_wait(empty_bar + 8 * s, ((it / kFewStages) & 1u) ^ 1u, abort_flag);
+            warp_wait(empty_bar + 8 * s, ((it / kFewStages) & 1u) ^ 1u, abort_flag);
+            ok = ok && !warp_aborted(abort_flag);
             if (ok && lane == 0) { info[2 * s] = item; info[2 * s + 1] = tile; }
             ++it;
             return s;
@@ -87,20 +89,16 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
             const uint32_t s = stage(item, -1);
             if (ok && lane == 0) mbar_arrive(full_bar + 8 * s);
         };
-        ItemDraw draw;
-        draw.init(lane, a.status, pl.n_items);
-        int w = blockIdx.x;
-        while (ok && w < pl.n_items) {
-            const int w_now = w;
-            w = draw.next(lane);
-            const int split = w_now % pl.splits, u = w_now / pl.splits, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
+        if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, -1, 0, 0};
+        for (int u = share.item0; ok && u <= share.item1 && u < pl.n_items; ++u) {
+            const int b = u / a.n_kv_heads, h = u % a.n_kv_heads;
             const PairRange x = pair_range(a, pl, u, 0);
-            if (split == 0 && lane == 0) {
-                const int rows = a.n_rows[u], more = a.n_new ? a.n_new[b] : a.max_new;
-                if (rows != x.rows || more != x.n_new || x.n_new > x.rows) atomicOr(a.status, CSP_DEV_BAD_LEN);
+            const int tile0 = u == share.item0 ? share.tile0 : 0, tile1 = u == share.item1 ? share.tile1 : x.tiles;
+            if (x.count <= 0 || (u == share.item1 && tile1 == 0)) continue;
+            if (lane == 0) {
+                if (tile0 > 0) { parts[blockIdx.x].more = u; parts[blockIdx.x].last = tile1 == x.tiles; }
+                else if (tile1 < x.tiles) parts[blockIdx.x].first = u;
             }
-            if (x.count <= 0 || split >= x.active) continue;
-            const int tile0 = split * x.per_split, tile1 = min(x.tiles, tile0 + x.per_split);
             const int32_t* const docs = md.documents ? md.documents + int64_t(b) * md.doc_sb + int64_t(h) * md.doc_sh : nullptr;
             int doc_lo = INT_MAX, doc_hi = INT_MIN;
             if (docs) {                                  // sixteen rows at most
@@ -140,7 +138,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                     }
                     row %= a.page_rows;
                 }
-                const uint32_t s = stage(w_now, tile);
+                const uint32_t s = stage(u, tile);
                 if (ok && lane == 0) {
                     mbar_expect_tx(full_bar + 8 * s, kStageBytes);
 #pragma unroll
@@ -150,7 +148,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                     }
                 }
             }
-            marker(w_now);
+            marker(u);
         }
         if (ok) marker(-1);
         if (lane == 0) {
@@ -162,7 +160,6 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                 }
                 atomicOr(a.status, CSP_DEV_TIMEOUT);
             }
-            draw.done();
         }
     } else {
         // =============================== consumer warps ===============================
@@ -177,7 +174,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         // capped: x = c tanh(o / c) = c - 2 c / (1 + e^{2 o / c}), all in the base-2 domain
         const float cap2 = md.softcap * kLog2e, cap_in = capped ? 2.f * kLog2e * a.scale / md.softcap : 0.f;
         uint32_t it = 0, n_join = 0;
-        int item = -1, b = 0, h = 0, u = 0, split = 0;
+        int item = -1, b = 0, h = 0, u = 0;
         PairRange x = {};
         uint32_t qa[KS][4];
         float acc[NT][4];
@@ -187,13 +184,14 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         const int32_t* poss = nullptr;
         for (;;) {
             const uint32_t s = it % kFewStages;
-            if (!warp_wait(full_bar + 8 * s, (it / kFewStages) & 1u, abort_flag)) break;
+            warp_wait(full_bar + 8 * s, (it / kFewStages) & 1u, abort_flag);
+            if (warp_aborted(abort_flag)) break;
             ++it;
             const int w = info[2 * s], tile = info[2 * s + 1];
             if (w < 0) break;
             if (w != item) {
                 item = w;
-                split = w % pl.splits; u = w / pl.splits; b = u / a.n_kv_heads; h = u % a.n_kv_heads;
+                u = w; b = u / a.n_kv_heads; h = u % a.n_kv_heads;
                 x = pair_range(a, pl, u, 0);
                 docs = md.documents ? md.documents + int64_t(b) * md.doc_sb + int64_t(h) * md.doc_sh : nullptr;
                 poss = md.slopes && md.positions ? md.positions + int64_t(b) * md.pos_sb + int64_t(h) * md.pos_sh : nullptr;
@@ -309,7 +307,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
             __syncwarp();
             if (lane == 0) mbar_arrive(empty_bar + 8 * s);
             // everybody has read what the previous item left there
-            if (n_join > 0 && !warp_wait(join_bar, (n_join - 1u) & 1u, abort_flag)) break;
+            if (n_join > 0) warp_wait(join_bar, (n_join - 1u) & 1u, abort_flag);
 #pragma unroll
             for (int rr = 0; rr < RH; ++rr) {
                 l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 1);
@@ -322,9 +320,12 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(join_bar);
-            if (!warp_wait(join_bar, n_join & 1u, abort_flag)) break;
+            warp_wait(join_bar, n_join & 1u, abort_flag);
             n_join += 2;
-            const bool final = x.active == 1;
+            // the item is whole, or this is the rest (partial result 2 c) or the beginning (2 c + 1) of a cut one
+            const int part_slot = u == share.item0 && share.tile0 > 0 ? 2 * int(blockIdx.x)
+                                  : u == share.item1 && share.tile1 < x.tiles ? 2 * int(blockIdx.x) + 1 : -1;
+            const bool final = part_slot < 0;
             constexpr int C = D / 32;                    // columns per lane: a warp takes every fourth row
             for (int m = warp; m < x.count * G; m += kFewWarps) {
                 float2 st[kFewWarps];
@@ -357,9 +358,13 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                     if (a.lse && lane == 0)
                         a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
                 } else {
-                    const int64_t slot = (int64_t(u) * pl.splits + split) * pl.row_slots + m;
+                    const int64_t slot = int64_t(part_slot) * pl.row_slots + m;
 #pragma unroll
-                    for (int c = 0; c < C; c += 2) *reinterpret_cast<float2*>(partial + slot * D + lane * C + c) = make_float2(o[c], o[c + 1]);
+                    for (int c = 0; c < C; c += 2) {     // laid out [column / 4][row][4]
+                        const int col = lane * C + c;
+                        *reinterpret_cast<float2*>(partial + ((slot - m) * (D / 4) + int64_t(col / 4) * pl.row_slots + m) * 4 + col % 4) =
+                            make_float2(o[c], o[c + 1]);
+                    }
                     if (lane == 0) partial_ml[slot] = make_float2(mm, l);
                 }
             }
@@ -371,25 +376,25 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
 
 template <int NH, int RH>
 csp_status launch_few(const ChunkArgs& a, const ChunkPlan& pl, const FewQuery& q, const CUtensorMap& tk, const CUtensorMap& tv,
-                      float* partial, float2* ml, cudaStream_t s) {
+                      ChunkParts* parts, float* partial, float2* ml, cudaStream_t s) {
     constexpr int smem = int(FewShape<NH, RH>::kTotal) + 1024;
     static_assert(smem <= 227 * 1024, "shared memory of one CTA");
     auto kern = chunk_few_kernel<NH, RH>;
     static std::atomic<bool> configured[kMaxDevices];
     if (!raise_smem_limit(kern, smem, configured)) return CSP_ERR_CUDA;
-    const int sms = sm_count();
-    kern<<<pl.n_items < sms ? pl.n_items : sms, kFewThreads, smem, s>>>(tk, tv, a, pl, q, partial, ml);
+    kern<<<pl.grid, kFewThreads, smem, s>>>(tk, tv, a, pl, q, parts, partial, ml);
     return cudaGetLastError() == cudaSuccess ? CSP_OK : CSP_ERR_CUDA;
 }
 
 }  // namespace
 
 csp_status launch_chunk_few(const csp_params& p, const ChunkArgs& a, const ChunkPlan& pl, const csp_tensor& q,
-                            const CUtensorMap& tk, const CUtensorMap& tv, float* partial, float2* ml, cudaStream_t s) {
+                            const CUtensorMap& tk, const CUtensorMap& tv, ChunkParts* parts, float* partial, float2* ml,
+                            cudaStream_t s) {
     const FewQuery qy = {static_cast<const uint16_t*>(q.ptr), q.stride_b, q.stride_h, q.stride_t};
     if (pl.row_slots <= 8)
-        return p.head_dim == 64 ? launch_few<1, 1>(a, pl, qy, tk, tv, partial, ml, s) : launch_few<2, 1>(a, pl, qy, tk, tv, partial, ml, s);
-    return p.head_dim == 64 ? launch_few<1, 2>(a, pl, qy, tk, tv, partial, ml, s) : launch_few<2, 2>(a, pl, qy, tk, tv, partial, ml, s);
+        return p.head_dim == 64 ? launch_few<1, 1>(a, pl, qy, tk, tv, parts, partial, ml, s) : launch_few<2, 1>(a, pl, qy, tk, tv, parts, partial, ml, s);
+    return p.head_dim == 64 ? launch_few<1, 2>(a, pl, qy, tk, tv, parts, partial, ml, s) : launch_few<2, 2>(a, pl, qy, tk, tv, parts, partial, ml, s);
 }
 
 }  // namespace csp

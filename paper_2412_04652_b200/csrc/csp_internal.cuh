@@ -204,6 +204,7 @@ struct ChunkArgs {
     const int32_t* n_rows;                           // [B, Hkv]
     const int32_t* n_new;                            // [B], or null: max_new
     uint16_t* out; int64_t o_sb, o_sh, o_st;         // bf16, element strides
+    bool out_wide;                                   // rows start at multiples of 32 bytes
     float* lse;                                      // [B, Hq, max_new] or null
     int32_t* status;
     int32_t batch, n_kv_heads, group, capacity, max_new;

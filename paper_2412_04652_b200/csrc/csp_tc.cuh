@@ -105,6 +105,13 @@ __device__ __forceinline__ void tc_ld_16x16(uint32_t (&v)[8], uint32_t taddr) {
 }
 __device__ __forceinline__ void tc_ld_frag(uint32_t (&v)[16], uint32_t taddr) { tc_ld_16x32(v, taddr); }
 __device__ __forceinline__ void tc_ld_frag(uint32_t (&v)[8], uint32_t taddr) { tc_ld_16x16(v, taddr); }
+// one lane of a converged warp, the same every time; unlike a test of the lane number it lets the compiler keep what the
+// lane works with in uniform registers, where the tcgen05 instructions want it
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 // shared-memory matrix descriptor: K-major operand, 128-byte swizzle, 8-row groups 1024 bytes apart
 __device__ __forceinline__ uint64_t sw128_desc(uint32_t smem_addr) {
     uint64_t d = uint64_t((smem_addr & 0x3FFFFu) >> 4);
@@ -177,6 +184,20 @@ __device__ __forceinline__ float2 ex2_fma2(float2 x) {
     p = __ffma2_rn(p, f, make_float2(0.9999280572f, 0.9999280572f));
     return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
                        __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+
+// three-input maximum that hands a NaN on
+__device__ __forceinline__ float fmax3_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// Orders the use of loaded registers behind the tc_wait_ld in front of it.
+__device__ __forceinline__ void tc_loaded(uint32_t (&v)[32]) {
+    asm volatile("" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                      "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]),
+                      "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
+                      "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]));
 }
 
 // ---- pass-1 row statistics of one accumulator block of 32 rows x 8 NB columns ----------------------------
