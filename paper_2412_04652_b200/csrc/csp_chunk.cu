@@ -700,20 +700,20 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     }
 }
 
-// out = sum_s O_s 2^(m_s - m) / (n 2^-m + sum_s l_s 2^(m_s - m)) over the parts of a cut item; one warp per query row.  Block
-// (c, .) joins the item that begins in block c of the main kernel and goes on in c + 1, ... until one says it is the last.
+// out = sum_s O_s 2^(m_s - m) / (n 2^-m + sum_s l_s 2^(m_s - m)) over the parts of a cut item.  Block (c, r) joins 32 rows of
+// the item that begins in block c of the main kernel and goes on in c + 1, ... until one says it is the last.  A lane has a
+// row, a warp an eighth of the columns: the parts are laid out [column / 4][row][4], so every load is one piece.
 constexpr int kJoinWarps = 8;
 template <int D>
 __global__ void __launch_bounds__(32 * kJoinWarps) chunk_join_kernel(const ChunkArgs a, const ChunkPlan pl, const ChunkParts* parts,
                                                                      const float* partial, const float2* partial_ml) {
+    constexpr int C = D / 4 / kJoinWarps;                // chunks of four columns per lane
     asm volatile("griddepcontrol.wait;" ::: "memory");   // launched early: the main kernel has to be through
     const int c0 = blockIdx.x, item = parts[c0].first;
     if (item < 0) return;
-    const int lane = threadIdx.x & 31, G = a.group, row = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = a.group;
     const int u = item / pl.n_pairs, pair = item - u * pl.n_pairs, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
-    const int tok = pair * 2 * pl.tok_tile + row / G, head = h * G + row % G;
     const int n_new = a.n_new ? min(max(a.n_new[b], 0), a.max_new) : a.max_new;
-    if (row >= pl.row_slots || tok >= n_new) return;
     int n_parts = 1;
     for (int c = c0 + 1; c < pl.grid; c += 32) {
         const bool in = c + lane < pl.grid;
@@ -722,26 +722,33 @@ __global__ void __launch_bounds__(32 * kJoinWarps) chunk_join_kernel(const Chunk
         n_parts += 32;
     }
     n_parts = min(n_parts, pl.grid - c0);
-    auto slot = [&](int s) { return (int64_t(2 * (c0 + s)) + (s == 0 ? 1 : 0)) * pl.row_slots + row; };
+    const int row = blockIdx.y * 32 + lane, tok = pair * 2 * pl.tok_tile + row / G, head = h * G + row % G;
+    if (row >= pl.row_slots || tok >= n_new) return;
+    // partial results 2 c0 + 1, 2 (c0 + 1), 2 (c0 + 2), ...
+    auto slot = [&](int s) { return int64_t(2 * (c0 + s) + (s == 0 ? 1 : 0)) * pl.row_slots; };
     float m = kNeg;
-    for (int s = lane; s < n_parts; s += 32) m = fmaxf(m, partial_ml[slot(s)].x);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    float l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int chunk = lane % (D / 4);                    // (d = 64: the lanes' second half repeats the first's work)
 #pragma unroll 4
+    for (int s = 0; s < n_parts; ++s) m = fmaxf(m, partial_ml[slot(s) + row].x);
+    float l = 0.f;
+    float4 o[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
     for (int s = 0; s < n_parts; ++s) {
-        const float2 p = partial_ml[slot(s)];
+        const float2 p = partial_ml[slot(s) + row];
         const float w = ex2f(p.x - m);
-        const float4 y = *reinterpret_cast<const float4*>(partial + ((slot(s) - row) * (D / 4) + int64_t(chunk) * pl.row_slots + row) * 4);
         l += p.y * w;
-        o.x += y.x * w; o.y += y.y * w; o.z += y.z * w; o.w += y.w * w;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const float4 y = *reinterpret_cast<const float4*>(partial + (slot(s) * (D / 4) + int64_t(warp * C + c) * pl.row_slots + row) * 4);
+            o[c].x += y.x * w; o[c].y += y.y * w; o[c].z += y.z * w; o[c].w += y.w * w;
+        }
     }
     const float inv = l == 0.f ? 0.f : 1.f / (a.n * ex2f(-m) + l);
-    uint2* const out = reinterpret_cast<uint2*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st + chunk * 4);
-    if (lane < D / 4) *out = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-    if (a.lse && lane == 0)
+    uint2* const out = reinterpret_cast<uint2*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st) + warp * C;
+#pragma unroll
+    for (int c = 0; c < C; ++c) out[c] = make_uint2(pack_bf16(o[c].x * inv, o[c].y * inv), pack_bf16(o[c].z * inv, o[c].w * inv));
+    if (a.lse && warp == 0)
         a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
@@ -843,7 +850,7 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
     }
     if (st != CSP_OK || pl.grid == 1) return st;         // a single block cuts nothing
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(pl.grid, (pl.row_slots + kJoinWarps - 1) / kJoinWarps);
+    cfg.gridDim = dim3(pl.grid, (pl.row_slots + 31) / 32);
     cfg.blockDim = dim3(32 * kJoinWarps);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];

@@ -5,11 +5,13 @@
 //
 // Same organisation as the decode kernel: one CTA per SM stays resident and works off an equal share of all
 // 64-key tiles of all units.
-//   warp 4      producer: streams tiles of K and V with TMA (128-byte swizzle, no multicast) through a ring of six
-//               stages and says with each stage which tile it holds; an item ends with a stage without data
-//   warps 0-3   each owns 16 keys of every tile: S = Q K^T, modifiers and mask, running softmax with a lazily raised
+//   warp 8      producer: streams tiles of K and V with TMA (128-byte swizzle, no multicast) through a ring of
+//               stages, puts the keys' positions and documents beside them and says with each stage which tile it
+//               holds; an item ends with a stage without data
+//   warps 0-3, 4-7  two groups that take turns, so that one computes while the other one's tile arrives.  A warp owns
+//               16 keys of its group's tiles: S = Q K^T, modifiers and mask, running softmax with a lazily raised
 //               reference, then P V with the weights as a bf16 head plus a bf16 remainder (two products per fragment),
-//               so that only the result is rounded to bf16.  At the end of an item the four warps' results are
+//               so that only the result is rounded to bf16.  At the end of an item the eight warps' results are
 //               joined in a fixed order; an undivided unit is finished here, a divided one leaves a partial result
 #include <limits.h>
 
@@ -20,9 +22,9 @@ namespace {
 using namespace dev;
 
 constexpr int kFewTile = 64;                             // keys per stage
-constexpr int kFewWarps = 4;                             // consumer warps, 16 keys of every tile each
-constexpr int kFewThreads = 32 * (kFewWarps + 1);
-constexpr int kFewStages = 6;                            // 32 KB each at d = 128
+constexpr int kFewWarps = 4;                             // warps of a group, 16 keys of a tile each
+constexpr int kFewConsumers = 2 * kFewWarps;
+constexpr int kFewThreads = 32 * (kFewConsumers + 1);
 constexpr int kFewBlock = kFewTile * 128;                // bytes of one 64-column block of a tile
 
 struct FewQuery { const uint16_t* q; int64_t sb, sh, st; };
@@ -35,11 +37,13 @@ __device__ __forceinline__ void ldsm_x4_t(uint32_t (&r)[4], uint32_t addr) {
 template <int NH, int RH>
 struct FewShape {
     static constexpr int D = 64 * NH, R = 8 * RH;
+    static constexpr int kStages = NH == 2 && RH == 2 ? 5 : 6;                         // 32 KB each at d = 128
     static constexpr uint32_t kTileBytes = NH * kFewBlock, kStageBytes = 2 * kTileBytes;
-    static constexpr uint32_t kMerge = kFewStages * kStageBytes;                       // [warp][R][D + 2] floats
-    static constexpr uint32_t kBars = kMerge + kFewWarps * R * (D + 2) * 4;            // full, empty, join
-    static constexpr uint32_t kInfo = kBars + (2 * kFewStages + 1) * 8;                // int2 per stage: item, tile
-    static constexpr uint32_t kMisc = kInfo + kFewStages * 8;
+    static constexpr uint32_t kMerge = kStages * kStageBytes;                          // [warp of a group][R][D + 2] floats
+    static constexpr uint32_t kMeta = kMerge + kFewWarps * R * (D + 2) * 4;            // per stage: 64 positions, 64 documents
+    static constexpr uint32_t kBars = kMeta + kStages * kFewTile * 8;                  // full, empty, join
+    static constexpr uint32_t kInfo = kBars + (2 * kStages + 2) * 8;                   // int2 per stage: item, tile
+    static constexpr uint32_t kMisc = kInfo + kStages * 8;
     static constexpr uint32_t kTotal = kMisc + 16;
 };
 
@@ -48,7 +52,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
 chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const ChunkArgs a,
                  const ChunkPlan pl, const FewQuery qy, ChunkParts* const parts, float* const partial, float2* const partial_ml) {
     using Shape = FewShape<NH, RH>;
-    constexpr int D = Shape::D, R = Shape::R;
+    constexpr int D = Shape::D, R = Shape::R, NST = Shape::kStages;
     constexpr int KS = D / 16;                           // k-steps of S = Q K^T
     constexpr int NT = D / 8;                            // 8-column tiles of the output
     constexpr uint32_t kTileBytes = Shape::kTileBytes, kStageBytes = Shape::kStageBytes;
@@ -57,31 +61,31 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
     float* const merge = reinterpret_cast<float*>(base_ptr + Shape::kMerge);
-    const uint32_t full_bar = base + Shape::kBars, empty_bar = full_bar + 8 * kFewStages, join_bar = empty_bar + 8 * kFewStages;
-    volatile int* const info = reinterpret_cast<volatile int*>(base_ptr + Shape::kInfo);
+    const uint32_t full_bar = base + Shape::kBars, empty_bar = full_bar + 8 * NST, join_bar = empty_bar + 8 * NST;
+    int2* const info = reinterpret_cast<int2*>(base_ptr + Shape::kInfo);
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(base_ptr + Shape::kMisc);
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.group;
     const ModArgs& md = a.mods;
     if (tid == 0) {
         *abort_flag = 0;
-        for (int s = 0; s < kFewStages; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, kFewWarps); }
-        mbar_init(join_bar, kFewWarps);
+        for (int s = 0; s < NST; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, kFewConsumers); }
+        mbar_init(join_bar, kFewConsumers);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     const Share share = find_share<kFewThreads>(a, pl, reinterpret_cast<int*>(merge));      // (synchronises)
     asm volatile("griddepcontrol.launch_dependents;");   // the joining kernel may get ready
 
-    if (warp == kFewWarps) {
+    if (warp == kFewConsumers) {
         // =============================== producer ===============================
         uint32_t it = 0;
         bool ok = true;
         auto stage = [&](int item, int tile) {           // the next stage, free, with what it holds written beside it
-            const uint32_t s = it % kFewStages;
-            warp_wait(empty_bar + 8 * s, ((it / kFewStages) & 1u) ^ 1u, abort_flag);
+            const uint32_t s = it % NST;
+            warp_wait(empty_bar + 8 * s, ((it / NST) & 1u) ^ 1u, abort_flag);
             ok = ok && !warp_aborted(abort_flag);
-            if (ok && lane == 0) { info[2 * s] = item; info[2 * s + 1] = tile; }
+            if (ok && lane == 0) info[s] = make_int2(item, tile);
             ++it;
             return s;
         };
@@ -90,16 +94,35 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
             if (ok && lane == 0) mbar_arrive(full_bar + 8 * s);
         };
         if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, -1, 0, 0};
+        const uint32_t tiles_per_page = uint32_t(a.page_rows) / uint32_t(kFewTile);      // (dense: not used)
+        auto page_of = [&](int b, int tile) {            // the page of a tile that lies inside the cache
+            return a.page_table[int64_t(b) * a.max_pages + uint32_t(tile) / tiles_per_page];
+        };
+        PairRange next = {};
+        int next_page = 0;                               // lane l: page of the next item's tile l (of its first 32)
+        auto look_up = [&](int u) {                      // while the current item streams
+            if (u > share.item1 || u >= pl.n_items) return;
+            next = pair_range(a, pl, u, 0);
+            const int tile = (u == share.item0 ? share.tile0 : 0) + lane;
+            if (a.page_table && next.count > 0 && tile < next.tiles) next_page = page_of(u / a.n_kv_heads, tile);
+        };
+        look_up(share.item0);
         for (int u = share.item0; ok && u <= share.item1 && u < pl.n_items; ++u) {
             const int b = u / a.n_kv_heads, h = u % a.n_kv_heads;
-            const PairRange x = pair_range(a, pl, u, 0);
+            const PairRange x = next;
+            int pages = next_page;                       // lane l: the page of tile 32 j + l
             const int tile0 = u == share.item0 ? share.tile0 : 0, tile1 = u == share.item1 ? share.tile1 : x.tiles;
-            if (x.count <= 0 || (u == share.item1 && tile1 == 0)) continue;
+            if (x.count <= 0 || (u == share.item1 && tile1 == 0)) { look_up(u + 1); continue; }
             if (lane == 0) {
                 if (tile0 > 0) { parts[blockIdx.x].more = u; parts[blockIdx.x].last = tile1 == x.tiles; }
                 else if (tile1 < x.tiles) parts[blockIdx.x].first = u;
             }
             const int32_t* const docs = md.documents ? md.documents + int64_t(b) * md.doc_sb + int64_t(h) * md.doc_sh : nullptr;
+            const int32_t* const poss = md.slopes && md.positions ? md.positions + int64_t(b) * md.pos_sb + int64_t(h) * md.pos_sh : nullptr;
+            const bool meta = docs || md.slopes;
+            // positions are staged relative to the last token's, so that near ones are exact in fp32
+            const int row_last = max(x.row0 + x.count - 1, 0);
+            const int pos_ref = md.slopes && x.rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
             int doc_lo = INT_MAX, doc_hi = INT_MIN;
             if (docs) {                                  // sixteen rows at most
                 const int r = x.row0 + lane;
@@ -107,25 +130,29 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                 doc_lo = __reduce_min_sync(0xffffffffu, doc_lo);
                 doc_hi = __reduce_max_sync(0xffffffffu, doc_hi);
             }
-            int pages = 0, d_next[2] = {0, 0};
-            auto fetch_docs = [&](int tile) {
+            // documents and positions of four tiles' keys at once, fetched before the first of them is needed
+            int d_now[8], p_now[8];
+            auto fetch_meta = [&](int tile) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
+                for (int j = 0; j < 8; ++j) {
                     const int t = tile * kFewTile + lane + 32 * j;
-                    d_next[j] = t < x.kv_end[1] ? docs[t] : INT_MIN;
+                    d_now[j] = docs && t < x.rows ? docs[t] : 0;
+                    p_now[j] = !md.slopes ? 0 : poss ? (t < x.rows ? poss[t] : pos_ref) : t;
                 }
             };
-            if (docs && tile0 < tile1) fetch_docs(tile0);
+            bool looked = false;
             for (int tile = tile0; tile < tile1 && ok; ++tile) {
-                if (a.page_table && ((tile - tile0) & 31) == 0) {
-                    const int mine = tile + lane;
-                    pages = mine < tile1 ? a.page_table[int64_t(b) * a.max_pages + int64_t(mine) * kFewTile / a.page_rows] : 0;
-                }
+                const int turn = (tile - tile0) & 3;
+                if (meta && turn == 0) fetch_meta(tile);
+                if (a.page_table && tile > tile0 && ((tile - tile0) & 31) == 0) pages = tile + lane < tile1 ? page_of(b, tile + lane) : 0;
+                int dd[2] = {0, 0}, pp[2] = {0, 0};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (turn == j) { dd[0] = d_now[2 * j]; dd[1] = d_now[2 * j + 1]; pp[0] = p_now[2 * j]; pp[1] = p_now[2 * j + 1]; }
                 if (docs) {                              // a tile without any of the tokens' documents is skipped
                     bool hit = false;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) hit |= tile * kFewTile + lane + 32 * j < x.kv_end[1] && d_next[j] >= doc_lo && d_next[j] <= doc_hi;
-                    if (tile + 1 < tile1) fetch_docs(tile + 1);
+                    for (int j = 0; j < 2; ++j) hit |= tile * kFewTile + lane + 32 * j < x.kv_end[1] && dd[j] >= doc_lo && dd[j] <= doc_hi;
                     if (!__any_sync(0xffffffffu, hit)) continue;
                 }
                 int outer = b, row = tile * kFewTile;
@@ -136,9 +163,18 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                         if (lane == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
                         outer = a.n_pages;
                     }
-                    row %= a.page_rows;
+                    row = int(uint32_t(tile) % tiles_per_page) * kFewTile;
                 }
                 const uint32_t s = stage(u, tile);
+                if (meta) {
+                    float* const mp = reinterpret_cast<float*>(base_ptr + Shape::kMeta + s * kFewTile * 8);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        mp[lane + 32 * j] = float(pp[j] - pos_ref);
+                        reinterpret_cast<int32_t*>(mp)[kFewTile + lane + 32 * j] = dd[j];
+                    }
+                    __syncwarp();
+                }
                 if (ok && lane == 0) {
                     mbar_expect_tx(full_bar + 8 * s, kStageBytes);
 #pragma unroll
@@ -147,14 +183,16 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                         tma_load_4d(base + s * kStageBytes + kTileBytes + hb * kFewBlock, &tmap_v, full_bar + 8 * s, hb * 64, row, h, outer);
                     }
                 }
+                if (!looked) { look_up(u + 1); looked = true; }
             }
+            if (!looked) look_up(u + 1);
             marker(u);
         }
         if (ok) marker(-1);
         if (lane == 0) {
             if (!ok) {
                 // let copies that were issued land before the CTA's shared memory is given up
-                for (int s = 0; s < kFewStages; ++s) {
+                for (int s = 0; s < NST; ++s) {
                     const unsigned long long t0 = global_ns();
                     while (!mbar_try_wait(full_bar + 8 * s, 0) && !mbar_try_wait(full_bar + 8 * s, 1) && global_ns() - t0 < kWaitLimitNs / 8) {}
                 }
@@ -163,41 +201,39 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         }
     } else {
         // =============================== consumer warps ===============================
+        const int group = warp / kFewWarps, wi = warp % kFewWarps;
         const int gq = lane >> 2, qd = lane & 3;         // this thread's query row (and row + 8) and column pair
         // ldmatrix row addresses: lane l supplies row (l % 8) of matrix (l / 8)
-        const int kr = warp * 16 + ((lane >> 4) << 3) + (lane & 7);      // K: matrices 2,3 are the second 8 rows
+        const int kr = wi * 16 + ((lane >> 4) << 3) + (lane & 7);      // K: matrices 2,3 are the second 8 rows
         const int kc = (lane >> 3) & 1;                                  //    matrices 1,3 the second 8 columns
-        const int vr = warp * 16 + (((lane >> 3) & 1) << 3) + (lane & 7);  // V: matrices 1,3 are the second 8 rows
+        const int vr = wi * 16 + (((lane >> 3) & 1) << 3) + (lane & 7);  // V: matrices 1,3 are the second 8 rows
         const int vc = lane >> 4;                                        //    matrices 2,3 the next 8 columns
         const float scale2 = a.scale * kLog2e;
         const bool capped = md.softcap > 0.f;
         // capped: x = c tanh(o / c) = c - 2 c / (1 + e^{2 o / c}), all in the base-2 domain
         const float cap2 = md.softcap * kLog2e, cap_in = capped ? 2.f * kLog2e * a.scale / md.softcap : 0.f;
-        uint32_t it = 0, n_join = 0;
+        uint32_t it = 0, n_tile = 0, n_join = 0;
         int item = -1, b = 0, h = 0, u = 0;
         PairRange x = {};
         uint32_t qa[KS][4];
         float acc[NT][4];
         float m_run[RH], l_run[RH], q_pos[RH], slope2[RH];
-        int lim[RH], q_doc[RH], pos_ref = 0;
-        const int32_t* docs = nullptr;
-        const int32_t* poss = nullptr;
+        int lim[RH], q_doc[RH];
         for (;;) {
-            const uint32_t s = it % kFewStages;
-            warp_wait(full_bar + 8 * s, (it / kFewStages) & 1u, abort_flag);
+            const uint32_t s = it % NST;
+            warp_wait(full_bar + 8 * s, (it / NST) & 1u, abort_flag);
             if (warp_aborted(abort_flag)) break;
             ++it;
-            const int w = info[2 * s], tile = info[2 * s + 1];
+            const int w = info[s].x, tile = info[s].y;
             if (w < 0) break;
             if (w != item) {
                 item = w;
                 u = w; b = u / a.n_kv_heads; h = u % a.n_kv_heads;
                 x = pair_range(a, pl, u, 0);
-                docs = md.documents ? md.documents + int64_t(b) * md.doc_sb + int64_t(h) * md.doc_sh : nullptr;
-                poss = md.slopes && md.positions ? md.positions + int64_t(b) * md.pos_sb + int64_t(h) * md.pos_sh : nullptr;
-                // positions count from the last token's, so that near ones are exact in fp32
+                const int32_t* const docs = md.documents ? md.documents + int64_t(b) * md.doc_sb + int64_t(h) * md.doc_sh : nullptr;
+                const int32_t* const poss = md.slopes && md.positions ? md.positions + int64_t(b) * md.pos_sb + int64_t(h) * md.pos_sh : nullptr;
                 const int row_last = max(x.row0 + x.count - 1, 0);
-                pos_ref = md.slopes && x.rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
+                const int pos_ref = md.slopes && x.rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
 #pragma unroll
                 for (int rr = 0; rr < RH; ++rr) {
                     const int m = gq + 8 * rr, tok = m / G, head = h * G + m % G, r = x.row0 + tok;
@@ -223,21 +259,29 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                 for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
             }
             if (tile >= 0) {
-                const uint32_t k_s = base + s * kStageBytes, v_s = k_s + kTileBytes;
-                const int row_t = tile * kFewTile, row_w = row_t + warp * 16, r0 = row_w + 2 * qd;
-                // what the modifiers need to know of this thread's four keys, fetched before the products
-                int k_doc[4] = {0, 0, 0, 0}, k_pos[4] = {0, 0, 0, 0};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int t = r0 + (j & 1) + (j >> 1) * 8;
-                    if (docs && t < x.rows) k_doc[j] = docs[t];
-                    if (md.slopes) k_pos[j] = poss ? (t < x.rows ? poss[t] : pos_ref) : t;
+                if ((n_tile++ & 1u) != uint32_t(group)) {        // the other group's
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(empty_bar + 8 * s);
+                    continue;
                 }
+                const uint32_t k_s = base + s * kStageBytes, v_s = k_s + kTileBytes;
+                const int row_t = tile * kFewTile, row_w = row_t + wi * 16, r0 = row_w + 2 * qd;
+                // what the modifiers need to know of this thread's four keys
+                const float* const mp = reinterpret_cast<const float*>(base_ptr + Shape::kMeta + s * kFewTile * 8) + wi * 16 + 2 * qd;
+                float2 pos[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                int2 doc[2] = {make_int2(0, 0), make_int2(0, 0)};
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (md.slopes) pos[j] = *reinterpret_cast<const float2*>(mp + 8 * j);
+                    if (md.documents) doc[j] = *reinterpret_cast<const int2*>(mp + kFewTile + 8 * j);
+                }
+                const float k_pos[4] = {pos[0].x, pos[0].y, pos[1].x, pos[1].y};
+                const int k_doc[4] = {doc[0].x, doc[0].y, doc[1].x, doc[1].y};
                 if (row_w + 16 > x.rows) {
                     // Rows past the end hold whatever the cache holds: their weights are zero, but zero times a
                     // non-finite value is not, so clear this warp's value rows beyond the end.
                     for (int j = lane; j < 16 * NH * 8; j += 32) {
-                        const int r = warp * 16 + j / (NH * 8), c = j % (NH * 8);
+                        const int r = wi * 16 + j / (NH * 8), c = j % (NH * 8);
                         if (row_t + r >= x.rows)
                             *reinterpret_cast<uint4*>(base_ptr + (v_s - base) + (c >> 3) * kFewBlock + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
                                 make_uint4(0, 0, 0, 0);
@@ -262,8 +306,8 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                     for (int j = 0; j < 4; ++j) {
                         const int t = r0 + (j & 1) + (j >> 1) * 8;
                         xs[j] = capped ? fmaf(-2.f * cap2, rcpf(1.f + ex2f(xs[j] * cap_in)), cap2) : xs[j] * scale2;
-                        if (md.slopes) xs[j] = fmaf(-slope2[rr], fabsf(q_pos[rr] - float(k_pos[j] - pos_ref)), xs[j]);
-                        const bool sees = t <= lim[rr] && t < x.rows && (!docs || k_doc[j] == q_doc[rr]);
+                        if (md.slopes) xs[j] = fmaf(-slope2[rr], fabsf(q_pos[rr] - k_pos[j]), xs[j]);
+                        const bool sees = t <= lim[rr] && t < x.rows && (!md.documents || k_doc[j] == q_doc[rr]);
                         xs[j] = sees ? xs[j] : kNeg;
                     }
                     float mx = fmaxf(fmaxf(xs[0], xs[1]), fmaxf(xs[2], xs[3]));
@@ -303,31 +347,53 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                 if (lane == 0) mbar_arrive(empty_bar + 8 * s);
                 continue;
             }
-            // ---- end of the item: this warp's rows to shared memory, then the four warps' results joined in order
+            // ---- end of the item: the second group's warps hand their rows to the first's, whose joined results then go
+            // to shared memory once more and are joined in order by all eight
             __syncwarp();
             if (lane == 0) mbar_arrive(empty_bar + 8 * s);
-            // everybody has read what the previous item left there
-            if (n_join > 0) warp_wait(join_bar, (n_join - 1u) & 1u, abort_flag);
+            auto join = [&] {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(join_bar);
+                warp_wait(join_bar, n_join++ & 1u, abort_flag);
+            };
 #pragma unroll
             for (int rr = 0; rr < RH; ++rr) {
                 l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 1);
                 l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 2);
-                float* const mine = merge + (warp * R + gq + 8 * rr) * (D + 2);
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    *reinterpret_cast<float2*>(mine + t * 8 + 2 * qd) = make_float2(acc[t][2 * rr], acc[t][2 * rr + 1]);
-                if (qd == 0) *reinterpret_cast<float2*>(mine + D) = make_float2(m_run[rr], l_run[rr]);
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(join_bar);
-            warp_wait(join_bar, n_join & 1u, abort_flag);
-            n_join += 2;
+#pragma unroll
+            for (int turn = 1; turn >= 0; --turn) {
+                if (group == turn) {
+#pragma unroll
+                    for (int rr = 0; rr < RH; ++rr) {
+                        float* const mine = merge + (wi * R + gq + 8 * rr) * (D + 2);
+                        if (turn == 0) {                 // what the second group left here
+                            const float2 st = *reinterpret_cast<const float2*>(mine + D);
+                            const float mm = fmaxf(m_run[rr], st.x), w0 = ex2f(m_run[rr] - mm), w1 = ex2f(st.x - mm);
+                            l_run[rr] = l_run[rr] * w0 + st.y * w1;
+                            m_run[rr] = mm;
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) {
+                                const float2 y = *reinterpret_cast<const float2*>(mine + t * 8 + 2 * qd);
+                                acc[t][2 * rr] = acc[t][2 * rr] * w0 + y.x * w1;
+                                acc[t][2 * rr + 1] = acc[t][2 * rr + 1] * w0 + y.y * w1;
+                            }
+                            __syncwarp();                // all lanes of the row have read its reference and sum
+                        }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+                            *reinterpret_cast<float2*>(mine + t * 8 + 2 * qd) = make_float2(acc[t][2 * rr], acc[t][2 * rr + 1]);
+                        if (qd == 0) *reinterpret_cast<float2*>(mine + D) = make_float2(m_run[rr], l_run[rr]);
+                    }
+                }
+                join();
+            }
             // the item is whole, or this is the rest (partial result 2 c) or the beginning (2 c + 1) of a cut one
             const int part_slot = u == share.item0 && share.tile0 > 0 ? 2 * int(blockIdx.x)
                                   : u == share.item1 && share.tile1 < x.tiles ? 2 * int(blockIdx.x) + 1 : -1;
             const bool final = part_slot < 0;
-            constexpr int C = D / 32;                    // columns per lane: a warp takes every fourth row
-            for (int m = warp; m < x.count * G; m += kFewWarps) {
+            constexpr int C = D / 32;                    // columns per lane: a warp takes every eighth row
+            for (int m = warp; m < x.count * G; m += kFewConsumers) {
                 float2 st[kFewWarps];
                 float mm = kNeg;
 #pragma unroll
@@ -368,8 +434,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                     if (lane == 0) partial_ml[slot] = make_float2(mm, l);
                 }
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(join_bar);        // waited for before the area is written again
+            join();                                      // the area is free again
         }
     }
 }
