@@ -157,7 +157,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         PairRange next = {};
         int next_page = 0;                               // lane l: page of the next item's tile l (of its first 32)
         auto look_up = [&](int item) {
-            if (item > share.item1 || item >= pl.n_items) return;
+            if (item > share.item1 || (item == share.item1 && share.tile1 == 0 && !drawn) || item >= pl.n_items) return;
             const int u = item / pl.n_pairs;
             next = pair_range(a, pl, u, item - u * pl.n_pairs);
             const int tile = (item == share.item0 ? share.tile0 : 0) + lane;
@@ -298,10 +298,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     ok = ok && !warp_aborted(abort_flag);
                     if (ok && lane == 0) {
                         mbar_expect_tx(kv_full + 8 * s, kStageBytes);
-#pragma unroll
-                        for (int hb = 0; hb < NH; ++hb)
-                            tma_load_4d(base + s * kStageBytes + hb * kBlockBytes, which ? &tmap_v : &tmap_k, kv_full + 8 * s, hb * 64,
-                                        row, h, outer);
+                        tma_load_5d(base + s * kStageBytes, which ? &tmap_v : &tmap_k, kv_full + 8 * s, 0, row, 0, h, outer);
                     }
                 }
                 // Q goes behind the first two tiles (which need no more than four stages) if its slot is still in use
@@ -727,13 +724,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps) chunk_join_kernel(const Chunk
     // partial results 2 c0 + 1, 2 (c0 + 1), 2 (c0 + 2), ...
     auto slot = [&](int s) { return int64_t(2 * (c0 + s) + (s == 0 ? 1 : 0)) * pl.row_slots; };
     float m = kNeg;
-#pragma unroll 4
+#pragma unroll 8
     for (int s = 0; s < n_parts; ++s) m = fmaxf(m, partial_ml[slot(s) + row].x);
     float l = 0.f;
     float4 o[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) o[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
+#pragma unroll 4
     for (int s = 0; s < n_parts; ++s) {
         const float2 p = partial_ml[slot(s) + row];
         const float w = ex2f(p.x - m);
@@ -837,8 +834,8 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
     const int map_rows = pages ? pages->page_rows : (p.out_capacity > 0 ? p.out_capacity : 1);
     const int map_outer = pages ? pages->n_pages : p.batch;
     const int box_tokens = pl.tok_tile < a.max_new ? pl.tok_tile : a.max_new;
-    if (!make_cache_tensor_map(&tk, k, p.dtype, p.head_dim, map_rows, p.n_kv_heads, map_outer, pl.key_tile) ||
-        !make_cache_tensor_map(&tv, v, p.dtype, p.head_dim, map_rows, p.n_kv_heads, map_outer, pl.key_tile))
+    if (!make_cache_block_map(&tk, k, p.head_dim, map_rows, p.n_kv_heads, map_outer, pl.key_tile) ||
+        !make_cache_block_map(&tv, v, p.head_dim, map_rows, p.n_kv_heads, map_outer, pl.key_tile))
         return CSP_ERR_UNSUPPORTED;
     csp_status st;
     if (pl.row_slots <= kFewRows) {

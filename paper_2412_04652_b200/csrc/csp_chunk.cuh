@@ -77,6 +77,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& a, const ChunkPlan&
     const int per = (pl.n_items + kThreads - 1) / kThreads;
     const int i0 = min(tid * per, pl.n_items), i1 = min(i0 + per, pl.n_items);
     int mine = 0, tiles = 0;
+#pragma unroll 4
     for (int i = i0; i < i1; ++i) mine += item_weight(a, pl, i, blockIdx.x == 0, tiles);
     int x = mine;
 #pragma unroll

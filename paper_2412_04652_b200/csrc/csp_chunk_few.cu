@@ -11,8 +11,11 @@
 //   warps 0-3, 4-7  two groups that take turns, so that one computes while the other one's tile arrives.  A warp owns
 //               16 keys of its group's tiles: S = Q K^T, modifiers and mask, running softmax with a lazily raised
 //               reference, then P V with the weights as a bf16 head plus a bf16 remainder (two products per fragment),
-//               so that only the result is rounded to bf16.  At the end of an item the eight warps' results are
-//               joined in a fixed order; an undivided unit is finished here, a divided one leaves a partial result
+//               so that only the result is rounded to bf16.  At the end of an item they leave their results in
+//               shared memory and go on with the next one
+//   warp 9      joins the eight results of an item in a fixed order: a whole unit is finished here, a cut one leaves a
+//               partial result.  The query rows and what else an item needs come with its first stage, so that nobody
+//               waits for memory between items
 #include <limits.h>
 
 #include "csp_chunk.cuh"
@@ -24,7 +27,10 @@ using namespace dev;
 constexpr int kFewTile = 64;                             // keys per stage
 constexpr int kFewWarps = 4;                             // warps of a group, 16 keys of a tile each
 constexpr int kFewConsumers = 2 * kFewWarps;
-constexpr int kFewThreads = 32 * (kFewConsumers + 1);
+constexpr int kFewProducer = kFewConsumers, kFewFinisher = kFewConsumers + 1;
+constexpr int kFewThreads = 32 * (kFewConsumers + 2);
+constexpr int kItemWords = 8;                            // of a stage's info: see ItemWord
+enum ItemWord { kwItem, kwTile, kwRows, kwRow0, kwCount, kwPrefix, kwPart, kwPosRef };
 constexpr int kFewBlock = kFewTile * 128;                // bytes of one 64-column block of a tile
 
 struct FewQuery { const uint16_t* q; int64_t sb, sh, st; };
@@ -37,13 +43,14 @@ __device__ __forceinline__ void ldsm_x4_t(uint32_t (&r)[4], uint32_t addr) {
 template <int NH, int RH>
 struct FewShape {
     static constexpr int D = 64 * NH, R = 8 * RH;
-    static constexpr int kStages = NH == 2 && RH == 2 ? 5 : 6;                         // 32 KB each at d = 128
+    static constexpr int kStages = NH == 2 ? (RH == 2 ? 4 : 5) : (RH == 2 ? 7 : 8);                    // 32 KB each at d = 128
     static constexpr uint32_t kTileBytes = NH * kFewBlock, kStageBytes = 2 * kTileBytes;
-    static constexpr uint32_t kMerge = kStages * kStageBytes;                          // [warp of a group][R][D + 2] floats
-    static constexpr uint32_t kMeta = kMerge + kFewWarps * R * (D + 2) * 4;            // per stage: 64 positions, 64 documents
-    static constexpr uint32_t kBars = kMeta + kStages * kFewTile * 8;                  // full, empty, join
-    static constexpr uint32_t kInfo = kBars + (2 * kStages + 2) * 8;                   // int2 per stage: item, tile
-    static constexpr uint32_t kMisc = kInfo + kStages * 8;
+    static constexpr uint32_t kMerge = kStages * kStageBytes;                          // [warp][R][D + 2] floats
+    static constexpr uint32_t kQ = kMerge + kFewConsumers * R * (D + 2) * 4;           // per stage: R query rows
+    static constexpr uint32_t kMeta = kQ + kStages * R * D * 2;                        // per stage: 64 positions, 64 documents
+    static constexpr uint32_t kInfo = kMeta + kStages * kFewTile * 8;                  // per stage: what it holds; then: the item to finish
+    static constexpr uint32_t kBars = kInfo + (kStages + 1) * kItemWords * 4;          // full, empty, results there, results read
+    static constexpr uint32_t kMisc = kBars + (2 * kStages + 2) * 8;
     static constexpr uint32_t kTotal = kMisc + 16;
 };
 
@@ -61,8 +68,10 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
     float* const merge = reinterpret_cast<float*>(base_ptr + Shape::kMerge);
-    const uint32_t full_bar = base + Shape::kBars, empty_bar = full_bar + 8 * NST, join_bar = empty_bar + 8 * NST;
-    int2* const info = reinterpret_cast<int2*>(base_ptr + Shape::kInfo);
+    const uint32_t full_bar = base + Shape::kBars, empty_bar = full_bar + 8 * NST;
+    const uint32_t done_bar = empty_bar + 8 * NST, read_bar = done_bar + 8;
+    int32_t* const info = reinterpret_cast<int32_t*>(base_ptr + Shape::kInfo);
+    int32_t* const finish = info + NST * kItemWords;
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(base_ptr + Shape::kMisc);
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.group;
@@ -70,27 +79,30 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     if (tid == 0) {
         *abort_flag = 0;
         for (int s = 0; s < NST; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, kFewConsumers); }
-        mbar_init(join_bar, kFewConsumers);
+        mbar_init(done_bar, kFewConsumers);
+        mbar_init(read_bar, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     const Share share = find_share<kFewThreads>(a, pl, reinterpret_cast<int*>(merge));      // (synchronises)
     asm volatile("griddepcontrol.launch_dependents;");   // the joining kernel may get ready
 
-    if (warp == kFewConsumers) {
+    if (warp == kFewProducer) {
         // =============================== producer ===============================
         uint32_t it = 0;
         bool ok = true;
+        int32_t word = 0;                                // lane l: word l of the current item's info
         auto stage = [&](int item, int tile) {           // the next stage, free, with what it holds written beside it
             const uint32_t s = it % NST;
             warp_wait(empty_bar + 8 * s, ((it / NST) & 1u) ^ 1u, abort_flag);
             ok = ok && !warp_aborted(abort_flag);
-            if (ok && lane == 0) info[s] = make_int2(item, tile);
+            if (lane < kItemWords) info[s * kItemWords + lane] = lane == kwItem ? item : lane == kwTile ? tile : word;
             ++it;
             return s;
         };
         auto marker = [&](int item) {                    // a stage without data: the item has no more tiles (-1: no more items)
             const uint32_t s = stage(item, -1);
+            __syncwarp();
             if (ok && lane == 0) mbar_arrive(full_bar + 8 * s);
         };
         if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, -1, 0, 0};
@@ -98,13 +110,24 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         auto page_of = [&](int b, int tile) {            // the page of a tile that lies inside the cache
             return a.page_table[int64_t(b) * a.max_pages + uint32_t(tile) / tiles_per_page];
         };
+        constexpr int kQChunks = R * D / 8 / 32;
+        uint4 next_q[kQChunks];
         PairRange next = {};
         int next_page = 0;                               // lane l: page of the next item's tile l (of its first 32)
         auto look_up = [&](int u) {                      // while the current item streams
-            if (u > share.item1 || u >= pl.n_items) return;
+            if (u > share.item1 || (u == share.item1 && share.tile1 == 0) || u >= pl.n_items) return;
             next = pair_range(a, pl, u, 0);
             const int tile = (u == share.item0 ? share.tile0 : 0) + lane;
             if (a.page_table && next.count > 0 && tile < next.tiles) next_page = page_of(u / a.n_kv_heads, tile);
+            // the query rows: 16-byte chunk `lane + 32 j` of [row][d]; rows that are none are zeros
+            const int b = u / a.n_kv_heads, h = u % a.n_kv_heads;
+#pragma unroll
+            for (int j = 0; j < kQChunks; ++j) {
+                const int c = lane + 32 * j, m = c / (D / 8), tok = m / G;
+                next_q[j] = tok < next.count ? *reinterpret_cast<const uint4*>(qy.q + int64_t(b) * qy.sb + int64_t(h * G + m % G) * qy.sh +
+                                                                               int64_t(tok) * qy.st + c % (D / 8) * 8)
+                                             : make_uint4(0, 0, 0, 0);
+            }
         };
         look_up(share.item0);
         for (int u = share.item0; ok && u <= share.item1 && u < pl.n_items; ++u) {
@@ -140,7 +163,61 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                     p_now[j] = !md.slopes ? 0 : poss ? (t < x.rows ? poss[t] : pos_ref) : t;
                 }
             };
+            const int part_slot = tile0 > 0 ? 2 * int(blockIdx.x) : tile1 < x.tiles ? 2 * int(blockIdx.x) + 1 : -1;
+            switch (lane) {
+                case kwRows: word = x.rows; break;
+                case kwRow0: word = x.row0; break;
+                case kwCount: word = x.count; break;
+                case kwPrefix: word = x.prefix; break;
+                case kwPart: word = part_slot; break;
+                case kwPosRef: word = pos_ref; break;
+            }
+            auto put_q = [&](uint32_t s) {
+#pragma unroll
+                for (int j = 0; j < kQChunks; ++j) *reinterpret_cast<uint4*>(base_ptr + Shape::kQ + s * R * D * 2 + (lane + 32 * j) * 16) = next_q[j];
+            };
             bool looked = false;
+            if (!meta) {
+                // Without positions and documents one lane does everything from the second tile on: at the full rate of HBM a
+                // tile is due every 1400 clocks, and the steps below take a whole warp as long as that.
+                auto load = [&](uint32_t s, int tile, int outer) {
+                    mbar_expect_tx(full_bar + 8 * s, kStageBytes);
+                    const int row = a.page_table ? int(uint32_t(tile) % tiles_per_page) * kFewTile : tile * kFewTile;
+                    tma_load_5d(base + s * kStageBytes, &tmap_k, full_bar + 8 * s, 0, row, 0, h, outer);
+                    tma_load_5d(base + s * kStageBytes + kTileBytes, &tmap_v, full_bar + 8 * s, 0, row, 0, h, outer);
+                };
+                auto checked = [&](int page) {           // outside the pool: an out-of-range coordinate, zeros arrive
+                    if (uint32_t(page) < uint32_t(a.n_pages)) return page;
+                    atomicOr(a.status, CSP_DEV_BAD_LEN);
+                    return a.n_pages;
+                };
+                if (tile0 < tile1) {
+                    const uint32_t s = stage(u, tile0);
+                    put_q(s);
+                    __syncwarp();
+                    if (ok && lane == 0) load(s, tile0, a.page_table ? checked(pages) : b);
+                    looked = true;
+                }
+                const bool elected = elect_one();
+                if (elected && ok) {
+                    int page = a.page_table && tile0 + 1 < tile1 ? page_of(b, tile0 + 1) : 0;
+                    for (int tile = tile0 + 1; tile < tile1; ++tile) {
+                        const uint32_t n = it + uint32_t(tile - tile0 - 1), s = n % NST;
+                        const int outer = a.page_table ? checked(page) : b;
+                        if (a.page_table && tile + 1 < tile1) page = page_of(b, tile + 1);        // in time for the next tile
+                        lean_wait(empty_bar + 8 * s, ((n / NST) & 1u) ^ 1u, abort_flag);
+                        if (*abort_flag) break;
+                        *reinterpret_cast<int2*>(info + s * kItemWords) = make_int2(u, tile);
+                        load(s, tile, outer);
+                    }
+                }
+                it += uint32_t(max(tile1 - tile0 - 1, 0));
+                look_up(u + 1);
+                __syncwarp();
+                ok = ok && !warp_aborted(abort_flag);
+                marker(u);
+                continue;
+            }
             for (int tile = tile0; tile < tile1 && ok; ++tile) {
                 const int turn = (tile - tile0) & 3;
                 if (meta && turn == 0) fetch_meta(tile);
@@ -166,6 +243,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                     row = int(uint32_t(tile) % tiles_per_page) * kFewTile;
                 }
                 const uint32_t s = stage(u, tile);
+                if (!looked) put_q(s);
                 if (meta) {
                     float* const mp = reinterpret_cast<float*>(base_ptr + Shape::kMeta + s * kFewTile * 8);
 #pragma unroll
@@ -173,15 +251,12 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                         mp[lane + 32 * j] = float(pp[j] - pos_ref);
                         reinterpret_cast<int32_t*>(mp)[kFewTile + lane + 32 * j] = dd[j];
                     }
-                    __syncwarp();
                 }
+                __syncwarp();
                 if (ok && lane == 0) {
                     mbar_expect_tx(full_bar + 8 * s, kStageBytes);
-#pragma unroll
-                    for (int hb = 0; hb < NH; ++hb) {
-                        tma_load_4d(base + s * kStageBytes + hb * kFewBlock, &tmap_k, full_bar + 8 * s, hb * 64, row, h, outer);
-                        tma_load_4d(base + s * kStageBytes + kTileBytes + hb * kFewBlock, &tmap_v, full_bar + 8 * s, hb * 64, row, h, outer);
-                    }
+                    tma_load_5d(base + s * kStageBytes, &tmap_k, full_bar + 8 * s, 0, row, 0, h, outer);
+                    tma_load_5d(base + s * kStageBytes + kTileBytes, &tmap_v, full_bar + 8 * s, 0, row, 0, h, outer);
                 }
                 if (!looked) { look_up(u + 1); looked = true; }
             }
@@ -199,6 +274,60 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                 atomicOr(a.status, CSP_DEV_TIMEOUT);
             }
         }
+    } else if (warp == kFewFinisher) {
+        // =============================== finisher ===============================
+        for (uint32_t n = 0;; ++n) {
+            warp_wait(done_bar, n & 1u, abort_flag);
+            if (warp_aborted(abort_flag)) break;
+            const int u = finish[kwItem], count = finish[kwCount], part_slot = finish[kwPart];
+            if (u < 0) break;
+            const int b = u / a.n_kv_heads, h = u % a.n_kv_heads;
+            const bool final = part_slot < 0;
+            constexpr int C = D / 32;                    // columns per lane
+            for (int m = 0; m < count * G; ++m) {
+                float2 st[kFewConsumers];
+                float mm = kNeg;
+#pragma unroll
+                for (int ww = 0; ww < kFewConsumers; ++ww) {
+                    st[ww] = *reinterpret_cast<const float2*>(merge + (ww * R + m) * (D + 2) + D);
+                    mm = fmaxf(mm, st[ww].x);
+                }
+                float l = 0.f, o[C];
+#pragma unroll
+                for (int c = 0; c < C; ++c) o[c] = 0.f;
+#pragma unroll
+                for (int ww = 0; ww < kFewConsumers; ++ww) {
+                    const float wgt = ex2f(st[ww].x - mm);
+                    l += st[ww].y * wgt;
+#pragma unroll
+                    for (int c = 0; c < C; c += 2) {
+                        const float2 y = *reinterpret_cast<const float2*>(merge + (ww * R + m) * (D + 2) + lane * C + c);
+                        o[c] += y.x * wgt;
+                        o[c + 1] += y.y * wgt;
+                    }
+                }
+                const int tok = m / G, head = h * G + m % G;
+                if (final) {
+                    const float inv = l == 0.f ? 0.f : 1.f / (a.n * ex2f(-mm) + l);      // l == 0: nothing was seen
+                    uint32_t* const out = reinterpret_cast<uint32_t*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st + lane * C);
+#pragma unroll
+                    for (int c = 0; c < C; c += 2) out[c / 2] = l == 0.f ? 0u : pack_bf16(o[c] * inv, o[c + 1] * inv);
+                    if (a.lse && lane == 0)
+                        a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
+                } else {
+                    const int64_t slot = int64_t(part_slot) * pl.row_slots;
+#pragma unroll
+                    for (int c = 0; c < C; c += 2) {     // laid out [column / 4][row][4]
+                        const int col = lane * C + c;
+                        *reinterpret_cast<float2*>(partial + (slot * (D / 4) + int64_t(col / 4) * pl.row_slots + m) * 4 + col % 4) =
+                            make_float2(o[c], o[c + 1]);
+                    }
+                    if (lane == 0) partial_ml[slot + m] = make_float2(mm, l);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(read_bar);        // the area may be written again
+        }
     } else {
         // =============================== consumer warps ===============================
         const int group = warp / kFewWarps, wi = warp % kFewWarps;
@@ -212,9 +341,8 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         const bool capped = md.softcap > 0.f;
         // capped: x = c tanh(o / c) = c - 2 c / (1 + e^{2 o / c}), all in the base-2 domain
         const float cap2 = md.softcap * kLog2e, cap_in = capped ? 2.f * kLog2e * a.scale / md.softcap : 0.f;
-        uint32_t it = 0, n_tile = 0, n_join = 0;
-        int item = -1, b = 0, h = 0, u = 0;
-        PairRange x = {};
+        uint32_t it = 0, n_tile = 0, n_done = 0;
+        int item = -1, rows = 0;
         uint32_t qa[KS][4];
         float acc[NT][4];
         float m_run[RH], l_run[RH], q_pos[RH], slope2[RH];
@@ -224,29 +352,27 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
             warp_wait(full_bar + 8 * s, (it / NST) & 1u, abort_flag);
             if (warp_aborted(abort_flag)) break;
             ++it;
-            const int w = info[s].x, tile = info[s].y;
-            if (w < 0) break;
-            if (w != item) {
+            const int32_t* const in = info + s * kItemWords;
+            const int w = in[kwItem], tile = in[kwTile];
+            if (w != item && w >= 0) {
                 item = w;
-                u = w; b = u / a.n_kv_heads; h = u % a.n_kv_heads;
-                x = pair_range(a, pl, u, 0);
+                rows = in[kwRows];
+                const int row0 = in[kwRow0], count = in[kwCount], b = w / a.n_kv_heads, h = w % a.n_kv_heads;
                 const int32_t* const docs = md.documents ? md.documents + int64_t(b) * md.doc_sb + int64_t(h) * md.doc_sh : nullptr;
                 const int32_t* const poss = md.slopes && md.positions ? md.positions + int64_t(b) * md.pos_sb + int64_t(h) * md.pos_sh : nullptr;
-                const int row_last = max(x.row0 + x.count - 1, 0);
-                const int pos_ref = md.slopes && x.rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
 #pragma unroll
                 for (int rr = 0; rr < RH; ++rr) {
-                    const int m = gq + 8 * rr, tok = m / G, head = h * G + m % G, r = x.row0 + tok;
-                    const bool valid = tok < x.count, sees = valid && r >= 0;
-                    const uint16_t* const qrow = qy.q + int64_t(b) * qy.sb + int64_t(head) * qy.sh + int64_t(tok) * qy.st;
+                    const int m = gq + 8 * rr, tok = m / G, head = h * G + m % G, r = row0 + tok;
+                    const bool valid = tok < count, sees = valid && r >= 0;
+                    const uint32_t* const qrow = reinterpret_cast<const uint32_t*>(base_ptr + Shape::kQ + s * R * D * 2 + m * D * 2);
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) {
-                        qa[ks][rr] = valid ? *reinterpret_cast<const uint32_t*>(qrow + ks * 16 + 2 * qd) : 0u;
-                        qa[ks][rr + 2] = valid ? *reinterpret_cast<const uint32_t*>(qrow + ks * 16 + 8 + 2 * qd) : 0u;
+                        qa[ks][rr] = qrow[ks * 8 + qd];
+                        qa[ks][rr + 2] = qrow[ks * 8 + 4 + qd];
                     }
-                    lim[rr] = !valid ? kSeesAll : sees ? max(r, x.prefix - 1) : -1;
+                    lim[rr] = !valid ? kSeesAll : sees ? max(r, in[kwPrefix] - 1) : -1;
                     q_doc[rr] = docs && sees ? docs[r] : 0;
-                    q_pos[rr] = md.slopes && sees ? float((poss ? poss[r] : r) - pos_ref) : 0.f;
+                    q_pos[rr] = md.slopes && sees ? float((poss ? poss[r] : r) - in[kwPosRef]) : 0.f;
                     slope2[rr] = md.slopes && sees ? md.slopes[head] * kLog2e : 0.f;
                     m_run[rr] = kNeg;
                     l_run[rr] = 0.f;
@@ -277,12 +403,12 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                 }
                 const float k_pos[4] = {pos[0].x, pos[0].y, pos[1].x, pos[1].y};
                 const int k_doc[4] = {doc[0].x, doc[0].y, doc[1].x, doc[1].y};
-                if (row_w + 16 > x.rows) {
+                if (row_w + 16 > rows) {
                     // Rows past the end hold whatever the cache holds: their weights are zero, but zero times a
                     // non-finite value is not, so clear this warp's value rows beyond the end.
                     for (int j = lane; j < 16 * NH * 8; j += 32) {
                         const int r = wi * 16 + j / (NH * 8), c = j % (NH * 8);
-                        if (row_t + r >= x.rows)
+                        if (row_t + r >= rows)
                             *reinterpret_cast<uint4*>(base_ptr + (v_s - base) + (c >> 3) * kFewBlock + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
                                 make_uint4(0, 0, 0, 0);
                     }
@@ -307,7 +433,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                         const int t = r0 + (j & 1) + (j >> 1) * 8;
                         xs[j] = capped ? fmaf(-2.f * cap2, rcpf(1.f + ex2f(xs[j] * cap_in)), cap2) : xs[j] * scale2;
                         if (md.slopes) xs[j] = fmaf(-slope2[rr], fabsf(q_pos[rr] - k_pos[j]), xs[j]);
-                        const bool sees = t <= lim[rr] && t < x.rows && (!md.documents || k_doc[j] == q_doc[rr]);
+                        const bool sees = t <= lim[rr] && t < rows && (!md.documents || k_doc[j] == q_doc[rr]);
                         xs[j] = sees ? xs[j] : kNeg;
                     }
                     float mx = fmaxf(fmaxf(xs[0], xs[1]), fmaxf(xs[2], xs[3]));
@@ -342,99 +468,28 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                     mma_bf16(acc[t + 1], ph, vb[2], vb[3]);
                     mma_bf16(acc[t + 1], pr, vb[2], vb[3]);
                 }
-                if (row_w + 16 > x.rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                if (row_w + 16 > rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(empty_bar + 8 * s);
                 continue;
             }
-            // ---- end of the item: the second group's warps hand their rows to the first's, whose joined results then go
-            // to shared memory once more and are joined in order by all eight
-            __syncwarp();
-            if (lane == 0) mbar_arrive(empty_bar + 8 * s);
-            auto join = [&] {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(join_bar);
-                warp_wait(join_bar, n_join++ & 1u, abort_flag);
-            };
+            // ---- end of the item: this warp's rows to shared memory, once the finisher has read the previous ones
+            if (n_done > 0) warp_wait(read_bar, (n_done - 1u) & 1u, abort_flag);
 #pragma unroll
             for (int rr = 0; rr < RH; ++rr) {
                 l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 1);
                 l_run[rr] += __shfl_xor_sync(0xffffffffu, l_run[rr], 2);
+                float* const mine = merge + (warp * R + gq + 8 * rr) * (D + 2);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    *reinterpret_cast<float2*>(mine + t * 8 + 2 * qd) = make_float2(acc[t][2 * rr], acc[t][2 * rr + 1]);
+                if (qd == 0) *reinterpret_cast<float2*>(mine + D) = make_float2(m_run[rr], l_run[rr]);
             }
-#pragma unroll
-            for (int turn = 1; turn >= 0; --turn) {
-                if (group == turn) {
-#pragma unroll
-                    for (int rr = 0; rr < RH; ++rr) {
-                        float* const mine = merge + (wi * R + gq + 8 * rr) * (D + 2);
-                        if (turn == 0) {                 // what the second group left here
-                            const float2 st = *reinterpret_cast<const float2*>(mine + D);
-                            const float mm = fmaxf(m_run[rr], st.x), w0 = ex2f(m_run[rr] - mm), w1 = ex2f(st.x - mm);
-                            l_run[rr] = l_run[rr] * w0 + st.y * w1;
-                            m_run[rr] = mm;
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) {
-                                const float2 y = *reinterpret_cast<const float2*>(mine + t * 8 + 2 * qd);
-                                acc[t][2 * rr] = acc[t][2 * rr] * w0 + y.x * w1;
-                                acc[t][2 * rr + 1] = acc[t][2 * rr + 1] * w0 + y.y * w1;
-                            }
-                            __syncwarp();                // all lanes of the row have read its reference and sum
-                        }
-#pragma unroll
-                        for (int t = 0; t < NT; ++t)
-                            *reinterpret_cast<float2*>(mine + t * 8 + 2 * qd) = make_float2(acc[t][2 * rr], acc[t][2 * rr + 1]);
-                        if (qd == 0) *reinterpret_cast<float2*>(mine + D) = make_float2(m_run[rr], l_run[rr]);
-                    }
-                }
-                join();
-            }
-            // the item is whole, or this is the rest (partial result 2 c) or the beginning (2 c + 1) of a cut one
-            const int part_slot = u == share.item0 && share.tile0 > 0 ? 2 * int(blockIdx.x)
-                                  : u == share.item1 && share.tile1 < x.tiles ? 2 * int(blockIdx.x) + 1 : -1;
-            const bool final = part_slot < 0;
-            constexpr int C = D / 32;                    // columns per lane: a warp takes every eighth row
-            for (int m = warp; m < x.count * G; m += kFewConsumers) {
-                float2 st[kFewWarps];
-                float mm = kNeg;
-#pragma unroll
-                for (int ww = 0; ww < kFewWarps; ++ww) {
-                    st[ww] = *reinterpret_cast<const float2*>(merge + (ww * R + m) * (D + 2) + D);
-                    mm = fmaxf(mm, st[ww].x);
-                }
-                float l = 0.f, o[C];
-#pragma unroll
-                for (int c = 0; c < C; ++c) o[c] = 0.f;
-#pragma unroll
-                for (int ww = 0; ww < kFewWarps; ++ww) {
-                    const float wgt = ex2f(st[ww].x - mm);
-                    l += st[ww].y * wgt;
-#pragma unroll
-                    for (int c = 0; c < C; c += 2) {
-                        const float2 y = *reinterpret_cast<const float2*>(merge + (ww * R + m) * (D + 2) + lane * C + c);
-                        o[c] += y.x * wgt;
-                        o[c + 1] += y.y * wgt;
-                    }
-                }
-                const int tok = m / G, head = h * G + m % G;
-                if (final) {
-                    const float inv = l == 0.f ? 0.f : 1.f / (a.n * ex2f(-mm) + l);      // l == 0: nothing was seen
-                    uint32_t* const out = reinterpret_cast<uint32_t*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st + lane * C);
-#pragma unroll
-                    for (int c = 0; c < C; c += 2) out[c / 2] = l == 0.f ? 0u : pack_bf16(o[c] * inv, o[c + 1] * inv);
-                    if (a.lse && lane == 0)
-                        a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
-                } else {
-                    const int64_t slot = int64_t(part_slot) * pl.row_slots + m;
-#pragma unroll
-                    for (int c = 0; c < C; c += 2) {     // laid out [column / 4][row][4]
-                        const int col = lane * C + c;
-                        *reinterpret_cast<float2*>(partial + ((slot - m) * (D / 4) + int64_t(col / 4) * pl.row_slots + m) * 4 + col % 4) =
-                            make_float2(o[c], o[c + 1]);
-                    }
-                    if (lane == 0) partial_ml[slot] = make_float2(mm, l);
-                }
-            }
-            join();                                      // the area is free again
+            if (warp == 0 && lane < kItemWords) finish[lane] = in[lane];
+            ++n_done;
+            __syncwarp();
+            if (lane == 0) { mbar_arrive(done_bar); mbar_arrive(empty_bar + 8 * s); }
+            if (w < 0) break;                            // no more items: the finisher reads that too
         }
     }
 }

@@ -170,6 +170,10 @@ csp_status launch_select_compact(const csp_params& p, const SelectArgs& sa, cons
 bool make_cache_tensor_map(CUtensorMap* map, const csp_tensor& t, int dtype, int head_dim, int rows, int heads,
                            int batch, int box_rows);
 
+// 5-D tensor map over a bf16 cache [batch, heads, rows, head_dim] whose boxes hold box_rows whole rows as blocks of 64
+// columns, one behind the other: coordinates (0, row, 0, head, batch)
+bool make_cache_block_map(CUtensorMap* map, const csp_tensor& t, int head_dim, int rows, int heads, int batch, int box_rows);
+
 // 4-D tensor map over bf16 queries [batch, heads, tokens, head_dim] whose boxes hold 64 columns of box_tokens tokens, the
 // box_heads heads of a token as neighbouring rows
 bool make_query_tensor_map(CUtensorMap* map, const csp_tensor& t, int head_dim, int heads, int tokens, int batch,

@@ -584,6 +584,22 @@ bool make_cache_tensor_map(CUtensorMap* map, const csp_tensor& t, int dtype, int
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_cache_block_map(CUtensorMap* map, const csp_tensor& t, int head_dim, int rows, int heads, int batch, int box_rows) {
+    EncodeTiledFn encode = encode_tiled_fn();
+    if (!encode) return false;
+    const uint64_t st = uint64_t(t.stride_t) * 2;
+    const uint64_t sh = heads > 1 ? uint64_t(t.stride_h) * 2 : st * uint64_t(rows);
+    const uint64_t sb = batch > 1 ? uint64_t(t.stride_b) * 2 : sh * uint64_t(heads);
+    if (t.stride_t < head_dim || (st % 16) || (sh % 16) || (sb % 16) || (uintptr_t(t.ptr) % 16)) return false;
+    const cuuint32_t blocks = cuuint32_t(head_dim / 64);
+    const cuuint64_t dims[5] = {64, cuuint64_t(rows), blocks, cuuint64_t(heads), cuuint64_t(batch)};
+    const cuuint64_t strides[4] = {st, 128, sh, sb};
+    const cuuint32_t box[5] = {64, cuuint32_t(box_rows), blocks, 1, 1};
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, t.ptr, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool make_query_tensor_map(CUtensorMap* map, const csp_tensor& t, int head_dim, int heads, int tokens, int batch,
                            int box_heads, int box_tokens) {
     EncodeTiledFn encode = encode_tiled_fn();

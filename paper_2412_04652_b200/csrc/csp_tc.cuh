@@ -105,13 +105,6 @@ __device__ __forceinline__ void tc_ld_16x16(uint32_t (&v)[8], uint32_t taddr) {
 }
 __device__ __forceinline__ void tc_ld_frag(uint32_t (&v)[16], uint32_t taddr) { tc_ld_16x32(v, taddr); }
 __device__ __forceinline__ void tc_ld_frag(uint32_t (&v)[8], uint32_t taddr) { tc_ld_16x16(v, taddr); }
-// one lane of a converged warp, the same every time; unlike a test of the lane number it lets the compiler keep what the
-// lane works with in uniform registers, where the tcgen05 instructions want it
-__device__ __forceinline__ bool elect_one() {
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
-    return r != 0;
-}
 // shared-memory matrix descriptor: K-major operand, 128-byte swizzle, 8-row groups 1024 bytes apart
 __device__ __forceinline__ uint64_t sw128_desc(uint32_t smem_addr) {
     uint64_t d = uint64_t((smem_addr & 0x3FFFFu) >> 4);
