@@ -87,9 +87,13 @@ class Params:
     head_reduce: int = HEADS_PER_KV
 
     def c(self) -> CParams:
-        return CParams(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.window,
-                       self.recent, self.max_len, self.out_capacity, self.dtype, self.n, self.scale,
-                       self.combine, self.select_mode, self.head_reduce)
+        now = (self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.window,
+               self.recent, self.max_len, self.out_capacity, self.dtype, self.n, self.scale,
+               self.combine, self.select_mode, self.head_reduce)
+        made = self.__dict__.get("_made")               # the struct of the last call, while nothing has changed
+        if made is None or made[0] != now:
+            made = self.__dict__["_made"] = (now, CParams(*now))
+        return made[1]
 
 
 @dataclass
@@ -139,13 +143,13 @@ class PageState:
     page_rows: int
 
     def c(self) -> CPageState:
-        for t in (self.page_table, self.held, self.refs, self.n_rows):
-            assert t.dtype == torch.int32 and t.is_contiguous()
-        assert self.page_table.dim() == 2 and self.n_rows.dim() == 2
-        assert self.held.numel() == self.page_table.shape[0] == self.n_rows.shape[0]
-        return CPageState(self.page_table.data_ptr(), self.held.data_ptr(), self.refs.data_ptr(), self.n_rows.data_ptr(),
-                          self.page_table.shape[0], self.n_rows.shape[1], self.page_table.shape[1], self.page_rows,
-                          self.refs.numel())
+        table, held, refs, rows = self.page_table, self.held, self.refs, self.n_rows
+        for t in (table, held, refs, rows):
+            assert t.dtype is torch.int32 and t.is_contiguous()
+        ts, rs = table.shape, rows.shape
+        assert len(ts) == 2 and len(rs) == 2 and held.numel() == ts[0] == rs[0]
+        return CPageState(table.data_ptr(), held.data_ptr(), refs.data_ptr(), rows.data_ptr(), ts[0], rs[1], ts[1],
+                          self.page_rows, refs.numel())
 
 
 def new_page_state(batch: int, n_heads: int, max_pages: int, page_rows: int, n_pages: int, device="cuda") -> PageState:
@@ -256,17 +260,18 @@ def _check(code: int, where: str):
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else C.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return torch.cuda.current_stream().cuda_stream
 
 
 def tensor4(t: torch.Tensor) -> CTensor:
     """[B, H, T, d] tensor -> (pointer, element strides); the last axis must be contiguous."""
-    assert t.dim() == 4 and (t.stride(3) == 1 or t.shape[3] == 1), "head_dim axis must be contiguous"
-    return CTensor(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    s = t.stride()
+    assert len(s) == 4 and (s[3] == 1 or t.shape[3] == 1), "head_dim axis must be contiguous"
+    return CTensor(t.data_ptr(), s[0], s[1], s[2])
 
 
 def _mod_strides(modality: torch.Tensor):
@@ -430,17 +435,18 @@ def decode_attn_paged(p: Params, q, k_pool, v_pool, page_table, n_rows, out, ws)
 
 
 def _here(*tensors):
-    """The kernels run on the current device and stream: refuses tensors that live elsewhere."""
-    dev = torch.device("cuda", torch.cuda.current_device())
+    """The kernels run on the current device: refuses tensors that live elsewhere."""
+    dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensor on {t.device}, but the current device is {dev}")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{dev}")
 
 
 def _counts(t: Optional[torch.Tensor], shape):
-    assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == tuple(shape)), \
-        f"int32 tensor of shape {tuple(shape)} expected"
-    return _ptr(t)
+    if t is None:
+        return None
+    assert t.dtype is torch.int32 and t.shape == shape and t.is_contiguous(), f"int32 tensor of shape {tuple(shape)} expected"
+    return t.data_ptr()
 
 
 def _status_workspace(n: int, where: str, device) -> torch.Tensor:
@@ -460,14 +466,14 @@ def new_chunk_workspace(p: Params, max_new: int, device="cuda") -> torch.Tensor:
 
 
 def _chunk_args(p: Params, q, k, v, n_rows, out, ws, n_new, mods, lse):
-    _here(q, k, v, n_rows, out, ws, n_new, lse, *(mods.tensors() if mods is not None else []))
-    T = q.shape[2] if q.dim() == 4 else -1
-    want = (p.batch, p.n_q_heads, T, p.head_dim)
-    assert tuple(q.shape) == want and tuple(out.shape) == want, f"q and out: [B, Hq, new tokens, d] = {want}"
-    assert all(t.dtype == torch.bfloat16 for t in (q, k, v, out)), "bf16 tensors expected"
-    assert k.shape[1] == v.shape[1] == p.n_kv_heads and k.shape[3] == v.shape[3] == p.head_dim
-    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == want[:3])
-    return T, _counts(n_rows, (p.batch, p.n_kv_heads)), _counts(n_new, (p.batch,)), \
+    _here(q, k, v, n_rows, out, ws, n_new, lse, *(mods.tensors() if mods is not None else ()))
+    shape, ks, vs, bf16 = q.shape, k.shape, v.shape, torch.bfloat16
+    assert len(shape) == 4 and shape[0] == p.batch and shape[1] == p.n_q_heads and shape[3] == p.head_dim and out.shape == shape, \
+        f"q and out: [B, Hq, new tokens, d] = ({p.batch}, {p.n_q_heads}, new tokens, {p.head_dim})"
+    assert q.dtype is bf16 and k.dtype is bf16 and v.dtype is bf16 and out.dtype is bf16, "bf16 tensors expected"
+    assert ks[1] == vs[1] == p.n_kv_heads and ks[3] == vs[3] == p.head_dim
+    assert lse is None or (lse.dtype is torch.float32 and lse.shape == shape[:3] and lse.is_contiguous())
+    return shape[2], _counts(n_rows, (p.batch, p.n_kv_heads)), _counts(n_new, (p.batch,)), \
         None if mods is None else C.byref(mods.c(p))
 
 
@@ -493,9 +499,10 @@ def chunk_attn_paged(p: Params, q, k_pool, v_pool, page_table, n_rows, out, ws, 
 
 def _pool_pages(p: Params, k_pool, v_pool, page_table) -> CPages:
     _here(k_pool, v_pool, page_table)
-    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.dim() == 2
-    assert page_table.shape[0] == p.batch and k_pool.shape == v_pool.shape and k_pool.dim() == 4
-    return CPages(page_table.data_ptr(), page_table.shape[1], k_pool.shape[2], k_pool.shape[0])
+    ts, ks = page_table.shape, k_pool.shape
+    assert page_table.dtype is torch.int32 and len(ts) == 2 and ts[0] == p.batch and page_table.is_contiguous()
+    assert len(ks) == 4 and v_pool.shape == ks
+    return CPages(page_table.data_ptr(), ts[1], ks[2], ks[0])
 
 
 def new_append_workspace(p: Params, device="cuda") -> torch.Tensor:
@@ -506,7 +513,9 @@ def new_append_workspace(p: Params, device="cuda") -> torch.Tensor:
 
 def _cache_dtype(p: Params, *tensors):
     want = torch.float32 if p.dtype == F32 else torch.bfloat16
-    assert all(t.dtype == want and t.shape[1] == p.n_kv_heads and t.shape[3] == p.head_dim for t in tensors)
+    for t in tensors:
+        ts = t.shape
+        assert t.dtype is want and len(ts) == 4 and ts[1] == p.n_kv_heads and ts[3] == p.head_dim
 
 
 def append_paged(p: Params, k_new, v_new, k_pool, v_pool, page_table, n_rows, n_rows_out, ws, n_new=None):
@@ -534,8 +543,9 @@ def _page_state(state: PageState, ws, *tensors) -> CPageState:
 
 
 def _moves(moves, n_moves):
-    assert moves.dtype == torch.int32 and moves.is_contiguous() and moves.dim() == 2 and moves.shape[1] == 2
-    return _ptr(moves), moves.shape[0], _counts(n_moves, (1,))
+    ms = moves.shape
+    assert moves.dtype is torch.int32 and len(ms) == 2 and ms[1] == 2 and moves.is_contiguous()
+    return moves.data_ptr(), ms[0], _counts(n_moves, (1,))
 
 
 def pages_fork(state: PageState, src, dst, ws):
