@@ -385,32 +385,40 @@ __device__ __forceinline__ int append_rows(const AppendArgs& a, int u, int b, in
     return more;
 }
 
-// One 16-byte chunk of one new row per thread and step; K and V rows of a token next to each other in the grid.
-__global__ void __launch_bounds__(kCopyThreads) append_kernel(const AppendArgs a, int count_here) {
-    const int cpr = a.chunks_per_row;
-    const int64_t total = int64_t(a.units) * a.max_new * 2 * cpr;
-    for (int64_t x = int64_t(blockIdx.x) * kCopyThreads + threadIdx.x; x < total; x += int64_t(gridDim.x) * kCopyThreads) {
-        const int c = int(x % cpr), which = int(x / cpr % 2);
-        const int64_t row = x / (2 * cpr);
-        const int i = int(row % a.max_new), u = int(row / a.max_new), b = u / a.n_kv_heads, h = u % a.n_kv_heads;
-        int first;
-        const bool lead = i == 0 && which == 0 && c == 0;
-        const int more = append_rows(a, u, b, first, lead);
-        if (lead && count_here) a.n_rows_out[u] = first + more;
-        if (i >= more) continue;
-        const int t = first + i;
-        const int page = a.page_table[int64_t(b) * a.max_pages + t / a.page_rows];
-        if (page < 0 || page >= a.n_pages) {
-            if (which == 0 && c == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
-            continue;
+// Block (., u) moves up to kAppendRows new rows of unit u, K and V: 16 bytes per thread and step, four steps in flight.  Bound
+// by memory: every byte is read and written once.
+constexpr int kAppendRows = 32;
+__global__ void __launch_bounds__(kCopyThreads) append_kernel(const AppendArgs a, int log_chunks, int count_here) {
+    const int u = blockIdx.y, b = u / a.n_kv_heads, h = u - b * a.n_kv_heads, i0 = blockIdx.x * kAppendRows;
+    int first;
+    const bool lead = i0 == 0 && threadIdx.x == 0;
+    const int more = append_rows(a, u, b, first, lead);
+    if (lead && count_here) a.n_rows_out[u] = first + more;
+    const int rows = min(more - i0, kAppendRows);
+    if (rows <= 0) return;
+    const uint4* const from[2] = {static_cast<const uint4*>(a.k_new) + int64_t(b) * a.kn_sb + int64_t(h) * a.kn_sh + int64_t(i0) * a.kn_st,
+                                  static_cast<const uint4*>(a.v_new) + int64_t(b) * a.vn_sb + int64_t(h) * a.vn_sh + int64_t(i0) * a.vn_st};
+    const int total = rows << (log_chunks + 1);          // chunks of [row][K or V][16 bytes]
+    const int32_t* const table = a.page_table + int64_t(b) * a.max_pages;
+    for (int x0 = threadIdx.x; x0 < total; x0 += 4 * blockDim.x) {
+        uint4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int x = x0 + j * int(blockDim.x), c = x & ((1 << log_chunks) - 1), which = (x >> log_chunks) & 1, i = x >> (log_chunks + 1);
+            if (x < total) v[j] = ld_stream((which ? from[1] + i * a.vn_st : from[0] + i * a.kn_st) + c);
         }
-        const int64_t slot = t % a.page_rows;
-        if (which == 0) {
-            const uint4 v = ld_stream(static_cast<const uint4*>(a.k_new) + int64_t(b) * a.kn_sb + int64_t(h) * a.kn_sh + int64_t(i) * a.kn_st + c);
-            static_cast<uint4*>(a.k)[int64_t(page) * a.k_sb + int64_t(h) * a.k_sh + slot * a.k_st + c] = v;
-        } else {
-            const uint4 v = ld_stream(static_cast<const uint4*>(a.v_new) + int64_t(b) * a.vn_sb + int64_t(h) * a.vn_sh + int64_t(i) * a.vn_st + c);
-            static_cast<uint4*>(a.v)[int64_t(page) * a.v_sb + int64_t(h) * a.v_sh + slot * a.v_st + c] = v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int x = x0 + j * int(blockDim.x), c = x & ((1 << log_chunks) - 1), which = (x >> log_chunks) & 1, i = x >> (log_chunks + 1);
+            if (x >= total) continue;
+            const uint32_t t = uint32_t(first + i0 + i), slot = t % uint32_t(a.page_rows);
+            const int page = table[t / uint32_t(a.page_rows)];
+            if (page < 0 || page >= a.n_pages) {
+                if (which == 0 && c == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
+                continue;
+            }
+            if (which) static_cast<uint4*>(a.v)[int64_t(page) * a.v_sb + int64_t(h) * a.v_sh + int64_t(slot) * a.v_st + c] = v[j];
+            else static_cast<uint4*>(a.k)[int64_t(page) * a.k_sb + int64_t(h) * a.k_sh + int64_t(slot) * a.k_st + c] = v[j];
         }
     }
 }
@@ -481,9 +489,11 @@ csp_status launch_append(const AppendArgs& a, cudaStream_t s) {
     if (a.units == 0) return CSP_OK;
     const bool in_place = a.n_rows_out == a.n_rows;
     if (a.max_new > 0) {
-        const int64_t blocks = (int64_t(a.units) * a.max_new * 2 * a.chunks_per_row + kCopyThreads - 1) / kCopyThreads;
-        const int64_t fill = 32 * int64_t(sm_count());
-        append_kernel<<<int(blocks < fill ? blocks : fill), kCopyThreads, 0, s>>>(a, in_place ? 0 : 1);
+        const int log_chunks = a.chunks_per_row == 8 ? 3 : a.chunks_per_row == 16 ? 4 : 5;
+        // a single row needs one or two warps
+        const int chunks = (a.max_new < kAppendRows ? a.max_new : kAppendRows) * 2 * a.chunks_per_row;
+        const int threads = chunks < kCopyThreads ? (chunks + 31) / 32 * 32 : kCopyThreads;
+        append_kernel<<<dim3((a.max_new + kAppendRows - 1) / kAppendRows, a.units), threads, 0, s>>>(a, log_chunks, in_place ? 0 : 1);
         if (const csp_status st = launched()) return st;
     }
     if (in_place || a.max_new == 0) append_count_kernel<<<(a.units + 127) / 128, 128, 0, s>>>(a);
