@@ -22,7 +22,6 @@
 // softmax runs while the tensor cores work for the other.
 #include <limits.h>
 
-#include <type_traits>
 
 #include "csp_chunk.cuh"
 #include "csp_tc.cuh"
@@ -147,7 +146,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, -1, 0, 0};
         // Documents make the weight of an item unknown (tiles without any of its documents are skipped): where every block
         // has several items anyway, they are drawn whole, one after the other.
+        // The last tokens of every unit come first: they see the most keys, and an item drawn near the end is a short one.
         const bool drawn = kDoc && pl.n_items >= 2 * pl.grid;
+        const int n_units = pl.n_items / pl.n_pairs;
+        auto unit_of = [&](int item) { return drawn ? item % n_units : item / pl.n_pairs; };
         ItemDraw draw;
         if (drawn) share = Share{-1, 0, pl.n_items, 0};
         const uint32_t tiles_per_page = uint32_t(a.page_rows) / uint32_t(kTileKeys);      // (dense: not used)
@@ -158,8 +160,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         int next_page = 0;                               // lane l: page of the next item's tile l (of its first 32)
         auto look_up = [&](int item) {
             if (item > share.item1 || (item == share.item1 && share.tile1 == 0 && !drawn) || item >= pl.n_items) return;
-            const int u = item / pl.n_pairs;
-            next = pair_range(a, pl, u, item - u * pl.n_pairs);
+            const int u = unit_of(item);
+            next = pair_range(a, pl, u, drawn ? pl.n_pairs - 1 - item / n_units : item - u * pl.n_pairs);
             const int tile = (item == share.item0 ? share.tile0 : 0) + lane;
             if (a.page_table && next.count > 0 && tile < next.tiles) next_page = page_of(u / a.n_kv_heads, tile);
         };
@@ -168,7 +170,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         look_up(item);
         for (; ok && item <= share.item1 && item < pl.n_items; item = coming) {
             coming = drawn ? draw.next(lane) : item + 1;
-            const int u = item / pl.n_pairs, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
+            const int u = unit_of(item), b = u / a.n_kv_heads, h = u % a.n_kv_heads;
             const PairRange x = next;
             int pages = next_page;                       // lane l: the page of tile 32 j + l
             const int tile0 = item == share.item0 ? share.tile0 : 0, tile1 = item == share.item1 ? share.tile1 : x.tiles;
@@ -241,7 +243,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 }
             };
             if (kMeta && tile0 < tile1) fetch_meta(tile0);
-            bool q_free = tile0 < tile1 && !kDoc;        // (with documents it is not known yet whether Q is needed at all)
+            bool q_free = tile0 < tile1;
 #pragma unroll
             for (int slot = 0; slot < 2; ++slot)
                 if (q_slots & kSlot0 << slot) q_free = q_free && mbar_test(q_empty + 8 * slot, (q_uses[slot] & 1u) ^ 1u);
@@ -357,16 +359,17 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             if (lane == 0) mbar_arrive(ent_empty + 8 * e);
             ++n_entry;
             if (flags & kStop) break;
-            if (!(flags & kEnd)) {
-                if (flags & kFirst) {
-                    started[0] = started[1] = false;
+            if (flags & kFirst) {
+                started[0] = started[1] = false;
+                // (an item without any tile, an END at once, has its Q or not; one that was loaded is waited for all the same)
 #pragma unroll
-                    for (int slot = 0; slot < 2; ++slot) {
-                        if (!(flags & kSlot0 << slot)) continue;
-                        warp_wait(q_full + 8 * slot, q_uses[slot] & 1u, abort_flag);
-                        ++q_uses[slot];
-                    }
+                for (int slot = 0; slot < 2; ++slot) {
+                    if (!(flags & kSlot0 << slot) || (flags & (kEnd | kHasQ)) == kEnd) continue;
+                    warp_wait(q_full + 8 * slot, q_uses[slot] & 1u, abort_flag);
+                    ++q_uses[slot];
                 }
+            }
+            if (!(flags & kEnd)) {
                 const uint32_t n = 2u * uint32_t(n_tile), s = n % NST;
                 warp_wait(kv_full + 8 * s, (n / NST) & 1u, abort_flag);
                 const uint64_t kd = sw128_desc(base + s * kStageBytes);
@@ -845,7 +848,8 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
             return CSP_ERR_UNSUPPORTED;
         st = p.head_dim == 64 ? launch_nh<1>(a, pl, tq, tk, tv, parts, partial, ml, s) : launch_nh<2>(a, pl, tq, tk, tv, parts, partial, ml, s);
     }
-    if (st != CSP_OK || pl.grid == 1) return st;         // a single block cuts nothing
+    // a single block cuts nothing, and an item is cut only where both parts have min_tiles
+    if (st != CSP_OK || pl.grid == 1 || p.out_capacity <= (2 * pl.min_tiles - 1) * pl.key_tile) return st;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(pl.grid, (pl.row_slots + 31) / 32);
     cfg.blockDim = dim3(32 * kJoinWarps);
