@@ -122,7 +122,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     Share share = find_share<kChThreads>(a, pl, reinterpret_cast<int*>(base_ptr + sp.pair));      // (synchronises)
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    asm volatile("griddepcontrol.launch_dependents;");   // the joining kernel may get ready
     const uint32_t tmem_o[2] = {tmem, tmem + 128u}, tmem_s[2] = {tmem + 256u, tmem + 384u};
 
     if (warp >= kSoftmaxWarps) {
@@ -700,20 +699,20 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     }
 }
 
-// out = sum_s O_s 2^(m_s - m) / (n 2^-m + sum_s l_s 2^(m_s - m)) over the parts of a cut item.  Block (c, r) joins 32 rows of
-// the item that begins in block c of the main kernel and goes on in c + 1, ... until one says it is the last.  A lane has a
-// row, a warp an eighth of the columns: the parts are laid out [column / 4][row][4], so every load is one piece.
-constexpr int kJoinWarps = 8;
-template <int D>
-__global__ void __launch_bounds__(32 * kJoinWarps) chunk_join_kernel(const ChunkArgs a, const ChunkPlan pl, const ChunkParts* parts,
-                                                                     const float* partial, const float2* partial_ml) {
-    constexpr int C = D / 4 / kJoinWarps;                // chunks of four columns per lane
-    asm volatile("griddepcontrol.wait;" ::: "memory");   // launched early: the main kernel has to be through
+// out = sum_s O_s 2^(m_s - m) / (n 2^-m + sum_s l_s 2^(m_s - m)) over the parts of a cut item.  Block (c, r) joins 16 rows of
+// the item that begins in block c of the main kernel and goes on in c + 1, ... until one says it is the last.  A thread has
+// four columns of a row; the parts are laid out [column / 4][row][4], so that eight rows are one line.  Bound by the latency
+// of its few loads and of its instructions (which are cold), so the code is kept short.  Parts in flight: eight where few rows
+// are cut often (one token over 8 K - 32 K rows, ten parts: 6.7 us; with four 8.6), four elsewhere (512 tokens over 4 K, two or
+// three parts of 256 rows: 11.5 us, with eight 12.6; 32 rows per block: 12.6).  Launched ahead of the main kernel's end
+// (programmatic dependence) it gained nothing.
+constexpr int kJoinRows = 16;
+template <int D, int kJoinAhead>
+__global__ void __launch_bounds__(2 * D) chunk_join_kernel(const ChunkArgs a, const ChunkPlan pl, const ChunkParts* parts,
+                                                           const float* partial, const float2* partial_ml) {
     const int c0 = blockIdx.x, item = parts[c0].first;
     if (item < 0) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = a.group;
-    const int u = item / pl.n_pairs, pair = item - u * pl.n_pairs, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
-    const int n_new = a.n_new ? min(max(a.n_new[b], 0), a.max_new) : a.max_new;
+    const int lane = threadIdx.x & 31, col = threadIdx.x / 8, G = a.group;
     int n_parts = 1;
     for (int c = c0 + 1; c < pl.grid; c += 32) {
         const bool in = c + lane < pl.grid;
@@ -722,34 +721,50 @@ __global__ void __launch_bounds__(32 * kJoinWarps) chunk_join_kernel(const Chunk
         n_parts += 32;
     }
     n_parts = min(n_parts, pl.grid - c0);
-    const int row = blockIdx.y * 32 + lane, tok = pair * 2 * pl.tok_tile + row / G, head = h * G + row % G;
-    if (row >= pl.row_slots || tok >= n_new) return;
-    // partial results 2 c0 + 1, 2 (c0 + 1), 2 (c0 + 2), ...
-    auto slot = [&](int s) { return int64_t(2 * (c0 + s) + (s == 0 ? 1 : 0)) * pl.row_slots; };
-    float m = kNeg;
-#pragma unroll 8
-    for (int s = 0; s < n_parts; ++s) m = fmaxf(m, partial_ml[slot(s) + row].x);
-    float l = 0.f;
-    float4 o[C];
+    const int u = item / pl.n_pairs, pair = item - u * pl.n_pairs, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
+    const int n_new = a.n_new ? min(max(a.n_new[b], 0), a.max_new) : a.max_new;
+    const int row_end = min((n_new - pair * 2 * pl.tok_tile) * G, min(pl.row_slots, int(blockIdx.y + 1) * kJoinRows));
+#pragma unroll 1
+    for (int row = blockIdx.y * kJoinRows + threadIdx.x % 8; row < row_end; row += 8) {
+        float m = kNeg, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int s0 = 0; s0 < n_parts; s0 += kJoinAhead) {
+            float2 ml[kJoinAhead];
+            float4 y[kJoinAhead];
 #pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int s = 0; s < n_parts; ++s) {
-        const float2 p = partial_ml[slot(s) + row];
-        const float w = ex2f(p.x - m);
-        l += p.y * w;
+            for (int j = 0; j < kJoinAhead; ++j) {
+                // partial results 2 c0 + 1, 2 (c0 + 1), 2 (c0 + 2), ...
+                const int s = s0 + j;
+                const int slot = (2 * (c0 + s) + (s == 0 ? 1 : 0)) * pl.row_slots;
+                ml[j] = make_float2(kNeg, 0.f);
+                y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (s < n_parts) {
+                    ml[j] = partial_ml[slot + row];
+                    y[j] = reinterpret_cast<const float4*>(partial)[slot * (D / 4) + col * pl.row_slots + row];
+                }
+            }
+            float m_now = m;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const float4 y = *reinterpret_cast<const float4*>(partial + (slot(s) * (D / 4) + int64_t(warp * C + c) * pl.row_slots + row) * 4);
-            o[c].x += y.x * w; o[c].y += y.y * w; o[c].z += y.z * w; o[c].w += y.w * w;
+            for (int j = 0; j < kJoinAhead; ++j) m_now = fmaxf(m_now, ml[j].x);
+            const float keep = ex2f(m - m_now);
+            m = m_now;
+            l *= keep;
+            o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+#pragma unroll
+            for (int j = 0; j < kJoinAhead; ++j) {
+                const float w = ex2f(ml[j].x - m_now);
+                l += ml[j].y * w;
+                o.x += y[j].x * w; o.y += y[j].y * w; o.z += y[j].z * w; o.w += y[j].w * w;
+            }
         }
+        const float inv = l == 0.f ? 0.f : 1.f / (a.n * ex2f(-m) + l);
+        const int i = row / G, head = h * G + row - i * G, tok = pair * 2 * pl.tok_tile + i;
+        reinterpret_cast<uint2*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st)[col] =
+            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        if (a.lse && col == 0)
+            a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / (a.n * ex2f(-m) + l);
-    uint2* const out = reinterpret_cast<uint2*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st) + warp * C;
-#pragma unroll
-    for (int c = 0; c < C; ++c) out[c] = make_uint2(pack_bf16(o[c].x * inv, o[c].y * inv), pack_bf16(o[c].z * inv, o[c].w * inv));
-    if (a.lse && warp == 0)
-        a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
@@ -850,18 +865,11 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
     }
     // a single block cuts nothing, and an item is cut only where both parts have min_tiles
     if (st != CSP_OK || pl.grid == 1 || p.out_capacity <= (2 * pl.min_tiles - 1) * pl.key_tile) return st;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(pl.grid, (pl.row_slots + 31) / 32);
-    cfg.blockDim = dim3(32 * kJoinWarps);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;         // it waits for the main kernel by itself
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
-    const cudaError_t err = p.head_dim == 64 ? cudaLaunchKernelEx(&cfg, chunk_join_kernel<64>, a, pl, (const ChunkParts*)parts, (const float*)partial, (const float2*)ml)
-                                             : cudaLaunchKernelEx(&cfg, chunk_join_kernel<128>, a, pl, (const ChunkParts*)parts, (const float*)partial, (const float2*)ml);
-    if (err != cudaSuccess) { cudaGetLastError(); return CSP_ERR_CUDA; }
-    return CSP_OK;
+    const dim3 blocks(pl.grid, (pl.row_slots + kJoinRows - 1) / kJoinRows);
+    const bool few = pl.row_slots <= kFewRows;
+    if (p.head_dim == 64) (few ? chunk_join_kernel<64, 8> : chunk_join_kernel<64, 4>)<<<blocks, 128, 0, s>>>(a, pl, parts, partial, ml);
+    else (few ? chunk_join_kernel<128, 8> : chunk_join_kernel<128, 4>)<<<blocks, 256, 0, s>>>(a, pl, parts, partial, ml);
+    return cudaGetLastError() == cudaSuccess ? CSP_OK : CSP_ERR_CUDA;
 }
 
 }  // namespace csp

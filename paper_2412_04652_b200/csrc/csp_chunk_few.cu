@@ -85,7 +85,6 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     const Share share = find_share<kFewThreads>(a, pl, reinterpret_cast<int*>(merge));      // (synchronises)
-    asm volatile("griddepcontrol.launch_dependents;");   // the joining kernel may get ready
 
     if (warp == kFewProducer) {
         // =============================== producer ===============================
