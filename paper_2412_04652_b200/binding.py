@@ -264,7 +264,8 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    # (current_stream() builds an object around this handle: 3 us, half of what a whole small call takes)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def tensor4(t: torch.Tensor) -> CTensor:
