@@ -42,28 +42,47 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums, 
 // from L2, where atomics land.
 __device__ __forceinline__ int32_t ld(const int32_t* p) { return __ldcg(p); }
 
-// Table entry e = b * max_pages + i as csp_pages_reserve sees it.
+// Table entries e = b * max_pages + i as csp_pages_reserve sees them.  A thread takes kPerThread neighbours at a time, so that
+// the chains of dependent loads (sequence, entry, count) of all four are under way together.
 struct Entry { int page; bool claim, fresh; };
-__device__ __forceinline__ Entry reserve_entry(const PageArgs& a, int64_t e, bool flag) {
-    Entry x = {-1, false, false};
-    const int b = int(e / a.max_pages), i = int(e % a.max_pages);
-    const int held = ld(a.held + b), need = ld(a.need + b);
-    x.fresh = i >= held && i < need;
-    if (i >= ld(a.first + b) && i < held && i < need) {
-        x.page = ld(a.table + e);
-        if (x.page < 0 || x.page >= a.n_pages || ld(a.refs + x.page) <= 0) {
-            if (flag) atomicOr(a.status, CSP_DEV_BAD_LEN);
-            x.page = -1;
-        } else {
-            x.claim = ld(a.refs + x.page) > 1;
+__device__ __forceinline__ void reserve_entries(const PageArgs& a, uint32_t entries, uint32_t e0, bool flag, Entry (&x)[kPerThread],
+                                                int (&refs)[kPerThread]) {
+    int held[kPerThread], need[kPerThread], first[kPerThread], i[kPerThread];
+#pragma unroll
+    for (int j = 0; j < kPerThread; ++j) {
+        const uint32_t e = e0 + j, b = e / uint32_t(a.max_pages);
+        i[j] = int(e - b * uint32_t(a.max_pages));
+        held[j] = need[j] = first[j] = 0;
+        x[j] = Entry{-1, false, false};
+        if (e < entries) { held[j] = ld(a.held + b); need[j] = ld(a.need + b); first[j] = ld(a.first + b); }
+    }
+#pragma unroll
+    for (int j = 0; j < kPerThread; ++j) {
+        x[j].fresh = i[j] >= held[j] && i[j] < need[j];
+        if (i[j] >= first[j] && i[j] < held[j] && i[j] < need[j]) {
+            const int page = ld(a.table + e0 + j);
+            if (page >= 0 && page < a.n_pages) x[j].page = page;
+            else if (flag) atomicOr(a.status, CSP_DEV_BAD_LEN);
         }
     }
-    return x;
+#pragma unroll
+    for (int j = 0; j < kPerThread; ++j) refs[j] = x[j].page >= 0 ? ld(a.refs + x[j].page) : 1;
+#pragma unroll
+    for (int j = 0; j < kPerThread; ++j) {
+        if (refs[j] <= 0) {
+            if (flag) atomicOr(a.status, CSP_DEV_BAD_LEN);
+            x[j].page = -1;
+        }
+        x[j].claim = refs[j] > 1;
+    }
 }
 
 // A shared page is copied for whoever asks for it, except that the last one to ask keeps it when all who share it ask.
-__device__ __forceinline__ bool reserve_copies(const PageArgs& a, const Entry& x, int64_t e) {
-    return x.claim && !(ld(a.claims + x.page) == ld(a.refs + x.page) && ld(a.last + x.page) == int32_t(e));
+__device__ __forceinline__ void reserve_copies(const PageArgs& a, uint32_t e0, const Entry (&x)[kPerThread],
+                                               const int (&refs)[kPerThread], bool (&copies)[kPerThread]) {
+#pragma unroll
+    for (int j = 0; j < kPerThread; ++j)
+        copies[j] = x[j].claim && !(ld(a.claims + x[j].page) == refs[j] && ld(a.last + x[j].page) == int32_t(e0 + j));
 }
 
 __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const PageArgs a, const int32_t* n_new, int whole,
@@ -94,22 +113,29 @@ __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const Page
     }
     for (int p = tid; p < a.n_pages; p += kTableThreads) { a.claims[p] = 0; a.last[p] = -1; }
     __syncthreads();
-    const int64_t entries = int64_t(a.batch) * a.max_pages;
+    const uint32_t entries = uint32_t(a.batch) * uint32_t(a.max_pages);          // (31 bits)
+    constexpr uint32_t kStep = kTableThreads * kPerThread;
+    Entry x[kPerThread];
+    int refs[kPerThread];
+    bool copies[kPerThread];
     if (!fail) {
-        for (int64_t e = tid; e < entries; e += kTableThreads) {
-            const Entry x = reserve_entry(a, e, true);
-            if (x.claim) { atomicAdd(a.claims + x.page, 1); atomicMax(a.last + x.page, int32_t(e)); }
+        for (uint32_t e0 = tid * kPerThread; e0 < entries; e0 += kStep) {
+            reserve_entries(a, entries, e0, true, x, refs);
+#pragma unroll
+            for (int j = 0; j < kPerThread; ++j)
+                if (x[j].claim) { atomicAdd(a.claims + x[j].page, 1); atomicMax(a.last + x[j].page, int32_t(e0 + j)); }
         }
     }
     __syncthreads();
     if (!fail) {
         uint32_t want = 0, copy = 0, free_pages = 0;
-        for (int64_t e = tid; e < entries; e += kTableThreads) {
-            const Entry x = reserve_entry(a, e, false);
-            const bool c = reserve_copies(a, x, e);
-            copy += c;
-            want += c || x.fresh;
+        for (uint32_t e0 = tid * kPerThread; e0 < entries; e0 += kStep) {
+            if (entries > kStep) reserve_entries(a, entries, e0, false, x, refs);        // (else they are here still)
+            reserve_copies(a, e0, x, refs, copies);
+#pragma unroll
+            for (int j = 0; j < kPerThread; ++j) { copy += copies[j]; want += copies[j] || x[j].fresh; }
         }
+#pragma unroll 4
         for (int p = tid; p < a.n_pages; p += kTableThreads) free_pages += ld(a.refs + p) == 0;
         want = __reduce_add_sync(0xffffffffu, want);
         copy = __reduce_add_sync(0xffffffffu, copy);
@@ -144,16 +170,16 @@ __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const Page
     __syncthreads();
     // hand them out in the order of sequence and table index
     uint32_t base_want = 0, base_copy = 0;
-    for (int64_t e0 = 0; e0 < entries; e0 += kTableThreads * kPerThread) {
-        Entry x[kPerThread];
-        bool copies[kPerThread];
+    for (uint32_t e_base = 0; e_base < entries; e_base += kStep) {
+        const uint32_t e0 = e_base + tid * kPerThread;
+        if (entries > kStep) {
+            reserve_entries(a, entries, e0, false, x, refs);
+            reserve_copies(a, e0, x, refs, copies);
+        }
         uint32_t n = 0, total;
 #pragma unroll
         for (int j = 0; j < kPerThread; ++j) {
-            const int64_t e = e0 + tid * kPerThread + j;
-            x[j] = Entry{-1, false, false};
-            if (e < entries) x[j] = reserve_entry(a, e, false);
-            copies[j] = reserve_copies(a, x[j], e);
+            if (e0 >= entries) { x[j].fresh = false; copies[j] = false; }
             n += (copies[j] || x[j].fresh ? 1u : 0u) + (copies[j] ? 0x10000u : 0u);
         }
         const uint32_t before = block_scan(n, warp_sums, total);
@@ -163,7 +189,7 @@ __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const Page
             if (!copies[j] && !x[j].fresh) continue;
             const int to = ld(a.list + want++);
             if (copies[j]) moves[copy++] = make_int2(x[j].page, to);
-            a.table[e0 + tid * kPerThread + j] = to;
+            a.table[e0 + j] = to;
             a.refs[to] = 1;                              // it was free: nobody claims it
         }
         base_want += total & 0xffffu;
@@ -385,17 +411,17 @@ __device__ __forceinline__ int append_rows(const AppendArgs& a, int u, int b, in
     return more;
 }
 
-// Block (., u) moves up to kAppendRows new rows of unit u, K and V: 16 bytes per thread and step, four steps in flight.  Bound
+// Block (u, .) moves kAppendRows new rows of unit u at a time, K and V: 16 bytes per thread and step, four steps in flight.  Bound
 // by memory: every byte is read and written once.
 constexpr int kAppendRows = 32;
 __global__ void __launch_bounds__(kCopyThreads) append_kernel(const AppendArgs a, int log_chunks, int count_here) {
-    const int u = blockIdx.y, b = u / a.n_kv_heads, h = u - b * a.n_kv_heads, i0 = blockIdx.x * kAppendRows;
+    const int u = blockIdx.x, b = u / a.n_kv_heads, h = u - b * a.n_kv_heads;
     int first;
-    const bool lead = i0 == 0 && threadIdx.x == 0;
+    const bool lead = blockIdx.y == 0 && threadIdx.x == 0;
     const int more = append_rows(a, u, b, first, lead);
     if (lead && count_here) a.n_rows_out[u] = first + more;
+    for (int i0 = blockIdx.y * kAppendRows; i0 < more; i0 += int(gridDim.y) * kAppendRows) {
     const int rows = min(more - i0, kAppendRows);
-    if (rows <= 0) return;
     const uint4* const from[2] = {static_cast<const uint4*>(a.k_new) + int64_t(b) * a.kn_sb + int64_t(h) * a.kn_sh + int64_t(i0) * a.kn_st,
                                   static_cast<const uint4*>(a.v_new) + int64_t(b) * a.vn_sb + int64_t(h) * a.vn_sh + int64_t(i0) * a.vn_st};
     const int total = rows << (log_chunks + 1);          // chunks of [row][K or V][16 bytes]
@@ -420,6 +446,7 @@ __global__ void __launch_bounds__(kCopyThreads) append_kernel(const AppendArgs a
             if (which) static_cast<uint4*>(a.v)[int64_t(page) * a.v_sb + int64_t(h) * a.v_sh + int64_t(slot) * a.v_st + c] = v[j];
             else static_cast<uint4*>(a.k)[int64_t(page) * a.k_sb + int64_t(h) * a.k_sh + int64_t(slot) * a.k_st + c] = v[j];
         }
+    }
     }
 }
 
@@ -493,7 +520,8 @@ csp_status launch_append(const AppendArgs& a, cudaStream_t s) {
         // a single row needs one or two warps
         const int chunks = (a.max_new < kAppendRows ? a.max_new : kAppendRows) * 2 * a.chunks_per_row;
         const int threads = chunks < kCopyThreads ? (chunks + 31) / 32 * 32 : kCopyThreads;
-        append_kernel<<<dim3((a.max_new + kAppendRows - 1) / kAppendRows, a.units), threads, 0, s>>>(a, log_chunks, in_place ? 0 : 1);
+        const int blocks = a.max_new / kAppendRows + (a.max_new % kAppendRows ? 1 : 0);
+        append_kernel<<<dim3(a.units, blocks < 65535 ? blocks : 65535), threads, 0, s>>>(a, log_chunks, in_place ? 0 : 1);
         if (const csp_status st = launched()) return st;
     }
     if (in_place || a.max_new == 0) append_count_kernel<<<(a.units + 127) / 128, 128, 0, s>>>(a);
