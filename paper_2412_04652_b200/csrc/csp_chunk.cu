@@ -642,7 +642,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             if (live) {
                 const int local = m / G, head = h * G + m - local * G, tok = tok0 + (big ? g * pl.tok_tile : 0) + local;
                 const bool final = part_slot < 0;
-                const float denom = a.n * ex2f(-m_all) + l_all;
+                const float denom = n_term(a.n, m_all) + l_all;
                 const float inv = final ? 1.f / denom : 1.f;
                 const uint32_t o0 = (big ? tmem_o[g] : tmem_o[0]) + lane_base, o1 = tmem_o[1] + lane_base;
                 uint16_t* const out = a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st;
@@ -758,7 +758,7 @@ __global__ void __launch_bounds__(2 * D) chunk_join_kernel(const ChunkArgs a, co
                 o.x += y[j].x * w; o.y += y[j].y * w; o.z += y[j].z * w; o.w += y[j].w * w;
             }
         }
-        const float inv = l == 0.f ? 0.f : 1.f / (a.n * ex2f(-m) + l);
+        const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, m) + l);
         const int i = row / G, head = h * G + row - i * G, tok = pair * 2 * pl.tok_tile + i;
         reinterpret_cast<uint2*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st)[col] =
             make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));

@@ -307,7 +307,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                 }
                 const int tok = m / G, head = h * G + m % G;
                 if (final) {
-                    const float inv = l == 0.f ? 0.f : 1.f / (a.n * ex2f(-mm) + l);      // l == 0: nothing was seen
+                    const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, mm) + l);      // l == 0: nothing was seen
                     uint32_t* const out = reinterpret_cast<uint32_t*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st + lane * C);
 #pragma unroll
                     for (int c = 0; c < C; c += 2) out[c / 2] = l == 0.f ? 0u : pack_bf16(o[c] * inv, o[c + 1] * inv);

@@ -390,3 +390,44 @@ def test_random_launches(csp):
             mods["prefix"] = torch.from_numpy(rng.randint(0, cap + 1, size=(B, Hkv)).astype(np.int32))
         case = _case(trial, B, G * Hkv, Hkv, d, cap, rows, new, gain=float(rng.choice([0.5, 1.5, 4.0])), T=T)
         _run(csp, case, int(rng.choice([0, 128, 256])), n=float(rng.choice([0.0, 1.0])), seed=trial, what=f"trial {trial}", **mods)
+
+
+# ---- logits far below zero
+
+@pytest.mark.parametrize("T,rows,page_rows", [(1, 333, 0), (1, 6000, 128), (40, 6000, 0), (150, 333, 128)])
+@pytest.mark.parametrize("n", [0.0, 1.0])
+def test_logits_far_below_zero(csp, T, rows, page_rows, n):
+    """Near -362 e^-o is not a float any more: without n the weights are still those of a softmax, with n they are zeros."""
+    g = torch.Generator().manual_seed(T + rows)
+    q = torch.full((1, T, 4, 128), 4.0).to(torch.bfloat16).transpose(1, 2)
+    k = (-8.0 + torch.randint(-4, 5, (1, 2, rows, 128), generator=g) / 16.0).to(torch.bfloat16)
+    v = torch.randn(1, 2, rows, 128, generator=g).to(torch.bfloat16)
+    case = q, k, v, torch.full((1, 2), rows, dtype=torch.int32), torch.tensor([T], dtype=torch.int32)
+    out, _ = _run(csp, case, page_rows, n=n)
+    assert (out != 0).any() == (n == 0.0)
+
+
+# ---- documents: items that are drawn one by one, and shares without any of the tokens' documents
+
+@pytest.mark.parametrize("T", [20, 150])
+def test_documents_of_many_units(csp, T):
+    B, H, cap = 4, 160 if T == 20 else 80, 260
+    g = np.random.RandomState(T)
+    new = [T, 1, 0, T - 3]
+    rows = np.maximum(g.randint(1, cap + 1, size=(B, H)), np.array(new)[:, None])
+    case = _case(T, B, H, H, 64, cap, rows, new)
+    doc = torch.from_numpy((np.arange(cap)[None, :] * 5 // cap + np.arange(B)[:, None]).astype(np.int32))
+    first = _run(csp, case, 0, documents=doc)
+    again = _run(csp, case, 0, check=False, documents=doc)
+    for x, y in zip(first, again):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("T", [4, 200])
+def test_shares_without_the_tokens_documents(csp, T):
+    cap = 6000
+    case = _case(T, 1, 4, 1, 128, cap, [cap - 1], [T])
+    doc = (torch.arange(cap, dtype=torch.int32) // 1200)[None, :].contiguous()
+    _run(csp, case, 128, documents=doc, what="the last of five")
+    _run(csp, case, 0, documents=(doc == 4).int() * torch.tensor(7, dtype=torch.int32) + (doc == 1).int() * torch.tensor(7, dtype=torch.int32),
+         what="the second and the last are one")
