@@ -319,7 +319,7 @@ csp_status csp_decode_step(const csp_params* p, csp_tensor q, csp_tensor k, csp_
 
 /*
  * What csp_chunk_attn does to a logit o = scale <q, k> before the softmax.  Zeros and null pointers change nothing.
- *   softcap    c > 0: o becomes c tanh(o / c)
+ *   softcap    c in [1e-6, 1000]: o becomes c tanh(o / c), with an absolute error of up to c 2^-20 (hence the upper end)
  *   slopes     [H_q] fp32 or NULL: slopes[hq] * |position of the query - position of the key| is subtracted, after the cap
  *   positions  int32, >= 0, of the cached rows: element (b,h,t) at positions[b*pos_stride_b + h*pos_stride_h + t]; NULL: row
  *              t is at position t.  A pruned cache keeps the positions its rows had (the keep_idx of the prune), per
@@ -327,7 +327,8 @@ csp_status csp_decode_step(const csp_params* p, csp_tensor q, csp_tensor k, csp_
  *   documents  int32 document of every cached row, addressed like positions, or NULL: a query sees rows of its own only
  *   prefix     int32 element (b,h) at prefix[b*prefix_stride_b + h*prefix_stride_h], or NULL: the first that many rows of
  *              the unit are seen by every query of the chunk, also by those in front of them (an image in the prompt that
- *              is attended to in both directions); values are clamped to [0, n_rows]
+ *              is attended to in both directions); values are clamped to [0, n_rows].  With documents as well, a query
+ *              sees the prefix rows of its own document only
  */
 typedef struct {
     float softcap;
@@ -339,7 +340,8 @@ typedef struct {
 
 /* Bytes of scratch that csp_chunk_attn and csp_chunk_attn_paged need for chunks of up to max_new tokens (status word,
  * work counters, partial results of split caches).  The first 256 bytes must be zero before first use
- * (csp_workspace_reset). */
+ * (csp_workspace_reset).  Calls, or replays of captured ones, that may run at the same time need a workspace each; the same
+ * holds for the workspaces below. */
 size_t csp_chunk_workspace_bytes(const csp_params* p, int32_t max_new);
 
 /*
@@ -349,8 +351,8 @@ size_t csp_chunk_workspace_bytes(const csp_params* p, int32_t max_new);
  * rows t <= r (and those that `mods` adds or takes away):
  *   out[b,hq,i,:] = sum_t e^{o_t} / (n + sum_j e^{o_j}) v[b,hkv,t,:],   lse[b,hq,i] = ln sum_t e^{o_t}
  *   q       [B, H_q, max_new, d] bf16, out [B, H_q, max_new, d] bf16; any strides (e.g. of a [B, max_new, H_q, d] tensor)
- *   k, v    [B, H_kv, out_capacity, d] bf16; p->out_capacity is the row capacity, p->max_len / window / recent are not
- *           used.  Rows t >= n_rows[b,h] may hold anything; rows that are only masked must be finite
+ *   k, v    [B, H_kv, out_capacity, d] bf16; p->out_capacity is the row capacity (at most 2^30), p->max_len / window /
+ *           recent are not used.  Rows t >= n_rows[b,h] may hold anything; rows that are only masked must be finite
  *   n_rows  [B, H_kv] int32 device: rows per head, the chunk's own included; values outside [0, out_capacity] are
  *           clamped and flagged CSP_DEV_BAD_LEN
  *   n_new_or_null [B] int32 device; NULL: max_new for every sequence.  Values outside [0, max_new] are clamped and

@@ -158,3 +158,14 @@ def test_unsupported_sizes_have_no_workspace(csp):
     assert csp.chunk_workspace_bytes(_params(csp, n_q_heads=64), 4) == 0
     assert csp.chunk_workspace_bytes(_params(csp), -1) == 0
     assert csp.chunk_workspace_bytes(_params(csp), 4) >= 256
+
+
+@pytest.mark.parametrize("cap", [1e-7, 1001.0, 1e30])
+def test_caps_outside_the_accurate_range_are_refused(csp, cap):
+    assert _chunk(csp, _params(csp), mods=csp.CScoreMods(softcap=cap)) == csp.ERR_INVALID_ARG
+
+
+def test_capacities_past_the_row_index_are_refused(csp):
+    p = _params(csp, out_capacity=(1 << 30) + 1)
+    assert _chunk(csp, p) == csp.ERR_UNSUPPORTED
+    assert _chunk(csp, p, paged=True, pages=csp.CPages(256, 1 << 23 | 1, 128, 9)) == csp.ERR_UNSUPPORTED
