@@ -143,10 +143,9 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             ++n_entry;
         };
         if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, -1, 0, 0};
-        // Documents make the weight of an item unknown (tiles without any of its documents are skipped): where every block
-        // has several items anyway, they are drawn whole, one after the other.
-        // The last tokens of every unit come first: they see the most keys, and an item drawn near the end is a short one.
-        const bool drawn = kDoc && pl.n_items >= 2 * pl.grid;
+        // Items drawn whole, one after the other, are the last tokens of every unit first: these see the most keys, and an item
+        // drawn near the end is a short one.
+        const bool drawn = kDoc && pl.drawn;
         const int n_units = pl.n_items / pl.n_pairs;
         auto unit_of = [&](int item) { return drawn ? item % n_units : item / pl.n_pairs; };
         ItemDraw draw;
@@ -699,20 +698,25 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     }
 }
 
-// out = sum_s O_s 2^(m_s - m) / (n 2^-m + sum_s l_s 2^(m_s - m)) over the parts of a cut item.  Block (c, r) joins 16 rows of
+// out = sum_s O_s 2^(m_s - m) / (n 2^-m + sum_s l_s 2^(m_s - m)) over the parts of a cut item.  Block (c, r) joins kRows rows of
 // the item that begins in block c of the main kernel and goes on in c + 1, ... until one says it is the last.  A thread has
-// four columns of a row; the parts are laid out [column / 4][row][4], so that eight rows are one line.  Bound by the latency
-// of its few loads and of its instructions (which are cold), so the code is kept short.  Parts in flight: eight where few rows
-// are cut often (one token over 8 K - 32 K rows, ten parts: 6.7 us; with four 8.6), four elsewhere (512 tokens over 4 K, two or
-// three parts of 256 rows: 11.5 us, with eight 12.6; 32 rows per block: 12.6).  Launched ahead of the main kernel's end
-// (programmatic dependence) it gained nothing.
-constexpr int kJoinRows = 16;
-template <int D, int kJoinAhead>
-__global__ void __launch_bounds__(2 * D) chunk_join_kernel(const ChunkArgs a, const ChunkPlan pl, const ChunkParts* parts,
-                                                           const float* partial, const float2* partial_ml) {
+// C chunks of four columns of a row; the parts are laid out [column / 4][row][4], so that eight rows are one line.  Bound by
+// the latency of its few loads and of its instructions (which are cold), so the code is kept short.  For few rows, which are
+// cut often, eight rows and eight parts in flight (one token over 8 K - 32 K rows, ten parts: 5.9 us; with 32 rows and
+// four parts 14); elsewhere 16 rows and two parts (an item has two or three, of 256 rows; 512 tokens over 4 K: 9.7 us, with eight rows
+// and parts 14; 1 K tokens over 8 K - 32 K: 15.5 us, with 32 rows or four parts 19).
+// Launched ahead of the main kernel's end (programmatic dependence) it gained nothing.
+template <int D, int kRows>
+struct JoinShape {
+    static constexpr int kCols = D / 4 < 256 / kRows ? D / 4 : 256 / kRows, C = D / 4 / kCols, kThreads = kRows * kCols;
+};
+template <int D, int kRows, int kAhead>
+__global__ void __launch_bounds__(JoinShape<D, kRows>::kThreads)
+chunk_join_kernel(const ChunkArgs a, const ChunkPlan pl, const ChunkParts* parts, const float* partial, const float2* partial_ml) {
+    constexpr int C = JoinShape<D, kRows>::C;
     const int c0 = blockIdx.x, item = parts[c0].first;
     if (item < 0) return;
-    const int lane = threadIdx.x & 31, col = threadIdx.x / 8, G = a.group;
+    const int lane = threadIdx.x & 31, col = threadIdx.x / kRows * C, G = a.group;
     int n_parts = 1;
     for (int c = c0 + 1; c < pl.grid; c += 32) {
         const bool in = c + lane < pl.grid;
@@ -723,48 +727,55 @@ __global__ void __launch_bounds__(2 * D) chunk_join_kernel(const ChunkArgs a, co
     n_parts = min(n_parts, pl.grid - c0);
     const int u = item / pl.n_pairs, pair = item - u * pl.n_pairs, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
     const int n_new = a.n_new ? min(max(a.n_new[b], 0), a.max_new) : a.max_new;
-    const int row_end = min((n_new - pair * 2 * pl.tok_tile) * G, min(pl.row_slots, int(blockIdx.y + 1) * kJoinRows));
+    const int row = blockIdx.y * kRows + threadIdx.x % kRows, i = row / G, head = h * G + row - i * G, tok = pair * 2 * pl.tok_tile + i;
+    if (row >= pl.row_slots || tok >= n_new) return;
+    float m = kNeg, l = 0.f;
+    float4 o[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-    for (int row = blockIdx.y * kJoinRows + threadIdx.x % 8; row < row_end; row += 8) {
-        float m = kNeg, l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-        for (int s0 = 0; s0 < n_parts; s0 += kJoinAhead) {
-            float2 ml[kJoinAhead];
-            float4 y[kJoinAhead];
+    for (int s0 = 0; s0 < n_parts; s0 += kAhead) {
+        float2 ml[kAhead];
+        float4 y[kAhead][C];
 #pragma unroll
-            for (int j = 0; j < kJoinAhead; ++j) {
-                // partial results 2 c0 + 1, 2 (c0 + 1), 2 (c0 + 2), ...
-                const int s = s0 + j;
-                const int slot = (2 * (c0 + s) + (s == 0 ? 1 : 0)) * pl.row_slots;
-                ml[j] = make_float2(kNeg, 0.f);
-                y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (s < n_parts) {
-                    ml[j] = partial_ml[slot + row];
-                    y[j] = reinterpret_cast<const float4*>(partial)[slot * (D / 4) + col * pl.row_slots + row];
-                }
-            }
-            float m_now = m;
+        for (int j = 0; j < kAhead; ++j) {
+            // partial results 2 c0 + 1, 2 (c0 + 1), 2 (c0 + 2), ...
+            const int s = s0 + j, slot = (2 * (c0 + s) + (s == 0 ? 1 : 0)) * pl.row_slots;
+            const bool in = s < n_parts;
+            ml[j] = in ? partial_ml[slot + row] : make_float2(kNeg, 0.f);
 #pragma unroll
-            for (int j = 0; j < kJoinAhead; ++j) m_now = fmaxf(m_now, ml[j].x);
-            const float keep = ex2f(m - m_now);
-            m = m_now;
-            l *= keep;
-            o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+            for (int c = 0; c < C; ++c)
+                y[j][c] = in ? reinterpret_cast<const float4*>(partial)[slot * (D / 4) + (col + c) * pl.row_slots + row] : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        float m_now = m;
 #pragma unroll
-            for (int j = 0; j < kJoinAhead; ++j) {
-                const float w = ex2f(ml[j].x - m_now);
-                l += ml[j].y * w;
-                o.x += y[j].x * w; o.y += y[j].y * w; o.z += y[j].z * w; o.w += y[j].w * w;
+        for (int j = 0; j < kAhead; ++j) m_now = fmaxf(m_now, ml[j].x);
+        const float keep = ex2f(m - m_now);
+        m = m_now;
+        l *= keep;
+#pragma unroll
+        for (int c = 0; c < C; ++c) { o[c].x *= keep; o[c].y *= keep; o[c].z *= keep; o[c].w *= keep; }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const float w = ex2f(ml[j].x - m_now);
+            l += ml[j].y * w;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                o[c].x += y[j][c].x * w; o[c].y += y[j][c].y * w; o[c].z += y[j][c].z * w; o[c].w += y[j][c].w * w;
             }
         }
-        const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, m) + l);
-        const int i = row / G, head = h * G + row - i * G, tok = pair * 2 * pl.tok_tile + i;
-        reinterpret_cast<uint2*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st)[col] =
-            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-        if (a.lse && col == 0)
-            a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
     }
+    const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, m) + l);
+    uint2* const out = reinterpret_cast<uint2*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st) + col;
+#pragma unroll
+    for (int c = 0; c < C; ++c) out[c] = make_uint2(pack_bf16(o[c].x * inv, o[c].y * inv), pack_bf16(o[c].z * inv, o[c].w * inv));
+    if (a.lse && col == 0)
+        a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+template <int D, int kRows, int kAhead>
+void join_parts(const ChunkArgs& a, const ChunkPlan& pl, const ChunkParts* parts, const float* partial, const float2* ml, cudaStream_t s) {
+    const dim3 blocks(pl.grid, (pl.row_slots + kRows - 1) / kRows);
+    chunk_join_kernel<D, kRows, kAhead><<<blocks, JoinShape<D, kRows>::kThreads, 0, s>>>(a, pl, parts, partial, ml);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
@@ -778,6 +789,7 @@ ChunkPlan chunk_plan(const csp_params& p, int max_new) {
     ChunkPlan pl;
     const int G = p.n_q_heads / p.n_kv_heads;
     pl.tok_tile = 128 / G;
+    pl.drawn = false;
     pl.n_pairs = (max_new + 2 * pl.tok_tile - 1) / (2 * pl.tok_tile);
     if (pl.n_pairs < 1) pl.n_pairs = 1;
     pl.row_slots = (max_new < 2 * pl.tok_tile ? max_new : 2 * pl.tok_tile) * G;
@@ -785,6 +797,10 @@ ChunkPlan chunk_plan(const csp_params& p, int max_new) {
     pl.key_tile = few ? 64 : kTileKeys;
     pl.min_tiles = 2;
     pl.item_cost = 2;
+    // A cut costs a row pair about four tiles (256 rows of partial results and their joining), few rows next to nothing,
+    // but there an uneven share costs nothing either: HBM is the bound, whoever reads.  1 K tokens over 8 K - 32 K: 905 us without
+    // this limit, 835 with 4, 858 with 2, 878 with 0; one token, serving batch: 113 us without, 114 - 116 with 8 to 1.
+    pl.snap = few ? 0x3fffffff : 4;
     const int64_t items = int64_t(p.batch) * p.n_kv_heads * pl.n_pairs;
     const int64_t weight = (int64_t(p.out_capacity) + pl.key_tile - 1) / pl.key_tile + pl.item_cost;      // of an item, at most
     pl.n_items = items > 0x3fffffffLL / weight ? -1 : int(items);
@@ -842,7 +858,10 @@ size_t chunk_workspace_bytes(const csp_params& p, int max_new) {
 
 csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_tensor& q, const csp_tensor& k,
                              const csp_tensor& v, const csp_pages* pages, void* ws, cudaStream_t s) {
-    const ChunkPlan pl = chunk_plan(p, a.max_new);
+    ChunkPlan pl = chunk_plan(p, a.max_new);
+    // Documents make the weight of an item unknown (tiles without any of its documents are skipped): where every block has
+    // several items anyway, they are drawn whole.  2 x 32 heads, 2 K tokens of four documents: 85 us shared out, 76 drawn.
+    pl.drawn = a.mods.documents && pl.row_slots > kFewRows && pl.n_items >= 2 * pl.grid;
     if (pl.n_items < 0) return CSP_ERR_UNSUPPORTED;      // key tiles are counted in 32 bits
     const PartialLayout lay = partial_layout(p, pl);
     ChunkParts* const parts = reinterpret_cast<ChunkParts*>(static_cast<char*>(ws) + lay.parts);
@@ -863,12 +882,11 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
             return CSP_ERR_UNSUPPORTED;
         st = p.head_dim == 64 ? launch_nh<1>(a, pl, tq, tk, tv, parts, partial, ml, s) : launch_nh<2>(a, pl, tq, tk, tv, parts, partial, ml, s);
     }
-    // a single block cuts nothing, and an item is cut only where both parts have min_tiles
-    if (st != CSP_OK || pl.grid == 1 || p.out_capacity <= (2 * pl.min_tiles - 1) * pl.key_tile) return st;
-    const dim3 blocks(pl.grid, (pl.row_slots + kJoinRows - 1) / kJoinRows);
+    // nothing is cut where items are drawn, by a single block, and where two parts of min_tiles are more than a cache has
+    if (st != CSP_OK || pl.drawn || pl.grid == 1 || p.out_capacity <= (2 * pl.min_tiles - 1) * pl.key_tile) return st;
     const bool few = pl.row_slots <= kFewRows;
-    if (p.head_dim == 64) (few ? chunk_join_kernel<64, 8> : chunk_join_kernel<64, 4>)<<<blocks, 128, 0, s>>>(a, pl, parts, partial, ml);
-    else (few ? chunk_join_kernel<128, 8> : chunk_join_kernel<128, 4>)<<<blocks, 256, 0, s>>>(a, pl, parts, partial, ml);
+    if (p.head_dim == 64) (few ? join_parts<64, 8, 8> : join_parts<64, 16, 2>)(a, pl, parts, partial, ml, s);
+    else (few ? join_parts<128, 8, 8> : join_parts<128, 16, 2>)(a, pl, parts, partial, ml, s);
     return cudaGetLastError() == cudaSuccess ? CSP_OK : CSP_ERR_CUDA;
 }
 

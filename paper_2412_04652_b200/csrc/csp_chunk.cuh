@@ -14,6 +14,8 @@ struct ChunkPlan {                                       // sizes that host and 
     int grid;                                            // resident blocks
     int key_tile, min_tiles;                             // keys per tile; tiles that a part of a cut item has at least
     int item_cost;                                       // what an item costs besides its key tiles, in key tiles
+    bool drawn;                                          // items are drawn whole from a counter instead of shared out
+    int snap;                                            // tiles by which a share may differ from an equal one to avoid a cut
 };
 
 // What a block says about the items it was given only part of (see Share).
@@ -54,8 +56,8 @@ __device__ __forceinline__ PairRange pair_range(const ChunkArgs& a, const ChunkP
 // The resident blocks share the work evenly, whatever the lengths are: laid end to end, the items (a pair of row tiles of one
 // unit, `tiles` key tiles and item_cost more) are cut into as many equal shares as there are blocks.  A cut inside an item
 // divides its key tiles; the parts are joined afterwards.  Cuts that fall near an item's end go to the end (a share
-// may be an eighth larger or smaller), so that work that divides by itself is not cut at all, and no share is smaller
-// than an item of min_tiles tiles.  Block c handles tiles [tile0, ...) of item0 up to [.., tile1) of item1: at most its
+// may be an eighth, but no more than `snap` tiles, larger or smaller), so that work that divides by itself is not cut at
+// all, and no share is smaller than an item of min_tiles tiles.  Block c handles tiles [tile0, ...) of item0 up to [.., tile1) of item1: at most its
 // first item is the rest of a cut one (partial result 2 c) and its last one the beginning (2 c + 1).
 struct Share { int item0, tile0, item1, tile1; };
 __device__ __forceinline__ int item_weight(const ChunkArgs& a, const ChunkPlan& pl, int item, bool flag, int& tiles) {
@@ -92,7 +94,7 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& a, const ChunkPlan&
     const int sums = lane < kThreads / 32 ? scratch[lane] : 0;
     const int total = __reduce_add_sync(0xffffffffu, sums);
     const int before = __reduce_add_sync(0xffffffffu, lane < warp ? sums : 0) + x - mine;
-    const int share = max((total + int(gridDim.x) - 1) / int(gridDim.x), pl.item_cost + pl.min_tiles), snap = share / 8;
+    const int share = max((total + int(gridDim.x) - 1) / int(gridDim.x), pl.item_cost + pl.min_tiles), snap = min(share / 8, pl.snap);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const long long cut = (long long)(share) * (blockIdx.x + k);
