@@ -145,11 +145,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, -1, 0, 0};
         // Items drawn whole, one after the other, are the last tokens of every unit first: these see the most keys, and an item
         // drawn near the end is a short one.
-        const bool drawn = kDoc && pl.drawn;
+        const bool drawn = kDoc && share.drawn;
         const int n_units = pl.n_items / pl.n_pairs;
         auto unit_of = [&](int item) { return drawn ? item % n_units : item / pl.n_pairs; };
         ItemDraw draw;
-        if (drawn) share = Share{-1, 0, pl.n_items, 0};
         const uint32_t tiles_per_page = uint32_t(a.page_rows) / uint32_t(kTileKeys);      // (dense: not used)
         auto page_of = [&](int b, int tile) {            // the page of a tile that lies inside the cache
             return a.page_table[int64_t(b) * a.max_pages + uint32_t(tile) / tiles_per_page];
@@ -782,7 +781,7 @@ void join_parts(const ChunkArgs& a, const ChunkPlan& pl, const ChunkParts* parts
 
 // Up to sixteen query rows per KV head (single tokens above all) go to the kernel that streams the cache through
 // warp-level products: its rows are spread over all threads, where a tcgen05 row tile would leave most of them idle.
-// Measured for one token, 32 sequences x 32 heads, 410 - 1640 rows each, d = 128: TODO us there, 173 us in row tiles.
+// Measured for one token, 32 sequences x 32 heads, 410 - 1640 rows each, d = 128: 112 us there, 173 us in row tiles.
 constexpr int kFewRows = 16;
 
 ChunkPlan chunk_plan(const csp_params& p, int max_new) {
@@ -860,7 +859,8 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
                              const csp_tensor& v, const csp_pages* pages, void* ws, cudaStream_t s) {
     ChunkPlan pl = chunk_plan(p, a.max_new);
     // Documents make the weight of an item unknown (tiles without any of its documents are skipped): where every block has
-    // several items anyway, they are drawn whole.  2 x 32 heads, 2 K tokens of four documents: 85 us shared out, 76 drawn.
+    // several items anyway, and none is longer than a share, they are drawn whole.  2 x 32 heads, 2 K tokens of four documents:
+    // 101 us shared out, 79 drawn with the longest first; in ascending order it was a tenth slower.
     pl.drawn = a.mods.documents && pl.row_slots > kFewRows && pl.n_items >= 2 * pl.grid;
     if (pl.n_items < 0) return CSP_ERR_UNSUPPORTED;      // key tiles are counted in 32 bits
     const PartialLayout lay = partial_layout(p, pl);
@@ -882,8 +882,8 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
             return CSP_ERR_UNSUPPORTED;
         st = p.head_dim == 64 ? launch_nh<1>(a, pl, tq, tk, tv, parts, partial, ml, s) : launch_nh<2>(a, pl, tq, tk, tv, parts, partial, ml, s);
     }
-    // nothing is cut where items are drawn, by a single block, and where two parts of min_tiles are more than a cache has
-    if (st != CSP_OK || pl.drawn || pl.grid == 1 || p.out_capacity <= (2 * pl.min_tiles - 1) * pl.key_tile) return st;
+    // nothing is cut by a single block, and where two parts of min_tiles are more than a cache has
+    if (st != CSP_OK || pl.grid == 1 || p.out_capacity <= (2 * pl.min_tiles - 1) * pl.key_tile) return st;
     const bool few = pl.row_slots <= kFewRows;
     if (p.head_dim == 64) (few ? join_parts<64, 8, 8> : join_parts<64, 16, 2>)(a, pl, parts, partial, ml, s);
     else (few ? join_parts<128, 8, 8> : join_parts<128, 16, 2>)(a, pl, parts, partial, ml, s);

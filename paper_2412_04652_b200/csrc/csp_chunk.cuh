@@ -14,7 +14,7 @@ struct ChunkPlan {                                       // sizes that host and 
     int grid;                                            // resident blocks
     int key_tile, min_tiles;                             // keys per tile; tiles that a part of a cut item has at least
     int item_cost;                                       // what an item costs besides its key tiles, in key tiles
-    bool drawn;                                          // items are drawn whole from a counter instead of shared out
+    bool drawn;                                          // items may be drawn whole from a counter instead of shared out
     int snap;                                            // tiles by which a share may differ from an equal one to avoid a cut
 };
 
@@ -59,7 +59,7 @@ __device__ __forceinline__ PairRange pair_range(const ChunkArgs& a, const ChunkP
 // may be an eighth, but no more than `snap` tiles, larger or smaller), so that work that divides by itself is not cut at
 // all, and no share is smaller than an item of min_tiles tiles.  Block c handles tiles [tile0, ...) of item0 up to [.., tile1) of item1: at most its
 // first item is the rest of a cut one (partial result 2 c) and its last one the beginning (2 c + 1).
-struct Share { int item0, tile0, item1, tile1; };
+struct Share { int item0, tile0, item1, tile1; bool drawn; };
 __device__ __forceinline__ int item_weight(const ChunkArgs& a, const ChunkPlan& pl, int item, bool flag, int& tiles) {
     const int u = item / pl.n_pairs, pair = item - u * pl.n_pairs;
     const PairRange x = pair_range(a, pl, u, pair);
@@ -70,7 +70,7 @@ __device__ __forceinline__ int item_weight(const ChunkArgs& a, const ChunkPlan& 
     tiles = x.count > 0 ? x.tiles : 0;
     return x.count > 0 ? x.tiles + pl.item_cost : 0;
 }
-// All threads of the block; scratch: 36 words of shared memory.  Every block goes over all items (a few per thread): that
+// All threads of the block; scratch: 68 words of shared memory.  Every block goes over all items (a few per thread): that
 // costs less than a launch of its own would.  (The launcher has made sure that the total fits 30 bits.)
 template <int kThreads>
 __device__ __forceinline__ Share find_share(const ChunkArgs& a, const ChunkPlan& pl, int* scratch) {
@@ -78,16 +78,21 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& a, const ChunkPlan&
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (pl.n_items + kThreads - 1) / kThreads;
     const int i0 = min(tid * per, pl.n_items), i1 = min(i0 + per, pl.n_items);
-    int mine = 0, tiles = 0;
+    int mine = 0, most = 0, tiles = 0;
 #pragma unroll 4
-    for (int i = i0; i < i1; ++i) mine += item_weight(a, pl, i, blockIdx.x == 0, tiles);
+    for (int i = i0; i < i1; ++i) {
+        const int w = item_weight(a, pl, i, blockIdx.x == 0, tiles);
+        mine += w;
+        most = max(most, w);
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
     int x = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, x, d);
         if (lane >= d) x += y;
     }
-    if (lane == 31) scratch[warp] = x;
+    if (lane == 31) { scratch[warp] = x; scratch[36 + warp] = most; }
     int* const found = scratch + 32;                     // two (item, tile) pairs
     if (tid < 2) { found[2 * tid] = pl.n_items; found[2 * tid + 1] = 0; }
     __syncthreads();
@@ -114,7 +119,11 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& a, const ChunkPlan&
         }
     }
     __syncthreads();
-    const Share mine_now = {found[0], found[1], found[2], found[3]};
+    Share mine_now = {found[0], found[1], found[2], found[3], false};
+    if (pl.drawn) {                                      // not where one item is more than a share
+        most = __reduce_max_sync(0xffffffffu, lane < kThreads / 32 ? scratch[36 + lane] : 0);
+        if (most <= share) mine_now = Share{-1, 0, pl.n_items, 0, true};
+    }
     __syncthreads();                                     // the scratch is free again
     return mine_now;
 }

@@ -431,3 +431,13 @@ def test_shares_without_the_tokens_documents(csp, T):
     _run(csp, case, 128, documents=doc, what="the last of five")
     _run(csp, case, 0, documents=(doc == 4).int() * torch.tensor(7, dtype=torch.int32) + (doc == 1).int() * torch.tensor(7, dtype=torch.int32),
          what="the second and the last are one")
+
+
+def test_documents_of_one_long_unit_among_many(csp):
+    """More items than are shared out as a rule, one of them longer than everybody's share: it is cut all the same."""
+    B, H, cap, T = 80, 4, 5000, 20
+    rows = np.full((B, H), T, dtype=np.int64)
+    rows[3, 1] = cap
+    case = _case(T, B, H, H, 64, cap, rows, [T] * B)
+    doc = (torch.arange(cap, dtype=torch.int32) % 3)[None, :].expand(B, cap).contiguous()
+    _run(csp, case, 0, documents=doc)
