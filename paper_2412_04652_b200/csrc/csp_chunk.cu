@@ -488,9 +488,12 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     if (lane == 0) mbar_arrive(ent_empty + 8 * e);
                     continue;
                 }
+                warp_wait(s_full + 8 * g, n_mine & 1u, abort_flag);
                 if (t0 + kTileKeys > rows) {
                     // Rows past the end hold whatever the cache holds: their weights are zero, but zero times a non-finite
-                    // value is not, so clear these rows of V.  (Both groups may do it: they write the same zeros.)
+                    // value is not, so clear these rows of V.  (Both groups may do it: they write the same zeros.)  Only now that
+                    // S is there: the product with what this stage held before has been issued, so that stage's barrier cannot be two
+                    // phases behind, where the parity waited for would look complete.
                     const uint32_t s = v_stage % NST;
                     warp_wait(kv_full + 8 * s, (v_stage / NST) & 1u, abort_flag);
                     for (int j = tid % (32 * kGroupWarps); j < (kTileKeys - (rows - t0)) * NH * 8; j += 32 * kGroupWarps) {
@@ -500,7 +503,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
-                warp_wait(s_full + 8 * g, n_mine & 1u, abort_flag);
                 tc_fence_after();
                 if (live) {
                     constexpr bool kScaled = kCap || kBias;           // the logits are scaled before the maximum is known

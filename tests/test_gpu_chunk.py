@@ -441,3 +441,28 @@ def test_documents_of_one_long_unit_among_many(csp):
     case = _case(T, B, H, H, 64, cap, rows, [T] * B)
     doc = (torch.arange(cap, dtype=torch.int32) % 3)[None, :].expand(B, cap).contiguous()
     _run(csp, case, 0, documents=doc)
+
+
+@pytest.mark.parametrize("page_rows", [0, 256])
+def test_ends_of_caches_under_load(csp, page_rows):
+    """Tiles that end behind the last row, in many units at once and call after call: every call gives the first one's bits."""
+    B, H, T, cap = 6, 32, 60, 1103
+    g = np.random.RandomState(8)
+    rows = g.randint(900, cap + 1, size=(B, H))
+    new = [60, 41, 59, 18, 33, 60]
+    q, k, v, rows, new = _case(T, B, H, H, 128, cap, rows, new)
+    p = csp.Params(B, H, H, 128, 1, 0, cap, cap)
+    ws, first = csp.new_chunk_workspace(p, T), None
+    q, k, v, rows, new = (x.cuda() for x in (q, k, v, rows, new))
+    kp, vp, table = paged_copy(k, v, rows, page_rows, 1) if page_rows else (None, None, None)
+    for _ in range(60):
+        out = torch.zeros(B, T, H, 128, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+        if page_rows:
+            csp.chunk_attn_paged(p, q, kp, vp, table, rows, out, ws, n_new=new)
+        else:
+            csp.chunk_attn(p, q, k, v, rows, out, ws, n_new=new)
+        first = out if first is None else first
+        assert torch.equal(out, first)
+    few = slice(0, 2)                                   # (the definition is slow: two heads of it)
+    ref = reference(q[:, few].cpu(), k[:, few].cpu(), v[:, few].cpu(), rows[:, few].cpu(), new.cpu())
+    assert_chunk_close(first[:, few], None, ref, new.cpu())
