@@ -22,7 +22,6 @@
 // softmax runs while the tensor cores work for the other.
 #include <limits.h>
 
-
 #include "csp_chunk.cuh"
 #include "csp_tc.cuh"
 
@@ -572,7 +571,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                             warp_wait(pv_done + 8 * g, (n_mine - 1u) & 1u, abort_flag);
                             tc_fence_after();
 #pragma unroll 1
-                            for (int c = 0; c < D / 2; c += 16) {     
+                            for (int c = 0; c < D / 2; c += 16) {
                                 uint32_t o[16];
                                 tc_ld_row16(o, my_o + c);
                                 tc_wait_ld();

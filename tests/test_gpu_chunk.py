@@ -466,3 +466,47 @@ def test_ends_of_caches_under_load(csp, page_rows):
     few = slice(0, 2)                                   # (the definition is slow: two heads of it)
     ref = reference(q[:, few].cpu(), k[:, few].cpu(), v[:, few].cpu(), rows[:, few].cpu(), new.cpu())
     assert_chunk_close(first[:, few], None, ref, new.cpu())
+
+
+# ---- where the tensors live, and what is captured
+
+def test_tensors_on_another_device_are_refused(csp):
+    q, k, v, rows, new = _case(40, 1, 4, 2, 64, 100, [100, 90], [3])
+    p = csp.Params(1, 4, 2, 64, 1, 0, 100, 100)
+    ws, out = csp.new_chunk_workspace(p, 3), torch.zeros(1, 4, 3, 64, dtype=torch.bfloat16, device="cuda")
+    good = dict(q=q.cuda(), k=k.cuda(), v=v.cuda(), n_rows=rows.cuda(), out=out, ws=ws, n_new=new.cuda())
+    for name in good:
+        bad = dict(good, **{name: good[name].cpu()})
+        with pytest.raises(ValueError):
+            csp.chunk_attn(p, bad["q"], bad["k"], bad["v"], bad["n_rows"], bad["out"], bad["ws"], n_new=bad["n_new"])
+    for m in (csp.ScoreMods(slopes=torch.ones(4)), csp.ScoreMods(documents=torch.zeros(1, 100, dtype=torch.int32)),
+              csp.ScoreMods(prefix=torch.zeros(1, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            csp.chunk_attn(p, good["q"], good["k"], good["v"], good["n_rows"], out, ws, n_new=good["n_new"], mods=m)
+
+
+@pytest.mark.parametrize("T,B,H,cap", [(2, 2, 2, 6000), (40, 1, 2, 6000), (20, 4, 80, 260)])
+def test_captured_calls_replay_on_new_inputs(csp, T, B, H, cap):
+    """Cut items and their joining, few rows and many, and items drawn from a counter, each replayed twice."""
+    doc = (torch.arange(cap, dtype=torch.int32) * 4 // cap)[None, :].expand(B, cap).contiguous().cuda()
+    cases = [_case(50 + i, B, H, H, 64, cap, np.full((B, H), cap - 7 * i), [T] * B) for i in range(2)]
+    p, dev = csp.Params(B, H, H, 64, 1, 0, cap, cap), [t.cuda() for t in cases[0]]
+    ws, out = csp.new_chunk_workspace(p, T), torch.zeros(B, H, T, 64, dtype=torch.bfloat16, device="cuda")
+    mods = csp.ScoreMods(documents=doc)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        csp.chunk_attn(p, *dev[:4], out, ws, n_new=dev[4], mods=mods)
+    for c in cases[::-1]:
+        for d, s in zip(dev, c):
+            d.copy_(s)
+        seen = []
+        for _ in range(2):
+            out.zero_()
+            graph.replay()
+            seen.append(out.clone())
+        csp.chunk_attn(p, *dev[:4], out, ws, n_new=dev[4], mods=mods)
+        assert csp.device_status(ws) == 0
+        assert torch.equal(seen[0], out) and torch.equal(seen[1], out)
+        two = slice(0, 2)
+        ref = reference(c[0][:1, two], c[1][:1, two], c[2][:1, two], c[3][:1, two], c[4][:1], documents=doc[:1].cpu())
+        assert_chunk_close(out[:1, two], None, ref, c[4][:1])
