@@ -20,6 +20,10 @@
 // With more than 128 rows in an item, group g takes row tile g and both see every key tile; with fewer, both take the
 // same rows and alternate over the key tiles (their results are joined when the item ends): either way one group's
 // softmax runs while the tensor cores work for the other.
+//
+// Bound by the exponentials and the matrix products, which need the same 1024 clocks per 128 x 128 tile and are both busy 54 % of
+// the time.  Measured at d = 128: 513 - 1024 tokens over 8 K - 32 K positions, 4 sequences, 28 / 4 heads (904 GFLOP): 840 us, 1.08
+// PFLOP/s; 512 tokens over 4 K, 32 heads (32 GFLOP): 47 us, of which 10 are the start and end of items, and 10 us for joining.
 #include <limits.h>
 
 #include "csp_chunk.cuh"
