@@ -65,7 +65,7 @@ struct ChunkShape {
         s.pair = off;    off += 2 * 4 * 128 * 4;                         // [parity][group][half][row]: exchanged by the halves of a row
         s.join = off;    off += 2 * 2 * 128 * 4;                         // [group][row] reference, then sum
         s.bars = off;    off += kBars * 8;
-        s.misc = off;    off += 16;
+        s.misc = off;    off += 32;
         s.total = off;
         return s;
     }
@@ -100,6 +100,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     const uint32_t pair_bar = drain_bar + 8;                                      // [2][4]: the two warps of a lane quarter
     volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + sp.misc);
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(base_ptr + sp.misc + 4);
+    volatile uint32_t* const fills = tmem_slot + 2;      // when the producer ends: its loads into the ring and into the slots of Q
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
@@ -222,8 +223,9 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     if (!(q_slots & kSlot0 << slot)) continue;
                     warp_wait(q_empty + 8 * slot, (q_uses[slot] & 1u) ^ 1u, abort_flag);
                     ok = ok && !warp_aborted(abort_flag);
+                    if (!ok) return;
                     ++q_uses[slot];
-                    if (ok && lane == 0) {
+                    if (lane == 0) {
                         mbar_expect_tx(q_full + 8 * slot, uint32_t(NH * a.group * min(pl.tok_tile, a.max_new)) * 128u);
 #pragma unroll
                         for (int hb = 0; hb < NH; ++hb)
@@ -298,7 +300,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     const uint32_t s = n_stage % NST;
                     warp_wait(kv_empty + 8 * s, ((n_stage / NST) & 1u) ^ 1u, abort_flag);
                     ok = ok && !warp_aborted(abort_flag);
-                    if (ok && lane == 0) {
+                    if (!ok) break;
+                    if (lane == 0) {
                         mbar_expect_tx(kv_full + 8 * s, kStageBytes);
                         tma_load_5d(base + s * kStageBytes, which ? &tmap_v : &tmap_k, kv_full + 8 * s, 0, row, 0, h, outer);
                     }
@@ -313,15 +316,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         }
         if (ok) announce(publish(lane == kFlags ? kStop : 0));
         if (lane == 0) {
-            if (!ok) {
-                // let copies that were issued land before the CTA's shared memory is given up
-                for (int s = 0; s < NST; ++s) {
-                    const unsigned long long t0 = global_ns();
-                    while (!mbar_try_wait(kv_full + 8 * s, 0) && !mbar_try_wait(kv_full + 8 * s, 1) && global_ns() - t0 < kWaitLimitNs / 8) {}
-                }
-                atomicOr(a.status, CSP_DEV_TIMEOUT);
-            }
             if (drawn) draw.done();
+            fills[0] = n_stage;
+            fills[1] = q_uses[0];
+            fills[2] = q_uses[1];
         }
         __syncwarp();
     } else if (warp == kChMmaWarp) {
@@ -696,6 +694,12 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
 
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag && tid == 0) {
+        atomicOr(a.status, CSP_DEV_TIMEOUT);
+        drain_ring(kv_full, fills[0], NST);
+        drain_ring(q_full, fills[1], 1);
+        drain_ring(q_full + 8, fills[2], 1);
+    }
     if (warp == kChMmaWarp) {
         tc_fence_after();
         tmem_dealloc(tmem, 512u);

@@ -89,6 +89,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     }
     const Share share = find_share<kFewThreads>(a, pl, reinterpret_cast<int*>(merge));      // (synchronises)
 
+    uint32_t fills = 0;                                  // of the ring, by this thread
     if (warp == kFewProducer) {
         // =============================== producer ===============================
         uint32_t it = 0;
@@ -98,6 +99,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
             const uint32_t s = it % NST;
             warp_wait(empty_bar + 8 * s, ((it / NST) & 1u) ^ 1u, abort_flag);
             ok = ok && !warp_aborted(abort_flag);
+            if (!ok) return s;
             if (lane < kItemWords) info[s * kItemWords + lane] = lane == kwItem ? item : lane == kwTile ? tile : word;
             ++it;
             return s;
@@ -201,10 +203,11 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                     looked = true;
                 }
                 const bool elected = elect_one();
+                uint32_t issued = 0;                     // (of the elected lane: fewer than there are tiles if a wait runs out)
                 if (elected && ok) {
                     int page = a.page_table && tile0 + 1 < tile1 ? page_of(b, tile0 + 1) : 0;
-                    for (int tile = tile0 + 1; tile < tile1; ++tile) {
-                        const uint32_t n = it + uint32_t(tile - tile0 - 1), s = n % NST;
+                    for (int tile = tile0 + 1; tile < tile1; ++tile, ++issued) {
+                        const uint32_t n = it + issued, s = n % NST;
                         const int outer = a.page_table ? checked(page) : b;
                         if (a.page_table && tile + 1 < tile1) page = page_of(b, tile + 1);        // in time for the next tile
                         lean_wait(empty_bar + 8 * s, ((n / NST) & 1u) ^ 1u, abort_flag);
@@ -213,7 +216,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                         load(s, tile, outer);
                     }
                 }
-                it += uint32_t(max(tile1 - tile0 - 1, 0));
+                it += __reduce_max_sync(0xffffffffu, issued);
                 look_up(u + 1);
                 __syncwarp();
                 ok = ok && !warp_aborted(abort_flag);
@@ -266,16 +269,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
             marker(u);
         }
         if (ok) marker(-1);
-        if (lane == 0) {
-            if (!ok) {
-                // let copies that were issued land before the CTA's shared memory is given up
-                for (int s = 0; s < NST; ++s) {
-                    const unsigned long long t0 = global_ns();
-                    while (!mbar_try_wait(full_bar + 8 * s, 0) && !mbar_try_wait(full_bar + 8 * s, 1) && global_ns() - t0 < kWaitLimitNs / 8) {}
-                }
-                atomicOr(a.status, CSP_DEV_TIMEOUT);
-            }
-        }
+        if (lane == 0) fills = it;
     } else if (warp == kFewFinisher) {
         // =============================== finisher ===============================
         for (uint32_t n = 0;; ++n) {
@@ -493,6 +487,12 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
             if (lane == 0) { mbar_arrive(done_bar); mbar_arrive(empty_bar + 8 * s); }
             if (w < 0) break;                            // no more items: the finisher reads that too
         }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (*abort_flag) {
+        if (tid == 0) atomicOr(a.status, CSP_DEV_TIMEOUT);
+        drain_ring(full_bar, fills, NST);
     }
 }
 

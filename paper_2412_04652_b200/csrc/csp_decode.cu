@@ -137,6 +137,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
     __syncthreads();
 
+    uint32_t fills = 0;                            // of the ring, by this thread
     if (warp == kDecWarps) {
         // =============================== TMA producer ===============================
         if (lane == 0) {
@@ -172,16 +173,9 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 const int s = it % kDecStages;
                 mbar_wait(empty_bar + 8 * s, (uint32_t(it / kDecStages) & 1u) ^ 1u, abort_flag);
                 item_q[j % kQueue] = -1;
-                mbar_arrive(full_bar + 8 * s);
+                if (!*abort_flag) { mbar_arrive(full_bar + 8 * s); ++it; }
             }
-            if (*abort_flag) {
-                // let copies that were issued land before the CTA's shared memory is given up
-                for (int s = 0; s < kDecStages; ++s) {
-                    const unsigned long long t0 = global_ns();
-                    while (!mbar_try_wait(full_bar + 8 * s, 0) && !mbar_try_wait(full_bar + 8 * s, 1) &&
-                           global_ns() - t0 < kWaitLimitNs / 8) {}
-                }
-            }
+            fills = uint32_t(it);
         }
     } else {
         // =============================== consumer warps ===============================
@@ -322,7 +316,12 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             }
             // the barrier at the top of the next item also frees the merge area
         }
-        if (*abort_flag && tid == 0) atomicOr(a.status, CSP_DEV_TIMEOUT);
+    }
+    __syncwarp();
+    __syncthreads();
+    if (*abort_flag) {
+        if (tid == 0) atomicOr(a.status, CSP_DEV_TIMEOUT);
+        drain_ring(full_bar, fills, kDecStages);
     }
 }
 

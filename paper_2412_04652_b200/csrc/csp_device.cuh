@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "csp_ring.cuh"
+
 namespace csp {
 namespace dev {
 
@@ -60,6 +62,17 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
         if (mbar_try_wait(bar, parity)) return true;
         if (*abort_flag) return false;
         if (global_ns() - t0 > kWaitLimitNs) { *abort_flag = 1; return false; }
+    }
+}
+// Lets the copies that were issued land before the CTA's shared memory is given up (one thread, after a wait that ran out, when
+// nobody in the CTA fills or waits any more): waits for the last of `issued` fills at every stage of the ring, with a limit
+// for all of them together.
+__device__ __forceinline__ void drain_ring(uint32_t full_bar, uint32_t issued, uint32_t stages) {
+    const unsigned long long t0 = global_ns();
+    for (uint32_t s = 0; s < stages; ++s) {
+        const int parity = last_fill_parity(issued, stages, s);
+        if (parity < 0) break;
+        while (!mbar_try_wait(full_bar + 8 * s, uint32_t(parity)) && global_ns() - t0 < kWaitLimitNs / 2) {}
     }
 }
 // one lane of a converged warp, the same every time; unlike a test of the lane number it lets the compiler keep what the

@@ -123,6 +123,7 @@ score_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArgs a, const 
     if (warp == kConsumerWarps) {
         // =============================== producer warp ===============================
         cluster_arrive();                         // barrier 1: nothing of ours to publish
+        uint32_t fills = 0;                       // of the ring, by this thread
         if (lane == 0) {
             const int total = my_all + my_cand;
             for (int it = 0; it < total; ++it) {
@@ -136,21 +137,14 @@ score_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArgs a, const 
                 for (int hb = 0; hb < NH; ++hb)
                     tma_load_4d(base + slot * kStageBytes + hb * kBlockBytes, &tmap, full_bar + 8 * slot,
                                 hb * int(128 / sizeof(T)), tile * kTileKeys, h, b);
-            }
-            if (*abort_flag) {
-                // let copies that were issued land before the CTA's shared memory is given up
-                const int issued = total < n_stages ? total : n_stages;
-                for (int s = 0; s < issued; ++s) {
-                    const unsigned long long t0 = global_ns();
-                    while (!mbar_try_wait(full_bar + 8 * s, 0) && !mbar_try_wait(full_bar + 8 * s, 1) &&
-                           global_ns() - t0 < kWaitLimitNs) {}
-                }
+                ++fills;
             }
         }
         __syncwarp();
         cluster_wait();
         cluster_arrive();                         // barrier 2: keep shared memory alive for peers
         cluster_wait();
+        if (*abort_flag) drain_ring(full_bar, fills, uint32_t(n_stages));
         return;
     }
 

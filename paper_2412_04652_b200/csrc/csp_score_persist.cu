@@ -178,6 +178,7 @@ score_tc_persist_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArg
         return u < n_units ? u : -1;
     };
 
+    uint32_t fills = 0;                            // of the ring, by this thread
     if (warp == kPsProducerWarp) {
         // =============================== TMA producer ===============================
         if (lane == 0) {
@@ -202,14 +203,7 @@ score_tc_persist_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArg
                                     hb * 64, row_now, x.h, outer_now);
                 }
             }
-            if (*abort_flag) {
-                // let copies that were issued land before the CTA's shared memory is given up
-                for (int s = 0; s < n_stages; ++s) {
-                    const unsigned long long t0 = global_ns();
-                    while (!mbar_try_wait(full_k + 8 * s, 0) && !mbar_try_wait(full_k + 8 * s, 1) &&
-                           global_ns() - t0 < kWaitLimitNs / 8) {}
-                }
-            }
+            fills = uint32_t(it);
         }
         __syncwarp();
     } else if (warp == kPsMmaWarp) {
@@ -493,6 +487,7 @@ score_tc_persist_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArg
     }
     cluster_arrive();
     cluster_wait();
+    if (*abort_flag) drain_ring(full_k, fills, uint32_t(n_stages));
 }
 
 template <int NH>

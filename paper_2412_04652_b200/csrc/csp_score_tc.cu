@@ -164,6 +164,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArgs a, con
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
 
+    uint32_t fills = 0;                            // of the ring, by this thread
     if (warp == kProducerWarp) {
         // =============================== TMA producer ===============================
         cluster_arrive();                         // cluster barrier 1: nothing of ours to publish
@@ -184,15 +185,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArgs a, con
                 for (int hb = 0; hb < NH; ++hb)
                     tma_load_4d(base + slot * kStageBytes + hb * kBlockBytes, &tmap, full_k + 8 * slot,
                                 hb * 64, row_now, h, outer_now);
-            }
-            if (*abort_flag) {
-                // let copies that were issued land before the CTA's shared memory is given up
-                const int issued = total < n_stages ? total : n_stages;
-                for (int s = 0; s < issued; ++s) {
-                    const unsigned long long t0 = global_ns();
-                    while (!mbar_try_wait(full_k + 8 * s, 0) && !mbar_try_wait(full_k + 8 * s, 1) &&
-                           global_ns() - t0 < kWaitLimitNs) {}
-                }
+                ++fills;
             }
         }
         __syncwarp();
@@ -513,6 +506,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArgs a, con
     }
     cluster_arrive();                             // cluster barrier 2
     cluster_wait();
+    if (*abort_flag) drain_ring(full_k, fills, uint32_t(n_stages));
 }
 
 template <int NH, int G, bool kHist>
