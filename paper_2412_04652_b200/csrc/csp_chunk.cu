@@ -860,8 +860,12 @@ csp_status launch_nh(const ChunkArgs& a, const ChunkPlan& pl, const CUtensorMap&
 }  // namespace
 
 size_t chunk_workspace_bytes(const csp_params& p, int max_new) {
-    const ChunkPlan pl = chunk_plan(p, max_new);
-    return partial_layout(p, pl).total;
+    // Enough for shorter chunks as well: those of few rows have smaller key tiles, so more blocks have a share of them, and may
+    // need more than a somewhat longer chunk.  (Among chunks of either kind the size grows with max_new.)
+    const int few = kFewRows / (p.n_q_heads / p.n_kv_heads);
+    const size_t mine = partial_layout(p, chunk_plan(p, max_new)).total;
+    const size_t shorter = partial_layout(p, chunk_plan(p, max_new < few ? max_new : few)).total;
+    return mine > shorter ? mine : shorter;
 }
 
 csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_tensor& q, const csp_tensor& k,

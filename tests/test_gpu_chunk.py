@@ -510,3 +510,18 @@ def test_captured_calls_replay_on_new_inputs(csp, T, B, H, cap):
         two = slice(0, 2)
         ref = reference(c[0][:1, two], c[1][:1, two], c[2][:1, two], c[3][:1, two], c[4][:1], documents=doc[:1].cpu())
         assert_chunk_close(out[:1, two], None, ref, c[4][:1])
+
+
+def test_one_workspace_for_chunks_of_all_lengths(csp):
+    """Made for the longest chunk, used for that one, for the lengths around a change of kernel and for single tokens."""
+    for Hq, Hkv, longest in ((28, 4, 3), (4, 4, 40), (16, 2, 300)):
+        cap = 2000
+        ws = csp.new_chunk_workspace(csp.Params(1, Hq, Hkv, 128, 1, 0, cap, cap), longest)
+        for T in sorted({longest, 1, 2, min(longest, 17), min(longest, 16), min(longest, 11)}, reverse=True):
+            q, k, v, rows, new = _case(T, 1, Hq, Hkv, 128, cap, [cap - 3 * h for h in range(Hkv)], [T])
+            p = csp.Params(1, Hq, Hkv, 128, 1, 0, cap, cap)
+            out = torch.zeros(1, Hq, T, 128, dtype=torch.bfloat16, device="cuda")
+            csp.chunk_attn(p, q.cuda(), k.cuda(), v.cuda(), rows.cuda(), out, ws)
+            assert csp.device_status(ws) == 0
+            if T <= 17:
+                assert_chunk_close(out, None, reference(q, k, v, rows, new), new, f"T={T}")

@@ -169,3 +169,14 @@ def test_capacities_past_the_row_index_are_refused(csp):
     p = _params(csp, out_capacity=(1 << 30) + 1)
     assert _chunk(csp, p) == csp.ERR_UNSUPPORTED
     assert _chunk(csp, p, paged=True, pages=csp.CPages(256, 1 << 23 | 1, 128, 9)) == csp.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("batch,n_kv,cap", [(1, 1, 512), (1, 4, 1024), (1, 4, 4096), (1, 8, 1024), (3, 2, 700), (2, 4, 20000)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_workspace_for_longer_chunks_is_enough_for_shorter_ones(csp, batch, n_kv, cap, d):
+    """Also where fewer tokens take another kernel with smaller tiles, whose work is cut into more parts."""
+    for G in range(1, 9):
+        p = _params(csp, batch=batch, n_q_heads=n_kv * G, n_kv_heads=n_kv, head_dim=d, max_len=cap, out_capacity=cap)
+        sizes = [csp.chunk_workspace_bytes(p, T) for T in list(range(0, 300)) + [511, 1024, 5000]]
+        falls = [(T, a, b) for T, (a, b) in enumerate(zip(sizes, sizes[1:])) if b < a]
+        assert not falls, (G, falls[0])
