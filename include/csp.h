@@ -340,8 +340,8 @@ typedef struct {
 
 /* Bytes of scratch that csp_chunk_attn and csp_chunk_attn_paged need for chunks of up to max_new tokens (status word,
  * work counters, partial results of split caches).  The first 256 bytes must be zero before first use
- * (csp_workspace_reset).  Calls, or replays of captured ones, that may run at the same time need a workspace each; the same
- * holds for the workspaces below. */
+ * (csp_workspace_reset).  0 for shapes that these calls refuse.  Calls, or replays of captured ones, that may run at the
+ * same time need a workspace each; the same holds for the workspaces below. */
 size_t csp_chunk_workspace_bytes(const csp_params* p, int32_t max_new);
 
 /*

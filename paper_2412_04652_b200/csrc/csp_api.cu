@@ -585,12 +585,11 @@ csp_status chunk_attn(const csp_params* p, int32_t max_new, const csp_tensor& q,
     if (st != CSP_OK) return st;
     if (max_new < 0 || !q.ptr || !k.ptr || !v.ptr || !n_rows || !out.ptr) return CSP_ERR_INVALID_ARG;
     if (mods && !(mods->softcap == 0.f || (mods->softcap >= 1e-6f && mods->softcap <= 1000.f))) return CSP_ERR_INVALID_ARG;
-    if (p->dtype != CSP_BF16 || (p->head_dim != 64 && p->head_dim != 128)) return CSP_ERR_UNSUPPORTED;
+    const size_t need = chunk_workspace_bytes(*p, max_new);
+    if (need == 0) return CSP_ERR_UNSUPPORTED;
     if (!tensor_ok(*p, q) || !tensor_ok(*p, k) || !tensor_ok(*p, v) || !tensor_ok(*p, out)) return CSP_ERR_UNSUPPORTED;
     if (!rows_apart(*p, out, p->batch, p->n_q_heads, max_new)) return CSP_ERR_UNSUPPORTED;
-    if (int64_t(max_new) * (p->n_q_heads / p->n_kv_heads) > (1 << 24)) return CSP_ERR_UNSUPPORTED;
-    if (p->out_capacity > (1 << 30)) return CSP_ERR_UNSUPPORTED;                 // a row index plus some tiles fits 32 bits
-    if (!status_area_ok(workspace, workspace_bytes, chunk_workspace_bytes(*p, max_new))) return CSP_ERR_WORKSPACE;
+    if (!status_area_ok(workspace, workspace_bytes, need)) return CSP_ERR_WORKSPACE;
     if ((st = check_arch()) != CSP_OK) return st;
     ChunkArgs a;
     a.n_rows = n_rows; a.n_new = n_new;

@@ -860,10 +860,15 @@ csp_status launch_nh(const ChunkArgs& a, const ChunkPlan& pl, const CUtensorMap&
 }  // namespace
 
 size_t chunk_workspace_bytes(const csp_params& p, int max_new) {
+    if (p.dtype != CSP_BF16 || (p.head_dim != 64 && p.head_dim != 128)) return 0;
+    if (p.out_capacity > (1 << 30)) return 0;                                    // a row index plus some tiles fits 32 bits
+    if (int64_t(max_new) * (p.n_q_heads / p.n_kv_heads) > (1 << 24)) return 0;   // and so do a chunk's rows
+    const ChunkPlan pl = chunk_plan(p, max_new);
+    if (pl.n_items < 0) return 0;                                                // key tiles are counted in 32 bits
     // Enough for shorter chunks as well: those of few rows have smaller key tiles, so more blocks have a share of them, and may
     // need more than a somewhat longer chunk.  (Among chunks of either kind the size grows with max_new.)
     const int few = kFewRows / (p.n_q_heads / p.n_kv_heads);
-    const size_t mine = partial_layout(p, chunk_plan(p, max_new)).total;
+    const size_t mine = partial_layout(p, pl).total;
     const size_t shorter = partial_layout(p, chunk_plan(p, max_new < few ? max_new : few)).total;
     return mine > shorter ? mine : shorter;
 }
@@ -875,7 +880,6 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
     // several items anyway, and none is longer than a share, they are drawn whole.  2 x 32 heads, 2 K tokens of four documents:
     // 101 us shared out, 79 drawn with the longest first; in ascending order it was a tenth slower.
     pl.drawn = a.mods.documents && pl.row_slots > kFewRows && pl.n_items >= 2 * pl.grid;
-    if (pl.n_items < 0) return CSP_ERR_UNSUPPORTED;      // key tiles are counted in 32 bits
     const PartialLayout lay = partial_layout(p, pl);
     ChunkParts* const parts = reinterpret_cast<ChunkParts*>(static_cast<char*>(ws) + lay.parts);
     float* const partial = reinterpret_cast<float*>(static_cast<char*>(ws) + lay.o);

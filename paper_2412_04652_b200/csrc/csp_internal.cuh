@@ -216,7 +216,7 @@ struct ChunkArgs {
     ModArgs mods;
     const int32_t* page_table; int32_t max_pages, page_rows, n_pages;   // null: dense cache
 };
-size_t chunk_workspace_bytes(const csp_params& p, int max_new);
+size_t chunk_workspace_bytes(const csp_params& p, int max_new);      // 0: shapes that launch_chunk_attn does not take
 csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_tensor& q, const csp_tensor& k,
                              const csp_tensor& v, const csp_pages* pages, void* ws, cudaStream_t s);
 

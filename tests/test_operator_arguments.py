@@ -180,3 +180,25 @@ def test_a_workspace_for_longer_chunks_is_enough_for_shorter_ones(csp, batch, n_
         sizes = [csp.chunk_workspace_bytes(p, T) for T in list(range(0, 300)) + [511, 1024, 5000]]
         falls = [(T, a, b) for T, (a, b) in enumerate(zip(sizes, sizes[1:])) if b < a]
         assert not falls, (G, falls[0])
+
+
+@pytest.mark.parametrize("kw,max_new", [
+    (dict(dtype="F32", head_dim=64), 4),
+    (dict(head_dim=256), 4),
+    (dict(out_capacity=(1 << 30) + 1), 4),
+    (dict(), 1 << 24), (dict(), (1 << 31) - 1), (dict(n_q_heads=4), (1 << 24) + 1),
+    (dict(batch=16383, out_capacity=1 << 30), 1),        # more key tiles than are counted in 30 bits
+    (dict(batch=4000, out_capacity=1 << 20), 5000),
+])
+def test_shapes_that_the_attention_refuses_have_no_workspace(csp, kw, max_new):
+    if "dtype" in kw:
+        kw = dict(kw, dtype=csp.F32)
+    p = _params(csp, **kw)
+    assert csp.chunk_workspace_bytes(p, max_new) == 0
+    with pytest.raises(csp.CspError):
+        csp.new_chunk_workspace(p, max_new, device="cpu")
+    assert _chunk(csp, p, max_new=max_new) == csp.ERR_UNSUPPORTED
+
+
+def test_the_longest_chunk_has_a_workspace(csp):
+    assert csp.chunk_workspace_bytes(_params(csp, n_q_heads=4), 1 << 24) >= csp.chunk_workspace_bytes(_params(csp, n_q_heads=4), 1 << 23) > 0
