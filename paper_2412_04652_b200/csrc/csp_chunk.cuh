@@ -151,9 +151,6 @@ __device__ __forceinline__ float rcpf(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// n 2^-m, the n of the denominator relative to the reference m: of logits far below zero 2^-m is no float any more, and zero
-// times infinity would be no number
-__device__ __forceinline__ float n_term(float n, float m) { return n > 0.f ? n * ex2f(-m) : 0.f; }
 // 32 bytes at once (the address a multiple of 32)
 __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&v)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"

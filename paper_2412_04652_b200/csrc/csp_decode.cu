@@ -343,7 +343,7 @@ __global__ void decode_merge_kernel(const DecodeArgs a) {
     for (int s = 0; s < used; ++s) m = fmaxf(m, part[s * stride + D]);
     float l = 0.f;
     for (int s = 0; s < used; ++s) l += part[s * stride + D + 1] * ex2f(part[s * stride + D] - m);
-    const float denom = a.n * ex2f(-m) + l;
+    const float denom = n_term(a.n, m) + l;
     for (int c = threadIdx.x; c < D; c += blockDim.x) {
         float v = 0.f;
         for (int s = 0; s < used; ++s) v += part[s * stride + c] * ex2f(part[s * stride + D] - m);
@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(kStepThreads) decode_merge_accumulate_kernel(c
         for (int s = 0; s < used; ++s) m = fmaxf(m, part[s * stride + D]);
         float l = 0.f;
         for (int s = 0; s < used; ++s) l += part[s * stride + D + 1] * ex2f(part[s * stride + D] - m);
-        const float denom = a.n * ex2f(-m) + l;
+        const float denom = n_term(a.n, m) + l;
         const bool ok = used > 0 && denom > 0.f;
         if (threadIdx.x == 0) { ref[g] = m; wgt[g] = ok ? 1.0f / (float(G) * denom) : 0.f; }
         for (int c = threadIdx.x; c < D; c += kStepThreads) {

@@ -29,6 +29,9 @@ __device__ __forceinline__ float ex2f(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// n 2^-m, the n of the denominator relative to the reference m: of logits far below zero 2^-m is no float any more, and zero
+// times infinity would be no number
+__device__ __forceinline__ float n_term(float n, float m) { return n > 0.f ? n * ex2f(-m) : 0.f; }
 __device__ __forceinline__ unsigned long long global_ns() {
     unsigned long long t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));

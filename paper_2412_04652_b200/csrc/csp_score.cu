@@ -321,7 +321,7 @@ score_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArgs a, const 
             }
         }
         // weight of one unit of 2^(x-m): 1 / (G (n 2^-m + Z)); padding rows of the window get 0
-        const float denom = a.n * ex2f(-m) + z;
+        const float denom = n_term(a.n, m) + z;
         fstats[tid] = col < W ? make_float2(m, a.weight / denom) : make_float2(0.f, 0.f);
     }
     consumer_sync();

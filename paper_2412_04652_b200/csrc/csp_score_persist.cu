@@ -324,7 +324,7 @@ score_tc_persist_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArg
                 if (tw == 0) {
                     const float m = (lane < W && !x.skip)
                                         ? a.lse[(int64_t(x.b) * a.n_kv_heads + x.h) * W + lane] * 1.4426950408889634f : 0.f;
-                    const float denom = a.n * ex2f(-m) + 1.f;          // (max, sum) = (lse, 1)
+                    const float denom = n_term(a.n, m) + 1.f;          // (max, sum) = (lse, 1)
                     cv_team[lane] = lane < W ? lg2f(a.weight / denom) - m : -INFINITY;
                     mbar_wait(q_ready + 8 * qs, uint32_t(j / kQSets) & 1u, abort_flag);   // label table of this unit
                 }
@@ -385,7 +385,7 @@ score_tc_persist_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArg
                     merge_stats(m, z, cr.x, cr.y);
                 }
                 // weight of 2^(x - m) is 1 / (n 2^-m + Z); fold it and -m into one additive constant
-                const float denom = a.n * ex2f(-m) + z;
+                const float denom = n_term(a.n, m) + z;
                 cv_team[lane] = lane < W ? lg2f(a.weight / denom) - m : -INFINITY;
                 mbar_wait(q_ready + 8 * qs, uint32_t(j / kQSets) & 1u, abort_flag);   // label table of this unit
             }

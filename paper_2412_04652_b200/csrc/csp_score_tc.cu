@@ -349,7 +349,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap, const ScoreArgs a, con
                 }
             }
             // weight of 2^(x - m) is 1 / (G (n 2^-m + Z)); fold it and -m into one additive constant
-            const float denom = a.n * ex2f(-m) + z;
+            const float denom = n_term(a.n, m) + z;
             cvec[tid] = col < W ? lg2f(a.weight / denom) - m : -INFINITY;
         }
         epi_sync();
