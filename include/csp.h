@@ -439,7 +439,9 @@ csp_status csp_pages_fork(const csp_page_state* s, const int32_t* src, const int
  *   moves          [max_moves, 2] int32 device: (from, to) of the pages whose rows csp_pages_copy has to copy next, in
  *                  every layer's pools; n_moves [1] int32 device: how many.  No `to` is a `from`, and none is named twice
  * If the pool, a table row or moves is too small, nothing is changed, n_moves is 0 and CSP_DEV_CAPACITY is flagged; a
- * negative n_rows or n_new does the same with CSP_DEV_BAD_LEN.
+ * negative n_rows or n_new does the same with CSP_DEV_BAD_LEN.  Of contradictions, the entries that may have to be replaced
+ * are looked at: a page that more of them name than it is counted for stays with all of them and keeps its count, one
+ * that is counted free is not given to anybody else; both are flagged CSP_DEV_BAD_LEN.
  */
 csp_status csp_pages_reserve(const csp_page_state* s, const int32_t* n_new_or_null, int32_t whole,
                              int32_t* moves, int32_t max_moves, int32_t* n_moves,

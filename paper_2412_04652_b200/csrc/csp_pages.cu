@@ -45,8 +45,9 @@ __device__ __forceinline__ int32_t ld(const int32_t* p) { return __ldcg(p); }
 // Table entries e = b * max_pages + i as csp_pages_reserve sees them.  A thread takes kPerThread neighbours at a time, so that
 // the chains of dependent loads (sequence, entry, count) of all four are under way together.
 struct Entry { int page; bool claim, fresh; };
+constexpr int kNamed = INT_MAX;                          // in PageArgs::last: a table entry names the page, but it is counted free
 __device__ __forceinline__ void reserve_entries(const PageArgs& a, uint32_t entries, uint32_t e0, bool flag, Entry (&x)[kPerThread],
-                                                int (&refs)[kPerThread]) {
+                                                int (&refs)[kPerThread], int* named) {
     int held[kPerThread], need[kPerThread], first[kPerThread], i[kPerThread];
 #pragma unroll
     for (int j = 0; j < kPerThread; ++j) {
@@ -70,19 +71,22 @@ __device__ __forceinline__ void reserve_entries(const PageArgs& a, uint32_t entr
 #pragma unroll
     for (int j = 0; j < kPerThread; ++j) {
         if (refs[j] <= 0) {
-            if (flag) atomicOr(a.status, CSP_DEV_BAD_LEN);
+            if (flag) { atomicOr(a.status, CSP_DEV_BAD_LEN); a.last[x[j].page] = kNamed; *named = 1; }
             x[j].page = -1;
         }
         x[j].claim = refs[j] > 1;
     }
 }
 
-// A shared page is copied for whoever asks for it, except that the last one to ask keeps it when all who share it ask.
+// A shared page is copied for whoever asks for it, except that the last one to ask keeps it when all who share it ask.  One
+// that more ask for than it is counted for contradicts itself and stays as it is.
 __device__ __forceinline__ void reserve_copies(const PageArgs& a, uint32_t e0, const Entry (&x)[kPerThread],
                                                const int (&refs)[kPerThread], bool (&copies)[kPerThread]) {
 #pragma unroll
-    for (int j = 0; j < kPerThread; ++j)
-        copies[j] = x[j].claim && !(ld(a.claims + x[j].page) == refs[j] && ld(a.last + x[j].page) == int32_t(e0 + j));
+    for (int j = 0; j < kPerThread; ++j) {
+        const int claims = x[j].claim ? ld(a.claims + x[j].page) : 0;
+        copies[j] = x[j].claim && claims <= refs[j] && !(claims == refs[j] && ld(a.last + x[j].page) == int32_t(e0 + j));
+    }
 }
 
 // One block: bound by the latency of its chains of loads (9 us for 12 sequences), with thousands of entries by the scattered
@@ -90,10 +94,10 @@ __device__ __forceinline__ void reserve_copies(const PageArgs& a, uint32_t e0, c
 __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const PageArgs a, const int32_t* n_new, int whole,
                                                                       int2* moves, int max_moves, int32_t* n_moves) {
     __shared__ uint32_t warp_sums[32];
-    __shared__ int fail;
+    __shared__ int fail, named;                          // named: some page is counted free, but a table entry names it
     __shared__ uint32_t sum_want, sum_copy, sum_free;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) { fail = 0; sum_want = sum_copy = sum_free = 0; }
+    if (tid == 0) { fail = named = 0; sum_want = sum_copy = sum_free = 0; }
     __syncthreads();
     // how many pages every sequence needs, and from which on they have to be its own: one warp per sequence
     for (int b = warp; b < a.batch; b += kTableThreads / 32) {
@@ -122,23 +126,25 @@ __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const Page
     bool copies[kPerThread];
     if (!fail) {
         for (uint32_t e0 = tid * kPerThread; e0 < entries; e0 += kStep) {
-            reserve_entries(a, entries, e0, true, x, refs);
+            reserve_entries(a, entries, e0, true, x, refs, &named);
 #pragma unroll
             for (int j = 0; j < kPerThread; ++j)
                 if (x[j].claim) { atomicAdd(a.claims + x[j].page, 1); atomicMax(a.last + x[j].page, int32_t(e0 + j)); }
         }
     }
     __syncthreads();
+    // a page that can be given out; one that is named all the same is left alone
+    auto is_free_page = [&](int p) { return ld(a.refs + p) == 0 && (!named || ld(a.last + p) != kNamed); };
     if (!fail) {
         uint32_t want = 0, copy = 0, free_pages = 0;
         for (uint32_t e0 = tid * kPerThread; e0 < entries; e0 += kStep) {
-            if (entries > kStep) reserve_entries(a, entries, e0, false, x, refs);        // (else they are here still)
+            if (entries > kStep) reserve_entries(a, entries, e0, false, x, refs, &named);        // (else they are here still)
             reserve_copies(a, e0, x, refs, copies);
 #pragma unroll
             for (int j = 0; j < kPerThread; ++j) { copy += copies[j]; want += copies[j] || x[j].fresh; }
         }
 #pragma unroll 4
-        for (int p = tid; p < a.n_pages; p += kTableThreads) free_pages += ld(a.refs + p) == 0;
+        for (int p = tid; p < a.n_pages; p += kTableThreads) free_pages += is_free_page(p);
         want = __reduce_add_sync(0xffffffffu, want);
         copy = __reduce_add_sync(0xffffffffu, copy);
         free_pages = __reduce_add_sync(0xffffffffu, free_pages);
@@ -160,7 +166,7 @@ __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const Page
 #pragma unroll
         for (int j = 0; j < kPerThread; ++j) {
             const int p = p0 + tid * kPerThread + j;
-            is_free[j] = p < a.n_pages && ld(a.refs + p) == 0;
+            is_free[j] = p < a.n_pages && is_free_page(p);
             n += is_free[j];
         }
         uint32_t rank = base + block_scan(n, warp_sums, total);
@@ -175,7 +181,7 @@ __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const Page
     for (uint32_t e_base = 0; e_base < entries; e_base += kStep) {
         const uint32_t e0 = e_base + tid * kPerThread;
         if (entries > kStep) {
-            reserve_entries(a, entries, e0, false, x, refs);
+            reserve_entries(a, entries, e0, false, x, refs, &named);
             reserve_copies(a, e0, x, refs, copies);
         }
         uint32_t n = 0, total;
@@ -200,7 +206,11 @@ __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const Page
     __syncthreads();
     for (int p = tid; p < a.n_pages; p += kTableThreads) {
         const int c = ld(a.claims + p);
-        if (c > 0) { const int r = ld(a.refs + p); a.refs[p] = c == r ? 1 : r - c; }
+        if (c > 0) {
+            const int r = ld(a.refs + p);
+            if (c > r) atomicOr(a.status, CSP_DEV_BAD_LEN);
+            else a.refs[p] = c == r ? 1 : r - c;
+        }
     }
     for (int b = tid; b < a.batch; b += kTableThreads) a.held[b] = max(ld(a.held + b), ld(a.need + b));
 }

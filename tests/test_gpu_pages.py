@@ -517,3 +517,42 @@ def test_a_captured_round_replays(csp):
         assert torch.equal(out, want)
         for a, b in zip(state, (x.s.held, x.s.refs, x.s.page_table[:2, :2])):
             assert torch.equal(a, b)
+
+
+# ---- a state that contradicts itself
+
+def test_reserve_leaves_a_page_that_is_named_more_often_than_counted(csp):
+    x = Pages(csp, 5, 1, 4, 128, 12)
+    x.reserve([200, 0, 0, 0, 100])
+    x.set_rows([[200], [0], [0], [0], [100]])
+    x.fork([0, 0], [1, 2])                              # page 1 is the last one of three sequences
+    x.s.refs[1] = 2
+    table, held, refs = (t.clone() for t in (x.s.page_table, x.s.held, x.s.refs))
+    csp.pages_reserve(x.s, x.moves, x.n, x.ws, n_new=torch.tensor([1, 1, 1, 1, 100], dtype=torch.int32, device="cuda"))
+    assert csp.device_status(x.ws) == csp.DEV_BAD_LEN and int(x.n) == 0
+    table[3, 0], table[4, 1] = 3, 4                     # the others get what they asked for
+    refs[3] = refs[4] = 1
+    held[3], held[4] = 1, 2
+    assert torch.equal(x.s.page_table, table) and torch.equal(x.s.refs, refs) and torch.equal(x.s.held, held)
+    # fewer ask than it is counted for: as far as this call sees nothing is wrong
+    x.s.n_rows[1:3] = 128
+    csp.pages_reserve(x.s, x.moves, x.n, x.ws)
+    assert csp.device_status(x.ws) == 0 and x.got_moves() == [(1, 5)]
+    assert x.s.refs.tolist() == [3, 1, 1, 1, 1, 1, 0, 0, 0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("batch,max_pages", [(3, 4), (3, 5000)])
+def test_reserve_does_not_give_away_a_page_that_is_named(csp, batch, max_pages):
+    """A page that a table entry names, but that is counted free; also with more entries than one step of the scan has."""
+    x = Pages(csp, batch, 1, max_pages, 128, 9)
+    x.reserve([300, 0, 0])
+    x.set_rows([[300], [0], [0]])
+    x.s.refs[2] = 0
+    csp.pages_reserve(x.s, x.moves, x.n, x.ws, n_new=torch.tensor([1, 100, 300], dtype=torch.int32, device="cuda"))
+    assert csp.device_status(x.ws) == csp.DEV_BAD_LEN and int(x.n) == 0
+    assert x.s.page_table[:, :4].tolist() == [[0, 1, 2, -1], [3, -1, -1, -1], [4, 5, 6, -1]]
+    assert x.s.refs.tolist() == [1, 1, 0, 1, 1, 1, 1, 0, 0] and x.s.held.tolist() == [3, 1, 3]
+    # it counts as taken when the pool runs short
+    csp.pages_reserve(x.s, x.moves, x.n, x.ws, n_new=torch.tensor([1, 0, 700], dtype=torch.int32, device="cuda"))
+    assert csp.device_status(x.ws) & csp.DEV_CAPACITY and int(x.n) == 0
+    assert x.s.held.tolist() == [3, 1, 3]
