@@ -457,7 +457,8 @@ csp_status csp_pages_free(const csp_page_state* s, void* workspace, size_t works
  * Moves the pages in use together: afterwards they are the pages [0, live) of the pool, and everything behind can be
  * given to someone else.  The pages in use at or behind `live` move to the free ones in front of it, both in ascending
  * order; tables and refs follow.  moves, max_moves and n_moves as for csp_pages_reserve (csp_pages_copy comes next);
- * with moves too small nothing is changed and CSP_DEV_CAPACITY is flagged.
+ * with moves too small nothing is changed and CSP_DEV_CAPACITY is flagged; so it is, with CSP_DEV_BAD_LEN, where a table
+ * entry names a page that is counted free.
  */
 csp_status csp_pages_compact(const csp_page_state* s, int32_t* moves, int32_t max_moves, int32_t* n_moves,
                              void* workspace, size_t workspace_bytes, void* cuda_stream);

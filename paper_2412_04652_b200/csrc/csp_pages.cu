@@ -219,9 +219,17 @@ __global__ void __launch_bounds__(kTableThreads) pages_compact_kernel(const Page
                                                                       int32_t* n_moves) {
     __shared__ uint32_t warp_sums[32];
     __shared__ uint32_t sum_live, sum_movers;
+    __shared__ int named;                                // some page is counted free, but a table entry names it
     const int tid = threadIdx.x, lane = tid & 31;
-    if (tid == 0) sum_live = sum_movers = 0;
+    if (tid == 0) { sum_live = sum_movers = 0; named = 0; }
     __syncthreads();
+    const uint32_t entries = uint32_t(a.batch) * uint32_t(a.max_pages);          // (31 bits)
+#pragma unroll 4
+    for (uint32_t e = tid; e < entries; e += kTableThreads) {
+        const uint32_t b = e / uint32_t(a.max_pages);
+        const int p = a.table[e];
+        if (int(e - b * uint32_t(a.max_pages)) < ld(a.held + b) && p >= 0 && p < a.n_pages && ld(a.refs + p) <= 0) named = 1;
+    }
     uint32_t n = 0;
     for (int p = tid; p < a.n_pages; p += kTableThreads) n += ld(a.refs + p) > 0;
     n = __reduce_add_sync(0xffffffffu, n);
@@ -235,10 +243,10 @@ __global__ void __launch_bounds__(kTableThreads) pages_compact_kernel(const Page
     __syncthreads();
     const bool fits = sum_movers <= uint32_t(max_moves);
     if (tid == 0) {
-        if (!fits) atomicOr(a.status, CSP_DEV_CAPACITY);
-        *n_moves = fits ? int(sum_movers) : 0;
+        if (!fits || named) atomicOr(a.status, (fits ? 0 : CSP_DEV_CAPACITY) | (named ? CSP_DEV_BAD_LEN : 0));
+        *n_moves = fits && !named ? int(sum_movers) : 0;
     }
-    if (!fits) return;
+    if (!fits || named) return;                          // a page that moved into a hole would be named by others
     // as many holes in front of `live` as pages in use behind it; both lists ascending
     uint32_t base = 0;
     for (int p0 = 0; p0 < live; p0 += kTableThreads * kPerThread) {
@@ -284,10 +292,9 @@ __global__ void __launch_bounds__(kTableThreads) pages_compact_kernel(const Page
         base += total;
     }
     __syncthreads();
-    const int64_t entries = int64_t(a.batch) * a.max_pages;
-    for (int64_t e = tid; e < entries; e += kTableThreads) {
-        const int b = int(e / a.max_pages), i = int(e % a.max_pages);
-        if (i >= ld(a.held + b)) continue;
+    for (uint32_t e = tid; e < entries; e += kTableThreads) {
+        const uint32_t b = e / uint32_t(a.max_pages);
+        if (int(e - b * uint32_t(a.max_pages)) >= ld(a.held + b)) continue;
         const int p = a.table[e];
         if (p >= 0 && p < live) continue;
         const int to = p >= live && p < a.n_pages ? ld(a.claims + p) : -1;

@@ -556,3 +556,21 @@ def test_reserve_does_not_give_away_a_page_that_is_named(csp, batch, max_pages):
     csp.pages_reserve(x.s, x.moves, x.n, x.ws, n_new=torch.tensor([1, 0, 700], dtype=torch.int32, device="cuda"))
     assert csp.device_status(x.ws) & csp.DEV_CAPACITY and int(x.n) == 0
     assert x.s.held.tolist() == [3, 1, 3]
+
+
+@pytest.mark.parametrize("page", [1, 6])
+def test_compact_moves_nothing_where_a_free_page_is_named(csp, page):
+    """In front of the last live page, where another page would move in, and behind it."""
+    x = Pages(csp, 3, 1, 3, 128, 10)
+    x.reserve([300, 300, 300])
+    x.set_rows([[300], [0], [300]])
+    x.free()                                            # pages 0, 1, 2 and 6, 7, 8 are in use
+    keep = [t.clone() for t in (x.s.page_table, x.s.held, x.s.refs)]
+    x.s.refs[page] = 0
+    keep[2][page] = 0
+    csp.pages_compact(x.s, x.moves, x.n, x.ws)
+    assert csp.device_status(x.ws) == csp.DEV_BAD_LEN and int(x.n) == 0
+    for a, b in zip(keep, (x.s.page_table, x.s.held, x.s.refs)):
+        assert torch.equal(a, b)
+    x.s.refs[page] = 1
+    assert x.compact() == [(6, 3), (7, 4), (8, 5)]
