@@ -133,8 +133,7 @@ __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const Page
         }
     }
     __syncthreads();
-    // a page that can be given out; one that is named all the same is left alone
-    auto is_free_page = [&](int p) { return ld(a.refs + p) == 0 && (!named || ld(a.last + p) != kNamed); };
+    const bool any_named = named != 0;                   // such pages are left alone
     if (!fail) {
         uint32_t want = 0, copy = 0, free_pages = 0;
         for (uint32_t e0 = tid * kPerThread; e0 < entries; e0 += kStep) {
@@ -144,7 +143,9 @@ __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const Page
             for (int j = 0; j < kPerThread; ++j) { copy += copies[j]; want += copies[j] || x[j].fresh; }
         }
 #pragma unroll 4
-        for (int p = tid; p < a.n_pages; p += kTableThreads) free_pages += is_free_page(p);
+        for (int p = tid; p < a.n_pages; p += kTableThreads) free_pages += ld(a.refs + p) == 0;
+        if (any_named)
+            for (int p = tid; p < a.n_pages; p += kTableThreads) free_pages -= ld(a.refs + p) == 0 && ld(a.last + p) == kNamed;
         want = __reduce_add_sync(0xffffffffu, want);
         copy = __reduce_add_sync(0xffffffffu, copy);
         free_pages = __reduce_add_sync(0xffffffffu, free_pages);
@@ -166,7 +167,8 @@ __global__ void __launch_bounds__(kTableThreads) pages_reserve_kernel(const Page
 #pragma unroll
         for (int j = 0; j < kPerThread; ++j) {
             const int p = p0 + tid * kPerThread + j;
-            is_free[j] = p < a.n_pages && is_free_page(p);
+            is_free[j] = p < a.n_pages && ld(a.refs + p) == 0;
+            if (any_named) is_free[j] = is_free[j] && ld(a.last + p) != kNamed;
             n += is_free[j];
         }
         uint32_t rank = base + block_scan(n, warp_sums, total);
