@@ -450,7 +450,8 @@ csp_status csp_pages_reserve(const csp_page_state* s, const int32_t* n_new_or_nu
 /* Pages behind the rows in use go back: sequence b keeps its first ceil(largest n_rows[b,:] / page_rows) pages, the table
  * entries behind them become -1 and refs count down (n_rows of zero gives a sequence up altogether).  A sequence with a
  * negative n_rows (a prune that did not fit) is flagged CSP_DEV_BAD_LEN and keeps all; so is one with more rows than
- * its pages hold. */
+ * its pages hold.  An entry given up that names no page of the pool, or one that is counted free, is flagged as well: it
+ * stays as it is, and nothing is counted. */
 csp_status csp_pages_free(const csp_page_state* s, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*

@@ -330,9 +330,9 @@ __global__ void pages_free_kernel(const PageArgs a) {
     int32_t* const row = a.table + int64_t(b) * a.max_pages;
     for (int i = int(need) + threadIdx.x; i < held; i += blockDim.x) {
         const int p = row[i];
-        row[i] = -1;
         if (p < 0 || p >= a.n_pages) { atomicOr(a.status, CSP_DEV_BAD_LEN); continue; }
-        if (atomicSub(a.refs + p, 1) <= 0) { atomicAdd(a.refs + p, 1); atomicOr(a.status, CSP_DEV_BAD_LEN); }
+        if (atomicSub(a.refs + p, 1) <= 0) { atomicAdd(a.refs + p, 1); atomicOr(a.status, CSP_DEV_BAD_LEN); continue; }
+        row[i] = -1;
     }
     if (threadIdx.x == 0) a.held[b] = int(need);
 }

@@ -574,3 +574,15 @@ def test_compact_moves_nothing_where_a_free_page_is_named(csp, page):
         assert torch.equal(a, b)
     x.s.refs[page] = 1
     assert x.compact() == [(6, 3), (7, 4), (8, 5)]
+
+
+def test_free_leaves_entries_that_contradict_the_counts(csp):
+    x = Pages(csp, 2, 1, 4, 128, 10)
+    x.reserve([500, 300])
+    x.set_rows([[0], [300]])
+    x.s.page_table[0, 1] = 77
+    x.s.refs[2] = 0
+    csp.pages_free(x.s, x.ws)
+    assert csp.device_status(x.ws) == csp.DEV_BAD_LEN
+    assert x.s.page_table.tolist() == [[-1, 77, 2, -1], [4, 5, 6, -1]]
+    assert x.s.held.tolist() == [0, 3] and x.s.refs.tolist() == [0, 1, 0, 0, 1, 1, 1, 0, 0, 0]
