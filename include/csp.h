@@ -423,8 +423,8 @@ size_t csp_pages_workspace_bytes(const csp_page_state* s);
  * Sequence dst[i] becomes a copy of sequence src[i] that shares its pages: table row, held and n_rows are copied, refs
  * counted up; no row is moved (csp_pages_reserve gives pages of its own to whoever writes).
  *   src, dst   [n] int32 device.  dst[i] must hold no pages, is named once, and is no src of the same call; a fork that
- *              breaks this, or names a sequence outside [0, batch), is flagged CSP_DEV_BAD_LEN and skipped (of two
- *              forks to one dst the first is done)
+ *              breaks this, that names a sequence outside [0, batch), or whose src names no page of the pool or one that
+ *              is counted free, is flagged CSP_DEV_BAD_LEN and skipped (of two forks to one dst the first is done)
  */
 csp_status csp_pages_fork(const csp_page_state* s, const int32_t* src, const int32_t* dst, int32_t n,
                           void* workspace, size_t workspace_bytes, void* cuda_stream);

@@ -341,30 +341,40 @@ __global__ void __launch_bounds__(kTableThreads) pages_fork_kernel(const PageArg
                                                                    int n) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int32_t* const owner = a.first;                      // [batch]: the first fork that names the sequence as its dst
-    for (int b = tid; b < a.batch; b += kTableThreads) owner[b] = INT_MAX;
+    for (int b = tid; b < a.batch; b += kTableThreads) { owner[b] = INT_MAX; a.need[b] = -1; }
     __syncthreads();
     for (int i = tid; i < n; i += kTableThreads) {
         const int d = dst[i];
         if (d >= 0 && d < a.batch) atomicMin(owner + d, i);
     }
     __syncthreads();
-    // one warp per fork; a dst is written by its owner only, and no src is a dst: no order matters
+    // One warp per fork; a dst is written by its owner only, and no src is a dst: no order matters.  First all of them are
+    // looked at, while the counts are those of the call's start (4.1 us for 8 forks instead of 3.1; need[d]: the fork that is done).
     for (int i = warp; i < n; i += kTableThreads / 32) {
         const int s = src[i], d = dst[i];
         bool ok = s >= 0 && s < a.batch && d >= 0 && d < a.batch;
         ok = ok && ld(owner + d) == i && ld(owner + s) == INT_MAX && ld(a.held + d) == 0;
         const int held = ok ? ld(a.held + s) : 0;
         ok = ok && held >= 0 && held <= a.max_pages;
-        __syncwarp();                                    // all lanes have looked at held[d] before lane 0 writes it
-        if (!ok) {
-            if (lane == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
-            continue;
+        for (int j = lane; ok && j < held; j += 32) {
+            const int p = a.table[int64_t(s) * a.max_pages + j];
+            ok = p >= 0 && p < a.n_pages && ld(a.refs + p) > 0;
         }
+        ok = __all_sync(0xffffffffu, ok);
+        if (lane == 0) {
+            if (ok) a.need[d] = i;
+            else atomicOr(a.status, CSP_DEV_BAD_LEN);
+        }
+    }
+    __syncthreads();
+    for (int i = warp; i < n; i += kTableThreads / 32) {
+        const int s = src[i], d = dst[i];
+        if (d < 0 || d >= a.batch || ld(a.need + d) != i) continue;
+        const int held = ld(a.held + s);
         for (int j = lane; j < held; j += 32) {
             const int p = a.table[int64_t(s) * a.max_pages + j];
             a.table[int64_t(d) * a.max_pages + j] = p;
-            if (p >= 0 && p < a.n_pages) atomicAdd(a.refs + p, 1);
-            else atomicOr(a.status, CSP_DEV_BAD_LEN);
+            atomicAdd(a.refs + p, 1);
         }
         for (int h = lane; h < a.n_heads; h += 32)
             a.n_rows[int64_t(d) * a.n_heads + h] = a.n_rows[int64_t(s) * a.n_heads + h];

@@ -586,3 +586,19 @@ def test_free_leaves_entries_that_contradict_the_counts(csp):
     assert csp.device_status(x.ws) == csp.DEV_BAD_LEN
     assert x.s.page_table.tolist() == [[-1, 77, 2, -1], [4, 5, 6, -1]]
     assert x.s.held.tolist() == [0, 3] and x.s.refs.tolist() == [0, 1, 0, 0, 1, 1, 1, 0, 0, 0]
+
+
+def test_forks_of_sequences_that_contradict_the_counts_are_skipped(csp):
+    x = Pages(csp, 7, 1, 50, 128, 120)
+    x.reserve([5000, 5000, 300, 0, 0, 0, 0])
+    x.set_rows([[5000], [5000], [300], [0], [0], [0], [0]])
+    x.s.page_table[0, 39] = 200
+    x.s.refs[int(x.s.page_table[1, 33])] = 0
+    table, held, refs, rows = (t.clone() for t in (x.s.page_table, x.s.held, x.s.refs, x.s.n_rows))
+    t = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    csp.pages_fork(x.s, t(0, 1, 2, 1), t(3, 4, 5, 6), x.ws)
+    assert csp.device_status(x.ws) == csp.DEV_BAD_LEN
+    table[5], held[5], rows[5] = table[2], held[2], rows[2]
+    refs[table[2, :3].long()] = 2
+    for a, b in zip((table, held, refs, rows), (x.s.page_table, x.s.held, x.s.refs, x.s.n_rows)):
+        assert torch.equal(a, b)
