@@ -360,6 +360,8 @@ size_t csp_chunk_workspace_bytes(const csp_params* p, int32_t max_new);
  *   lse_or_null [B, H_q, max_new] fp32 dense: without n, so that the last W tokens' values are what csp_score and
  *           csp_prune_layer take as lse_or_null (when mods is NULL)
  * A token that sees nothing (or whose row would be negative: flagged) gets a zero vector and a lse of -infinity.
+ * Without tokens or sequences (max_new or batch 0) there is nothing to do, and the tensors may have no address; the same
+ * holds for csp_append_paged (whose counts are copied all the same) and for page calls over 0 sequences.
  * bf16 caches with head_dim 64 or 128.  Sums and the softmax are held in fp32; weights are rounded to bf16 once before
  * they meet V, the result once more.  Nothing is allocated; the caller owns the workspace.
  */

@@ -573,8 +573,8 @@ bool rows_apart(const csp_params& p, const csp_tensor& t, int batch, int heads, 
            (batch <= 1 || t.stride_b >= p.head_dim);
 }
 
-bool pages_ok(const csp_pages* pg, int64_t rows) {
-    return pg && pg->page_table && pg->page_rows > 0 && pg->page_rows % 128 == 0 && pg->max_pages > 0 && pg->n_pages > 0 &&
+bool pages_ok(const csp_pages* pg, int64_t rows, int batch) {
+    return pg && (pg->page_table || batch == 0) && pg->page_rows > 0 && pg->page_rows % 128 == 0 && pg->max_pages > 0 && pg->n_pages > 0 &&
            int64_t(pg->max_pages) * pg->page_rows >= rows;
 }
 
@@ -583,14 +583,16 @@ csp_status chunk_attn(const csp_params* p, int32_t max_new, const csp_tensor& q,
                       const csp_tensor& out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     csp_status st = check_params(p);
     if (st != CSP_OK) return st;
-    if (max_new < 0 || !q.ptr || !k.ptr || !v.ptr || !n_rows || !out.ptr) return CSP_ERR_INVALID_ARG;
+    const bool any = p->batch > 0 && max_new > 0;        // (empty tensors have no address)
+    if (max_new < 0 || (any && (!q.ptr || !k.ptr || !v.ptr || !n_rows || !out.ptr))) return CSP_ERR_INVALID_ARG;
     if (mods && !(mods->softcap == 0.f || (mods->softcap >= 1e-6f && mods->softcap <= 1000.f))) return CSP_ERR_INVALID_ARG;
     const size_t need = chunk_workspace_bytes(*p, max_new);
     if (need == 0) return CSP_ERR_UNSUPPORTED;
-    if (!tensor_ok(*p, q) || !tensor_ok(*p, k) || !tensor_ok(*p, v) || !tensor_ok(*p, out)) return CSP_ERR_UNSUPPORTED;
-    if (!rows_apart(*p, out, p->batch, p->n_q_heads, max_new)) return CSP_ERR_UNSUPPORTED;
+    if (any && (!tensor_ok(*p, q) || !tensor_ok(*p, k) || !tensor_ok(*p, v) || !tensor_ok(*p, out))) return CSP_ERR_UNSUPPORTED;
+    if (any && !rows_apart(*p, out, p->batch, p->n_q_heads, max_new)) return CSP_ERR_UNSUPPORTED;
     if (!status_area_ok(workspace, workspace_bytes, need)) return CSP_ERR_WORKSPACE;
     if ((st = check_arch()) != CSP_OK) return st;
+    if (!any) return CSP_OK;
     ChunkArgs a;
     a.n_rows = n_rows; a.n_new = n_new;
     a.out = static_cast<uint16_t*>(out.ptr); a.o_sb = out.stride_b; a.o_sh = out.stride_h; a.o_st = out.stride_t;
@@ -612,7 +614,6 @@ csp_status chunk_attn(const csp_params* p, int32_t max_new, const csp_tensor& q,
     a.max_pages = pages ? pages->max_pages : 0;
     a.page_rows = pages ? pages->page_rows : 1;
     a.n_pages = pages ? pages->n_pages : 0;
-    if (p->batch == 0 || max_new == 0) return CSP_OK;
     return launch_chunk_attn(*p, a, q, k, v, pages, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -634,7 +635,7 @@ csp_status csp_chunk_attn_paged(const csp_params* p, int32_t max_new, csp_tensor
                                 const csp_pages* pages, const int32_t* n_rows, const int32_t* n_new_or_null,
                                 const csp_score_mods* mods_or_null, csp_tensor out, float* lse_or_null, void* workspace,
                                 size_t workspace_bytes, void* cuda_stream) {
-    if (!p || !pages_ok(pages, p->out_capacity)) return CSP_ERR_INVALID_ARG;
+    if (!p || !pages_ok(pages, p->out_capacity, p->batch)) return CSP_ERR_INVALID_ARG;
     return chunk_attn(p, max_new, q, k_pool, v_pool, pages, n_rows, n_new_or_null, mods_or_null, out, lse_or_null,
                       workspace, workspace_bytes, cuda_stream);
 }
@@ -648,10 +649,11 @@ csp_status csp_append_paged(const csp_params* p, int32_t max_new, csp_tensor k_n
                             void* cuda_stream) {
     csp_status st = check_params(p);
     if (st != CSP_OK) return st;
-    if (max_new < 0 || !k_new.ptr || !v_new.ptr || !k_pool.ptr || !v_pool.ptr || !n_rows || !n_rows_out)
+    const bool any = p->batch > 0 && max_new > 0;        // (empty tensors have no address)
+    if (max_new < 0 || (any && (!k_new.ptr || !v_new.ptr)) || !k_pool.ptr || !v_pool.ptr || (p->batch > 0 && (!n_rows || !n_rows_out)))
         return CSP_ERR_INVALID_ARG;
-    if (!pages_ok(pages, p->out_capacity)) return CSP_ERR_INVALID_ARG;
-    if (!tensor_ok(*p, k_new) || !tensor_ok(*p, v_new) || !tensor_ok(*p, k_pool) || !tensor_ok(*p, v_pool))
+    if (!pages_ok(pages, p->out_capacity, p->batch)) return CSP_ERR_INVALID_ARG;
+    if ((any && (!tensor_ok(*p, k_new) || !tensor_ok(*p, v_new))) || !tensor_ok(*p, k_pool) || !tensor_ok(*p, v_pool))
         return CSP_ERR_UNSUPPORTED;
     if (!rows_apart(*p, k_pool, pages->n_pages, p->n_kv_heads, pages->page_rows) ||
         !rows_apart(*p, v_pool, pages->n_pages, p->n_kv_heads, pages->page_rows))
@@ -688,7 +690,7 @@ csp_status check_page_state(const csp_page_state* s) {
 csp_status check_page_call(const csp_page_state* s, const void* ws, size_t bytes) {
     csp_status st = check_page_state(s);
     if (st != CSP_OK) return st;
-    if (!s->page_table || !s->held || !s->refs || !s->n_rows) return CSP_ERR_INVALID_ARG;
+    if (!s->refs || (s->batch > 0 && (!s->page_table || !s->held || !s->n_rows))) return CSP_ERR_INVALID_ARG;
     if (!status_area_ok(ws, bytes, pages_workspace_bytes(*s))) return CSP_ERR_WORKSPACE;
     return CSP_OK;
 }

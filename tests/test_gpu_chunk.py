@@ -525,3 +525,18 @@ def test_one_workspace_for_chunks_of_all_lengths(csp):
             assert csp.device_status(ws) == 0
             if T <= 17:
                 assert_chunk_close(out, None, reference(q, k, v, rows, new), new, f"T={T}")
+
+
+@pytest.mark.parametrize("B,T", [(2, 0), (0, 3), (0, 0)])
+def test_nothing_to_do(csp, B, T):
+    """Chunks without tokens and batches without sequences: empty tensors, which have no address."""
+    p = csp.Params(B, 4, 2, 64, 1, 0, 256, 256)
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    q, k, pool = torch.zeros(B, 4, T, 64, **bf), torch.zeros(B, 2, 256, 64, **bf), torch.zeros(5, 2, 128, 64, **bf)
+    rows, new = torch.full((B, 2), 7, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    table = torch.zeros(B, 2, dtype=torch.int32, device="cuda")
+    out, lse, ws = torch.zeros_like(q), torch.zeros(B, 4, T, device="cuda"), csp.new_chunk_workspace(p, T)
+    csp.chunk_attn(p, q, k, k, rows, out, ws, lse=lse)
+    csp.chunk_attn(p, q, k, k, rows, out, ws, n_new=new, mods=csp.ScoreMods(prefix=new))
+    csp.chunk_attn_paged(p, q, pool, pool, table, rows, out, ws, n_new=new)
+    assert csp.device_status(ws) == 0

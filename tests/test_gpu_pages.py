@@ -602,3 +602,28 @@ def test_forks_of_sequences_that_contradict_the_counts_are_skipped(csp):
     refs[table[2, :3].long()] = 2
     for a, b in zip((table, held, refs, rows), (x.s.page_table, x.s.held, x.s.refs, x.s.n_rows)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("B,T", [(2, 0), (0, 3), (0, 0)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_nothing_to_append(csp, B, T, in_place):
+    p = csp.Params(B, 2, 2, 64, 1, 0, 256, 256)
+    pool = _pool(5, 2, 128, 64, torch.bfloat16)
+    before, rows = pool.clone(), torch.arange(2 * B, dtype=torch.int32, device="cuda").reshape(B, 2)
+    after = rows if in_place else torch.full_like(rows, -9)
+    new, ws = torch.zeros(B, 2, T, 64, dtype=torch.bfloat16, device="cuda"), csp.new_append_workspace(p)
+    csp.append_paged(p, new, new, pool, pool, torch.zeros(B, 2, dtype=torch.int32, device="cuda"), rows, after, ws)
+    assert csp.device_status(ws) == 0 and torch.equal(pool, before)
+    assert after.tolist() == [[2 * b, 2 * b + 1] for b in range(B)]
+
+
+def test_a_pool_without_sequences(csp):
+    x = Pages(csp, 0, 2, 3, 128, 6)
+    x.ws[:256] = 0
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    csp.pages_fork(x.s, none, none, x.ws)
+    csp.pages_reserve(x.s, x.moves, x.n, x.ws, n_new=none)
+    assert int(x.n) == 0
+    csp.pages_free(x.s, x.ws)
+    csp.pages_compact(x.s, x.moves, x.n, x.ws)
+    assert int(x.n) == 0 and csp.device_status(x.ws) == 0

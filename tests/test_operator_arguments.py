@@ -202,3 +202,25 @@ def test_shapes_that_the_attention_refuses_have_no_workspace(csp, kw, max_new):
 
 def test_the_longest_chunk_has_a_workspace(csp):
     assert csp.chunk_workspace_bytes(_params(csp, n_q_heads=4), 1 << 24) >= csp.chunk_workspace_bytes(_params(csp, n_q_heads=4), 1 << 23) > 0
+
+
+def test_empty_tensors_are_no_missing_ones(csp):
+    """A chunk without tokens and a batch without sequences have no addresses to pass; what is needed still is."""
+    null = csp.CTensor(None, 1, 1, 1)
+    fine = (csp.OK,) if torch.cuda.is_available() else (csp.ERR_CUDA, csp.ERR_ARCH)
+    assert _chunk(csp, _params(csp), max_new=0, q=null, out=null) in fine
+    assert _chunk(csp, _params(csp, batch=0), q=null, k=null, v=null, out=null, rows=None) in fine
+    assert _chunk(csp, _params(csp), max_new=0, q=null, out=null, ws=None) == csp.ERR_WORKSPACE
+    assert _chunk(csp, _params(csp), q=null) == csp.ERR_INVALID_ARG
+    lib, p = csp.lib(), _params(csp)
+    cp, t, pg = p.c(), _tensor(csp), csp.CPages(256, 4, 128, 9)
+    append = lambda cp, new, max_new, pool, rows: lib.csp_append_paged(  # noqa: E731
+        C.byref(cp), max_new, new, new, None, pool, pool, C.byref(pg), rows, rows, 256, BIG, None)
+    assert append(cp, null, 0, null, 256) == csp.ERR_INVALID_ARG
+    assert append(cp, null, 0, t, None) == csp.ERR_INVALID_ARG
+    assert append(cp, null, 1, t, 256) == csp.ERR_INVALID_ARG
+    assert append(_params(csp, batch=0).c(), null, 1, t, None) in fine
+    s = _state(csp, batch=0, page_table=None, held=None, n_rows=None)
+    assert lib.csp_pages_free(C.byref(s), 256, BIG, None) in fine
+    s = _state(csp, batch=0, page_table=None, held=None, n_rows=None, refs=None)
+    assert lib.csp_pages_free(C.byref(s), 256, BIG, None) == csp.ERR_INVALID_ARG
