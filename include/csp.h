@@ -323,7 +323,9 @@ csp_status csp_decode_step(const csp_params* p, csp_tensor q, csp_tensor k, csp_
  *   slopes     [H_q] fp32 or NULL: slopes[hq] * |position of the query - position of the key| is subtracted, after the cap
  *   positions  int32, >= 0, of the cached rows: element (b,h,t) at positions[b*pos_stride_b + h*pos_stride_h + t]; NULL: row
  *              t is at position t.  A pruned cache keeps the positions its rows had (the keep_idx of the prune), per
- *              head; a head stride of 0 shares one row of positions.  Read only when slopes are given
+ *              head; a head stride of 0 shares one row of positions.  Read only when slopes are given.  The cached rows may
+ *              lie anywhere, the tokens of a chunk up to 2^23 positions apart: distances keep 23 bits then.  Where they
+ *              lie farther apart and the distances are rounded, CSP_DEV_BAD_LEN is flagged
  *   documents  int32 document of every cached row, addressed like positions, or NULL: a query sees rows of its own only
  *   prefix     int32 element (b,h) at prefix[b*prefix_stride_b + h*prefix_stride_h], or NULL: the first that many rows of
  *              the unit are seen by every query of the chunk, also by those in front of them (an image in the prompt that

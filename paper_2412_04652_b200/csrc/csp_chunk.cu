@@ -620,6 +620,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             __syncwarp();
             if (lane == 0) mbar_arrive(ent_empty + 8 * e);
             ++n_entry;
+            if (kBias && fabsf(q_pos) > kFarToken) atomicOr(a.status, CSP_DEV_BAD_LEN);
             if (started) warp_wait(pv_done + 8 * g, (n_mine - 1u) & 1u, abort_flag);
             tc_fence_after();
             float l_all = l_run + other_half(l_run);

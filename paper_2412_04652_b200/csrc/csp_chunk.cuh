@@ -30,6 +30,12 @@ namespace dev {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kSeesAll = 1 << 30;
 
+// Positions are held in fp32 relative to the last token's of the item.  A token's own is exact up to 2^24 from there; up to half
+// of that, a key whose position is rounded (by 2^-24 of its distance from the last token) is at least half as far from the token,
+// so that every distance keeps 23 bits.  A token farther off is flagged at the item's end.  (Integer distances would cost a conversion
+// per logit.)
+constexpr float kFarToken = 8388608.f;
+
 // What the rows of a pair look at.
 struct PairRange {
     int rows, n_new, tok0, count;                        // rows of the unit, tokens of the sequence, first token, tokens here

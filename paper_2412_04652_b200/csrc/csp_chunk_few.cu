@@ -480,6 +480,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
                 for (int t = 0; t < NT; ++t)
                     *reinterpret_cast<float2*>(mine + t * 8 + 2 * qd) = make_float2(acc[t][2 * rr], acc[t][2 * rr + 1]);
                 if (qd == 0) *reinterpret_cast<float2*>(mine + D) = make_float2(m_run[rr], l_run[rr]);
+                if (md.slopes && w >= 0 && fabsf(q_pos[rr]) > kFarToken) atomicOr(a.status, CSP_DEV_BAD_LEN);
             }
             if (warp == 0 && lane < kItemWords) finish[lane] = in[lane];
             ++n_done;

@@ -540,3 +540,28 @@ def test_nothing_to_do(csp, B, T):
     csp.chunk_attn(p, q, k, k, rows, out, ws, n_new=new, mods=csp.ScoreMods(prefix=new))
     csp.chunk_attn_paged(p, q, pool, pool, table, rows, out, ws, n_new=new)
     assert csp.device_status(ws) == 0
+
+
+# ---- positions far apart
+
+@pytest.mark.parametrize("T,page_rows", [(3, 0), (3, 128), (200, 0), (200, 128)])
+@pytest.mark.parametrize("gap", [2 ** 23 - 400, 2 ** 24, 2 ** 30])
+def test_tokens_far_apart(csp, T, page_rows, gap):
+    """A chunk whose first tokens lie `gap` positions in front of the others: exact distances up to 2^23, flagged beyond."""
+    cap, Hq, Hkv = 300, 4, 2
+    case = _case(T, 1, Hq, Hkv, 64, cap, [300, 299], [T])
+    pos = torch.arange(cap, dtype=torch.int32)[None, :].repeat(1, 1)
+    pos[:, cap - T // 2 - 2:] += gap
+    fine = gap < 2 ** 23
+    _run(csp, case, page_rows, status=0 if fine else csp.DEV_BAD_LEN, check=fine, slopes=_slopes(Hq), positions=pos)
+
+
+@pytest.mark.parametrize("T", [1, 3, 200])
+def test_cached_rows_far_from_the_tokens(csp, T):
+    """Rows of a cache up to 2^30 positions in front of the chunk, and slopes so small that they still have a weight."""
+    cap, Hq, Hkv = 400, 4, 2
+    case = _case(T, 1, Hq, Hkv, 64, cap, [400, 399], [T])
+    pos = torch.arange(cap, dtype=torch.int32)[None, :].repeat(1, 1)
+    pos[:, 60:] += 2 ** 25 + 1
+    pos[:, 130:] += 2 ** 30 - 3
+    _run(csp, case, 0, slopes=torch.tensor([2.0 ** -30, 2.0 ** -29, 0.5, 0.01]), positions=pos)
