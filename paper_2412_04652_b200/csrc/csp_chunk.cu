@@ -146,7 +146,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             if (ok && lane == 0) mbar_arrive(ent_full + 8 * e);
             ++n_entry;
         };
-        if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, -1, 0, 0};
+        if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, 0};
         // Items drawn whole, one after the other, are the last tokens of every unit first: these see the most keys, and an item
         // drawn near the end is a short one.
         const bool drawn = kDoc && share.drawn;
@@ -179,7 +179,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             // which partial result the item goes to: none (the item is whole), the one that goes on, the one that begins
             const int part = tile0 > 0 ? 2 * int(blockIdx.x) : tile1 < x.tiles ? 2 * int(blockIdx.x) + 1 : -1;
             if (lane == 0 && part >= 0) {
-                if (tile0 > 0) { parts[blockIdx.x].more = item; parts[blockIdx.x].last = tile1 == x.tiles; }
+                if (tile0 > 0) parts[blockIdx.x].last = tile1 == x.tiles;
                 else parts[blockIdx.x].first = item;
             }
             const bool big = x.count > pl.tok_tile;      // more than one row tile

@@ -18,8 +18,9 @@ struct ChunkPlan {                                       // sizes that host and 
     int snap;                                            // tiles by which a share may differ from an equal one to avoid a cut
 };
 
-// What a block says about the items it was given only part of (see Share).
-struct ChunkParts { int32_t first, more, last, unused; };
+// What a block says about the items it was given only part of (see Share): the one that begins with it (-1: none), and whether
+// the one it goes on with ends with it.
+struct ChunkParts { int32_t first, last; };
 
 csp_status launch_chunk_few(const csp_params& p, const ChunkArgs& a, const ChunkPlan& pl, const csp_tensor& q,
                             const CUtensorMap& tk, const CUtensorMap& tv, ChunkParts* parts, float* partial, float2* ml,

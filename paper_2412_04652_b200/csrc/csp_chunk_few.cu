@@ -109,7 +109,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
             __syncwarp();
             if (ok && lane == 0) mbar_arrive(full_bar + 8 * s);
         };
-        if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, -1, 0, 0};
+        if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, 0};
         const uint32_t tiles_per_page = uint32_t(a.page_rows) / uint32_t(kFewTile);      // (dense: not used)
         auto page_of = [&](int b, int tile) {            // the page of a tile that lies inside the cache
             return a.page_table[int64_t(b) * a.max_pages + uint32_t(tile) / tiles_per_page];
@@ -141,7 +141,7 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
             const int tile0 = u == share.item0 ? share.tile0 : 0, tile1 = u == share.item1 ? share.tile1 : x.tiles;
             if (x.count <= 0 || (u == share.item1 && tile1 == 0)) { look_up(u + 1); continue; }
             if (lane == 0) {
-                if (tile0 > 0) { parts[blockIdx.x].more = u; parts[blockIdx.x].last = tile1 == x.tiles; }
+                if (tile0 > 0) parts[blockIdx.x].last = tile1 == x.tiles;
                 else if (tile1 < x.tiles) parts[blockIdx.x].first = u;
             }
             const int32_t* const docs = md.documents ? md.documents + int64_t(b) * md.doc_sb + int64_t(h) * md.doc_sh : nullptr;
