@@ -21,9 +21,18 @@
 // same rows and alternate over the key tiles (their results are joined when the item ends): either way one group's
 // softmax runs while the tensor cores work for the other.
 //
-// Bound by the exponentials and the matrix products, which need the same 1024 clocks per 128 x 128 tile and are both busy 54 % of
-// the time.  Measured at d = 128: 513 - 1024 tokens over 8 K - 32 K positions, 4 sequences, 28 / 4 heads (904 GFLOP): 840 us, 1.08
-// PFLOP/s; 512 tokens over 4 K, 32 heads (32 GFLOP): 47 us, of which 10 are the start and end of items, and 10 us for joining.
+// Bound by the exponentials and the matrix products, which need the same 1024 clocks per 128 x 128 tile and are both busy 55 % of
+// the clocks in which an SM works.  Measured at d = 128: 513 - 1024 tokens over 8 K - 32 K positions, 4 sequences, 28 / 4 heads (904
+// GFLOP): 835 - 870 us (1.04 - 1.08 PFLOP/s) at first, 945 - 980 (0.92 - 0.96) back to back, when the power limit lowers the
+// clocks; 512 tokens over 4 K, 32 heads (32 GFLOP): 48 us, of which 10 are the start and end of items, and 9 us for joining.
+//
+// Precision.  Sums, maxima and O are fp32.  The weights are rounded to bf16 (by 2^-8 of a weight at most, independently of
+// each other): the error of the result against 64 bits is 0.0023 of it instead of the 0.0017 that its own rounding
+// to bf16 leaves.  A second product with the weights' remainders brings it back to 0.0017, but takes half as many matrix
+// operations again: 66 us instead of 57 for 512 tokens over 4 K, 81 instead of 75 with documents, 1150 - 1200 instead of 870 - 950
+// for the largest; for long prompts the faster one was chosen (few rows have both products: HBM is their bound).  The cap
+// is c - 2 c / (1 + e^{2 o / c}): one exponential and one reciprocal on the pipe that is the bound, exact to c 2^-20; the tanh
+// instruction, the only shorter form, has 11 bits.
 #include <limits.h>
 
 #include "csp_chunk.cuh"
@@ -712,7 +721,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
 // C chunks of four columns of a row; the parts are laid out [column / 4][row][4], so that eight rows are one line.  Bound by
 // the latency of its few loads and of its instructions (which are cold), so the code is kept short.  For few rows, which are
 // cut often, eight rows and eight parts in flight (one token over 8 K - 32 K rows, ten parts: 5.9 us; with 32 rows and
-// four parts 14); elsewhere 16 rows and two parts (an item has two or three, of 256 rows; 512 tokens over 4 K: 9.7 us, with eight rows
+// four parts 14); elsewhere 16 rows and two parts (an item has two or three, of 256 rows; 512 tokens over 4 K: 9.4 us, with eight rows
 // and parts 14; 1 K tokens over 8 K - 32 K: 15.5 us, with 32 rows or four parts 19).
 // Launched ahead of the main kernel's end (programmatic dependence) it gained nothing.
 template <int D, int kRows>
@@ -791,7 +800,10 @@ void join_parts(const ChunkArgs& a, const ChunkPlan& pl, const ChunkParts* parts
 
 // Up to sixteen query rows per KV head (single tokens above all) go to the kernel that streams the cache through
 // warp-level products: its rows are spread over all threads, where a tcgen05 row tile would leave most of them idle.
-// Measured for one token, 32 sequences x 32 heads, 410 - 1640 rows each, d = 128: 112 us there, 173 us in row tiles.
+// Measured at d = 128, here and in row tiles: 32 sequences x 32 heads, 410 - 1640 rows each, 1 row 103 and 133 us, 8 rows 110 and
+// 135, 12 rows 133 and 135, 16 rows 144 and 135; 4 x 28 / 4 heads, 8 K - 32 K, 7 rows 42.5 and 52.6, 14 rows 47.9 and 52.5; 8 x 32 / 4
+// heads, 1 K - 6 K, 8 rows 26.7 and 30.8, 16 rows 30.8 and 30.8; one short sequence, 2 rows 10.3 and 17, 16 rows 18 and 16.4.  Up
+// to eight rows it is faster everywhere; from there to sixteen the two are about even, and here only the result is rounded.
 constexpr int kFewRows = 16;
 
 ChunkPlan chunk_plan(const csp_params& p, int max_new) {
@@ -807,8 +819,8 @@ ChunkPlan chunk_plan(const csp_params& p, int max_new) {
     pl.min_tiles = 2;
     pl.item_cost = 2;
     // A cut costs a row pair about four tiles (256 rows of partial results and their joining), few rows next to nothing,
-    // but there an uneven share costs nothing either: HBM is the bound, whoever reads.  1 K tokens over 8 K - 32 K: 905 us without
-    // this limit, 835 with 4, 858 with 2, 878 with 0; one token, serving batch: 113 us without, 114 - 116 with 8 to 1.
+    // but there an uneven share costs nothing either: HBM is the bound, whoever reads.  1 K tokens over 8 K - 32 K: 923 us without
+    // this limit, 850 - 870 with 4, 862 with 2, 840 - 874 with 0; one token, serving batch: 103 us without, 104 with 8, 100 with 1.
     pl.snap = few ? 0x3fffffff : 4;
     const int64_t items = int64_t(p.batch) * p.n_kv_heads * pl.n_pairs;
     const int64_t weight = (int64_t(p.out_capacity) + pl.key_tile - 1) / pl.key_tile + pl.item_cost;      // of an item, at most
@@ -879,7 +891,7 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
     ChunkPlan pl = chunk_plan(p, a.max_new);
     // Documents make the weight of an item unknown (tiles without any of its documents are skipped): where every block has
     // several items anyway, and none is longer than a share, they are drawn whole.  2 x 32 heads, 2 K tokens of four documents:
-    // 101 us shared out, 79 drawn with the longest first; in ascending order it was a tenth slower.
+    // 98.5 us shared out, 72.5 drawn with the longest first; in ascending order it was a tenth slower.
     pl.drawn = a.mods.documents && pl.row_slots > kFewRows && pl.n_items >= 2 * pl.grid;
     const PartialLayout lay = partial_layout(p, pl);
     ChunkParts* const parts = reinterpret_cast<ChunkParts*>(static_cast<char*>(ws) + lay.parts);

@@ -16,9 +16,10 @@
 //   warp 9      joins the eight results of an item in a fixed order: a whole unit is finished here, a cut one leaves a
 //               partial result.  The query rows and what else an item needs come with its first stage, so that nobody
 //               waits for memory between items
-// Measured for one token, d = 128: 32 sequences x 32 heads, 410 - 1640 rows (530 MB) 112 us, 5.2 TB/s over all and 6.5 while all
-// blocks stream (they start after 7 us and end up to 15 % apart); 4 sequences of 8 K - 32 K rows, 28 / 4 heads with a bias (169 MB)
-// 41 us and 6 us for joining; one short sequence 8 us.
+// Measured for one token, d = 128: 32 sequences x 32 heads, 410 - 1640 rows (530 MB) 102 us, 5.2 TB/s over all and 5.6 behind the
+// first 7 us, when the first tiles arrive (the last block ends 14 % later than the average); 4 sequences of 8 K - 32 K rows,
+// 28 / 4 heads with a bias (169 MB) 41.5 us, 4.1 TB/s over all and 4.9 behind the start, and 6 us for joining; one short
+// sequence 8 us.
 #include <limits.h>
 
 #include "csp_chunk.cuh"
