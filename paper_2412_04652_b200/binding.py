@@ -71,6 +71,7 @@ class CParams(C.Structure):
 
 @dataclass
 class Params:
+    __slots__ = ("_made", "__dict__", "__weakref__")    # (_made is no attribute that vars() shows or a copy of it hands on)
     batch: int
     n_q_heads: int
     n_kv_heads: int
@@ -86,13 +87,19 @@ class Params:
     select_mode: int = SELECT_SEGMENTED
     head_reduce: int = HEADS_PER_KV
 
+    def _fields(self):
+        return (self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.window,
+                self.recent, self.max_len, self.out_capacity, self.dtype, self.n, self.scale,
+                self.combine, self.select_mode, self.head_reduce)
+
     def c(self) -> CParams:
-        now = (self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.window,
-               self.recent, self.max_len, self.out_capacity, self.dtype, self.n, self.scale,
-               self.combine, self.select_mode, self.head_reduce)
-        made = self.__dict__.get("_made")               # the struct of the last call, while nothing has changed
+        return CParams(*self._fields())
+
+    def _c(self) -> CParams:
+        """What the calls below pass, which nobody changes: the struct of the last call, while nothing has changed."""
+        now, made = self._fields(), getattr(self, "_made", None)
         if made is None or made[0] != now:
-            made = self.__dict__["_made"] = (now, CParams(*now))
+            made = self._made = (now, CParams(*now))
         return made[1]
 
 
@@ -284,7 +291,7 @@ def _mod_strides(modality: torch.Tensor):
 
 
 def workspace_bytes(p: Params) -> int:
-    cp = p.c()
+    cp = p._c()
     return int(lib().csp_workspace_bytes(C.byref(cp)))
 
 
@@ -301,7 +308,7 @@ def workspace_reset(ws: torch.Tensor):
 
 
 def decode_workspace_bytes(p: Params) -> int:
-    cp = p.c()
+    cp = p._c()
     return int(lib().csp_decode_workspace_bytes(C.byref(cp)))
 
 
@@ -315,7 +322,7 @@ def new_decode_workspace(p: Params, device="cuda") -> torch.Tensor:
 
 def decode_attn(p: Params, q, k, v, n_rows, out, ws):
     """q [B, Hq, d]; k, v [B, Hkv, out_capacity, d]; n_rows int32 [B, Hkv]; out fp32 [B, Hq, d] (dense)."""
-    cp = p.c()
+    cp = p._c()
     assert q.dim() == 3 and q.stride(2) == 1 and out.is_contiguous() and out.dtype == torch.float32
     qt = CTensor(q.data_ptr(), q.stride(0), q.stride(1), q.shape[2])
     _check(lib().csp_decode_attn(C.byref(cp), qt, tensor4(k), tensor4(v), _ptr(n_rows), _ptr(out), _ptr(ws),
@@ -324,7 +331,7 @@ def decode_attn(p: Params, q, k, v, n_rows, out, ws):
 
 def new_decode_step_workspace(p: Params, device="cuda") -> torch.Tensor:
     """Allocates (with torch) and zeroes a workspace for csp_decode_step."""
-    cp = p.c()
+    cp = p._c()
     n = int(lib().csp_decode_step_workspace_bytes(C.byref(cp)))
     if n == 0:
         raise CspError(ERR_UNSUPPORTED, "csp_decode_step_workspace_bytes")
@@ -334,7 +341,7 @@ def new_decode_step_workspace(p: Params, device="cuda") -> torch.Tensor:
 def decode_step(p: Params, q, k, v, n_rows, modality, query_label, first_step, out, acc_self, acc_cross, ws):
     """csp_decode_attn plus the running intra / inter sums: modality uint8 [B, Hkv, cap] (or [B, cap]), query_label
     uint8 [B], acc_self / acc_cross fp32 [B, Hkv, cap] (dense)."""
-    cp = p.c()
+    cp = p._c()
     assert q.dim() == 3 and q.stride(2) == 1 and out.is_contiguous() and out.dtype == torch.float32
     assert acc_self.is_contiguous() and acc_cross.is_contiguous() and acc_self.dtype == torch.float32
     assert query_label.dtype == torch.uint8 and query_label.is_contiguous()
@@ -346,7 +353,7 @@ def decode_step(p: Params, q, k, v, n_rows, modality, query_label, first_step, o
 
 
 def score(p: Params, q_win, k, modality, seq_lens, score_self, score_cross, ws, lse=None):
-    cp = p.c()
+    cp = p._c()
     sb, sh = _mod_strides(modality)
     _check(lib().csp_score(C.byref(cp), tensor4(q_win), tensor4(k), _ptr(modality), sb, sh, _ptr(seq_lens),
                            _ptr(lse), _ptr(score_self), _ptr(score_cross), _ptr(ws), ws.numel(), _stream()),
@@ -355,7 +362,7 @@ def score(p: Params, q_win, k, modality, seq_lens, score_self, score_cross, ws, 
 
 def weight_histogram(p: Params, q_win, k, modality, seq_lens, hist, ws, js=None, js_all=None, lse=None):
     """hist uint32-as-int32 [B, Hkv, 2, HIST_BINS]; js fp32 [B, Hkv]; js_all fp32 [1]."""
-    cp = p.c()
+    cp = p._c()
     sb, sh = _mod_strides(modality)
     assert hist.is_contiguous() and hist.element_size() == 4
     _check(lib().csp_weight_histogram(C.byref(cp), tensor4(q_win), tensor4(k), _ptr(modality), sb, sh, _ptr(seq_lens),
@@ -373,7 +380,7 @@ def probe_ex2_rate(fma_pipe: bool, iterations: int, sink: Optional[torch.Tensor]
 
 def select(p: Params, score_self, score_cross, modality, seq_lens, budgets, keep_idx, n_out, ws,
            total_budget=None):
-    cp = p.c()
+    cp = p._c()
     sb, sh = _mod_strides(modality)
     _check(lib().csp_select(C.byref(cp), _ptr(score_self), _ptr(score_cross), _ptr(modality), sb, sh,
                             _ptr(seq_lens), _ptr(budgets), _ptr(total_budget), _ptr(keep_idx), _ptr(n_out),
@@ -381,7 +388,7 @@ def select(p: Params, score_self, score_cross, modality, seq_lens, budgets, keep
 
 
 def compact(p: Params, k, v, modality, keep_idx, n_out, k_out, v_out, mod_out=None):
-    cp = p.c()
+    cp = p._c()
     sb, sh = _mod_strides(modality) if modality is not None else (0, 0)
     _check(lib().csp_compact(C.byref(cp), tensor4(k), tensor4(v), _ptr(modality), sb, sh, _ptr(keep_idx),
                              _ptr(n_out), tensor4(k_out), tensor4(v_out), _ptr(mod_out), _stream()),
@@ -390,7 +397,7 @@ def compact(p: Params, k, v, modality, keep_idx, n_out, k_out, v_out, mod_out=No
 
 def select_compact(p: Params, score_self, score_cross, k, v, modality, seq_lens, budgets, k_out, v_out, mod_out, n_out,
                    ws, total_budget=None, keep_idx=None):
-    cp = p.c()
+    cp = p._c()
     sb, sh = _mod_strides(modality)
     _check(lib().csp_select_compact(C.byref(cp), _ptr(score_self), _ptr(score_cross), tensor4(k), tensor4(v),
                                     _ptr(modality), sb, sh, _ptr(seq_lens), _ptr(budgets), _ptr(total_budget),
@@ -400,7 +407,7 @@ def select_compact(p: Params, score_self, score_cross, k, v, modality, seq_lens,
 
 def prune_layer(p: Params, q_win, k, v, modality, seq_lens, budgets, k_out, v_out, mod_out, n_out, ws,
                 total_budget=None, lse=None, score_self=None, score_cross=None, keep_idx=None):
-    cp = p.c()
+    cp = p._c()
     sb, sh = _mod_strides(modality)
     _check(lib().csp_prune_layer(C.byref(cp), tensor4(q_win), tensor4(k), tensor4(v), _ptr(modality), sb, sh,
                                  _ptr(seq_lens), _ptr(budgets), _ptr(total_budget), _ptr(lse),
@@ -413,7 +420,7 @@ def prune_layer_paged(p: Params, q_win, k_pool, v_pool, page_table, modality, se
                       n_out, ws, total_budget=None, lse=None, score_self=None, score_cross=None, keep_idx=None):
     """k_pool, v_pool [n_pages, Hkv, page_rows, d]; page_table int32 [B, max_pages] (dense).  k_out / v_out dense
     [B, Hkv, cap, d], or the pools themselves for pruning in place."""
-    cp = p.c()
+    cp = p._c()
     sb, sh = _mod_strides(modality)
     assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.dim() == 2
     pg = CPages(page_table.data_ptr(), page_table.shape[1], k_pool.shape[2], k_pool.shape[0])
@@ -426,7 +433,7 @@ def prune_layer_paged(p: Params, q_win, k_pool, v_pool, page_table, modality, se
 
 def decode_attn_paged(p: Params, q, k_pool, v_pool, page_table, n_rows, out, ws):
     """csp_decode_attn over pools [n_pages, Hkv, page_rows, d] addressed through page_table int32 [B, max_pages]."""
-    cp = p.c()
+    cp = p._c()
     assert q.dim() == 3 and q.stride(2) == 1 and out.is_contiguous() and out.dtype == torch.float32
     assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.dim() == 2
     qt = CTensor(q.data_ptr(), q.stride(0), q.stride(1), q.shape[2])
@@ -457,7 +464,7 @@ def _status_workspace(n: int, where: str, device) -> torch.Tensor:
 
 
 def chunk_workspace_bytes(p: Params, max_new: int) -> int:
-    cp = p.c()
+    cp = p._c()
     return int(lib().csp_chunk_workspace_bytes(C.byref(cp), int(max_new)))
 
 
@@ -481,7 +488,7 @@ def _chunk_args(p: Params, q, k, v, n_rows, out, ws, n_new, mods, lse):
 def chunk_attn(p: Params, q, k, v, n_rows, out, ws, n_new=None, mods: Optional[ScoreMods] = None, lse=None):
     """q, out bf16 [B, Hq, new tokens, d] (any strides); k, v [B, Hkv, out_capacity, d]; n_rows int32 [B, Hkv], the new rows
     included; n_new int32 [B]; lse fp32 [B, Hq, new tokens]."""
-    cp = p.c()
+    cp = p._c()
     T, rows, new, m = _chunk_args(p, q, k, v, n_rows, out, ws, n_new, mods, lse)
     assert k.shape[0] == v.shape[0] == p.batch and k.shape[2] >= p.out_capacity and v.shape[2] >= p.out_capacity
     _check(lib().csp_chunk_attn(C.byref(cp), T, tensor4(q), tensor4(k), tensor4(v), rows, new, m, tensor4(out), _ptr(lse),
@@ -491,7 +498,7 @@ def chunk_attn(p: Params, q, k, v, n_rows, out, ws, n_new=None, mods: Optional[S
 def chunk_attn_paged(p: Params, q, k_pool, v_pool, page_table, n_rows, out, ws, n_new=None,
                      mods: Optional[ScoreMods] = None, lse=None):
     """chunk_attn over pools [n_pages, Hkv, page_rows, d] addressed through page_table int32 [B, max_pages]."""
-    cp = p.c()
+    cp = p._c()
     T, rows, new, m = _chunk_args(p, q, k_pool, v_pool, n_rows, out, ws, n_new, mods, lse)
     pg = _pool_pages(p, k_pool, v_pool, page_table)
     _check(lib().csp_chunk_attn_paged(C.byref(cp), T, tensor4(q), tensor4(k_pool), tensor4(v_pool), C.byref(pg), rows, new, m,
@@ -508,7 +515,7 @@ def _pool_pages(p: Params, k_pool, v_pool, page_table) -> CPages:
 
 def new_append_workspace(p: Params, device="cuda") -> torch.Tensor:
     """Allocates (with torch) and zeroes a workspace for append_paged and pages_copy."""
-    cp = p.c()
+    cp = p._c()
     return _status_workspace(int(lib().csp_append_workspace_bytes(C.byref(cp))), "csp_append_workspace_bytes", device)
 
 
@@ -521,7 +528,7 @@ def _cache_dtype(p: Params, *tensors):
 
 def append_paged(p: Params, k_new, v_new, k_pool, v_pool, page_table, n_rows, n_rows_out, ws, n_new=None):
     """k_new, v_new [B, Hkv, new tokens, d] go behind the n_rows rows of every head; n_rows_out may be n_rows."""
-    cp = p.c()
+    cp = p._c()
     _here(k_new, v_new, n_rows, n_rows_out, ws, n_new)
     pg = _pool_pages(p, k_pool, v_pool, page_table)
     _cache_dtype(p, k_new, v_new, k_pool, v_pool)
@@ -581,7 +588,7 @@ def pages_compact(state: PageState, moves, n_moves, ws):
 
 def pages_copy(p: Params, k_pool, v_pool, moves, n_moves, ws):
     """Copies the pages listed in moves, K and V, all heads: one call per layer."""
-    cp = p.c()
+    cp = p._c()
     _here(k_pool, v_pool, moves, n_moves, ws)
     _cache_dtype(p, k_pool, v_pool)
     assert k_pool.shape == v_pool.shape
@@ -598,7 +605,7 @@ def prune_layer_static(p: Params, q_win, k, v, modality, seq_lens, budgets, k_ou
                        total_budget=None, lse=None, dev_status_out=None):
     """csp_prune_layer without a caller workspace: the library's built-in scratch array is used, so
     nothing is allocated.  Raises CspError(ERR_WORKSPACE) for shapes beyond static_workspace_limit()."""
-    cp = p.c()
+    cp = p._c()
     sb, sh = _mod_strides(modality)
     _check(lib().csp_prune_layer_static(C.byref(cp), tensor4(q_win), tensor4(k), tensor4(v), _ptr(modality), sb, sh,
                                         _ptr(seq_lens), _ptr(budgets), _ptr(total_budget), _ptr(lse),
@@ -607,7 +614,7 @@ def prune_layer_static(p: Params, q_win, k, v, modality, seq_lens, budgets, k_ou
 
 
 def host_staging_bytes(p: Params) -> int:
-    cp = p.c()
+    cp = p._c()
     return int(lib().csp_host_staging_bytes(C.byref(cp)))
 
 
@@ -615,7 +622,7 @@ def prune_layer_host(p: Params, q, k, v, modality, seq_lens, budgets, k_out, v_o
                      staging: torch.Tensor, total_budget=None) -> int:
     """All tensors but `staging` are dense CPU tensors (pinned for asynchronous copies).
     Returns the device status word."""
-    cp = p.c()
+    cp = p._c()
     for t in (q, k, v, modality, seq_lens, budgets, k_out, v_out, n_out):
         assert t.device.type == "cpu" and t.is_contiguous()
     word = C.c_int32(0)

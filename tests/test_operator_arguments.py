@@ -224,3 +224,24 @@ def test_empty_tensors_are_no_missing_ones(csp):
     assert lib.csp_pages_free(C.byref(s), 256, BIG, None) in fine
     s = _state(csp, batch=0, page_table=None, held=None, n_rows=None, refs=None)
     assert lib.csp_pages_free(C.byref(s), 256, BIG, None) == csp.ERR_INVALID_ARG
+
+
+def test_parameters_stay_plain_after_a_call(csp):
+    """What a call keeps beside them is no attribute that a copy through __dict__ would hand to the constructor."""
+    import copy
+    import dataclasses
+    import pickle
+    p = _params(csp, n=2.0)
+    fields = {f.name for f in dataclasses.fields(p)}
+    first, size = bytes(p.c()), csp.chunk_workspace_bytes(p, 3)
+    assert set(vars(p)) == fields
+    own = p.c()
+    own.head_dim = 64                                   # a caller's struct is the caller's
+    assert bytes(p.c()) == first and csp.chunk_workspace_bytes(p, 3) == size
+    for q in (csp.Params(**{**p.__dict__, "batch": 7}), dataclasses.replace(p, batch=7), copy.copy(p), copy.deepcopy(p), pickle.loads(pickle.dumps(p))):
+        q.batch = 7
+        csp.chunk_workspace_bytes(q, 3)
+        assert q.c().batch == 7 and q.c().n == 2.0 and set(vars(q)) == fields
+    assert bytes(p.c()) == first and p == _params(csp, n=2.0)
+    p.n_q_heads = 4
+    assert csp.chunk_workspace_bytes(p, 3) == csp.chunk_workspace_bytes(_params(csp, n_q_heads=4), 3) != size
