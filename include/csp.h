@@ -403,6 +403,98 @@ csp_status csp_append_paged(const csp_params* p, int32_t max_new, csp_tensor k_n
                             void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * Rotary position embedding: dimensions (x1, x2) of a pair become (x1 cos - x2 sin, x2 cos + x1 sin).
+ *   cos_sin      fp32: row `position` at cos_sin[position * row_stride] holds the cosines of rope_dim / 2 angles, then their
+ *                sines; 16-byte aligned, row_stride a multiple of 4
+ *   rope_dim     rotated leading dimensions, a multiple of 16 up to head_dim; the others stay as they are
+ *   interleaved  0: dimension i is paired with i + rope_dim / 2; 1: 2 i with 2 i + 1.  Angle i belongs to pair i
+ *   positions    int32: token i of sequence b stands at positions[b * pos_stride_b + i]; NULL: where its row is (n_rows + i), as
+ *                in a cache that was not pruned.  A position outside [0, table_rows) is flagged CSP_DEV_BAD_LEN and takes the
+ *                table's nearest row
+ */
+typedef struct {
+    const float* cos_sin;
+    int64_t row_stride;
+    int32_t table_rows, rope_dim, interleaved;
+    const int32_t* positions;
+    int64_t pos_stride_b;
+} csp_rope;
+
+/*
+ * csp_append_paged with the position rotation on the way: row n_rows[b,h] + i of unit (b,h) becomes the rotated k_new[b,h,i,:]
+ * and, as it is, v_new[b,h,i,:].  With queries, q_out[b,hq,i,:] becomes the rotated q[b,hq,i,:] in the same launch (also of
+ * tokens whose rows do not fit).  Rotated in fp32, each product and sum rounded, and rounded once to p->dtype.
+ *   n_new_or_null   as for csp_append_paged; with n_new_per_head != 0 it is [B, H_kv] (what a prune leaves in n_out)
+ *   q, q_out        [B, H_q, max_new, d] (any strides) like k_new; q_out may be q itself.  q.ptr NULL: no queries
+ *   n_rows_out      may be n_rows itself
+ * Everything else, and what is flagged, as for csp_append_paged.  Workspace: csp_append_workspace_bytes.
+ */
+csp_status csp_append_rope_paged(const csp_params* p, int32_t max_new, csp_tensor k_new, csp_tensor v_new,
+                                 const int32_t* n_new_or_null, int32_t n_new_per_head, const csp_rope* rope,
+                                 csp_tensor q, csp_tensor q_out, csp_tensor k_pool, csp_tensor v_pool, const csp_pages* pages,
+                                 const int32_t* n_rows, int32_t* n_rows_out,
+                                 void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The pages of K or of V in 4 bits.  A row of d values x is held as base + scale * code with base = min x, scale =
+ * (max x - base) / 15 rounded to bf16, and the code, a whole number from 0 to 15, nearest to (x - base) / scale (the upper one
+ * where two are; within 2^-20 of the middle either).  Where scale is below 2^-126 it is 0: the row reads as base.  A row with
+ * an infinity or NaN, or whose spread is no finite number, reads as NaN.
+ *   codes   uint8 [n_pages, H_kv, page_rows, d / 2]: byte i holds the code of value 2 i (low half) and of 2 i + 1.  Strides in
+ *           bytes; stride_t is d / 2, the others multiples of 16
+ *   scales  bf16 [n_pages, H_kv, page_rows, 2]: scale and base.  Strides in elements; stride_t is 2, the others multiples of 8
+ * Both 16-byte aligned.  d is 64 or 128: a row and its two numbers take d / 2 + 4 bytes instead of 2 d.  A cache that is not
+ * paged is one of a page per sequence (page_rows a multiple of 128).  Whole pages are copied by csp_pages_copy, which may see
+ * the rows of a page as rows of 256 bytes: codes as bf16 [n_pages, H_kv, page_rows * d / 512, 128], scales as
+ * [n_pages, H_kv, page_rows / 64, 128].
+ */
+typedef struct { csp_tensor codes, scales; } csp_q4_cache;
+
+/*
+ * csp_append_paged into pages in 4 bits, with the rotation on the way where rope is given: the rotated row is rounded to bf16, as
+ * a bf16 cache would hold it, and then to 4 bits.  k_new, v_new, q bf16 (p->dtype), head_dim 64 or 128; q needs a rope.
+ * Together with csp_prune_layer (k_out, v_out and n_out of the prune as k_new, v_new and n_new per head, no rope) it
+ * keeps what a prune left in a quarter of the bytes.  Everything else as for csp_append_rope_paged.
+ */
+csp_status csp_append_q4_paged(const csp_params* p, int32_t max_new, csp_tensor k_new, csp_tensor v_new,
+                               const int32_t* n_new_or_null, int32_t n_new_per_head, const csp_rope* rope_or_null,
+                               csp_tensor q, csp_tensor q_out, const csp_q4_cache* k_cache, const csp_q4_cache* v_cache,
+                               const csp_pages* pages, const int32_t* n_rows, int32_t* n_rows_out,
+                               void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Rows of a 4-bit cache as numbers again, e.g. the keys that csp_score needs: k_out[b,h,i,:] = row first[b,h] + i of unit
+ * (b,h), for all rows up to n_rows[b,h].
+ *   v_cache_or_null  NULL: K only (v_out is not used)
+ *   first_or_null    [B, H_kv] int32 device; NULL: from row 0.  A negative one counts as 0 (CSP_DEV_BAD_LEN)
+ *   n_rows           [B, H_kv] int32 device; clamped to [0, out_capacity] (CSP_DEV_BAD_LEN)
+ *   k_out, v_out     [B, H_kv, max_rows, d] (any strides) in p->dtype, bf16 or fp32; slots behind the last row are left as
+ *                    they were, rows that do not fit are left out (CSP_DEV_CAPACITY)
+ * A page number outside the pool is flagged CSP_DEV_BAD_LEN; its rows read as zeros.  Workspace:
+ * csp_append_workspace_bytes.
+ */
+csp_status csp_load_q4_paged(const csp_params* p, const csp_q4_cache* k_cache, const csp_q4_cache* v_cache_or_null,
+                             const csp_pages* pages, const int32_t* first_or_null, const int32_t* n_rows, int32_t max_rows,
+                             csp_tensor k_out, csp_tensor v_out,
+                             void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Bytes of scratch that csp_chunk_attn_q4_paged needs for chunks of up to max_new tokens; as csp_chunk_workspace_bytes. */
+size_t csp_chunk_q4_workspace_bytes(const csp_params* p, int32_t max_new);
+
+/*
+ * csp_chunk_attn_paged over a cache in 4 bits: the same attention of the values base + scale * code, with everything that it
+ * says of n_rows, n_new, mods, out and lse (rows that are only masked must have finite scale and base, rows behind n_rows may
+ * hold anything).  q and out bf16, head_dim 64 or 128.
+ * The codes enter the products as they are, whole numbers, and the two numbers of a row are applied to sums in fp32, so that
+ * nothing of K is rounded again; a weight, times its row's scale in V, is rounded to fp16 (11 bits) before it meets V.  Of a
+ * query, parts below 2^-24 of its largest one are lost.
+ */
+csp_status csp_chunk_attn_q4_paged(const csp_params* p, int32_t max_new, csp_tensor q, const csp_q4_cache* k_cache,
+                                   const csp_q4_cache* v_cache, const csp_pages* pages, const int32_t* n_rows,
+                                   const int32_t* n_new_or_null, const csp_score_mods* mods_or_null, csp_tensor out,
+                                   float* lse_or_null, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Whose pages are whose.  All arrays are device memory of the caller, changed in place:
  *   page_table [batch, max_pages]  as in csp_pages; entries at or behind held[b] are not read
  *   held       [batch]             pages that the sequence holds: the leading entries of its table row

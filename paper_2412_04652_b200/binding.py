@@ -30,7 +30,8 @@ EXPORTS = ("csp_workspace_bytes", "csp_workspace_reset", "csp_score", "csp_selec
            "csp_weight_histogram", "csp_probe_ex2_rate", "csp_prune_layer_paged",
            "csp_decode_attn_paged", "csp_select_compact", "csp_chunk_workspace_bytes", "csp_chunk_attn", "csp_chunk_attn_paged",
            "csp_append_workspace_bytes", "csp_append_paged", "csp_pages_workspace_bytes", "csp_pages_fork",
-           "csp_pages_reserve", "csp_pages_free", "csp_pages_compact", "csp_pages_copy")
+           "csp_pages_reserve", "csp_pages_free", "csp_pages_compact", "csp_pages_copy", "csp_append_rope_paged",
+           "csp_append_q4_paged", "csp_load_q4_paged", "csp_chunk_q4_workspace_bytes", "csp_chunk_attn_q4_paged")
 HIST_BINS, HIST_LO, HIST_WIDTH = 64, -32.0, 0.5
 
 
@@ -59,6 +60,15 @@ class CPageState(C.Structure):
     _fields_ = [("page_table", C.c_void_p), ("held", C.c_void_p), ("refs", C.c_void_p), ("n_rows", C.c_void_p),
                 ("batch", C.c_int32), ("n_heads", C.c_int32), ("max_pages", C.c_int32), ("page_rows", C.c_int32),
                 ("n_pages", C.c_int32)]
+
+
+class CRope(C.Structure):
+    _fields_ = [("cos_sin", C.c_void_p), ("row_stride", C.c_int64), ("table_rows", C.c_int32), ("rope_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("positions", C.c_void_p), ("pos_stride_b", C.c_int64)]
+
+
+class CQ4Cache(C.Structure):
+    _fields_ = [("codes", CTensor), ("scales", CTensor)]
 
 
 class CParams(C.Structure):
@@ -159,6 +169,49 @@ class PageState:
                           self.page_rows, refs.numel())
 
 
+@dataclass
+class Rope:
+    """Rotary position embedding (csp_rope).  cos_sin fp32 [table rows, rope_dim]: the cosines of rope_dim / 2 angles, then their
+    sines; positions int32 [B, new tokens], or None where a row's number is its position; interleaved: dimension 2 i is
+    paired with 2 i + 1, else i with i + rope_dim / 2."""
+    cos_sin: torch.Tensor
+    positions: Optional[torch.Tensor] = None
+    interleaved: bool = False
+
+    def c(self, batch: int, max_new: int) -> CRope:
+        t, pos = self.cos_sin, self.positions
+        assert t.dtype is torch.float32 and t.dim() == 2 and t.stride(1) == 1, "cos_sin: fp32 [table rows, rope_dim]"
+        r = CRope(t.data_ptr(), t.stride(0), t.shape[0], t.shape[1], int(self.interleaved))
+        if pos is not None:
+            ps = pos.shape
+            assert pos.dtype is torch.int32 and len(ps) == 2 and ps[0] == batch and ps[1] >= max_new and (pos.stride(1) == 1 or ps[1] <= 1), \
+                "positions: int32 [B, new tokens]"
+            r.positions, r.pos_stride_b = pos.data_ptr(), pos.stride(0)
+        return r
+
+
+@dataclass
+class Q4Cache:
+    """The pages of K or of V in 4 bits (csp_q4_cache): codes uint8 [n_pages, Hkv, page_rows, d / 2], scales bf16 [n_pages,
+    Hkv, page_rows, 2] (scale, base)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    def c(self, p: "Params") -> CQ4Cache:
+        codes, scales = self.codes, self.scales
+        cs = codes.shape
+        assert codes.dtype is torch.uint8 and scales.dtype is torch.bfloat16
+        assert len(cs) == 4 and cs[1] == p.n_kv_heads and 2 * cs[3] == p.head_dim and scales.shape == (*cs[:3], 2), \
+            "codes [n_pages, Hkv, page_rows, d / 2], scales [n_pages, Hkv, page_rows, 2]"
+        return CQ4Cache(tensor4(codes), tensor4(scales))
+
+
+def new_q4_cache(n_pages: int, n_kv_heads: int, page_rows: int, head_dim: int, device="cuda") -> Q4Cache:
+    """A pool of pages in 4 bits, all rows zero."""
+    return Q4Cache(torch.zeros(n_pages, n_kv_heads, page_rows, head_dim // 2, dtype=torch.uint8, device=device),
+                   torch.zeros(n_pages, n_kv_heads, page_rows, 2, dtype=torch.bfloat16, device=device))
+
+
 def new_page_state(batch: int, n_heads: int, max_pages: int, page_rows: int, n_pages: int, device="cuda") -> PageState:
     """A pool of n_pages free pages and `batch` sequences that hold none."""
     z = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device=device)  # noqa: E731
@@ -245,6 +298,17 @@ def lib() -> C.CDLL:
         l.csp_pages_compact.argtypes = [S, vp, i32, vp, vp, sz, vp]
         l.csp_pages_copy.restype = C.c_int
         l.csp_pages_copy.argtypes = [P, CTensor, CTensor, i32, i32, vp, i32, vp, vp, sz, vp]
+        RP, Q4 = C.POINTER(CRope), C.POINTER(CQ4Cache)
+        l.csp_append_rope_paged.restype = C.c_int
+        l.csp_append_rope_paged.argtypes = [P, i32, CTensor, CTensor, vp, i32, RP, CTensor, CTensor, CTensor, CTensor, G, vp, vp, vp, sz, vp]
+        l.csp_append_q4_paged.restype = C.c_int
+        l.csp_append_q4_paged.argtypes = [P, i32, CTensor, CTensor, vp, i32, RP, CTensor, CTensor, Q4, Q4, G, vp, vp, vp, sz, vp]
+        l.csp_load_q4_paged.restype = C.c_int
+        l.csp_load_q4_paged.argtypes = [P, Q4, Q4, G, vp, vp, i32, CTensor, CTensor, vp, sz, vp]
+        l.csp_chunk_q4_workspace_bytes.restype = sz
+        l.csp_chunk_q4_workspace_bytes.argtypes = [P, i32]
+        l.csp_chunk_attn_q4_paged.restype = C.c_int
+        l.csp_chunk_attn_q4_paged.argtypes = [P, i32, CTensor, Q4, Q4, G, vp, vp, M, CTensor, vp, vp, sz, vp]
         l.csp_probe_ex2_rate.restype = C.c_int
         l.csp_probe_ex2_rate.argtypes = [C.c_int32, C.c_int32, vp, sz, C.POINTER(C.c_int64), vp]
         l.csp_weight_histogram.restype = C.c_int
@@ -537,6 +601,110 @@ def append_paged(p: Params, k_new, v_new, k_pool, v_pool, page_table, n_rows, n_
                                   tensor4(k_pool), tensor4(v_pool), C.byref(pg), _counts(n_rows, (p.batch, p.n_kv_heads)),
                                   _counts(n_rows_out, (p.batch, p.n_kv_heads)), _ptr(ws), ws.numel(), _stream()),
            "csp_append_paged")
+
+
+_NOTHING = CTensor(None, 0, 0, 0)
+
+
+def _append_args(p: Params, k_new, v_new, n_rows, n_rows_out, ws, rope, n_new, q, q_out):
+    _here(k_new, v_new, n_rows, n_rows_out, ws, n_new, q, q_out)
+    _cache_dtype(p, k_new, v_new)
+    ks, B, H = k_new.shape, p.batch, p.n_kv_heads
+    T = ks[2]
+    assert v_new.shape == ks and ks[0] == B, "k_new, v_new: [B, Hkv, new tokens, d]"
+    per_head = n_new is not None and n_new.dim() == 2
+    cr = None
+    if rope is not None:
+        _here(rope.cos_sin, rope.positions)
+        cr = C.byref(rope.c(B, T))
+    qt = qo = _NOTHING
+    assert (q is None) == (q_out is None), "q and q_out go together"
+    if q is not None:
+        assert q.dtype is k_new.dtype is q_out.dtype and q.shape == q_out.shape == (B, p.n_q_heads, T, p.head_dim), \
+            "q, q_out: [B, Hq, new tokens, d] of the new rows' type"
+        qt, qo = tensor4(q), tensor4(q_out)
+    return T, _counts(n_new, (B, H) if per_head else (B,)), int(per_head), cr, qt, qo, _counts(n_rows, (B, H)), _counts(n_rows_out, (B, H))
+
+
+def append_rope_paged(p: Params, k_new, v_new, k_pool, v_pool, page_table, n_rows, n_rows_out, ws, rope: Rope, n_new=None,
+                      q=None, q_out=None):
+    """append_paged with the keys rotated on the way, and with them the queries q [B, Hq, new tokens, d] into q_out (which may be
+    q); n_new int32 [B] or [B, Hkv]."""
+    cp = p._c()
+    T, new, per_head, cr, qt, qo, rows, rows_out = _append_args(p, k_new, v_new, n_rows, n_rows_out, ws, rope, n_new, q, q_out)
+    pg = _pool_pages(p, k_pool, v_pool, page_table)
+    _cache_dtype(p, k_pool, v_pool)
+    _check(lib().csp_append_rope_paged(C.byref(cp), T, tensor4(k_new), tensor4(v_new), new, per_head, cr, qt, qo, tensor4(k_pool),
+                                       tensor4(v_pool), C.byref(pg), rows, rows_out, _ptr(ws), ws.numel(), _stream()),
+           "csp_append_rope_paged")
+
+
+def _q4_pages(p: Params, k_cache: Q4Cache, v_cache: Optional[Q4Cache], page_table):
+    """(K, V, pages) of a cache in 4 bits."""
+    _here(k_cache.codes, k_cache.scales, page_table)
+    ck, cv, ks = k_cache.c(p), None, k_cache.codes.shape
+    if v_cache is not None:
+        _here(v_cache.codes, v_cache.scales)
+        assert v_cache.codes.shape == ks
+        cv = C.byref(v_cache.c(p))
+    ts = page_table.shape
+    assert page_table.dtype is torch.int32 and len(ts) == 2 and ts[0] == p.batch and page_table.is_contiguous()
+    return C.byref(ck), cv, C.byref(CPages(page_table.data_ptr(), ts[1], ks[2], ks[0]))
+
+
+def append_q4_paged(p: Params, k_new, v_new, k_cache: Q4Cache, v_cache: Q4Cache, page_table, n_rows, n_rows_out, ws, n_new=None,
+                    rope: Optional[Rope] = None, q=None, q_out=None):
+    """append_rope_paged into pages in 4 bits; without rope nothing is rotated."""
+    cp = p._c()
+    T, new, per_head, cr, qt, qo, rows, rows_out = _append_args(p, k_new, v_new, n_rows, n_rows_out, ws, rope, n_new, q, q_out)
+    ck, cv, pg = _q4_pages(p, k_cache, v_cache, page_table)
+    _check(lib().csp_append_q4_paged(C.byref(cp), T, tensor4(k_new), tensor4(v_new), new, per_head, cr, qt, qo, ck, cv, pg, rows,
+                                     rows_out, _ptr(ws), ws.numel(), _stream()), "csp_append_q4_paged")
+
+
+def load_q4_paged(p: Params, k_cache: Q4Cache, v_cache: Optional[Q4Cache], page_table, n_rows, k_out, v_out, ws, first=None):
+    """Rows [first, n_rows) of a 4-bit cache as numbers: k_out, v_out [B, Hkv, rows, d] in p.dtype; without v_cache K only."""
+    cp = p._c()
+    _here(n_rows, first, k_out, v_out, ws)
+    ck, cv, pg = _q4_pages(p, k_cache, v_cache, page_table)
+    assert (v_cache is None) == (v_out is None), "v_cache and v_out go together"
+    _cache_dtype(p, *((k_out,) if v_out is None else (k_out, v_out)))
+    assert k_out.shape[0] == p.batch and (v_out is None or v_out.shape == k_out.shape)
+    B, H = p.batch, p.n_kv_heads
+    _check(lib().csp_load_q4_paged(C.byref(cp), ck, cv, pg, _counts(first, (B, H)), _counts(n_rows, (B, H)), k_out.shape[2],
+                                   tensor4(k_out), _NOTHING if v_out is None else tensor4(v_out), _ptr(ws), ws.numel(), _stream()),
+           "csp_load_q4_paged")
+
+
+def new_chunk_q4_workspace(p: Params, max_new: int, device="cuda") -> torch.Tensor:
+    """Allocates (with torch) and zeroes a workspace for chunk_attn_q4_paged with chunks of up to max_new tokens."""
+    cp = p._c()
+    return _status_workspace(int(lib().csp_chunk_q4_workspace_bytes(C.byref(cp), int(max_new))), "csp_chunk_q4_workspace_bytes", device)
+
+
+def chunk_attn_q4_paged(p: Params, q, k_cache: Q4Cache, v_cache: Q4Cache, page_table, n_rows, out, ws, n_new=None,
+                        mods: Optional[ScoreMods] = None, lse=None):
+    """chunk_attn_paged over pages in 4 bits."""
+    cp = p._c()
+    _here(q, n_rows, out, ws, n_new, lse, *(mods.tensors() if mods is not None else ()))
+    shape, bf16 = q.shape, torch.bfloat16
+    assert len(shape) == 4 and shape[0] == p.batch and shape[1] == p.n_q_heads and shape[3] == p.head_dim and out.shape == shape, \
+        f"q and out: [B, Hq, new tokens, d] = ({p.batch}, {p.n_q_heads}, new tokens, {p.head_dim})"
+    assert q.dtype is bf16 and out.dtype is bf16, "bf16 tensors expected"
+    assert lse is None or (lse.dtype is torch.float32 and lse.shape == shape[:3] and lse.is_contiguous())
+    ck, cv, pg = _q4_pages(p, k_cache, v_cache, page_table)
+    _check(lib().csp_chunk_attn_q4_paged(C.byref(cp), shape[2], tensor4(q), ck, cv, pg, _counts(n_rows, (p.batch, p.n_kv_heads)),
+                                         _counts(n_new, (p.batch,)), None if mods is None else C.byref(mods.c(p)), tensor4(out),
+                                         _ptr(lse), _ptr(ws), ws.numel(), _stream()), "csp_chunk_attn_q4_paged")
+
+
+def pages_copy_q4(p: Params, k_cache: Q4Cache, v_cache: Q4Cache, moves, n_moves, ws):
+    """pages_copy of pages in 4 bits (whose rows it sees as rows of 256 bytes): two launches."""
+    for a, b in ((k_cache.codes, v_cache.codes), (k_cache.scales, v_cache.scales)):
+        n, H, R, w = a.shape
+        rows = R * w * a.element_size() // 256
+        views = [t.view(torch.bfloat16).view(n, H, rows, 128) for t in (a, b)]
+        pages_copy(Params(p.batch, p.n_q_heads, H, 128, 1, 0, 0, 0), *views, moves, n_moves, ws)
 
 
 def new_pages_workspace(state: PageState, device="cuda") -> torch.Tensor:

@@ -578,31 +578,37 @@ bool pages_ok(const csp_pages* pg, int64_t rows, int batch) {
            int64_t(pg->max_pages) * pg->page_rows >= rows;
 }
 
-csp_status chunk_attn(const csp_params* p, int32_t max_new, const csp_tensor& q, const csp_tensor& k, const csp_tensor& v,
-                      const csp_pages* pages, const int32_t* n_rows, const int32_t* n_new, const csp_score_mods* mods,
-                      const csp_tensor& out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
-    csp_status st = check_params(p);
-    if (st != CSP_OK) return st;
-    const bool any = p->batch > 0 && max_new > 0;        // (empty tensors have no address)
-    if (max_new < 0 || (any && (!q.ptr || !k.ptr || !v.ptr || !n_rows || !out.ptr))) return CSP_ERR_INVALID_ARG;
-    if (mods && !(mods->softcap == 0.f || (mods->softcap >= 1e-6f && mods->softcap <= 1000.f))) return CSP_ERR_INVALID_ARG;
-    const size_t need = chunk_workspace_bytes(*p, max_new);
-    if (need == 0) return CSP_ERR_UNSUPPORTED;
-    if (any && (!tensor_ok(*p, q) || !tensor_ok(*p, k) || !tensor_ok(*p, v) || !tensor_ok(*p, out))) return CSP_ERR_UNSUPPORTED;
-    if (any && !rows_apart(*p, out, p->batch, p->n_q_heads, max_new)) return CSP_ERR_UNSUPPORTED;
-    if (!status_area_ok(workspace, workspace_bytes, need)) return CSP_ERR_WORKSPACE;
-    if ((st = check_arch()) != CSP_OK) return st;
-    if (!any) return CSP_OK;
+bool mods_valid(const csp_score_mods* m) {
+    return !m || m->softcap == 0.f || (m->softcap >= 1e-6f && m->softcap <= 1000.f);
+}
+
+// codes and scales of a cache in 4 bits: the rows of a head in a page lie one behind the other
+bool q4_ok(const csp_params& p, const csp_q4_cache& c) {
+    return uintptr_t(c.codes.ptr) % 16 == 0 && uintptr_t(c.scales.ptr) % 16 == 0 && c.codes.stride_t == p.head_dim / 2 &&
+           c.scales.stride_t == 2 && c.codes.stride_b >= 0 && c.codes.stride_h >= 0 && c.scales.stride_b >= 0 && c.scales.stride_h >= 0 &&
+           c.codes.stride_b % 16 == 0 && c.codes.stride_h % 16 == 0 && c.scales.stride_b % 8 == 0 && c.scales.stride_h % 8 == 0;
+}
+// (for those that are written) no two rows share memory
+bool q4_apart(const csp_params& p, const csp_q4_cache& c, const csp_pages& pg) {
+    const int64_t codes = int64_t(pg.page_rows) * (p.head_dim / 2), scales = int64_t(pg.page_rows) * 2;
+    return (p.n_kv_heads <= 1 || (c.codes.stride_h >= codes && c.scales.stride_h >= scales)) &&
+           (pg.n_pages <= 1 || (c.codes.stride_b >= codes && c.scales.stride_b >= scales));
+}
+
+RowTensor row_tensor(const csp_tensor& t, int64_t elem) { return RowTensor{t.ptr, t.stride_b * elem, t.stride_h * elem, t.stride_t * elem}; }
+
+ChunkArgs chunk_args(const csp_params& p, int32_t max_new, const csp_pages* pages, const int32_t* n_rows, const int32_t* n_new,
+                     const csp_score_mods* mods, const csp_tensor& out, float* lse, void* workspace) {
     ChunkArgs a;
     a.n_rows = n_rows; a.n_new = n_new;
     a.out = static_cast<uint16_t*>(out.ptr); a.o_sb = out.stride_b; a.o_sh = out.stride_h; a.o_st = out.stride_t;
     a.out_wide = uintptr_t(out.ptr) % 32 == 0 && out.stride_b % 16 == 0 && out.stride_h % 16 == 0 && out.stride_t % 16 == 0;
     a.lse = lse;
     a.status = static_cast<int32_t*>(workspace);
-    a.batch = p->batch; a.n_kv_heads = p->n_kv_heads; a.group = p->n_q_heads / p->n_kv_heads;
-    a.capacity = p->out_capacity; a.max_new = max_new;
-    a.n = p->n;
-    a.scale = p->scale > 0.f ? p->scale : 1.0f / sqrtf(float(p->head_dim));
+    a.batch = p.batch; a.n_kv_heads = p.n_kv_heads; a.group = p.n_q_heads / p.n_kv_heads;
+    a.capacity = p.out_capacity; a.max_new = max_new;
+    a.n = p.n;
+    a.scale = p.scale > 0.f ? p.scale : 1.0f / sqrtf(float(p.head_dim));
     a.mods = ModArgs{0.f, nullptr, nullptr, 0, 0, nullptr, 0, 0, nullptr, 0, 0};
     if (mods) {
         a.mods = ModArgs{mods->softcap, mods->slopes,
@@ -614,6 +620,25 @@ csp_status chunk_attn(const csp_params* p, int32_t max_new, const csp_tensor& q,
     a.max_pages = pages ? pages->max_pages : 0;
     a.page_rows = pages ? pages->page_rows : 1;
     a.n_pages = pages ? pages->n_pages : 0;
+    return a;
+}
+
+csp_status chunk_attn(const csp_params* p, int32_t max_new, const csp_tensor& q, const csp_tensor& k, const csp_tensor& v,
+                      const csp_pages* pages, const int32_t* n_rows, const int32_t* n_new, const csp_score_mods* mods,
+                      const csp_tensor& out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    csp_status st = check_params(p);
+    if (st != CSP_OK) return st;
+    const bool any = p->batch > 0 && max_new > 0;        // (empty tensors have no address)
+    if (max_new < 0 || (any && (!q.ptr || !k.ptr || !v.ptr || !n_rows || !out.ptr))) return CSP_ERR_INVALID_ARG;
+    if (!mods_valid(mods)) return CSP_ERR_INVALID_ARG;
+    const size_t need = chunk_workspace_bytes(*p, max_new);
+    if (need == 0) return CSP_ERR_UNSUPPORTED;
+    if (any && (!tensor_ok(*p, q) || !tensor_ok(*p, k) || !tensor_ok(*p, v) || !tensor_ok(*p, out))) return CSP_ERR_UNSUPPORTED;
+    if (any && !rows_apart(*p, out, p->batch, p->n_q_heads, max_new)) return CSP_ERR_UNSUPPORTED;
+    if (!status_area_ok(workspace, workspace_bytes, need)) return CSP_ERR_WORKSPACE;
+    if ((st = check_arch()) != CSP_OK) return st;
+    if (!any) return CSP_OK;
+    const ChunkArgs a = chunk_args(*p, max_new, pages, n_rows, n_new, mods, out, lse, workspace);
     return launch_chunk_attn(*p, a, q, k, v, pages, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -674,6 +699,152 @@ csp_status csp_append_paged(const csp_params* p, int32_t max_new, csp_tensor k_n
     a.n_pages = pages->n_pages;
     a.status = static_cast<int32_t*>(workspace);
     return launch_append(a, static_cast<cudaStream_t>(cuda_stream));
+}
+
+// ---- rotated appends, and a cache in 4 bits
+namespace {
+
+bool rope_valid(const csp_rope& r) {
+    return r.cos_sin && r.table_rows > 0 && r.rope_dim > 0 && r.rope_dim % 16 == 0 && (r.interleaved == 0 || r.interleaved == 1) &&
+           r.row_stride >= r.rope_dim;
+}
+
+// What both appends check and fill in alike; the pools come in afterwards.
+csp_status append_rows_args(const csp_params* p, int32_t max_new, const csp_tensor& k_new, const csp_tensor& v_new,
+                            const int32_t* n_new, int32_t n_new_per_head, const csp_rope* rope, const csp_tensor& q,
+                            const csp_tensor& q_out, const csp_pages* pages, const int32_t* n_rows, int32_t* n_rows_out,
+                            AppendRowsArgs& a) {
+    const bool any = p->batch > 0 && max_new > 0;        // (empty tensors have no address)
+    if (max_new < 0 || (any && (!k_new.ptr || !v_new.ptr)) || (p->batch > 0 && (!n_rows || !n_rows_out))) return CSP_ERR_INVALID_ARG;
+    if (any && q.ptr && (!q_out.ptr || !rope)) return CSP_ERR_INVALID_ARG;
+    if (rope && !rope_valid(*rope)) return CSP_ERR_INVALID_ARG;
+    if (!pages_ok(pages, p->out_capacity, p->batch)) return CSP_ERR_INVALID_ARG;
+    if (any && (!tensor_ok(*p, k_new) || !tensor_ok(*p, v_new))) return CSP_ERR_UNSUPPORTED;
+    const bool with_q = any && q.ptr;
+    if (with_q && (!tensor_ok(*p, q) || !tensor_ok(*p, q_out) || !rows_apart(*p, q_out, p->batch, p->n_q_heads, max_new))) return CSP_ERR_UNSUPPORTED;
+    if (rope && (rope->rope_dim > p->head_dim || uintptr_t(rope->cos_sin) % 16 || rope->row_stride % 4)) return CSP_ERR_UNSUPPORTED;
+    const int64_t es = elem_size(*p);
+    a = AppendRowsArgs{};
+    a.k_new = row_tensor(k_new, es); a.v_new = row_tensor(v_new, es);
+    if (with_q) { a.q = row_tensor(q, es); a.q_out = row_tensor(q_out, es); }
+    if (rope)
+        a.rope = RopeArgs{rope->cos_sin, rope->row_stride, rope->table_rows, rope->rope_dim, rope->interleaved != 0,
+                          rope->positions, rope->pos_stride_b};
+    a.n_new = n_new; a.n_new_per_head = n_new_per_head != 0;
+    a.n_rows = n_rows; a.n_rows_out = n_rows_out;
+    a.batch = p->batch; a.n_kv_heads = p->n_kv_heads; a.n_q_heads = with_q ? p->n_q_heads : 0;
+    a.group = p->n_q_heads / p->n_kv_heads; a.max_new = max_new; a.capacity = p->out_capacity;
+    a.page_table = pages->page_table; a.max_pages = pages->max_pages; a.page_rows = pages->page_rows; a.n_pages = pages->n_pages;
+    return CSP_OK;
+}
+
+}  // namespace
+
+csp_status csp_append_rope_paged(const csp_params* p, int32_t max_new, csp_tensor k_new, csp_tensor v_new,
+                                 const int32_t* n_new_or_null, int32_t n_new_per_head, const csp_rope* rope, csp_tensor q,
+                                 csp_tensor q_out, csp_tensor k_pool, csp_tensor v_pool, const csp_pages* pages,
+                                 const int32_t* n_rows, int32_t* n_rows_out, void* workspace, size_t workspace_bytes,
+                                 void* cuda_stream) {
+    csp_status st = check_params(p);
+    if (st != CSP_OK) return st;
+    if (!rope || !k_pool.ptr || !v_pool.ptr) return CSP_ERR_INVALID_ARG;
+    AppendRowsArgs a;
+    st = append_rows_args(p, max_new, k_new, v_new, n_new_or_null, n_new_per_head, rope, q, q_out, pages, n_rows, n_rows_out, a);
+    if (st != CSP_OK) return st;
+    if (!tensor_ok(*p, k_pool) || !tensor_ok(*p, v_pool) ||
+        !rows_apart(*p, k_pool, pages->n_pages, p->n_kv_heads, pages->page_rows) ||
+        !rows_apart(*p, v_pool, pages->n_pages, p->n_kv_heads, pages->page_rows))
+        return CSP_ERR_UNSUPPORTED;
+    if (!status_area_ok(workspace, workspace_bytes, kStatusBytes)) return CSP_ERR_WORKSPACE;
+    if ((st = check_arch()) != CSP_OK) return st;
+    a.k = row_tensor(k_pool, elem_size(*p)); a.v = row_tensor(v_pool, elem_size(*p));
+    a.status = static_cast<int32_t*>(workspace);
+    return launch_append_rows(a, p->head_dim, p->dtype == CSP_F32, false, static_cast<cudaStream_t>(cuda_stream));
+}
+
+csp_status csp_append_q4_paged(const csp_params* p, int32_t max_new, csp_tensor k_new, csp_tensor v_new,
+                               const int32_t* n_new_or_null, int32_t n_new_per_head, const csp_rope* rope_or_null, csp_tensor q,
+                               csp_tensor q_out, const csp_q4_cache* k_cache, const csp_q4_cache* v_cache,
+                               const csp_pages* pages, const int32_t* n_rows, int32_t* n_rows_out, void* workspace,
+                               size_t workspace_bytes, void* cuda_stream) {
+    csp_status st = check_params(p);
+    if (st != CSP_OK) return st;
+    if (!k_cache || !v_cache || !k_cache->codes.ptr || !v_cache->codes.ptr || !k_cache->scales.ptr || !v_cache->scales.ptr)
+        return CSP_ERR_INVALID_ARG;
+    if (p->dtype != CSP_BF16 || (p->head_dim != 64 && p->head_dim != 128)) return CSP_ERR_UNSUPPORTED;
+    AppendRowsArgs a;
+    st = append_rows_args(p, max_new, k_new, v_new, n_new_or_null, n_new_per_head, rope_or_null, q, q_out, pages, n_rows, n_rows_out, a);
+    if (st != CSP_OK) return st;
+    if (!q4_ok(*p, *k_cache) || !q4_ok(*p, *v_cache) || !q4_apart(*p, *k_cache, *pages) || !q4_apart(*p, *v_cache, *pages))
+        return CSP_ERR_UNSUPPORTED;
+    if (!status_area_ok(workspace, workspace_bytes, kStatusBytes)) return CSP_ERR_WORKSPACE;
+    if ((st = check_arch()) != CSP_OK) return st;
+    a.k = row_tensor(k_cache->codes, 1); a.v = row_tensor(v_cache->codes, 1);
+    a.k_scales = row_tensor(k_cache->scales, 2); a.v_scales = row_tensor(v_cache->scales, 2);
+    a.status = static_cast<int32_t*>(workspace);
+    return launch_append_rows(a, p->head_dim, false, true, static_cast<cudaStream_t>(cuda_stream));
+}
+
+csp_status csp_load_q4_paged(const csp_params* p, const csp_q4_cache* k_cache, const csp_q4_cache* v_cache_or_null,
+                             const csp_pages* pages, const int32_t* first_or_null, const int32_t* n_rows, int32_t max_rows,
+                             csp_tensor k_out, csp_tensor v_out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    csp_status st = check_params(p);
+    if (st != CSP_OK) return st;
+    const csp_q4_cache* const v = v_cache_or_null;
+    const bool any = p->batch > 0 && max_rows > 0;       // (empty tensors have no address)
+    if (max_rows < 0 || !k_cache || !k_cache->codes.ptr || !k_cache->scales.ptr || (v && (!v->codes.ptr || !v->scales.ptr)) ||
+        (any && (!n_rows || !k_out.ptr || (v && !v_out.ptr))))
+        return CSP_ERR_INVALID_ARG;
+    if (!pages_ok(pages, p->out_capacity, p->batch)) return CSP_ERR_INVALID_ARG;
+    if (p->head_dim != 64 && p->head_dim != 128) return CSP_ERR_UNSUPPORTED;
+    if (!q4_ok(*p, *k_cache) || (v && !q4_ok(*p, *v))) return CSP_ERR_UNSUPPORTED;
+    if (any && (!tensor_ok(*p, k_out) || !rows_apart(*p, k_out, p->batch, p->n_kv_heads, max_rows) ||
+                (v && (!tensor_ok(*p, v_out) || !rows_apart(*p, v_out, p->batch, p->n_kv_heads, max_rows)))))
+        return CSP_ERR_UNSUPPORTED;
+    if (!status_area_ok(workspace, workspace_bytes, kStatusBytes)) return CSP_ERR_WORKSPACE;
+    if ((st = check_arch()) != CSP_OK) return st;
+    if (!any) return CSP_OK;
+    const int64_t es = elem_size(*p);
+    LoadRowsArgs a = {};
+    a.k = row_tensor(k_cache->codes, 1); a.k_scales = row_tensor(k_cache->scales, 2); a.k_out = row_tensor(k_out, es);
+    if (v) { a.v = row_tensor(v->codes, 1); a.v_scales = row_tensor(v->scales, 2); a.v_out = row_tensor(v_out, es); }
+    a.first = first_or_null; a.n_rows = n_rows;
+    a.units = p->batch * p->n_kv_heads; a.n_kv_heads = p->n_kv_heads; a.max_rows = max_rows; a.capacity = p->out_capacity;
+    a.page_table = pages->page_table; a.max_pages = pages->max_pages; a.page_rows = pages->page_rows; a.n_pages = pages->n_pages;
+    a.status = static_cast<int32_t*>(workspace);
+    return launch_load_rows(a, p->head_dim, p->dtype == CSP_F32, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t csp_chunk_q4_workspace_bytes(const csp_params* p, int32_t max_new) {
+    if (check_params(p) != CSP_OK || max_new < 0) return 0;
+    return chunk_q4_workspace_bytes(*p, max_new);
+}
+
+csp_status csp_chunk_attn_q4_paged(const csp_params* p, int32_t max_new, csp_tensor q, const csp_q4_cache* k_cache,
+                                   const csp_q4_cache* v_cache, const csp_pages* pages, const int32_t* n_rows,
+                                   const int32_t* n_new_or_null, const csp_score_mods* mods_or_null, csp_tensor out,
+                                   float* lse_or_null, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    csp_status st = check_params(p);
+    if (st != CSP_OK) return st;
+    const bool any = p->batch > 0 && max_new > 0;        // (empty tensors have no address)
+    if (max_new < 0 || (any && (!q.ptr || !n_rows || !out.ptr)) || !k_cache || !v_cache || !k_cache->codes.ptr || !k_cache->scales.ptr ||
+        !v_cache->codes.ptr || !v_cache->scales.ptr)
+        return CSP_ERR_INVALID_ARG;
+    if (!pages_ok(pages, p->out_capacity, p->batch)) return CSP_ERR_INVALID_ARG;
+    if (!mods_valid(mods_or_null)) return CSP_ERR_INVALID_ARG;
+    const size_t need = chunk_q4_workspace_bytes(*p, max_new);
+    if (need == 0 || !q4_ok(*p, *k_cache) || !q4_ok(*p, *v_cache)) return CSP_ERR_UNSUPPORTED;
+    if (any && (!tensor_ok(*p, q) || !tensor_ok(*p, out) || !rows_apart(*p, out, p->batch, p->n_q_heads, max_new)))
+        return CSP_ERR_UNSUPPORTED;
+    if (!status_area_ok(workspace, workspace_bytes, need)) return CSP_ERR_WORKSPACE;
+    if ((st = check_arch()) != CSP_OK) return st;
+    if (!any) return CSP_OK;
+    const ChunkArgs a = chunk_args(*p, max_new, pages, n_rows, n_new_or_null, mods_or_null, out, lse_or_null, workspace);
+    const RowTensor k = row_tensor(k_cache->codes, 1), v = row_tensor(v_cache->codes, 1);
+    const RowTensor ks = row_tensor(k_cache->scales, 2), vs = row_tensor(v_cache->scales, 2);
+    const auto bytes = [](const RowTensor& t) { return static_cast<const uint8_t*>(t.ptr); };
+    const Q4Args c = {bytes(k), k.sb, k.sh, bytes(v), v.sb, v.sh, bytes(ks), ks.sb, ks.sh, bytes(vs), vs.sb, vs.sh};
+    return launch_chunk_q4(*p, a, q, c, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 
 namespace {

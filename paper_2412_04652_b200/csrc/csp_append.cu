@@ -1,0 +1,375 @@
+// New rows on their way into the pages: keys and queries rotated by their positions, rows quantised to 4 bits, and rows of a
+// 4-bit cache read back.
+//
+// Rotation.  Dimensions (x1, x2) of a pair become (x1 cos - x2 sin, x2 cos + x1 sin), the angles from the caller's table; four
+// products and two sums, each rounded to fp32, and one rounding to the row's type.
+// Four bits.  base = min x, scale = bf16((max x - base) / 15), code = the whole number nearest to (x - base) / scale.  The
+// quotient is a product with 1 / scale (1 + 2^-21): the three roundings on the way (2^-24 each) cannot bring a quotient that lies
+// halfway between two codes, which values of 8 bits often do, below the middle, so that the upper code is taken always and not
+// now and then.
+//
+// A row of d values is held by d / 16 neighbouring lanes, sixteen values each, so that the row's extremes take three shuffles, and
+// a pair is always in one thread: with halves paired a lane takes eight values from each half.  A group of lanes keeps its
+// token and goes over the heads, so that its eight cosines and sines are loaded once.
+#include "csp_internal.cuh"
+
+namespace csp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kCountWord = 12;                           // of the status area: blocks that are done; left at zero
+constexpr float kSmallest = 1.17549435e-38f;             // 2^-126
+
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint4 ld_stream(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float bf16_lo(uint32_t x) { return __uint_as_float(x << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
+
+// eight neighbouring values of a row, as they lie in memory
+template <bool kF32> struct Eight { uint4 x[kF32 ? 2 : 1]; };
+template <bool kF32>
+__device__ __forceinline__ Eight<kF32> load_eight(const void* row, int chunk) {
+    Eight<kF32> r;
+    const uint4* const p = static_cast<const uint4*>(row) + chunk * (kF32 ? 2 : 1);
+#pragma unroll
+    for (int j = 0; j < (kF32 ? 2 : 1); ++j) r.x[j] = ld_stream(p + j);
+    return r;
+}
+template <bool kF32>
+__device__ __forceinline__ void store_eight(void* row, int chunk, const Eight<kF32>& r) {
+    uint4* const p = static_cast<uint4*>(row) + chunk * (kF32 ? 2 : 1);
+#pragma unroll
+    for (int j = 0; j < (kF32 ? 2 : 1); ++j) p[j] = r.x[j];
+}
+template <bool kF32>
+__device__ __forceinline__ void widen(const Eight<kF32>& r, float* f) {
+    const uint32_t* const w = reinterpret_cast<const uint32_t*>(&r);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = kF32 ? __uint_as_float(w[j]) : (j & 1 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]));
+}
+template <bool kF32>
+__device__ __forceinline__ Eight<kF32> narrow(const float* f) {
+    Eight<kF32> r;
+    uint32_t* const w = reinterpret_cast<uint32_t*>(&r);
+#pragma unroll
+    for (int j = 0; j < (kF32 ? 8 : 4); ++j) w[j] = kF32 ? __float_as_uint(f[j]) : pack_bf16(f[2 * j], f[2 * j + 1]);
+    return r;
+}
+
+// What the call does with unit (b, h): its first new row, how many follow, and how many the caller brings (of which none
+// are stored where they do not fit).  Flags what it refuses.
+struct NewRows { int first, stored, brought; };
+__device__ __forceinline__ NewRows new_rows(const AppendRowsArgs& a, int b, int h, bool flag) {
+    NewRows x;
+    int bad = 0;
+    const int u = b * a.n_kv_heads + h;
+    x.first = a.n_rows[u];
+    x.brought = a.n_new ? a.n_new[a.n_new_per_head ? u : b] : a.max_new;
+    if (x.brought < 0 || x.brought > a.max_new) { bad |= CSP_DEV_BAD_LEN; x.brought = x.brought < 0 ? 0 : a.max_new; }
+    x.stored = x.brought;
+    if (x.first < 0) { bad |= CSP_DEV_BAD_LEN; x.stored = 0; }
+    else if (int64_t(x.first) + x.brought > a.capacity) { bad |= CSP_DEV_CAPACITY; x.stored = 0; }
+    if (flag && bad) atomicOr(a.status, bad);
+    return x;
+}
+
+// the sixteen values' extremes over the lanes of a row
+template <int kLanes>
+__device__ __forceinline__ void row_range(const float (&f)[16], float& lo, float& hi) {
+    lo = hi = f[0];
+#pragma unroll
+    for (int j = 1; j < 16; ++j) { lo = min_nan(lo, f[j]); hi = max_nan(hi, f[j]); }
+#pragma unroll
+    for (int d = 1; d < kLanes; d <<= 1) {
+        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+    }
+}
+__device__ __forceinline__ uint32_t eight_codes(const float* f, float lo, float inv) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        // (adding 1.5 x 2^23 rounds to a whole number, which is then in the low bits)
+        const uint32_t c = __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(f[j], lo), inv), 12582912.f)) & 15u;
+        w |= c << (4 * j);
+    }
+    return w;
+}
+
+// Grid (token tiles of a sequence x sequences, pieces of the heads).  Bound by memory: every byte is read and written once.
+template <bool kF32, bool kFour, int kLanes>             // kLanes = d / 16
+__global__ void __launch_bounds__(kThreads) append_rows_kernel(const AppendRowsArgs a) {
+    const int tid = threadIdx.x, L = tid % kLanes, group = tid / kLanes;
+    const int b = blockIdx.x / a.token_tiles, tile = blockIdx.x - b * a.token_tiles;
+    const int H = a.n_kv_heads, slots = 2 * H + a.n_q_heads;         // K rows, V rows, rows of Q
+    const int log_tok = a.log_tokens, strides = (kThreads / kLanes) >> log_tok;      // groups per token
+    const int local = group & ((1 << log_tok) - 1);
+    const int slot0 = int(blockIdx.y) * a.slots_per_block, slot_end = min(slot0 + a.slots_per_block, slots);
+    const int pair_lanes = a.rope.dim / 16;              // lanes whose values are rotated
+    const bool turned = L < pair_lanes;
+    const bool halves = turned && !a.rope.interleaved;
+    const bool lead = tile == 0 && blockIdx.y == 0;
+    // (token tiles beyond the grid's: a tile per step)
+    for (int t0 = tile << log_tok; t0 < a.max_new; t0 += a.token_tiles << log_tok) {
+        const int i = t0 + local;
+        float cs[8], sn[8];
+        int at = -1;                                     // row of the table that cs and sn come from
+#pragma unroll 2
+        for (int s_base = slot0; s_base < slot_end; s_base += strides) {
+            const int s = s_base + (group >> log_tok);
+            // (every lane goes through the shuffles, with or without a row)
+            const bool is_q = s >= 2 * H, is_v = !is_q && s >= H;
+            const int hq = s - 2 * H, h = is_q ? hq / a.group : is_v ? s - H : s;
+            bool here = s < slot_end && i < a.max_new;
+            NewRows x = {0, 0, 0};
+            if (here) x = new_rows(a, b, h, false);
+            here = here && i < (is_q ? x.brought : x.stored);
+            const bool turn = !is_v && turned, apart = !is_v && halves;
+            const int c0 = apart ? L : 2 * L, c1 = apart ? L + pair_lanes : 2 * L + 1;
+            float f[16];
+            Eight<kF32> r0, r1;
+            if (here) {
+                const RowTensor& from = is_q ? a.q : is_v ? a.v_new : a.k_new;
+                const char* const row = static_cast<const char*>(from.ptr) + b * from.sb + (is_q ? hq : h) * from.sh + i * from.st;
+                r0 = load_eight<kF32>(row, c0);
+                r1 = load_eight<kF32>(row, c1);
+                if (turn) {
+                    int pos = a.rope.positions ? a.rope.positions[b * a.rope.pos_sb + i] : x.first + i;
+                    if (pos < 0 || pos >= a.rope.table_rows) {
+                        if (L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
+                        pos = pos < 0 ? 0 : a.rope.table_rows - 1;
+                    }
+                    if (pos != at) {
+                        at = pos;
+                        const float* const row_cs = a.rope.cos_sin + pos * a.rope.row_stride + 8 * L;
+                        const float* const row_sn = row_cs + a.rope.dim / 2;
+#pragma unroll
+                        for (int j = 0; j < 8; j += 4) {
+                            const float4 y = *reinterpret_cast<const float4*>(row_cs + j), z = *reinterpret_cast<const float4*>(row_sn + j);
+                            cs[j] = y.x; cs[j + 1] = y.y; cs[j + 2] = y.z; cs[j + 3] = y.w;
+                            sn[j] = z.x; sn[j + 1] = z.y; sn[j + 2] = z.z; sn[j + 3] = z.w;
+                        }
+                    }
+                }
+            }
+            if (here && (turn || kFour)) {
+                widen<kF32>(r0, f);
+                widen<kF32>(r1, f + 8);
+                if (turn) {
+                    if (apart) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float x1 = f[j], x2 = f[j + 8];
+                            f[j] = __fsub_rn(__fmul_rn(x1, cs[j]), __fmul_rn(x2, sn[j]));
+                            f[j + 8] = __fadd_rn(__fmul_rn(x2, cs[j]), __fmul_rn(x1, sn[j]));
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float x1 = f[2 * j], x2 = f[2 * j + 1];
+                            f[2 * j] = __fsub_rn(__fmul_rn(x1, cs[j]), __fmul_rn(x2, sn[j]));
+                            f[2 * j + 1] = __fadd_rn(__fmul_rn(x2, cs[j]), __fmul_rn(x1, sn[j]));
+                        }
+                    }
+                    r0 = narrow<kF32>(f);
+                    r1 = narrow<kF32>(f + 8);
+                    if (kFour) { widen<kF32>(r0, f); widen<kF32>(r1, f + 8); }       // what a bf16 cache would hold
+                }
+            }
+            float lo = 0.f, hi = 0.f;
+            if (kFour) {
+                if (!here) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) f[j] = 0.f;
+                }
+                row_range<kLanes>(f, lo, hi);
+            }
+            if (!here) continue;
+            if (is_q) {
+                char* const row = static_cast<char*>(a.q_out.ptr) + b * a.q_out.sb + hq * a.q_out.sh + i * a.q_out.st;
+                store_eight<kF32>(row, c0, r0);
+                store_eight<kF32>(row, c1, r1);
+                continue;
+            }
+            const uint32_t t = uint32_t(x.first + i), slot = t % uint32_t(a.page_rows);
+            const int page = a.page_table[int64_t(b) * a.max_pages + t / uint32_t(a.page_rows)];
+            if (page < 0 || page >= a.n_pages) {
+                if (L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
+                continue;
+            }
+            const RowTensor& to = is_v ? a.v : a.k;
+            char* const row = static_cast<char*>(to.ptr) + page * to.sb + h * to.sh + slot * to.st;
+            if (!kFour) {
+                store_eight<kF32>(row, c0, r0);
+                store_eight<kF32>(row, c1, r1);
+            } else {
+                uint32_t pair = pack_bf16(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), lo);
+                float scale = bf16_lo(pair);
+                if (scale < kSmallest) { scale = 0.f; pair &= 0xffff0000u; }
+                if (!(scale < INFINITY)) pair |= 0x7fffu;        // the whole row is no number
+                const float inv = scale > 0.f ? __fmul_rn(__frcp_rn(scale), 1.f + 0x1p-21f) : 0.f;
+                const uint32_t w0 = eight_codes(f, lo, inv), w1 = eight_codes(f + 8, lo, inv);
+                if (apart) {
+                    reinterpret_cast<uint32_t*>(row)[c0] = w0;
+                    reinterpret_cast<uint32_t*>(row)[c1] = w1;
+                } else {
+                    reinterpret_cast<uint2*>(row)[L] = make_uint2(w0, w1);
+                }
+                if (L == 0) {
+                    const RowTensor& sc = is_v ? a.v_scales : a.k_scales;
+                    *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page * sc.sb + h * sc.sh + slot * 4) = pair;
+                }
+            }
+        }
+    }
+    // The counts.  Where they are updated in place, only the last block to finish does it: all others have read them.
+    if (a.n_rows_out != a.n_rows) {
+        if (!lead) return;
+        for (int h = tid; h < H; h += kThreads) {
+            const NewRows x = new_rows(a, b, h, true);
+            a.n_rows_out[b * H + h] = x.first + x.stored;
+        }
+        return;
+    }
+    __shared__ int last;
+    __syncthreads();
+    if (tid == 0) {
+        __threadfence();
+        last = atomicAdd(a.status + kCountWord, 1) == int(gridDim.x * gridDim.y) - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    for (int u = tid; u < a.batch * H; u += kThreads) {
+        const NewRows x = new_rows(a, u / H, u % H, true);
+        a.n_rows_out[u] = x.first + x.stored;
+    }
+    if (tid == 0) a.status[kCountWord] = 0;
+}
+
+// Rows [first, n_rows) of every unit as numbers again: base + scale code, rounded once to fp32 and, for bf16, once more.  Block
+// (u, .) takes kLoadRows rows of a unit at a time; a lane has sixteen values (8 bytes of codes), a row d / 16 lanes, four rows
+// in flight per lane.  Bound by memory, above all by what it writes.
+constexpr int kLoadDepth = 4;
+template <bool kF32, int kLanes>
+__global__ void __launch_bounds__(kThreads) load_rows_kernel(const LoadRowsArgs a) {
+    constexpr int kGroups = kThreads / kLanes;           // rows per step
+    const int u = blockIdx.x, b = u / a.n_kv_heads, h = u - b * a.n_kv_heads;
+    const int L = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+    int rows = a.n_rows[u], first = a.first ? a.first[u] : 0, bad = 0;
+    if (rows < 0 || rows > a.capacity) { bad |= CSP_DEV_BAD_LEN; rows = rows < 0 ? 0 : a.capacity; }
+    if (first < 0) { bad |= CSP_DEV_BAD_LEN; first = 0; }
+    int count = first < rows ? rows - first : 0;
+    if (count > a.max_rows) { bad |= CSP_DEV_CAPACITY; count = a.max_rows; }
+    if (bad && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(a.status, bad);
+    const int32_t* const table = a.page_table + int64_t(b) * a.max_pages;
+#pragma unroll 1
+    for (int which = 0; which < (a.v.ptr ? 2 : 1); ++which) {
+        const RowTensor& from = which ? a.v : a.k;
+        const RowTensor& sc = which ? a.v_scales : a.k_scales;
+        const RowTensor& to = which ? a.v_out : a.k_out;
+        const char* const codes = static_cast<const char*>(from.ptr) + h * from.sh;
+        const char* const scales = static_cast<const char*>(sc.ptr) + h * sc.sh;
+        char* const out = static_cast<char*>(to.ptr) + b * to.sb + h * to.sh;
+        for (int i0 = blockIdx.y * kGroups * kLoadDepth; i0 < count; i0 += int(gridDim.y) * kGroups * kLoadDepth) {
+            uint2 w[kLoadDepth];
+            uint32_t pair[kLoadDepth];
+#pragma unroll
+            for (int j = 0; j < kLoadDepth; ++j) {
+                const int i = i0 + j * kGroups + group;
+                w[j] = make_uint2(0u, 0u);
+                pair[j] = 0u;
+                if (i >= count) continue;
+                const uint32_t t = uint32_t(first + i), slot = t % uint32_t(a.page_rows);
+                const int page = table[t / uint32_t(a.page_rows)];
+                if (page < 0 || page >= a.n_pages) {     // reads as zeros
+                    if (which == 0 && L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
+                    continue;
+                }
+                w[j] = __ldcs(reinterpret_cast<const uint2*>(codes + page * from.sb + slot * from.st) + L);
+                pair[j] = *reinterpret_cast<const uint32_t*>(scales + page * sc.sb + slot * 4);
+            }
+#pragma unroll
+            for (int j = 0; j < kLoadDepth; ++j) {
+                const int i = i0 + j * kGroups + group;
+                if (i >= count) continue;
+                const float scale = bf16_lo(pair[j]), base = bf16_hi(pair[j]);
+                float f[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const uint32_t c = ((k < 8 ? w[j].x : w[j].y) >> (4 * (k & 7))) & 15u;
+                    f[k] = fmaf(scale, __uint_as_float(0x4b000000u | c) - 8388608.f, base);      // (2^23 + c) - 2^23
+                }
+                char* const row = out + i * to.st;
+                const Eight<kF32> r0 = narrow<kF32>(f), r1 = narrow<kF32>(f + 8);
+                store_eight<kF32>(row, 2 * L, r0);
+                store_eight<kF32>(row, 2 * L + 1, r1);
+            }
+        }
+    }
+}
+
+inline csp_status launched() { return cudaGetLastError() == cudaSuccess ? CSP_OK : CSP_ERR_CUDA; }
+
+template <bool kF32, bool kFour, int kLanes>
+csp_status append_rows(const AppendRowsArgs& a, dim3 grid, cudaStream_t s) {
+    append_rows_kernel<kF32, kFour, kLanes><<<grid, kThreads, 0, s>>>(a);
+    return launched();
+}
+
+}  // namespace
+
+csp_status launch_append_rows(AppendRowsArgs a, int head_dim, bool f32, bool four, cudaStream_t s) {
+    if (a.batch == 0) return CSP_OK;
+    const int groups = kThreads / (head_dim / 16), slots = 2 * a.n_kv_heads + a.n_q_heads;
+    // Few tokens: the lane groups of a block spread over the heads; from eight on, eight tokens share a block and every group goes
+    // over some of the heads with one set of cosines.
+    a.log_tokens = 0;
+    while (a.log_tokens < 3 && (2 << a.log_tokens) <= a.max_new && (2 << a.log_tokens) <= groups) ++a.log_tokens;
+    const int tiles = a.max_new > 0 ? (a.max_new + (1 << a.log_tokens) - 1) >> a.log_tokens : 1;
+    const int most = (1 << 30) / a.batch;
+    a.token_tiles = tiles < most ? tiles : most;
+    const int step = groups >> a.log_tokens;             // heads at a time
+    const int64_t blocks = int64_t(a.token_tiles) * a.batch;
+    // as many pieces of the heads as it takes to give every SM four blocks
+    int pieces = (slots + step - 1) / step;
+    const int64_t want = (4 * int64_t(sm_count()) + blocks - 1) / blocks;
+    if (pieces > want) pieces = int(want);
+    a.slots_per_block = ((slots + step - 1) / step + pieces - 1) / pieces * step;
+    pieces = (slots + a.slots_per_block - 1) / a.slots_per_block;
+    const dim3 grid{unsigned(blocks), unsigned(pieces)};
+    if (four) return head_dim == 64 ? append_rows<false, true, 4>(a, grid, s) : append_rows<false, true, 8>(a, grid, s);
+    if (f32) return head_dim == 32 ? append_rows<true, false, 2>(a, grid, s) : head_dim == 64 ? append_rows<true, false, 4>(a, grid, s) : append_rows<true, false, 8>(a, grid, s);
+    return head_dim == 64 ? append_rows<false, false, 4>(a, grid, s) : head_dim == 128 ? append_rows<false, false, 8>(a, grid, s) : append_rows<false, false, 16>(a, grid, s);
+}
+
+csp_status launch_load_rows(const LoadRowsArgs& a, int head_dim, bool f32, cudaStream_t s) {
+    if (a.units == 0 || a.max_rows == 0) return CSP_OK;
+    const int rows = kThreads / (head_dim / 16) * kLoadDepth;
+    const int64_t tiles = (int64_t(a.max_rows < a.capacity ? a.max_rows : a.capacity) + rows - 1) / rows;
+    if (tiles == 0) return CSP_OK;
+    const dim3 grid{unsigned(a.units), unsigned(tiles < 65535 ? tiles : 65535)};
+    if (head_dim == 64) f32 ? load_rows_kernel<true, 4><<<grid, kThreads, 0, s>>>(a) : load_rows_kernel<false, 4><<<grid, kThreads, 0, s>>>(a);
+    else f32 ? load_rows_kernel<true, 8><<<grid, kThreads, 0, s>>>(a) : load_rows_kernel<false, 8><<<grid, kThreads, 0, s>>>(a);
+    return launched();
+}
+
+}  // namespace csp

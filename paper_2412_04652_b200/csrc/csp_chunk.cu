@@ -831,17 +831,6 @@ ChunkPlan chunk_plan(const csp_params& p, int max_new) {
     return pl;
 }
 
-struct PartialLayout { size_t parts, ml, o, total; };
-PartialLayout partial_layout(const csp_params& p, const ChunkPlan& pl) {
-    PartialLayout x;
-    const size_t rows = size_t(2) * pl.grid * pl.row_slots;
-    x.parts = kStatusBytes;
-    x.ml = x.parts + round256(size_t(pl.grid) * sizeof(ChunkParts));
-    x.o = x.ml + round256(rows * sizeof(float2));
-    x.total = x.o + round256(rows * size_t(p.head_dim) * 4);
-    return x;
-}
-
 template <int NH, bool kCap, bool kBias, bool kDoc>
 csp_status launch_variant(const ChunkArgs& a, const ChunkPlan& pl, const CUtensorMap& tq, const CUtensorMap& tk,
                           const CUtensorMap& tv, ChunkParts* parts, float* partial, float2* ml, cudaStream_t s) {
@@ -871,6 +860,23 @@ csp_status launch_nh(const ChunkArgs& a, const ChunkPlan& pl, const CUtensorMap&
 }
 
 }  // namespace
+
+PartialLayout partial_layout(const csp_params& p, const ChunkPlan& pl) {
+    PartialLayout x;
+    const size_t rows = size_t(2) * pl.grid * pl.row_slots;
+    x.parts = kStatusBytes;
+    x.ml = x.parts + round256(size_t(pl.grid) * sizeof(ChunkParts));
+    x.o = x.ml + round256(rows * sizeof(float2));
+    x.total = x.o + round256(rows * size_t(p.head_dim) * 4);
+    return x;
+}
+
+csp_status launch_chunk_join(const csp_params& p, const ChunkArgs& a, const ChunkPlan& pl, bool few, ChunkParts* parts,
+                             float* partial, float2* ml, cudaStream_t s) {
+    if (p.head_dim == 64) (few ? join_parts<64, 8, 8> : join_parts<64, 16, 2>)(a, pl, parts, partial, ml, s);
+    else (few ? join_parts<128, 8, 8> : join_parts<128, 16, 2>)(a, pl, parts, partial, ml, s);
+    return cudaGetLastError() == cudaSuccess ? CSP_OK : CSP_ERR_CUDA;
+}
 
 size_t chunk_workspace_bytes(const csp_params& p, int max_new) {
     if (p.dtype != CSP_BF16 || (p.head_dim != 64 && p.head_dim != 128)) return 0;
@@ -914,10 +920,7 @@ csp_status launch_chunk_attn(const csp_params& p, const ChunkArgs& a, const csp_
     }
     // nothing is cut by a single block, and where two parts of min_tiles are more than a cache has
     if (st != CSP_OK || pl.grid == 1 || p.out_capacity <= (2 * pl.min_tiles - 1) * pl.key_tile) return st;
-    const bool few = pl.row_slots <= kFewRows;
-    if (p.head_dim == 64) (few ? join_parts<64, 8, 8> : join_parts<64, 16, 2>)(a, pl, parts, partial, ml, s);
-    else (few ? join_parts<128, 8, 8> : join_parts<128, 16, 2>)(a, pl, parts, partial, ml, s);
-    return cudaGetLastError() == cudaSuccess ? CSP_OK : CSP_ERR_CUDA;
+    return launch_chunk_join(p, a, pl, pl.row_slots <= kFewRows, parts, partial, ml, s);
 }
 
 }  // namespace csp

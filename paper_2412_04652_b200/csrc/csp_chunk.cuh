@@ -22,6 +22,13 @@ struct ChunkPlan {                                       // sizes that host and 
 // the one it goes on with ends with it.
 struct ChunkParts { int32_t first, last; };
 
+// where a workspace keeps the partial results
+struct PartialLayout { size_t parts, ml, o, total; };
+PartialLayout partial_layout(const csp_params& p, const ChunkPlan& pl);
+// joins them; few: up to sixteen rows per item
+csp_status launch_chunk_join(const csp_params& p, const ChunkArgs& a, const ChunkPlan& pl, bool few, ChunkParts* parts,
+                             float* partial, float2* ml, cudaStream_t s);
+
 csp_status launch_chunk_few(const csp_params& p, const ChunkArgs& a, const ChunkPlan& pl, const csp_tensor& q,
                             const CUtensorMap& tk, const CUtensorMap& tv, ChunkParts* parts, float* partial, float2* ml,
                             cudaStream_t s);

@@ -243,6 +243,46 @@ struct AppendArgs {
     const int32_t* page_table; int32_t max_pages, page_rows, n_pages;
     int32_t* status;
 };
+// a tensor of rows as the append kernels take it: strides in bytes
+struct RowTensor { void* ptr; int64_t sb, sh, st; };
+struct RopeArgs {
+    const float* cos_sin; int64_t row_stride;        // cosines of dim / 2 angles, then their sines, per row
+    int32_t table_rows, dim;                         // dim 0: nothing is rotated
+    bool interleaved;
+    const int32_t* positions; int64_t pos_sb;        // null: a row's own number
+};
+// new rows for pages in bf16 or fp32, or (with scales) in 4 bits (csp_append.cu)
+struct AppendRowsArgs {
+    RowTensor k_new, v_new, q, q_out, k, v, k_scales, v_scales;
+    RopeArgs rope;
+    const int32_t* n_new; bool n_new_per_head;
+    const int32_t* n_rows; int32_t* n_rows_out;
+    int32_t batch, n_kv_heads, n_q_heads, group, max_new, capacity;   // n_q_heads 0: no queries
+    const int32_t* page_table; int32_t max_pages, page_rows, n_pages;
+    int32_t* status;
+    // chosen by the launcher: tokens per block (base-2 logarithm), blocks along the tokens of a sequence, heads per block
+    int32_t log_tokens, token_tiles, slots_per_block;
+};
+struct LoadRowsArgs {
+    RowTensor k, v, k_scales, v_scales, k_out, v_out;    // v.ptr null: K only
+    const int32_t* first; const int32_t* n_rows;
+    int32_t units, n_kv_heads, max_rows, capacity;
+    const int32_t* page_table; int32_t max_pages, page_rows, n_pages;
+    int32_t* status;
+};
+csp_status launch_append_rows(AppendRowsArgs a, int head_dim, bool f32, bool four, cudaStream_t s);
+csp_status launch_load_rows(const LoadRowsArgs& a, int head_dim, bool f32, cudaStream_t s);
+
+// a cache in 4 bits as the attention kernels take it: rows of a head in a page lie one behind the other (strides in bytes)
+struct Q4Args {
+    const uint8_t* k; int64_t k_sb, k_sh;
+    const uint8_t* v; int64_t v_sb, v_sh;
+    const uint8_t* ks; int64_t ks_sb, ks_sh;
+    const uint8_t* vs; int64_t vs_sb, vs_sh;
+};
+size_t chunk_q4_workspace_bytes(const csp_params& p, int max_new);   // 0: shapes that launch_chunk_q4 does not take
+csp_status launch_chunk_q4(const csp_params& p, const ChunkArgs& a, const csp_tensor& q, const Q4Args& c, void* ws, cudaStream_t s);
+
 size_t pages_workspace_bytes(const csp_page_state& s);
 PageArgs page_args(const csp_page_state& s, void* ws);
 csp_status launch_pages_fork(const PageArgs& a, const int32_t* src, const int32_t* dst, int n, cudaStream_t s);
