@@ -17,8 +17,8 @@
 // of two that follows the largest scale seen as the softmax's reference follows the largest logit.
 //
 // Organisation: one CTA per SM works off an equal share of all 64-key tiles.
-//   producer     streams tiles (codes and scales of K and V) with bulk copies into rings, one ring for each group of two
-//                warps, and the items' queries and descriptions into a ring of their own
+//   producers    two warps stream tiles (codes and scales of K and V) with bulk copies into rings, one ring for each group of
+//                two warps, and the items' queries and descriptions into a ring of their own
 //   groups       take the tiles in turn, 32 keys per warp; at the end of an item every warp leaves its sums in shared memory
 //   finisher     joins them in a fixed order
 #include <limits.h>
@@ -67,7 +67,6 @@ struct Q4Shape {
     static constexpr int NG = RH == 1 ? 8 : 4;           // groups of two warps
     static constexpr int NW = 2 * NG;
     static constexpr int kSlots = (RH == 1 ? 2 : 4) * (NH == 1 ? 2 : 1);               // tiles in flight per group
-    static constexpr int kEntries = kSlots + 2;
     static constexpr uint32_t kCodeBytes = kQ4Tile * D / 2, kScaleBytes = kQ4Tile * 4; // of K or of V
     static constexpr uint32_t kSlotBytes = 2 * kCodeBytes + 2 * kScaleBytes;
     static constexpr uint32_t kQRow = D * 2 + 16;                                      // padded: rows start in other banks
@@ -76,13 +75,13 @@ struct Q4Shape {
     static constexpr uint32_t kQ = kMeta + NG * kSlots * kQ4Tile * 8;                  // per item: R query rows,
     static constexpr uint32_t kRowConst = kQ + kItems * R * kQRow;                     //   [R] (factor of the logits, sum of q),
     static constexpr uint32_t kInfo = kRowConst + kItems * R * 8;                      //   words; then the item to finish
-    static constexpr uint32_t kEntry = kInfo + (kItems + 1) * kItemWords * 4;          // [group][entry] int2
-    static constexpr uint32_t kBars = kEntry + NG * kEntries * 8;
-    static constexpr int kBarCount = NG * (2 * kEntries + kSlots) + kItems + 2;
+    static constexpr uint32_t kEntry = kInfo + (kItems + 1) * kItemWords * 4;          // [group][slot] int2: tile, flags
+    static constexpr uint32_t kBars = kEntry + NG * kSlots * 8;
+    static constexpr int kBarCount = 2 * NG * kSlots + 2 * kItems + 2;
     static constexpr uint32_t kFills = kBars + kBarCount * 8;
     static constexpr uint32_t kMisc = kFills + NG * 4;
     static constexpr uint32_t kTotal = kMisc + 16;
-    static constexpr int kThreads = 32 * (NW + 2);
+    static constexpr int kThreads = 32 * (NW + 3);
 };
 
 template <int NH, int RH>
@@ -90,7 +89,7 @@ __global__ void __launch_bounds__(Q4Shape<NH, RH>::kThreads, 1)
 chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, const Q4Args cache, ChunkParts* const parts,
                     float* const partial, float2* const partial_ml) {
     using Shape = Q4Shape<NH, RH>;
-    constexpr int D = Shape::D, R = Shape::R, NG = Shape::NG, NW = Shape::NW, NST = Shape::kSlots, NE = Shape::kEntries;
+    constexpr int D = Shape::D, R = Shape::R, NG = Shape::NG, NW = Shape::NW, NST = Shape::kSlots;
     constexpr int KW = D / 32;                           // words of a key that a lane has in the first product
     constexpr int VW = D / 64;                           // and in the second one
     constexpr int MT = D / 16;                           // 16-dimension tiles of the output
@@ -105,16 +104,16 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     int2* const entry = reinterpret_cast<int2*>(base_ptr + Shape::kEntry);
     uint32_t* const fills = reinterpret_cast<uint32_t*>(base_ptr + Shape::kFills);
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(base_ptr + Shape::kMisc);
-    const uint32_t ent_full = base + Shape::kBars, ent_empty = ent_full + 8 * NG * NE, slot_empty = ent_empty + 8 * NG * NE;
-    const uint32_t item_empty = slot_empty + 8 * NG * NST, done_bar = item_empty + 8 * kItems, read_bar = done_bar + 8;
+    const uint32_t full_bar = base + Shape::kBars, empty_bar = full_bar + 8 * NG * NST;
+    const uint32_t item_full = empty_bar + 8 * NG * NST, item_empty = item_full + 8 * kItems;
+    const uint32_t done_bar = item_empty + 8 * kItems, read_bar = done_bar + 8;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.group;
     const ModArgs& md = a.mods;
     if (tid == 0) {
         *abort_flag = 0;
-        for (int i = 0; i < NG * NE; ++i) { mbar_init(ent_full + 8 * i, 1); mbar_init(ent_empty + 8 * i, 2); }
-        for (int i = 0; i < NG * NST; ++i) mbar_init(slot_empty + 8 * i, 2);
-        for (int i = 0; i < kItems; ++i) mbar_init(item_empty + 8 * i, NW);
+        for (int i = 0; i < NG * NST; ++i) { mbar_init(full_bar + 8 * i, 1); mbar_init(empty_bar + 8 * i, 2); }
+        for (int i = 0; i < kItems; ++i) { mbar_init(item_full + 8 * i, 1); mbar_init(item_empty + 8 * i, NW); }
         mbar_init(done_bar, NW);
         mbar_init(read_bar, 1);
         for (int g = 0; g < NG; ++g) fills[g] = 0;
@@ -123,31 +122,35 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     }
     const Share share = find_share<Shape::kThreads>(a, pl, reinterpret_cast<int*>(merge));      // (synchronises)
 
-    if (warp == NW) {
-        // =============================== producer ===============================
+    if (warp >= NW + 1) {
+        // =============================== producers ===============================
+        // Both go over the same items; tile n of the block goes to group n % NG, and producer n & 1 brings it.
+        const int me = warp - (NW + 1);
         bool ok = true;
-        uint32_t n_tile = 0, n_item = 0;
-        uint32_t ents = 0, slots = 0;                    // lane g: entries and tiles that group g has been given
+        uint32_t n_tile = 0, n_item = 0;                 // tiles of all items before the current one; items
+        // How many slots each group has been given, in 8 bits per group of this producer's.  Beyond 4 NST it goes on at 2 NST:
+        // what tells the phases is the number modulo 2 NST.
+        static_assert(NG <= 8 && 4 * NST < 256 && (NST & (NST - 1)) == 0, "counts in 8 bits");
+        uint32_t given = 0;
+        auto count_of = [&](int g) { return (given >> (8 * (g >> 1))) & 255u; };
+        auto give = [&](int g) {
+            const uint32_t n = count_of(g) + 1, sh = 8 * (g >> 1);
+            given = (given & ~(255u << sh)) | ((n == 4 * NST ? 2 * NST : n) << sh);
+        };
+        auto slot_of = [&](int g) { return uint32_t(g) * NST + count_of(g) % NST; };
+        auto phase_of = [&](int g) { return ((count_of(g) / NST) & 1u) ^ 1u; };
         auto wait = [&](uint32_t bar, uint32_t parity) {
             warp_wait(bar, parity, abort_flag);
             ok = ok && !warp_aborted(abort_flag);
         };
-        auto get = [&](uint32_t of_lane, int g) { return __shfl_sync(0xffffffffu, of_lane, g); };
-        // the next entry of group g, free; without data, or with a tile whose copies the caller issues
-        auto open = [&](int g, int tile, int flags) {
-            const uint32_t n = get(ents, g), e = g * NE + n % NE;
-            wait(ent_empty + 8 * e, ((n / NE) & 1u) ^ 1u);
-            if (lane == g) ++ents;
-            if (ok && lane == 0) entry[e] = make_int2(tile, flags);
-            return ent_full + 8 * e;
+        auto marker = [&](int g, int tile, int flags) {  // a slot without data
+            const uint32_t s = slot_of(g);
+            wait(empty_bar + 8 * s, phase_of(g));
+            if (!ok) return;
+            if (lane == 0) { entry[s] = make_int2(tile, flags); mbar_arrive(full_bar + 8 * s); }
+            give(g);
         };
-        auto marker = [&](int g, int tile, int flags) {
-            const uint32_t bar = open(g, tile, flags);
-            __syncwarp();
-            if (ok && lane == 0) mbar_arrive(bar);
-            if (!ok && lane == g) --ents;
-        };
-        if (lane == 0) parts[blockIdx.x] = ChunkParts{-1, 0};
+        if (me == 0 && lane == 0) parts[blockIdx.x] = ChunkParts{-1, 0};
         const uint32_t tiles_per_page = uint32_t(a.page_rows) / uint32_t(kQ4Tile);
         auto page_of = [&](int b, int tile) {            // the page of a tile that lies inside the cache
             return a.page_table[int64_t(b) * a.max_pages + uint32_t(tile) / tiles_per_page];
@@ -156,13 +159,15 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         constexpr int kQChunks = R * D / 8 / 32;
         uint4 next_q[kQChunks];
         PairRange next = {};
-        int next_page = 0;                               // lane l: page of the next item's tile l (of its first 32)
-        auto look_up = [&](int item) {                   // while the current item streams
+        int next_page = 0;                               // page of this producer's first tile of the next item
+        auto my_first = [&](int tile0, uint32_t n0) { return tile0 + int((n0 ^ uint32_t(me)) & 1u); };
+        auto look_up = [&](int item, uint32_t n0) {      // while the current item streams; n0: n_tile when it comes
             if (item > share.item1 || (item == share.item1 && share.tile1 == 0) || item >= pl.n_items) return;
             const int u = item / pl.n_pairs, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
             next = pair_range(a, pl, u, item - u * pl.n_pairs);
-            const int tile = (item == share.item0 ? share.tile0 : 0) + lane;
+            const int tile = my_first(item == share.item0 ? share.tile0 : 0, n0);
             if (next.count > 0 && tile < next.tiles) next_page = page_of(b, tile);
+            if (me) return;
             // the query rows: 16-byte chunk `lane + 32 j` of [row][d]; rows that are none are zeros
 #pragma unroll
             for (int j = 0; j < kQChunks; ++j) {
@@ -172,144 +177,190 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                                              : make_uint4(0, 0, 0, 0);
             }
         };
-        look_up(share.item0);
+        look_up(share.item0, 0);
         for (int item = share.item0; ok && item <= share.item1 && item < pl.n_items; ++item) {
             const int u = item / pl.n_pairs, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
             const PairRange x = next;
-            int pages = next_page;                       // lane l: the page of tile 32 j + l
             const int tile0 = item == share.item0 ? share.tile0 : 0, tile1 = item == share.item1 ? share.tile1 : x.tiles;
-            if (x.count <= 0 || (item == share.item1 && tile1 == 0)) { look_up(item + 1); continue; }
-            if (lane == 0) {
-                if (tile0 > 0) parts[blockIdx.x].last = tile1 == x.tiles;
-                else if (tile1 < x.tiles) parts[blockIdx.x].first = item;
-            }
+            if (x.count <= 0 || (item == share.item1 && tile1 == 0)) { look_up(item + 1, n_tile); continue; }
             const int32_t* const docs = md.documents ? md.documents + int64_t(b) * md.doc_sb + int64_t(h) * md.doc_sh : nullptr;
             const int32_t* const poss = md.slopes && md.positions ? md.positions + int64_t(b) * md.pos_sb + int64_t(h) * md.pos_sh : nullptr;
-            const bool meta = docs || md.slopes;
             // positions are staged relative to the last token's, so that near ones are exact in fp32
             const int row_last = max(x.row0 + x.count - 1, 0);
             const int pos_ref = md.slopes && x.rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
-            int doc_lo = INT_MAX, doc_hi = INT_MIN;
-            if (docs) {                                  // sixteen rows at most
-                const int r = x.row0 + lane;
-                if (lane < x.count && r >= 0) doc_lo = doc_hi = docs[r];
-                doc_lo = __reduce_min_sync(0xffffffffu, doc_lo);
-                doc_hi = __reduce_max_sync(0xffffffffu, doc_hi);
-            }
-            // ---- the item's description and queries, in halves and in the order of the codes
-            const uint32_t is = n_item % kItems;
-            wait(item_empty + 8 * is, ((n_item / kItems) & 1u) ^ 1u);
-            if (!ok) break;
-            ++n_item;
-            int32_t word = 0;
-            switch (lane) {
-                case kwItem: word = item; break;
-                case kwRows: word = x.rows; break;
-                case kwRow0: word = x.row0; break;
-                case kwCount: word = x.count; break;
-                case kwPrefix: word = x.prefix; break;
-                case kwPart: word = tile0 > 0 ? 2 * int(blockIdx.x) : tile1 < x.tiles ? 2 * int(blockIdx.x) + 1 : -1; break;
-                case kwPosRef: word = pos_ref; break;
-                case kwTok0: word = x.tok0; break;
-            }
-            if (lane < kItemWords) info[is * kItemWords + lane] = word;
-#pragma unroll
-            for (int j = 0; j < kQChunks; ++j) {
-                const int c = lane + 32 * j, m = c / kRowLanes;
-                const uint32_t w[4] = {next_q[j].x, next_q[j].y, next_q[j].z, next_q[j].w};
-                float f[8];
-                uint32_t top = 0;                        // bits of the row's largest magnitude
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    f[2 * k] = lo_bf16(w[k]); f[2 * k + 1] = hi_bf16(w[k]);
-                    top = max(top, max((w[k] << 16) & 0x7fffffffu, w[k] & 0x7fff0000u));
+            if (me == 0) {
+                // ---- the item's description and queries, in halves and in the order of the codes
+                if (lane == 0) {
+                    if (tile0 > 0) parts[blockIdx.x].last = tile1 == x.tiles;
+                    else if (tile1 < x.tiles) parts[blockIdx.x].first = item;
                 }
+                const uint32_t is = n_item % kItems;
+                wait(item_empty + 8 * is, ((n_item / kItems) & 1u) ^ 1u);
+                if (!ok) break;
+                int32_t word = 0;
+                switch (lane) {
+                    case kwItem: word = item; break;
+                    case kwRows: word = x.rows; break;
+                    case kwRow0: word = x.row0; break;
+                    case kwCount: word = x.count; break;
+                    case kwPrefix: word = x.prefix; break;
+                    case kwPart: word = tile0 > 0 ? 2 * int(blockIdx.x) : tile1 < x.tiles ? 2 * int(blockIdx.x) + 1 : -1; break;
+                    case kwPosRef: word = pos_ref; break;
+                    case kwTok0: word = x.tok0; break;
+                }
+                if (lane < kItemWords) info[is * kItemWords + lane] = word;
 #pragma unroll
-                for (int d = 1; d < kRowLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-                const uint32_t ex = top >> 23;           // 255: an infinity or NaN, the row is no number
-                const float down = ex == 255u ? 0.f : __uint_as_float((254u - ex) << 23);        // 2^-e (0: 2^127)
-                float sum = 0.f;
+                for (int j = 0; j < kQChunks; ++j) {
+                    const int c = lane + 32 * j, m = c / kRowLanes;
+                    const uint32_t w[4] = {next_q[j].x, next_q[j].y, next_q[j].z, next_q[j].w};
+                    float f[8];
+                    uint32_t top = 0;                    // bits of the row's largest magnitude
 #pragma unroll
-                for (int k = 0; k < 8; ++k) { f[k] *= down; sum += f[k]; }
+                    for (int k = 0; k < 4; ++k) {
+                        f[2 * k] = lo_bf16(w[k]); f[2 * k + 1] = hi_bf16(w[k]);
+                        top = max(top, max((w[k] << 16) & 0x7fffffffu, w[k] & 0x7fff0000u));
+                    }
 #pragma unroll
-                for (int d = 1; d < kRowLanes; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                const float up = ex == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(ex << 23);
-                *reinterpret_cast<uint4*>(base_ptr + Shape::kQ + (is * R + m) * Shape::kQRow + (c % kRowLanes) * 16) =
-                    make_uint4(pack_f16(16.f * f[0], 16.f * f[4]), pack_f16(f[1], f[5]), pack_f16(16.f * f[2], 16.f * f[6]), pack_f16(f[3], f[7]));
-                // logit = up 2^20 (scale S + base sum 2^-20), S the product with codes 2^-20
-                if (c % kRowLanes == 0) row_const[is * R + m] = make_float2(a.scale * kLog2e * 0x1p20f * up, sum * 0x1p-20f);
+                    for (int d = 1; d < kRowLanes; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    const uint32_t ex = top >> 23;       // 255: an infinity or NaN, the row is no number
+                    const float down = ex == 255u ? 0.f : __uint_as_float((254u - ex) << 23);        // 2^-e (0: 2^127)
+                    float sum = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) { f[k] *= down; sum += f[k]; }
+#pragma unroll
+                    for (int d = 1; d < kRowLanes; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                    const float up = ex == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(ex << 23);
+                    *reinterpret_cast<uint4*>(base_ptr + Shape::kQ + (is * R + m) * Shape::kQRow + (c % kRowLanes) * 16) =
+                        make_uint4(pack_f16(16.f * f[0], 16.f * f[4]), pack_f16(f[1], f[5]), pack_f16(16.f * f[2], 16.f * f[6]), pack_f16(f[3], f[7]));
+                    // logit = up 2^20 (scale S + base sum 2^-20), S the product with codes 2^-20
+                    if (c % kRowLanes == 0) row_const[is * R + m] = make_float2(a.scale * kLog2e * 0x1p20f * up, sum * 0x1p-20f);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(item_full + 8 * is);
+                ++n_item;
             }
-            __syncwarp();
-            look_up(item + 1);
             // ---- its tiles
             uint32_t ended = 0;                          // bit g: the group has been told that it has no more
-            int d_next[2] = {0, 0}, p_next[2] = {0, 0};
-            auto fetch_meta = [&](int tile) {            // documents and positions of one tile's keys, a tile ahead of their use
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int t = tile * kQ4Tile + lane + 32 * j;
-                    d_next[j] = docs && t < x.rows ? docs[t] : 0;
-                    p_next[j] = !md.slopes ? 0 : poss ? (t < x.rows ? poss[t] : pos_ref) : t;
-                }
+            const uint8_t* const k_from = cache.k + h * cache.k_sh, * const v_from = cache.v + h * cache.v_sh;
+            const uint8_t* const ks_from = cache.ks + h * cache.ks_sh, * const vs_from = cache.vs + h * cache.vs_sh;
+            auto load = [&](uint32_t s, int64_t page, uint32_t tile) {       // one thread
+                const int64_t row = int64_t(tile % tiles_per_page) * kQ4Tile;
+                const uint32_t bar = full_bar + 8 * s, to = base + s * Shape::kSlotBytes;
+                mbar_expect_tx(bar, Shape::kSlotBytes);
+                bulk_load(to, k_from + page * cache.k_sb + row * (D / 2), Shape::kCodeBytes, bar);
+                bulk_load(to + Shape::kCodeBytes, v_from + page * cache.v_sb + row * (D / 2), Shape::kCodeBytes, bar);
+                bulk_load(to + 2 * Shape::kCodeBytes, ks_from + page * cache.ks_sb + row * 4, Shape::kScaleBytes, bar);
+                bulk_load(to + 2 * Shape::kCodeBytes + Shape::kScaleBytes, vs_from + page * cache.vs_sb + row * 4, Shape::kScaleBytes, bar);
             };
-            if (meta && tile0 < tile1) fetch_meta(tile0);
-            for (int tile = tile0; tile < tile1 && ok; ++tile) {
-                if (tile > tile0 && ((tile - tile0) & 31) == 0) pages = tile + lane < tile1 ? page_of(b, tile + lane) : 0;
-                const int dd[2] = {d_next[0], d_next[1]}, pp[2] = {p_next[0], p_next[1]};
-                if (meta && tile + 1 < tile1) fetch_meta(tile + 1);
-                if (docs) {                              // a tile without any of the tokens' documents is skipped
-                    bool hit = false;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) hit |= tile * kQ4Tile + lane + 32 * j < x.kv_end[1] && dd[j] >= doc_lo && dd[j] <= doc_hi;
-                    if (!__any_sync(0xffffffffu, hit)) continue;
+            // a page outside the pool: rows of zeros, whatever their codes
+            auto blank = [&](uint32_t s, int from, int step) {
+                uint32_t* const sc = reinterpret_cast<uint32_t*>(base_ptr + s * Shape::kSlotBytes + 2 * Shape::kCodeBytes);
+                for (int j = from; j < 2 * kQ4Tile; j += step) sc[j] = 0u;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            };
+            const int first = my_first(tile0, n_tile);
+            if (!docs && !md.slopes) {
+                // Without positions and documents one lane does everything: at the full rate of HBM each producer has a tile to
+                // bring every 750 clocks, and a whole warp takes longer for the steps below.
+                const bool elected = elect_one();
+                if (elected) {
+                    int page = next_page;
+                    for (int tile = first; tile < tile1; tile += 2) {
+                        const int g = int((n_tile + uint32_t(tile - tile0)) % NG), now = page;
+                        if (tile + 2 < tile1) page = page_of(b, tile + 2);        // in time for the next tile
+                        const uint32_t s = slot_of(g);
+                        lean_wait(empty_bar + 8 * s, phase_of(g), abort_flag);
+                        if (*abort_flag) break;
+                        const bool last = tile + NG >= tile1;
+                        entry[s] = make_int2(tile, last ? kEndOfItem : 0);
+                        if (uint32_t(now) < uint32_t(a.n_pages)) {
+                            load(s, now, tile);
+                        } else {
+                            atomicOr(a.status, CSP_DEV_BAD_LEN);
+                            blank(s, 0, 1);
+                            mbar_arrive(full_bar + 8 * s);
+                        }
+                        give(g);
+                        if (last) ended |= 1u << g;
+                    }
                 }
-                const int g = int(n_tile++ % NG);
-                // (with documents nobody knows yet which tile is the last)
-                const bool last = !docs && tile + NG >= tile1;
-                if (last) ended |= 1u << g;
-                const uint32_t n = get(slots, g), s = g * NST + n % NST;
-                wait(slot_empty + 8 * s, ((n / NST) & 1u) ^ 1u);
-                const uint32_t bar = open(g, tile, last ? kEndOfItem : 0);
-                if (!ok) { if (lane == g) --ents; break; }
-                if (lane == g) ++slots;
-                const uint32_t dst = s * Shape::kSlotBytes;
-                if (meta) {
+                const uint32_t who = __ballot_sync(0xffffffffu, elected), from = __ffs(who) - 1;
+                given = __shfl_sync(0xffffffffu, given, from);
+                ended = __shfl_sync(0xffffffffu, ended, from);
+                ok = ok && !warp_aborted(abort_flag);
+                n_tile += tile1 > tile0 ? tile1 - tile0 : 0;
+                look_up(item + 1, n_tile);
+            } else {
+                int doc_lo = INT_MAX, doc_hi = INT_MIN;
+                if (docs) {                              // sixteen rows at most
+                    const int r = x.row0 + lane;
+                    if (lane < x.count && r >= 0) doc_lo = doc_hi = docs[r];
+                    doc_lo = __reduce_min_sync(0xffffffffu, doc_lo);
+                    doc_hi = __reduce_max_sync(0xffffffffu, doc_hi);
+                }
+                int d_next[2] = {0, 0}, p_next[2] = {0, 0}, page_next = 0;
+                auto fetch = [&](int tile) {             // a tile's page, documents and positions, one step ahead of their use
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int t = tile * kQ4Tile + lane + 32 * j;
+                        d_next[j] = docs && t < x.rows ? docs[t] : 0;
+                        p_next[j] = !md.slopes ? 0 : poss ? (t < x.rows ? poss[t] : pos_ref) : t;
+                    }
+                    page_next = page_of(b, tile);
+                };
+                // (with documents every tile is looked at, by both: who takes which depends on how many were skipped)
+                const int step = docs ? 1 : 2;
+                uint32_t n = n_tile;
+                int tile = docs ? tile0 : first;
+                if (tile < tile1) fetch(tile);
+                for (; tile < tile1 && ok; tile += step) {
+                    const int dd[2] = {d_next[0], d_next[1]}, pp[2] = {p_next[0], p_next[1]}, page = page_next;
+                    if (tile + step < tile1) fetch(tile + step);
+                    if (docs) {                          // a tile without any of the tokens' documents is skipped
+                        bool hit = false;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) hit |= tile * kQ4Tile + lane + 32 * j < x.kv_end[1] && dd[j] >= doc_lo && dd[j] <= doc_hi;
+                        if (!__any_sync(0xffffffffu, hit)) continue;
+                        if ((n++ & 1u) != uint32_t(me)) continue;
+                    }
+                    const int g = int((docs ? n - 1 : n_tile + uint32_t(tile - tile0)) % NG);
+                    // (with documents nobody knows yet which tile is the last)
+                    const bool last = !docs && tile + NG >= tile1;
+                    const uint32_t s = slot_of(g);
+                    wait(empty_bar + 8 * s, phase_of(g));
+                    if (!ok) break;
+                    if (last) ended |= 1u << g;
                     float* const mp = reinterpret_cast<float*>(base_ptr + Shape::kMeta + s * kQ4Tile * 8);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         mp[lane + 32 * j] = float(pp[j] - pos_ref);
                         reinterpret_cast<int32_t*>(mp)[kQ4Tile + lane + 32 * j] = dd[j];
                     }
-                }
-                const int page = __shfl_sync(0xffffffffu, pages, (tile - tile0) & 31);
-                if (page < 0 || page >= a.n_pages) {     // outside the pool: rows of zeros, whatever their codes
-                    uint32_t* const sc = reinterpret_cast<uint32_t*>(base_ptr + dst + 2 * Shape::kCodeBytes);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sc[lane + 32 * j] = 0u;
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    const bool there = uint32_t(page) < uint32_t(a.n_pages);
+                    if (!there) blank(s, lane, 32);
                     __syncwarp();
-                    if (lane == 0) { atomicOr(a.status, CSP_DEV_BAD_LEN); mbar_arrive(bar); }
-                    continue;
+                    if (elect_one()) {
+                        entry[s] = make_int2(tile, last ? kEndOfItem : 0);
+                        if (there) {
+                            load(s, page, tile);
+                        } else {
+                            atomicOr(a.status, CSP_DEV_BAD_LEN);
+                            mbar_arrive(full_bar + 8 * s);
+                        }
+                    }
+                    __syncwarp();
+                    give(g);
                 }
-                const int64_t row = int64_t(uint32_t(tile) % tiles_per_page) * kQ4Tile;
-                __syncwarp();
-                if (lane == 0) mbar_expect_tx(bar, Shape::kSlotBytes);
-                __syncwarp();
-                if (lane < 4) {                          // codes of K and V, scales of K and V
-                    const bool is_v = lane & 1, is_scale = lane & 2;
-                    const uint8_t* const from = is_scale ? (is_v ? cache.vs + page * cache.vs_sb + h * cache.vs_sh : cache.ks + page * cache.ks_sb + h * cache.ks_sh) + row * 4
-                                                         : (is_v ? cache.v + page * cache.v_sb + h * cache.v_sh : cache.k + page * cache.k_sb + h * cache.k_sh) + row * (D / 2);
-                    const uint32_t size = is_scale ? Shape::kScaleBytes : Shape::kCodeBytes;
-                    bulk_load(base + dst + (is_scale ? 2 * Shape::kCodeBytes : 0u) + (is_v ? size : 0u), from, size, bar);
-                }
-                __syncwarp();
+                n_tile = docs ? n : n_tile + (tile1 > tile0 ? tile1 - tile0 : 0);
+                look_up(item + 1, n_tile);
             }
-            for (int g = 0; g < NG && ok; ++g)
+            for (int g = me; g < NG && ok; g += 2)
                 if (!(ended >> g & 1u)) marker(g, -1, kEndOfItem);
         }
-        for (int g = 0; g < NG && ok; ++g) marker(g, -2, 0);           // no more items
-        if (lane < NG) fills[lane] = ents;
-    } else if (warp == NW + 1) {
+        for (int g = me; g < NG && ok; g += 2) marker(g, -2, 0);       // no more items
+        if (lane == 0)
+            for (int g = me; g < NG; g += 2) fills[g] = count_of(g);
+    } else if (warp == NW) {
         // =============================== finisher ===============================
         for (uint32_t n = 0;; ++n) {
             warp_wait(done_bar, n & 1u, abort_flag);
@@ -374,7 +425,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         const bool capped = md.softcap > 0.f;
         // capped: x = c tanh(o / c) = c - 2 c / (1 + e^{2 o / c}), all in the base-2 domain
         const float cap2 = md.softcap * kLog2e, cap_in = capped ? 2.f / md.softcap : 0.f;
-        uint32_t n_ent = 0, n_slot = 0, n_item = 0;
+        uint32_t it = 0, n_item = 0;
         bool fresh = true;
         int rows = 0, live_rows = 0, lim_all = 0;
         uint32_t qb[RH][2 * KW][2];
@@ -383,14 +434,12 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         int lim[RH][2], q_doc[RH][2];
         float v_ref = kTiny, v_inv = 1.f / kTiny;        // power of two that the scales of V are relative to
         for (;;) {
-            const uint32_t e = group * NE + n_ent % NE;
-            warp_wait(ent_full + 8 * e, (n_ent / NE) & 1u, abort_flag);
+            const uint32_t s = group * NST + it % NST;
+            warp_wait(full_bar + 8 * s, (it / NST) & 1u, abort_flag);
             if (warp_aborted(abort_flag)) break;
-            ++n_ent;
-            const int2 en = entry[e];
+            ++it;
+            const int2 en = entry[s];
             const int tile = en.x;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(ent_empty + 8 * e);
             if (tile == -2) {
                 if (n_item > 0) warp_wait(read_bar, (n_item - 1u) & 1u, abort_flag);
                 if (warp == 0 && lane == 0) finish[kwItem] = -1;
@@ -402,6 +451,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
             const int32_t* const in = info + is * kItemWords;
             if (fresh) {
                 fresh = false;
+                warp_wait(item_full + 8 * is, (n_item / kItems) & 1u, abort_flag);
                 rows = in[kwRows];
                 const int item = in[kwItem], row0 = in[kwRow0], count = in[kwCount], u = item / pl.n_pairs, b = u / a.n_kv_heads, h = u % a.n_kv_heads;
                 live_rows = count * G;
@@ -440,8 +490,6 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                 v_inv = 1.f / kTiny;
             }
             if (tile >= 0) {
-                const uint32_t s = group * NST + n_slot % NST;
-                ++n_slot;
                 const uint8_t* const k_s = base_ptr + s * Shape::kSlotBytes + wi * 32 * (D / 2);
                 const uint8_t* const v_s = k_s + Shape::kCodeBytes;
                 const uint32_t* const ks_s = reinterpret_cast<const uint32_t*>(base_ptr + s * Shape::kSlotBytes + 2 * Shape::kCodeBytes) + wi * 32;
@@ -608,9 +656,9 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                             }
                         }
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(slot_empty + 8 * s);
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty_bar + 8 * s);
             if (!(en.y & kEndOfItem)) continue;
             // ---- end of the item: this warp's rows to shared memory, once the finisher has read the previous ones
             if (n_item > 0) warp_wait(read_bar, (n_item - 1u) & 1u, abort_flag);
@@ -644,7 +692,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     __syncthreads();
     if (*abort_flag && tid == 0) {
         atomicOr(a.status, CSP_DEV_TIMEOUT);
-        for (int g = 0; g < NG; ++g) drain_ring(ent_full + 8 * NE * g, fills[g], NE);
+        for (int g = 0; g < NG; ++g) drain_ring(full_bar + 8 * NST * g, fills[g], NST);
     }
 }
 
