@@ -51,20 +51,25 @@ struct PairRange {
     int kv_end[2];                                       // keys that row tile 0 / the whole pair can see: [0, kv_end)
     int tiles;
 };
-__device__ __forceinline__ PairRange pair_range(const ChunkArgs& a, const ChunkPlan& pl, int u, int pair) {
+// (rows, tokens and prefix as they stand in memory)
+__device__ __forceinline__ PairRange pair_range_of(const ChunkArgs& a, const ChunkPlan& pl, int rows, int n_new, int prefix, int pair) {
     PairRange x;
-    const int b = u / a.n_kv_heads, h = u % a.n_kv_heads;
-    x.rows = min(max(a.n_rows[u], 0), a.capacity);
-    x.n_new = a.n_new ? min(max(a.n_new[b], 0), a.max_new) : a.max_new;
+    x.rows = min(max(rows, 0), a.capacity);
+    x.n_new = min(max(n_new, 0), a.max_new);
     x.tok0 = pair * 2 * pl.tok_tile;
     x.count = min(x.n_new - x.tok0, 2 * pl.tok_tile);
     x.row0 = x.rows - x.n_new + x.tok0;
-    x.prefix = a.mods.prefix ? min(max(a.mods.prefix[int64_t(b) * a.mods.prefix_sb + int64_t(h) * a.mods.prefix_sh], 0), x.rows) : 0;
+    x.prefix = min(max(prefix, 0), x.rows);
     const int last0 = x.row0 + min(x.count, pl.tok_tile) - 1, last1 = x.row0 + x.count - 1;
     x.kv_end[0] = last0 < 0 ? 0 : max(last0 + 1, x.prefix);
     x.kv_end[1] = last1 < 0 ? 0 : max(last1 + 1, x.prefix);
     x.tiles = (x.kv_end[1] + pl.key_tile - 1) / pl.key_tile;
     return x;
+}
+__device__ __forceinline__ PairRange pair_range(const ChunkArgs& a, const ChunkPlan& pl, int u, int pair) {
+    const int b = u / a.n_kv_heads, h = u % a.n_kv_heads;
+    return pair_range_of(a, pl, a.n_rows[u], a.n_new ? a.n_new[b] : a.max_new,
+                         a.mods.prefix ? a.mods.prefix[int64_t(b) * a.mods.prefix_sb + int64_t(h) * a.mods.prefix_sh] : 0, pair);
 }
 
 // The resident blocks share the work evenly, whatever the lengths are: laid end to end, the items (a pair of row tiles of one
