@@ -10,18 +10,23 @@
 // Keys are the M of the warp-level products and the query rows the N, so that eight rows cost one product where rows as M would
 // pad them to sixteen:  S^T = K Q^T,  O^T = V^T P^T.  The transposed fragments fit each other up to one 8 x 8 transposition
 // per eight keys and rows (movmatrix).  In the first product a lane takes 16 bytes of each of its keys, in whatever order the
-// dimensions come (the query is laid out alike), in the second one 8 bytes, i.e. sixteen dimensions of four keys.
+// dimensions come: the query is laid out alike.  For the second one the rows of V are transposed as 16-bit pieces of four codes on
+// their way into registers.
 //
 // Queries are scaled by a power of two, row by row, so that their largest value lies in [1, 2): a half holds every bf16
 // value exactly from there down to 2^-14 of it.  A weight times its row's scale is rounded to a half (11 bits), relative to a power
 // of two that follows the largest scale seen as the softmax's reference follows the largest logit.
+// (Codes of K as e4m3 bytes, which four zeros and a code are as well, take half of the ANDs, but the compiler makes halves of
+// them before it multiplies: 650 instructions per tile of 32 keys instead of 510.)
 //
 // Organisation: one CTA per SM works off an equal share of all 32-key tiles, and inside it every warp an equal share of that,
-// tile after tile: no warp waits for another one before the end.  A warp has a ring of its own that it refills itself with bulk
-// copies as soon as it has read a slot.  An item (up to sixteen query rows of a unit) that lies in one warp's share is finished by
+// tile after tile: no warp waits for another one before the end.  A warp has a ring of its own that it refills itself as soon as it
+// has read a slot.  An item (up to sixteen query rows of a unit) that lies in one warp's share is finished by
 // it; of one that is cut the pieces stay in shared memory until all warps are done and are joined then, in order; what
 // goes on in another CTA is left as a partial result for the joining kernel.
+#include <cuda_fp16.h>
 #include <limits.h>
+#include <type_traits>
 
 #include "csp_chunk.cuh"
 
@@ -50,9 +55,13 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+__device__ __forceinline__ void ldsm_x4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ float fmax3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 // four bytes of global memory into shared memory, zeros where there is nothing
 __device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src, bool there) {
@@ -69,15 +78,14 @@ struct Q4Shape {
     static constexpr uint32_t kCodeBytes = kQ4Tile * D / 2, kScaleBytes = kQ4Tile * 4; // of K or of V
     static constexpr uint32_t kLoadBytes = 2 * kCodeBytes + 2 * kScaleBytes;
     static constexpr uint32_t kSlotBytes = kLoadBytes + 2 * kQ4Tile * 4;               // then positions and documents
-    static constexpr uint32_t kPieceBytes = R * (D + 2) * 4;                           // [R][D + 2] floats: sums, reference, sum of weights
+    static constexpr int kPieceRow = D + 4;                                            // floats: sums, reference, sum of weights
+    static constexpr uint32_t kPieceBytes = R * kPieceRow * 4;
     static constexpr uint32_t kFront = kWarps * kSlots * kSlotBytes;                   // [warp]: the piece that a warp begins with
-    static constexpr uint32_t kNotes = kFront + kWarps * kPieceBytes;                  // [warp] int4: see Notes
-    static constexpr uint32_t kEntry = kNotes + kWarps * 16;                           // [warp][slot] int2: segment, tile
-    static constexpr uint32_t kBars = kEntry + kWarps * kSlots * 8;
-    static constexpr uint32_t kFills = kBars + kWarps * kSlots * 8;
-    static constexpr uint32_t kScratch = kFills + kWarps * 4;                          // of find_share
-    static constexpr uint32_t kMisc = kScratch + 68 * 4;
-    static constexpr uint32_t kTotal = kMisc + 16;
+    static constexpr uint32_t kNotes = kFront + kWarps * kPieceBytes;                  // [warp]
+    static constexpr uint32_t kTable = kNotes + kWarps * 16;                           // [warp][R] RowNote
+    static constexpr uint32_t kDesk = kTable + kWarps * R * 16;                        // [warp] two Segments: loaded, computed
+    static constexpr uint32_t kScratch = kDesk + kWarps * 128;                         // of find_share
+    static constexpr uint32_t kTotal = kScratch + 68 * 4;
     static constexpr int kThreads = 32 * kWarps;
     static_assert(kSlots * kSlotBytes >= kPieceBytes, "the piece that a warp ends with goes into its ring");
 };
@@ -127,8 +135,13 @@ __device__ __forceinline__ WarpShare warp_share(const ChunkArgs& a, const ChunkP
 // What a warp says of its pieces: the item that it went on with (-1: none) and whether that ended with it, the item that it began
 // and did not end.
 struct Notes { int front, front_ends, back, unused; };
+// What a warp has of one item: its tiles [lo, hi).
+struct Segment { int item, b, h, lo, hi; PairRange x; };
+static_assert(sizeof(Segment) <= 64, "two of them in 128 bytes");
+// A query row's last visible key, document, position and slope.
+struct RowNote { int lim, doc; float pos, slope2; };
 
-template <int NH, int RH>
+template <int NH, int RH, bool kMods>                   // kMods: a cap, a bias or documents
 __global__ void __launch_bounds__(Q4Shape<NH, RH>::kThreads, 1)
 chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, const Q4Args cache, ChunkParts* const parts,
                     float* const partial, float2* const partial_ml) {
@@ -142,35 +155,19 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     const uint32_t base = (smem_u32(smem_raw) + 127u) & ~127u;
     uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
     Notes* const notes = reinterpret_cast<Notes*>(base_ptr + Shape::kNotes);
-    uint32_t* const fills = reinterpret_cast<uint32_t*>(base_ptr + Shape::kFills);
-    volatile int* const abort_flag = reinterpret_cast<volatile int*>(base_ptr + Shape::kMisc);
-
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.group;
-    const uint32_t my_full = base + Shape::kBars + 8 * NST * warp;
     const ModArgs& md = a.mods;
-    if (tid == 0) *abort_flag = 0;
-    if (lane == 0) {
-        for (int i = 0; i < NST; ++i) mbar_init(my_full + 8 * i, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    }
     const Share share = find_share<Shape::kThreads>(a, pl, reinterpret_cast<int*>(base_ptr + Shape::kScratch));      // (synchronises)
     const WarpShare mine = warp_share(a, pl, share, warp, NW, lane);
 
     const int gr = lane >> 2, qd = lane & 3;             // fragment row (a key, then dimensions) and column pair (query rows)
-    // Which key of eight is fragment row i: i with the pairs (2, 3) and (6, 7) exchanged, so that the four keys that the
-    // lanes of a half warp read together in the second product start in two halves of the banks, not in one.
-    const int key_r = gr ^ ((gr >> 1) & 1);
-    const int key_0 = 2 * qd + (qd & 1), key_1 = 2 * qd + 1 - (qd & 1);
-    const bool capped = md.softcap > 0.f, meta = md.documents || md.slopes;
+    const bool capped = kMods && md.softcap > 0.f, by_doc = kMods && md.documents, biased = kMods && md.slopes;
     // capped: x = c tanh(o / c) = c - 2 c / (1 + e^{2 o / c}), all in the base-2 domain
     const float cap2 = md.softcap * kLog2e, cap_in = capped ? 2.f / md.softcap : 0.f;
     uint8_t* const my_ring = base_ptr + warp * NST * Shape::kSlotBytes;
-    int2* const my_entry = reinterpret_cast<int2*>(base_ptr + Shape::kEntry) + warp * NST;
+    const uint32_t ring = base + warp * NST * Shape::kSlotBytes;
     const int tiles_per_page = a.page_rows / kQ4Tile;
 
-    // A segment is what the warp has of one item.
-    struct Segment { int item, b, h, lo, hi; PairRange x; };
     auto segment = [&](int from, Segment& s) {           // the first one at or behind item `from`
         for (s.item = from; s.item <= min(mine.end, share.item1) && s.item < pl.n_items; ++s.item) {
             const int u = s.item / pl.n_pairs, block_lo = s.item == share.item0 ? share.tile0 : 0;
@@ -184,25 +181,51 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         return false;
     };
 
-    // ---- what comes: tiles on their way into the ring
-    uint32_t n_used = 0, n_load = 0;                     // slots read, slots filled
-    uint32_t f_seg = 0;                                  // number of the segment that is being loaded
+    // ---- what comes: tiles on their way into the ring.  A lane copies 16 bytes of every 512 of the codes, the first sixteen lanes the
+    // scales.  V's 16-byte chunks change places, so that eight rows' pieces of one column lie in different banks.
+    constexpr int kCopies = Shape::kCodeBytes / 512;
+    const uint32_t v_to = NH == 2 ? (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 3)) << 4) : (lane >> 1) * 32 + (((lane & 1) ^ ((lane >> 3) & 1)) << 4);
+    uint32_t n_used = 0;                                 // slots read
     bool f_open = false, f_more = true;
-    Segment f;
-    f.item = mine.begin - 1;
-    int f_tile = 0, f_left = 0, f_page = 0, f_next = 0, f_index = 0, f_lo = 0, f_hi = 0;   // f_left: tiles of the current page
-    const int32_t* f_table = nullptr;
-    auto page_at = [&](int index) { return index < a.max_pages ? f_table[index] : -1; };
-    auto refill = [&] {                                  // a tile into the slot that has been read
+    Segment* const desk = reinterpret_cast<Segment*>(base_ptr + Shape::kDesk) + 2 * warp;    // (what is seldom needed stays out of the registers)
+    int f_item = mine.begin - 1, f_end = 0, f_tile = 0, f_left = 0, f_next = 0, f_index = 0, f_lo = 0, f_hi = 0;     // f_left: tiles of the current page
+    bool f_there = false;                                // the current page lies in the pool
+    const uint8_t* f_k = nullptr, * f_v = nullptr, * f_s = nullptr;              // what this lane copies of the next tile
+    int tile_of[NST], item_of[NST];                      // what is in the slots, the next one first; item -1: no more
+    auto page_at = [&](int index) { return index < a.max_pages ? a.page_table[int64_t(desk[0].b) * a.max_pages + index] : -1; };
+    auto turn_page = [&](int page, int row) {
+        const int h = desk[0].h;
+        f_there = uint32_t(page) < uint32_t(a.n_pages);
+        if (!f_there) page = 0;                          // (nothing is read through it)
+        f_k = cache.k + page * cache.k_sb + h * cache.k_sh + int64_t(row) * (D / 2) + lane * 16;
+        f_v = cache.v + page * cache.v_sb + h * cache.v_sh + int64_t(row) * (D / 2) + lane * 16;
+        f_s = (lane < 8 ? cache.ks + page * cache.ks_sb + h * cache.ks_sh : cache.vs + page * cache.vs_sb + h * cache.vs_sh) +
+              int64_t(row) * 4 + (lane & 7) * 16;
+    };
+    auto refill = [&](int j) {                           // the next tile into slot j, which has been read
+#pragma unroll
+        for (int i = 1; i < NST; ++i) { item_of[i - 1] = item_of[i]; tile_of[i - 1] = tile_of[i]; }
+        item_of[NST - 1] = -1;
         for (;;) {
             if (!f_open) {
-                if (!f_more || !segment(f.item + 1, f)) { f_more = false; return; }
+                if (!f_more) break;
+                Segment f;
+                f_more = segment(f_item + 1, f);
+                if (!f_more) break;
+                __syncwarp();
+                if (lane == 0) desk[0] = f;
+                __syncwarp();
+                f_item = f.item;
+                f_end = f.hi;
                 f_tile = f.lo;
-                f_table = a.page_table + int64_t(f.b) * a.max_pages;
                 f_index = f_tile / tiles_per_page;
                 f_left = (f_index + 1) * tiles_per_page - f_tile;
-                if (f_tile < f.hi) { f_page = page_at(f_index); f_next = page_at(f_index + 1); }
-                if (md.documents) {                      // of the tokens: sixteen rows at most
+                if (f_tile < f_end) {
+                    const int page = page_at(f_index);
+                    f_next = page_at(f_index + 1);
+                    turn_page(page, (tiles_per_page - f_left) * kQ4Tile);
+                }
+                if (by_doc) {                            // of the tokens: sixteen rows at most
                     const int r = f.x.row0 + lane;
                     const bool in = lane < f.x.count && r >= 0;
                     const int d = in ? md.documents[int64_t(f.b) * md.doc_sb + int64_t(f.h) * md.doc_sh + r] : 0;
@@ -211,74 +234,83 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                 }
                 f_open = true;
             }
-            if (f_tile >= f.hi) { f_open = false; ++f_seg; continue; }
+            if (f_tile >= f_end) { f_open = false; continue; }
             if (f_left == 0) {
-                f_page = f_next;
+                turn_page(f_next, 0);
                 f_next = page_at(++f_index + 1);
                 f_left = tiles_per_page;
             }
-            const int tile = f_tile++, page = f_page, row = (tiles_per_page - f_left--) * kQ4Tile, t = tile * kQ4Tile + lane;
-            const bool in = t < f.x.rows;
-            int64_t at_doc = 0;
-            if (md.documents) {                          // a tile without any of the tokens' documents is skipped
-                at_doc = int64_t(f.b) * md.doc_sb + int64_t(f.h) * md.doc_sh + (in ? t : 0);
-                const int doc = md.documents[at_doc];
-                if (!__any_sync(0xffffffffu, in && doc >= f_lo && doc <= f_hi)) continue;
-            }
-            const uint32_t s = n_load % NST, bar = my_full + 8 * s, to = base + (warp * NST + s) * Shape::kSlotBytes;
-            if (meta) {
-                const uint32_t at = to + Shape::kLoadBytes + 4 * lane;
-                if (md.slopes) {
-                    if (md.positions) cp_async_4(at, md.positions + int64_t(f.b) * md.pos_sb + int64_t(f.h) * md.pos_sh + (in ? t : 0), in);
-                    else *reinterpret_cast<int32_t*>(my_ring + s * Shape::kSlotBytes + Shape::kLoadBytes + 4 * lane) = t;
+            const int tile = f_tile++;
+            const uint8_t* const k_from = f_k, * const v_from = f_v, * const s_from = f_s;
+            f_k += Shape::kCodeBytes; f_v += Shape::kCodeBytes; f_s += Shape::kScaleBytes;
+            --f_left;
+            const uint32_t to = ring + j * Shape::kSlotBytes;
+            if (by_doc || biased) {
+                const int t = tile * kQ4Tile + lane;
+                const Segment& f = desk[0];
+                const bool in = t < f.x.rows;
+                if (by_doc) {                            // a tile without any of the tokens' documents is skipped
+                    const int32_t* const at = md.documents + int64_t(f.b) * md.doc_sb + int64_t(f.h) * md.doc_sh + (in ? t : 0);
+                    const int doc = *at;
+                    if (!__any_sync(0xffffffffu, in && doc >= f_lo && doc <= f_hi)) continue;
+                    cp_async_4(to + Shape::kLoadBytes + 4 * (kQ4Tile + lane), at, in);
                 }
-                if (md.documents) cp_async_4(at + 4 * kQ4Tile, md.documents + at_doc, in);
+                if (biased) {
+                    if (md.positions) cp_async_4(to + Shape::kLoadBytes + 4 * lane, md.positions + int64_t(f.b) * md.pos_sb + int64_t(f.h) * md.pos_sh + (in ? t : 0), in);
+                    else *reinterpret_cast<int32_t*>(my_ring + j * Shape::kSlotBytes + Shape::kLoadBytes + 4 * lane) = t;
+                }
             }
-            const bool there = uint32_t(page) < uint32_t(a.n_pages);
-            if (!there) {                                // outside the pool: rows of zeros, whatever their codes
-                uint32_t* const sc = reinterpret_cast<uint32_t*>(my_ring + s * Shape::kSlotBytes + 2 * Shape::kCodeBytes);
+            if (f_there) {
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i) {
+                    cp_async_16(to + lane * 16 + i * 512, k_from + i * 512);
+                    cp_async_16(to + Shape::kCodeBytes + v_to + i * 512, v_from + i * 512);
+                }
+                if (lane < 16) cp_async_16(to + 2 * Shape::kCodeBytes + lane * 16, s_from);
+            } else {                                     // outside the pool: rows of zeros, whatever their codes
+                uint32_t* const sc = reinterpret_cast<uint32_t*>(my_ring + j * Shape::kSlotBytes + 2 * Shape::kCodeBytes);
                 sc[lane] = sc[lane + kQ4Tile] = 0u;
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
+                if (lane == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
             }
-            if (elect_one()) {
-                my_entry[s] = make_int2(int(f_seg), tile);
-                if (there) {
-                    mbar_expect_tx(bar, Shape::kLoadBytes);
-                    bulk_load(to, cache.k + page * cache.k_sb + f.h * cache.k_sh + row * (D / 2), Shape::kCodeBytes, bar);
-                    bulk_load(to + Shape::kCodeBytes, cache.v + page * cache.v_sb + f.h * cache.v_sh + row * (D / 2), Shape::kCodeBytes, bar);
-                    bulk_load(to + 2 * Shape::kCodeBytes, cache.ks + page * cache.ks_sb + f.h * cache.ks_sh + row * 4, Shape::kScaleBytes, bar);
-                    bulk_load(to + 2 * Shape::kCodeBytes + Shape::kScaleBytes, cache.vs + page * cache.vs_sb + f.h * cache.vs_sh + row * 4, Shape::kScaleBytes, bar);
-                } else {
-                    atomicOr(a.status, CSP_DEV_BAD_LEN);
-                    mbar_arrive(bar);
-                }
-            }
-            __syncwarp();
-            ++n_load;
-            return;
+            item_of[NST - 1] = f_item;
+            tile_of[NST - 1] = tile;
+            break;
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    for (int j = 0; j < NST; ++j) refill();
+#pragma unroll 1
+    for (int j = 0; j < NST; ++j) refill(j);
 
     int note_front = -1, note_ends = 0, note_back = -1;
-    Segment seg;
-    seg.item = mine.begin - 1;
-    for (uint32_t n_seg = 0; segment(seg.item + 1, seg); ++n_seg) {
-        if (warp_aborted(abort_flag)) break;
-        const int rows = seg.x.rows, count = seg.x.count;
-        const int32_t* const docs = md.documents ? md.documents + int64_t(seg.b) * md.doc_sb + int64_t(seg.h) * md.doc_sh : nullptr;
-        const int32_t* const poss = md.slopes && md.positions ? md.positions + int64_t(seg.b) * md.pos_sb + int64_t(seg.h) * md.pos_sh : nullptr;
-        // positions are taken relative to the last token's, so that near ones are exact in fp32
-        const int row_last = max(seg.x.row0 + count - 1, 0);
-        const int pos_ref = md.slopes && rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
-        int lim_all = kSeesAll;
+    RowNote* const table = reinterpret_cast<RowNote*>(base_ptr + Shape::kTable) + warp * Shape::R;
+    for (int item = mine.begin - 1;;) {
+        int lim_all = kSeesAll, rows, pos_ref;
         uint32_t qb[RH][2 * KW][2];
         float acc[RH][MT][4];
         float2 factor[RH], q_sum[RH], m_run[RH], l_run[RH], b_run[RH];           // of query rows 2 qd and 2 qd + 1
-        float q_pos[RH][2], slope2[RH][2];
-        int lim[RH][2], q_doc[RH][2];
         float v_ref = kTiny, v_inv = 1.f / kTiny;        // power of two that the scales of V are relative to
+        {
+        Segment seg;
+        if (!segment(item + 1, seg)) break;
+        __syncwarp();
+        if (lane == 0) desk[1] = seg;
+        item = seg.item;
+        rows = seg.x.rows;
+        const int count = seg.x.count;
+        const int32_t* const docs = by_doc ? md.documents + int64_t(seg.b) * md.doc_sb + int64_t(seg.h) * md.doc_sh : nullptr;
+        const int32_t* const poss = biased && md.positions ? md.positions + int64_t(seg.b) * md.pos_sb + int64_t(seg.h) * md.pos_sh : nullptr;
+        // positions are taken relative to the last token's, so that near ones are exact in fp32
+        const int row_last = max(seg.x.row0 + count - 1, 0);
+        pos_ref = biased && rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
+        if (lane < Shape::R) {
+            const int tok = lane / G, head = seg.h * G + lane - tok * G, r = seg.x.row0 + tok;
+            const bool valid = tok < count, sees = valid && r >= 0;
+            // rows that nobody asked for see everything: they must not send their warp through the masked path
+            lim_all = !valid ? kSeesAll : sees ? max(r, seg.x.prefix - 1) : -1;
+            table[lane] = RowNote{lim_all, docs && sees ? docs[r] : 0, biased && sees ? float((poss ? poss[r] : r) - pos_ref) : 0.f,
+                                  biased && sees ? md.slopes[head] * kLog2e : 0.f};
+        }
+        lim_all = min(__reduce_min_sync(0xffffffffu, lim_all), rows - 1);
 #pragma unroll
         for (int n = 0; n < RH; ++n) {
             // ---- query row 8 n + gr, this lane's quarter of it: in halves and in the order of the codes
@@ -323,211 +355,196 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
             sum *= 0x1p-20f;
             factor[n] = make_float2(__shfl_sync(0xffffffffu, up, 8 * qd), __shfl_sync(0xffffffffu, up, 8 * qd + 4));
             q_sum[n] = make_float2(__shfl_sync(0xffffffffu, sum, 8 * qd), __shfl_sync(0xffffffffu, sum, 8 * qd + 4));
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int m = 8 * n + 2 * qd + c, tok = m / G, head = seg.h * G + m - tok * G, r = seg.x.row0 + tok;
-                const bool valid = tok < count, sees = valid && r >= 0;
-                // rows that nobody asked for see everything: they must not send their warp through the masked path
-                lim[n][c] = !valid ? kSeesAll : sees ? max(r, seg.x.prefix - 1) : -1;
-                lim_all = min(lim_all, lim[n][c]);
-                q_doc[n][c] = docs && sees ? docs[r] : 0;
-                q_pos[n][c] = md.slopes && sees ? float((poss ? poss[r] : r) - pos_ref) : 0.f;
-                slope2[n][c] = md.slopes && sees ? md.slopes[head] * kLog2e : 0.f;
-            }
             m_run[n] = make_float2(kNeg, kNeg);
             l_run[n] = b_run[n] = make_float2(0.f, 0.f);
 #pragma unroll
             for (int t = 0; t < MT; ++t) acc[n][t][0] = acc[n][t][1] = acc[n][t][2] = acc[n][t][3] = 0.f;
         }
-        lim_all = min(__reduce_min_sync(0xffffffffu, lim_all), rows - 1);
+        }
+        __syncwarp();
         for (;;) {
-            if (n_load == n_used) refill();              // (nothing is known of what comes: tiles may have been skipped)
-            const uint32_t s = n_used % NST;
-            const int2 en = my_entry[s];
-            if (n_load == n_used || en.x != int(n_seg)) break;
-            lean_wait(my_full + 8 * s, (n_used / NST) & 1u, abort_flag);
-            ++n_used;
-            const uint8_t* const k_s = my_ring + s * Shape::kSlotBytes;
-            const uint8_t* const v_s = k_s + Shape::kCodeBytes;
-            const uint32_t* const ks_s = reinterpret_cast<const uint32_t*>(k_s + 2 * Shape::kCodeBytes);
-            const uint32_t* const vs_s = ks_s + kQ4Tile;
-            const int32_t* const pos_s = reinterpret_cast<const int32_t*>(vs_s + kQ4Tile), * const doc_s = pos_s + kQ4Tile;
-            const int t0 = en.y * kQ4Tile;
-            if (meta) asm volatile("cp.async.wait_all;" ::: "memory");
+            if (item_of[0] != item) break;
+            const int j = int(n_used % NST), tile = tile_of[0];
+            asm volatile("cp.async.wait_group %0;" ::"n"(NST - 1) : "memory");
             __syncwarp();
-            // ---- S^T = K Q^T for 32 keys: two blocks of sixteen
-            float2 x[2][RH][2];                      // [block][..][i]: key 8 i + key_r, query rows 2 qd and 2 qd + 1
-            uint32_t k_pair[2][2], v_pair[2][2];     // scale and base
+            // kEdge: some query row does not see all of the tile's keys
+            auto step = [&](auto edge) {
+                constexpr bool kEdge = decltype(edge)::value;
+                const uint8_t* const k_s = my_ring + j * Shape::kSlotBytes;
+                const uint32_t v_s = ring + j * Shape::kSlotBytes + Shape::kCodeBytes;
+                const uint32_t* const ks_s = reinterpret_cast<const uint32_t*>(k_s + 2 * Shape::kCodeBytes);
+                const uint32_t* const vs_s = ks_s + kQ4Tile;
+                const int32_t* const pos_s = reinterpret_cast<const int32_t*>(vs_s + kQ4Tile), * const doc_s = pos_s + kQ4Tile;
+                const int t0 = tile * kQ4Tile;
+                // ---- S^T = K Q^T for 32 keys: two blocks of sixteen
+                float2 x[2][RH][2];                      // [block][..][i]: key 8 i + gr, query rows 2 qd and 2 qd + 1
+                uint32_t k_pair[2][2], v_pair[2][2];     // scale and base
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                uint32_t kw[2][KW];
-                float sum[RH][4];
+                for (int k = 0; k < 2; ++k) {
+                    uint32_t kw[2][KW];
+                    float sum[RH][4];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int key = 16 * k + 8 * i + key_r;
-                    k_pair[k][i] = ks_s[key];
-                    v_pair[k][i] = vs_s[key];
-                    const uint8_t* const from = k_s + key * (D / 2) + qd * KW * 4;
-                    if (KW == 4) {
-                        const uint4 y = *reinterpret_cast<const uint4*>(from);
-                        kw[i][0] = y.x; kw[i][1] = y.y; kw[i][KW - 2] = y.z; kw[i][KW - 1] = y.w;
-                    } else {
-                        const uint2 y = *reinterpret_cast<const uint2*>(from);
-                        kw[i][0] = y.x; kw[i][1] = y.y;
+                    for (int i = 0; i < 2; ++i) {
+                        const int key = 16 * k + 8 * i + gr;
+                        k_pair[k][i] = ks_s[key];
+                        v_pair[k][i] = vs_s[key];
+                        const uint8_t* const from = k_s + key * (D / 2) + qd * KW * 4;
+                        if (KW == 4) {
+                            const uint4 y = *reinterpret_cast<const uint4*>(from);
+                            kw[i][0] = y.x; kw[i][1] = y.y; kw[i][KW - 2] = y.z; kw[i][KW - 1] = y.w;
+                        } else {
+                            const uint2 y = *reinterpret_cast<const uint2*>(from);
+                            kw[i][0] = y.x; kw[i][1] = y.y;
+                        }
                     }
-                }
 #pragma unroll
-                for (int n = 0; n < RH; ++n) sum[n][0] = sum[n][1] = sum[n][2] = sum[n][3] = 0.f;
+                    for (int n = 0; n < RH; ++n) sum[n][0] = sum[n][1] = sum[n][2] = sum[n][3] = 0.f;
 #pragma unroll
-                for (int w = 0; w < KW; ++w) {
-                    const uint32_t y0 = kw[0][w], y1 = kw[1][w], z0 = y0 >> 8, z1 = y1 >> 8;
+                    for (int w = 0; w < KW; ++w) {
+                        const uint32_t y0 = kw[0][w], y1 = kw[1][w];
+                        const uint32_t z0 = y0 >> 8, z1 = y1 >> 8;
 #pragma unroll
-                    for (int n = 0; n < RH; ++n) {
-                        mma_f16(sum[n], y0 & kLow, y1 & kLow, y0 & kHigh, y1 & kHigh, qb[n][2 * w][0], qb[n][2 * w][1]);
-                        mma_f16(sum[n], z0 & kLow, z1 & kLow, z0 & kHigh, z1 & kHigh, qb[n][2 * w + 1][0], qb[n][2 * w + 1][1]);
+                        for (int n = 0; n < RH; ++n) {
+                            mma_f16(sum[n], y0 & kLow, y1 & kLow, y0 & kHigh, y1 & kHigh, qb[n][2 * w][0], qb[n][2 * w][1]);
+                            mma_f16(sum[n], z0 & kLow, z1 & kLow, z0 & kHigh, z1 & kHigh, qb[n][2 * w + 1][0], qb[n][2 * w + 1][1]);
+                        }
                     }
+#pragma unroll
+                    for (int n = 0; n < RH; ++n) { x[k][n][0] = make_float2(sum[n][0], sum[n][1]); x[k][n][1] = make_float2(sum[n][2], sum[n][3]); }
                 }
+                if (kEdge) {                             // what stands behind the last row may be no number
 #pragma unroll
-                for (int n = 0; n < RH; ++n) { x[k][n][0] = make_float2(sum[n][0], sum[n][1]); x[k][n][1] = make_float2(sum[n][2], sum[n][3]); }
-            }
-            if (t0 + 32 > rows) {                    // what stands behind the last row may be no number
+                    for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (t0 + 16 * k + 8 * i + key_r >= rows) k_pair[k][i] = v_pair[k][i] = 0u;
-            }
-            // ---- logits (base 2)
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float sk = lo_bf16(k_pair[k][i]), bk = hi_bf16(k_pair[k][i]);
-#pragma unroll
-                    for (int n = 0; n < RH; ++n)
-                        x[k][n][i] = __fmul2_rn(__ffma2_rn(make_float2(sk, sk), x[k][n][i], __fmul2_rn(make_float2(bk, bk), q_sum[n])), factor[n]);
+                        for (int i = 0; i < 2; ++i)
+                            if (t0 + 16 * k + 8 * i + gr >= rows) k_pair[k][i] = v_pair[k][i] = 0u;
                 }
-            if (capped || md.slopes) {
+                // ---- logits (base 2)
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const float pos = md.slopes ? float(pos_s[16 * k + 8 * i + key_r] - pos_ref) : 0.f;
+                        const float sk = lo_bf16(k_pair[k][i]), bk = hi_bf16(k_pair[k][i]);
 #pragma unroll
-                        for (int n = 0; n < RH; ++n) {
-                            float2& y = x[k][n][i];
-                            if (capped) {
+                        for (int n = 0; n < RH; ++n)
+                            x[k][n][i] = make_float2(fmaf(sk, x[k][n][i].x, bk * q_sum[n].x) * factor[n].x, fmaf(sk, x[k][n][i].y, bk * q_sum[n].y) * factor[n].y);
+                    }
+                if (capped) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int n = 0; n < RH; ++n)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                float2& y = x[k][n][i];
                                 y.x = fmaf(-2.f * cap2, rcpf(1.f + ex2f(y.x * cap_in)), cap2);
                                 y.y = fmaf(-2.f * cap2, rcpf(1.f + ex2f(y.y * cap_in)), cap2);
                             }
-                            if (md.slopes) {
-                                y.x = fmaf(-slope2[n][0], fabsf(q_pos[n][0] - pos), y.x);
-                                y.y = fmaf(-slope2[n][1], fabsf(q_pos[n][1] - pos), y.y);
+                }
+                if (kEdge || biased) {
+#pragma unroll
+                    for (int n = 0; n < RH; ++n) {
+                        const RowNote r0 = table[8 * n + 2 * qd], r1 = table[8 * n + 2 * qd + 1];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int key = 16 * k + 8 * i + gr, t = t0 + key;
+                                float2& y = x[k][n][i];
+                                if (biased) {
+                                    const float pos = float(pos_s[key] - pos_ref);
+                                    y.x = fmaf(-r0.slope2, fabsf(r0.pos - pos), y.x);
+                                    y.y = fmaf(-r1.slope2, fabsf(r1.pos - pos), y.y);
+                                }
+                                if (kEdge) {
+                                    const int doc = by_doc ? doc_s[key] : 0;
+                                    if (t > r0.lim || t >= rows || (by_doc && doc != r0.doc)) y.x = kNeg;
+                                    if (t > r1.lim || t >= rows || (by_doc && doc != r1.doc)) y.y = kNeg;
+                                }
                             }
-                        }
                     }
-            }
-            const bool masked = md.documents || t0 + 31 > lim_all;
-            if (masked) {
+                }
+                // ---- references: of the softmax per query row, of the scales per warp; raised when exceeded by 2^8 and 2^4
+                const float v_top = fmaxf(fmax3(lo_bf16(v_pair[0][0]), lo_bf16(v_pair[0][1]), lo_bf16(v_pair[1][0])), lo_bf16(v_pair[1][1]));
+                float2 mx[RH];
+                float over = v_top * (v_inv * (kLazy / 16.f));
+#pragma unroll
+                for (int n = 0; n < RH; ++n) {
+                    mx[n].x = fmaxf(fmax3(x[0][n][0].x, x[0][n][1].x, x[1][n][0].x), x[1][n][1].x);
+                    mx[n].y = fmaxf(fmax3(x[0][n][0].y, x[0][n][1].y, x[1][n][0].y), x[1][n][1].y);
+                    over = fmax3(over, mx[n].x - m_run[n].x, mx[n].y - m_run[n].y);
+                }
+                const bool raise = over > kLazy;
+                if (__any_sync(0xffffffffu, raise)) {
+                    // (the same power of two in all lanes; scales are not negative, so their bits are in order)
+                    const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(fminf(fmaxf(v_top, v_ref), kHuge))) & 0x7f800000u;
+                    v_inv = __uint_as_float((254u << 23) - top);
+                    const float shrink = v_ref * v_inv;
+                    v_ref = __uint_as_float(top);
+#pragma unroll
+                    for (int n = 0; n < RH; ++n) {
+                        float2 y = mx[n], alpha = make_float2(1.f, 1.f);
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) {
+                            y.x = fmaxf(y.x, __shfl_xor_sync(0xffffffffu, y.x, d));
+                            y.y = fmaxf(y.y, __shfl_xor_sync(0xffffffffu, y.y, d));
+                        }
+                        if (y.x > m_run[n].x + kLazy) { alpha.x = ex2f(m_run[n].x - y.x); m_run[n].x = y.x; }
+                        if (y.y > m_run[n].y + kLazy) { alpha.y = ex2f(m_run[n].y - y.y); m_run[n].y = y.y; }
+                        l_run[n] = __fmul2_rn(l_run[n], alpha);
+                        b_run[n] = __fmul2_rn(b_run[n], alpha);
+                        alpha.x *= shrink;
+                        alpha.y *= shrink;
+#pragma unroll
+                        for (int t = 0; t < MT; ++t) { acc[n][t][0] *= alpha.x; acc[n][t][1] *= alpha.y; acc[n][t][2] *= alpha.x; acc[n][t][3] *= alpha.y; }
+                    }
+                }
+                // ---- weights
+                uint32_t pb[2][RH][2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const int key = 16 * k + 8 * i + key_r, t = t0 + key, doc = md.documents ? doc_s[key] : 0;
+                        const float sv = lo_bf16(v_pair[k][i]) * v_inv, bv = hi_bf16(v_pair[k][i]);
 #pragma unroll
                         for (int n = 0; n < RH; ++n) {
-                            if (t > lim[n][0] || t >= rows || (md.documents && doc != q_doc[n][0])) x[k][n][i].x = kNeg;
-                            if (t > lim[n][1] || t >= rows || (md.documents && doc != q_doc[n][1])) x[k][n][i].y = kNeg;
+                            const float2 y = __fadd2_rn(x[k][n][i], make_float2(-m_run[n].x, -m_run[n].y));
+                            float2 p = make_float2(ex2f(y.x), ex2f(y.y));
+                            if (kEdge) {                 // (a row that has seen nothing yet: its reference is as low)
+                                if (x[k][n][i].x == kNeg) p.x = 0.f;
+                                if (x[k][n][i].y == kNeg) p.y = 0.f;
+                            }
+                            l_run[n] = __fadd2_rn(l_run[n], p);
+                            b_run[n] = make_float2(fmaf(p.x, bv, b_run[n].x), fmaf(p.y, bv, b_run[n].y));
+                            pb[k][n][i] = transpose8(pack_f16(p.x * sv, p.y * sv));
                         }
                     }
-            }
-            // ---- references: of the softmax per query row, of the scales per warp; raised when exceeded by 2^8 and 2^4
-            const float v_top = fmaxf(fmaxf(lo_bf16(v_pair[0][0]), lo_bf16(v_pair[0][1])), fmaxf(lo_bf16(v_pair[1][0]), lo_bf16(v_pair[1][1])));
-            float2 mx[RH];
-            bool raise = v_top > 16.f * v_ref && v_ref < kHuge;
+                // ---- O^T += V^T P^T: pieces of four codes (dimensions 4 gr to 4 gr + 3 of 32), two keys each
 #pragma unroll
-            for (int n = 0; n < RH; ++n) {
-                mx[n].x = fmaxf(fmaxf(x[0][n][0].x, x[0][n][1].x), fmaxf(x[1][n][0].x, x[1][n][1].x));
-                mx[n].y = fmaxf(fmaxf(x[0][n][0].y, x[0][n][1].y), fmaxf(x[1][n][0].y, x[1][n][1].y));
-                raise = raise || mx[n].x > m_run[n].x + kLazy || mx[n].y > m_run[n].y + kLazy;
-            }
-            if (__any_sync(0xffffffffu, raise)) {
-                // (the same power of two in all lanes; scales are not negative, so their bits are in order)
-                const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(fminf(fmaxf(v_top, v_ref), kHuge))) & 0x7f800000u;
-                v_inv = __uint_as_float((254u << 23) - top);
-                const float shrink = v_ref * v_inv;
-                v_ref = __uint_as_float(top);
+                for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int n = 0; n < RH; ++n) {
-                    float2 y = mx[n], alpha = make_float2(1.f, 1.f);
+                    for (int c = 0; c < D / 32; c += 2) {
+                        // matrices 1, 3: the second eight keys; 2, 3: the next sixteen bytes
+                        const int row = 16 * k + ((lane >> 3) & 1) * 8 + (lane & 7), chunk = c + (lane >> 4);
+                        uint32_t y[4];
+                        ldsm_x4_t(y, v_s + row * (D / 2) + ((NH == 2 ? chunk ^ ((row >> 1) & 3) : chunk ^ ((row >> 2) & 1)) << 4));
 #pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) {
-                        y.x = fmaxf(y.x, __shfl_xor_sync(0xffffffffu, y.x, d));
-                        y.y = fmaxf(y.y, __shfl_xor_sync(0xffffffffu, y.y, d));
-                    }
-                    if (y.x > m_run[n].x + kLazy) { alpha.x = ex2f(m_run[n].x - y.x); m_run[n].x = y.x; }
-                    if (y.y > m_run[n].y + kLazy) { alpha.y = ex2f(m_run[n].y - y.y); m_run[n].y = y.y; }
-                    l_run[n] = __fmul2_rn(l_run[n], alpha);
-                    b_run[n] = __fmul2_rn(b_run[n], alpha);
-                    alpha.x *= shrink;
-                    alpha.y *= shrink;
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t y0 = y[2 * i], y1 = y[2 * i + 1], z0 = y0 >> 8, z1 = y1 >> 8;
+                            const int t = 2 * (c + i);
 #pragma unroll
-                    for (int t = 0; t < MT; ++t) { acc[n][t][0] *= alpha.x; acc[n][t][1] *= alpha.y; acc[n][t][2] *= alpha.x; acc[n][t][3] *= alpha.y; }
-                }
-            }
-            // ---- weights
-            uint32_t pb[2][RH][2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float sv = lo_bf16(v_pair[k][i]) * v_inv, bv = hi_bf16(v_pair[k][i]);
-#pragma unroll
-                    for (int n = 0; n < RH; ++n) {
-                        const float2 y = __fadd2_rn(x[k][n][i], make_float2(-m_run[n].x, -m_run[n].y));
-                        float2 p = make_float2(ex2f(y.x), ex2f(y.y));
-                        if (masked) {                // (a row that has seen nothing yet: its reference is as low)
-                            if (x[k][n][i].x == kNeg) p.x = 0.f;
-                            if (x[k][n][i].y == kNeg) p.y = 0.f;
-                        }
-                        l_run[n] = __fadd2_rn(l_run[n], p);
-                        b_run[n] = __ffma2_rn(p, make_float2(bv, bv), b_run[n]);
-                        const float2 w = __fmul2_rn(p, make_float2(sv, sv));
-                        pb[k][n][i] = transpose8(pack_f16(w.x, w.y));
-                    }
-                }
-            // ---- O^T += V^T P^T
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                uint32_t vw[4][VW];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = 16 * k + 8 * (i >> 1) + (i & 1 ? key_1 : key_0);
-                    const uint8_t* const from = v_s + key * (D / 2) + gr * VW * 4;
-                    if (VW == 2) {
-                        const uint2 y = *reinterpret_cast<const uint2*>(from);
-                        vw[i][0] = y.x; vw[i][VW - 1] = y.y;
-                    } else {
-                        vw[i][0] = *reinterpret_cast<const uint32_t*>(from);
-                    }
-                }
-#pragma unroll
-                for (int w = 0; w < VW; ++w)
-#pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {                 // values 0 - 3 and 4 - 7 of the word, of two keys each
-                        const uint32_t y0 = __byte_perm(vw[0][w], vw[1][w], hf ? 0x7632 : 0x5410);
-                        const uint32_t y1 = __byte_perm(vw[2][w], vw[3][w], hf ? 0x7632 : 0x5410);
-                        const uint32_t z0 = y0 >> 8, z1 = y1 >> 8;
-                        const int t = 4 * w + 2 * hf;
-#pragma unroll
-                        for (int n = 0; n < RH; ++n) {
-                            mma_f16(acc[n][t], y0 & kLow, y0 & kHigh, y1 & kLow, y1 & kHigh, pb[k][n][0], pb[k][n][1]);
-                            mma_f16(acc[n][t + 1], z0 & kLow, z0 & kHigh, z1 & kLow, z1 & kHigh, pb[k][n][0], pb[k][n][1]);
+                            for (int n = 0; n < RH; ++n) {
+                                mma_f16(acc[n][t], y0 & kLow, y0 & kHigh, y1 & kLow, y1 & kHigh, pb[k][n][0], pb[k][n][1]);
+                                mma_f16(acc[n][t + 1], z0 & kLow, z0 & kHigh, z1 & kLow, z1 & kHigh, pb[k][n][0], pb[k][n][1]);
+                            }
                         }
                     }
-            }
+            };
+            if (by_doc || tile * kQ4Tile + 31 > lim_all) step(std::true_type{});
+            else step(std::false_type{});
             __syncwarp();
-            refill();
+            refill(j);
+            ++n_used;
         }
         // ---- the item's end: sums over the lanes' keys
 #pragma unroll
@@ -539,6 +556,8 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                 b_run[n].x += __shfl_xor_sync(0xffffffffu, b_run[n].x, d);
                 b_run[n].y += __shfl_xor_sync(0xffffffffu, b_run[n].y, d);
             }
+        const Segment seg = desk[1];
+        const int count = seg.x.count;
         const bool begins = seg.lo == 0, ends = seg.hi >= seg.x.tiles;
         if (!begins) { note_front = seg.item; note_ends = ends; }
         else if (!ends) note_back = seg.item;
@@ -549,46 +568,30 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int m = 8 * n + 2 * qd + c;
-                if (md.slopes && fabsf(q_pos[n][c]) > kFarToken) atomicOr(a.status, CSP_DEV_BAD_LEN);
+                if (biased && fabsf(table[m].pos) > kFarToken) atomicOr(a.status, CSP_DEV_BAD_LEN);
                 if (m >= count * G) continue;
                 const float base_sum = c ? b_run[n].y : b_run[n].x, l = c ? l_run[n].y : l_run[n].x, mm = c ? m_run[n].y : m_run[n].x;
-                float2 o[MT];                            // dimensions 2 t and 2 t + 1 of this lane's D / 8
+                const int tok = m / G, head = seg.h * G + m - tok * G;
+                const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, mm) + l);      // l == 0: nothing was seen
+                uint16_t* const out = a.out + int64_t(seg.b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(seg.x.tok0 + tok) * a.o_st + 4 * gr;
 #pragma unroll
-                for (int t = 0; t < MT; ++t)
-                    o[t] = make_float2(fmaf(acc[n][t][c] * 0x1p24f, v_ref, base_sum), fmaf(acc[n][t][2 + c] * 0x1p20f, v_ref, base_sum));
-                if (begins && ends) {
-                    const int tok = m / G, head = seg.h * G + m - tok * G;
-                    const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, mm) + l);          // l == 0: nothing was seen
-                    uint4* const out = reinterpret_cast<uint4*>(a.out + int64_t(seg.b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(seg.x.tok0 + tok) * a.o_st + gr * (D / 8));
-                    uint32_t y[MT];
-#pragma unroll
-                    for (int t = 0; t < MT; ++t) y[t] = l == 0.f ? 0u : pack_bf16(o[t].x * inv, o[t].y * inv);
-#pragma unroll
-                    for (int t = 0; t < MT; t += 4) out[t / 4] = make_uint4(y[t], y[t + 1], y[t + 2], y[t + 3]);
-                    if (a.lse && gr == 0)
+                for (int t = 0; t < MT; t += 2) {        // dimensions 16 t + 4 gr to 16 t + 4 gr + 3
+                    const float4 o = make_float4(fmaf(acc[n][t][c] * 0x1p24f, v_ref, base_sum), fmaf(acc[n][t][2 + c] * 0x1p20f, v_ref, base_sum),
+                                                 fmaf(acc[n][t + 1][c] * 0x1p24f, v_ref, base_sum), fmaf(acc[n][t + 1][2 + c] * 0x1p20f, v_ref, base_sum));
+                    if (begins && ends)
+                        *reinterpret_cast<uint2*>(out + 16 * t) = l == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+                    else
+                        *reinterpret_cast<float4*>(piece + m * Shape::kPieceRow + 16 * t + 4 * gr) = o;
+                }
+                if (gr == 0) {
+                    if (!(begins && ends)) *reinterpret_cast<float2*>(piece + m * Shape::kPieceRow + D) = make_float2(mm, l);
+                    else if (a.lse)
                         a.lse[(int64_t(seg.b) * a.n_kv_heads * G + head) * a.max_new + seg.x.tok0 + tok] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
-                } else {
-                    float* const to = piece + m * (D + 2);
-#pragma unroll
-                    for (int t = 0; t < MT; ++t) *reinterpret_cast<float2*>(to + gr * (D / 8) + 2 * t) = o[t];
-                    if (gr == 0) *reinterpret_cast<float2*>(to + D) = make_float2(mm, l);
                 }
             }
     }
-    if (lane == 0) {
-        notes[warp] = Notes{note_front, note_ends, note_back, 0};
-        fills[warp] = n_load;
-    }
-    __syncwarp();
+    if (lane == 0) notes[warp] = Notes{note_front, note_ends, note_back, 0};
     __syncthreads();
-    if (*abort_flag) {
-        if (tid == 0) {
-            atomicOr(a.status, CSP_DEV_TIMEOUT);
-            parts[blockIdx.x] = ChunkParts{-1, 0};
-            for (int w = 0; w < NW; ++w) drain_ring(base + Shape::kBars + 8 * NST * w, fills[w], NST);
-        }
-        return;
-    }
     // ---- the pieces of cut items: chain 0 goes on with what the block before began, chain c begins with warp c - 1's back piece
     ChunkParts said = {-1, 0};
     for (int c = 0; c <= NW; ++c) {
@@ -606,7 +609,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         constexpr int C = D / 32;                        // columns per lane
         for (int m = warp; m < x.count * G; m += NW) {
             auto piece = [&](int w) {
-                return reinterpret_cast<const float*>(c > 0 && w == w0 ? base_ptr + w * NST * Shape::kSlotBytes : base_ptr + Shape::kFront + w * Shape::kPieceBytes) + m * (D + 2);
+                return reinterpret_cast<const float*>(c > 0 && w == w0 ? base_ptr + w * NST * Shape::kSlotBytes : base_ptr + Shape::kFront + w * Shape::kPieceBytes) + m * Shape::kPieceRow;
             };
             float mm = kNeg;
             for (int w = w0; w < next; ++w) mm = fmaxf(mm, piece(w)[D]);
@@ -675,16 +678,23 @@ ChunkPlan chunk_q4_plan(const csp_params& p, int max_new) {
     return pl;
 }
 
-template <int NH, int RH>
-csp_status launch_few(const ChunkArgs& a, const ChunkPlan& pl, const FewQuery& q, const Q4Args& c, ChunkParts* parts, float* partial,
+template <int NH, int RH, bool kMods>
+csp_status launch_few_mods(const ChunkArgs& a, const ChunkPlan& pl, const FewQuery& q, const Q4Args& c, ChunkParts* parts, float* partial,
                       float2* ml, cudaStream_t s) {
     constexpr int smem = int(Q4Shape<NH, RH>::kTotal) + 128;
     static_assert(smem <= 227 * 1024, "shared memory of one CTA");
-    auto kern = chunk_q4_few_kernel<NH, RH>;
+    auto kern = chunk_q4_few_kernel<NH, RH, kMods>;
     static std::atomic<bool> configured[kMaxDevices];
     if (!raise_smem_limit(kern, smem, configured)) return CSP_ERR_CUDA;
     kern<<<pl.grid, Q4Shape<NH, RH>::kThreads, smem, s>>>(a, pl, q, c, parts, partial, ml);
     return cudaGetLastError() == cudaSuccess ? CSP_OK : CSP_ERR_CUDA;
+}
+
+template <int NH, int RH>
+csp_status launch_few(const ChunkArgs& a, const ChunkPlan& pl, const FewQuery& q, const Q4Args& c, ChunkParts* parts, float* partial,
+                      float2* ml, cudaStream_t s) {
+    return a.mods.softcap > 0.f || a.mods.slopes || a.mods.documents ? launch_few_mods<NH, RH, true>(a, pl, q, c, parts, partial, ml, s)
+                                                                     : launch_few_mods<NH, RH, false>(a, pl, q, c, parts, partial, ml, s);
 }
 
 }  // namespace
