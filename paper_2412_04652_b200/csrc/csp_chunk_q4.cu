@@ -26,7 +26,6 @@
 // goes on in another CTA is left as a partial result for the joining kernel.
 #include <cuda_fp16.h>
 #include <limits.h>
-#include <type_traits>
 
 #include "csp_chunk.cuh"
 
@@ -58,6 +57,12 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 __device__ __forceinline__ void ldsm_x4_t(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+// of two pairs of bf16 numbers: the larger magnitudes
+__device__ __forceinline__ uint32_t max_abs2(uint32_t x, uint32_t y) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x & 0x7fff7fffu), "r"(y & 0x7fff7fffu));
+    return r;
 }
 __device__ __forceinline__ float fmax3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
@@ -95,39 +100,41 @@ struct Q4Shape {
 // over the block's items, a lane per item.
 struct WarpShare { int begin, begin_tile, end, end_tile; };
 __device__ __forceinline__ WarpShare warp_share(const ChunkArgs& a, const ChunkPlan& pl, const Share& sh, int warp, int warps, int lane) {
-    auto weight = [&](int item, int& lo) {
-        lo = item == sh.item0 ? sh.tile0 : 0;
-        if (item > sh.item1 || item >= pl.n_items || (item == sh.item1 && sh.tile1 == 0)) return 0;
-        const int u = item / pl.n_pairs;
-        const PairRange x = pair_range(a, pl, u, item - u * pl.n_pairs);
-        return x.count > 0 ? max((item == sh.item1 ? sh.tile1 : x.tiles) - lo, 0) + 1 : 0;
-    };
     const int last = min(sh.item1, pl.n_items - 1);
-    int total = 0, lo, w = 0;
-    for (int i = sh.item0; i <= last; i += 32) { w = weight(i + lane, lo); total += __reduce_add_sync(0xffffffffu, w); }
-    const int part = max((total + warps - 1) / warps, 2);
-    int before = 0, got[4] = {pl.n_items, 0, pl.n_items, 0};
-    for (int i = sh.item0; i <= last; i += 32) {
-        if (last - sh.item0 >= 32) w = weight(i + lane, lo);         // (else it is there still)
-        else lo = i + lane == sh.item0 ? sh.tile0 : 0;
-        int x = w;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, x, d);
-            if (lane >= d) x += y;
-        }
-        const int p = before + x - w;                    // weight in front of this lane's item
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int cut = (warp + k) * part;
-            const uint32_t hit = __ballot_sync(0xffffffffu, cut >= p && cut < p + w);
-            if (hit) {
-                const int from = __ffs(hit) - 1;
-                got[2 * k] = i + from;
-                got[2 * k + 1] = __shfl_sync(0xffffffffu, lo + max(cut - p - 1, 0), from);
+    int total = 0, part = 0, got[4] = {pl.n_items, 0, pl.n_items, 0};
+    // (the code of this kernel is fetched once per launch, which costs more than running it: both passes are one)
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        int before = 0;
+#pragma unroll 1
+        for (int i = sh.item0; i <= last; i += 32) {
+            const int item = i + lane, lo = item == sh.item0 ? sh.tile0 : 0;
+            int w = 0;
+            if (item <= last && !(item == sh.item1 && sh.tile1 == 0)) {
+                const int u = item / pl.n_pairs;
+                const PairRange x = pair_range(a, pl, u, item - u * pl.n_pairs);
+                w = x.count > 0 ? max((item == sh.item1 ? sh.tile1 : x.tiles) - lo, 0) + 1 : 0;
             }
+            int x = w;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, x, d);
+                if (lane >= d) x += y;
+            }
+            const int p = before + x - w;                // weight in front of this lane's item
+#pragma unroll 1
+            for (int k = 0; k < 2 && pass; ++k) {
+                const int cut = (warp + k) * part;
+                const uint32_t hit = __ballot_sync(0xffffffffu, cut >= p && cut < p + w);
+                if (!hit) continue;
+                const int from = __ffs(hit) - 1, tile = __shfl_sync(0xffffffffu, lo + max(cut - p - 1, 0), from);
+                if (k == 0) { got[0] = i + from; got[1] = tile; }
+                else { got[2] = i + from; got[3] = tile; }
+            }
+            before += __shfl_sync(0xffffffffu, x, 31);
         }
-        before += __shfl_sync(0xffffffffu, x, 31);
+        total = before;
+        part = max((total + warps - 1) / warps, 2);
     }
     return WarpShare{got[0], got[1], got[2], got[3]};
 }
@@ -185,7 +192,6 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     // scales.  V's 16-byte chunks change places, so that eight rows' pieces of one column lie in different banks.
     constexpr int kCopies = Shape::kCodeBytes / 512;
     const uint32_t v_to = NH == 2 ? (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 3)) << 4) : (lane >> 1) * 32 + (((lane & 1) ^ ((lane >> 3) & 1)) << 4);
-    uint32_t n_used = 0;                                 // slots read
     bool f_open = false, f_more = true;
     Segment* const desk = reinterpret_cast<Segment*>(base_ptr + Shape::kDesk) + 2 * warp;    // (what is seldom needed stays out of the registers)
     int f_item = mine.begin - 1, f_end = 0, f_tile = 0, f_left = 0, f_next = 0, f_index = 0, f_lo = 0, f_hi = 0;     // f_left: tiles of the current page
@@ -278,20 +284,68 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-#pragma unroll 1
-    for (int j = 0; j < NST; ++j) refill(j);
-
     int note_front = -1, note_ends = 0, note_back = -1;
     RowNote* const table = reinterpret_cast<RowNote*>(base_ptr + Shape::kTable) + warp * Shape::R;
-    for (int item = mine.begin - 1;;) {
-        int lim_all = kSeesAll, rows, pos_ref;
-        uint32_t qb[RH][2 * KW][2];
-        float acc[RH][MT][4];
-        float2 factor[RH], q_sum[RH], m_run[RH], l_run[RH], b_run[RH];           // of query rows 2 qd and 2 qd + 1
-        float v_ref = kTiny, v_inv = 1.f / kTiny;        // power of two that the scales of V are relative to
-        {
+    int item = mine.begin - 1, lim_all = 0, rows = 0, pos_ref = 0;
+    bool open = false;                                   // an item is being worked on
+    uint32_t qb[RH][2 * KW][2];
+    float acc[RH][MT][4];
+    float2 factor[RH], q_sum[RH], m_run[RH], l_run[RH], b_run[RH];               // of query rows 2 qd and 2 qd + 1
+    float v_ref = kTiny, v_inv = 1.f / kTiny;            // power of two that the scales of V are relative to
+    // (one loop for everything, so that the code stands here once; the first NST rounds only fill the ring)
+    for (int n_used = -NST;; ++n_used) {
+        const int j = (n_used + NST) % NST;
+        if (n_used >= 0) {
+        if (open && item_of[0] != item) {
+            // ---- the item's end: sums over the lanes' keys
+#pragma unroll
+            for (int n = 0; n < RH; ++n)
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) {
+                    l_run[n].x += __shfl_xor_sync(0xffffffffu, l_run[n].x, d);
+                    l_run[n].y += __shfl_xor_sync(0xffffffffu, l_run[n].y, d);
+                    b_run[n].x += __shfl_xor_sync(0xffffffffu, b_run[n].x, d);
+                    b_run[n].y += __shfl_xor_sync(0xffffffffu, b_run[n].y, d);
+                }
+            const Segment seg = desk[1];
+            const int count = seg.x.count;
+            const bool begins = seg.lo == 0, ends = seg.hi >= seg.x.tiles;
+            if (!begins) { note_front = seg.item; note_ends = ends; }
+            else if (!ends) note_back = seg.item;
+            // (a back piece is the last thing that its warp has: nothing is on its way into the ring any more)
+            float* const piece = reinterpret_cast<float*>(begins ? my_ring : base_ptr + Shape::kFront + warp * Shape::kPieceBytes);
+#pragma unroll
+            for (int n = 0; n < RH; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int m = 8 * n + 2 * qd + c;
+                    if (biased && fabsf(table[m].pos) > kFarToken) atomicOr(a.status, CSP_DEV_BAD_LEN);
+                    if (m >= count * G) continue;
+                    const float base_sum = c ? b_run[n].y : b_run[n].x, l = c ? l_run[n].y : l_run[n].x, mm = c ? m_run[n].y : m_run[n].x;
+                    const int tok = m / G, head = seg.h * G + m - tok * G;
+                    const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, mm) + l);      // l == 0: nothing was seen
+                    uint16_t* const out = a.out + int64_t(seg.b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(seg.x.tok0 + tok) * a.o_st + 4 * gr;
+#pragma unroll
+                    for (int t = 0; t < MT; t += 2) {        // dimensions 16 t + 4 gr to 16 t + 4 gr + 3
+                        const float4 o = make_float4(fmaf(acc[n][t][c] * 0x1p24f, v_ref, base_sum), fmaf(acc[n][t][2 + c] * 0x1p20f, v_ref, base_sum),
+                                                     fmaf(acc[n][t + 1][c] * 0x1p24f, v_ref, base_sum), fmaf(acc[n][t + 1][2 + c] * 0x1p20f, v_ref, base_sum));
+                        if (begins && ends)
+                            *reinterpret_cast<uint2*>(out + 16 * t) = l == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+                        else
+                            *reinterpret_cast<float4*>(piece + m * Shape::kPieceRow + 16 * t + 4 * gr) = o;
+                    }
+                    if (gr == 0) {
+                        if (!(begins && ends)) *reinterpret_cast<float2*>(piece + m * Shape::kPieceRow + D) = make_float2(mm, l);
+                        else if (a.lse)
+                            a.lse[(int64_t(seg.b) * a.n_kv_heads * G + head) * a.max_new + seg.x.tok0 + tok] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
+                    }
+                }
+            open = false;
+        }
+        if (!open) {
         Segment seg;
         if (!segment(item + 1, seg)) break;
+        open = true;
         __syncwarp();
         if (lane == 0) desk[1] = seg;
         item = seg.item;
@@ -302,6 +356,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         // positions are taken relative to the last token's, so that near ones are exact in fp32
         const int row_last = max(seg.x.row0 + count - 1, 0);
         pos_ref = biased && rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
+        lim_all = kSeesAll;
         if (lane < Shape::R) {
             const int tok = lane / G, head = seg.h * G + lane - tok * G, r = seg.x.row0 + tok;
             const bool valid = tok < count, sees = valid && r >= 0;
@@ -321,274 +376,212 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
 #pragma unroll
                 for (int w = 0; w < KW; ++w) q[w] = tok < count ? reinterpret_cast<const uint4*>(from)[w] : make_uint4(0, 0, 0, 0);
             }
-            uint32_t top = 0;                            // bits of the row's largest magnitude
+            uint32_t top2 = 0;                           // the row's largest magnitude, two candidates
 #pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                const uint32_t y[4] = {q[w].x, q[w].y, q[w].z, q[w].w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) top = max(top, max((y[k] << 16) & 0x7fffffffu, y[k] & 0x7fff0000u));
-            }
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const uint32_t ex = top >> 23;               // 255: an infinity or NaN, the row is no number
-            const float down = ex == 255u ? 0.f : __uint_as_float((254u - ex) << 23);        // 2^-e (0: 2^127)
-            float sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                const uint32_t y[4] = {q[w].x, q[w].y, q[w].z, q[w].w};
-                float v[8];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    v[2 * k] = lo_bf16(y[k]) * down;
-                    v[2 * k + 1] = hi_bf16(y[k]) * down;
-                    sum += v[2 * k] + v[2 * k + 1];
-                }
-                qb[n][2 * w][0] = pack_f16(16.f * v[0], 16.f * v[4]);
-                qb[n][2 * w][1] = pack_f16(v[1], v[5]);
-                qb[n][2 * w + 1][0] = pack_f16(16.f * v[2], 16.f * v[6]);
-                qb[n][2 * w + 1][1] = pack_f16(v[3], v[7]);
-            }
-            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            for (int w = 0; w < KW; ++w) top2 = max_abs2(max_abs2(max_abs2(max_abs2(top2, q[w].x), q[w].y), q[w].z), q[w].w);
+            top2 = max_abs2(top2, top2 >> 16 | top2 << 16);
+            top2 = max_abs2(top2, __shfl_xor_sync(0xffffffffu, top2, 1));
+            top2 = max_abs2(top2, __shfl_xor_sync(0xffffffffu, top2, 2));
+            const uint32_t ex = (top2 & 0x7fffu) >> 7;   // 255: an infinity, the row is no number
+            const float down = ex == 255u ? 0.f : __uint_as_float((254u - ex) << 23), down16 = 16.f * down;      // 2^-e (0: 2^127)
             // logit = up 2^20 (scale S + base sum 2^-20), S the product with codes 2^-20
             const float up = a.scale * kLog2e * 0x1p20f * (ex == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(ex << 23));
-            sum *= 0x1p-20f;
             factor[n] = make_float2(__shfl_sync(0xffffffffu, up, 8 * qd), __shfl_sync(0xffffffffu, up, 8 * qd + 4));
-            q_sum[n] = make_float2(__shfl_sync(0xffffffffu, sum, 8 * qd), __shfl_sync(0xffffffffu, sum, 8 * qd + 4));
+            float ones[4] = {0.f, 0.f, 0.f, 0.f};        // the product with codes of one: the query's sum 2^-20
+#pragma unroll
+            for (int w = 0; w < KW; ++w) {
+                qb[n][2 * w][0] = pack_f16(down16 * lo_bf16(q[w].x), down16 * lo_bf16(q[w].z));
+                qb[n][2 * w][1] = pack_f16(down * hi_bf16(q[w].x), down * hi_bf16(q[w].z));
+                qb[n][2 * w + 1][0] = pack_f16(down16 * lo_bf16(q[w].y), down16 * lo_bf16(q[w].w));
+                qb[n][2 * w + 1][1] = pack_f16(down * hi_bf16(q[w].y), down * hi_bf16(q[w].w));
+                mma_f16(ones, 0x00010001u, 0x00010001u, 0x00100010u, 0x00100010u, qb[n][2 * w][0], qb[n][2 * w][1]);
+                mma_f16(ones, 0x00010001u, 0x00010001u, 0x00100010u, 0x00100010u, qb[n][2 * w + 1][0], qb[n][2 * w + 1][1]);
+            }
+            q_sum[n] = make_float2(ones[0], ones[1]);
             m_run[n] = make_float2(kNeg, kNeg);
             l_run[n] = b_run[n] = make_float2(0.f, 0.f);
 #pragma unroll
             for (int t = 0; t < MT; ++t) acc[n][t][0] = acc[n][t][1] = acc[n][t][2] = acc[n][t][3] = 0.f;
         }
-        }
+        v_ref = kTiny;
+        v_inv = 1.f / kTiny;
         __syncwarp();
-        for (;;) {
-            if (item_of[0] != item) break;
-            const int j = int(n_used % NST), tile = tile_of[0];
+        if (item_of[0] != item) { --n_used; continue; }  // (an item without any tile for this warp)
+        }
+        {
+            const int tile = tile_of[0];
             asm volatile("cp.async.wait_group %0;" ::"n"(NST - 1) : "memory");
             __syncwarp();
-            // kEdge: some query row does not see all of the tile's keys
-            auto step = [&](auto edge) {
-                constexpr bool kEdge = decltype(edge)::value;
-                const uint8_t* const k_s = my_ring + j * Shape::kSlotBytes;
-                const uint32_t v_s = ring + j * Shape::kSlotBytes + Shape::kCodeBytes;
-                const uint32_t* const ks_s = reinterpret_cast<const uint32_t*>(k_s + 2 * Shape::kCodeBytes);
-                const uint32_t* const vs_s = ks_s + kQ4Tile;
-                const int32_t* const pos_s = reinterpret_cast<const int32_t*>(vs_s + kQ4Tile), * const doc_s = pos_s + kQ4Tile;
-                const int t0 = tile * kQ4Tile;
-                // ---- S^T = K Q^T for 32 keys: two blocks of sixteen
-                float2 x[2][RH][2];                      // [block][..][i]: key 8 i + gr, query rows 2 qd and 2 qd + 1
-                uint32_t k_pair[2][2], v_pair[2][2];     // scale and base
+            const uint8_t* const k_s = my_ring + j * Shape::kSlotBytes;
+            const uint32_t v_s = ring + j * Shape::kSlotBytes + Shape::kCodeBytes;
+            const uint32_t* const ks_s = reinterpret_cast<const uint32_t*>(k_s + 2 * Shape::kCodeBytes);
+            const uint32_t* const vs_s = ks_s + kQ4Tile;
+            const int32_t* const pos_s = reinterpret_cast<const int32_t*>(vs_s + kQ4Tile), * const doc_s = pos_s + kQ4Tile;
+            const int t0 = tile * kQ4Tile;
+            // ---- S^T = K Q^T for 32 keys: two blocks of sixteen
+            float2 x[2][RH][2];                      // [block][..][i]: key 8 i + gr, query rows 2 qd and 2 qd + 1
+            uint32_t k_pair[2][2], v_pair[2][2];     // scale and base
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    uint32_t kw[2][KW];
-                    float sum[RH][4];
+            for (int k = 0; k < 2; ++k) {
+                uint32_t kw[2][KW];
+                float sum[RH][4];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int key = 16 * k + 8 * i + gr;
-                        k_pair[k][i] = ks_s[key];
-                        v_pair[k][i] = vs_s[key];
-                        const uint8_t* const from = k_s + key * (D / 2) + qd * KW * 4;
-                        if (KW == 4) {
-                            const uint4 y = *reinterpret_cast<const uint4*>(from);
-                            kw[i][0] = y.x; kw[i][1] = y.y; kw[i][KW - 2] = y.z; kw[i][KW - 1] = y.w;
-                        } else {
-                            const uint2 y = *reinterpret_cast<const uint2*>(from);
-                            kw[i][0] = y.x; kw[i][1] = y.y;
-                        }
+                for (int i = 0; i < 2; ++i) {
+                    const int key = 16 * k + 8 * i + gr;
+                    k_pair[k][i] = ks_s[key];
+                    v_pair[k][i] = vs_s[key];
+                    const uint8_t* const from = k_s + key * (D / 2) + qd * KW * 4;
+                    if (KW == 4) {
+                        const uint4 y = *reinterpret_cast<const uint4*>(from);
+                        kw[i][0] = y.x; kw[i][1] = y.y; kw[i][KW - 2] = y.z; kw[i][KW - 1] = y.w;
+                    } else {
+                        const uint2 y = *reinterpret_cast<const uint2*>(from);
+                        kw[i][0] = y.x; kw[i][1] = y.y;
                     }
-#pragma unroll
-                    for (int n = 0; n < RH; ++n) sum[n][0] = sum[n][1] = sum[n][2] = sum[n][3] = 0.f;
-#pragma unroll
-                    for (int w = 0; w < KW; ++w) {
-                        const uint32_t y0 = kw[0][w], y1 = kw[1][w];
-                        const uint32_t z0 = y0 >> 8, z1 = y1 >> 8;
-#pragma unroll
-                        for (int n = 0; n < RH; ++n) {
-                            mma_f16(sum[n], y0 & kLow, y1 & kLow, y0 & kHigh, y1 & kHigh, qb[n][2 * w][0], qb[n][2 * w][1]);
-                            mma_f16(sum[n], z0 & kLow, z1 & kLow, z0 & kHigh, z1 & kHigh, qb[n][2 * w + 1][0], qb[n][2 * w + 1][1]);
-                        }
-                    }
-#pragma unroll
-                    for (int n = 0; n < RH; ++n) { x[k][n][0] = make_float2(sum[n][0], sum[n][1]); x[k][n][1] = make_float2(sum[n][2], sum[n][3]); }
                 }
-                if (kEdge) {                             // what stands behind the last row may be no number
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
+                for (int n = 0; n < RH; ++n) sum[n][0] = sum[n][1] = sum[n][2] = sum[n][3] = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            if (t0 + 16 * k + 8 * i + gr >= rows) k_pair[k][i] = v_pair[k][i] = 0u;
-                }
-                // ---- logits (base 2)
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float sk = lo_bf16(k_pair[k][i]), bk = hi_bf16(k_pair[k][i]);
-#pragma unroll
-                        for (int n = 0; n < RH; ++n)
-                            x[k][n][i] = make_float2(fmaf(sk, x[k][n][i].x, bk * q_sum[n].x) * factor[n].x, fmaf(sk, x[k][n][i].y, bk * q_sum[n].y) * factor[n].y);
-                    }
-                if (capped) {
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int n = 0; n < RH; ++n)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                float2& y = x[k][n][i];
-                                y.x = fmaf(-2.f * cap2, rcpf(1.f + ex2f(y.x * cap_in)), cap2);
-                                y.y = fmaf(-2.f * cap2, rcpf(1.f + ex2f(y.y * cap_in)), cap2);
-                            }
-                }
-                if (kEdge || biased) {
+                for (int w = 0; w < KW; ++w) {
+                    const uint32_t y0 = kw[0][w], y1 = kw[1][w];
+                    const uint32_t z0 = y0 >> 8, z1 = y1 >> 8;
 #pragma unroll
                     for (int n = 0; n < RH; ++n) {
-                        const RowNote r0 = table[8 * n + 2 * qd], r1 = table[8 * n + 2 * qd + 1];
-#pragma unroll
-                        for (int k = 0; k < 2; ++k)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const int key = 16 * k + 8 * i + gr, t = t0 + key;
-                                float2& y = x[k][n][i];
-                                if (biased) {
-                                    const float pos = float(pos_s[key] - pos_ref);
-                                    y.x = fmaf(-r0.slope2, fabsf(r0.pos - pos), y.x);
-                                    y.y = fmaf(-r1.slope2, fabsf(r1.pos - pos), y.y);
-                                }
-                                if (kEdge) {
-                                    const int doc = by_doc ? doc_s[key] : 0;
-                                    if (t > r0.lim || t >= rows || (by_doc && doc != r0.doc)) y.x = kNeg;
-                                    if (t > r1.lim || t >= rows || (by_doc && doc != r1.doc)) y.y = kNeg;
-                                }
-                            }
+                        mma_f16(sum[n], y0 & kLow, y1 & kLow, y0 & kHigh, y1 & kHigh, qb[n][2 * w][0], qb[n][2 * w][1]);
+                        mma_f16(sum[n], z0 & kLow, z1 & kLow, z0 & kHigh, z1 & kHigh, qb[n][2 * w + 1][0], qb[n][2 * w + 1][1]);
                     }
                 }
-                // ---- references: of the softmax per query row, of the scales per warp; raised when exceeded by 2^8 and 2^4
-                const float v_top = fmaxf(fmax3(lo_bf16(v_pair[0][0]), lo_bf16(v_pair[0][1]), lo_bf16(v_pair[1][0])), lo_bf16(v_pair[1][1]));
-                float2 mx[RH];
-                float over = v_top * (v_inv * (kLazy / 16.f));
 #pragma unroll
-                for (int n = 0; n < RH; ++n) {
-                    mx[n].x = fmaxf(fmax3(x[0][n][0].x, x[0][n][1].x, x[1][n][0].x), x[1][n][1].x);
-                    mx[n].y = fmaxf(fmax3(x[0][n][0].y, x[0][n][1].y, x[1][n][0].y), x[1][n][1].y);
-                    over = fmax3(over, mx[n].x - m_run[n].x, mx[n].y - m_run[n].y);
+                for (int n = 0; n < RH; ++n) { x[k][n][0] = make_float2(sum[n][0], sum[n][1]); x[k][n][1] = make_float2(sum[n][2], sum[n][3]); }
+            }
+            // ---- logits (base 2)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float sk = lo_bf16(k_pair[k][i]), bk = hi_bf16(k_pair[k][i]);
+#pragma unroll
+                    for (int n = 0; n < RH; ++n)
+                        x[k][n][i] = make_float2(fmaf(sk, x[k][n][i].x, bk * q_sum[n].x) * factor[n].x, fmaf(sk, x[k][n][i].y, bk * q_sum[n].y) * factor[n].y);
                 }
-                const bool raise = over > kLazy;
-                if (__any_sync(0xffffffffu, raise)) {
-                    // (the same power of two in all lanes; scales are not negative, so their bits are in order)
-                    const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(fminf(fmaxf(v_top, v_ref), kHuge))) & 0x7f800000u;
-                    v_inv = __uint_as_float((254u << 23) - top);
-                    const float shrink = v_ref * v_inv;
-                    v_ref = __uint_as_float(top);
-#pragma unroll
-                    for (int n = 0; n < RH; ++n) {
-                        float2 y = mx[n], alpha = make_float2(1.f, 1.f);
-#pragma unroll
-                        for (int d = 4; d < 32; d <<= 1) {
-                            y.x = fmaxf(y.x, __shfl_xor_sync(0xffffffffu, y.x, d));
-                            y.y = fmaxf(y.y, __shfl_xor_sync(0xffffffffu, y.y, d));
-                        }
-                        if (y.x > m_run[n].x + kLazy) { alpha.x = ex2f(m_run[n].x - y.x); m_run[n].x = y.x; }
-                        if (y.y > m_run[n].y + kLazy) { alpha.y = ex2f(m_run[n].y - y.y); m_run[n].y = y.y; }
-                        l_run[n] = __fmul2_rn(l_run[n], alpha);
-                        b_run[n] = __fmul2_rn(b_run[n], alpha);
-                        alpha.x *= shrink;
-                        alpha.y *= shrink;
-#pragma unroll
-                        for (int t = 0; t < MT; ++t) { acc[n][t][0] *= alpha.x; acc[n][t][1] *= alpha.y; acc[n][t][2] *= alpha.x; acc[n][t][3] *= alpha.y; }
-                    }
-                }
-                // ---- weights
-                uint32_t pb[2][RH][2];
+            if (capped) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float sv = lo_bf16(v_pair[k][i]) * v_inv, bv = hi_bf16(v_pair[k][i]);
-#pragma unroll
-                        for (int n = 0; n < RH; ++n) {
-                            const float2 y = __fadd2_rn(x[k][n][i], make_float2(-m_run[n].x, -m_run[n].y));
-                            float2 p = make_float2(ex2f(y.x), ex2f(y.y));
-                            if (kEdge) {                 // (a row that has seen nothing yet: its reference is as low)
-                                if (x[k][n][i].x == kNeg) p.x = 0.f;
-                                if (x[k][n][i].y == kNeg) p.y = 0.f;
-                            }
-                            l_run[n] = __fadd2_rn(l_run[n], p);
-                            b_run[n] = make_float2(fmaf(p.x, bv, b_run[n].x), fmaf(p.y, bv, b_run[n].y));
-                            pb[k][n][i] = transpose8(pack_f16(p.x * sv, p.y * sv));
-                        }
-                    }
-                // ---- O^T += V^T P^T: pieces of four codes (dimensions 4 gr to 4 gr + 3 of 32), two keys each
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int c = 0; c < D / 32; c += 2) {
-                        // matrices 1, 3: the second eight keys; 2, 3: the next sixteen bytes
-                        const int row = 16 * k + ((lane >> 3) & 1) * 8 + (lane & 7), chunk = c + (lane >> 4);
-                        uint32_t y[4];
-                        ldsm_x4_t(y, v_s + row * (D / 2) + ((NH == 2 ? chunk ^ ((row >> 1) & 3) : chunk ^ ((row >> 2) & 1)) << 4));
+                    for (int n = 0; n < RH; ++n)
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const uint32_t y0 = y[2 * i], y1 = y[2 * i + 1], z0 = y0 >> 8, z1 = y1 >> 8;
-                            const int t = 2 * (c + i);
+                            float2& y = x[k][n][i];
+                            y.x = fmaf(-2.f * cap2, rcpf(1.f + ex2f(y.x * cap_in)), cap2);
+                            y.y = fmaf(-2.f * cap2, rcpf(1.f + ex2f(y.y * cap_in)), cap2);
+                        }
+            }
+            if (biased) {
 #pragma unroll
-                            for (int n = 0; n < RH; ++n) {
-                                mma_f16(acc[n][t], y0 & kLow, y0 & kHigh, y1 & kLow, y1 & kHigh, pb[k][n][0], pb[k][n][1]);
-                                mma_f16(acc[n][t + 1], z0 & kLow, z0 & kHigh, z1 & kLow, z1 & kHigh, pb[k][n][0], pb[k][n][1]);
-                            }
+                for (int n = 0; n < RH; ++n) {
+                    const RowNote r0 = table[8 * n + 2 * qd], r1 = table[8 * n + 2 * qd + 1];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const float pos = float(pos_s[16 * k + 8 * i + gr] - pos_ref);
+                            float2& y = x[k][n][i];
+                            y.x = fmaf(-r0.slope2, fabsf(r0.pos - pos), y.x);
+                            y.y = fmaf(-r1.slope2, fabsf(r1.pos - pos), y.y);
+                        }
+                }
+            }
+            if (by_doc || t0 + 31 > lim_all) {           // some query row does not see all of the tile's keys
+                asm volatile("");                        // (a branch, and not all of it with predicates)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int key = 16 * k + 8 * i + gr, t = t0 + key, doc = by_doc ? doc_s[key] : 0;
+                        if (t >= rows) v_pair[k][i] = 0u;            // what stands behind the last row may be no number
+#pragma unroll
+                        for (int n = 0; n < RH; ++n) {
+                            const RowNote r0 = table[8 * n + 2 * qd], r1 = table[8 * n + 2 * qd + 1];
+                            if (t > r0.lim || t >= rows || (by_doc && doc != r0.doc)) x[k][n][i].x = -INFINITY;
+                            if (t > r1.lim || t >= rows || (by_doc && doc != r1.doc)) x[k][n][i].y = -INFINITY;
                         }
                     }
-            };
-            if (by_doc || tile * kQ4Tile + 31 > lim_all) step(std::true_type{});
-            else step(std::false_type{});
+            }
+            // ---- references: of the softmax per query row, of the scales per warp; raised when exceeded by 2^8 and 2^4
+            const float v_top = fmaxf(fmax3(lo_bf16(v_pair[0][0]), lo_bf16(v_pair[0][1]), lo_bf16(v_pair[1][0])), lo_bf16(v_pair[1][1]));
+            float2 mx[RH];
+            float over = v_top * (v_inv * (kLazy / 16.f));
+#pragma unroll
+            for (int n = 0; n < RH; ++n) {
+                mx[n].x = fmaxf(fmax3(x[0][n][0].x, x[0][n][1].x, x[1][n][0].x), x[1][n][1].x);
+                mx[n].y = fmaxf(fmax3(x[0][n][0].y, x[0][n][1].y, x[1][n][0].y), x[1][n][1].y);
+                over = fmax3(over, mx[n].x - m_run[n].x, mx[n].y - m_run[n].y);
+            }
+            const bool raise = over > kLazy;
+            if (__any_sync(0xffffffffu, raise)) {
+                // (the same power of two in all lanes; scales are not negative, so their bits are in order)
+                const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(fminf(fmaxf(v_top, v_ref), kHuge))) & 0x7f800000u;
+                v_inv = __uint_as_float((254u << 23) - top);
+                const float shrink = v_ref * v_inv;
+                v_ref = __uint_as_float(top);
+#pragma unroll
+                for (int n = 0; n < RH; ++n) {
+                    float2 y = mx[n], alpha = make_float2(1.f, 1.f);
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) {
+                        y.x = fmaxf(y.x, __shfl_xor_sync(0xffffffffu, y.x, d));
+                        y.y = fmaxf(y.y, __shfl_xor_sync(0xffffffffu, y.y, d));
+                    }
+                    if (y.x > m_run[n].x + kLazy) { alpha.x = ex2f(m_run[n].x - y.x); m_run[n].x = y.x; }
+                    if (y.y > m_run[n].y + kLazy) { alpha.y = ex2f(m_run[n].y - y.y); m_run[n].y = y.y; }
+                    l_run[n] = __fmul2_rn(l_run[n], alpha);
+                    b_run[n] = __fmul2_rn(b_run[n], alpha);
+                    alpha.x *= shrink;
+                    alpha.y *= shrink;
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) { acc[n][t][0] *= alpha.x; acc[n][t][1] *= alpha.y; acc[n][t][2] *= alpha.x; acc[n][t][3] *= alpha.y; }
+                }
+            }
+            // ---- weights
+            uint32_t pb[2][RH][2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float sv = lo_bf16(v_pair[k][i]) * v_inv, bv = hi_bf16(v_pair[k][i]);
+#pragma unroll
+                    for (int n = 0; n < RH; ++n) {
+                        const float2 y = __fadd2_rn(x[k][n][i], make_float2(-m_run[n].x, -m_run[n].y));
+                        float2 p = make_float2(ex2f(y.x), ex2f(y.y));
+                        l_run[n] = __fadd2_rn(l_run[n], p);
+                        b_run[n] = make_float2(fmaf(p.x, bv, b_run[n].x), fmaf(p.y, bv, b_run[n].y));
+                        pb[k][n][i] = transpose8(pack_f16(p.x * sv, p.y * sv));
+                    }
+                }
+            // ---- O^T += V^T P^T: pieces of four codes (dimensions 4 gr to 4 gr + 3 of 32), two keys each
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int c = 0; c < D / 32; c += 2) {
+                    // matrices 1, 3: the second eight keys; 2, 3: the next sixteen bytes
+                    const int row = 16 * k + ((lane >> 3) & 1) * 8 + (lane & 7), chunk = c + (lane >> 4);
+                    uint32_t y[4];
+                    ldsm_x4_t(y, v_s + row * (D / 2) + ((NH == 2 ? chunk ^ ((row >> 1) & 3) : chunk ^ ((row >> 2) & 1)) << 4));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t y0 = y[2 * i], y1 = y[2 * i + 1], z0 = y0 >> 8, z1 = y1 >> 8;
+                        const int t = 2 * (c + i);
+#pragma unroll
+                        for (int n = 0; n < RH; ++n) {
+                            mma_f16(acc[n][t], y0 & kLow, y0 & kHigh, y1 & kLow, y1 & kHigh, pb[k][n][0], pb[k][n][1]);
+                            mma_f16(acc[n][t + 1], z0 & kLow, z0 & kHigh, z1 & kLow, z1 & kHigh, pb[k][n][0], pb[k][n][1]);
+                        }
+                    }
+                }
             __syncwarp();
-            refill(j);
-            ++n_used;
         }
-        // ---- the item's end: sums over the lanes' keys
-#pragma unroll
-        for (int n = 0; n < RH; ++n)
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) {
-                l_run[n].x += __shfl_xor_sync(0xffffffffu, l_run[n].x, d);
-                l_run[n].y += __shfl_xor_sync(0xffffffffu, l_run[n].y, d);
-                b_run[n].x += __shfl_xor_sync(0xffffffffu, b_run[n].x, d);
-                b_run[n].y += __shfl_xor_sync(0xffffffffu, b_run[n].y, d);
-            }
-        const Segment seg = desk[1];
-        const int count = seg.x.count;
-        const bool begins = seg.lo == 0, ends = seg.hi >= seg.x.tiles;
-        if (!begins) { note_front = seg.item; note_ends = ends; }
-        else if (!ends) note_back = seg.item;
-        // (a back piece is the last thing that its warp has: nothing is on its way into the ring any more)
-        float* const piece = reinterpret_cast<float*>(begins ? my_ring : base_ptr + Shape::kFront + warp * Shape::kPieceBytes);
-#pragma unroll
-        for (int n = 0; n < RH; ++n)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int m = 8 * n + 2 * qd + c;
-                if (biased && fabsf(table[m].pos) > kFarToken) atomicOr(a.status, CSP_DEV_BAD_LEN);
-                if (m >= count * G) continue;
-                const float base_sum = c ? b_run[n].y : b_run[n].x, l = c ? l_run[n].y : l_run[n].x, mm = c ? m_run[n].y : m_run[n].x;
-                const int tok = m / G, head = seg.h * G + m - tok * G;
-                const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, mm) + l);      // l == 0: nothing was seen
-                uint16_t* const out = a.out + int64_t(seg.b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(seg.x.tok0 + tok) * a.o_st + 4 * gr;
-#pragma unroll
-                for (int t = 0; t < MT; t += 2) {        // dimensions 16 t + 4 gr to 16 t + 4 gr + 3
-                    const float4 o = make_float4(fmaf(acc[n][t][c] * 0x1p24f, v_ref, base_sum), fmaf(acc[n][t][2 + c] * 0x1p20f, v_ref, base_sum),
-                                                 fmaf(acc[n][t + 1][c] * 0x1p24f, v_ref, base_sum), fmaf(acc[n][t + 1][2 + c] * 0x1p20f, v_ref, base_sum));
-                    if (begins && ends)
-                        *reinterpret_cast<uint2*>(out + 16 * t) = l == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-                    else
-                        *reinterpret_cast<float4*>(piece + m * Shape::kPieceRow + 16 * t + 4 * gr) = o;
-                }
-                if (gr == 0) {
-                    if (!(begins && ends)) *reinterpret_cast<float2*>(piece + m * Shape::kPieceRow + D) = make_float2(mm, l);
-                    else if (a.lse)
-                        a.lse[(int64_t(seg.b) * a.n_kv_heads * G + head) * a.max_new + seg.x.tok0 + tok] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
-                }
-            }
+        }
+        refill(j);
     }
     if (lane == 0) notes[warp] = Notes{note_front, note_ends, note_back, 0};
     __syncthreads();
@@ -607,7 +600,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         const PairRange x = pair_range(a, pl, u, item - u * pl.n_pairs);
         const int w0 = c == 0 ? 0 : c - 1;               // pieces: of warps w0 up to next - 1
         constexpr int C = D / 32;                        // columns per lane
-        for (int m = warp; m < x.count * G; m += NW) {
+        for (int m = (warp + NW - c % NW) % NW; m < x.count * G; m += NW) {    // (another chain begins with another warp)
             auto piece = [&](int w) {
                 return reinterpret_cast<const float*>(c > 0 && w == w0 ? base_ptr + w * NST * Shape::kSlotBytes : base_ptr + Shape::kFront + w * Shape::kPieceBytes) + m * Shape::kPieceRow;
             };
