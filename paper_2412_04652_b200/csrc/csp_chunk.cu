@@ -806,31 +806,6 @@ void join_parts(const ChunkArgs& a, const ChunkPlan& pl, const ChunkParts* parts
 // to eight rows it is faster everywhere; from there to sixteen the two are about even, and here only the result is rounded.
 constexpr int kFewRows = 16;
 
-ChunkPlan chunk_plan(const csp_params& p, int max_new) {
-    ChunkPlan pl;
-    const int G = p.n_q_heads / p.n_kv_heads;
-    pl.tok_tile = 128 / G;
-    pl.drawn = false;
-    pl.n_pairs = (max_new + 2 * pl.tok_tile - 1) / (2 * pl.tok_tile);
-    if (pl.n_pairs < 1) pl.n_pairs = 1;
-    pl.row_slots = (max_new < 2 * pl.tok_tile ? max_new : 2 * pl.tok_tile) * G;
-    const bool few = pl.row_slots <= kFewRows;
-    pl.key_tile = few ? 64 : kTileKeys;
-    pl.min_tiles = 2;
-    pl.item_cost = 2;
-    // A cut costs a row pair about four tiles (256 rows of partial results and their joining), few rows next to nothing,
-    // but there an uneven share costs nothing either: HBM is the bound, whoever reads.  1 K tokens over 8 K - 32 K: 923 us without
-    // this limit, 850 - 870 with 4, 862 with 2, 840 - 874 with 0; one token, serving batch: 103 us without, 104 with 8, 100 with 1.
-    pl.snap = few ? 0x3fffffff : 4;
-    const int64_t items = int64_t(p.batch) * p.n_kv_heads * pl.n_pairs;
-    const int64_t weight = (int64_t(p.out_capacity) + pl.key_tile - 1) / pl.key_tile + pl.item_cost;      // of an item, at most
-    pl.n_items = items > 0x3fffffffLL / weight ? -1 : int(items);
-    // no more blocks than there can be shares of the smallest size
-    const int64_t most = (items > 65536 ? 65536 : items) * weight / (pl.item_cost + pl.min_tiles) + 1;
-    pl.grid = most < sm_count() ? int(most) : sm_count();
-    return pl;
-}
-
 template <int NH, bool kCap, bool kBias, bool kDoc>
 csp_status launch_variant(const ChunkArgs& a, const ChunkPlan& pl, const CUtensorMap& tq, const CUtensorMap& tk,
                           const CUtensorMap& tv, ChunkParts* parts, float* partial, float2* ml, cudaStream_t s) {
@@ -860,6 +835,31 @@ csp_status launch_nh(const ChunkArgs& a, const ChunkPlan& pl, const CUtensorMap&
 }
 
 }  // namespace
+
+ChunkPlan chunk_plan(const csp_params& p, int max_new) {
+    ChunkPlan pl;
+    const int G = p.n_q_heads / p.n_kv_heads;
+    pl.tok_tile = 128 / G;
+    pl.drawn = false;
+    pl.n_pairs = (max_new + 2 * pl.tok_tile - 1) / (2 * pl.tok_tile);
+    if (pl.n_pairs < 1) pl.n_pairs = 1;
+    pl.row_slots = (max_new < 2 * pl.tok_tile ? max_new : 2 * pl.tok_tile) * G;
+    const bool few = pl.row_slots <= kFewRows;
+    pl.key_tile = few ? 64 : kTileKeys;
+    pl.min_tiles = 2;
+    pl.item_cost = 2;
+    // A cut costs a row pair about four tiles (256 rows of partial results and their joining), few rows next to nothing,
+    // but there an uneven share costs nothing either: HBM is the bound, whoever reads.  1 K tokens over 8 K - 32 K: 923 us without
+    // this limit, 850 - 870 with 4, 862 with 2, 840 - 874 with 0; one token, serving batch: 103 us without, 104 with 8, 100 with 1.
+    pl.snap = few ? 0x3fffffff : 4;
+    const int64_t items = int64_t(p.batch) * p.n_kv_heads * pl.n_pairs;
+    const int64_t weight = (int64_t(p.out_capacity) + pl.key_tile - 1) / pl.key_tile + pl.item_cost;      // of an item, at most
+    pl.n_items = items > 0x3fffffffLL / weight ? -1 : int(items);
+    // no more blocks than there can be shares of the smallest size
+    const int64_t most = (items > 65536 ? 65536 : items) * weight / (pl.item_cost + pl.min_tiles) + 1;
+    pl.grid = most < sm_count() ? int(most) : sm_count();
+    return pl;
+}
 
 PartialLayout partial_layout(const csp_params& p, const ChunkPlan& pl) {
     PartialLayout x;

@@ -29,6 +29,11 @@ PartialLayout partial_layout(const csp_params& p, const ChunkPlan& pl);
 csp_status launch_chunk_join(const csp_params& p, const ChunkArgs& a, const ChunkPlan& pl, bool few, ChunkParts* parts,
                              float* partial, float2* ml, cudaStream_t s);
 
+// how a chunk of bf16 queries is cut into items; for more than sixteen query rows per KV head a cache in 4 bits is cut alike
+ChunkPlan chunk_plan(const csp_params& p, int max_new);
+csp_status launch_chunk_q4_many(const csp_params& p, const ChunkArgs& a, const ChunkPlan& pl, const csp_tensor& q, const Q4Args& c,
+                                ChunkParts* parts, float* partial, float2* ml, cudaStream_t s);
+
 csp_status launch_chunk_few(const csp_params& p, const ChunkArgs& a, const ChunkPlan& pl, const csp_tensor& q,
                             const CUtensorMap& tk, const CUtensorMap& tv, ChunkParts* parts, float* partial, float2* ml,
                             cudaStream_t s);

@@ -647,22 +647,16 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
 
 // ---- host side -----------------------------------------------------------------------------------------------------
 
-constexpr int kQ4Rows = 16;                              // query rows of an item at most
+constexpr int kQ4Rows = 16;                              // query rows per KV head up to which this kernel is taken
 
 ChunkPlan chunk_q4_plan(const csp_params& p, int max_new) {
-    ChunkPlan pl;
     const int G = p.n_q_heads / p.n_kv_heads;
-    // (an item has 2 tok_tile tokens)
-    pl.tok_tile = int64_t(max_new) * G <= kQ4Rows ? kQ4Rows : kQ4Rows / 2 / G;
-    pl.drawn = false;
-    pl.n_pairs = max_new / (2 * pl.tok_tile) + (max_new % (2 * pl.tok_tile) ? 1 : 0);
-    if (pl.n_pairs < 1) pl.n_pairs = 1;
-    pl.row_slots = (max_new < 2 * pl.tok_tile ? max_new : 2 * pl.tok_tile) * G;
+    ChunkPlan pl = chunk_plan(p, max_new);
+    if (int64_t(max_new) * G > kQ4Rows) return pl;
     pl.key_tile = kQ4Tile;
     pl.min_tiles = 4;
     pl.item_cost = 4;
-    pl.snap = 0x3fffffff;
-    const int64_t items = int64_t(p.batch) * p.n_kv_heads * pl.n_pairs;
+    const int64_t items = int64_t(p.batch) * p.n_kv_heads;       // (n_pairs is 1)
     const int64_t weight = (int64_t(p.out_capacity) + pl.key_tile - 1) / pl.key_tile + pl.item_cost;      // of an item, at most
     pl.n_items = items > 0x3fffffffLL / weight ? -1 : int(items);
     // no more blocks than there can be shares of the smallest size
@@ -705,20 +699,25 @@ size_t chunk_q4_workspace_bytes(const csp_params& p, int max_new) {
 }
 
 csp_status launch_chunk_q4(const csp_params& p, const ChunkArgs& a, const csp_tensor& q, const Q4Args& c, void* ws, cudaStream_t s) {
-    const ChunkPlan pl = chunk_q4_plan(p, a.max_new);
+    ChunkPlan pl = chunk_q4_plan(p, a.max_new);
     const PartialLayout lay = partial_layout(p, pl);
     ChunkParts* const parts = reinterpret_cast<ChunkParts*>(static_cast<char*>(ws) + lay.parts);
     float* const partial = reinterpret_cast<float*>(static_cast<char*>(ws) + lay.o);
     float2* const ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + lay.ml);
-    const FewQuery qy = {static_cast<const uint16_t*>(q.ptr), q.stride_b, q.stride_h, q.stride_t};
     csp_status st;
-    if (pl.row_slots <= 8)
-        st = p.head_dim == 64 ? launch_few<1, 1>(a, pl, qy, c, parts, partial, ml, s) : launch_few<2, 1>(a, pl, qy, c, parts, partial, ml, s);
-    else
-        st = p.head_dim == 64 ? launch_few<1, 2>(a, pl, qy, c, parts, partial, ml, s) : launch_few<2, 2>(a, pl, qy, c, parts, partial, ml, s);
+    if (pl.row_slots > kQ4Rows) {
+        pl.drawn = a.mods.documents && pl.n_items >= 2 * pl.grid;
+        st = launch_chunk_q4_many(p, a, pl, q, c, parts, partial, ml, s);
+    } else {
+        const FewQuery qy = {static_cast<const uint16_t*>(q.ptr), q.stride_b, q.stride_h, q.stride_t};
+        if (pl.row_slots <= 8)
+            st = p.head_dim == 64 ? launch_few<1, 1>(a, pl, qy, c, parts, partial, ml, s) : launch_few<2, 1>(a, pl, qy, c, parts, partial, ml, s);
+        else
+            st = p.head_dim == 64 ? launch_few<1, 2>(a, pl, qy, c, parts, partial, ml, s) : launch_few<2, 2>(a, pl, qy, c, parts, partial, ml, s);
+    }
     // nothing is cut by a single block, and where two parts of min_tiles are more than a cache has
     if (st != CSP_OK || pl.grid == 1 || p.out_capacity <= (2 * pl.min_tiles - 1) * pl.key_tile) return st;
-    return launch_chunk_join(p, a, pl, true, parts, partial, ml, s);
+    return launch_chunk_join(p, a, pl, pl.row_slots <= kQ4Rows, parts, partial, ml, s);
 }
 
 }  // namespace csp
