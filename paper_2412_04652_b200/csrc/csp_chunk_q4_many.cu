@@ -2,13 +2,14 @@
 // for a bf16 cache (two row tiles to an item, one CTA per SM, equal shares of all 128-key tiles), except that a tile of keys is
 // unpacked on its way.
 //
-// A row is base + scale code.  The products see the codes, exactly: a half whose lowest four bits are a code is the number
+// A row is base + scale code.  Of K the products see the codes, exactly: a half whose lowest four bits are a code is the number
 // code 2^-24, with the code in the next four bits it is code 2^-20, so that unpacking eight codes takes four ANDs and a
 // shift and no arithmetic.  S = Q' codes^T with Q' the query in halves, scaled by a power of two per row (largest value in [1, 2)) and by
-// 16 where a code is in the lower place; then
-//   logit = up (scale_t S + base_t sum Q'),   O = sum_t (p_t scale'_t) code'_t + sum_t p_t base'_t,
-// with the two numbers of a row applied in fp32 by the softmax threads: nothing of K is rounded, and a weight times its
-// row's scale is rounded to a half (11 bits) relative to a power of two that follows the largest scale of the item.
+// 16 where a code is in the lower place; then  logit = up (scale_t S + base_t sum Q')  with the two numbers of a row applied in fp32
+// by the softmax threads: nothing of K is rounded.  (Half of the products scale x code would not fit the eleven bits of a half.)
+// Of V they see the values base + scale code, rounded to halves relative to a power of two that follows the largest value of
+// the item; the weights are rounded to halves as well.  (Applied to the weights instead, scale and base of V cost the softmax threads
+// another two of seven instructions per logit: 1.37 ms for the largest case below.)
 //
 // Inside a CTA
 //   warp 16     producer: looks up pages, brings the scales and bases of a tile's keys (and positions, documents) beside the entry
@@ -63,10 +64,27 @@ __device__ __forceinline__ uint32_t max_abs2(uint32_t x, uint32_t y) {
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-// eight codes -> eight halves, values 0, 4, 1, 5, 2, 6, 3, 7 of the word
-__device__ __forceinline__ uint4 unpack_eight(uint32_t x) {
+// eight codes -> eight halves, values 0, 4, 1, 5, 2, 6, 3, 7 of the word: for K as they are (times 2^-24, the odd ones 2^-20) ...
+__device__ __forceinline__ uint4 unpack_codes(uint32_t x) {
     const uint32_t y = x >> 8;
     return make_uint4(x & kLow, x & kHigh, y & kLow, y & kHigh);
+}
+// ... for V with scale and base (both halves of `scale` and of `base` the same): 1024 + code and 1024 + 16 code are exact, and
+// so is the code taken from them; one rounding
+__device__ __forceinline__ uint32_t fma_f16(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t low_values(uint32_t x, uint32_t scale, uint32_t base) {
+    return fma_f16(fma_f16((x & kLow) | 0x64006400u, 0x3c003c00u, 0xe400e400u), scale, base);        // x - 1024
+}
+__device__ __forceinline__ uint32_t high_values(uint32_t x, uint32_t scale, uint32_t base) {
+    return fma_f16(fma_f16((x & kHigh) | 0x64006400u, 0x2c002c00u, 0xd400d400u), scale, base);       // x / 16 - 64
+}
+__device__ __forceinline__ uint4 unpack_values(uint32_t x, uint32_t scale, uint32_t base) {
+    const uint32_t y = x >> 8;
+    return make_uint4(low_values(x, scale, base), high_values(x, scale, base), low_values(y, scale, base), high_values(y, scale, base));
 }
 
 struct ManySmem { uint32_t q, raw, meta, entries, pair, join, rows, bars, misc, total; };
@@ -76,8 +94,8 @@ struct ManyShape {
     static constexpr uint32_t kStageBytes = NH * kBlockBytes;            // one tile of K or of V in halves
     static constexpr uint32_t kQBytes = NH * kBlockBytes;                // one row tile of Q
     static constexpr uint32_t kRawBytes = kStageBytes / 4;               // one tile of K or of V in 4 bits
-    // [128] scale of K, base of K, scale of V, base of V, (position, document)
-    static constexpr uint32_t kMetaBytes = (kMeta ? 6 : 4) * kTileKeys * 4;
+    // [128] scale of K, base of K, scale and base of V in halves, (position, document)
+    static constexpr uint32_t kMetaBytes = (kMeta ? 5 : 3) * kTileKeys * 4, kPositions = 3 * kTileKeys * 4, kDocuments = 4 * kTileKeys * 4;
     static constexpr int kBars = 2 * kStages + 2 * kEntries + 6 + 6 + 2 + 8;
     __host__ __device__ static constexpr ManySmem plan() {
         ManySmem s = {};
@@ -87,7 +105,7 @@ struct ManyShape {
         s.meta = off;    off += kEntries * kMetaBytes;
         s.entries = off; off += kEntries * kEntryWords * 4;
         s.pair = off;    off += 2 * 4 * 128 * 4;                         // [parity][group][half][row]: exchanged by the halves of a row
-        s.join = off;    off += 4 * 2 * 128 * 4;                         // [what][group][row]: reference, sum, base part, scales' reference
+        s.join = off;    off += 3 * 2 * 128 * 4;                         // [what][group][row]: reference, sum, the values' reference
         s.rows = off;    off += 2 * 128 * 8;                             // [slot][row]: factor of the logits, sum of the query
         s.bars = off;    off += kBars * 8;
         s.misc = off;    off += 32;
@@ -262,7 +280,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
             int d_next[4] = {0, 0, 0, 0}, p_next[4] = {0, 0, 0, 0};
             uint4 ks_next = make_uint4(0, 0, 0, 0), vs_next = ks_next;       // scales and bases of keys 4 lane to 4 lane + 3
             int page_next = -1;                          // -1: outside the pool, zeros
-            float v_ref = kTiny;                         // power of two that the scales of V are relative to
+            float v_ref = kTiny;                         // power of two that the values of V are relative to
             auto fetch_scales = [&](int tile, int page) {
                 page_next = page >= 0 && page < a.n_pages ? page : -1;
                 ks_next = vs_next = make_uint4(0, 0, 0, 0);
@@ -322,9 +340,9 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                     const bool in = t0 + 4 * lane + j < x.rows;
                     sk[j] = in ? lo_bf16(kp[j]) : 0.f; bk[j] = in ? hi_bf16(kp[j]) : 0.f;
                     sv[j] = in ? lo_bf16(vp[j]) : 0.f; bv[j] = in ? hi_bf16(vp[j]) : 0.f;
-                    v_top = fmaxf(v_top, sv[j]);
+                    v_top = fmaxf(v_top, fmaxf(fabsf(bv[j]), fabsf(fmaf(15.f, sv[j], bv[j]))));
                 }
-                // (scales are not negative, so their bits are in order)
+                // (magnitudes: their bits are in order)
                 const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(fminf(v_top, kHuge))) & 0x7f800000u;
                 if (__uint_as_float(top) > 16.f * v_ref || v_ref == kTiny) v_ref = fmaxf(__uint_as_float(top), kTiny);
                 if (page < 0 && lane == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
@@ -342,11 +360,12 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 float4* const numbers = reinterpret_cast<float4*>(base_ptr + sp.meta + e * Shape::kMetaBytes);
                 numbers[lane] = make_float4(sk[0], sk[1], sk[2], sk[3]);
                 numbers[lane + 32] = make_float4(bk[0], bk[1], bk[2], bk[3]);
-                numbers[lane + 64] = make_float4(sv[0], sv[1], sv[2], sv[3]);
-                numbers[lane + 96] = make_float4(bv[0], bv[1], bv[2], bv[3]);
+                const float v_inv = 1.f / v_ref;
+                reinterpret_cast<uint4*>(numbers)[lane + 64] = make_uint4(pack_f16(sv[0] * v_inv, bv[0] * v_inv), pack_f16(sv[1] * v_inv, bv[1] * v_inv),
+                                                                          pack_f16(sv[2] * v_inv, bv[2] * v_inv), pack_f16(sv[3] * v_inv, bv[3] * v_inv));
                 if (kMeta) {
-                    float* const mp = reinterpret_cast<float*>(base_ptr + sp.meta + e * Shape::kMetaBytes + 2048);
-                    int32_t* const md = reinterpret_cast<int32_t*>(base_ptr + sp.meta + e * Shape::kMetaBytes + 2560);
+                    float* const mp = reinterpret_cast<float*>(base_ptr + sp.meta + e * Shape::kMetaBytes + Shape::kPositions);
+                    int32_t* const md = reinterpret_cast<int32_t*>(base_ptr + sp.meta + e * Shape::kMetaBytes + Shape::kDocuments);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         if (kBias) mp[lane + 32 * j] = float(p_now[j] - pos_ref);
@@ -469,7 +488,9 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
         constexpr int kRowStep = kThreads / kRowPieces;
         const uint32_t raw = base + sp.raw + ut * 16;
         uint32_t n_entry = 0, n_copied = 0, n_done = 0;
+        int entry_of[kRawTiles] = {};                    // of the tiles that have been copied, the oldest first
         auto unpack = [&] {                              // the oldest tile that has been copied
+            const uint32_t* const v_numbers = reinterpret_cast<const uint32_t*>(base_ptr + sp.meta + entry_of[0] * Shape::kMetaBytes + 2 * kTileKeys * 4);
             if (n_copied - n_done == kRawTiles) asm volatile("cp.async.wait_group %0;" ::"n"(kRawTiles - 1) : "memory");
             else asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll 1
@@ -488,15 +509,24 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                     if (turn) x = make_uint4(x.z, x.w, x.x, x.y);
                     uint8_t* const line = to + (piece >> 1) * kBlockBytes + row * 128;
                     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    auto place = [&](int j) { return reinterpret_cast<uint4*>(line + ((((piece & 1) * 4 + (j ^ turn)) ^ (row & 7)) << 4)); };
+                    if (which == 0) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        *reinterpret_cast<uint4*>(line + ((((piece & 1) * 4 + (j ^ turn)) ^ (row & 7)) << 4)) = unpack_eight(w[j]);
+                        for (int j = 0; j < 4; ++j) *place(j) = unpack_codes(w[j]);
+                    } else {
+                        const uint32_t pair = v_numbers[row], scale = __byte_perm(pair, pair, 0x1010), zero = __byte_perm(pair, pair, 0x3232);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) *place(j) = unpack_values(w[j], scale, zero);
+                    }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(kv_full + 8 * s);
             }
             ++n_done;
+            if (lane == 0) mbar_arrive(ent_empty + 8 * entry_of[0]);
+#pragma unroll
+            for (int i = 1; i < kRawTiles; ++i) entry_of[i - 1] = entry_of[i];
         };
         for (;;) {
             const uint32_t e = n_entry % kEntries, parity = (n_entry / kEntries) & 1u;
@@ -506,12 +536,17 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
             if (warp_aborted(abort_flag)) break;
             const int32_t* const en = entries + e * kEntryWords;
             const int flags = en[kFlags], page = en[kPage], row0 = en[kPageRow], h = en[kHead];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(ent_empty + 8 * e);
             ++n_entry;
-            if (flags & kStop) break;
-            if (flags & kEnd) continue;
+            if (flags & (kStop | kEnd)) {                // (the entry of a tile is held until the tile has been unpacked)
+                __syncwarp();
+                if (lane == 0) mbar_arrive(ent_empty + 8 * e);
+                if (flags & kStop) break;
+                continue;
+            }
             if (n_copied - n_done == kRawTiles) unpack();
+#pragma unroll
+            for (int i = 0; i < kRawTiles; ++i)
+                if (int(n_copied - n_done) == i) entry_of[i] = int(e);
             if (page >= 0) {
                 // (pieces lie one behind the other: all rows of a head in a page are neighbours)
                 const int64_t at = int64_t(row0) * (D / 2) + ut * 16;
@@ -540,7 +575,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
         // capped: x = c tanh(o / c) = c - 2 c / (1 + e^{2 o / c}), all in the base-2 domain
         const float cap2 = kCap ? a.mods.softcap * kLog2e : 0.f, cap_in = kCap ? 2.f / a.mods.softcap : 0.f;
         uint32_t n_entry = 0, n_mine = 0, n_join = 0, n_pair = 0, q_uses = 0;        // q_uses: bit s, the parity of slot s
-        float m_run = kNeg, l_run = 0.f, b_run = 0.f, v_run = kTiny;        // b_run: sum of weight times base
+        float m_run = kNeg, l_run = 0.f, v_run = kTiny;
         float factor = 0.f, q_sum = 0.f;                 // logit = factor (scale S + base q_sum)
         int lim = -1, q_doc = 0, rows = 0;
         float q_pos = 0.f, slope2 = 0.f;
@@ -584,7 +619,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 lim = !valid ? kSeesAll : r >= 0 ? max(r, en[kPrefix] - 1) : -1;
                 live = __any_sync(0xffffffffu, valid);
                 m_run = kNeg;
-                l_run = b_run = 0.f;
+                l_run = 0.f;
                 v_run = kTiny;
                 if ((flags & (kEnd | kHasQ)) != kEnd) {  // (an item without any tile may come without its queries)
                     const int slot = big ? g : (flags & kSlot1) ? 1 : 0;
@@ -669,13 +704,14 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
 #pragma unroll
                         for (int c = 0; c < 32; c += 4) {
                             const float4 sk = numbers[8 * j + (c >> 2)], bk = numbers[32 + 8 * j + (c >> 2)];
-                            const float2 y0 = __fmul2_rn(__ffma2_rn(make_float2(sk.x, sk.y), make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), __fmul2_rn(make_float2(bk.x, bk.y), q2)), f2);
-                            const float2 y1 = __fmul2_rn(__ffma2_rn(make_float2(sk.z, sk.w), make_float2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), __fmul2_rn(make_float2(bk.z, bk.w), q2)), f2);
+                            float2 y0 = __ffma2_rn(make_float2(sk.x, sk.y), make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), __fmul2_rn(make_float2(bk.x, bk.y), q2));
+                            float2 y1 = __ffma2_rn(make_float2(sk.z, sk.w), make_float2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), __fmul2_rn(make_float2(bk.z, bk.w), q2));
+                            if (kCap || kBias) { y0 = __fmul2_rn(y0, f2); y1 = __fmul2_rn(y1, f2); }     // (else when the weights are computed)
                             v[c] = __float_as_uint(y0.x); v[c + 1] = __float_as_uint(y0.y);
                             v[c + 2] = __float_as_uint(y1.x); v[c + 3] = __float_as_uint(y1.y);
                         }
                         if (kCap || kBias) {
-                            const float4* const mp = reinterpret_cast<const float4*>(base_ptr + sp.meta + e * Shape::kMetaBytes + 2048 + 256 * half) + 8 * j;
+                            const float4* const mp = reinterpret_cast<const float4*>(base_ptr + sp.meta + e * Shape::kMetaBytes + Shape::kPositions + 256 * half) + 8 * j;
 #pragma unroll
                             for (int c = 0; c < 32; c += 4) {
                                 float4 pos = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -691,7 +727,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                             }
                         }
                         if (kDoc) {
-                            const int4* const md = reinterpret_cast<const int4*>(base_ptr + sp.meta + e * Shape::kMetaBytes + 2560 + 256 * half) + 8 * j;
+                            const int4* const md = reinterpret_cast<const int4*>(base_ptr + sp.meta + e * Shape::kMetaBytes + Shape::kDocuments + 256 * half) + 8 * j;
 #pragma unroll
                             for (int c = 0; c < 32; c += 4) {
                                 const int4 d4 = md[c >> 2];
@@ -717,6 +753,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                         mx = fmax3_nan(fmax3_nan(m4[0], m4[1], m4[2]), m4[3], m4[3]);
                     }
                     tc_wait_st();
+                    if (!(kCap || kBias)) mx *= factor;
                     const float mx_other = other_half(mx);
                     mx = fmax3_nan(mx, mx_other, mx_other);
                     // (a NaN among the logits raises the reference to NaN, and the whole row with it)
@@ -740,13 +777,11 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                             }
                         }
                         l_run *= alpha;
-                        b_run *= alpha;
                         m_run = m_new;
                     }
                     const float ref = m_run == kNeg ? 0.f : m_run;    // a row that has seen nothing yet: all weights zero
-                    const float v_inv = 1.f / v_run;
-                    const float2 neg = make_float2(-ref, -ref), vi = make_float2(v_inv, v_inv);
-                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)}, bsum[2] = {sum[0], sum[0]};
+                    const float2 neg = make_float2(-ref, -ref), f2 = make_float2(factor, factor);
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
                     for (int j = 0; j < 2; ++j) {
                         uint32_t v[32], pk[16];
@@ -754,23 +789,16 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                         tc_wait_ld();
                         tc_loaded(v);
 #pragma unroll
-                        for (int c = 0; c < 32; c += 4) {
-                            const float4 sv = numbers[64 + 8 * j + (c >> 2)], bv = numbers[96 + 8 * j + (c >> 2)];
-                            const float2 x0 = __fadd2_rn(make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), neg);
-                            const float2 x1 = __fadd2_rn(make_float2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), neg);
-                            const float2 p0 = ex2f2(x0), p1 = ex2f2(x1);
-                            sum[0] = __fadd2_rn(sum[0], p0);
-                            sum[1] = __fadd2_rn(sum[1], p1);
-                            bsum[0] = __ffma2_rn(p0, make_float2(bv.x, bv.y), bsum[0]);
-                            bsum[1] = __ffma2_rn(p1, make_float2(bv.z, bv.w), bsum[1]);
-                            const float2 w0 = __fmul2_rn(p0, __fmul2_rn(make_float2(sv.x, sv.y), vi)), w1 = __fmul2_rn(p1, __fmul2_rn(make_float2(sv.z, sv.w), vi));
-                            pk[c >> 1] = pack_f16(w0.x, w0.y);
-                            pk[(c >> 1) + 1] = pack_f16(w1.x, w1.y);
+                        for (int c = 0; c < 32; c += 2) {
+                            float2 x = make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+                            x = kCap || kBias ? __fadd2_rn(x, neg) : __ffma2_rn(x, f2, neg);
+                            const float2 p = ex2f2(x);
+                            sum[c / 2 % 2] = __fadd2_rn(sum[c / 2 % 2], p);
+                            pk[c >> 1] = pack_f16(p.x, p.y);
                         }
                         tc_st_row16(my_s + 16u * j, pk);
                     }
                     l_run += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                    b_run += (bsum[0].x + bsum[0].y) + (bsum[1].x + bsum[1].y);
                     tc_wait_st();
                 }
                 tc_fence_before();
@@ -789,7 +817,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
             if (kBias && fabsf(q_pos) > kFarToken) atomicOr(a.status, CSP_DEV_BAD_LEN);
             if (started) warp_wait(pv_done + 8 * g, (n_mine - 1u) & 1u, abort_flag);
             tc_fence_after();
-            float l_all = l_run + other_half(l_run), b_all = b_run + other_half(b_run);
+            float l_all = l_run + other_half(l_run);
             float m_all = m_run, w0 = v_run, w1 = 0.f;       // w0, w1: what the two groups' products are multiplied by
             bool has0 = started, has1 = false;
             if (!big) {
@@ -797,8 +825,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 if (half == 0) {
                     join_buf[g * 128 + m] = m_run;
                     join_buf[256 + g * 128 + m] = started ? l_all : __uint_as_float(kUnset);     // the group had no tile: its O is not set
-                    join_buf[512 + g * 128 + m] = b_all;
-                    join_buf[768 + g * 128 + m] = v_run;
+                    join_buf[512 + g * 128 + m] = v_run;
                 }
                 join();
                 const float m0 = join_buf[m], m1 = join_buf[128 + m], l0 = join_buf[256 + m], l1 = join_buf[384 + m];
@@ -808,9 +835,8 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 w0 = ex2f(m0 - m_all);
                 w1 = ex2f(m1 - m_all);
                 l_all = (has0 ? l0 * w0 : 0.f) + (has1 ? l1 * w1 : 0.f);
-                b_all = (has0 ? join_buf[512 + m] * w0 : 0.f) + (has1 ? join_buf[640 + m] * w1 : 0.f);
-                w0 *= join_buf[768 + m];
-                w1 *= join_buf[896 + m];
+                w0 *= join_buf[512 + m];
+                w1 *= join_buf[640 + m];
             }
             if (live) {
                 const int local = m / G, head = h * G + m - local * G, tok = tok0 + (big ? g * pl.tok_tile : 0) + local;
@@ -832,11 +858,10 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                     tc_wait_ld();
                     float o[16];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {       // dimension c + j; even ones are codes 2^-24, odd ones codes 2^-20
+                    for (int j = 0; j < 16; ++j) {       // dimension c + j
                         const int d = j & 7, at = (j & 8) + (d < 4 ? 2 * d : 2 * d - 7);
-                        const float up = j & 1 ? 0x1p20f : 0x1p24f;
-                        const float y0 = has0 ? __uint_as_float(x0[at]) * up * w0 : 0.f, y1 = has1 ? __uint_as_float(x1[at]) * up * w1 : 0.f;
-                        o[j] = zero ? 0.f : ((y0 + y1) + b_all) * inv;
+                        const float y0 = has0 ? __uint_as_float(x0[at]) * w0 : 0.f, y1 = has1 ? __uint_as_float(x1[at]) * w1 : 0.f;
+                        o[j] = zero ? 0.f : (y0 + y1) * inv;
                     }
                     if (!valid) continue;
                     if (final) {
