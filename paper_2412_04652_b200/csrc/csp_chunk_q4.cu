@@ -78,7 +78,7 @@ __device__ __forceinline__ float hi_bf16(uint32_t x) { return __uint_as_float(x 
 template <int NH, int RH>   // head_dim = 64 NH, 8 RH query rows
 struct Q4Shape {
     static constexpr int D = 64 * NH, R = 8 * RH;
-    static constexpr int kWarps = RH == 1 ? 16 : 12;
+    static constexpr int kWarps = RH == 1 ? 12 : 8;
     static constexpr int kSlots = NH == 2 ? 2 : 4;                                     // tiles in flight per warp
     static constexpr uint32_t kCodeBytes = kQ4Tile * D / 2, kScaleBytes = kQ4Tile * 4; // of K or of V
     static constexpr uint32_t kLoadBytes = 2 * kCodeBytes + 2 * kScaleBytes;
@@ -647,16 +647,27 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
 
 // ---- host side -----------------------------------------------------------------------------------------------------
 
-constexpr int kQ4Rows = 16;                              // query rows per KV head up to which this kernel is taken
+constexpr int kQ4Rows = 16;                              // query rows of an item here
+// Up to two such items per KV head: this kernel, which reads the cache once for each of them.  Beyond that row tiles of 128.
+// Measured here and there: 8 x 32 / 8 heads, 2 K - 8 K rows, 20 query rows 57 and 80 us.
+constexpr int kQ4Items = 2;
 
-ChunkPlan chunk_q4_plan(const csp_params& p, int max_new) {
+ChunkPlan chunk_q4_plan(const csp_params& p, int max_new, bool* few) {
     const int G = p.n_q_heads / p.n_kv_heads;
     ChunkPlan pl = chunk_plan(p, max_new);
-    if (int64_t(max_new) * G > kQ4Rows) return pl;
+    const int tile = kQ4Rows / 2 / G, pairs = max_new / (2 * tile) + (max_new % (2 * tile) ? 1 : 0);
+    *few = int64_t(max_new) * G <= kQ4Rows || pairs <= kQ4Items;
+    if (!*few) return pl;
+    if (int64_t(max_new) * G > kQ4Rows) {                // (an item has 2 tok_tile tokens)
+        pl.tok_tile = tile;
+        pl.n_pairs = pairs;
+        pl.row_slots = 2 * tile * G;
+    }
+    pl.snap = 0x3fffffff;
     pl.key_tile = kQ4Tile;
     pl.min_tiles = 4;
     pl.item_cost = 4;
-    const int64_t items = int64_t(p.batch) * p.n_kv_heads;       // (n_pairs is 1)
+    const int64_t items = int64_t(p.batch) * p.n_kv_heads * pl.n_pairs;
     const int64_t weight = (int64_t(p.out_capacity) + pl.key_tile - 1) / pl.key_tile + pl.item_cost;      // of an item, at most
     pl.n_items = items > 0x3fffffffLL / weight ? -1 : int(items);
     // no more blocks than there can be shares of the smallest size
@@ -690,22 +701,29 @@ size_t chunk_q4_workspace_bytes(const csp_params& p, int max_new) {
     if (p.dtype != CSP_BF16 || (p.head_dim != 64 && p.head_dim != 128)) return 0;
     if (p.out_capacity > (1 << 30)) return 0;                                    // a row index plus some tiles fits 32 bits
     if (int64_t(max_new) * (p.n_q_heads / p.n_kv_heads) > (1 << 24)) return 0;   // and so do a chunk's rows
-    const ChunkPlan pl = chunk_q4_plan(p, max_new);
+    bool few;
+    const ChunkPlan pl = chunk_q4_plan(p, max_new, &few);
     if (pl.n_items < 0) return 0;                                                // key tiles are counted in 32 bits
-    // enough for shorter chunks as well: the longest that is one item may have more rows in it
-    const int few = kQ4Rows / (p.n_q_heads / p.n_kv_heads);
-    const size_t mine = partial_layout(p, pl).total, shorter = partial_layout(p, chunk_q4_plan(p, max_new < few ? max_new : few)).total;
-    return mine > shorter ? mine : shorter;
+    // Enough for shorter chunks as well: those of one or two small items have other tiles and shares.  (Among chunks of one kind
+    // the size grows with max_new.)
+    const int G = p.n_q_heads / p.n_kv_heads, longest[2] = {kQ4Rows / G, kQ4Items * 2 * (kQ4Rows / 2 / G)};
+    size_t mine = partial_layout(p, pl).total;
+    for (const int n : longest) {
+        const size_t shorter = partial_layout(p, chunk_q4_plan(p, max_new < n ? max_new : n, &few)).total;
+        if (shorter > mine) mine = shorter;
+    }
+    return mine;
 }
 
 csp_status launch_chunk_q4(const csp_params& p, const ChunkArgs& a, const csp_tensor& q, const Q4Args& c, void* ws, cudaStream_t s) {
-    ChunkPlan pl = chunk_q4_plan(p, a.max_new);
+    bool few;
+    ChunkPlan pl = chunk_q4_plan(p, a.max_new, &few);
     const PartialLayout lay = partial_layout(p, pl);
     ChunkParts* const parts = reinterpret_cast<ChunkParts*>(static_cast<char*>(ws) + lay.parts);
     float* const partial = reinterpret_cast<float*>(static_cast<char*>(ws) + lay.o);
     float2* const ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + lay.ml);
     csp_status st;
-    if (pl.row_slots > kQ4Rows) {
+    if (!few) {
         pl.drawn = a.mods.documents && pl.n_items >= 2 * pl.grid;
         st = launch_chunk_q4_many(p, a, pl, q, c, parts, partial, ml, s);
     } else {
@@ -717,7 +735,7 @@ csp_status launch_chunk_q4(const csp_params& p, const ChunkArgs& a, const csp_te
     }
     // nothing is cut by a single block, and where two parts of min_tiles are more than a cache has
     if (st != CSP_OK || pl.grid == 1 || p.out_capacity <= (2 * pl.min_tiles - 1) * pl.key_tile) return st;
-    return launch_chunk_join(p, a, pl, pl.row_slots <= kQ4Rows, parts, partial, ml, s);
+    return launch_chunk_join(p, a, pl, few, parts, partial, ml, s);
 }
 
 }  // namespace csp

@@ -42,7 +42,7 @@ constexpr int kEntryWords = 12;
 constexpr int kRawTiles = 2;                             // tiles of codes under way
 constexpr uint32_t kUnset = 0xBF800000u;                 // -1.0f: no sum of weights has these bits
 constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
-constexpr float kTiny = 0x1p-126f, kHuge = 0x1p126f;     // bounds of the reference of the scales
+constexpr float kTiny = 0x1p-110f, kHuge = 0x1p110f;     // bounds of the reference of the values
 
 // What an entry says.  The first two words are all that a tile needs at once: flags and the tile's first key.
 enum EntryWord { kFlags, kTile0, kSeq, kHead, kTok0, kRows, kNew, kPart, kPrefix, kPage, kPageRow, kScaleRef };
@@ -69,23 +69,19 @@ __device__ __forceinline__ uint4 unpack_codes(uint32_t x) {
     const uint32_t y = x >> 8;
     return make_uint4(x & kLow, x & kHigh, y & kLow, y & kHigh);
 }
-// ... for V with scale and base (both halves of `scale` and of `base` the same): 1024 + code and 1024 + 16 code are exact, and
-// so is the code taken from them; one rounding
+// ... for V as values: times scale 2^24 or 2^20, plus base, with one rounding (both halves of the factors and of `base` the same)
 __device__ __forceinline__ uint32_t fma_f16(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t r;
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
     return r;
 }
-__device__ __forceinline__ uint32_t low_values(uint32_t x, uint32_t scale, uint32_t base) {
-    return fma_f16(fma_f16((x & kLow) | 0x64006400u, 0x3c003c00u, 0xe400e400u), scale, base);        // x - 1024
+__device__ __forceinline__ uint4 unpack_values(uint32_t x, uint32_t scale24, uint32_t scale20, uint32_t base) {
+    const uint4 y = unpack_codes(x);
+    return make_uint4(fma_f16(y.x, scale24, base), fma_f16(y.y, scale20, base), fma_f16(y.z, scale24, base), fma_f16(y.w, scale20, base));
 }
-__device__ __forceinline__ uint32_t high_values(uint32_t x, uint32_t scale, uint32_t base) {
-    return fma_f16(fma_f16((x & kHigh) | 0x64006400u, 0x2c002c00u, 0xd400d400u), scale, base);       // x / 16 - 64
-}
-__device__ __forceinline__ uint4 unpack_values(uint32_t x, uint32_t scale, uint32_t base) {
-    const uint32_t y = x >> 8;
-    return make_uint4(low_values(x, scale, base), high_values(x, scale, base), low_values(y, scale, base), high_values(y, scale, base));
-}
+// Values of V are held as value / reference x 2^-7, the reference the power of two that is at most the largest value so far: below
+// 2^-6, so that scale 2^24 is still a half (15 scale <= 2^-5); a value below 2^-7 of the largest has its error of 2^-18 of it.
+constexpr float kValueUnit = 0x1p-7f;
 
 struct ManySmem { uint32_t q, raw, meta, entries, pair, join, rows, bars, misc, total; };
 template <int NH, bool kMeta>
@@ -94,8 +90,9 @@ struct ManyShape {
     static constexpr uint32_t kStageBytes = NH * kBlockBytes;            // one tile of K or of V in halves
     static constexpr uint32_t kQBytes = NH * kBlockBytes;                // one row tile of Q
     static constexpr uint32_t kRawBytes = kStageBytes / 4;               // one tile of K or of V in 4 bits
-    // [128] scale of K, base of K, scale and base of V in halves, (position, document)
-    static constexpr uint32_t kMetaBytes = (kMeta ? 5 : 3) * kTileKeys * 4, kPositions = 3 * kTileKeys * 4, kDocuments = 4 * kTileKeys * 4;
+    // [128] scale of K, base of K, (position, document); then as pairs of halves scale 2^24 of V, scale 2^20, base
+    static constexpr uint32_t kPositions = 2 * kTileKeys * 4, kDocuments = 3 * kTileKeys * 4, kValues = (kMeta ? 4 : 2) * kTileKeys * 4;
+    static constexpr uint32_t kMetaBytes = kValues + 4 * kTileKeys * 4;
     static constexpr int kBars = 2 * kStages + 2 * kEntries + 6 + 6 + 2 + 8;
     __host__ __device__ static constexpr ManySmem plan() {
         ManySmem s = {};
@@ -344,7 +341,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 }
                 // (magnitudes: their bits are in order)
                 const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(fminf(v_top, kHuge))) & 0x7f800000u;
-                if (__uint_as_float(top) > 16.f * v_ref || v_ref == kTiny) v_ref = fmaxf(__uint_as_float(top), kTiny);
+                v_ref = fmaxf(v_ref, __uint_as_float(top));
                 if (page < 0 && lane == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
                 const int page_row = int(uint32_t(tile) % tiles_per_page) * kTileKeys;
                 int32_t told = word;
@@ -360,9 +357,13 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 float4* const numbers = reinterpret_cast<float4*>(base_ptr + sp.meta + e * Shape::kMetaBytes);
                 numbers[lane] = make_float4(sk[0], sk[1], sk[2], sk[3]);
                 numbers[lane + 32] = make_float4(bk[0], bk[1], bk[2], bk[3]);
-                const float v_inv = 1.f / v_ref;
-                reinterpret_cast<uint4*>(numbers)[lane + 64] = make_uint4(pack_f16(sv[0] * v_inv, bv[0] * v_inv), pack_f16(sv[1] * v_inv, bv[1] * v_inv),
-                                                                          pack_f16(sv[2] * v_inv, bv[2] * v_inv), pack_f16(sv[3] * v_inv, bv[3] * v_inv));
+                const float v_unit = kValueUnit / v_ref;
+                uint4* const values = reinterpret_cast<uint4*>(base_ptr + sp.meta + e * Shape::kMetaBytes + Shape::kValues);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float s24 = sv[j] * v_unit * 0x1p24f, zero = bv[j] * v_unit;
+                    values[4 * lane + j] = make_uint4(pack_f16(s24, s24), pack_f16(0x1p-4f * s24, 0x1p-4f * s24), pack_f16(zero, zero), 0u);
+                }
                 if (kMeta) {
                     float* const mp = reinterpret_cast<float*>(base_ptr + sp.meta + e * Shape::kMetaBytes + Shape::kPositions);
                     int32_t* const md = reinterpret_cast<int32_t*>(base_ptr + sp.meta + e * Shape::kMetaBytes + Shape::kDocuments);
@@ -490,7 +491,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
         uint32_t n_entry = 0, n_copied = 0, n_done = 0;
         int entry_of[kRawTiles] = {};                    // of the tiles that have been copied, the oldest first
         auto unpack = [&] {                              // the oldest tile that has been copied
-            const uint32_t* const v_numbers = reinterpret_cast<const uint32_t*>(base_ptr + sp.meta + entry_of[0] * Shape::kMetaBytes + 2 * kTileKeys * 4);
+            const uint4* const values = reinterpret_cast<const uint4*>(base_ptr + sp.meta + entry_of[0] * Shape::kMetaBytes + Shape::kValues);
             if (n_copied - n_done == kRawTiles) asm volatile("cp.async.wait_group %0;" ::"n"(kRawTiles - 1) : "memory");
             else asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll 1
@@ -514,9 +515,9 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
 #pragma unroll
                         for (int j = 0; j < 4; ++j) *place(j) = unpack_codes(w[j]);
                     } else {
-                        const uint32_t pair = v_numbers[row], scale = __byte_perm(pair, pair, 0x1010), zero = __byte_perm(pair, pair, 0x3232);
+                        const uint4 f = values[row];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) *place(j) = unpack_values(w[j], scale, zero);
+                        for (int j = 0; j < 4; ++j) *place(j) = unpack_values(w[j], f.x, f.y, f.z);
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -651,7 +652,8 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         sum += other_half(sum);
                         // S is the product with codes 2^-20
-                        factor = a.scale * kLog2e * 0x1p20f * (ex == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(ex << 23));
+                        // (never zero: it meets the minus infinities of hidden keys)
+                        factor = ex == 255u ? __uint_as_float(0x7fc00000u) : fmaxf(a.scale * kLog2e * 0x1p20f * __uint_as_float(ex << 23), 0x1p-126f);
                         q_sum = sum * 0x1p-20f;
                         if (half == 0) row_const[slot * 128 + m] = make_float2(factor, q_sum);
                         __syncwarp();
@@ -818,7 +820,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
             if (started) warp_wait(pv_done + 8 * g, (n_mine - 1u) & 1u, abort_flag);
             tc_fence_after();
             float l_all = l_run + other_half(l_run);
-            float m_all = m_run, w0 = v_run, w1 = 0.f;       // w0, w1: what the two groups' products are multiplied by
+            float m_all = m_run, w0 = v_run * (1.f / kValueUnit), w1 = 0.f;       // w0, w1: what the two groups' products are multiplied by
             bool has0 = started, has1 = false;
             if (!big) {
                 // both groups hold part of the same rows: exchange reference and sum, then each half row writes a quarter
@@ -835,8 +837,8 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 w0 = ex2f(m0 - m_all);
                 w1 = ex2f(m1 - m_all);
                 l_all = (has0 ? l0 * w0 : 0.f) + (has1 ? l1 * w1 : 0.f);
-                w0 *= join_buf[512 + m];
-                w1 *= join_buf[640 + m];
+                w0 *= join_buf[512 + m] * (1.f / kValueUnit);
+                w1 *= join_buf[640 + m] * (1.f / kValueUnit);
             }
             if (live) {
                 const int local = m / G, head = h * G + m - local * G, tok = tok0 + (big ? g * pl.tok_tile : 0) + local;
