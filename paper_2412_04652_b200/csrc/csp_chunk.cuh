@@ -96,8 +96,10 @@ __device__ __forceinline__ int item_weight(const ChunkArgs& a, const ChunkPlan& 
 }
 // All threads of the block; scratch: 68 words of shared memory.  Every block goes over all items (a few per thread): that
 // costs less than a launch of its own would.  (The launcher has made sure that the total fits 30 bits.)
+// chains, if given: four words, of item0 where it is the rest of a cut item and of item1 where it is cut: the block that the item
+// begins in, and in how many blocks its parts are.
 template <int kThreads>
-__device__ __forceinline__ Share find_share(const ChunkArgs& a, const ChunkPlan& pl, int* scratch) {
+__device__ __forceinline__ Share find_share(const ChunkArgs& a, const ChunkPlan& pl, int* scratch, int* chains = nullptr) {
     static_assert(kThreads % 32 == 0 && kThreads <= 1024, "one partial sum per warp");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (pl.n_items + kThreads - 1) / kThreads;
@@ -136,7 +138,14 @@ __device__ __forceinline__ Share find_share(const ChunkArgs& a, const ChunkPlan&
                 const int t = at - s - pl.item_cost;
                 if (at - s <= snap || t < pl.min_tiles) { found[2 * k] = i; found[2 * k + 1] = 0; }
                 else if (s + w - at <= snap || tiles - t < pl.min_tiles) { found[2 * k] = i + 1; found[2 * k + 1] = 0; }
-                else { found[2 * k] = i; found[2 * k + 1] = t; }
+                else {
+                    found[2 * k] = i; found[2 * k + 1] = t;
+                    if (chains) {                        // cuts number first to last fall into the item like this one
+                        const int first = (s + max(snap, pl.item_cost + pl.min_tiles - 1)) / share + 1;
+                        const int last = (s + w - max(snap, pl.min_tiles - 1) - 1) / share;
+                        chains[2 * k] = first - 1; chains[2 * k + 1] = last - first + 2;
+                    }
+                }
                 break;
             }
             s += w;

@@ -22,8 +22,8 @@
 // Organisation: one CTA per SM works off an equal share of all 32-key tiles, and inside it every warp an equal share of that,
 // tile after tile: no warp waits for another one before the end.  A warp has a ring of its own that it refills itself as soon as it
 // has read a slot.  An item (up to sixteen query rows of a unit) that lies in one warp's share is finished by
-// it; of one that is cut the pieces stay in shared memory until all warps are done and are joined then, in order; what
-// goes on in another CTA is left as a partial result for the joining kernel.
+// it; of one that is cut the pieces stay in shared memory until all warps are done and are joined then, in order; of one that
+// goes on in another CTA a partial result is left, and the CTA that leaves the last one joins them, in order.
 #include <cuda_fp16.h>
 #include <limits.h>
 
@@ -34,6 +34,7 @@ namespace {
 using namespace dev;
 
 constexpr int kQ4Tile = 32;                              // keys per tile
+constexpr int kCountWord = 16, kMostBlocks = 192;        // of the status area: a byte per block
 constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
 constexpr float kTiny = 0x1p-126f, kHuge = 0x1p126f;     // bounds of the reference of the scales
 
@@ -88,9 +89,10 @@ struct Q4Shape {
     static constexpr uint32_t kFront = kWarps * kSlots * kSlotBytes;                   // [warp]: the piece that a warp begins with
     static constexpr uint32_t kNotes = kFront + kWarps * kPieceBytes;                  // [warp]
     static constexpr uint32_t kTable = kNotes + kWarps * 16;                           // [warp][R] RowNote
-    static constexpr uint32_t kDesk = kTable + kWarps * R * 16;                        // [warp] two Segments: loaded, computed
-    static constexpr uint32_t kScratch = kDesk + kWarps * 128;                         // of find_share
-    static constexpr uint32_t kTotal = kScratch + 68 * 4;
+    static constexpr uint32_t kDesk = kTable + kWarps * R * 16;                        // [warp] three Segments: loaded, computed, of the front piece
+    static constexpr uint32_t kScratch = kDesk + kWarps * 192;                         // of find_share
+    static constexpr uint32_t kChains = kScratch + 68 * 4;                             // of find_share; then whether this block joins them
+    static constexpr uint32_t kTotal = kChains + 6 * 4;
     static constexpr int kThreads = 32 * kWarps;
     static_assert(kSlots * kSlotBytes >= kPieceBytes, "the piece that a warp ends with goes into its ring");
 };
@@ -101,10 +103,13 @@ struct Q4Shape {
 struct WarpShare { int begin, begin_tile, end, end_tile; };
 __device__ __forceinline__ WarpShare warp_share(const ChunkArgs& a, const ChunkPlan& pl, const Share& sh, int warp, int warps, int lane) {
     const int last = min(sh.item1, pl.n_items - 1);
-    int total = 0, part = 0, got[4] = {pl.n_items, 0, pl.n_items, 0};
-    // (the code of this kernel is fetched once per launch, which costs more than running it: both passes are one)
+    WarpShare got = {pl.n_items, 0, pl.n_items, 0};
+    int total = 0, part = 0;
+    // (Most of this kernel's code runs once, at the speed at which it is fetched: both passes are one, and the second is all there
+    // is where one step covers the block's items.)
+    const bool once = last - sh.item0 < 32;
 #pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
+    for (int pass = once ? 1 : 0; pass < 2; ++pass) {
         int before = 0;
 #pragma unroll 1
         for (int i = sh.item0; i <= last; i += 32) {
@@ -121,22 +126,26 @@ __device__ __forceinline__ WarpShare warp_share(const ChunkArgs& a, const ChunkP
                 const int y = __shfl_up_sync(0xffffffffu, x, d);
                 if (lane >= d) x += y;
             }
-            const int p = before + x - w;                // weight in front of this lane's item
+            const int all = __shfl_sync(0xffffffffu, x, 31);
+            if (once) part = max((all + warps - 1) / warps, 2);
+            if (pass) {
+                const int p = before + x - w;            // weight in front of this lane's item
 #pragma unroll 1
-            for (int k = 0; k < 2 && pass; ++k) {
-                const int cut = (warp + k) * part;
-                const uint32_t hit = __ballot_sync(0xffffffffu, cut >= p && cut < p + w);
-                if (!hit) continue;
-                const int from = __ffs(hit) - 1, tile = __shfl_sync(0xffffffffu, lo + max(cut - p - 1, 0), from);
-                if (k == 0) { got[0] = i + from; got[1] = tile; }
-                else { got[2] = i + from; got[3] = tile; }
+                for (int k = 0; k < 2; ++k) {
+                    const int cut = (warp + k) * part;
+                    const uint32_t hit = __ballot_sync(0xffffffffu, cut >= p && cut < p + w);
+                    if (!hit) continue;
+                    const int from = __ffs(hit) - 1, tile = __shfl_sync(0xffffffffu, lo + max(cut - p - 1, 0), from);
+                    if (k == 0) { got.begin = i + from; got.begin_tile = tile; }
+                    else { got.end = i + from; got.end_tile = tile; }
+                }
             }
-            before += __shfl_sync(0xffffffffu, x, 31);
+            before += all;
         }
         total = before;
-        part = max((total + warps - 1) / warps, 2);
+        if (!once) part = max((total + warps - 1) / warps, 2);
     }
-    return WarpShare{got[0], got[1], got[2], got[3]};
+    return got;
 }
 
 // What a warp says of its pieces: the item that it went on with (-1: none) and whether that ended with it, the item that it began
@@ -144,13 +153,13 @@ __device__ __forceinline__ WarpShare warp_share(const ChunkArgs& a, const ChunkP
 struct Notes { int front, front_ends, back, unused; };
 // What a warp has of one item: its tiles [lo, hi).
 struct Segment { int item, b, h, lo, hi; PairRange x; };
-static_assert(sizeof(Segment) <= 64, "two of them in 128 bytes");
+static_assert(sizeof(Segment) <= 64, "three of them in 192 bytes");
 // A query row's last visible key, document, position and slope.
 struct RowNote { int lim, doc; float pos, slope2; };
 
 template <int NH, int RH, bool kMods>                   // kMods: a cap, a bias or documents
 __global__ void __launch_bounds__(Q4Shape<NH, RH>::kThreads, 1)
-chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, const Q4Args cache, ChunkParts* const parts,
+chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, const Q4Args cache,
                     float* const partial, float2* const partial_ml) {
     using Shape = Q4Shape<NH, RH>;
     constexpr int D = Shape::D, NW = Shape::kWarps, NST = Shape::kSlots;
@@ -164,7 +173,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     Notes* const notes = reinterpret_cast<Notes*>(base_ptr + Shape::kNotes);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.group;
     const ModArgs& md = a.mods;
-    const Share share = find_share<Shape::kThreads>(a, pl, reinterpret_cast<int*>(base_ptr + Shape::kScratch));      // (synchronises)
+    const Share share = find_share<Shape::kThreads>(a, pl, reinterpret_cast<int*>(base_ptr + Shape::kScratch), reinterpret_cast<int*>(base_ptr + Shape::kChains));      // (synchronises)
     const WarpShare mine = warp_share(a, pl, share, warp, NW, lane);
 
     const int gr = lane >> 2, qd = lane & 3;             // fragment row (a key, then dimensions) and column pair (query rows)
@@ -193,7 +202,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     constexpr int kCopies = Shape::kCodeBytes / 512;
     const uint32_t v_to = NH == 2 ? (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 3)) << 4) : (lane >> 1) * 32 + (((lane & 1) ^ ((lane >> 3) & 1)) << 4);
     bool f_open = false, f_more = true;
-    Segment* const desk = reinterpret_cast<Segment*>(base_ptr + Shape::kDesk) + 2 * warp;    // (what is seldom needed stays out of the registers)
+    Segment* const desk = reinterpret_cast<Segment*>(base_ptr + Shape::kDesk + 192 * warp);    // (what is seldom needed stays out of the registers)
     int f_item = mine.begin - 1, f_end = 0, f_tile = 0, f_left = 0, f_next = 0, f_index = 0, f_lo = 0, f_hi = 0;     // f_left: tiles of the current page
     bool f_there = false;                                // the current page lies in the pool
     const uint8_t* f_k = nullptr, * f_v = nullptr, * f_s = nullptr;              // what this lane copies of the next tile
@@ -310,7 +319,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
             const Segment seg = desk[1];
             const int count = seg.x.count;
             const bool begins = seg.lo == 0, ends = seg.hi >= seg.x.tiles;
-            if (!begins) { note_front = seg.item; note_ends = ends; }
+            if (!begins) { note_front = seg.item; note_ends = ends; if (lane == 0) desk[2] = seg; }
             else if (!ends) note_back = seg.item;
             // (a back piece is the last thing that its warp has: nothing is on its way into the ring any more)
             float* const piece = reinterpret_cast<float*>(begins ? my_ring : base_ptr + Shape::kFront + warp * Shape::kPieceBytes);
@@ -586,63 +595,115 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     if (lane == 0) notes[warp] = Notes{note_front, note_ends, note_back, 0};
     __syncthreads();
     // ---- the pieces of cut items: chain 0 goes on with what the block before began, chain c begins with warp c - 1's back piece
-    ChunkParts said = {-1, 0};
-    for (int c = 0; c <= NW; ++c) {
-        const int item = c == 0 ? notes[0].front : notes[c - 1].back;
-        if (item < 0) continue;
-        int next = c == 0 ? 1 : c;                       // the warp whose front piece comes next
-        bool ended = c == 0 && notes[0].front_ends;
-        while (!ended && next < NW && notes[next].front == item) ended = notes[next++].front_ends;
-        const bool final = c > 0 && ended;
-        if (c == 0) said.last = ended;
-        else if (!ended) said.first = item;
-        const int u = item / pl.n_pairs, b = u / a.n_kv_heads, h = u - b * a.n_kv_heads;
-        const PairRange x = pair_range(a, pl, u, item - u * pl.n_pairs);
-        const int w0 = c == 0 ? 0 : c - 1;               // pieces: of warps w0 up to next - 1
-        constexpr int C = D / 32;                        // columns per lane
-        for (int m = (warp + NW - c % NW) % NW; m < x.count * G; m += NW) {    // (another chain begins with another warp)
-            auto piece = [&](int w) {
-                return reinterpret_cast<const float*>(c > 0 && w == w0 ? base_ptr + w * NST * Shape::kSlotBytes : base_ptr + Shape::kFront + w * Shape::kPieceBytes) + m * Shape::kPieceRow;
-            };
-            float mm = kNeg;
-            for (int w = w0; w < next; ++w) mm = fmaxf(mm, piece(w)[D]);
-            float l = 0.f, o[C];
+    // query row m of an item, joined: four columns per lane
+    auto finish = [&](int b, int h, int tok0, int m, float mm, float l, const float4& o) {
+        const int tok = tok0 + m / G, head = h * G + m % G;
+        const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, mm) + l);
+        if (lane < D / 4)
+            *reinterpret_cast<uint2*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st + 4 * lane) =
+                l == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        if (a.lse && lane == 0)
+            a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
+    };
+    int cut[2] = {-1, -1};                               // the item that goes on from the block before, the one that goes on in the next
+    const Notes said = lane < NW ? notes[lane] : Notes{-1, 0, -1, 0};
+    const uint32_t fronts = __ballot_sync(0xffffffffu, said.front >= 0), ended = __ballot_sync(0xffffffffu, said.front >= 0 && said.front_ends);
+    uint32_t starts = __ballot_sync(0xffffffffu, said.back >= 0) << 1 | (fronts & 1u);
+    // (the weighted sum of n rows of sums that lie at `row(p)`, with reference and sum of weights behind them: lane p looks at those)
+    auto join = [&](auto row, int n, float& mm, float& l, float4& o) {
+        mm = kNeg;
+        l = 0.f;
+        o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p0 = 0; p0 < n; p0 += 32) {
+            const float2 ml = p0 + lane < n ? row.ml(p0 + lane) : make_float2(kNeg, 0.f);
+            float top = fmaxf(mm, ml.x);
 #pragma unroll
-            for (int k = 0; k < C; ++k) o[k] = 0.f;
+            for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float keep = ex2f(mm - top), mine = ex2f(ml.x - top);
+            mm = top;
+            float sum = ml.y * mine;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            l = fmaf(l, keep, sum);
+            o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
 #pragma unroll 4
-            for (int w = w0; w < next; ++w) {
-                const float* const from = piece(w);
-                const float2 ml = *reinterpret_cast<const float2*>(from + D);
-                const float wgt = ex2f(ml.x - mm);
-                l += ml.y * wgt;
-#pragma unroll
-                for (int k = 0; k < C; k += 2) {
-                    const float2 y = *reinterpret_cast<const float2*>(from + lane * C + k);
-                    o[k] += y.x * wgt;
-                    o[k + 1] += y.y * wgt;
-                }
+            for (int p = 0; p < min(n - p0, 32); ++p) {
+                const float w = __shfl_sync(0xffffffffu, mine, p);
+                const float4 y = row.sums(p0 + p);
+                o.x = fmaf(y.x, w, o.x); o.y = fmaf(y.y, w, o.y); o.z = fmaf(y.z, w, o.z); o.w = fmaf(y.w, w, o.w);
             }
-            const int tok = x.tok0 + m / G, head = h * G + m % G;
-            if (final) {
-                const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, mm) + l);
-                uint32_t* const out = reinterpret_cast<uint32_t*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st + lane * C);
-#pragma unroll
-                for (int k = 0; k < C; k += 2) out[k / 2] = l == 0.f ? 0u : pack_bf16(o[k] * inv, o[k + 1] * inv);
-                if (a.lse && lane == 0)
-                    a.lse[(int64_t(b) * a.n_kv_heads * G + head) * a.max_new + tok] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
+        }
+    };
+    const int col = lane % (D / 4) * 4;                  // four columns per lane (at d = 64 two lanes have the same)
+    while (starts) {
+        const int c = __ffs(starts) - 1;
+        starts &= starts - 1;
+        const int from = c == 0 ? 0 : c - 1;             // pieces: of warps from up to next - 1
+        const uint32_t mine_f = fronts >> c, mine_e = ended >> c;
+        int next = c + __ffs(~mine_f) - 1;               // the first warp from c on that did not go on with anything
+        const int end = mine_e ? c + __ffs(mine_e) : NW + 1;
+        const bool done = end <= next;
+        if (done) next = end;
+        const Segment* const d = reinterpret_cast<const Segment*>(base_ptr + Shape::kDesk + 192 * from) + (c == 0 ? 2 : 1);
+        if (!(c > 0 && done)) cut[c > 0] = d->item;
+        struct Pieces {
+            const uint8_t* front; const uint8_t* first; int col;
+            __device__ __forceinline__ const float* at(int p) const { return reinterpret_cast<const float*>(p == 0 ? first : front + p * Shape::kPieceBytes); }
+            __device__ __forceinline__ float2 ml(int p) const { return *reinterpret_cast<const float2*>(at(p) + D); }
+            __device__ __forceinline__ float4 sums(int p) const { return *reinterpret_cast<const float4*>(at(p) + col); }
+        };
+        for (int m = (warp + NW - c % NW) % NW; m < d->x.count * G; m += NW) {           // (another chain begins with another warp)
+            const uint8_t* const front = base_ptr + Shape::kFront + from * Shape::kPieceBytes + m * Shape::kPieceRow * 4;
+            float mm, l;
+            float4 o;
+            join(Pieces{front, c == 0 ? front : base_ptr + from * NST * Shape::kSlotBytes + m * Shape::kPieceRow * 4, col}, next - from, mm, l, o);
+            if (c > 0 && done) {
+                finish(d->b, d->h, d->x.tok0, m, mm, l, o);
             } else {
-                const int64_t slot = int64_t(2 * blockIdx.x + (c > 0 ? 1 : 0)) * pl.row_slots;
-#pragma unroll
-                for (int k = 0; k < C; k += 2) {         // laid out [column / 4][row][4]
-                    const int col = lane * C + k;
-                    *reinterpret_cast<float2*>(partial + (slot * (D / 4) + int64_t(col / 4) * pl.row_slots + m) * 4 + col % 4) =
-                        make_float2(o[k], o[k + 1]);
-                }
-                if (lane == 0) partial_ml[slot + m] = make_float2(mm, l);
+                const int64_t slot = int64_t(2 * blockIdx.x + (c > 0 ? 1 : 0)) * pl.row_slots + m;
+                *reinterpret_cast<float4*>(partial + slot * D + col) = o;
+                if (lane == 0) partial_ml[slot] = make_float2(mm, l);
             }
         }
     }
-    if (tid == 0) parts[blockIdx.x] = said;
+    if (cut[0] < 0 && cut[1] < 0) return;
+    // ---- the parts of an item that is cut between blocks are joined by the block that brings the last one.  Of how many have
+    // been brought, the status area counts in a byte for each block that such an item begins in; they are zero again at the end.
+    int* const chains = reinterpret_cast<int*>(base_ptr + Shape::kChains);
+    __syncthreads();
+    if (tid == 0) {
+        __threadfence();
+        for (int k = 0; k < 2; ++k) {
+            chains[4 + k] = 0;
+            if (cut[k] < 0) continue;
+            const int first = chains[2 * k], n = chains[2 * k + 1], shift = 8 * (first & 3);
+            uint32_t* const count = reinterpret_cast<uint32_t*>(a.status) + kCountWord + (first >> 2);
+            if (int(atomicAdd(count, 1u << shift) >> shift & 255u) != n - 1) continue;
+            atomicSub(count, uint32_t(n) << shift);
+            chains[4 + k] = 1;
+        }
+        __threadfence();
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+        if (cut[k] < 0 || !chains[4 + k]) continue;
+        const int first = chains[2 * k], n = chains[2 * k + 1], item = cut[k];
+        const int u = item / pl.n_pairs, b = u / a.n_kv_heads, h = u - b * a.n_kv_heads;
+        const PairRange x = pair_range(a, pl, u, item - u * pl.n_pairs);
+        struct Parts {
+            const float* o; const float2* m; int first, rows, col;
+            __device__ __forceinline__ int64_t at(int p) const { return int64_t(2 * (first + p) + (p == 0 ? 1 : 0)) * rows; }
+            __device__ __forceinline__ float2 ml(int p) const { return __ldcg(m + at(p)); }
+            __device__ __forceinline__ float4 sums(int p) const { return __ldcg(reinterpret_cast<const float4*>(o + at(p) * D + col)); }
+        };
+        for (int m = warp; m < x.count * G; m += NW) {
+            float mm, l;
+            float4 o;
+            join(Parts{partial + m * D, partial_ml + m, first, pl.row_slots, col}, n, mm, l, o);
+            finish(b, h, x.tok0, m, mm, l, o);
+        }
+    }
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
@@ -672,27 +733,28 @@ ChunkPlan chunk_q4_plan(const csp_params& p, int max_new, bool* few) {
     pl.n_items = items > 0x3fffffffLL / weight ? -1 : int(items);
     // no more blocks than there can be shares of the smallest size
     const int64_t most = (items > 65536 ? 65536 : items) * weight / (pl.item_cost + pl.min_tiles) + 1;
-    pl.grid = most < sm_count() ? int(most) : sm_count();
+    const int blocks = sm_count() < kMostBlocks ? sm_count() : kMostBlocks;
+    pl.grid = most < blocks ? int(most) : blocks;
     return pl;
 }
 
 template <int NH, int RH, bool kMods>
-csp_status launch_few_mods(const ChunkArgs& a, const ChunkPlan& pl, const FewQuery& q, const Q4Args& c, ChunkParts* parts, float* partial,
-                      float2* ml, cudaStream_t s) {
+csp_status launch_few_mods(const ChunkArgs& a, const ChunkPlan& pl, const FewQuery& q, const Q4Args& c, float* partial, float2* ml,
+                      cudaStream_t s) {
     constexpr int smem = int(Q4Shape<NH, RH>::kTotal) + 128;
     static_assert(smem <= 227 * 1024, "shared memory of one CTA");
     auto kern = chunk_q4_few_kernel<NH, RH, kMods>;
     static std::atomic<bool> configured[kMaxDevices];
     if (!raise_smem_limit(kern, smem, configured)) return CSP_ERR_CUDA;
-    kern<<<pl.grid, Q4Shape<NH, RH>::kThreads, smem, s>>>(a, pl, q, c, parts, partial, ml);
+    kern<<<pl.grid, Q4Shape<NH, RH>::kThreads, smem, s>>>(a, pl, q, c, partial, ml);
     return cudaGetLastError() == cudaSuccess ? CSP_OK : CSP_ERR_CUDA;
 }
 
 template <int NH, int RH>
-csp_status launch_few(const ChunkArgs& a, const ChunkPlan& pl, const FewQuery& q, const Q4Args& c, ChunkParts* parts, float* partial,
-                      float2* ml, cudaStream_t s) {
-    return a.mods.softcap > 0.f || a.mods.slopes || a.mods.documents ? launch_few_mods<NH, RH, true>(a, pl, q, c, parts, partial, ml, s)
-                                                                     : launch_few_mods<NH, RH, false>(a, pl, q, c, parts, partial, ml, s);
+csp_status launch_few(const ChunkArgs& a, const ChunkPlan& pl, const FewQuery& q, const Q4Args& c, float* partial, float2* ml,
+                      cudaStream_t s) {
+    return a.mods.softcap > 0.f || a.mods.slopes || a.mods.documents ? launch_few_mods<NH, RH, true>(a, pl, q, c, partial, ml, s)
+                                                                     : launch_few_mods<NH, RH, false>(a, pl, q, c, partial, ml, s);
 }
 
 }  // namespace
@@ -719,23 +781,20 @@ csp_status launch_chunk_q4(const csp_params& p, const ChunkArgs& a, const csp_te
     bool few;
     ChunkPlan pl = chunk_q4_plan(p, a.max_new, &few);
     const PartialLayout lay = partial_layout(p, pl);
-    ChunkParts* const parts = reinterpret_cast<ChunkParts*>(static_cast<char*>(ws) + lay.parts);
     float* const partial = reinterpret_cast<float*>(static_cast<char*>(ws) + lay.o);
     float2* const ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + lay.ml);
-    csp_status st;
-    if (!few) {
-        pl.drawn = a.mods.documents && pl.n_items >= 2 * pl.grid;
-        st = launch_chunk_q4_many(p, a, pl, q, c, parts, partial, ml, s);
-    } else {
+    if (few) {
         const FewQuery qy = {static_cast<const uint16_t*>(q.ptr), q.stride_b, q.stride_h, q.stride_t};
         if (pl.row_slots <= 8)
-            st = p.head_dim == 64 ? launch_few<1, 1>(a, pl, qy, c, parts, partial, ml, s) : launch_few<2, 1>(a, pl, qy, c, parts, partial, ml, s);
-        else
-            st = p.head_dim == 64 ? launch_few<1, 2>(a, pl, qy, c, parts, partial, ml, s) : launch_few<2, 2>(a, pl, qy, c, parts, partial, ml, s);
+            return p.head_dim == 64 ? launch_few<1, 1>(a, pl, qy, c, partial, ml, s) : launch_few<2, 1>(a, pl, qy, c, partial, ml, s);
+        return p.head_dim == 64 ? launch_few<1, 2>(a, pl, qy, c, partial, ml, s) : launch_few<2, 2>(a, pl, qy, c, partial, ml, s);
     }
+    pl.drawn = a.mods.documents && pl.n_items >= 2 * pl.grid;
+    ChunkParts* const parts = reinterpret_cast<ChunkParts*>(static_cast<char*>(ws) + lay.parts);
+    const csp_status st = launch_chunk_q4_many(p, a, pl, q, c, parts, partial, ml, s);
     // nothing is cut by a single block, and where two parts of min_tiles are more than a cache has
     if (st != CSP_OK || pl.grid == 1 || p.out_capacity <= (2 * pl.min_tiles - 1) * pl.key_tile) return st;
-    return launch_chunk_join(p, a, pl, few, parts, partial, ml, s);
+    return launch_chunk_join(p, a, pl, false, parts, partial, ml, s);
 }
 
 }  // namespace csp
