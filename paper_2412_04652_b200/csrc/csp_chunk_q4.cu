@@ -240,6 +240,12 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                     f_next = page_at(f_index + 1);
                     turn_page(page, (tiles_per_page - f_left) * kQ4Tile);
                 }
+                {                                        // the item's queries will be asked for soon
+                    constexpr int kLines = D / 64;       // of 128 bytes
+                    const int m = lane / kLines, tok = m / G;
+                    if (tok < f.x.count && m < Shape::R)
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(qy.q + int64_t(f.b) * qy.sb + int64_t(f.h * G + m - tok * G) * qy.sh + int64_t(f.x.tok0 + tok) * qy.st + lane % kLines * 64));
+                }
                 if (by_doc) {                            // of the tokens: sixteen rows at most
                     const int r = f.x.row0 + lane;
                     const bool in = lane < f.x.count && r >= 0;
@@ -362,32 +368,34 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         const int count = seg.x.count;
         const int32_t* const docs = by_doc ? md.documents + int64_t(seg.b) * md.doc_sb + int64_t(seg.h) * md.doc_sh : nullptr;
         const int32_t* const poss = biased && md.positions ? md.positions + int64_t(seg.b) * md.pos_sb + int64_t(seg.h) * md.pos_sh : nullptr;
-        // positions are taken relative to the last token's, so that near ones are exact in fp32
-        const int row_last = max(seg.x.row0 + count - 1, 0);
-        pos_ref = biased && rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
-        lim_all = kSeesAll;
-        if (lane < Shape::R) {
-            const int tok = lane / G, head = seg.h * G + lane - tok * G, r = seg.x.row0 + tok;
-            const bool valid = tok < count, sees = valid && r >= 0;
-            // rows that nobody asked for see everything: they must not send their warp through the masked path
-            lim_all = !valid ? kSeesAll : sees ? max(r, seg.x.prefix - 1) : -1;
-            table[lane] = RowNote{lim_all, docs && sees ? docs[r] : 0, biased && sees ? float((poss ? poss[r] : r) - pos_ref) : 0.f,
-                                  biased && sees ? md.slopes[head] * kLog2e : 0.f};
-        }
-        lim_all = min(__reduce_min_sync(0xffffffffu, lim_all), rows - 1);
+        // ---- what comes from memory, all of it asked for before any of it is looked at: query row 8 n + gr, this lane's quarter of
+        // it, and what the modifiers need to know of query row `lane`
+        uint4 q[RH][KW];
 #pragma unroll
         for (int n = 0; n < RH; ++n) {
-            // ---- query row 8 n + gr, this lane's quarter of it: in halves and in the order of the codes
-            uint4 q[KW];
-            {
-                const int m = 8 * n + gr, tok = m / G;   // rows that are none are zeros
-                const uint16_t* const from = qy.q + int64_t(seg.b) * qy.sb + int64_t(seg.h * G + m - tok * G) * qy.sh + int64_t(seg.x.tok0 + tok) * qy.st + qd * KW * 8;
+            const int m = 8 * n + gr, tok = m / G;       // rows that are none are zeros
+            const uint16_t* const from = qy.q + int64_t(seg.b) * qy.sb + int64_t(seg.h * G + m - tok * G) * qy.sh + int64_t(seg.x.tok0 + tok) * qy.st + qd * KW * 8;
 #pragma unroll
-                for (int w = 0; w < KW; ++w) q[w] = tok < count ? reinterpret_cast<const uint4*>(from)[w] : make_uint4(0, 0, 0, 0);
-            }
+            for (int w = 0; w < KW; ++w) q[n][w] = tok < count ? reinterpret_cast<const uint4*>(from)[w] : make_uint4(0, 0, 0, 0);
+        }
+        {
+            // positions are taken relative to the last token's, so that near ones are exact in fp32
+            const int tok = lane / G, r = seg.x.row0 + tok, row_last = max(seg.x.row0 + count - 1, 0);
+            const bool valid = lane < Shape::R && tok < count, sees = valid && r >= 0;
+            pos_ref = biased && rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
+            const int pos = biased && sees ? (poss ? poss[r] : r) : pos_ref, doc = docs && sees ? docs[r] : 0;
+            const float slope = biased && sees ? md.slopes[seg.h * G + lane - tok * G] : 0.f;
+            // rows that nobody asked for see everything: they must not send their warp through the masked path
+            lim_all = !valid ? kSeesAll : sees ? max(r, seg.x.prefix - 1) : -1;
+            if (lane < Shape::R) table[lane] = RowNote{lim_all, doc, float(pos - pos_ref), slope * kLog2e};
+        }
+        lim_all = min(__reduce_min_sync(0xffffffffu, lim_all), rows - 1);
+        // ---- the queries in halves and in the order of the codes
+#pragma unroll
+        for (int n = 0; n < RH; ++n) {
             uint32_t top2 = 0;                           // the row's largest magnitude, two candidates
 #pragma unroll
-            for (int w = 0; w < KW; ++w) top2 = max_abs2(max_abs2(max_abs2(max_abs2(top2, q[w].x), q[w].y), q[w].z), q[w].w);
+            for (int w = 0; w < KW; ++w) top2 = max_abs2(max_abs2(max_abs2(max_abs2(top2, q[n][w].x), q[n][w].y), q[n][w].z), q[n][w].w);
             top2 = max_abs2(top2, top2 >> 16 | top2 << 16);
             top2 = max_abs2(top2, __shfl_xor_sync(0xffffffffu, top2, 1));
             top2 = max_abs2(top2, __shfl_xor_sync(0xffffffffu, top2, 2));
@@ -399,10 +407,10 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
             float ones[4] = {0.f, 0.f, 0.f, 0.f};        // the product with codes of one: the query's sum 2^-20
 #pragma unroll
             for (int w = 0; w < KW; ++w) {
-                qb[n][2 * w][0] = pack_f16(down16 * lo_bf16(q[w].x), down16 * lo_bf16(q[w].z));
-                qb[n][2 * w][1] = pack_f16(down * hi_bf16(q[w].x), down * hi_bf16(q[w].z));
-                qb[n][2 * w + 1][0] = pack_f16(down16 * lo_bf16(q[w].y), down16 * lo_bf16(q[w].w));
-                qb[n][2 * w + 1][1] = pack_f16(down * hi_bf16(q[w].y), down * hi_bf16(q[w].w));
+                qb[n][2 * w][0] = pack_f16(down16 * lo_bf16(q[n][w].x), down16 * lo_bf16(q[n][w].z));
+                qb[n][2 * w][1] = pack_f16(down * hi_bf16(q[n][w].x), down * hi_bf16(q[n][w].z));
+                qb[n][2 * w + 1][0] = pack_f16(down16 * lo_bf16(q[n][w].y), down16 * lo_bf16(q[n][w].w));
+                qb[n][2 * w + 1][1] = pack_f16(down * hi_bf16(q[n][w].y), down * hi_bf16(q[n][w].w));
                 mma_f16(ones, 0x00010001u, 0x00010001u, 0x00100010u, 0x00100010u, qb[n][2 * w][0], qb[n][2 * w][1]);
                 mma_f16(ones, 0x00010001u, 0x00010001u, 0x00100010u, 0x00100010u, qb[n][2 * w + 1][0], qb[n][2 * w + 1][1]);
             }
