@@ -169,41 +169,49 @@ class PageState:
                           self.page_rows, refs.numel())
 
 
-@dataclass
+@dataclass(frozen=True, eq=False)
 class Rope:
     """Rotary position embedding (csp_rope).  cos_sin fp32 [table rows, rope_dim]: the cosines of rope_dim / 2 angles, then their
     sines; positions int32 [B, new tokens], or None where a row's number is its position; interleaved: dimension 2 i is
-    paired with 2 i + 1, else i with i + rope_dim / 2."""
+    paired with 2 i + 1, else i with i + rope_dim / 2.  Says where the tensors lie when it is made; their values may change."""
     cos_sin: torch.Tensor
     positions: Optional[torch.Tensor] = None
     interleaved: bool = False
 
-    def c(self, batch: int, max_new: int) -> CRope:
+    def __post_init__(self):
         t, pos = self.cos_sin, self.positions
         assert t.dtype is torch.float32 and t.dim() == 2 and t.stride(1) == 1, "cos_sin: fp32 [table rows, rope_dim]"
         r = CRope(t.data_ptr(), t.stride(0), t.shape[0], t.shape[1], int(self.interleaved))
         if pos is not None:
-            ps = pos.shape
-            assert pos.dtype is torch.int32 and len(ps) == 2 and ps[0] == batch and ps[1] >= max_new and (pos.stride(1) == 1 or ps[1] <= 1), \
-                "positions: int32 [B, new tokens]"
+            assert pos.dtype is torch.int32 and pos.dim() == 2 and (pos.stride(1) == 1 or pos.shape[1] <= 1), "positions: int32 [B, new tokens]"
             r.positions, r.pos_stride_b = pos.data_ptr(), pos.stride(0)
-        return r
+        object.__setattr__(self, "_made", (C.byref(r), r, None if pos is None else tuple(pos.shape)))
+
+    def _ref(self, batch: int, max_new: int):
+        ref, _, at = self._made
+        assert at is None or (at[0] == batch and at[1] >= max_new), "positions: int32 [B, new tokens]"
+        return ref
 
 
-@dataclass
+@dataclass(frozen=True, eq=False)
 class Q4Cache:
     """The pages of K or of V in 4 bits (csp_q4_cache): codes uint8 [n_pages, Hkv, page_rows, d / 2], scales bf16 [n_pages,
-    Hkv, page_rows, 2] (scale, base)."""
+    Hkv, page_rows, 2] (scale, base).  Says where the tensors lie when it is made; their values may change."""
     codes: torch.Tensor
     scales: torch.Tensor
 
-    def c(self, p: "Params") -> CQ4Cache:
+    def __post_init__(self):
         codes, scales = self.codes, self.scales
-        cs = codes.shape
+        cs = tuple(codes.shape)
         assert codes.dtype is torch.uint8 and scales.dtype is torch.bfloat16
-        assert len(cs) == 4 and cs[1] == p.n_kv_heads and 2 * cs[3] == p.head_dim and scales.shape == (*cs[:3], 2), \
-            "codes [n_pages, Hkv, page_rows, d / 2], scales [n_pages, Hkv, page_rows, 2]"
-        return CQ4Cache(tensor4(codes), tensor4(scales))
+        assert len(cs) == 4 and tuple(scales.shape) == (*cs[:3], 2), "codes [n_pages, Hkv, page_rows, d / 2], scales [n_pages, Hkv, page_rows, 2]"
+        c = CQ4Cache(tensor4(codes), tensor4(scales))
+        object.__setattr__(self, "_made", (C.byref(c), c, cs))
+
+    def _ref(self, p: "Params"):
+        ref, _, cs = self._made
+        assert cs[1] == p.n_kv_heads and 2 * cs[3] == p.head_dim, "codes [n_pages, Hkv, page_rows, d / 2], scales [n_pages, Hkv, page_rows, 2]"
+        return ref
 
 
 def new_q4_cache(n_pages: int, n_kv_heads: int, page_rows: int, head_dim: int, device="cuda") -> Q4Cache:
@@ -508,7 +516,7 @@ def decode_attn_paged(p: Params, q, k_pool, v_pool, page_table, n_rows, out, ws)
 
 def _here(*tensors):
     """The kernels run on the current device: refuses tensors that live elsewhere."""
-    dev = torch.cuda.current_device()
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{dev}")
@@ -606,24 +614,27 @@ def append_paged(p: Params, k_new, v_new, k_pool, v_pool, page_table, n_rows, n_
 _NOTHING = CTensor(None, 0, 0, 0)
 
 
-def _append_args(p: Params, k_new, v_new, n_rows, n_rows_out, ws, rope, n_new, q, q_out):
-    _here(k_new, v_new, n_rows, n_rows_out, ws, n_new, q, q_out)
+def _append_args(p: Params, k_new, v_new, n_rows, n_rows_out, rope, n_new, q, q_out):
     _cache_dtype(p, k_new, v_new)
     ks, B, H = k_new.shape, p.batch, p.n_kv_heads
     T = ks[2]
     assert v_new.shape == ks and ks[0] == B, "k_new, v_new: [B, Hkv, new tokens, d]"
     per_head = n_new is not None and n_new.dim() == 2
-    cr = None
-    if rope is not None:
-        _here(rope.cos_sin, rope.positions)
-        cr = C.byref(rope.c(B, T))
     qt = qo = _NOTHING
     assert (q is None) == (q_out is None), "q and q_out go together"
     if q is not None:
-        assert q.dtype is k_new.dtype is q_out.dtype and q.shape == q_out.shape == (B, p.n_q_heads, T, p.head_dim), \
+        qs = q.shape
+        assert q.dtype is k_new.dtype is q_out.dtype and qs == q_out.shape == (B, p.n_q_heads, T, p.head_dim), \
             "q, q_out: [B, Hq, new tokens, d] of the new rows' type"
         qt, qo = tensor4(q), tensor4(q_out)
-    return T, _counts(n_new, (B, H) if per_head else (B,)), int(per_head), cr, qt, qo, _counts(n_rows, (B, H)), _counts(n_rows_out, (B, H))
+    heads = (B, H)
+    rows = _counts(n_rows, heads)
+    return T, tensor4(k_new), tensor4(v_new), _counts(n_new, heads if per_head else (B,)), int(per_head), \
+        None if rope is None else rope._ref(B, T), qt, qo, rows, rows if n_rows_out is n_rows else _counts(n_rows_out, heads)
+
+
+def _rope_tensors(rope: Optional[Rope]):
+    return () if rope is None else (rope.cos_sin, rope.positions)
 
 
 def append_rope_paged(p: Params, k_new, v_new, k_pool, v_pool, page_table, n_rows, n_rows_out, ws, rope: Rope, n_new=None,
@@ -631,41 +642,42 @@ def append_rope_paged(p: Params, k_new, v_new, k_pool, v_pool, page_table, n_row
     """append_paged with the keys rotated on the way, and with them the queries q [B, Hq, new tokens, d] into q_out (which may be
     q); n_new int32 [B] or [B, Hkv]."""
     cp = p._c()
-    T, new, per_head, cr, qt, qo, rows, rows_out = _append_args(p, k_new, v_new, n_rows, n_rows_out, ws, rope, n_new, q, q_out)
+    _here(k_new, v_new, n_rows, n_rows_out, ws, n_new, q, q_out, *_rope_tensors(rope))
+    T, kt, vt, new, per_head, cr, qt, qo, rows, rows_out = _append_args(p, k_new, v_new, n_rows, n_rows_out, rope, n_new, q, q_out)
     pg = _pool_pages(p, k_pool, v_pool, page_table)
     _cache_dtype(p, k_pool, v_pool)
-    _check(lib().csp_append_rope_paged(C.byref(cp), T, tensor4(k_new), tensor4(v_new), new, per_head, cr, qt, qo, tensor4(k_pool),
-                                       tensor4(v_pool), C.byref(pg), rows, rows_out, _ptr(ws), ws.numel(), _stream()),
-           "csp_append_rope_paged")
+    _check(lib().csp_append_rope_paged(C.byref(cp), T, kt, vt, new, per_head, cr, qt, qo, tensor4(k_pool), tensor4(v_pool),
+                                       C.byref(pg), rows, rows_out, ws.data_ptr(), ws.numel(), _stream()), "csp_append_rope_paged")
 
 
 def _q4_pages(p: Params, k_cache: Q4Cache, v_cache: Optional[Q4Cache], page_table):
     """(K, V, pages) of a cache in 4 bits."""
-    _here(k_cache.codes, k_cache.scales, page_table)
-    ck, cv, ks = k_cache.c(p), None, k_cache.codes.shape
+    ks = k_cache._made[2]
+    cv = None
     if v_cache is not None:
-        _here(v_cache.codes, v_cache.scales)
-        assert v_cache.codes.shape == ks
-        cv = C.byref(v_cache.c(p))
+        assert v_cache._made[2] == ks
+        cv = v_cache._ref(p)
     ts = page_table.shape
     assert page_table.dtype is torch.int32 and len(ts) == 2 and ts[0] == p.batch and page_table.is_contiguous()
-    return C.byref(ck), cv, C.byref(CPages(page_table.data_ptr(), ts[1], ks[2], ks[0]))
+    return k_cache._ref(p), cv, C.byref(CPages(page_table.data_ptr(), ts[1], ks[2], ks[0]))
 
 
 def append_q4_paged(p: Params, k_new, v_new, k_cache: Q4Cache, v_cache: Q4Cache, page_table, n_rows, n_rows_out, ws, n_new=None,
                     rope: Optional[Rope] = None, q=None, q_out=None):
     """append_rope_paged into pages in 4 bits; without rope nothing is rotated."""
     cp = p._c()
-    T, new, per_head, cr, qt, qo, rows, rows_out = _append_args(p, k_new, v_new, n_rows, n_rows_out, ws, rope, n_new, q, q_out)
+    _here(k_new, v_new, n_rows, n_rows_out, ws, n_new, q, q_out, k_cache.codes, k_cache.scales, v_cache.codes, v_cache.scales,
+          page_table, *_rope_tensors(rope))
+    T, kt, vt, new, per_head, cr, qt, qo, rows, rows_out = _append_args(p, k_new, v_new, n_rows, n_rows_out, rope, n_new, q, q_out)
     ck, cv, pg = _q4_pages(p, k_cache, v_cache, page_table)
-    _check(lib().csp_append_q4_paged(C.byref(cp), T, tensor4(k_new), tensor4(v_new), new, per_head, cr, qt, qo, ck, cv, pg, rows,
-                                     rows_out, _ptr(ws), ws.numel(), _stream()), "csp_append_q4_paged")
+    _check(lib().csp_append_q4_paged(C.byref(cp), T, kt, vt, new, per_head, cr, qt, qo, ck, cv, pg, rows, rows_out, ws.data_ptr(),
+                                     ws.numel(), _stream()), "csp_append_q4_paged")
 
 
 def load_q4_paged(p: Params, k_cache: Q4Cache, v_cache: Optional[Q4Cache], page_table, n_rows, k_out, v_out, ws, first=None):
     """Rows [first, n_rows) of a 4-bit cache as numbers: k_out, v_out [B, Hkv, rows, d] in p.dtype; without v_cache K only."""
     cp = p._c()
-    _here(n_rows, first, k_out, v_out, ws)
+    _here(n_rows, first, k_out, v_out, ws, k_cache.codes, k_cache.scales, page_table, *(() if v_cache is None else (v_cache.codes, v_cache.scales)))
     ck, cv, pg = _q4_pages(p, k_cache, v_cache, page_table)
     assert (v_cache is None) == (v_out is None), "v_cache and v_out go together"
     _cache_dtype(p, *((k_out,) if v_out is None else (k_out, v_out)))
@@ -686,7 +698,8 @@ def chunk_attn_q4_paged(p: Params, q, k_cache: Q4Cache, v_cache: Q4Cache, page_t
                         mods: Optional[ScoreMods] = None, lse=None):
     """chunk_attn_paged over pages in 4 bits."""
     cp = p._c()
-    _here(q, n_rows, out, ws, n_new, lse, *(mods.tensors() if mods is not None else ()))
+    _here(q, n_rows, out, ws, n_new, lse, k_cache.codes, k_cache.scales, v_cache.codes, v_cache.scales, page_table,
+          *(mods.tensors() if mods is not None else ()))
     shape, bf16 = q.shape, torch.bfloat16
     assert len(shape) == 4 and shape[0] == p.batch and shape[1] == p.n_q_heads and shape[3] == p.head_dim and out.shape == shape, \
         f"q and out: [B, Hq, new tokens, d] = ({p.batch}, {p.n_q_heads}, new tokens, {p.head_dim})"
