@@ -92,38 +92,58 @@ __device__ __forceinline__ NewRows new_rows(const AppendRowsArgs& a, int b, int 
     return x;
 }
 
-// the sixteen values' extremes over the lanes of a row
+__device__ __forceinline__ uint32_t min2_nan(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// the smallest and the largest of a bf16 row's values, of which every lane has sixteen (two at a time: they are bf16 values)
 template <int kLanes>
-__device__ __forceinline__ void row_range(const float (&f)[16], float& lo, float& hi) {
-    lo = hi = f[0];
+__device__ __forceinline__ void row_range(const Eight<false>& r0, const Eight<false>& r1, float& lo, float& hi) {
+    const uint32_t w[8] = {r0.x[0].x, r0.x[0].y, r0.x[0].z, r0.x[0].w, r1.x[0].x, r1.x[0].y, r1.x[0].z, r1.x[0].w};
+    uint32_t l = w[0], h = w[0];
 #pragma unroll
-    for (int j = 1; j < 16; ++j) { lo = min_nan(lo, f[j]); hi = max_nan(hi, f[j]); }
+    for (int j = 1; j < 8; ++j) { l = min2_nan(l, w[j]); h = max2_nan(h, w[j]); }
 #pragma unroll
     for (int d = 1; d < kLanes; d <<= 1) {
-        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+        l = min2_nan(l, __shfl_xor_sync(0xffffffffu, l, d));
+        h = max2_nan(h, __shfl_xor_sync(0xffffffffu, h, d));
     }
+    lo = min_nan(bf16_lo(l), bf16_hi(l));
+    hi = max_nan(bf16_lo(h), bf16_hi(h));
 }
 __device__ __forceinline__ uint32_t eight_codes(const float* f, float lo, float inv) {
+    // Adding 1.5 x 2^23 rounds to a whole number, which is then what the number's bits are more than 0x4b400000; of the eight of
+    // these, shifted to their places, what does not leave the word is 0x4b400000 x 0x11111111.
     uint32_t w = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        // (adding 1.5 x 2^23 rounds to a whole number, which is then in the low bits)
-        const uint32_t c = __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(f[j], lo), inv), 12582912.f)) & 15u;
-        w |= c << (4 * j);
-    }
-    return w;
+    for (int j = 7; j >= 0; --j) w = w * 16u + __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(f[j], lo), inv), 12582912.f));
+    return w - 0x4b400000u * 0x11111111u;
+}
+// t / n and what is left, with m = 2^32 / n + 1 rounded down (t < 2^31: the product is at most one too many)
+__device__ __forceinline__ uint32_t divide(uint32_t t, uint32_t n, uint32_t m, uint32_t& rest) {
+    uint32_t q = __umulhi(t, m);
+    rest = t - q * n;
+    if (int32_t(rest) < 0) { --q; rest += n; }
+    return q;
 }
 
-// Grid (token tiles of a sequence x sequences, pieces of the heads).  Bound by memory: every byte is read and written once.
+// Grid (token tiles of a sequence x sequences, pieces of the heads).  Bound by memory: every byte is read and written once.  A
+// step takes two rows of a token, K and V of a head or two heads of Q, so that what belongs to the token is computed once for
+// both and 64 bytes are on their way per lane.
 template <bool kF32, bool kFour, int kLanes>             // kLanes = d / 16
-__global__ void __launch_bounds__(kThreads) append_rows_kernel(const AppendRowsArgs a) {
+__global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(const AppendRowsArgs a) {
     const int tid = threadIdx.x, L = tid % kLanes, group = tid / kLanes;
     const int b = blockIdx.x / a.token_tiles, tile = blockIdx.x - b * a.token_tiles;
-    const int H = a.n_kv_heads, slots = 2 * H + a.n_q_heads;         // K rows, V rows, rows of Q
+    const int H = a.n_kv_heads, pairs = H + (a.n_q_heads + 1) / 2;
     const int log_tok = a.log_tokens, strides = (kThreads / kLanes) >> log_tok;      // groups per token
     const int local = group & ((1 << log_tok) - 1);
-    const int slot0 = int(blockIdx.y) * a.slots_per_block, slot_end = min(slot0 + a.slots_per_block, slots);
+    const int pair0 = int(blockIdx.y) * a.pairs_per_block, pair1 = min(pair0 + a.pairs_per_block, pairs);
     const int pair_lanes = a.rope.dim / 16;              // lanes whose values are rotated
     const bool turned = L < pair_lanes;
     const bool halves = turned && !a.rope.interleaved;
@@ -133,27 +153,45 @@ __global__ void __launch_bounds__(kThreads) append_rows_kernel(const AppendRowsA
         const int i = t0 + local;
         float cs[8], sn[8];
         int at = -1;                                     // row of the table that cs and sn come from
-#pragma unroll 2
-        for (int s_base = slot0; s_base < slot_end; s_base += strides) {
-            const int s = s_base + (group >> log_tok);
-            // (every lane goes through the shuffles, with or without a row)
-            const bool is_q = s >= 2 * H, is_v = !is_q && s >= H;
-            const int hq = s - 2 * H, h = is_q ? hq / a.group : is_v ? s - H : s;
-            bool here = s < slot_end && i < a.max_new;
-            NewRows x = {0, 0, 0};
-            if (here) x = new_rows(a, b, h, false);
-            here = here && i < (is_q ? x.brought : x.stored);
-            const bool turn = !is_v && turned, apart = !is_v && halves;
-            const int c0 = apart ? L : 2 * L, c1 = apart ? L + pair_lanes : 2 * L + 1;
-            float f[16];
-            Eight<kF32> r0, r1;
-            if (here) {
-                const RowTensor& from = is_q ? a.q : is_v ? a.v_new : a.k_new;
-                const char* const row = static_cast<const char*>(from.ptr) + b * from.sb + (is_q ? hq : h) * from.sh + i * from.st;
-                r0 = load_eight<kF32>(row, c0);
-                r1 = load_eight<kF32>(row, c1);
+        for (int s0 = pair0; s0 < pair1; s0 += strides) { // (the same for the whole block)
+            const int s = s0 + (group >> log_tok);
+            const bool is_q = s >= H, inside = s < pair1 && i < a.max_new;
+            int head[2], kv[2], start[2];                // of the two rows: heads, KV heads, rows in front of the new ones
+            bool here[2] = {false, false};
+            Eight<kF32> r[2][2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                head[k] = is_q ? 2 * (s - H) + k : s;
+                kv[k] = head[k];
+                start[k] = 0;
+                if (is_q && a.group > 1) { uint32_t rest; kv[k] = int(divide(uint32_t(head[k]), uint32_t(a.group), a.group_inverse, rest)); }
+                if (!inside || (is_q && head[k] >= a.n_q_heads)) continue;
+                const NewRows n = new_rows(a, b, kv[k], false);
+                start[k] = n.first;
+                here[k] = i < (is_q ? n.brought : n.stored);
+                if (!here[k]) continue;
+                const RowTensor& from = is_q ? a.q : k ? a.v_new : a.k_new;
+                const char* const row = static_cast<const char*>(from.ptr) + b * from.sb + head[k] * from.sh + i * from.st;
+                const bool apart = halves && (is_q || k == 0);
+                r[k][0] = load_eight<kF32>(row, apart ? L : 2 * L);
+                r[k][1] = load_eight<kF32>(row, apart ? L + pair_lanes : 2 * L + 1);
+            }
+            uint32_t slot = 0;
+            int page = 0;
+            if (!is_q && here[0]) page = a.page_table[int64_t(b) * a.max_pages + divide(uint32_t(start[0] + i), uint32_t(a.page_rows), a.page_inverse, slot)];
+            const bool astray = page < 0 || page >= a.n_pages;
+            if (astray && L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bool turn = here[k] && turned && (is_q || k == 0), apart = halves && (is_q || k == 0);
+                const int c0 = apart ? L : 2 * L, c1 = apart ? L + pair_lanes : 2 * L + 1;
+                float f[16];
+                if (turn || (kFour && here[k])) {
+                    widen<kF32>(r[k][0], f);
+                    widen<kF32>(r[k][1], f + 8);
+                }
                 if (turn) {
-                    int pos = a.rope.positions ? a.rope.positions[b * a.rope.pos_sb + i] : x.first + i;
+                    int pos = a.rope.positions ? a.rope.positions[b * a.rope.pos_sb + i] : start[k] + i;
                     if (pos < 0 || pos >= a.rope.table_rows) {
                         if (L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
                         pos = pos < 0 ? 0 : a.rope.table_rows - 1;
@@ -169,12 +207,6 @@ __global__ void __launch_bounds__(kThreads) append_rows_kernel(const AppendRowsA
                             sn[j] = z.x; sn[j + 1] = z.y; sn[j + 2] = z.z; sn[j + 3] = z.w;
                         }
                     }
-                }
-            }
-            if (here && (turn || kFour)) {
-                widen<kF32>(r0, f);
-                widen<kF32>(r1, f + 8);
-                if (turn) {
                     if (apart) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
@@ -190,53 +222,43 @@ __global__ void __launch_bounds__(kThreads) append_rows_kernel(const AppendRowsA
                             f[2 * j + 1] = __fadd_rn(__fmul_rn(x2, cs[j]), __fmul_rn(x1, sn[j]));
                         }
                     }
-                    r0 = narrow<kF32>(f);
-                    r1 = narrow<kF32>(f + 8);
-                    if (kFour) { widen<kF32>(r0, f); widen<kF32>(r1, f + 8); }       // what a bf16 cache would hold
+                    r[k][0] = narrow<kF32>(f);
+                    r[k][1] = narrow<kF32>(f + 8);
+                    if (kFour) { widen<kF32>(r[k][0], f); widen<kF32>(r[k][1], f + 8); }     // what a bf16 cache would hold
                 }
-            }
-            float lo = 0.f, hi = 0.f;
-            if (kFour) {
-                if (!here) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) f[j] = 0.f;
+                float lo = 0.f, hi = 0.f;
+                // (every lane goes through the shuffles, with or without a row)
+                if constexpr (kFour) row_range<kLanes>(r[k][0], r[k][1], lo, hi);
+                if (!here[k]) continue;
+                if (is_q) {
+                    char* const row = static_cast<char*>(a.q_out.ptr) + b * a.q_out.sb + head[k] * a.q_out.sh + i * a.q_out.st;
+                    store_eight<kF32>(row, c0, r[k][0]);
+                    store_eight<kF32>(row, c1, r[k][1]);
+                    continue;
                 }
-                row_range<kLanes>(f, lo, hi);
-            }
-            if (!here) continue;
-            if (is_q) {
-                char* const row = static_cast<char*>(a.q_out.ptr) + b * a.q_out.sb + hq * a.q_out.sh + i * a.q_out.st;
-                store_eight<kF32>(row, c0, r0);
-                store_eight<kF32>(row, c1, r1);
-                continue;
-            }
-            const uint32_t t = uint32_t(x.first + i), slot = t % uint32_t(a.page_rows);
-            const int page = a.page_table[int64_t(b) * a.max_pages + t / uint32_t(a.page_rows)];
-            if (page < 0 || page >= a.n_pages) {
-                if (L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
-                continue;
-            }
-            const RowTensor& to = is_v ? a.v : a.k;
-            char* const row = static_cast<char*>(to.ptr) + page * to.sb + h * to.sh + slot * to.st;
-            if (!kFour) {
-                store_eight<kF32>(row, c0, r0);
-                store_eight<kF32>(row, c1, r1);
-            } else {
-                uint32_t pair = pack_bf16(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), lo);
-                float scale = bf16_lo(pair);
-                if (scale < kSmallest) { scale = 0.f; pair &= 0xffff0000u; }
-                if (!(scale < INFINITY)) pair |= 0x7fffu;        // the whole row is no number
-                const float inv = scale > 0.f ? __fmul_rn(__frcp_rn(scale), 1.f + 0x1p-21f) : 0.f;
-                const uint32_t w0 = eight_codes(f, lo, inv), w1 = eight_codes(f + 8, lo, inv);
-                if (apart) {
-                    reinterpret_cast<uint32_t*>(row)[c0] = w0;
-                    reinterpret_cast<uint32_t*>(row)[c1] = w1;
+                if (astray) continue;
+                const RowTensor& to = k ? a.v : a.k;
+                char* const row = static_cast<char*>(to.ptr) + page * to.sb + s * to.sh + slot * to.st;
+                if (!kFour) {
+                    store_eight<kF32>(row, c0, r[k][0]);
+                    store_eight<kF32>(row, c1, r[k][1]);
                 } else {
-                    reinterpret_cast<uint2*>(row)[L] = make_uint2(w0, w1);
-                }
-                if (L == 0) {
-                    const RowTensor& sc = is_v ? a.v_scales : a.k_scales;
-                    *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page * sc.sb + h * sc.sh + slot * 4) = pair;
+                    uint32_t pair = pack_bf16(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), lo);
+                    float scale = bf16_lo(pair);
+                    if (scale < kSmallest) { scale = 0.f; pair &= 0xffff0000u; }
+                    if (!(scale < INFINITY)) pair |= 0x7fffu;    // the whole row is no number
+                    const float inv = scale > 0.f ? __fmul_rn(__frcp_rn(scale), 1.f + 0x1p-21f) : 0.f;
+                    const uint32_t w0 = eight_codes(f, lo, inv), w1 = eight_codes(f + 8, lo, inv);
+                    if (apart) {
+                        reinterpret_cast<uint32_t*>(row)[c0] = w0;
+                        reinterpret_cast<uint32_t*>(row)[c1] = w1;
+                    } else {
+                        reinterpret_cast<uint2*>(row)[L] = make_uint2(w0, w1);
+                    }
+                    if (L == 0) {
+                        const RowTensor& sc = k ? a.v_scales : a.k_scales;
+                        *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page * sc.sb + s * sc.sh + slot * 4) = pair;
+                    }
                 }
             }
         }
@@ -339,7 +361,9 @@ csp_status append_rows(const AppendRowsArgs& a, dim3 grid, cudaStream_t s) {
 
 csp_status launch_append_rows(AppendRowsArgs a, int head_dim, bool f32, bool four, cudaStream_t s) {
     if (a.batch == 0) return CSP_OK;
-    const int groups = kThreads / (head_dim / 16), slots = 2 * a.n_kv_heads + a.n_q_heads;
+    const int groups = kThreads / (head_dim / 16), pairs = a.n_kv_heads + (a.n_q_heads + 1) / 2;
+    a.page_inverse = uint32_t((uint64_t(1) << 32) / uint32_t(a.page_rows)) + 1u;
+    a.group_inverse = a.group > 1 ? uint32_t((uint64_t(1) << 32) / uint32_t(a.group)) + 1u : 0u;
     // Few tokens: the lane groups of a block spread over the heads; from eight on, eight tokens share a block and every group goes
     // over some of the heads with one set of cosines.
     a.log_tokens = 0;
@@ -350,11 +374,11 @@ csp_status launch_append_rows(AppendRowsArgs a, int head_dim, bool f32, bool fou
     const int step = groups >> a.log_tokens;             // heads at a time
     const int64_t blocks = int64_t(a.token_tiles) * a.batch;
     // as many pieces of the heads as it takes to give every SM four blocks
-    int pieces = (slots + step - 1) / step;
+    int pieces = (pairs + step - 1) / step;
     const int64_t want = (4 * int64_t(sm_count()) + blocks - 1) / blocks;
     if (pieces > want) pieces = int(want);
-    a.slots_per_block = ((slots + step - 1) / step + pieces - 1) / pieces * step;
-    pieces = (slots + a.slots_per_block - 1) / a.slots_per_block;
+    a.pairs_per_block = ((pairs + step - 1) / step + pieces - 1) / pieces * step;
+    pieces = (pairs + a.pairs_per_block - 1) / a.pairs_per_block;
     const dim3 grid{unsigned(blocks), unsigned(pieces)};
     if (four) return head_dim == 64 ? append_rows<false, true, 4>(a, grid, s) : append_rows<false, true, 8>(a, grid, s);
     if (f32) return head_dim == 32 ? append_rows<true, false, 2>(a, grid, s) : head_dim == 64 ? append_rows<true, false, 4>(a, grid, s) : append_rows<true, false, 8>(a, grid, s);

@@ -260,8 +260,10 @@ struct AppendRowsArgs {
     int32_t batch, n_kv_heads, n_q_heads, group, max_new, capacity;   // n_q_heads 0: no queries
     const int32_t* page_table; int32_t max_pages, page_rows, n_pages;
     int32_t* status;
-    // chosen by the launcher: tokens per block (base-2 logarithm), blocks along the tokens of a sequence, heads per block
-    int32_t log_tokens, token_tiles, slots_per_block;
+    // chosen by the launcher: tokens per block (base-2 logarithm), blocks along the tokens of a sequence, pairs of rows per block
+    // and token; 2^32 / page_rows and / group, for division
+    int32_t log_tokens, token_tiles, pairs_per_block;
+    uint32_t page_inverse, group_inverse;
 };
 struct LoadRowsArgs {
     RowTensor k, v, k_scales, v_scales, k_out, v_out;    // v.ptr null: K only
