@@ -485,9 +485,11 @@ size_t csp_chunk_q4_workspace_bytes(const csp_params* p, int32_t max_new);
  * csp_chunk_attn_paged over a cache in 4 bits: the same attention of the values base + scale * code, with everything that it
  * says of n_rows, n_new, mods, out and lse (rows that are only masked must have finite scale and base, rows behind n_rows may
  * hold anything).  q and out bf16, head_dim 64 or 128.
- * The codes enter the products as they are, whole numbers, and the two numbers of a row are applied to sums in fp32, so that
- * nothing of K is rounded again; a weight, times its row's scale in V, is rounded to fp16 (11 bits) before it meets V.  Of a
- * query, parts below 2^-24 of its largest one are lost.
+ * The codes of K enter the products as they are, whole numbers, and the two numbers of a row are applied to sums in fp32, so
+ * that nothing of K is rounded again.  Of a query, whose values have to be below 2^112, parts below 2^-34 of its largest one
+ * are lost.  With up to two groups of sixteen query rows per KV head (max_new x H_q / H_kv) the same holds of V, and a
+ * weight times its row's scale is rounded to fp16 (11 bits).  With more of them a weight is rounded to fp16, and so is a value
+ * base + scale * code of V, relative to the largest of the rows seen: one below 2^-7 of that is off by up to 2^-17 of it.
  */
 csp_status csp_chunk_attn_q4_paged(const csp_params* p, int32_t max_new, csp_tensor q, const csp_q4_cache* k_cache,
                                    const csp_q4_cache* v_cache, const csp_pages* pages, const int32_t* n_rows,

@@ -13,8 +13,8 @@
 // dimensions come: the query is laid out alike.  For the second one the rows of V are transposed as 16-bit pieces of four codes on
 // their way into registers.
 //
-// Queries are scaled by a power of two, row by row, so that their largest value lies in [1, 2): a half holds every bf16
-// value exactly from there down to 2^-14 of it.  A weight times its row's scale is rounded to a half (11 bits), relative to a power
+// Queries are scaled by a power of two, row by row, so that their largest value lies in [2^10, 2^11): a half holds every bf16
+// value exactly from there down to 2^-24 of it, and 16 times the largest.  A weight times its row's scale is rounded to a half (11 bits), relative to a power
 // of two that follows the largest scale seen as the softmax's reference follows the largest logit.
 // (Codes of K as e4m3 bytes, which four zeros and a code are as well, take half of the ANDs, but the compiler makes halves of
 // them before it multiplies: 650 instructions per tile of 32 keys instead of 510.)
@@ -399,10 +399,10 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
             top2 = max_abs2(top2, top2 >> 16 | top2 << 16);
             top2 = max_abs2(top2, __shfl_xor_sync(0xffffffffu, top2, 1));
             top2 = max_abs2(top2, __shfl_xor_sync(0xffffffffu, top2, 2));
-            const uint32_t ex = (top2 & 0x7fffu) >> 7;   // 255: an infinity, the row is no number
-            const float down = ex == 255u ? 0.f : __uint_as_float((254u - ex) << 23), down16 = 16.f * down;      // 2^-e (0: 2^127)
-            // logit = up 2^20 (scale S + base sum 2^-20), S the product with codes 2^-20
-            const float up = a.scale * kLog2e * 0x1p20f * (ex == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(ex << 23));
+            const uint32_t top = (top2 & 0x7fffu) >> 7, ex = max(top, 14u);      // top 255: an infinity, the row is no number
+            const float down = __uint_as_float((264u - ex) << 23), down16 = 16.f * down;                 // 2^(10 - e)
+            // logit = up (scale S + base sum 2^-20), S the product with codes 2^-20
+            const float up = a.scale * kLog2e * 0x1p10f * (top == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(ex << 23));
             factor[n] = make_float2(__shfl_sync(0xffffffffu, up, 8 * qd), __shfl_sync(0xffffffffu, up, 8 * qd + 4));
             float ones[4] = {0.f, 0.f, 0.f, 0.f};        // the product with codes of one: the query's sum 2^-20
 #pragma unroll

@@ -4,7 +4,7 @@
 //
 // A row is base + scale code.  Of K the products see the codes, exactly: a half whose lowest four bits are a code is the number
 // code 2^-24, with the code in the next four bits it is code 2^-20, so that unpacking eight codes takes four ANDs and a
-// shift and no arithmetic.  S = Q' codes^T with Q' the query in halves, scaled by a power of two per row (largest value in [1, 2)) and by
+// shift and no arithmetic.  S = Q' codes^T with Q' the query in halves, scaled by a power of two per row (largest value in [2^10, 2^11)) and by
 // 16 where a code is in the lower place; then  logit = up (scale_t S + base_t sum Q')  with the two numbers of a row applied in fp32
 // by the softmax threads: nothing of K is rounded.  (Half of the products scale x code would not fit the eleven bits of a half.)
 // Of V they see the values base + scale code, rounded to halves relative to a power of two that follows the largest value of
@@ -638,14 +638,15 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                         }
                         top2 = max_abs2(top2, top2 >> 16 | top2 << 16);
                         top2 = max_abs2(top2, __float_as_uint(other_half(__uint_as_float(top2))));
-                        const uint32_t ex = (top2 & 0x7fffu) >> 7;       // 255: an infinity, the row is no number
-                        const float down = ex == 255u ? 0.f : __uint_as_float((254u - ex) << 23), down16 = 16.f * down;      // 2^-e
+                        const uint32_t top = (top2 & 0x7fffu) >> 7, ex = max(top, 14u);      // top 255: an infinity, the row is no number
+                        const float down = __uint_as_float((264u - ex) << 23), down16 = 16.f * down;         // 2^(10 - e)
                         float sum = 0.f;
 #pragma unroll
                         for (int c = 0; c < kChunks; ++c) {
                             const uint4 y = *chunk(c);
                             const float f[8] = {lo_bf16(y.x), hi_bf16(y.x), lo_bf16(y.y), hi_bf16(y.y), lo_bf16(y.z), hi_bf16(y.z), lo_bf16(y.w), hi_bf16(y.w)};
-                            sum += ((f[0] + f[1]) + (f[2] + f[3])) * down + ((f[4] + f[5]) + (f[6] + f[7])) * down;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) sum = fmaf(f[j], down, sum);
                             *chunk(c) = make_uint4(pack_f16(down16 * f[0], down16 * f[4]), pack_f16(down * f[1], down * f[5]),
                                                    pack_f16(down16 * f[2], down16 * f[6]), pack_f16(down * f[3], down * f[7]));
                         }
@@ -653,7 +654,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                         sum += other_half(sum);
                         // S is the product with codes 2^-20
                         // (never zero: it meets the minus infinities of hidden keys)
-                        factor = ex == 255u ? __uint_as_float(0x7fc00000u) : fmaxf(a.scale * kLog2e * 0x1p20f * __uint_as_float(ex << 23), 0x1p-126f);
+                        factor = top == 255u ? __uint_as_float(0x7fc00000u) : fmaxf(a.scale * kLog2e * 0x1p10f * __uint_as_float(ex << 23), 0x1p-126f);
                         q_sum = sum * 0x1p-20f;
                         if (half == 0) row_const[slot * 128 + m] = make_float2(factor, q_sum);
                         __syncwarp();

@@ -83,7 +83,11 @@ def check(got_out, got_lse, q, dense, rows, new, what="", n=1.0, scale=0.0, **mo
                   + (r 2^-11 + 4 e + 2^-23 L) sum w (s c + |b|) r = 1: weights times scales are rounded to halves; r = 2, with more than
                                                             sixteen query rows per KV head: weights are, and the values of V; e as
                                                             there; L rows added up
-                  + L 2^-25 15 max s                            weights times scales below 2^-14 of the largest scale
+                  + L 2^-25 15 max s                            weights times scales below 2^-14 of the largest scale; r = 2: weights
+                                                            below 2^-14, of the largest values
+                  + (r = 2) 2^-17 max (15 s + |b|)              the values of V are halves times 2^7 of a power of two that is at most
+                                                            the largest of them: base and sum, each rounded by up to 2^-25 where
+                                                            they are below 2^-14, and the weights add up to one at most
                   + 2^-126"""
     (kc, ks), (vc, vs) = dense
     K, V = values(kc, ks), values(vc, vs)
@@ -107,8 +111,10 @@ def check(got_out, got_lse, q, dense, rows, new, what="", n=1.0, scale=0.0, **mo
             mk = mag_k[b, hq // G, :L]
             e = err[b, hq, :N] + sc * (2.0 ** -23 * (d + 4) * (qa @ mk.T).amax(1) + 2.0 ** -25 * qa.amax(1) * (K - ks[..., 1:].double())[b, hq // G, :L].sum(1).max())
             o, g, m = out[b, hq, :N], got[b, hq, :N], mass[b, hq, :N]
-            s_max = float(vs[b, hq // G, :L, 0].double().max())
-            tol = 2.0 ** -8 * o.abs() * (1 + 2.0 ** -8) + (rounds * 2.0 ** -11 + 4 * e[:, None] + 2.0 ** -23 * L) * m + L * 2.0 ** -25 * 15 * s_max + 2.0 ** -126
+            s_max = 15 * float(vs[b, hq // G, :L, 0].double().max())
+            v_max = float((15 * vs[b, hq // G, :L, 0].double() + vs[b, hq // G, :L, 1].double().abs()).max())
+            small = L * 2.0 ** -25 * s_max if rounds == 1 else (L * 2.0 ** -25 + 2.0 ** -17) * v_max
+            tol = 2.0 ** -8 * o.abs() * (1 + 2.0 ** -8) + (rounds * 2.0 ** -11 + 4 * e[:, None] + 2.0 ** -23 * L) * m + small + 2.0 ** -126
             assert torch.isfinite(g).all(), f"{what}: sequence {b}, head {hq}: non-finite outputs"
             bad = (g - o).abs() > tol
             assert not bad.any(), (f"{what}: sequence {b}, head {hq}: {int(bad.sum())} of {bad.numel()} outputs off, first at "

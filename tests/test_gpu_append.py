@@ -274,3 +274,135 @@ def test_flags(csp):
     assert call([[0, 1], [2, 3]], None, [[0, 1], [-1, 3]]) == (csp.DEV_BAD_LEN, [[4, 5], [6, 7]], 8)
     assert call([[0, 1], [2, 3]], None, ok, pos=[[0, 1, 10, 3], [0, 1, 2, -5]]) == (csp.DEV_BAD_LEN, [[4, 5], [6, 7]], 16)
     assert call([[0, 1], [2, 3]], [0, 0], ok) == (0, [[0, 1], [2, 3]], 0)
+
+
+@pytest.mark.parametrize("H,G", [(1, 1), (3, 1), (1, 7), (5, 3), (2, 8), (8, 5)])
+@pytest.mark.parametrize("T", [1, 6, 70])
+@pytest.mark.parametrize("four", [False, True])
+def test_heads_of_all_counts(csp, H, G, T, four):
+    """Odd numbers of query heads, more heads than a block has groups of lanes for, a batch of several sequences."""
+    B, d, R = 5, 64, 128
+    p, first, new, per, table, (k, v, q), n_pages = _setup(csp, [[3 + 40 * b] * H for b in range(B)], [T, max(T - 1, 0), T, 0, 1], H, G, d, torch.bfloat16, seed=H + G + T)
+    cs = _table(48, 400)
+    slots = k.shape[2]
+    q_out = torch.full((B, H * G, slots, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    K, V = (csp.new_q4_cache(n_pages, H, R, d) if four else torch.zeros(n_pages, H, R, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    rows, ws = first.cuda(), csp.new_append_workspace(p)
+    call = csp.append_q4_paged if four else csp.append_rope_paged
+    call(p, k.cuda(), v.cuda(), K, V, table.cuda(), rows, rows, ws, rope=csp.Rope(cs.cuda(), interleaved=bool(G % 2)), n_new=new.cuda(), q=q.cuda(), q_out=q_out)
+    assert csp.device_status(ws) == 0 and torch.equal(rows.cpu(), first + per)
+    at = first[:, :1, None] + torch.arange(slots)
+    for x, got_all, heads in ((q, q_out.cpu(), H * G), (k, None, H)):
+        want, mag = _rotated(x, cs, at.expand(B, heads, slots).clamp(max=399), bool(G % 2))
+        for b in range(B):
+            n = int(new[b])
+            if got_all is not None:
+                _close(got_all[b, :, :n], want[b, :, :n], mag[b, :, :n], torch.bfloat16)
+                assert (got_all[b, :, n:] == 9.0).all()
+            elif n:
+                page, slot = _where(table, b, first[b, 0] + torch.arange(n), R)
+                if four:
+                    c, s = K.codes.cpu()[page, :, slot], K.scales.cpu()[page, :, slot]
+                    step = s[..., :1].double().transpose(0, 1)
+                    # half a step, fifteen roundings of the step, and the rotated row's rounding to bf16 (the largest value's)
+                    slack = step * (0.5 + 15 * 2.0 ** -8) + 2.0 ** -7 * mag[b, :, :n].amax(-1, keepdim=True)
+                    assert ((values(c, s).transpose(0, 1) - want[b, :, :n]).abs() <= slack).all()
+                else:
+                    _close(K.cpu()[page, :, slot].transpose(0, 1), want[b, :, :n], mag[b, :, :n], torch.bfloat16)
+
+
+def test_captured_appends_replay(csp):
+    """Two appends in one graph, the counts updated in place: every replay goes on where the last one ended, and lands
+    where calls outside of a graph do."""
+    B, H, G, d, R = 2, 2, 2, 128, 128
+    p = csp.Params(B, H * G, H, d, 1, 0, 512, 512)
+    gen = torch.Generator().manual_seed(2)
+    k, v, q = (torch.randn(B, h, 40, d, generator=gen).to(torch.bfloat16).cuda() for h in (H, H, H * G))
+    table = torch.randperm(8, generator=gen).reshape(B, 4).to(torch.int32).cuda()
+    rope = csp.Rope(_table(d, 512).cuda())
+    ends = []
+    for captured in (False, True):
+        K, V = csp.new_q4_cache(8, H, R, d), csp.new_q4_cache(8, H, R, d)
+        rows, ws, new = torch.zeros(B, H, dtype=torch.int32, device="cuda"), csp.new_append_workspace(p), torch.tensor([40, 7], dtype=torch.int32, device="cuda")
+        q_out = torch.zeros_like(q)
+
+        def two():
+            csp.append_q4_paged(p, k, v, K, V, table, rows, rows, ws, n_new=new, rope=rope, q=q, q_out=q_out)
+            csp.append_q4_paged(p, v[:, :, :1], k[:, :, :1], K, V, table, rows, rows, ws)
+        two()
+        if captured:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                two()
+            for _ in range(3):
+                graph.replay()
+        else:
+            for _ in range(3):
+                two()
+        assert csp.device_status(ws) == 0
+        assert rows.cpu().tolist() == [[164, 164], [32, 32]]
+        ends.append((K.codes, K.scales, V.codes, V.scales, q_out))
+    assert all(torch.equal(a, b) for a, b in zip(*ends))
+
+
+def test_strided_pools_and_another_stream(csp):
+    B, H, d, R = 2, 3, 64, 128
+    p = csp.Params(B, H, H, d, 1, 0, 256, 256)
+    gen = torch.Generator().manual_seed(4)
+    k, v = (torch.randn(B, 33, H, d + 8, generator=gen).to(torch.bfloat16).cuda()[..., :d].transpose(1, 2) for _ in range(2))
+    table = torch.tensor([[3, 0], [2, 1]], dtype=torch.int32, device="cuda")
+    plain = [csp.new_q4_cache(4, H, R, d) for _ in range(2)]
+    codes = torch.full((2, H, 5, R * d // 2 + 16), 0x77, dtype=torch.uint8, device="cuda")
+    scales = torch.full((2, H, 5, R * 2 + 8), 3.0, dtype=torch.bfloat16, device="cuda")
+    gaps = [csp.Q4Cache(codes[i].as_strided((4, H, R, d // 2), (codes.stride(2), codes.stride(1), d // 2, 1), codes[i].storage_offset()),
+                        scales[i].as_strided((4, H, R, 2), (scales.stride(2), scales.stride(1), 2, 1), scales[i].storage_offset())) for i in range(2)]
+    for c in gaps:
+        c.codes.zero_(), c.scales.zero_()
+    before = [int((codes == 0x77).sum()), int((scales == 3.0).sum())]
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    outs = []
+    for pools in (plain, gaps):
+        rows, after, ws = (torch.full((B, H), 111, dtype=torch.int32, device="cuda"), torch.zeros(B, H, dtype=torch.int32, device="cuda"), csp.new_append_workspace(p))
+        back = [torch.zeros(B, 40, H, d + 8, dtype=torch.bfloat16, device="cuda")[..., :d].transpose(1, 2) for _ in range(2)]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            csp.append_q4_paged(p, k, v, *pools, table, rows, after, ws)
+            csp.load_q4_paged(p, *pools, table, after, *back, ws, first=rows)
+        stream.synchronize()
+        assert csp.device_status(ws) == 0 and (after == 144).all()
+        outs.append(back)
+    for i in range(2):
+        assert torch.equal(plain[i].codes, gaps[i].codes) and torch.equal(plain[i].scales, gaps[i].scales) and torch.equal(outs[0][i], outs[1][i])
+    gone = sum(int((c.codes == 0x77).sum()) for c in gaps)
+    assert int((codes == 0x77).sum()) - gone == before[0] and int((scales == 3.0).sum()) - sum(int((c.scales == 3.0).sum()) for c in gaps) == before[1]
+
+
+def test_tensors_on_another_device_are_refused(csp):
+    B, H, d = 1, 2, 64
+    p = csp.Params(B, H, H, d, 1, 0, 128, 128)
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    k, pool = torch.zeros(B, H, 3, d, **bf), torch.zeros(1, H, 128, d, **bf)
+    K = csp.new_q4_cache(1, H, 128, d)
+    rows, table = torch.zeros(B, H, dtype=torch.int32, device="cuda"), torch.zeros(B, 1, dtype=torch.int32, device="cuda")
+    ws, cs = csp.new_append_workspace(p), _table(d, 200).cuda()
+    pos = torch.zeros(B, 3, dtype=torch.int32)
+    half = csp.Q4Cache(K.codes, K.scales.cpu())
+    ropes = (csp.Rope(cs.cpu()), csp.Rope(cs, positions=pos))
+    good = dict(k=k, v=k, K=K, V=K, rows=rows, out=rows, table=table, ws=ws, rope=csp.Rope(cs), q=k, q_out=k.clone(), n_new=None)
+
+    def call(four, **kw):
+        a = dict(good, **kw)
+        if not four:
+            a["K"] = a["V"] = kw.get("pool", pool)
+        f = csp.append_q4_paged if four else csp.append_rope_paged
+        f(p, a["k"], a["v"], a["K"], a["V"], a["table"], a["rows"], a["out"], a["ws"], rope=a["rope"], n_new=a["n_new"], q=a["q"], q_out=a["q_out"])
+    for four in (True, False):
+        for kw in (dict(k=k.cpu()), dict(v=k.cpu()), dict(rows=rows.cpu()), dict(out=rows.cpu()), dict(table=table.cpu()), dict(ws=ws.cpu()),
+                   dict(rope=ropes[0]), dict(rope=ropes[1]), dict(q=k.cpu()), dict(q_out=k.cpu()), dict(n_new=torch.zeros(1, dtype=torch.int32)),
+                   dict(K=half) if four else dict(pool=pool.cpu())):
+            with pytest.raises(ValueError):
+                call(four, **kw)
+    for kw in (dict(a=half), dict(a=K, rows=rows.cpu()), dict(a=K, first=rows.cpu()), dict(a=K, table=table.cpu()), dict(a=K, out=k.cpu()), dict(a=K, ws=ws.cpu())):
+        with pytest.raises(ValueError):
+            csp.load_q4_paged(p, kw["a"], None, kw.get("table", table), kw.get("rows", rows), kw.get("out", k), None, kw.get("ws", ws), first=kw.get("first"))
