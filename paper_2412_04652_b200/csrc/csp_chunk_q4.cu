@@ -76,6 +76,10 @@ __device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src, bool t
 __device__ __forceinline__ float lo_bf16(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
 
+constexpr int kDeskBytes = 512;
+// What a variant's code deals with.  (One variant for all of them: 49 -> 52 us for five capped tokens, 30.5 -> 32 us for a bias.)
+enum Mods { kNone, kCap, kBias, kAny };
+
 template <int NH, int RH>   // head_dim = 64 NH, 8 RH query rows
 struct Q4Shape {
     static constexpr int D = 64 * NH, R = 8 * RH;
@@ -89,8 +93,8 @@ struct Q4Shape {
     static constexpr uint32_t kFront = kWarps * kSlots * kSlotBytes;                   // [warp]: the piece that a warp begins with
     static constexpr uint32_t kNotes = kFront + kWarps * kPieceBytes;                  // [warp]
     static constexpr uint32_t kTable = kNotes + kWarps * 16;                           // [warp][R] RowNote
-    static constexpr uint32_t kDesk = kTable + kWarps * R * 16;                        // [warp] three Segments: loaded, computed, of the front piece
-    static constexpr uint32_t kScratch = kDesk + kWarps * 192;                         // of find_share
+    static constexpr uint32_t kDesk = kTable + kWarps * R * 16;                        // [warp] Desk
+    static constexpr uint32_t kScratch = kDesk + kWarps * kDeskBytes;                  // of find_share
     static constexpr uint32_t kChains = kScratch + 68 * 4;                             // of find_share; then whether this block joins them
     static constexpr uint32_t kTotal = kChains + 6 * 4;
     static constexpr int kThreads = 32 * kWarps;
@@ -99,9 +103,9 @@ struct Q4Shape {
 
 // One warp's part of the block's share: from tile begin_tile of item begin on, up to tile end_tile of item end (none of that
 // item's where end_tile is the block's first).  The block's tiles, and one more per item, are cut into equal parts; everybody goes
-// over the block's items, a lane per item.
+// over the block's items, a lane per item.  *first: the range of item begin.
 struct WarpShare { int begin, begin_tile, end, end_tile; };
-__device__ __forceinline__ WarpShare warp_share(const ChunkArgs& a, const ChunkPlan& pl, const Share& sh, int warp, int warps, int lane) {
+__device__ __forceinline__ WarpShare warp_share(const ChunkArgs& a, const ChunkPlan& pl, const Share& sh, int warp, int warps, int lane, PairRange* first) {
     const int last = min(sh.item1, pl.n_items - 1);
     WarpShare got = {pl.n_items, 0, pl.n_items, 0};
     int total = 0, part = 0;
@@ -115,10 +119,11 @@ __device__ __forceinline__ WarpShare warp_share(const ChunkArgs& a, const ChunkP
         for (int i = sh.item0; i <= last; i += 32) {
             const int item = i + lane, lo = item == sh.item0 ? sh.tile0 : 0;
             int w = 0;
+            PairRange r = {};
             if (item <= last && !(item == sh.item1 && sh.tile1 == 0)) {
                 const int u = item / pl.n_pairs;
-                const PairRange x = pair_range(a, pl, u, item - u * pl.n_pairs);
-                w = x.count > 0 ? max((item == sh.item1 ? sh.tile1 : x.tiles) - lo, 0) + 1 : 0;
+                r = pair_range(a, pl, u, item - u * pl.n_pairs);
+                w = r.count > 0 ? max((item == sh.item1 ? sh.tile1 : r.tiles) - lo, 0) + 1 : 0;
             }
             int x = w;
 #pragma unroll
@@ -136,7 +141,7 @@ __device__ __forceinline__ WarpShare warp_share(const ChunkArgs& a, const ChunkP
                     const uint32_t hit = __ballot_sync(0xffffffffu, cut >= p && cut < p + w);
                     if (!hit) continue;
                     const int from = __ffs(hit) - 1, tile = __shfl_sync(0xffffffffu, lo + max(cut - p - 1, 0), from);
-                    if (k == 0) { got.begin = i + from; got.begin_tile = tile; }
+                    if (k == 0) { got.begin = i + from; got.begin_tile = tile; if (lane == from) *first = r; }
                     else { got.end = i + from; got.end_tile = tile; }
                 }
             }
@@ -153,11 +158,14 @@ __device__ __forceinline__ WarpShare warp_share(const ChunkArgs& a, const ChunkP
 struct Notes { int front, front_ends, back, unused; };
 // What a warp has of one item: its tiles [lo, hi).
 struct Segment { int item, b, h, lo, hi; PairRange x; };
-static_assert(sizeof(Segment) <= 64, "three of them in 192 bytes");
+// What is seldom needed stays out of the registers: what is loaded, what is computed, what the front piece belongs to, and the
+// range of the warp's first item.
+struct Desk { Segment loaded, computed, front; PairRange first; };
+static_assert(sizeof(Desk) <= kDeskBytes, "a warp's place in shared memory");
 // A query row's last visible key, document, position and slope.
 struct RowNote { int lim, doc; float pos, slope2; };
 
-template <int NH, int RH, bool kMods>                   // kMods: a cap, a bias or documents
+template <int NH, int RH, int kMods>
 __global__ void __launch_bounds__(Q4Shape<NH, RH>::kThreads, 1)
 chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, const Q4Args cache,
                     float* const partial, float2* const partial_ml) {
@@ -174,10 +182,13 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.group;
     const ModArgs& md = a.mods;
     const Share share = find_share<Shape::kThreads>(a, pl, reinterpret_cast<int*>(base_ptr + Shape::kScratch), reinterpret_cast<int*>(base_ptr + Shape::kChains));      // (synchronises)
-    const WarpShare mine = warp_share(a, pl, share, warp, NW, lane);
+    Desk& desk = *reinterpret_cast<Desk*>(base_ptr + Shape::kDesk + kDeskBytes * warp);
+    const WarpShare mine = warp_share(a, pl, share, warp, NW, lane, &desk.first);
+    __syncwarp();
 
     const int gr = lane >> 2, qd = lane & 3;             // fragment row (a key, then dimensions) and column pair (query rows)
-    const bool capped = kMods && md.softcap > 0.f, by_doc = kMods && md.documents, biased = kMods && md.slopes;
+    const bool capped = kMods == kCap || (kMods == kAny && md.softcap > 0.f), by_doc = kMods == kAny && md.documents;
+    const bool biased = kMods == kBias || (kMods == kAny && md.slopes);
     // capped: x = c tanh(o / c) = c - 2 c / (1 + e^{2 o / c}), all in the base-2 domain
     const float cap2 = md.softcap * kLog2e, cap_in = capped ? 2.f / md.softcap : 0.f;
     uint8_t* const my_ring = base_ptr + warp * NST * Shape::kSlotBytes;
@@ -190,7 +201,8 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
             s.lo = s.item == mine.begin ? mine.begin_tile : block_lo;
             if (s.item == mine.end && mine.end_tile == block_lo) return false;
             if (s.item == share.item1 && share.tile1 == 0) return false;
-            s.x = pair_range(a, pl, u, s.item - u * pl.n_pairs);
+            if (s.item == mine.begin) s.x = desk.first;
+            else s.x = pair_range(a, pl, u, s.item - u * pl.n_pairs);
             s.hi = s.item == mine.end ? mine.end_tile : s.item == share.item1 ? share.tile1 : s.x.tiles;
             if (s.x.count > 0) { s.b = u / a.n_kv_heads; s.h = u - s.b * a.n_kv_heads; return true; }
         }
@@ -202,14 +214,13 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     constexpr int kCopies = Shape::kCodeBytes / 512;
     const uint32_t v_to = NH == 2 ? (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 3)) << 4) : (lane >> 1) * 32 + (((lane & 1) ^ ((lane >> 3) & 1)) << 4);
     bool f_open = false, f_more = true;
-    Segment* const desk = reinterpret_cast<Segment*>(base_ptr + Shape::kDesk + 192 * warp);    // (what is seldom needed stays out of the registers)
     int f_item = mine.begin - 1, f_end = 0, f_tile = 0, f_left = 0, f_next = 0, f_index = 0, f_lo = 0, f_hi = 0;     // f_left: tiles of the current page
     bool f_there = false;                                // the current page lies in the pool
     const uint8_t* f_k = nullptr, * f_v = nullptr, * f_s = nullptr;              // what this lane copies of the next tile
     int tile_of[NST], item_of[NST];                      // what is in the slots, the next one first; item -1: no more
-    auto page_at = [&](int index) { return index < a.max_pages ? a.page_table[int64_t(desk[0].b) * a.max_pages + index] : -1; };
+    auto page_at = [&](int index) { return index < a.max_pages ? a.page_table[int64_t(desk.loaded.b) * a.max_pages + index] : -1; };
     auto turn_page = [&](int page, int row) {
-        const int h = desk[0].h;
+        const int h = desk.loaded.h;
         f_there = uint32_t(page) < uint32_t(a.n_pages);
         if (!f_there) page = 0;                          // (nothing is read through it)
         f_k = cache.k + page * cache.k_sb + h * cache.k_sh + int64_t(row) * (D / 2) + lane * 16;
@@ -228,23 +239,23 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                 f_more = segment(f_item + 1, f);
                 if (!f_more) break;
                 __syncwarp();
-                if (lane == 0) desk[0] = f;
+                if (lane == 0) desk.loaded = f;
                 __syncwarp();
                 f_item = f.item;
                 f_end = f.hi;
                 f_tile = f.lo;
                 f_index = f_tile / tiles_per_page;
                 f_left = (f_index + 1) * tiles_per_page - f_tile;
-                if (f_tile < f_end) {
-                    const int page = page_at(f_index);
-                    f_next = page_at(f_index + 1);
-                    turn_page(page, (tiles_per_page - f_left) * kQ4Tile);
-                }
-                {                                        // the item's queries will be asked for soon
+                {                                        // the item's queries, positions and slopes will be asked for soon
                     constexpr int kLines = D / 64;       // of 128 bytes
                     const int m = lane / kLines, tok = m / G;
                     if (tok < f.x.count && m < Shape::R)
                         asm volatile("prefetch.global.L2 [%0];" ::"l"(qy.q + int64_t(f.b) * qy.sb + int64_t(f.h * G + m - tok * G) * qy.sh + int64_t(f.x.tok0 + tok) * qy.st + lane % kLines * 64));
+                }
+                if (f_tile < f_end) {
+                    const int page = page_at(f_index);
+                    f_next = page_at(f_index + 1);
+                    turn_page(page, (tiles_per_page - f_left) * kQ4Tile);
                 }
                 if (by_doc) {                            // of the tokens: sixteen rows at most
                     const int r = f.x.row0 + lane;
@@ -268,7 +279,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
             const uint32_t to = ring + j * Shape::kSlotBytes;
             if (by_doc || biased) {
                 const int t = tile * kQ4Tile + lane;
-                const Segment& f = desk[0];
+                const Segment& f = desk.loaded;
                 const bool in = t < f.x.rows;
                 if (by_doc) {                            // a tile without any of the tokens' documents is skipped
                     const int32_t* const at = md.documents + int64_t(f.b) * md.doc_sb + int64_t(f.h) * md.doc_sh + (in ? t : 0);
@@ -322,10 +333,10 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                     b_run[n].x += __shfl_xor_sync(0xffffffffu, b_run[n].x, d);
                     b_run[n].y += __shfl_xor_sync(0xffffffffu, b_run[n].y, d);
                 }
-            const Segment seg = desk[1];
+            const Segment seg = desk.computed;
             const int count = seg.x.count;
             const bool begins = seg.lo == 0, ends = seg.hi >= seg.x.tiles;
-            if (!begins) { note_front = seg.item; note_ends = ends; if (lane == 0) desk[2] = seg; }
+            if (!begins) { note_front = seg.item; note_ends = ends; if (lane == 0) desk.front = seg; }
             else if (!ends) note_back = seg.item;
             // (a back piece is the last thing that its warp has: nothing is on its way into the ring any more)
             float* const piece = reinterpret_cast<float*>(begins ? my_ring : base_ptr + Shape::kFront + warp * Shape::kPieceBytes);
@@ -359,10 +370,11 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         }
         if (!open) {
         Segment seg;
-        if (!segment(item + 1, seg)) break;
+        if (f_item == item + 1) seg = desk.loaded;
+        else if (!segment(item + 1, seg)) break;
         open = true;
         __syncwarp();
-        if (lane == 0) desk[1] = seg;
+        if (lane == 0) desk.computed = seg;
         item = seg.item;
         rows = seg.x.rows;
         const int count = seg.x.count;
@@ -652,7 +664,8 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         const int end = mine_e ? c + __ffs(mine_e) : NW + 1;
         const bool done = end <= next;
         if (done) next = end;
-        const Segment* const d = reinterpret_cast<const Segment*>(base_ptr + Shape::kDesk + 192 * from) + (c == 0 ? 2 : 1);
+        const Desk* const whose = reinterpret_cast<const Desk*>(base_ptr + Shape::kDesk + kDeskBytes * from);
+        const Segment* const d = c == 0 ? &whose->front : &whose->computed;
         if (!(c > 0 && done)) cut[c > 0] = d->item;
         struct Pieces {
             const uint8_t* front; const uint8_t* first; int col;
@@ -746,7 +759,7 @@ ChunkPlan chunk_q4_plan(const csp_params& p, int max_new, bool* few) {
     return pl;
 }
 
-template <int NH, int RH, bool kMods>
+template <int NH, int RH, int kMods>
 csp_status launch_few_mods(const ChunkArgs& a, const ChunkPlan& pl, const FewQuery& q, const Q4Args& c, float* partial, float2* ml,
                       cudaStream_t s) {
     constexpr int smem = int(Q4Shape<NH, RH>::kTotal) + 128;
@@ -761,8 +774,10 @@ csp_status launch_few_mods(const ChunkArgs& a, const ChunkPlan& pl, const FewQue
 template <int NH, int RH>
 csp_status launch_few(const ChunkArgs& a, const ChunkPlan& pl, const FewQuery& q, const Q4Args& c, float* partial, float2* ml,
                       cudaStream_t s) {
-    return a.mods.softcap > 0.f || a.mods.slopes || a.mods.documents ? launch_few_mods<NH, RH, true>(a, pl, q, c, partial, ml, s)
-                                                                     : launch_few_mods<NH, RH, false>(a, pl, q, c, partial, ml, s);
+    const bool cap = a.mods.softcap > 0.f, bias = a.mods.slopes;
+    if (a.mods.documents || (cap && bias)) return launch_few_mods<NH, RH, kAny>(a, pl, q, c, partial, ml, s);
+    return cap ? launch_few_mods<NH, RH, kCap>(a, pl, q, c, partial, ml, s) : bias ? launch_few_mods<NH, RH, kBias>(a, pl, q, c, partial, ml, s)
+                                                                                   : launch_few_mods<NH, RH, kNone>(a, pl, q, c, partial, ml, s);
 }
 
 }  // namespace
