@@ -104,26 +104,32 @@ __device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
 }
 // the smallest and the largest of a bf16 row's values, of which every lane has sixteen (two at a time: they are bf16 values)
 template <int kLanes>
-__device__ __forceinline__ void row_range(const Eight<false>& r0, const Eight<false>& r1, float& lo, float& hi) {
+__device__ __forceinline__ void row_range(const Eight<false>& r0, const Eight<false>& r1, uint32_t lanes, float& lo, float& hi) {
     const uint32_t w[8] = {r0.x[0].x, r0.x[0].y, r0.x[0].z, r0.x[0].w, r1.x[0].x, r1.x[0].y, r1.x[0].z, r1.x[0].w};
     uint32_t l = w[0], h = w[0];
 #pragma unroll
     for (int j = 1; j < 8; ++j) { l = min2_nan(l, w[j]); h = max2_nan(h, w[j]); }
 #pragma unroll
     for (int d = 1; d < kLanes; d <<= 1) {
-        l = min2_nan(l, __shfl_xor_sync(0xffffffffu, l, d));
-        h = max2_nan(h, __shfl_xor_sync(0xffffffffu, h, d));
+        l = min2_nan(l, __shfl_xor_sync(lanes, l, d));
+        h = max2_nan(h, __shfl_xor_sync(lanes, h, d));
     }
     lo = min_nan(bf16_lo(l), bf16_hi(l));
     hi = max_nan(bf16_lo(h), bf16_hi(h));
 }
 __device__ __forceinline__ uint32_t eight_codes(const float* f, float lo, float inv) {
-    // Adding 1.5 x 2^23 rounds to a whole number, which is then what the number's bits are more than 0x4b400000; of the eight of
-    // these, shifted to their places, what does not leave the word is 0x4b400000 x 0x11111111.
-    uint32_t w = 0;
+    // Adding 1.5 x 2^23 rounds to a whole number, which is then what the number's bits are more than 0x4b400000.  The code before
+    // goes along as sixteen times itself, so that four of them end up in the lowest sixteen bits: values 0 - 3 in one float, 4 - 7 in
+    // another.
+    constexpr float kWhole = 12582912.f;
+    const float2 neg = make_float2(-lo, -lo), inv2 = make_float2(inv, inv);
+    float2 r = make_float2(kWhole, kWhole);
 #pragma unroll
-    for (int j = 7; j >= 0; --j) w = w * 16u + __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(f[j], lo), inv), 12582912.f));
-    return w - 0x4b400000u * 0x11111111u;
+    for (int j = 3; j >= 0; --j) {
+        if (j < 3) r = __ffma2_rn(r, make_float2(16.f, 16.f), make_float2(-15.f * kWhole, -15.f * kWhole));
+        r = __ffma2_rn(__fadd2_rn(make_float2(f[j], f[j + 4]), neg), inv2, r);
+    }
+    return __byte_perm(__float_as_uint(r.x), __float_as_uint(r.y), 0x5410);
 }
 // t / n and what is left, with m = 2^32 / n + 1 rounded down (t < 2^31: the product is at most one too many)
 __device__ __forceinline__ uint32_t divide(uint32_t t, uint32_t n, uint32_t m, uint32_t& rest) {
@@ -136,129 +142,128 @@ __device__ __forceinline__ uint32_t divide(uint32_t t, uint32_t n, uint32_t m, u
 // Grid (token tiles of a sequence x sequences, pieces of the heads).  Bound by memory: every byte is read and written once.  A
 // step takes two rows of a token, K and V of a head or two heads of Q, so that what belongs to the token is computed once for
 // both and 64 bytes are on their way per lane.
-template <bool kF32, bool kFour, int kLanes>             // kLanes = d / 16
+template <bool kF32, bool kFour, bool kTurn, int kLanes> // kLanes = d / 16
 __global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(const AppendRowsArgs a) {
     const int tid = threadIdx.x, L = tid % kLanes, group = tid / kLanes;
+    const uint32_t lanes = ((1u << kLanes) - 1u) << (tid % 32 - L);                  // of the row
     const int b = blockIdx.x / a.token_tiles, tile = blockIdx.x - b * a.token_tiles;
     const int H = a.n_kv_heads, pairs = H + (a.n_q_heads + 1) / 2;
     const int log_tok = a.log_tokens, strides = (kThreads / kLanes) >> log_tok;      // groups per token
     const int local = group & ((1 << log_tok) - 1);
     const int pair0 = int(blockIdx.y) * a.pairs_per_block, pair1 = min(pair0 + a.pairs_per_block, pairs);
     const int pair_lanes = a.rope.dim / 16;              // lanes whose values are rotated
-    const bool turned = L < pair_lanes;
-    const bool halves = turned && !a.rope.interleaved;
+    const bool turned = kTurn && L < pair_lanes, halves = turned && !a.rope.interleaved;
+    const int r0 = halves ? L : 2 * L, r1 = halves ? L + pair_lanes : 2 * L + 1;     // eights of a rotated row that the lane has
     const bool lead = tile == 0 && blockIdx.y == 0;
     // (token tiles beyond the grid's: a tile per step)
     for (int t0 = tile << log_tok; t0 < a.max_new; t0 += a.token_tiles << log_tok) {
         const int i = t0 + local;
+        if (i >= a.max_new) break;
+        auto token = [&](const RowTensor& x) { return static_cast<char*>(x.ptr) + b * x.sb + i * x.st; };
         float cs[8], sn[8];
         int at = -1;                                     // row of the table that cs and sn come from
-        for (int s0 = pair0; s0 < pair1; s0 += strides) { // (the same for the whole block)
-            const int s = s0 + (group >> log_tok);
-            const bool is_q = s >= H, inside = s < pair1 && i < a.max_new;
-            int head[2], kv[2], start[2];                // of the two rows: heads, KV heads, rows in front of the new ones
-            bool here[2] = {false, false};
-            Eight<kF32> r[2][2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                head[k] = is_q ? 2 * (s - H) + k : s;
-                kv[k] = head[k];
-                start[k] = 0;
-                if (is_q && a.group > 1) { uint32_t rest; kv[k] = int(divide(uint32_t(head[k]), uint32_t(a.group), a.group_inverse, rest)); }
-                if (!inside || (is_q && head[k] >= a.n_q_heads)) continue;
-                const NewRows n = new_rows(a, b, kv[k], false);
-                start[k] = n.first;
-                here[k] = i < (is_q ? n.brought : n.stored);
-                if (!here[k]) continue;
-                const RowTensor& from = is_q ? a.q : k ? a.v_new : a.k_new;
-                const char* const row = static_cast<const char*>(from.ptr) + b * from.sb + head[k] * from.sh + i * from.st;
-                const bool apart = halves && (is_q || k == 0);
-                r[k][0] = load_eight<kF32>(row, apart ? L : 2 * L);
-                r[k][1] = load_eight<kF32>(row, apart ? L + pair_lanes : 2 * L + 1);
+        auto turn = [&](Eight<kF32>& x0, Eight<kF32>& x1, int row) {
+            if (!turned) return;
+            float f[16];
+            widen<kF32>(x0, f);
+            widen<kF32>(x1, f + 8);
+            int pos = a.rope.positions ? a.rope.positions[b * a.rope.pos_sb + i] : row;
+            if (pos < 0 || pos >= a.rope.table_rows) {
+                if (L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
+                pos = pos < 0 ? 0 : a.rope.table_rows - 1;
             }
-            uint32_t slot = 0;
-            int page = 0;
-            if (!is_q && here[0]) page = a.page_table[int64_t(b) * a.max_pages + divide(uint32_t(start[0] + i), uint32_t(a.page_rows), a.page_inverse, slot)];
-            const bool astray = page < 0 || page >= a.n_pages;
-            if (astray && L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
+            if (pos != at) {
+                at = pos;
+                const float* const row_cs = a.rope.cos_sin + pos * a.rope.row_stride + 8 * L;
+                const float* const row_sn = row_cs + a.rope.dim / 2;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const bool turn = here[k] && turned && (is_q || k == 0), apart = halves && (is_q || k == 0);
-                const int c0 = apart ? L : 2 * L, c1 = apart ? L + pair_lanes : 2 * L + 1;
-                float f[16];
-                if (turn || (kFour && here[k])) {
-                    widen<kF32>(r[k][0], f);
-                    widen<kF32>(r[k][1], f + 8);
+                for (int j = 0; j < 8; j += 4) {
+                    const float4 y = *reinterpret_cast<const float4*>(row_cs + j), z = *reinterpret_cast<const float4*>(row_sn + j);
+                    cs[j] = y.x; cs[j + 1] = y.y; cs[j + 2] = y.z; cs[j + 3] = y.w;
+                    sn[j] = z.x; sn[j + 1] = z.y; sn[j + 2] = z.z; sn[j + 3] = z.w;
                 }
-                if (turn) {
-                    int pos = a.rope.positions ? a.rope.positions[b * a.rope.pos_sb + i] : start[k] + i;
-                    if (pos < 0 || pos >= a.rope.table_rows) {
-                        if (L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
-                        pos = pos < 0 ? 0 : a.rope.table_rows - 1;
-                    }
-                    if (pos != at) {
-                        at = pos;
-                        const float* const row_cs = a.rope.cos_sin + pos * a.rope.row_stride + 8 * L;
-                        const float* const row_sn = row_cs + a.rope.dim / 2;
+            }
+            if (halves) {
 #pragma unroll
-                        for (int j = 0; j < 8; j += 4) {
-                            const float4 y = *reinterpret_cast<const float4*>(row_cs + j), z = *reinterpret_cast<const float4*>(row_sn + j);
-                            cs[j] = y.x; cs[j + 1] = y.y; cs[j + 2] = y.z; cs[j + 3] = y.w;
-                            sn[j] = z.x; sn[j + 1] = z.y; sn[j + 2] = z.z; sn[j + 3] = z.w;
-                        }
-                    }
-                    if (apart) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float x1 = f[j], x2 = f[j + 8];
-                            f[j] = __fsub_rn(__fmul_rn(x1, cs[j]), __fmul_rn(x2, sn[j]));
-                            f[j + 8] = __fadd_rn(__fmul_rn(x2, cs[j]), __fmul_rn(x1, sn[j]));
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float x1 = f[2 * j], x2 = f[2 * j + 1];
-                            f[2 * j] = __fsub_rn(__fmul_rn(x1, cs[j]), __fmul_rn(x2, sn[j]));
-                            f[2 * j + 1] = __fadd_rn(__fmul_rn(x2, cs[j]), __fmul_rn(x1, sn[j]));
-                        }
-                    }
-                    r[k][0] = narrow<kF32>(f);
-                    r[k][1] = narrow<kF32>(f + 8);
-                    if (kFour) { widen<kF32>(r[k][0], f); widen<kF32>(r[k][1], f + 8); }     // what a bf16 cache would hold
+                for (int j = 0; j < 8; ++j) {
+                    const float y1 = f[j], y2 = f[j + 8];
+                    f[j] = __fsub_rn(__fmul_rn(y1, cs[j]), __fmul_rn(y2, sn[j]));
+                    f[j + 8] = __fadd_rn(__fmul_rn(y2, cs[j]), __fmul_rn(y1, sn[j]));
                 }
-                float lo = 0.f, hi = 0.f;
-                // (every lane goes through the shuffles, with or without a row)
-                if constexpr (kFour) row_range<kLanes>(r[k][0], r[k][1], lo, hi);
-                if (!here[k]) continue;
-                if (is_q) {
-                    char* const row = static_cast<char*>(a.q_out.ptr) + b * a.q_out.sb + head[k] * a.q_out.sh + i * a.q_out.st;
-                    store_eight<kF32>(row, c0, r[k][0]);
-                    store_eight<kF32>(row, c1, r[k][1]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float y1 = f[2 * j], y2 = f[2 * j + 1];
+                    f[2 * j] = __fsub_rn(__fmul_rn(y1, cs[j]), __fmul_rn(y2, sn[j]));
+                    f[2 * j + 1] = __fadd_rn(__fmul_rn(y2, cs[j]), __fmul_rn(y1, sn[j]));
+                }
+            }
+            x0 = narrow<kF32>(f);
+            x1 = narrow<kF32>(f + 8);
+        };
+        for (int s = pair0 + (group >> log_tok); s < pair1; s += strides) {
+            Eight<kF32> x[2], y[2];
+            if (s < H) {                                 // K and V of a head
+                const NewRows n = new_rows(a, b, s, false);
+                if (i >= n.stored) continue;
+                const char* const k_row = token(a.k_new) + s * a.k_new.sh, * const v_row = token(a.v_new) + s * a.v_new.sh;
+                x[0] = load_eight<kF32>(k_row, r0);
+                x[1] = load_eight<kF32>(k_row, r1);
+                y[0] = load_eight<kF32>(v_row, 2 * L);
+                y[1] = load_eight<kF32>(v_row, 2 * L + 1);
+                uint32_t slot;
+                const int page = a.page_table[int64_t(b) * a.max_pages + divide(uint32_t(n.first + i), uint32_t(a.page_rows), a.page_inverse, slot)];
+                if (page < 0 || page >= a.n_pages) {
+                    if (L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
                     continue;
                 }
-                if (astray) continue;
-                const RowTensor& to = k ? a.v : a.k;
-                char* const row = static_cast<char*>(to.ptr) + page * to.sb + s * to.sh + slot * to.st;
-                if (!kFour) {
-                    store_eight<kF32>(row, c0, r[k][0]);
-                    store_eight<kF32>(row, c1, r[k][1]);
-                } else {
-                    uint32_t pair = pack_bf16(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), lo);
-                    float scale = bf16_lo(pair);
-                    if (scale < kSmallest) { scale = 0.f; pair &= 0xffff0000u; }
-                    if (!(scale < INFINITY)) pair |= 0x7fffu;    // the whole row is no number
-                    const float inv = scale > 0.f ? __fmul_rn(__frcp_rn(scale), 1.f + 0x1p-21f) : 0.f;
-                    const uint32_t w0 = eight_codes(f, lo, inv), w1 = eight_codes(f + 8, lo, inv);
-                    if (apart) {
-                        reinterpret_cast<uint32_t*>(row)[c0] = w0;
-                        reinterpret_cast<uint32_t*>(row)[c1] = w1;
+                turn(x[0], x[1], n.first + i);           // (rounded to bf16 as a cache of these would hold it, and then to 4 bits)
+                auto store = [&](const RowTensor& to, const RowTensor& sc, const Eight<kF32>* z, int c0, int c1) {
+                    char* const row = static_cast<char*>(to.ptr) + page * to.sb + s * to.sh + slot * to.st;
+                    if constexpr (!kFour) {
+                        store_eight<kF32>(row, c0, z[0]);
+                        store_eight<kF32>(row, c1, z[1]);
                     } else {
-                        reinterpret_cast<uint2*>(row)[L] = make_uint2(w0, w1);
+                        float lo, hi, f[16];
+                        row_range<kLanes>(z[0], z[1], lanes, lo, hi);
+                        uint32_t pair = pack_bf16(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), lo);
+                        float scale = bf16_lo(pair);
+                        if (scale < kSmallest) { scale = 0.f; pair &= 0xffff0000u; }
+                        if (!(scale < INFINITY)) pair |= 0x7fffu;    // the whole row is no number
+                        const float inv = scale > 0.f ? __fmul_rn(__frcp_rn(scale), 1.f + 0x1p-21f) : 0.f;
+                        widen<false>(z[0], f);
+                        widen<false>(z[1], f + 8);
+                        const uint32_t w0 = eight_codes(f, lo, inv), w1 = eight_codes(f + 8, lo, inv);
+                        if (c1 == c0 + 1 && !halves) {
+                            reinterpret_cast<uint2*>(row)[L] = make_uint2(w0, w1);
+                        } else {
+                            reinterpret_cast<uint32_t*>(row)[c0] = w0;
+                            reinterpret_cast<uint32_t*>(row)[c1] = w1;
+                        }
+                        if (L == 0) *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page * sc.sb + s * sc.sh + slot * 4) = pair;
                     }
-                    if (L == 0) {
-                        const RowTensor& sc = k ? a.v_scales : a.k_scales;
-                        *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page * sc.sb + s * sc.sh + slot * 4) = pair;
-                    }
+                };
+                store(a.k, a.k_scales, x, r0, r1);
+                store(a.v, a.v_scales, y, 2 * L, 2 * L + 1);
+            } else if constexpr (kTurn) {                // two heads of Q
+                const int h0 = 2 * (s - H), h1 = h0 + 1;
+                uint32_t rest;
+                auto kv_head = [&](int h) { return a.group > 1 ? int(divide(uint32_t(h), uint32_t(a.group), a.group_inverse, rest)) : h; };
+                const NewRows n0 = new_rows(a, b, kv_head(h0), false), n1 = h1 < a.n_q_heads ? new_rows(a, b, kv_head(h1), false) : NewRows{0, 0, 0};
+                const char* const from = token(a.q);
+                char* const to = token(a.q_out);
+                const bool do0 = i < n0.brought, do1 = i < n1.brought;
+                if (do0) { x[0] = load_eight<kF32>(from + h0 * a.q.sh, r0); x[1] = load_eight<kF32>(from + h0 * a.q.sh, r1); }
+                if (do1) { y[0] = load_eight<kF32>(from + h1 * a.q.sh, r0); y[1] = load_eight<kF32>(from + h1 * a.q.sh, r1); }
+                if (do0) {
+                    turn(x[0], x[1], n0.first + i);
+                    store_eight<kF32>(to + h0 * a.q_out.sh, r0, x[0]);
+                    store_eight<kF32>(to + h0 * a.q_out.sh, r1, x[1]);
+                }
+                if (do1) {
+                    turn(y[0], y[1], n1.first + i);
+                    store_eight<kF32>(to + h1 * a.q_out.sh, r0, y[0]);
+                    store_eight<kF32>(to + h1 * a.q_out.sh, r1, y[1]);
                 }
             }
         }
@@ -353,7 +358,8 @@ inline csp_status launched() { return cudaGetLastError() == cudaSuccess ? CSP_OK
 
 template <bool kF32, bool kFour, int kLanes>
 csp_status append_rows(const AppendRowsArgs& a, dim3 grid, cudaStream_t s) {
-    append_rows_kernel<kF32, kFour, kLanes><<<grid, kThreads, 0, s>>>(a);
+    if (a.rope.dim) append_rows_kernel<kF32, kFour, true, kLanes><<<grid, kThreads, 0, s>>>(a);
+    else if constexpr (kFour) append_rows_kernel<kF32, kFour, false, kLanes><<<grid, kThreads, 0, s>>>(a);   // (only these may come without)
     return launched();
 }
 
