@@ -153,7 +153,11 @@ __global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(con
     const int pair0 = int(blockIdx.y) * a.pairs_per_block, pair1 = min(pair0 + a.pairs_per_block, pairs);
     const int pair_lanes = a.rope.dim / 16;              // lanes whose values are rotated
     const bool turned = kTurn && L < pair_lanes, halves = turned && !a.rope.interleaved;
-    const int r0 = halves ? L : 2 * L, r1 = halves ? L + pair_lanes : 2 * L + 1;     // eights of a rotated row that the lane has
+    // Eights of a row that the lane has: neighbouring lanes' side by side, so that 32-byte sectors are whole in every access (with
+    // 2 L and 2 L + 1 reading back takes 80 us instead of 72) ...
+    const int c0 = L, c1 = L + kLanes;
+    // ... but of a row that is rotated those with whole pairs, of which the first pair_lanes lanes have all
+    const int r0 = !kTurn || halves ? L : 2 * L, r1 = !kTurn ? L + kLanes : halves ? L + pair_lanes : 2 * L + 1;
     const bool lead = tile == 0 && blockIdx.y == 0;
     // (token tiles beyond the grid's: a tile per step)
     for (int t0 = tile << log_tok; t0 < a.max_new; t0 += a.token_tiles << log_tok) {
@@ -209,8 +213,8 @@ __global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(con
                 const char* const k_row = token(a.k_new) + s * a.k_new.sh, * const v_row = token(a.v_new) + s * a.v_new.sh;
                 x[0] = load_eight<kF32>(k_row, r0);
                 x[1] = load_eight<kF32>(k_row, r1);
-                y[0] = load_eight<kF32>(v_row, 2 * L);
-                y[1] = load_eight<kF32>(v_row, 2 * L + 1);
+                y[0] = load_eight<kF32>(v_row, c0);
+                y[1] = load_eight<kF32>(v_row, c1);
                 uint32_t slot;
                 const int page = a.page_table[int64_t(b) * a.max_pages + divide(uint32_t(n.first + i), uint32_t(a.page_rows), a.page_inverse, slot)];
                 if (page < 0 || page >= a.n_pages) {
@@ -218,11 +222,11 @@ __global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(con
                     continue;
                 }
                 turn(x[0], x[1], n.first + i);           // (rounded to bf16 as a cache of these would hold it, and then to 4 bits)
-                auto store = [&](const RowTensor& to, const RowTensor& sc, const Eight<kF32>* z, int c0, int c1) {
+                auto store = [&](const RowTensor& to, const RowTensor& sc, const Eight<kF32>* z, int z0, int z1) {
                     char* const row = static_cast<char*>(to.ptr) + page * to.sb + s * to.sh + slot * to.st;
                     if constexpr (!kFour) {
-                        store_eight<kF32>(row, c0, z[0]);
-                        store_eight<kF32>(row, c1, z[1]);
+                        store_eight<kF32>(row, z0, z[0]);
+                        store_eight<kF32>(row, z1, z[1]);
                     } else {
                         float lo, hi, f[16];
                         row_range<kLanes>(z[0], z[1], lanes, lo, hi);
@@ -234,17 +238,13 @@ __global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(con
                         widen<false>(z[0], f);
                         widen<false>(z[1], f + 8);
                         const uint32_t w0 = eight_codes(f, lo, inv), w1 = eight_codes(f + 8, lo, inv);
-                        if (c1 == c0 + 1 && !halves) {
-                            reinterpret_cast<uint2*>(row)[L] = make_uint2(w0, w1);
-                        } else {
-                            reinterpret_cast<uint32_t*>(row)[c0] = w0;
-                            reinterpret_cast<uint32_t*>(row)[c1] = w1;
-                        }
+                        reinterpret_cast<uint32_t*>(row)[z0] = w0;
+                        reinterpret_cast<uint32_t*>(row)[z1] = w1;
                         if (L == 0) *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page * sc.sb + s * sc.sh + slot * 4) = pair;
                     }
                 };
                 store(a.k, a.k_scales, x, r0, r1);
-                store(a.v, a.v_scales, y, 2 * L, 2 * L + 1);
+                store(a.v, a.v_scales, y, c0, c1);
             } else if constexpr (kTurn) {                // two heads of Q
                 const int h0 = 2 * (s - H), h1 = h0 + 1;
                 uint32_t rest;
@@ -325,13 +325,14 @@ __global__ void __launch_bounds__(kThreads) load_rows_kernel(const LoadRowsArgs 
                 w[j] = make_uint2(0u, 0u);
                 pair[j] = 0u;
                 if (i >= count) continue;
-                const uint32_t t = uint32_t(first + i), slot = t % uint32_t(a.page_rows);
-                const int page = table[t / uint32_t(a.page_rows)];
+                uint32_t slot;
+                const int page = table[divide(uint32_t(first + i), uint32_t(a.page_rows), a.page_inverse, slot)];
                 if (page < 0 || page >= a.n_pages) {     // reads as zeros
                     if (which == 0 && L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
                     continue;
                 }
-                w[j] = __ldcs(reinterpret_cast<const uint2*>(codes + page * from.sb + slot * from.st) + L);
+                const uint32_t* const row = reinterpret_cast<const uint32_t*>(codes + page * from.sb + slot * from.st);
+                w[j] = make_uint2(__ldcs(row + L), __ldcs(row + L + kLanes));
                 pair[j] = *reinterpret_cast<const uint32_t*>(scales + page * sc.sb + slot * 4);
             }
 #pragma unroll
@@ -339,16 +340,27 @@ __global__ void __launch_bounds__(kThreads) load_rows_kernel(const LoadRowsArgs 
                 const int i = i0 + j * kGroups + group;
                 if (i >= count) continue;
                 const float scale = bf16_lo(pair[j]), base = bf16_hi(pair[j]);
+                // A code in bits 4 k to 4 k + 3 of a float that is 2^23 otherwise is the number code 2^4k more: it stays where it is,
+                // and the scale is divided instead (exactly: of its eight bits none is lost, as 2^-126 2^-12 is still 2^11 times the
+                // smallest number).
                 float f[16];
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const uint32_t c = ((k < 8 ? w[j].x : w[j].y) >> (4 * (k & 7))) & 15u;
-                    f[k] = fmaf(scale, __uint_as_float(0x4b000000u | c) - 8388608.f, base);      // (2^23 + c) - 2^23
+                for (int k = 0; k < 4; ++k) {
+                    const float part = scale * (k == 0 ? 1.f : k == 1 ? 0x1p-4f : k == 2 ? 0x1p-8f : 0x1p-12f);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t x = e ? w[j].y : w[j].x, m = 15u << (4 * k);
+                        const float2 c = __fadd2_rn(make_float2(__uint_as_float((x & m) | 0x4b000000u), __uint_as_float(((x >> 16) & m) | 0x4b000000u)),
+                                                    make_float2(-8388608.f, -8388608.f));
+                        const float2 y = __ffma2_rn(c, make_float2(part, part), make_float2(base, base));
+                        f[8 * e + k] = y.x;
+                        f[8 * e + k + 4] = y.y;
+                    }
                 }
                 char* const row = out + i * to.st;
                 const Eight<kF32> r0 = narrow<kF32>(f), r1 = narrow<kF32>(f + 8);
-                store_eight<kF32>(row, 2 * L, r0);
-                store_eight<kF32>(row, 2 * L + 1, r1);
+                store_eight<kF32>(row, L, r0);
+                store_eight<kF32>(row, L + kLanes, r1);
             }
         }
     }
@@ -391,12 +403,13 @@ csp_status launch_append_rows(AppendRowsArgs a, int head_dim, bool f32, bool fou
     return head_dim == 64 ? append_rows<false, false, 4>(a, grid, s) : head_dim == 128 ? append_rows<false, false, 8>(a, grid, s) : append_rows<false, false, 16>(a, grid, s);
 }
 
-csp_status launch_load_rows(const LoadRowsArgs& a, int head_dim, bool f32, cudaStream_t s) {
+csp_status launch_load_rows(LoadRowsArgs a, int head_dim, bool f32, cudaStream_t s) {
     if (a.units == 0 || a.max_rows == 0) return CSP_OK;
     const int rows = kThreads / (head_dim / 16) * kLoadDepth;
     const int64_t tiles = (int64_t(a.max_rows < a.capacity ? a.max_rows : a.capacity) + rows - 1) / rows;
     if (tiles == 0) return CSP_OK;
     const dim3 grid{unsigned(a.units), unsigned(tiles < 65535 ? tiles : 65535)};
+    a.page_inverse = uint32_t((uint64_t(1) << 32) / uint32_t(a.page_rows)) + 1u;
     if (head_dim == 64) f32 ? load_rows_kernel<true, 4><<<grid, kThreads, 0, s>>>(a) : load_rows_kernel<false, 4><<<grid, kThreads, 0, s>>>(a);
     else f32 ? load_rows_kernel<true, 8><<<grid, kThreads, 0, s>>>(a) : load_rows_kernel<false, 8><<<grid, kThreads, 0, s>>>(a);
     return launched();

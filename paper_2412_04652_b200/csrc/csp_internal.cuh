@@ -271,9 +271,10 @@ struct LoadRowsArgs {
     int32_t units, n_kv_heads, max_rows, capacity;
     const int32_t* page_table; int32_t max_pages, page_rows, n_pages;
     int32_t* status;
+    uint32_t page_inverse;                               // 2^32 / page_rows, filled in by the launcher
 };
 csp_status launch_append_rows(AppendRowsArgs a, int head_dim, bool f32, bool four, cudaStream_t s);
-csp_status launch_load_rows(const LoadRowsArgs& a, int head_dim, bool f32, cudaStream_t s);
+csp_status launch_load_rows(LoadRowsArgs a, int head_dim, bool f32, cudaStream_t s);
 
 // a cache in 4 bits as the attention kernels take it: rows of a head in a page lie one behind the other (strides in bytes)
 struct Q4Args {
