@@ -139,10 +139,54 @@ __device__ __forceinline__ uint32_t divide(uint32_t t, uint32_t n, uint32_t m, u
     return q;
 }
 
+// A row of bf16 values in 4 bits: the lane's two words, and what the row's first lane writes beside them.
+template <int kLanes>
+__device__ __forceinline__ uint32_t quantise(const Eight<false>* z, uint32_t lanes, uint32_t& w0, uint32_t& w1) {
+    float lo, hi, f[16];
+    row_range<kLanes>(z[0], z[1], lanes, lo, hi);
+    uint32_t pair = pack_bf16(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), lo);
+    float scale = bf16_lo(pair);
+    if (scale < kSmallest) { scale = 0.f; pair &= 0xffff0000u; }
+    if (!(scale < INFINITY)) pair |= 0x7fffu;            // the whole row is no number
+    const float inv = scale > 0.f ? __fmul_rn(__frcp_rn(scale), 1.f + 0x1p-21f) : 0.f;
+    widen<false>(z[0], f);
+    widen<false>(z[1], f + 8);
+    w0 = eight_codes(f, lo, inv);
+    w1 = eight_codes(f + 8, lo, inv);
+    return pair;
+}
+
+// The counts.  Where they are updated in place, only the last block to finish does it: all others have read them.  `mine`: this block
+// writes heads [h0, h1) of sequence b where they go elsewhere.
+__device__ __forceinline__ void count_rows(const AppendRowsArgs& a, bool mine, int b, int h0, int h1) {
+    const int tid = threadIdx.x, H = a.n_kv_heads;
+    if (a.n_rows_out != a.n_rows) {
+        if (!mine) return;
+        for (int h = h0 + tid; h < h1; h += kThreads) {
+            const NewRows x = new_rows(a, b, h, true);
+            a.n_rows_out[b * H + h] = x.first + x.stored;
+        }
+        return;
+    }
+    __shared__ int last;
+    __syncthreads();
+    if (tid == 0) {
+        __threadfence();
+        last = atomicAdd(a.status + kCountWord, 1) == int(gridDim.x * gridDim.y) - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    for (int u = tid; u < a.batch * H; u += kThreads) {
+        const NewRows x = new_rows(a, u / H, u % H, true);
+        a.n_rows_out[u] = x.first + x.stored;
+    }
+    if (tid == 0) a.status[kCountWord] = 0;
+}
+
 // Grid (token tiles of a sequence x sequences, pieces of the heads).  Bound by memory: every byte is read and written once.  A
 // step takes two rows of a token, K and V of a head or two heads of Q, so that what belongs to the token is computed once for
 // both and 64 bytes are on their way per lane.
-template <bool kF32, bool kFour, bool kTurn, int kLanes> // kLanes = d / 16
+template <bool kF32, bool kFour, int kLanes>             // kLanes = d / 16
 __global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(const AppendRowsArgs a) {
     const int tid = threadIdx.x, L = tid % kLanes, group = tid / kLanes;
     const uint32_t lanes = ((1u << kLanes) - 1u) << (tid % 32 - L);                  // of the row
@@ -152,17 +196,16 @@ __global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(con
     const int local = group & ((1 << log_tok) - 1);
     const int pair0 = int(blockIdx.y) * a.pairs_per_block, pair1 = min(pair0 + a.pairs_per_block, pairs);
     const int pair_lanes = a.rope.dim / 16;              // lanes whose values are rotated
-    const bool turned = kTurn && L < pair_lanes, halves = turned && !a.rope.interleaved;
+    const bool turned = L < pair_lanes, halves = turned && !a.rope.interleaved;
     // Eights of a row that the lane has: neighbouring lanes' side by side, so that 32-byte sectors are whole in every access (with
     // 2 L and 2 L + 1 reading back takes 80 us instead of 72) ...
     const int c0 = L, c1 = L + kLanes;
     // ... but of a row that is rotated those with whole pairs, of which the first pair_lanes lanes have all
-    const int r0 = !kTurn || halves ? L : 2 * L, r1 = !kTurn ? L + kLanes : halves ? L + pair_lanes : 2 * L + 1;
+    const int r0 = halves ? L : 2 * L, r1 = halves ? L + pair_lanes : 2 * L + 1;
     const bool lead = tile == 0 && blockIdx.y == 0;
     // (token tiles beyond the grid's: a tile per step)
-    for (int t0 = tile << log_tok; t0 < a.max_new; t0 += a.token_tiles << log_tok) {
-        const int i = t0 + local;
-        if (i >= a.max_new) break;
+    for (int64_t t0 = int64_t(tile) << log_tok; t0 + local < a.max_new; t0 += int64_t(a.token_tiles) << log_tok) {
+        const int i = int(t0) + local;
         auto token = [&](const RowTensor& x) { return static_cast<char*>(x.ptr) + b * x.sb + i * x.st; };
         float cs[8], sn[8];
         int at = -1;                                     // row of the table that cs and sn come from
@@ -228,16 +271,8 @@ __global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(con
                         store_eight<kF32>(row, z0, z[0]);
                         store_eight<kF32>(row, z1, z[1]);
                     } else {
-                        float lo, hi, f[16];
-                        row_range<kLanes>(z[0], z[1], lanes, lo, hi);
-                        uint32_t pair = pack_bf16(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), lo);
-                        float scale = bf16_lo(pair);
-                        if (scale < kSmallest) { scale = 0.f; pair &= 0xffff0000u; }
-                        if (!(scale < INFINITY)) pair |= 0x7fffu;    // the whole row is no number
-                        const float inv = scale > 0.f ? __fmul_rn(__frcp_rn(scale), 1.f + 0x1p-21f) : 0.f;
-                        widen<false>(z[0], f);
-                        widen<false>(z[1], f + 8);
-                        const uint32_t w0 = eight_codes(f, lo, inv), w1 = eight_codes(f + 8, lo, inv);
+                        uint32_t w0, w1;
+                        const uint32_t pair = quantise<kLanes>(z, lanes, w0, w1);
                         reinterpret_cast<uint32_t*>(row)[z0] = w0;
                         reinterpret_cast<uint32_t*>(row)[z1] = w1;
                         if (L == 0) *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page * sc.sb + s * sc.sh + slot * 4) = pair;
@@ -245,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(con
                 };
                 store(a.k, a.k_scales, x, r0, r1);
                 store(a.v, a.v_scales, y, c0, c1);
-            } else if constexpr (kTurn) {                // two heads of Q
+            } else {                                     // two heads of Q
                 const int h0 = 2 * (s - H), h1 = h0 + 1;
                 uint32_t rest;
                 auto kv_head = [&](int h) { return a.group > 1 ? int(divide(uint32_t(h), uint32_t(a.group), a.group_inverse, rest)) : h; };
@@ -268,35 +303,65 @@ __global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(con
             }
         }
     }
-    // The counts.  Where they are updated in place, only the last block to finish does it: all others have read them.
-    if (a.n_rows_out != a.n_rows) {
-        if (!lead) return;
-        for (int h = tid; h < H; h += kThreads) {
-            const NewRows x = new_rows(a, b, h, true);
-            a.n_rows_out[b * H + h] = x.first + x.stored;
+    count_rows(a, lead, b, 0, H);
+}
+
+// Rows that are not rotated, to pages in 4 bits.  Block (u, .) takes kGroups x kAppendDepth rows of a unit's K and V at a time, so that
+// what belongs to the unit is computed once; behind the unit's last row there is nothing to do.  (In the kernel above, whose blocks
+// go over the heads: 42 us for 262 K rows, of which a head has between a quarter and all, against 37.)
+constexpr int kAppendDepth = 2;
+template <int kLanes>
+__global__ void __launch_bounds__(kThreads, 4) append_units_kernel(const AppendRowsArgs a) {
+    constexpr int kGroups = kThreads / kLanes;           // rows per step
+    const int u = blockIdx.x, b = u / a.n_kv_heads, h = u - b * a.n_kv_heads;
+    const int L = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+    const uint32_t lanes = ((1u << kLanes) - 1u) << (threadIdx.x % 32 - L);          // of the row
+    const NewRows n = new_rows(a, b, h, false);
+    const int32_t* const table = a.page_table + int64_t(b) * a.max_pages;
+    const char* const from[2] = {static_cast<const char*>(a.k_new.ptr) + b * a.k_new.sb + h * a.k_new.sh,
+                                 static_cast<const char*>(a.v_new.ptr) + b * a.v_new.sb + h * a.v_new.sh};
+    for (int64_t i0 = blockIdx.y * kGroups * kAppendDepth; i0 < n.stored; i0 += int64_t(gridDim.y) * kGroups * kAppendDepth) {
+        Eight<false> x[kAppendDepth][2][2];
+        int page[kAppendDepth];
+        uint32_t slot[kAppendDepth];
+#pragma unroll
+        for (int j = 0; j < kAppendDepth; ++j) {
+            const int i = int(i0) + j * kGroups + group;
+            if (i0 + j * kGroups + group >= n.stored) continue;
+            page[j] = table[divide(uint32_t(n.first + i), uint32_t(a.page_rows), a.page_inverse, slot[j])];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const char* const row = from[k] + i * (k ? a.v_new.st : a.k_new.st);
+                x[j][k][0] = load_eight<false>(row, L);
+                x[j][k][1] = load_eight<false>(row, L + kLanes);
+            }
         }
-        return;
+#pragma unroll
+        for (int j = 0; j < kAppendDepth; ++j) {
+            if (i0 + j * kGroups + group >= n.stored) continue;
+            if (page[j] < 0 || page[j] >= a.n_pages) {
+                if (L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
+                continue;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const RowTensor& to = k ? a.v : a.k, & sc = k ? a.v_scales : a.k_scales;
+                uint32_t w0, w1;
+                const uint32_t pair = quantise<kLanes>(x[j][k], lanes, w0, w1);
+                uint32_t* const row = reinterpret_cast<uint32_t*>(static_cast<char*>(to.ptr) + page[j] * to.sb + h * to.sh + slot[j] * to.st);
+                row[L] = w0;
+                row[L + kLanes] = w1;
+                if (L == 0) *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page[j] * sc.sb + h * sc.sh + slot[j] * 4) = pair;
+            }
+        }
     }
-    __shared__ int last;
-    __syncthreads();
-    if (tid == 0) {
-        __threadfence();
-        last = atomicAdd(a.status + kCountWord, 1) == int(gridDim.x * gridDim.y) - 1;
-    }
-    __syncthreads();
-    if (!last) return;
-    for (int u = tid; u < a.batch * H; u += kThreads) {
-        const NewRows x = new_rows(a, u / H, u % H, true);
-        a.n_rows_out[u] = x.first + x.stored;
-    }
-    if (tid == 0) a.status[kCountWord] = 0;
+    count_rows(a, blockIdx.y == 0, b, h, h + 1);
 }
 
 // Rows [first, n_rows) of every unit as numbers again: base + scale code, rounded once to fp32 and, for bf16, once more.  Block
-// (u, .) takes kLoadRows rows of a unit at a time; a lane has sixteen values (8 bytes of codes), a row d / 16 lanes, four rows
-// in flight per lane.  Bound by memory, above all by what it writes.
-constexpr int kLoadDepth = 4;
-template <bool kF32, int kLanes>
+// (u, .) takes kLoadDepth rows per group of lanes at a time; a lane has sixteen values (8 bytes of codes), a row d / 16 lanes.
+// Bound by memory, above all by what it writes.
+template <bool kF32, int kLanes, int kLoadDepth>
 __global__ void __launch_bounds__(kThreads) load_rows_kernel(const LoadRowsArgs a) {
     constexpr int kGroups = kThreads / kLanes;           // rows per step
     const int u = blockIdx.x, b = u / a.n_kv_heads, h = u - b * a.n_kv_heads;
@@ -370,8 +435,7 @@ inline csp_status launched() { return cudaGetLastError() == cudaSuccess ? CSP_OK
 
 template <bool kF32, bool kFour, int kLanes>
 csp_status append_rows(const AppendRowsArgs& a, dim3 grid, cudaStream_t s) {
-    if (a.rope.dim) append_rows_kernel<kF32, kFour, true, kLanes><<<grid, kThreads, 0, s>>>(a);
-    else if constexpr (kFour) append_rows_kernel<kF32, kFour, false, kLanes><<<grid, kThreads, 0, s>>>(a);   // (only these may come without)
+    append_rows_kernel<kF32, kFour, kLanes><<<grid, kThreads, 0, s>>>(a);
     return launched();
 }
 
@@ -382,6 +446,14 @@ csp_status launch_append_rows(AppendRowsArgs a, int head_dim, bool f32, bool fou
     const int groups = kThreads / (head_dim / 16), pairs = a.n_kv_heads + (a.n_q_heads + 1) / 2;
     a.page_inverse = uint32_t((uint64_t(1) << 32) / uint32_t(a.page_rows)) + 1u;
     a.group_inverse = a.group > 1 ? uint32_t((uint64_t(1) << 32) / uint32_t(a.group)) + 1u : 0u;
+    if (!a.rope.dim) {                                   // (only calls for 4 bits come without)
+        const int rows = groups * kAppendDepth;
+        const int64_t tiles = a.max_new > 0 ? (int64_t(a.max_new) + rows - 1) / rows : 1;
+        const dim3 grid{unsigned(a.batch * a.n_kv_heads), unsigned(tiles < 65535 ? tiles : 65535)};
+        if (head_dim == 64) append_units_kernel<4><<<grid, kThreads, 0, s>>>(a);
+        else append_units_kernel<8><<<grid, kThreads, 0, s>>>(a);
+        return launched();
+    }
     // Few tokens: the lane groups of a block spread over the heads; from eight on, eight tokens share a block and every group goes
     // over some of the heads with one set of cosines.
     a.log_tokens = 0;
@@ -391,9 +463,9 @@ csp_status launch_append_rows(AppendRowsArgs a, int head_dim, bool f32, bool fou
     a.token_tiles = tiles < most ? tiles : most;
     const int step = groups >> a.log_tokens;             // heads at a time
     const int64_t blocks = int64_t(a.token_tiles) * a.batch;
-    // as many pieces of the heads as it takes to give every SM four blocks
+    // as many pieces of the heads as it takes to give every SM eight blocks (four: 1 K rotated tokens 19 us instead of 17.7)
     int pieces = (pairs + step - 1) / step;
-    const int64_t want = (4 * int64_t(sm_count()) + blocks - 1) / blocks;
+    const int64_t want = (8 * int64_t(sm_count()) + blocks - 1) / blocks;
     if (pieces > want) pieces = int(want);
     a.pairs_per_block = ((pairs + step - 1) / step + pieces - 1) / pieces * step;
     pieces = (pairs + a.pairs_per_block - 1) / a.pairs_per_block;
@@ -405,13 +477,19 @@ csp_status launch_append_rows(AppendRowsArgs a, int head_dim, bool f32, bool fou
 
 csp_status launch_load_rows(LoadRowsArgs a, int head_dim, bool f32, cudaStream_t s) {
     if (a.units == 0 || a.max_rows == 0) return CSP_OK;
-    const int rows = kThreads / (head_dim / 16) * kLoadDepth;
-    const int64_t tiles = (int64_t(a.max_rows < a.capacity ? a.max_rows : a.capacity) + rows - 1) / rows;
+    a.page_inverse = uint32_t((uint64_t(1) << 32) / uint32_t(a.page_rows)) + 1u;
+    // Four rows in flight per lane, but one where that leaves SMs without a block (5 K rows as fp32: 2.5 us instead of 4.4; 2.6 M
+    // rows with two 72.5 us instead of 71).
+    const int groups = kThreads / (head_dim / 16), rows = a.max_rows < a.capacity ? a.max_rows : a.capacity;
+    const int depth = int64_t(a.units) * rows < 4 * int64_t(groups) * sm_count() ? 1 : 4;
+    const int64_t tiles = (int64_t(rows) + groups * depth - 1) / (groups * depth);
     if (tiles == 0) return CSP_OK;
     const dim3 grid{unsigned(a.units), unsigned(tiles < 65535 ? tiles : 65535)};
-    a.page_inverse = uint32_t((uint64_t(1) << 32) / uint32_t(a.page_rows)) + 1u;
-    if (head_dim == 64) f32 ? load_rows_kernel<true, 4><<<grid, kThreads, 0, s>>>(a) : load_rows_kernel<false, 4><<<grid, kThreads, 0, s>>>(a);
-    else f32 ? load_rows_kernel<true, 8><<<grid, kThreads, 0, s>>>(a) : load_rows_kernel<false, 8><<<grid, kThreads, 0, s>>>(a);
+    const auto kernel = head_dim == 64 ? f32 ? depth == 1 ? load_rows_kernel<true, 4, 1> : load_rows_kernel<true, 4, 4>
+                                             : depth == 1 ? load_rows_kernel<false, 4, 1> : load_rows_kernel<false, 4, 4>
+                                       : f32 ? depth == 1 ? load_rows_kernel<true, 8, 1> : load_rows_kernel<true, 8, 4>
+                                             : depth == 1 ? load_rows_kernel<false, 8, 1> : load_rows_kernel<false, 8, 4>;
+    kernel<<<grid, kThreads, 0, s>>>(a);
     return launched();
 }
 
