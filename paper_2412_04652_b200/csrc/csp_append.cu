@@ -320,15 +320,16 @@ __global__ void __launch_bounds__(kThreads, 4) append_units_kernel(const AppendR
     const int32_t* const table = a.page_table + int64_t(b) * a.max_pages;
     const char* const from[2] = {static_cast<const char*>(a.k_new.ptr) + b * a.k_new.sb + h * a.k_new.sh,
                                  static_cast<const char*>(a.v_new.ptr) + b * a.v_new.sb + h * a.v_new.sh};
-    for (int64_t i0 = blockIdx.y * kGroups * kAppendDepth; i0 < n.stored; i0 += int64_t(gridDim.y) * kGroups * kAppendDepth) {
+    const uint32_t stored = uint32_t(n.stored);          // (below 2^31: a step past it is still a number of 32 bits)
+    for (uint32_t i0 = blockIdx.y * kGroups * kAppendDepth; i0 < stored; i0 += gridDim.y * kGroups * kAppendDepth) {
         Eight<false> x[kAppendDepth][2][2];
         int page[kAppendDepth];
         uint32_t slot[kAppendDepth];
 #pragma unroll
         for (int j = 0; j < kAppendDepth; ++j) {
-            const int i = int(i0) + j * kGroups + group;
-            if (i0 + j * kGroups + group >= n.stored) continue;
-            page[j] = table[divide(uint32_t(n.first + i), uint32_t(a.page_rows), a.page_inverse, slot[j])];
+            const uint32_t i = i0 + j * kGroups + group;
+            if (i >= stored) continue;
+            page[j] = table[divide(uint32_t(n.first) + i, uint32_t(a.page_rows), a.page_inverse, slot[j])];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const char* const row = from[k] + i * (k ? a.v_new.st : a.k_new.st);
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 4) append_units_kernel(const AppendR
         }
 #pragma unroll
         for (int j = 0; j < kAppendDepth; ++j) {
-            if (i0 + j * kGroups + group >= n.stored) continue;
+            if (i0 + j * kGroups + group >= stored) continue;
             if (page[j] < 0 || page[j] >= a.n_pages) {
                 if (L == 0) atomicOr(a.status, CSP_DEV_BAD_LEN);
                 continue;
