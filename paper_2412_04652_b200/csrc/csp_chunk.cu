@@ -858,6 +858,7 @@ ChunkPlan chunk_plan(const csp_params& p, int max_new) {
     // no more blocks than there can be shares of the smallest size
     const int64_t most = (items > 65536 ? 65536 : items) * weight / (pl.item_cost + pl.min_tiles) + 1;
     pl.grid = most < sm_count() ? int(most) : sm_count();
+    set_dividers(p, pl);
     return pl;
 }
 

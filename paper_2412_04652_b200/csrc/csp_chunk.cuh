@@ -16,6 +16,7 @@ struct ChunkPlan {                                       // sizes that host and 
     int item_cost;                                       // what an item costs besides its key tiles, in key tiles
     bool drawn;                                          // items may be drawn whole from a counter instead of shared out
     int snap;                                            // tiles by which a share may differ from an equal one to avoid a cut
+    Divider by_pairs, by_heads, by_group, by_tile;       // n_pairs, KV heads, query heads per KV head, key_tile
 };
 
 // What a block says about the items it was given only part of (see Share): the one that begins with it (-1: none), and whether
@@ -31,6 +32,12 @@ csp_status launch_chunk_join(const csp_params& p, const ChunkArgs& a, const Chun
 
 // how a chunk of bf16 queries is cut into items; for more than sixteen query rows per KV head a cache in 4 bits is cut alike
 ChunkPlan chunk_plan(const csp_params& p, int max_new);
+inline void set_dividers(const csp_params& p, ChunkPlan& pl) {
+    pl.by_pairs = divider(pl.n_pairs);
+    pl.by_heads = divider(p.n_kv_heads);
+    pl.by_group = divider(p.n_q_heads / p.n_kv_heads);
+    pl.by_tile = divider(pl.key_tile);
+}
 csp_status launch_chunk_q4_many(const csp_params& p, const ChunkArgs& a, const ChunkPlan& pl, const csp_tensor& q, const Q4Args& c,
                                 ChunkParts* parts, float* partial, float2* ml, cudaStream_t s);
 
@@ -68,11 +75,11 @@ __device__ __forceinline__ PairRange pair_range_of(const ChunkArgs& a, const Chu
     const int last0 = x.row0 + min(x.count, pl.tok_tile) - 1, last1 = x.row0 + x.count - 1;
     x.kv_end[0] = last0 < 0 ? 0 : max(last0 + 1, x.prefix);
     x.kv_end[1] = last1 < 0 ? 0 : max(last1 + 1, x.prefix);
-    x.tiles = (x.kv_end[1] + pl.key_tile - 1) / pl.key_tile;
+    x.tiles = pl.by_tile(x.kv_end[1] + pl.key_tile - 1);
     return x;
 }
 __device__ __forceinline__ PairRange pair_range(const ChunkArgs& a, const ChunkPlan& pl, int u, int pair) {
-    const int b = u / a.n_kv_heads, h = u % a.n_kv_heads;
+    const int b = pl.by_heads(u), h = u - b * a.n_kv_heads;
     return pair_range_of(a, pl, a.n_rows[u], a.n_new ? a.n_new[b] : a.max_new,
                          a.mods.prefix ? a.mods.prefix[int64_t(b) * a.mods.prefix_sb + int64_t(h) * a.mods.prefix_sh] : 0, pair);
 }
@@ -85,10 +92,10 @@ __device__ __forceinline__ PairRange pair_range(const ChunkArgs& a, const ChunkP
 // first item is the rest of a cut one (partial result 2 c) and its last one the beginning (2 c + 1).
 struct Share { int item0, tile0, item1, tile1; bool drawn; };
 __device__ __forceinline__ int item_weight(const ChunkArgs& a, const ChunkPlan& pl, int item, bool flag, int& tiles) {
-    const int u = item / pl.n_pairs, pair = item - u * pl.n_pairs;
+    const int u = pl.by_pairs(item), pair = item - u * pl.n_pairs;
     const PairRange x = pair_range(a, pl, u, pair);
     if (flag && pair == 0) {
-        const int rows = a.n_rows[u], more = a.n_new ? a.n_new[u / a.n_kv_heads] : a.max_new;
+        const int rows = a.n_rows[u], more = a.n_new ? a.n_new[pl.by_heads(u)] : a.max_new;
         if (rows != x.rows || more != x.n_new || x.n_new > x.rows) atomicOr(a.status, CSP_DEV_BAD_LEN);
     }
     tiles = x.count > 0 ? x.tiles : 0;

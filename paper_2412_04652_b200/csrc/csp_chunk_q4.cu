@@ -38,7 +38,7 @@ constexpr int kCountWord = 16, kMostBlocks = 192;        // of the status area: 
 constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
 constexpr float kTiny = 0x1p-126f, kHuge = 0x1p126f;     // bounds of the reference of the scales
 
-struct FewQuery { const uint16_t* q; int64_t sb, sh, st; };
+struct FewQuery { const uint16_t* q; int64_t sb, sh, st; Divider by_page; };      // by_page: tiles per page
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -121,7 +121,7 @@ __device__ __forceinline__ WarpShare warp_share(const ChunkArgs& a, const ChunkP
             int w = 0;
             PairRange r = {};
             if (item <= last && !(item == sh.item1 && sh.tile1 == 0)) {
-                const int u = item / pl.n_pairs;
+                const int u = pl.by_pairs(item);
                 r = pair_range(a, pl, u, item - u * pl.n_pairs);
                 w = r.count > 0 ? max((item == sh.item1 ? sh.tile1 : r.tiles) - lo, 0) + 1 : 0;
             }
@@ -197,14 +197,14 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
 
     auto segment = [&](int from, Segment& s) {           // the first one at or behind item `from`
         for (s.item = from; s.item <= min(mine.end, share.item1) && s.item < pl.n_items; ++s.item) {
-            const int u = s.item / pl.n_pairs, block_lo = s.item == share.item0 ? share.tile0 : 0;
+            const int u = pl.by_pairs(s.item), block_lo = s.item == share.item0 ? share.tile0 : 0;
             s.lo = s.item == mine.begin ? mine.begin_tile : block_lo;
             if (s.item == mine.end && mine.end_tile == block_lo) return false;
             if (s.item == share.item1 && share.tile1 == 0) return false;
             if (s.item == mine.begin) s.x = desk.first;
             else s.x = pair_range(a, pl, u, s.item - u * pl.n_pairs);
             s.hi = s.item == mine.end ? mine.end_tile : s.item == share.item1 ? share.tile1 : s.x.tiles;
-            if (s.x.count > 0) { s.b = u / a.n_kv_heads; s.h = u - s.b * a.n_kv_heads; return true; }
+            if (s.x.count > 0) { s.b = pl.by_heads(u); s.h = u - s.b * a.n_kv_heads; return true; }
         }
         return false;
     };
@@ -244,11 +244,11 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                 f_item = f.item;
                 f_end = f.hi;
                 f_tile = f.lo;
-                f_index = f_tile / tiles_per_page;
+                f_index = qy.by_page(f_tile);
                 f_left = (f_index + 1) * tiles_per_page - f_tile;
                 {                                        // the item's queries, positions and slopes will be asked for soon
                     constexpr int kLines = D / 64;       // of 128 bytes
-                    const int m = lane / kLines, tok = m / G;
+                    const int m = lane / kLines, tok = pl.by_group(m);
                     if (tok < f.x.count && m < Shape::R)
                         asm volatile("prefetch.global.L2 [%0];" ::"l"(qy.q + int64_t(f.b) * qy.sb + int64_t(f.h * G + m - tok * G) * qy.sh + int64_t(f.x.tok0 + tok) * qy.st + lane % kLines * 64));
                 }
@@ -348,7 +348,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                     if (biased && fabsf(table[m].pos) > kFarToken) atomicOr(a.status, CSP_DEV_BAD_LEN);
                     if (m >= count * G) continue;
                     const float base_sum = c ? b_run[n].y : b_run[n].x, l = c ? l_run[n].y : l_run[n].x, mm = c ? m_run[n].y : m_run[n].x;
-                    const int tok = m / G, head = seg.h * G + m - tok * G;
+                    const int tok = pl.by_group(m), head = seg.h * G + m - tok * G;
                     const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, mm) + l);      // l == 0: nothing was seen
                     uint16_t* const out = a.out + int64_t(seg.b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(seg.x.tok0 + tok) * a.o_st + 4 * gr;
 #pragma unroll
@@ -385,14 +385,14 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
         uint4 q[RH][KW];
 #pragma unroll
         for (int n = 0; n < RH; ++n) {
-            const int m = 8 * n + gr, tok = m / G;       // rows that are none are zeros
+            const int m = 8 * n + gr, tok = pl.by_group(m);       // rows that are none are zeros
             const uint16_t* const from = qy.q + int64_t(seg.b) * qy.sb + int64_t(seg.h * G + m - tok * G) * qy.sh + int64_t(seg.x.tok0 + tok) * qy.st + qd * KW * 8;
 #pragma unroll
             for (int w = 0; w < KW; ++w) q[n][w] = tok < count ? reinterpret_cast<const uint4*>(from)[w] : make_uint4(0, 0, 0, 0);
         }
         {
             // positions are taken relative to the last token's, so that near ones are exact in fp32
-            const int tok = lane / G, r = seg.x.row0 + tok, row_last = max(seg.x.row0 + count - 1, 0);
+            const int tok = pl.by_group(lane), r = seg.x.row0 + tok, row_last = max(seg.x.row0 + count - 1, 0);
             const bool valid = lane < Shape::R && tok < count, sees = valid && r >= 0;
             pos_ref = biased && rows > 0 ? (poss ? poss[row_last] : row_last) : 0;
             const int pos = biased && sees ? (poss ? poss[r] : r) : pos_ref, doc = docs && sees ? docs[r] : 0;
@@ -617,7 +617,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     // ---- the pieces of cut items: chain 0 goes on with what the block before began, chain c begins with warp c - 1's back piece
     // query row m of an item, joined: four columns per lane
     auto finish = [&](int b, int h, int tok0, int m, float mm, float l, const float4& o) {
-        const int tok = tok0 + m / G, head = h * G + m % G;
+        const int at = pl.by_group(m), tok = tok0 + at, head = (h - at) * G + m;
         const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, mm) + l);
         if (lane < D / 4)
             *reinterpret_cast<uint2*>(a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st + 4 * lane) =
@@ -710,7 +710,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     for (int k = 0; k < 2; ++k) {
         if (cut[k] < 0 || !chains[4 + k]) continue;
         const int first = chains[2 * k], n = chains[2 * k + 1], item = cut[k];
-        const int u = item / pl.n_pairs, b = u / a.n_kv_heads, h = u - b * a.n_kv_heads;
+        const int u = pl.by_pairs(item), b = pl.by_heads(u), h = u - b * a.n_kv_heads;
         const PairRange x = pair_range(a, pl, u, item - u * pl.n_pairs);
         struct Parts {
             const float* o; const float2* m; int first, rows, col;
@@ -756,6 +756,7 @@ ChunkPlan chunk_q4_plan(const csp_params& p, int max_new, bool* few) {
     const int64_t most = (items > 65536 ? 65536 : items) * weight / (pl.item_cost + pl.min_tiles) + 1;
     const int blocks = sm_count() < kMostBlocks ? sm_count() : kMostBlocks;
     pl.grid = most < blocks ? int(most) : blocks;
+    set_dividers(p, pl);
     return pl;
 }
 
@@ -807,7 +808,7 @@ csp_status launch_chunk_q4(const csp_params& p, const ChunkArgs& a, const csp_te
     float* const partial = reinterpret_cast<float*>(static_cast<char*>(ws) + lay.o);
     float2* const ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + lay.ml);
     if (few) {
-        const FewQuery qy = {static_cast<const uint16_t*>(q.ptr), q.stride_b, q.stride_h, q.stride_t};
+        const FewQuery qy = {static_cast<const uint16_t*>(q.ptr), q.stride_b, q.stride_h, q.stride_t, divider(a.page_rows / kQ4Tile)};
         if (pl.row_slots <= 8)
             return p.head_dim == 64 ? launch_few<1, 1>(a, pl, qy, c, partial, ml, s) : launch_few<2, 1>(a, pl, qy, c, partial, ml, s);
         return p.head_dim == 64 ? launch_few<1, 2>(a, pl, qy, c, partial, ml, s) : launch_few<2, 2>(a, pl, qy, c, partial, ml, s);

@@ -244,6 +244,21 @@ struct AppendArgs {
     int32_t* status;
 };
 // a tensor of rows as the append kernels take it: strides in bytes
+// Division of whole numbers from 0 to 2^31 - 1 by n >= 1: with 2^(l-1) < n <= 2^l and m = 2^(31+l) / n rounded up (which fits 32
+// bits), t m / 2^(31+l) is more than t / n by less than 1 / n.  (A division by a variable is some thirty instructions.)
+struct Divider {
+    uint32_t m;
+    int s;
+#ifdef __CUDACC__
+    __device__ __forceinline__ int operator()(int t) const { return int((uint64_t(uint32_t(t)) * m) >> s); }
+#endif
+};
+inline Divider divider(int n) {
+    int l = 0;
+    while ((int64_t(1) << l) < n) ++l;
+    return Divider{uint32_t(((uint64_t(1) << (31 + l)) + uint64_t(n) - 1) / uint64_t(n)), 31 + l};
+}
+
 struct RowTensor { void* ptr; int64_t sb, sh, st; };
 struct RopeArgs {
     const float* cos_sin; int64_t row_stride;        // cosines of dim / 2 angles, then their sines, per row
