@@ -840,6 +840,7 @@ ChunkPlan chunk_plan(const csp_params& p, int max_new) {
     ChunkPlan pl;
     const int G = p.n_q_heads / p.n_kv_heads;
     pl.tok_tile = 128 / G;
+    pl.pair_tokens = 2 * pl.tok_tile;
     pl.drawn = false;
     pl.n_pairs = (max_new + 2 * pl.tok_tile - 1) / (2 * pl.tok_tile);
     if (pl.n_pairs < 1) pl.n_pairs = 1;

@@ -8,8 +8,8 @@
 namespace csp {
 
 struct ChunkPlan {                                       // sizes that host and device agree on
-    int tok_tile;                                        // tokens in a row tile: 128 / G
-    int n_pairs, row_slots;                              // row pairs per unit, rows of a partial result
+    int tok_tile, pair_tokens;                           // tokens in a row tile: 128 / G; in an item: a pair of these
+    int n_pairs, row_slots;                              // items per unit, rows of a partial result
     int n_items;                                         // units x pairs
     int grid;                                            // resident blocks
     int key_tile, min_tiles;                             // keys per tile; tiles that a part of a cut item has at least
@@ -68,8 +68,8 @@ __device__ __forceinline__ PairRange pair_range_of(const ChunkArgs& a, const Chu
     PairRange x;
     x.rows = min(max(rows, 0), a.capacity);
     x.n_new = min(max(n_new, 0), a.max_new);
-    x.tok0 = pair * 2 * pl.tok_tile;
-    x.count = min(x.n_new - x.tok0, 2 * pl.tok_tile);
+    x.tok0 = pair * pl.pair_tokens;
+    x.count = min(x.n_new - x.tok0, pl.pair_tokens);
     x.row0 = x.rows - x.n_new + x.tok0;
     x.prefix = min(max(prefix, 0), x.rows);
     const int last0 = x.row0 + min(x.count, pl.tok_tile) - 1, last1 = x.row0 + x.count - 1;

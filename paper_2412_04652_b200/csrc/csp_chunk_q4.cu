@@ -27,6 +27,8 @@
 #include <cuda_fp16.h>
 #include <limits.h>
 
+#include <initializer_list>
+
 #include "csp_chunk.cuh"
 
 namespace csp {
@@ -729,22 +731,27 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
 
 // ---- host side -----------------------------------------------------------------------------------------------------
 
-constexpr int kQ4Rows = 16;                              // query rows of an item here
-// Up to two such items per KV head: this kernel, which reads the cache once for each of them.  Beyond that row tiles of 128.
-// Measured here and there: 8 x 32 / 8 heads, 2 K - 8 K rows, 20 query rows 57 and 80 us.
-constexpr int kQ4Items = 2;
+// Tokens of an item here; 0: more query rows than this kernel is for, row tiles of 128.  The cache is read once per item, of which
+// there are n8 of up to eight rows or n16 of up to sixteen.  One of sixteen takes as long as one and a half of eight where caches
+// are long; where they are short the smaller code starts and ends 3 us earlier.  Measured, 8 x 32 / 8 heads, items of 8 and of 16:
+// 16 query rows over 4 K rows 26.5 and 28 us, over 16 K rows 65.5 and 58; 20 query rows 32.6 and 36, 94 and 99.5; 32 query rows
+// 38.6 and 38.2, 123 and 99; 48 query rows 51 and 47.4 (row tiles 59.6), 175 and 142 (157).
+constexpr int kMostItems = 3;                            // of sixteen rows
+int few_tokens(const csp_params& p, int max_new) {
+    const int G = p.n_q_heads / p.n_kv_heads, eight = 8 / G, sixteen = 16 / G;
+    const int64_t n8 = (int64_t(max_new) + eight - 1) / eight, n16 = (int64_t(max_new) + sixteen - 1) / sixteen;
+    if (n16 > kMostItems) return 0;
+    return (2 * n8 - 3 * n16) * p.batch * p.n_kv_heads <= (1 << 19) / (int64_t(p.out_capacity) + 1) ? eight : sixteen;
+}
 
 ChunkPlan chunk_q4_plan(const csp_params& p, int max_new, bool* few) {
-    const int G = p.n_q_heads / p.n_kv_heads;
     ChunkPlan pl = chunk_plan(p, max_new);
-    const int tile = kQ4Rows / 2 / G, pairs = max_new / (2 * tile) + (max_new % (2 * tile) ? 1 : 0);
-    *few = int64_t(max_new) * G <= kQ4Rows || pairs <= kQ4Items;
+    const int G = p.n_q_heads / p.n_kv_heads, tokens = few_tokens(p, max_new);
+    *few = tokens > 0;
     if (!*few) return pl;
-    if (int64_t(max_new) * G > kQ4Rows) {                // (an item has 2 tok_tile tokens)
-        pl.tok_tile = tile;
-        pl.n_pairs = pairs;
-        pl.row_slots = 2 * tile * G;
-    }
+    pl.tok_tile = pl.pair_tokens = tokens;
+    pl.n_pairs = max_new > tokens ? (max_new + tokens - 1) / tokens : 1;
+    pl.row_slots = (max_new < tokens ? max_new : tokens) * G;
     pl.snap = 0x3fffffff;
     pl.key_tile = kQ4Tile;
     pl.min_tiles = 4;
@@ -790,12 +797,15 @@ size_t chunk_q4_workspace_bytes(const csp_params& p, int max_new) {
     bool few;
     const ChunkPlan pl = chunk_q4_plan(p, max_new, &few);
     if (pl.n_items < 0) return 0;                                                // key tiles are counted in 32 bits
-    // Enough for shorter chunks as well: those of one or two small items have other tiles and shares.  (Among chunks of one kind
-    // the size grows with max_new.)
-    const int G = p.n_q_heads / p.n_kv_heads, longest[2] = {kQ4Rows / G, kQ4Items * 2 * (kQ4Rows / 2 / G)};
+    // Enough for shorter chunks as well: those of a few small items have other tiles and shares.  (Among chunks with items of one
+    // size the need grows with max_new.)
     size_t mine = partial_layout(p, pl).total;
-    for (const int n : longest) {
-        const size_t shorter = partial_layout(p, chunk_q4_plan(p, max_new < n ? max_new : n, &few)).total;
+    const int G = p.n_q_heads / p.n_kv_heads, longest = kMostItems * (16 / G);
+    int eight = -1, sixteen = -1;                        // the longest chunks of either kind
+    for (int n = 0; n <= (max_new < longest ? max_new : longest); ++n) (few_tokens(p, n) == 8 / G ? eight : sixteen) = n;
+    for (const int n : {eight, sixteen}) {
+        if (n < 0 || n == max_new) continue;
+        const size_t shorter = partial_layout(p, chunk_q4_plan(p, n, &few)).total;
         if (shorter > mine) mine = shorter;
     }
     return mine;
