@@ -414,21 +414,24 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
             top2 = max_abs2(top2, __shfl_xor_sync(0xffffffffu, top2, 1));
             top2 = max_abs2(top2, __shfl_xor_sync(0xffffffffu, top2, 2));
             const uint32_t top = (top2 & 0x7fffu) >> 7, ex = max(top, 14u);      // top 255: an infinity, the row is no number
-            const float down = __uint_as_float((264u - ex) << 23), down16 = 16.f * down;                 // 2^(10 - e)
+            const float down = __uint_as_float((264u - ex) << 23);        // 2^(10 - e)
             // logit = up (scale S + base sum 2^-20), S the product with codes 2^-20
             const float up = a.scale * kLog2e * 0x1p10f * (top == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(ex << 23));
             factor[n] = make_float2(__shfl_sync(0xffffffffu, up, 8 * qd), __shfl_sync(0xffffffffu, up, 8 * qd + 4));
-            float ones[4] = {0.f, 0.f, 0.f, 0.f};        // the product with codes of one: the query's sum 2^-20
+            float total = 0.f;                           // the query's sum (in fp32: an error of it is one of all logits)
 #pragma unroll
             for (int w = 0; w < KW; ++w) {
-                qb[n][2 * w][0] = pack_f16(down16 * lo_bf16(q[n][w].x), down16 * lo_bf16(q[n][w].z));
-                qb[n][2 * w][1] = pack_f16(down * hi_bf16(q[n][w].x), down * hi_bf16(q[n][w].z));
-                qb[n][2 * w + 1][0] = pack_f16(down16 * lo_bf16(q[n][w].y), down16 * lo_bf16(q[n][w].w));
-                qb[n][2 * w + 1][1] = pack_f16(down * hi_bf16(q[n][w].y), down * hi_bf16(q[n][w].w));
-                mma_f16(ones, 0x00010001u, 0x00010001u, 0x00100010u, 0x00100010u, qb[n][2 * w][0], qb[n][2 * w][1]);
-                mma_f16(ones, 0x00010001u, 0x00010001u, 0x00100010u, 0x00100010u, qb[n][2 * w + 1][0], qb[n][2 * w + 1][1]);
+                const float f[8] = {lo_bf16(q[n][w].x) * down, hi_bf16(q[n][w].x) * down, lo_bf16(q[n][w].y) * down, hi_bf16(q[n][w].y) * down,
+                                    lo_bf16(q[n][w].z) * down, hi_bf16(q[n][w].z) * down, lo_bf16(q[n][w].w) * down, hi_bf16(q[n][w].w) * down};
+                total += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+                qb[n][2 * w][0] = pack_f16(16.f * f[0], 16.f * f[4]);
+                qb[n][2 * w][1] = pack_f16(f[1], f[5]);
+                qb[n][2 * w + 1][0] = pack_f16(16.f * f[2], 16.f * f[6]);
+                qb[n][2 * w + 1][1] = pack_f16(f[3], f[7]);
             }
-            q_sum[n] = make_float2(ones[0], ones[1]);
+            total += __shfl_xor_sync(0xffffffffu, total, 1);
+            total = (total + __shfl_xor_sync(0xffffffffu, total, 2)) * 0x1p-20f;
+            q_sum[n] = make_float2(__shfl_sync(0xffffffffu, total, 8 * qd), __shfl_sync(0xffffffffu, total, 8 * qd + 4));
             m_run[n] = make_float2(kNeg, kNeg);
             l_run[n] = b_run[n] = make_float2(0.f, 0.f);
 #pragma unroll
