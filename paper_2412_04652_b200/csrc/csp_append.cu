@@ -11,6 +11,10 @@
 // A row of d values is held by d / 16 neighbouring lanes, sixteen values each, so that the row's extremes take three shuffles, and
 // a pair is always in one thread: with halves paired a lane takes eight values from each half.  A group of lanes keeps its
 // token and goes over the heads, so that its eight cosines and sines are loaded once.
+//
+// Measured (bound by HBM where there are many rows, by launch and dependent loads where there are few): rotation of one token of
+// 32 x 32 heads 2.8 us, of 513 - 1024 tokens of 4 x 32 / 8 heads 17.7 us (4.35 TB/s); 262 K unrotated rows to 4 bits 37 us (4.6 TB/s, two
+// thirds of the issue slots); 650 K rows read back as bf16 71 us (6 TB/s).
 #include "csp_internal.cuh"
 
 namespace csp {

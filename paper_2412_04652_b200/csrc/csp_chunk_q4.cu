@@ -1,4 +1,4 @@
-// Attention of new tokens over pages held in 4 bits, up to sixteen query rows (token x head) per item.
+// Attention of new tokens over pages held in 4 bits, up to sixteen query rows (token x head) per item, up to three of these per KV head.
 //
 // A row is base + scale code, so  <q, k_t> = scale_t <q, code_t> + base_t sum q  and
 // sum_t p_t v_t = sum_t (p_t scale'_t) code'_t + sum_t p_t base'_t: the products see whole numbers, and what belongs to a row is
@@ -24,6 +24,12 @@
 // has read a slot.  An item (up to sixteen query rows of a unit) that lies in one warp's share is finished by
 // it; of one that is cut the pieces stay in shared memory until all warps are done and are joined then, in order; of one that
 // goes on in another CTA a partial result is left, and the CTA that leaves the last one joins them, in order.
+//
+// Measured: 32 x 32 heads of 128, 410 - 1640 rows, one token: 39 us, 3.6 TB/s over all.  A tile takes a warp 2800 clocks (eight query
+// rows, twelve warps: 5.2 TB/s while they run); in front of the first one lie 12 K clocks, six dependent loads and 1500 instructions
+// that run once, and behind the last one 10 K, of which the jump into code that was not fetched yet is 3 K and the join across blocks
+// another 3 K.  So long GQA (five tiles per warp) takes 28.6 us where its bytes take 7.
+// Two more tiles in flight or eleven warps change nothing; sixteen warps leave too few registers.
 #include <cuda_fp16.h>
 #include <limits.h>
 

@@ -20,7 +20,11 @@
 //   warp 17     one elected lane issues tcgen05.mma
 //   warps 0-7, 8-15  two softmax groups, two threads per query row; at an item's start they turn the queries into halves in place
 //
-// Measured: to be filled in.
+// Measured: 513 - 1024 tokens, 4 x 28 / 4 heads of 128, over 8 K - 32 K rows: 1.16 ms, 780 TFLOP/s of the two products' 1650 (a bf16
+// cache 0.84 - 0.95 ms).  Neither HBM (5 %) nor the tensor cores (36 % of the clocks) nor instructions (50 %) are the bound, but the chain
+// of a step of 128 keys, some 5400 clocks for two row tiles: products, first pass over the logits, second pass with the weights, products.
+// Slower were: one pass with the weights in registers (they spill), four unpacking warps (1.19 ms), codes held in registers a tile ahead
+// (1.22), scales of V applied to the weights (1.37).
 #include <limits.h>
 
 #include "csp_chunk.cuh"
