@@ -49,7 +49,7 @@ def test_one_token_groups(csp, G):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("G,T", [(1, 2), (1, 8), (1, 9), (1, 16), (1, 17), (2, 9), (4, 5), (7, 2), (7, 3), (8, 33), (3, 100), (1, 130), (1, 257), (5, 70)])
+@pytest.mark.parametrize("G,T", [(1, 2), (1, 8), (1, 9), (1, 16), (1, 17), (2, 9), (4, 5), (7, 2), (7, 3), (7, 6), (7, 7), (1, 48), (1, 49), (4, 12), (4, 13), (3, 15), (8, 33), (3, 100), (1, 130), (1, 257), (5, 70)])
 def test_chunks(csp, G, T, d):
     _case(csp, [[T + 200, T], [T + 3, 333 + T]], [T, max(T - 3, 1)], G=G, d=d, seed=T)
 
@@ -94,14 +94,14 @@ def test_modifiers(csp, kind, T):
     _case(csp, [[400, 390], [222, 300]], [T, max(T - 1, 1)], G=3, mods=mods, seed=T)
 
 
-@pytest.mark.parametrize("T", [1, 30])
+@pytest.mark.parametrize("G,T", [(1, 1), (1, 30), (2, 30)])
 @pytest.mark.parametrize("n", [0.0, 1.0, 2.5])
-def test_normaliser(csp, n, T):
-    _case(csp, [[300, 40]], [T], n=n, seed=3)
-    _case(csp, [[300, 40]], [T], n=n, scale=0.01, seed=3)
+def test_normaliser(csp, n, G, T):
+    _case(csp, [[300, 40]], [T], G=G, n=n, seed=3)
+    _case(csp, [[300, 40]], [T], G=G, n=n, scale=0.01, seed=3)
 
 
-@pytest.mark.parametrize("T", [1, 30])
+@pytest.mark.parametrize("T", [1, 30, 60])
 def test_large_and_small_values(csp, T):
     """Scales of V that differ by many powers of two between the rows, queries far from one."""
     _case(csp, [[500, 129]], [T], gain=torch.exp2(torch.randint(-12, 12, (1, 2, 500, 1)).float()), q_gain=0.02, seed=9)
@@ -111,7 +111,7 @@ def test_large_and_small_values(csp, T):
     _case(csp, [[500, 129]], [T], gain=2.0 ** 110, q_gain=2.0 ** -118, seed=9)
 
 
-@pytest.mark.parametrize("T", [1, 40])
+@pytest.mark.parametrize("T", [1, 40, 60])
 def test_many_units_and_long_caches(csp, T):
     """More items than blocks, and caches that are cut between blocks."""
     _case(csp, [[70 + 13 * (b * 8 + h) % 500 + T for h in range(8)] for b in range(24)], [T] * 24, d=64, lse=False)
@@ -120,7 +120,7 @@ def test_many_units_and_long_caches(csp, T):
 
 # ---- what may be wrong with the inputs
 
-@pytest.mark.parametrize("T", [1, 40])
+@pytest.mark.parametrize("T", [1, 40, 60])
 def test_a_page_outside_the_pool_reads_as_zeros(csp, T):
     p, q, K, V, table, rows, out, z, ws = _case(csp, [[384, 300]], [T])
     (kc, ks), (vc, vs) = [(c.cpu(), s.cpu()) for c, s in ((K.codes, K.scales), (V.codes, V.scales))]
@@ -268,7 +268,7 @@ def test_offsets_past_32_bits(csp):
         dense.append((codes, scales))
         caches.append(c)
     p = csp.Params(1, H, H, d, 1, 0, 300, 300)
-    for T in (1, 20):
+    for T in (1, 20, 60):
         q = torch.randn(1, H, T, d, generator=gen).to(torch.bfloat16).cuda()
         out, ws = torch.zeros_like(q), csp.new_chunk_q4_workspace(p, T)
         csp.chunk_attn_q4_paged(p, q, *caches, table, rows.cuda(), out, ws)
@@ -288,7 +288,7 @@ def test_offsets_past_32_bits(csp):
         assert ((got[0, :, 2:9].double() - x[0].double()).abs().amax(-1) <= step * (0.5 + 16 * 2.0 ** -8) + 2.0 ** -8 * 8).all()
 
 
-SHAPES = [(2, 2, 2, 6000), (1, 3, 4, 2500), (40, 1, 2, 6000), (20, 4, 80, 250), (5, 2, 4, 890)]
+SHAPES = [(2, 2, 2, 6000), (1, 3, 4, 2500), (40, 1, 2, 6000), (20, 4, 80, 250), (30, 4, 80, 250), (5, 2, 4, 890)]
 
 
 @pytest.mark.parametrize("T,B,H,cap", SHAPES)
@@ -351,12 +351,12 @@ def test_two_streams_at_once(csp):
 
 def test_one_workspace_for_chunks_of_all_lengths(csp):
     """Made for the longest chunk, used for that one, for the lengths around a change of kernel and for single tokens."""
-    for G, H, longest in ((7, 2, 5), (1, 3, 40), (8, 2, 300)):
+    for G, H, longest in ((7, 2, 5), (1, 3, 40), (8, 2, 300), (3, 2, 20)):
         rows = torch.tensor([[1500 - 3 * h for h in range(H)]], dtype=torch.int32)
         dense, pools, table = paged_cache(rows, 1500, H, 128, 128, G)
         p = csp.Params(1, G * H, H, 128, 1, 0, 1500, 1500)
         ws = csp.new_chunk_q4_workspace(p, longest)
-        for T in sorted({longest, 1, 2, min(longest, 4), min(longest, 17), min(longest, 33)}, reverse=True):
+        for T in sorted({longest, 1, 2, min(longest, 4), min(longest, 6), min(longest, 17), min(longest, 33)}, reverse=True):
             q = torch.randn(1, G * H, T, 128, generator=torch.Generator().manual_seed(T)).to(torch.bfloat16).cuda()
             out = torch.zeros_like(q)
             csp.chunk_attn_q4_paged(p, q, csp.Q4Cache(*pools[0]), csp.Q4Cache(*pools[1]), table, rows.cuda(), out, ws)
@@ -422,6 +422,25 @@ def test_random_launches(csp):
             return m
         _case(csp, rows.tolist(), new, G=G, d=d, page_rows=int(rng.choice([128, 256])), n=float(rng.choice([0.0, 1.0])), seed=trial, cap=cap,
               q_gain=float(rng.choice([0.5, 1.5, 4.0])), mods=mods)
+
+
+def test_a_querys_sum_keeps_32_bits(csp):
+    """Keys that are all -8 (scale 0): every logit is -8 scale sum q, all weights are one, and the log-sum-exp shows what the sum is off
+    by.  Twelve roundings of partial sums at most (the scaling is exact), each by 2^-24 of what has the size |q| for random signs; the
+    logarithm and the last steps 2^-22 (1 + |lse|)."""
+    for T in (1, 3, 60):
+        rows = torch.full((4, 4), 512, dtype=torch.int32)
+        _, pools, table = paged_cache(rows, 512, 4, 128, 128, 31)
+        pools[0][1][..., 0], pools[0][1][..., 1] = 0, -8
+        q = torch.randn(4, 16, T, 128, generator=torch.Generator().manual_seed(T)).to(torch.bfloat16)
+        p = csp.Params(4, 16, 4, 128, 1, 0, 512, 512)
+        out, z, ws = torch.zeros_like(q).cuda(), torch.zeros(4, 16, T, device="cuda"), csp.new_chunk_q4_workspace(p, T)
+        csp.chunk_attn_q4_paged(p, q.cuda(), csp.Q4Cache(*pools[0]), csp.Q4Cache(*pools[1]), table, rows.cuda(), out, ws, lse=z)
+        sc = 128 ** -0.5
+        want = -8 * sc * q.double().sum(-1) + (512 - T + 1 + torch.arange(T)).double().log()
+        rms = (z.cpu().double() - want).square().mean().sqrt()
+        size = q.double().norm(dim=-1).square().mean().sqrt()
+        assert rms <= 12 * 2.0 ** -24 * 8 * sc * size + 2.0 ** -22 * (1 + want.square().mean().sqrt()), (T, float(rms))
 
 
 # ---- together
