@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, kF32 ? 3 : 4) append_rows_kernel(con
                         const uint32_t pair = quantise<kLanes>(z, lanes, w0, w1);
                         reinterpret_cast<uint32_t*>(row)[z0] = w0;
                         reinterpret_cast<uint32_t*>(row)[z1] = w1;
-                        if (L == 0) *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page * sc.sb + s * sc.sh + slot * 4) = pair;
+                        if (L == 0) *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page * sc.sb + s * sc.sh + int64_t(slot) * 4) = pair;
                     }
                 };
                 store(a.k, a.k_scales, x, r0, r1);
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 4) append_units_kernel(const AppendR
                 uint32_t* const row = reinterpret_cast<uint32_t*>(static_cast<char*>(to.ptr) + page[j] * to.sb + h * to.sh + slot[j] * to.st);
                 row[L] = w0;
                 row[L + kLanes] = w1;
-                if (L == 0) *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page[j] * sc.sb + h * sc.sh + slot[j] * 4) = pair;
+                if (L == 0) *reinterpret_cast<uint32_t*>(static_cast<char*>(sc.ptr) + page[j] * sc.sb + h * sc.sh + int64_t(slot[j]) * 4) = pair;
             }
         }
     }
@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(kThreads) load_rows_kernel(const LoadRowsArgs 
                 }
                 const uint32_t* const row = reinterpret_cast<const uint32_t*>(codes + page * from.sb + slot * from.st);
                 w[j] = make_uint2(__ldcs(row + L), __ldcs(row + L + kLanes));
-                pair[j] = *reinterpret_cast<const uint32_t*>(scales + page * sc.sb + slot * 4);
+                pair[j] = *reinterpret_cast<const uint32_t*>(scales + page * sc.sb + int64_t(slot) * 4);
             }
 #pragma unroll
             for (int j = 0; j < kLoadDepth; ++j) {
