@@ -91,8 +91,11 @@ enum Mods { kNone, kCap, kBias, kAny };
 template <int NH, int RH>   // head_dim = 64 NH, 8 RH query rows
 struct Q4Shape {
     static constexpr int D = 64 * NH, R = 8 * RH;
+    // As many warps as their registers allow: eight rows 160 each, sixteen 240.  (Eight warps for eight rows: 47 us instead of 45 for the
+    // serving batch, 33 instead of 30 for long GQA when this was measured.)
     static constexpr int kWarps = RH == 1 ? 12 : 8;
-    static constexpr int kSlots = NH == 2 ? 2 : 4;                                     // tiles in flight per warp
+    // Tiles in flight per warp, 4.6 KB each at d = 128.  (Three instead of two of them: serving batch 40.7 us instead of 39.5.)
+    static constexpr int kSlots = NH == 2 ? 2 : 4;
     static constexpr uint32_t kCodeBytes = kQ4Tile * D / 2, kScaleBytes = kQ4Tile * 4; // of K or of V
     static constexpr uint32_t kLoadBytes = 2 * kCodeBytes + 2 * kScaleBytes;
     static constexpr uint32_t kSlotBytes = kLoadBytes + 2 * kQ4Tile * 4;               // then positions and documents
