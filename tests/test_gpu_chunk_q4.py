@@ -14,7 +14,7 @@ def csp():
     return binding
 
 
-def _case(csp, rows, new, G=1, d=128, page_rows=128, n=1.0, scale=0.0, seed=1, cap=None, lse=True, gain=1.0, q_gain=1.5, mods=None, dense_edit=None):
+def _case(csp, rows, new, G=1, d=128, page_rows=128, n=1.0, scale=0.0, seed=1, cap=None, lse=True, gain=1.0, q_gain=1.5, mods=None, capacity=None):
     rows, new = torch.tensor(rows, dtype=torch.int32), torch.tensor(new, dtype=torch.int32)
     B, H = rows.shape
     T = max(int(new.max()), 1)
@@ -24,15 +24,22 @@ def _case(csp, rows, new, G=1, d=128, page_rows=128, n=1.0, scale=0.0, seed=1, c
     q = (torch.randn(B, T, H * G, d, generator=gen) * q_gain).to(torch.bfloat16).cuda().transpose(1, 2)
     out = torch.full((B, T, H * G, d), 7.0, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
     z = torch.full((B, H * G, T), 7.0, device="cuda") if lse else None
-    p = csp.Params(B, H * G, H, d, 1, 0, cap, cap, n=n, scale=scale)
+    if capacity:                                         # more than the rows need
+        wide = torch.full((B, -(-capacity // page_rows)), 10 ** 6, dtype=torch.int32, device="cuda")
+        wide[:, :table.shape[1]] = table
+        table = wide
+    p = csp.Params(B, H * G, H, d, 1, 0, capacity or cap, capacity or cap, n=n, scale=scale)
     ws = csp.new_chunk_q4_workspace(p, T)
-    kw = mods(B, H, G, cap) if mods else {}
+    kw = mods(B, H, G, capacity or cap) if mods else {}
     sm = csp.ScoreMods(**{k: v.cuda() if torch.is_tensor(v) else v for k, v in kw.items()}) if kw else None
     K, V = (csp.Q4Cache(*x) for x in pools)
     csp.chunk_attn_q4_paged(p, q, K, V, table, rows.cuda(), out, ws, n_new=new.cuda(), mods=sm, lse=z)
     assert csp.device_status(ws) == 0
     for b in range(B):                                   # tokens that nobody brought are left as they were
         assert (out[b, :, int(new[b]):] == 7.0).all() and (z is None or (z[b, :, int(new[b]):] == 7.0).all())
+    for k in ("positions", "documents"):
+        if k in kw:
+            kw[k] = kw[k][..., :cap]
     check(out, z, q, dense, rows, new, n=n, scale=scale, **kw)
     return p, q, K, V, table, rows, out, z, ws
 
@@ -74,9 +81,7 @@ def test_nothing_to_see(csp):
     assert (out[1, :2, :1] == 0).all() and (out[1, :, 1:] == 7.0).all()
 
 
-@pytest.mark.parametrize("T", [1, 4, 40])
-@pytest.mark.parametrize("kind", ["cap", "bias", "positions", "docs", "prefix", "all"])
-def test_modifiers(csp, kind, T):
+def _mods(kind):
     def mods(B, H, G, cap):
         gen = torch.Generator().manual_seed(5)
         m = {}
@@ -91,7 +96,48 @@ def test_modifiers(csp, kind, T):
         if kind in ("prefix", "all"):
             m["prefix"] = torch.tensor([[390, 10], [0, 1000]], dtype=torch.int32)
         return m
-    _case(csp, [[400, 390], [222, 300]], [T, max(T - 1, 1)], G=3, mods=mods, seed=T)
+    return mods
+
+
+@pytest.mark.parametrize("T", [1, 4, 40])
+@pytest.mark.parametrize("kind", ["cap", "bias", "positions", "docs", "prefix", "all"])
+def test_modifiers(csp, kind, T):
+    _case(csp, [[400, 390], [222, 300]], [T, max(T - 1, 1)], G=3, mods=_mods(kind), seed=T)
+
+
+WIDE = 1 << 18                                           # a capacity for which items of sixteen rows are taken where rows allow it
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,T", [(1, 9), (1, 16), (1, 31), (2, 8), (3, 4), (4, 4), (4, 8), (5, 3), (5, 5), (7, 2), (7, 4), (8, 2), (8, 5)])
+def test_items_of_sixteen_rows(csp, G, T, d):
+    _case(csp, [[T + 200, T], [T + 3, 333 + T]], [T, max(T - 3, 1)], G=G, d=d, seed=T, capacity=WIDE)
+    _case(csp, [[9000, 5000]], [T], G=G, d=d, capacity=2 * WIDE, lse=False)
+
+
+@pytest.mark.parametrize("kind", ["cap", "bias", "positions", "docs", "prefix", "all"])
+def test_modifiers_of_sixteen_rows(csp, kind):
+    _case(csp, [[400, 390], [222, 300]], [5, 4], G=3, mods=_mods(kind), capacity=WIDE)
+    _case(csp, [[400, 390], [222, 300]], [9, 10], G=3, d=64, mods=_mods(kind), capacity=WIDE)
+
+
+def test_numbers_of_sixteen_rows(csp):
+    """Normalisers, large and small values, NaN behind the last row and in front of it."""
+    for n in (0.0, 1.0, 2.5):
+        _case(csp, [[300, 40]], [12], n=n, seed=3, capacity=2 * WIDE)
+    _case(csp, [[500, 129]], [12], gain=torch.exp2(torch.randint(-12, 12, (1, 2, 500, 1)).float()), q_gain=0.02, seed=9, capacity=2 * WIDE)
+    _case(csp, [[500, 129]], [12], gain=2.0 ** -100, q_gain=2.0 ** 100, seed=9, capacity=2 * WIDE)
+    p, q, K, V, table, rows, out, z, ws = _case(csp, [[200, 150]], [6], G=2, capacity=2 * WIDE)
+    good = out.clone()
+    for x in (K, V):
+        keep = x.scales.clone()
+        x.scales[table[0, 0].long(), 0, 5, 0] = float("nan")
+        csp.chunk_attn_q4_paged(p, q, K, V, table, rows.cuda(), out, ws)
+        assert csp.device_status(ws) == 0 and torch.isnan(out[0, :2]).all() and torch.equal(out[0, 2:], good[0, 2:])
+        x.scales.copy_(keep)
+    q[0, 0, 0] = 0
+    csp.chunk_attn_q4_paged(p, q, K, V, table, rows.cuda(), out, ws)
+    assert torch.isfinite(out).all() and torch.equal(out[0, 1:], good[0, 1:])
 
 
 @pytest.mark.parametrize("G,T", [(1, 1), (1, 30), (2, 30)])
