@@ -26,10 +26,10 @@
 // goes on in another CTA a partial result is left, and the CTA that leaves the last one joins them, in order.
 //
 // Measured: 32 x 32 heads of 128, 410 - 1640 rows, one token: 39 us, 3.6 TB/s over all.  A tile takes a warp 2800 clocks (eight query
-// rows, twelve warps: 5.2 TB/s while they run); in front of the first one lie 12 K clocks, six dependent loads and 1500 instructions
-// that run once, and behind the last one 10 K, of which the jump into code that was not fetched yet is 3 K and the join across blocks
-// another 3 K.  So long GQA (five tiles per warp) takes 28.6 us where its bytes take 7.
-// Two more tiles in flight or eleven warps change nothing; sixteen warps leave too few registers.
+// rows, twelve warps: 5.2 TB/s while they run); in front of the first one lie 12 K clocks, six dependent loads and much code that runs
+// once, and behind the last one 10 K: the item's sums 3 K, from there to the first piece 3 K, the join across blocks 3 K.
+// So long GQA (five tiles per warp) takes 28.6 us where its bytes take 7.
+// A third tile in flight or eleven warps do not help; sixteen warps leave too few registers.
 #include <cuda_fp16.h>
 #include <limits.h>
 
