@@ -14,8 +14,11 @@
 // their way into registers.
 //
 // Queries are scaled by a power of two, row by row, so that their largest value lies in [2^10, 2^11): a half holds every bf16
-// value exactly from there down to 2^-24 of it, and 16 times the largest.  A weight times its row's scale is rounded to a half (11 bits), relative to a power
-// of two that follows the largest scale seen as the softmax's reference follows the largest logit.
+// value exactly from there down to 2^-24 of it, and 16 times the largest.  A weight times its row's scale is rounded to a half (11 bits)
+// after multiplication by a factor of the query's own, which follows the largest such product that the query has seen as the softmax's
+// reference follows the largest logit: it comes to 2^8 - 2^14, so that bits are lost below 2^-22 of it and a product below
+// 2^-33 of it is.  (One factor for all queries that followed the scales alone, hidden rows' and faint ones' among them, took 1 us less of
+// 30 with a bias, which raises the references tile by tile, and nothing elsewhere.)
 // (Codes of K as e4m3 bytes, which four zeros and a code are as well, take half of the ANDs, but the compiler makes halves of
 // them before it multiplies: 650 instructions per tile of 32 keys instead of 510.)
 //
@@ -44,7 +47,10 @@ using namespace dev;
 constexpr int kQ4Tile = 32;                              // keys per tile
 constexpr int kCountWord = 16, kMostBlocks = 192;        // of the status area: a byte per block
 constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
-constexpr float kTiny = 0x1p-126f, kHuge = 0x1p126f;     // bounds of the reference of the scales
+// Of a weight times its row's scale, which enters the second product as a half: the largest factor it is held by (times a weight of
+// at most 2^8 still a number), the largest value it may have, and what a query's largest one is brought to when it is above that.
+constexpr float kMostGain = 0x1p119f, kMostProduct = 0x1p14f, kMostProductLog = 14.f;
+constexpr uint32_t kTopProduct = 8;                      // 2^8 to 2^9
 
 struct FewQuery { const uint16_t* q; int64_t sb, sh, st; Divider by_page; };      // by_page: tiles per page
 
@@ -72,6 +78,11 @@ __device__ __forceinline__ uint32_t max_abs2(uint32_t x, uint32_t y) {
     uint32_t r;
     asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x & 0x7fff7fffu), "r"(y & 0x7fff7fffu));
     return r;
+}
+__device__ __forceinline__ float lg2f(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 __device__ __forceinline__ float fmax3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
@@ -328,7 +339,7 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     uint32_t qb[RH][2 * KW][2];
     float acc[RH][MT][4];
     float2 factor[RH], q_sum[RH], m_run[RH], l_run[RH], b_run[RH];               // of query rows 2 qd and 2 qd + 1
-    float v_ref = kTiny, v_inv = 1.f / kTiny;            // power of two that the scales of V are relative to
+    float2 gain[RH], room[RH];                           // what weight times scale is multiplied by; largest logit times scale (base 2) so far
     // (one loop for everything, so that the code stands here once; the first NST rounds only fill the ring)
     for (int n_used = -NST;; ++n_used) {
         const int j = (n_used + NST) % NST;
@@ -359,13 +370,14 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                     if (biased && fabsf(table[m].pos) > kFarToken) atomicOr(a.status, CSP_DEV_BAD_LEN);
                     if (m >= count * G) continue;
                     const float base_sum = c ? b_run[n].y : b_run[n].x, l = c ? l_run[n].y : l_run[n].x, mm = c ? m_run[n].y : m_run[n].x;
+                    const float unit = rcpf(c ? gain[n].y : gain[n].x);
                     const int tok = pl.by_group(m), head = seg.h * G + m - tok * G;
                     const float inv = l == 0.f ? 0.f : 1.f / (n_term(a.n, mm) + l);      // l == 0: nothing was seen
                     uint16_t* const out = a.out + int64_t(seg.b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(seg.x.tok0 + tok) * a.o_st + 4 * gr;
 #pragma unroll
                     for (int t = 0; t < MT; t += 2) {        // dimensions 16 t + 4 gr to 16 t + 4 gr + 3
-                        const float4 o = make_float4(fmaf(acc[n][t][c] * 0x1p24f, v_ref, base_sum), fmaf(acc[n][t][2 + c] * 0x1p20f, v_ref, base_sum),
-                                                     fmaf(acc[n][t + 1][c] * 0x1p24f, v_ref, base_sum), fmaf(acc[n][t + 1][2 + c] * 0x1p20f, v_ref, base_sum));
+                        const float4 o = make_float4(fmaf(acc[n][t][c] * 0x1p24f, unit, base_sum), fmaf(acc[n][t][2 + c] * 0x1p20f, unit, base_sum),
+                                                     fmaf(acc[n][t + 1][c] * 0x1p24f, unit, base_sum), fmaf(acc[n][t + 1][2 + c] * 0x1p20f, unit, base_sum));
                         if (begins && ends)
                             *reinterpret_cast<uint2*>(out + 16 * t) = l == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
                         else
@@ -443,11 +455,11 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
             q_sum[n] = make_float2(__shfl_sync(0xffffffffu, total, 8 * qd), __shfl_sync(0xffffffffu, total, 8 * qd + 4));
             m_run[n] = make_float2(kNeg, kNeg);
             l_run[n] = b_run[n] = make_float2(0.f, 0.f);
+            gain[n] = make_float2(kMostGain, kMostGain);
+            room[n] = make_float2(kNeg, kNeg);
 #pragma unroll
             for (int t = 0; t < MT; ++t) acc[n][t][0] = acc[n][t][1] = acc[n][t][2] = acc[n][t][3] = 0.f;
         }
-        v_ref = kTiny;
-        v_inv = 1.f / kTiny;
         __syncwarp();
         if (item_of[0] != item) { --n_used; continue; }  // (an item without any tile for this warp)
         }
@@ -550,39 +562,59 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
                         }
                     }
             }
-            // ---- references: of the softmax per query row, of the scales per warp; raised when exceeded by 2^8 and 2^4
-            const float v_top = fmaxf(fmax3(lo_bf16(v_pair[0][0]), lo_bf16(v_pair[0][1]), lo_bf16(v_pair[1][0])), lo_bf16(v_pair[1][1]));
+            // ---- references: of the softmax, raised when exceeded by 2^8, and the products' factors, lowered when a product may exceed
+            // kMostProduct (what it may be at most: the largest weight times the largest scale of this lane's keys)
             float2 mx[RH];
-            float over = v_top * (v_inv * (kLazy / 16.f));
+            const float v_top = lg2f(fmaxf(fmax3(lo_bf16(v_pair[0][0]), lo_bf16(v_pair[0][1]), lo_bf16(v_pair[1][0])), lo_bf16(v_pair[1][1])));
+            float over = -INFINITY;
 #pragma unroll
             for (int n = 0; n < RH; ++n) {
                 mx[n].x = fmaxf(fmax3(x[0][n][0].x, x[0][n][1].x, x[1][n][0].x), x[1][n][1].x);
                 mx[n].y = fmaxf(fmax3(x[0][n][0].y, x[0][n][1].y, x[1][n][0].y), x[1][n][1].y);
-                over = fmax3(over, mx[n].x - m_run[n].x, mx[n].y - m_run[n].y);
+                over = fmax3(over, mx[n].x - fminf(m_run[n].x + kLazy, room[n].x - v_top), mx[n].y - fminf(m_run[n].y + kLazy, room[n].y - v_top));
             }
-            const bool raise = over > kLazy;
-            if (__any_sync(0xffffffffu, raise)) {
-                // (the same power of two in all lanes; scales are not negative, so their bits are in order)
-                const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(fminf(fmaxf(v_top, v_ref), kHuge))) & 0x7f800000u;
-                v_inv = __uint_as_float((254u << 23) - top);
-                const float shrink = v_ref * v_inv;
-                v_ref = __uint_as_float(top);
+            if (__any_sync(0xffffffffu, over > 0.f)) {
 #pragma unroll
                 for (int n = 0; n < RH; ++n) {
-                    float2 y = mx[n], alpha = make_float2(1.f, 1.f);
+                    float2 y = mx[n], top = make_float2(0.f, 0.f), alpha, keep;
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) {
                         y.x = fmaxf(y.x, __shfl_xor_sync(0xffffffffu, y.x, d));
                         y.y = fmaxf(y.y, __shfl_xor_sync(0xffffffffu, y.y, d));
                     }
-                    if (y.x > m_run[n].x + kLazy) { alpha.x = ex2f(m_run[n].x - y.x); m_run[n].x = y.x; }
-                    if (y.y > m_run[n].y + kLazy) { alpha.y = ex2f(m_run[n].y - y.y); m_run[n].y = y.y; }
+                    const float2 m = make_float2(y.x > m_run[n].x + kLazy ? y.x : m_run[n].x, y.y > m_run[n].y + kLazy ? y.y : m_run[n].y);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {        // (2^-16: a number, whatever the scale)
+                            const float sv = lo_bf16(v_pair[k][i]);
+                            top.x = fmaxf(top.x, ex2f(x[k][n][i].x - m.x) * 0x1p-16f * sv);
+                            top.y = fmaxf(top.y, ex2f(x[k][n][i].y - m.y) * 0x1p-16f * sv);
+                        }
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) {
+                        top.x = fmaxf(top.x, __shfl_xor_sync(0xffffffffu, top.x, d));
+                        top.y = fmaxf(top.y, __shfl_xor_sync(0xffffffffu, top.y, d));
+                    }
+                    // With the softmax's reference raised, the products so far stay as they are and those to come are held by as much
+                    // more; where that is too much those so far are made smaller.
+                    auto settle = [](float& m_old, float& g, float& r, float m_new, float w, float& alpha, float& keep) {
+                        alpha = ex2f(m_old - m_new);
+                        const float most = w * kMostGain > kMostProduct * 0x1p-16f
+                            ? __uint_as_float(((254u - 16u + kTopProduct) << 23) - (__float_as_uint(fminf(w, 0x1p116f)) & 0x7f800000u)) : kMostGain;
+                        const float more = g * ex2f(m_new - m_old);
+                        const bool fits = more <= kMostGain && !(w * more > kMostProduct * 0x1p-16f);
+                        keep = fits ? 1.f : alpha * most * rcpf(g);
+                        g = fits ? more : most;
+                        m_old = m_new;
+                        r = m_new + (kMostProductLog - lg2f(g));
+                    };
+                    settle(m_run[n].x, gain[n].x, room[n].x, m.x, top.x, alpha.x, keep.x);
+                    settle(m_run[n].y, gain[n].y, room[n].y, m.y, top.y, alpha.y, keep.y);
                     l_run[n] = __fmul2_rn(l_run[n], alpha);
                     b_run[n] = __fmul2_rn(b_run[n], alpha);
-                    alpha.x *= shrink;
-                    alpha.y *= shrink;
 #pragma unroll
-                    for (int t = 0; t < MT; ++t) { acc[n][t][0] *= alpha.x; acc[n][t][1] *= alpha.y; acc[n][t][2] *= alpha.x; acc[n][t][3] *= alpha.y; }
+                    for (int t = 0; t < MT; ++t) { acc[n][t][0] *= keep.x; acc[n][t][1] *= keep.y; acc[n][t][2] *= keep.x; acc[n][t][3] *= keep.y; }
                 }
             }
             // ---- weights
@@ -591,14 +623,15 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const float sv = lo_bf16(v_pair[k][i]) * v_inv, bv = hi_bf16(v_pair[k][i]);
+                    const float sv = lo_bf16(v_pair[k][i]), bv = hi_bf16(v_pair[k][i]);
 #pragma unroll
                     for (int n = 0; n < RH; ++n) {
                         const float2 y = __fadd2_rn(x[k][n][i], make_float2(-m_run[n].x, -m_run[n].y));
-                        float2 p = make_float2(ex2f(y.x), ex2f(y.y));
+                        const float2 p = make_float2(ex2f(y.x), ex2f(y.y));
                         l_run[n] = __fadd2_rn(l_run[n], p);
-                        b_run[n] = make_float2(fmaf(p.x, bv, b_run[n].x), fmaf(p.y, bv, b_run[n].y));
-                        pb[k][n][i] = transpose8(pack_f16(p.x * sv, p.y * sv));
+                        b_run[n] = __ffma2_rn(p, make_float2(bv, bv), b_run[n]);
+                        const float2 w = __fmul2_rn(__fmul2_rn(p, gain[n]), make_float2(sv, sv));
+                        pb[k][n][i] = transpose8(pack_f16(w.x, w.y));
                     }
                 }
             // ---- O^T += V^T P^T: pieces of four codes (dimensions 4 gr to 4 gr + 3 of 32), two keys each
