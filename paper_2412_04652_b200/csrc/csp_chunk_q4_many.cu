@@ -290,10 +290,10 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 ks_next = *reinterpret_cast<const uint4*>(cache.ks + page * cache.ks_sb + h * cache.ks_sh + at);
                 vs_next = *reinterpret_cast<const uint4*>(cache.vs + page * cache.vs_sb + h * cache.vs_sh + at);
             };
-            auto fetch_meta = [&](int tile) {            // documents and positions of one tile's keys, a tile ahead of their use
+            auto fetch_meta = [&](int tile) {            // documents and positions of keys 4 lane to 4 lane + 3, a tile ahead of their use
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int t = tile * kTileKeys + lane + 32 * j;
+                    const int t = tile * kTileKeys + 4 * lane + j;
                     if (t >= x.rows) { d_next[j] = 0; p_next[j] = 0; continue; }
                     if (kDoc) d_next[j] = docs[t];
                     if (kBias) p_next[j] = poss ? poss[t] : t;
@@ -318,29 +318,31 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 for (int j = 0; j < 4; ++j) { d_now[j] = d_next[j]; p_now[j] = p_next[j]; }
                 if (kMeta && tile + 1 < tile1) fetch_meta(tile + 1);
                 int act = 0;
+                bool seen[4] = {false, false, false, false};     // keys that the tokens may see: not those behind all of them, nor other documents'
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     if (g == 1 && !big) continue;
                     const int end = big && g == 0 ? x.kv_end[0] : x.kv_end[1];
-                    bool any = t0 < end;
-                    if (kDoc) {                          // a tile without any of the tokens' documents is skipped
-                        bool hit = false;
+                    bool hit = false;                    // (a tile without any of the tokens' documents is skipped)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) hit |= t0 + lane + 32 * j < end && d_now[j] >= doc_lo[g] && d_now[j] <= doc_hi[g];
-                        any = __any_sync(0xffffffffu, hit);
+                    for (int j = 0; j < 4; ++j) {
+                        const bool here = t0 + 4 * lane + j < end && (!kDoc || (d_now[j] >= doc_lo[g] && d_now[j] <= doc_hi[g]));
+                        hit |= here;
+                        seen[j] |= here;
                     }
-                    act |= any ? 1 << g : 0;
+                    act |= (kDoc ? __any_sync(0xffffffffu, hit) : t0 < end) ? 1 << g : 0;
                 }
                 if (act == 0) continue;
                 if (!big) act = 1 << (n_done & 1);       // the groups take turns
-                // scales and bases in fp32, zeros behind the last row (what stands there may be no number)
+                // Scales and bases in fp32, zeros behind the last row (what stands there may be no number).  Of V zeros where nobody sees the
+                // row as well: what it holds must not be what the others are relative to.
                 const uint32_t kp[4] = {ks_now.x, ks_now.y, ks_now.z, ks_now.w}, vp[4] = {vs_now.x, vs_now.y, vs_now.z, vs_now.w};
                 float sk[4], bk[4], sv[4], bv[4], v_top = 0.f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const bool in = t0 + 4 * lane + j < x.rows;
                     sk[j] = in ? lo_bf16(kp[j]) : 0.f; bk[j] = in ? hi_bf16(kp[j]) : 0.f;
-                    sv[j] = in ? lo_bf16(vp[j]) : 0.f; bv[j] = in ? hi_bf16(vp[j]) : 0.f;
+                    sv[j] = seen[j] ? lo_bf16(vp[j]) : 0.f; bv[j] = seen[j] ? hi_bf16(vp[j]) : 0.f;
                     v_top = fmaxf(v_top, fmaxf(fabsf(bv[j]), fabsf(fmaf(15.f, sv[j], bv[j]))));
                 }
                 // (magnitudes: their bits are in order)
@@ -371,11 +373,8 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 if (kMeta) {
                     float* const mp = reinterpret_cast<float*>(base_ptr + sp.meta + e * Shape::kMetaBytes + Shape::kPositions);
                     int32_t* const md = reinterpret_cast<int32_t*>(base_ptr + sp.meta + e * Shape::kMetaBytes + Shape::kDocuments);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (kBias) mp[lane + 32 * j] = float(p_now[j] - pos_ref);
-                        if (kDoc) md[lane + 32 * j] = d_now[j];
-                    }
+                    if (kBias) reinterpret_cast<float4*>(mp)[lane] = make_float4(float(p_now[0] - pos_ref), float(p_now[1] - pos_ref), float(p_now[2] - pos_ref), float(p_now[3] - pos_ref));
+                    if (kDoc) reinterpret_cast<int4*>(md)[lane] = make_int4(d_now[0], d_now[1], d_now[2], d_now[3]);
                 }
                 announce(e);
                 // Q goes behind the first two tiles if its slot is still in use

@@ -12,6 +12,8 @@ pytestmark = pytest.mark.gpu
 WIDE = 1 << 18                                           # a capacity for which items of sixteen rows are taken where rows allow it
 # query heads per KV head, tokens, capacity or None, head_dim: one item of eight query rows, several, of sixteen, several ...
 FEW = [(1, 1, None, 128), (2, 3, None, 64), (4, 5, None, 128), (3, 5, WIDE, 128), (1, 40, 2 * WIDE, 64), (8, 6, 2 * WIDE, 128)]
+# ... and of row tiles of 128: one item, several, of 7 heads
+MANY = [(1, 60, None, 64), (4, 13, None, 128), (2, 200, None, 128), (7, 45, None, 64)]
 
 
 @pytest.fixture(scope="module")
@@ -116,14 +118,14 @@ def _queries(B, Hq, T, d, seed, gain=1.0):
     return (torch.randn(B, Hq, T, d, generator=torch.Generator().manual_seed(seed)) * gain).to(torch.bfloat16)
 
 
-@pytest.mark.parametrize("G,T,capacity,d", FEW)
+@pytest.mark.parametrize("G,T,capacity,d", FEW + MANY)
 def test_ordinary_values(csp, G, T, capacity, d):
     rows = torch.tensor([[700, 433], [T, T + 130]], dtype=torch.int32)
     _attend(csp, _queries(2, 2 * G, T, d, 1, 1.5), _cache((2, 2, 700, d), 2), rows, G, T, capacity, d)
 
 
 @pytest.mark.parametrize("power", [26, 100])
-@pytest.mark.parametrize("G,T,capacity,d", FEW)
+@pytest.mark.parametrize("G,T,capacity,d", FEW + MANY)
 def test_large_values_of_other_documents(csp, G, T, capacity, d, power):
     """Every third row is another document's, in the same tiles as the visible ones, with V 2^26 and 2^100 times as large."""
     L = 500
@@ -144,6 +146,19 @@ def test_large_values_behind_a_token(csp, G, T, capacity, d, power):
     for h in range(2):
         dense[1][1][0, h, int(rows[0, h]) - 1] *= 2.0 ** power
     _attend(csp, _queries(1, 2 * G, T, d, 6), dense, rows, G, T, capacity, d)
+
+
+@pytest.mark.parametrize("power", [26, 100])
+@pytest.mark.parametrize("G,T,d", [(1, 300, 64), (2, 300, 128), (5, 90, 64)])
+def test_large_values_behind_an_item(csp, G, T, d, power):
+    """Row tiles: the first items' tokens do not see the last rows, some of which lie in tiles that they do see."""
+    item = _item(G, T)
+    first = T // item * item if T % item else T - item   # tokens of the items in front of the last one
+    rows = torch.tensor([[T + 20, T]], dtype=torch.int32)
+    dense = _cache((1, 2, T + 20, d), 5)
+    for h in range(2):
+        dense[1][1][0, h, int(rows[0, h]) - T + first:] *= 2.0 ** power
+    _attend(csp, _queries(1, 2 * G, T, d, 6), dense, rows, G, T, None, d)
 
 
 @pytest.mark.parametrize("G,T,capacity,d", FEW)
