@@ -86,6 +86,11 @@ __device__ __forceinline__ uint4 unpack_values(uint32_t x, uint32_t scale24, uin
 // Values of V are held as value / reference x 2^-7, the reference the power of two that is at most the largest value so far: below
 // 2^-6, so that scale 2^24 is still a half (15 scale <= 2^-5); a value below 2^-7 of the largest has its error of 2^-18 of it.
 constexpr float kValueUnit = 0x1p-7f;
+// A weight is a half as well: the reference is put this far (powers of two) below a row's largest logit, so that a weight may be up to
+// 2^(7 + kLazy) and keeps its eleven bits down to 2^-21 of the largest; one below 2^-32 of it is lost.  A weight times kValueUnit
+// is then what it is, and products need only the values' reference.
+constexpr float kHeadroom = 7.f;
+static_assert(kValueUnit == 0x1p-7f && kHeadroom == 7.f, "these cancel");
 
 struct ManySmem { uint32_t q, raw, meta, entries, pair, join, rows, bars, misc, total; };
 template <int NH, bool kMeta>
@@ -763,9 +768,9 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                     const float mx_other = other_half(mx);
                     mx = fmax3_nan(mx, mx_other, mx_other);
                     // (a NaN among the logits raises the reference to NaN, and the whole row with it)
-                    const bool raise = valid && !(mx <= m_run + (started ? kLazy : 0.f));
+                    const bool raise = valid && !(mx <= m_run + (started ? kHeadroom + kLazy : kHeadroom));
                     if (__any_sync(0xffffffffu, raise) || v_ref != v_run) {
-                        const float m_new = raise ? mx : m_run, alpha = ex2f(m_run - m_new), shrink = alpha * (v_run / v_ref);
+                        const float m_new = raise ? mx - kHeadroom : m_run, alpha = ex2f(m_run - m_new), shrink = alpha * (v_run / v_ref);
                         v_run = v_ref;
                         if (started) {
                             // O holds products with weights relative to the old reference; each half rescales half of the row
@@ -823,13 +828,13 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
             if (kBias && fabsf(q_pos) > kFarToken) atomicOr(a.status, CSP_DEV_BAD_LEN);
             if (started) warp_wait(pv_done + 8 * g, (n_mine - 1u) & 1u, abort_flag);
             tc_fence_after();
-            float l_all = l_run + other_half(l_run);
-            float m_all = m_run, w0 = v_run * (1.f / kValueUnit), w1 = 0.f;       // w0, w1: what the two groups' products are multiplied by
+            float l_all = (l_run + other_half(l_run)) * kValueUnit;
+            float m_all = m_run + kHeadroom, w0 = v_run, w1 = 0.f;                // w0, w1: what the two groups' products are multiplied by
             bool has0 = started, has1 = false;
             if (!big) {
                 // both groups hold part of the same rows: exchange reference and sum, then each half row writes a quarter
                 if (half == 0) {
-                    join_buf[g * 128 + m] = m_run;
+                    join_buf[g * 128 + m] = m_all;
                     join_buf[256 + g * 128 + m] = started ? l_all : __uint_as_float(kUnset);     // the group had no tile: its O is not set
                     join_buf[512 + g * 128 + m] = v_run;
                 }
@@ -841,8 +846,8 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 w0 = ex2f(m0 - m_all);
                 w1 = ex2f(m1 - m_all);
                 l_all = (has0 ? l0 * w0 : 0.f) + (has1 ? l1 * w1 : 0.f);
-                w0 *= join_buf[512 + m] * (1.f / kValueUnit);
-                w1 *= join_buf[640 + m] * (1.f / kValueUnit);
+                w0 *= join_buf[512 + m];
+                w1 *= join_buf[640 + m];
             }
             if (live) {
                 const int local = m / G, head = h * G + m - local * G, tok = tok0 + (big ? g * pl.tok_tile : 0) + local;

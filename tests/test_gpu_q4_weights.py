@@ -36,7 +36,8 @@ def definition(q, dense, rows, documents=None, prefix=0, item=None):
       few rows    + 15 L 2^-33 max w s                    a query's products w s are held by a factor that brings the largest to 2^8
                                                           at least; below 2^-14 they are off by 2^-25
       row tiles   + L 2^-32 max w max v                   weights likewise, the largest 2^7
-                  + 2^-17 max v                           and values, base and sum each 2^-18 of the largest that the item sees
+                  + 2^-17 max v sum w [|v| or |b| < 2^-6 max v]    and values, base and sum each 2^-18 of the largest that the item
+                                                          sees where they are small beside it
                   + 2^-126"""
     (kc, ks), (vc, vs) = [tuple(x.cuda() for x in pair) for pair in dense]
     B, Hq, T, d = q.shape
@@ -63,8 +64,14 @@ def definition(q, dense, rows, documents=None, prefix=0, item=None):
                           2.0 ** -25 * x.abs().amax(1) * (K - kb).sum(1).max()) + 2.0 ** -21 + 2.0 ** -23 * torch.where(see, o.abs(), 0.0).amax(1)
                 w = torch.exp(o - torch.logaddexp(torch.logsumexp(o, 1), torch.zeros(1, dtype=torch.float64, device="cuda"))[:, None])
                 want[b, hq] = w @ V
-                small = 15 * L * 2.0 ** -33 * (w * s).amax(1) if not item else (L * 2.0 ** -32 * w.amax(1) + 2.0 ** -17) * top
-                tol[b, hq] = 2.0 ** -8 * (1 + 2.0 ** -8) * want[b, hq].abs() + ((2 if item else 1) * 2.0 ** -11 + 4 * e + 2.0 ** -23 * (L / 8 + 16))[:, None] * (w @ mv) + small[:, None] + 2.0 ** -126
+                small = (15 * L * 2.0 ** -33 * (w * s).amax(1))[:, None]
+                if item:
+                    few = (w.amax(1) * L * 2.0 ** -32 * top)[:, None].expand(T, d).clone()
+                    for i in range(0, T, item):
+                        tiny = (mv > 0) & ((V.abs() < 2.0 ** -6 * top[i]) | (vb.abs() < 2.0 ** -6 * top[i]))
+                        few[i:i + item] += 2.0 ** -17 * top[i] * (w[i:i + item] @ tiny.double())
+                    small = few
+                tol[b, hq] = 2.0 ** -8 * (1 + 2.0 ** -8) * want[b, hq].abs() + ((2 if item else 1) * 2.0 ** -11 + 4 * e + 2.0 ** -23 * (L / 8 + 16))[:, None] * (w @ mv) + small + 2.0 ** -126
     return want, tol
 
 
@@ -184,14 +191,14 @@ def _faint(L, d, seed, nats):
     return out
 
 
-@pytest.mark.parametrize("G,T,capacity,d", FEW)
+@pytest.mark.parametrize("G,T,capacity,d", FEW + MANY)
 def test_one_row_weighs_more_than_all_others(csp, G, T, capacity, d):
     """Weights of some 2^-26 beside one of one, whose values are zero: the others' are the result."""
     rows = torch.tensor([[2000, 1999]], dtype=torch.int32)
     _attend(csp, 1 + _queries(1, 2 * G, T, d, 10, 0.05), _faint(2000, d, 9, 18.0), rows, G, T, capacity, d)
 
 
-@pytest.mark.parametrize("G,T,capacity,d", [FEW[0], FEW[3]])
+@pytest.mark.parametrize("G,T,capacity,d", [FEW[0], FEW[3], MANY[0]])
 def test_a_million_faint_rows(csp, G, T, capacity, d):
     rows = torch.tensor([[1 << 20, 900000]], dtype=torch.int32)
     _attend(csp, 1 + _queries(1, 2 * G, T, d, 10, 0.05), _faint(1 << 20, d, 9, 17.7), rows, G, T, capacity, d, page_rows=1024)
