@@ -46,7 +46,7 @@ constexpr int kEntryWords = 12;
 constexpr int kRawTiles = 2;                             // tiles of codes under way
 constexpr uint32_t kUnset = 0xBF800000u;                 // -1.0f: no sum of weights has these bits
 constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;
-constexpr float kTiny = 0x1p-110f, kHuge = 0x1p110f;     // bounds of the reference of the values
+constexpr float kTiny = 0x1p-126f, kHuge = 0x1p126f;     // bounds of the reference of the values
 
 // What an entry says.  The first two words are all that a tile needs at once: flags and the tile's first key.
 enum EntryWord { kFlags, kTile0, kSeq, kHead, kTok0, kRows, kNew, kPart, kPrefix, kPage, kPageRow, kScaleRef };
@@ -829,7 +829,7 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
             if (started) warp_wait(pv_done + 8 * g, (n_mine - 1u) & 1u, abort_flag);
             tc_fence_after();
             float l_all = (l_run + other_half(l_run)) * kValueUnit;
-            float m_all = m_run + kHeadroom, w0 = v_run, w1 = 0.f;                // w0, w1: what the two groups' products are multiplied by
+            float m_all = m_run + kHeadroom, w0 = 1.f, w1 = 0.f, v0 = v_run, v1 = 0.f;        // what the two groups' products are multiplied by
             bool has0 = started, has1 = false;
             if (!big) {
                 // both groups hold part of the same rows: exchange reference and sum, then each half row writes a quarter
@@ -846,14 +846,16 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
                 w0 = ex2f(m0 - m_all);
                 w1 = ex2f(m1 - m_all);
                 l_all = (has0 ? l0 * w0 : 0.f) + (has1 ? l1 * w1 : 0.f);
-                w0 *= join_buf[512 + m];
-                w1 *= join_buf[640 + m];
+                v0 = join_buf[512 + m];
+                v1 = join_buf[640 + m];
             }
             if (live) {
                 const int local = m / G, head = h * G + m - local * G, tok = tok0 + (big ? g * pl.tok_tile : 0) + local;
                 const bool final = part_slot < 0;
                 const float denom = n_term(a.n, m_all) + l_all;
                 const float inv = final ? 1.f / denom : 1.f;
+                w0 *= inv;                               // (apart from the references, so that large values' sums are numbers)
+                w1 *= inv;
                 const uint32_t o0 = (big ? tmem_o[g] : tmem_o[0]) + lane_base, o1 = tmem_o[1] + lane_base;
                 uint16_t* const out = a.out + int64_t(b) * a.o_sb + int64_t(head) * a.o_sh + int64_t(tok) * a.o_st;
                 const int row = (tok - tok0) * G + (head - h * G);
@@ -871,8 +873,8 @@ chunk_q4_many_kernel(const __grid_constant__ CUtensorMap tmap_q, const Q4Args ca
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {       // dimension c + j
                         const int d = j & 7, at = (j & 8) + (d < 4 ? 2 * d : 2 * d - 7);
-                        const float y0 = has0 ? __uint_as_float(x0[at]) * w0 : 0.f, y1 = has1 ? __uint_as_float(x1[at]) * w1 : 0.f;
-                        o[j] = zero ? 0.f : (y0 + y1) * inv;
+                        const float y0 = has0 ? __uint_as_float(x0[at]) * w0 * v0 : 0.f, y1 = has1 ? __uint_as_float(x1[at]) * w1 * v1 : 0.f;
+                        o[j] = zero ? 0.f : y0 + y1;
                     }
                     if (!valid) continue;
                     if (final) {

@@ -131,6 +131,15 @@ def test_ordinary_values(csp, G, T, capacity, d):
     _attend(csp, _queries(2, 2 * G, T, d, 1, 1.5), _cache((2, 2, 700, d), 2), rows, G, T, capacity, d)
 
 
+@pytest.mark.parametrize("power", [116, -116])
+@pytest.mark.parametrize("G,T,capacity,d", FEW + MANY)
+def test_values_far_from_one(csp, G, T, capacity, d, power):
+    rows = torch.tensor([[500, 222]], dtype=torch.int32)
+    dense = _cache((1, 2, 500, d), 12)
+    dense[1][1].mul_(2.0 ** power)
+    _attend(csp, _queries(1, 2 * G, T, d, 13), dense, rows, G, T, capacity, d)
+
+
 @pytest.mark.parametrize("power", [26, 100])
 @pytest.mark.parametrize("G,T,capacity,d", FEW + MANY)
 def test_large_values_of_other_documents(csp, G, T, capacity, d, power):
