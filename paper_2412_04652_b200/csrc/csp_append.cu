@@ -143,12 +143,28 @@ __device__ __forceinline__ uint32_t divide(uint32_t t, uint32_t n, uint32_t m, u
     return q;
 }
 
+// (hi - lo) / 15 as a number that bf16 rounds like the exact quotient.  A product with fl(1/15) is off by less than two units in the last
+// place: enough to be on the other side of the middle between two bf16 numbers.  Only next to one is the remainder looked at: 15 times the
+// middle has thirteen bits, so that hi - lo less it, and what rounding hi - lo has lost, are exact in their signs.
+__device__ __forceinline__ float fifteenth(float lo, float hi) {
+    const float spread = __fsub_rn(hi, lo);
+    float q = __fmul_rn(spread, 1.f / 15.f);
+    const uint32_t bits = __float_as_uint(q);
+    if (((bits + 0x8004u) & 0xffffu) < 8u) {             // up to four units from the middle
+        const uint32_t middle = (bits & 0xffff0000u) | 0x8000u;
+        const float back = __fsub_rn(spread, hi);        // -lo, as far as it is in `spread`
+        const float lost = __fsub_rn(__fsub_rn(hi, __fsub_rn(spread, back)), __fadd_rn(lo, back));
+        const float rest = __fadd_rn(__fmaf_rn(-15.f, __uint_as_float(middle), spread), lost);
+        q = __uint_as_float(rest > 0.f ? middle + 1u : rest < 0.f ? middle - 1u : middle);
+    }
+    return q;
+}
 // A row of bf16 values in 4 bits: the lane's two words, and what the row's first lane writes beside them.
 template <int kLanes>
 __device__ __forceinline__ uint32_t quantise(const Eight<false>* z, uint32_t lanes, uint32_t& w0, uint32_t& w1) {
     float lo, hi, f[16];
     row_range<kLanes>(z[0], z[1], lanes, lo, hi);
-    uint32_t pair = pack_bf16(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), lo);
+    uint32_t pair = pack_bf16(fifteenth(lo, hi), lo);
     float scale = bf16_lo(pair);
     if (scale < kSmallest) { scale = 0.f; pair &= 0xffff0000u; }
     if (!(scale < INFINITY)) pair |= 0x7fffu;            // the whole row is no number
