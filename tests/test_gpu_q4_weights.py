@@ -211,3 +211,34 @@ def test_one_row_weighs_more_than_all_others(csp, G, T, capacity, d):
 def test_a_million_faint_rows(csp, G, T, capacity, d):
     rows = torch.tensor([[1 << 20, 900000]], dtype=torch.int32)
     _attend(csp, 1 + _queries(1, 2 * G, T, d, 10, 0.05), _faint(1 << 20, d, 9, 17.7), rows, G, T, capacity, d, page_rows=1024)
+
+
+@pytest.mark.parametrize("G,T,capacity,d", [(1, 1, None, 64), (2, 3, None, 64), (2, 8, 2 * WIDE, 64), (1, 1, None, 128)])
+def test_more_items_than_a_block_looks_at_at_once(csp, G, T, capacity, d):
+    """Some five thousand short caches, more than 32 to a block, some of them without rows or with fewer than there are tokens."""
+    B, H = 165, 32
+    gen = torch.Generator().manual_seed(3)
+    rows = torch.randint(T, 120, (B, H), generator=gen, dtype=torch.int32)
+    rows[::7, 3] = 0
+    rows[::5, 4:9] = T
+    cap = 128
+    pools, dense = [], []
+    for i in range(2):
+        codes, scales = random_rows((B, H, cap, d), gen)
+        dense.append((codes, scales))
+        pools.append(csp.Q4Cache(codes.cuda(), scales.cuda()))
+    wide = max(capacity or cap, cap)
+    table = torch.full((B, -(-wide // 128)), 10 ** 6, dtype=torch.int32, device="cuda")
+    table[:, 0] = torch.arange(B, device="cuda")         # (a cache that is not paged: a page per sequence)
+    p = csp.Params(B, H * G, H, d, 1, 0, wide, wide)
+    q, ws = _queries(B, H * G, T, d, 4), csp.new_chunk_q4_workspace(p, T)
+    out = torch.full((B, H * G, T, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    csp.chunk_attn_q4_paged(p, q.cuda(), *pools, table, rows.cuda(), out, ws)
+    assert csp.device_status(ws) == csp.DEV_BAD_LEN      # (rows without tokens: more tokens than rows)
+    empty = (rows == 0).repeat_interleave(G, 1).cuda()
+    assert (out[empty] == 0).all() and torch.isfinite(out).all() and not (out == 7.0).all(-1).any()
+    for b in range(0, B, 8):
+        heads = [h for h in range(H) if rows[b, h] > 0]
+        of_q = [h * G + g for h in heads for g in range(G)]
+        want, tol = definition(q[b:b + 1, of_q], [(c[b:b + 1, heads], s[b:b + 1, heads]) for c, s in dense], rows[b:b + 1, heads])
+        _holds(out[b:b + 1, of_q], want, tol, f"sequence {b}")
