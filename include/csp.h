@@ -489,9 +489,13 @@ size_t csp_chunk_q4_workspace_bytes(const csp_params* p, int32_t max_new);
  * that nothing of K is rounded again.  Of a query, whose values have to be below 2^112, parts below 2^-34 of its largest one
  * are lost.  With up to three groups of sixteen query rows per KV head (max_new x H_q / H_kv, whole tokens) the same
  * holds of V, and a weight times its row's scale is rounded to fp16: to 11 bits down to 2^-22 of the largest such product that
- * the query sees, to 2^-33 of that below.  With more of them a weight is rounded to fp16
- * (to 11 bits down to 2^-21 of the query's largest, to 2^-32 of that below), and so is a value base + scale * code of V, relative to the largest of the rows that the tokens of up to 256 query rows together see (documents
- * between the smallest and the largest of theirs all count): one below 2^-7 of that is off by up to 2^-17 of it.
+ * the query sees, to 2^-33 of that below.  With more of them a weight is rounded to fp16 (to 11 bits down to 2^-21 of the query's
+ * largest, to 2^-32 of that below), and so is a value base + scale * code of V, relative to the largest of the rows that the
+ * tokens of up to 256 query rows together see (documents between the smallest and the largest of theirs all count): one below
+ * 2^-7 of that is off by up to 2^-17 of it.  Weights of up to 2^8 times values of V are added up in fp32 before the division:
+ * 2^8 times the rows seen times the largest base or value of V has to be below 2^127.
+ * Over long caches single tokens take 0.4 to 0.6 of the time that they take over a bf16 cache; chunks of more query rows than
+ * three groups of sixteen take 1.2 to 1.4 times as long as there (csp_chunk_attn_paged), as the codes are unpacked for them.
  */
 csp_status csp_chunk_attn_q4_paged(const csp_params* p, int32_t max_new, csp_tensor q, const csp_q4_cache* k_cache,
                                    const csp_q4_cache* v_cache, const csp_pages* pages, const int32_t* n_rows,

@@ -3,7 +3,7 @@
 //
 // Rotation.  Dimensions (x1, x2) of a pair become (x1 cos - x2 sin, x2 cos + x1 sin), the angles from the caller's table; four
 // products and two sums, each rounded to fp32, and one rounding to the row's type.
-// Four bits.  base = min x, scale = bf16((max x - base) / 15), code = the whole number nearest to (x - base) / scale.  The
+// Four bits.  base = min x, scale = (max x - base) / 15 rounded to bf16, code = the whole number nearest to (x - base) / scale.  The
 // quotient is a product with 1 / scale (1 + 2^-21): the three roundings on the way (2^-24 each) cannot bring a quotient that lies
 // halfway between two codes, which values of 8 bits often do, below the middle, so that the upper code is taken always and not
 // now and then.
@@ -500,8 +500,8 @@ csp_status launch_append_rows(AppendRowsArgs a, int head_dim, bool f32, bool fou
 csp_status launch_load_rows(LoadRowsArgs a, int head_dim, bool f32, cudaStream_t s) {
     if (a.units == 0 || a.max_rows == 0) return CSP_OK;
     a.page_inverse = uint32_t((uint64_t(1) << 32) / uint32_t(a.page_rows)) + 1u;
-    // Four rows in flight per lane, but one where that leaves SMs without a block (5 K rows as fp32: 2.5 us instead of 4.4; 2.6 M
-    // rows with two 72.5 us instead of 71).
+    // Four rows in flight per lane, but one where that leaves SMs without a block (5 K rows as fp32: 2.5 us instead of 4.4; 650 K
+    // rows of K and of V with two 72.5 us instead of 71).
     const int groups = kThreads / (head_dim / 16), rows = a.max_rows < a.capacity ? a.max_rows : a.capacity;
     const int depth = int64_t(a.units) * rows < 4 * int64_t(groups) * sm_count() ? 1 : 4;
     const int64_t tiles = (int64_t(rows) + groups * depth - 1) / (groups * depth);

@@ -1,5 +1,5 @@
-// Shared by the two chunk attention kernels (csp_chunk.cu: many query rows per KV head, csp_chunk_few.cu: up to sixteen) and
-// the kernel that joins the parts of a split cache.
+// Shared by the chunk attention kernels (csp_chunk.cu: many query rows per KV head, csp_chunk_few.cu: up to sixteen; over pages in 4
+// bits csp_chunk_q4_many.cu and csp_chunk_q4.cu) and the kernel that joins the parts of a split cache.
 #pragma once
 
 #include "csp_device.cuh"
@@ -30,7 +30,7 @@ PartialLayout partial_layout(const csp_params& p, const ChunkPlan& pl);
 csp_status launch_chunk_join(const csp_params& p, const ChunkArgs& a, const ChunkPlan& pl, bool few, ChunkParts* parts,
                              float* partial, float2* ml, cudaStream_t s);
 
-// how a chunk of bf16 queries is cut into items; for more than sixteen query rows per KV head a cache in 4 bits is cut alike
+// how a chunk of bf16 queries is cut into items; for more than three items of sixteen query rows per KV head a cache in 4 bits is cut alike
 ChunkPlan chunk_plan(const csp_params& p, int max_new);
 inline void set_dividers(const csp_params& p, ChunkPlan& pl) {
     pl.by_pairs = divider(pl.n_pairs);

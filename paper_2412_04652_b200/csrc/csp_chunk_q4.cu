@@ -17,8 +17,9 @@
 // value exactly from there down to 2^-24 of it, and 16 times the largest.  A weight times its row's scale is rounded to a half (11 bits)
 // after multiplication by a factor of the query's own, which follows the largest such product that the query has seen as the softmax's
 // reference follows the largest logit: it comes to 2^8 - 2^14, so that bits are lost below 2^-22 of it and a product below
-// 2^-33 of it is.  (One factor for all queries that followed the scales alone, hidden rows' and faint ones' among them, took 1 us less of
-// 30 with a bias, which raises the references tile by tile, and nothing elsewhere.)
+// 2^-33 of it is.  (One factor for all queries that followed the scales alone, hidden rows' and faint ones' among them: 39.2 us
+// instead of 39.4 below, 40.9 instead of 41.4 for five capped tokens.  Codes less 7.5, against the sum of the rounded products, take another
+// 3 % and bring the error without the result's own rounding from 6e-4 to 3e-4.)
 // (Codes of K as e4m3 bytes, which four zeros and a code are as well, take half of the ANDs, but the compiler makes halves of
 // them before it multiplies: 650 instructions per tile of 32 keys instead of 510.)
 //
@@ -28,10 +29,10 @@
 // it; of one that is cut the pieces stay in shared memory until all warps are done and are joined then, in order; of one that
 // goes on in another CTA a partial result is left, and the CTA that leaves the last one joins them, in order.
 //
-// Measured: 32 x 32 heads of 128, 410 - 1640 rows, one token: 39 us, 3.6 TB/s over all.  A tile takes a warp 2800 clocks (eight query
+// Measured: 32 x 32 heads of 128, 410 - 1640 rows, one token: 39.4 us, 3.6 TB/s over all.  A tile takes a warp 2800 clocks (eight query
 // rows, twelve warps: 5.2 TB/s while they run); in front of the first one lie 12 K clocks, six dependent loads and much code that runs
 // once, and behind the last one 10 K: the item's sums 3 K, from there to the first piece 3 K, the join across blocks 3 K.
-// So long GQA (five tiles per warp) takes 28.6 us where its bytes take 7.
+// So long GQA (five tiles per warp) takes 27 us where its bytes take 7.
 // A third tile in flight or eleven warps do not help; sixteen warps leave too few registers.
 #include <cuda_fp16.h>
 #include <limits.h>
@@ -194,7 +195,6 @@ chunk_q4_few_kernel(const ChunkArgs a, const ChunkPlan pl, const FewQuery qy, co
     using Shape = Q4Shape<NH, RH>;
     constexpr int D = Shape::D, NW = Shape::kWarps, NST = Shape::kSlots;
     constexpr int KW = D / 32;                           // words of a key that a lane has in the first product
-    constexpr int VW = D / 64;                           // and in the second one
     constexpr int MT = D / 16;                           // 16-dimension tiles of the output
 
     extern __shared__ uint8_t smem_raw[];

@@ -243,7 +243,6 @@ struct AppendArgs {
     const int32_t* page_table; int32_t max_pages, page_rows, n_pages;
     int32_t* status;
 };
-// a tensor of rows as the append kernels take it: strides in bytes
 // Division of whole numbers from 0 to 2^31 - 1 by n >= 1: with 2^(l-1) < n <= 2^l and m = 2^(31+l) / n rounded up (which fits 32
 // bits), t m / 2^(31+l) is more than t / n by less than 1 / n.  (A division by a variable is some thirty instructions.)
 struct Divider {
@@ -259,6 +258,7 @@ inline Divider divider(int n) {
     return Divider{uint32_t(((uint64_t(1) << (31 + l)) + uint64_t(n) - 1) / uint64_t(n)), 31 + l};
 }
 
+// a tensor of rows as the append kernels take it: strides in bytes
 struct RowTensor { void* ptr; int64_t sb, sh, st; };
 struct RopeArgs {
     const float* cos_sin; int64_t row_stride;        // cosines of dim / 2 angles, then their sines, per row
